@@ -501,6 +501,158 @@ nvfp4_status nvfp4_qfit_calibrate(const void* q_pre_bf16, const void* k_pre_bf16
                                   double eps, int32_t kv_format, float* s_q, float* s_k, float* m,
                                   double* errors_host, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Paged cache.  An nvfp4_kv_cache whose `batch` is the number of pages of a
+ * pool and whose `capacity` is the tokens of a page (any number >= 1), so its
+ * arrays are [pages, num_kv_heads, page_tokens, ...], and the sequences over it:
+ *   table    : device int32 [batch, pages_per_seq]; token t of sequence b is
+ *              row t % page_tokens of page table[b, t / page_tokens].  An entry
+ *              outside [0, pages) is an absent page (for example one that a
+ *              sliding window left behind): an append or a read there sets
+ *              CAPACITY on the device, attention takes its tokens as hidden.
+ *              Entries past a sequence's last token are not read.  Sequences
+ *              may share pages.
+ *   seq_lens : device int32 [batch], tokens per sequence, the new ones included
+ *              (attention reads it; the append and the read do not).
+ * The calls below take `pages` = NULL for a contiguous cache: its sequences are
+ * then the cache's batch, with cache->seq_lens.  Both structs are read before
+ * the call returns.
+ */
+typedef struct {
+  const int32_t* table;
+  const int32_t* seq_lens;
+  int32_t batch;
+  int32_t pages_per_seq;
+} nvfp4_kv_pages;
+
+/*
+ * A layer's step between the qkv projection and attention, with rotary
+ * positions on several axes: Q is rotated and written as bf16, K is rotated,
+ * shifted (K~ = R(K_pre) - m, Eq. 2) and quantized into the cache with V, as
+ * kv_append_rope_nvfp4 does for K and V with one axis.
+ *   q_bf16, k_bf16, v_bf16 : [n_new, heads, 128] bf16, tokens ld_q, ld_k, ld_v
+ *                elements apart (the three may be parts of one projection's
+ *                output), heads 128 apart.  q_bf16 NULL: no queries (q_out,
+ *                ld_q and num_q_heads are then ignored).
+ *   seq_idx, pos : device int32 [n_new]: the token's sequence and its place in
+ *                the sequence's cache.
+ *   rope_pos   : device int32 [n_new, n_axes], 1 <= n_axes <= 4.
+ *   axis_of_pair : HOST uint8 [64]: the axis whose position rotates the channel
+ *                pair (c, c + 64); every entry < n_axes.  Read before returning.
+ *   rope_table : fp32 [rope_positions, 64, 2] as nvfp4_rope_table writes it; a
+ *                pair takes the row of its axis' position.
+ *   k_shift    : device float [num_kv_heads, 128] or NULL.
+ *   q_out      : [n_new, num_q_heads, 128] bf16, dense.
+ * The rotation is evaluated as in kv_append_rope_nvfp4 (one rounding for each
+ * product and sum): with one axis, rope_pos = pos and a contiguous cache the
+ * codes and scales are that call's bit for bit.  A token whose cache place is
+ * outside the cache (or on an absent page) is not stored; one with a rotary
+ * position outside the table is not stored either and its q_out rows are zero;
+ * both set CAPACITY on the device.  Two tokens of one call with the same place
+ * leave either row there.
+ * Pointers and ld in 16-B steps (ALIGN; seq_idx, pos, rope_pos 4 B), ld at
+ * least heads * 128 when n_new > 1, num_q_heads >= 1, n_axes and axis_of_pair
+ * in range (SHAPE, INVALID_ARG); n_new == 0 is a no-op.
+ */
+nvfp4_status kv_append_rope_axes_nvfp4(const nvfp4_kv_cache* cache, const nvfp4_kv_pages* pages, const void* q_bf16,
+                                       int64_t ld_q, int32_t num_q_heads, const void* k_bf16, int64_t ld_k,
+                                       const void* v_bf16, int64_t ld_v, const int32_t* seq_idx, const int32_t* pos,
+                                       const int32_t* rope_pos, int32_t n_axes, const uint8_t* axis_of_pair,
+                                       int64_t n_new, const float* rope_table, int64_t rope_positions,
+                                       const float* k_shift, void* q_out, void* stream);
+
+/*
+ * Cached rows back as bf16: k_out[i, h] = bf16_rne(e2m1 * e4m3 * g_K) (E1M2 by
+ * kv_format) of token pos[i] of sequence seq_idx[i], and v_out likewise; the
+ * product is formed in fp32, where e2m1 * e4m3 is exact.
+ *   seq_idx, pos : device int32 [n].
+ *   k_out, v_out : [n, num_kv_heads, 128] bf16, dense; one of them may be NULL.
+ * A row outside the cache or on an absent page reads as zeros and sets CAPACITY
+ * on the device.  n == 0 is a no-op.
+ */
+nvfp4_status kv_read_nvfp4(const nvfp4_kv_cache* cache, const nvfp4_kv_pages* pages, const int32_t* seq_idx,
+                           const int32_t* pos, int64_t n, void* k_out, void* v_out, void* stream);
+
+/* What a score is made of, and which keys a query sees (extend_attention_nvfp4). */
+typedef struct {
+  float softmax_scale;        /* > 0                                          */
+  float logit_cap;            /* c > 0: s <- c tanh(s / c); 0: no cap         */
+  const float* slopes;        /* device float [num_q_heads], or NULL: s <- s -
+                                 slopes[h] * |p - t|, after the cap           */
+  int32_t window;             /* w > 0: keys t > p - w only; 0: no window     */
+  const int32_t* prefix_lens; /* device int32 [batch] or NULL: keys below it
+                                 are visible to earlier queries too           */
+  const int32_t* doc_start;   /* device int32 [n_tokens] or NULL: the query
+                                 sees no key before it                        */
+} nvfp4_attention_options;
+
+/*
+ * Attention of new tokens over the 4-bit cache that already holds them: one
+ * token per sequence (decode), a few (drafted tokens), a chunk of a prompt or a
+ * whole one; sequences may bring different numbers.
+ *   q_bf16   : [n_tokens, num_q_heads, 128] bf16, tokens ld_q elements apart.
+ *   q_start  : device int32 [batch + 1]: sequence b's queries are tokens
+ *              q_start[b] .. q_start[b+1]-1 (ascending, from 0 to n_tokens), or
+ *              NULL: n_tokens / batch for each sequence.
+ *   out_bf16 : [n_tokens, num_q_heads, 128] bf16, dense.
+ * Query j of sequence b, which brings n_b tokens and has len_b cached ones,
+ * is at p = len_b - n_b + j and sees the keys t < len_b with
+ *   t >= doc_start, t > p - window, and t <= p or t < prefix_lens[b];
+ *   s_t = softmax_scale q . K_hat[t], capped, then biased; out = softmax(s) V_hat,
+ * kv head = h / (num_q_heads / num_kv_heads).  A query that sees nothing (n_b >
+ * len_b, a document that starts after it, absent pages) gets zeros.  Cached
+ * rows past len_b are never used, whatever their bytes.
+ * Softmax, sums and products are accumulated in fp32; Q enters the tensor core
+ * as f16 after an exact power-of-two scaling of each row, K and V as exact f16,
+ * softmax weights rounded to f16.
+ * Where the queries are too few to occupy the GPU, the keys of a group of rows
+ * are split and the parts are joined in a fixed order: the result is the same
+ * bits in every run for the same arguments, lengths and buffer sizes.
+ *   workspace : extend_attention_nvfp4_workspace_size(...) bytes, 16-B aligned
+ *              (NULL if that is 0); `context` is the cache's capacity, or
+ *              pages_per_seq * page tokens.  Contents on entry are ignored.
+ * num_q_heads % num_kv_heads == 0, a group of at most 16, n_tokens % batch == 0
+ * where q_start is NULL (SHAPE); softmax_scale > 0, cap and window >= 0, all
+ * finite (INVALID_ARG); q, out and cache arrays 16-B aligned, ld_q % 8 == 0
+ * (ALIGN).  A length above the capacity is clamped to it, and a length or a
+ * q_start out of range is taken as the nearest valid one; both set CAPACITY on
+ * the device.  n_tokens == 0 is a no-op.
+ */
+size_t extend_attention_nvfp4_workspace_size(int32_t batch, int64_t n_tokens, int32_t num_q_heads,
+                                             int32_t num_kv_heads, int64_t context);
+nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const nvfp4_kv_pages* pages, const void* q_bf16,
+                                    int64_t ld_q, int64_t n_tokens, int32_t num_q_heads, const int32_t* q_start,
+                                    const nvfp4_attention_options* options, void* out_bf16, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
+/*
+ * Between two blocks of the layer: the norm of a block's output, its gate, the
+ * residual sum, and the norm that the next block's linear reads, in one pass:
+ *   z = y;  z <- rms(z) * w_post (w_post given);  z <- z * gate (gate given)
+ *   r = x + alpha * z;  h = rms(r) * w_norm;  rms(a) = a / sqrt(mean(a^2) + eps)
+ * all in fp32 (h is made from the unrounded r), each output rounded once.
+ *   x_bf16, y_bf16 : [rows, cols] bf16, leading dimensions ld_x, ld_y.  y_bf16
+ *                NULL: r = x (r_out, w_post, gate and alpha are then unused).
+ *   w_norm, w_post : bf16 [cols]; w_norm NULL: no second norm (r alone).
+ *   gate       : bf16 [ceil(rows / rows_per_gate), cols], row i uses gate row
+ *                i / rows_per_gate: a gate per token, per sequence or for all.
+ *   r_out      : bf16 [rows, cols] dense, or NULL; may be x_bf16 where ld_x == cols.
+ *   h_out      : bf16 [rows, cols] dense, or NULL.
+ *   codes, scales, g_out : h as the next linear's NVFP4 A operand: h is rounded
+ *                to bf16 and quantized with the static device scale g_out by
+ *                the recipe of nvfp4_quantize (MMA layout, padding rows zero);
+ *                bit-identical to nvfp4_quantize(h_out).  All three or none.
+ *                g_out <= 0 or non-finite: zeros, INVALID_ARG on the device.
+ * cols % 8 == 0 (% 64 with codes), 8 <= cols <= 32768, ld >= cols, rows_per_gate
+ * >= 1 where gate is given (SHAPE); something to write, alpha and eps finite,
+ * eps > 0 (INVALID_ARG); 16-B aligned pointers, ld % 8 == 0 (ALIGN).  No output
+ * may overlap another input.  rows == 0 is a no-op.
+ */
+nvfp4_status residual_norm_nvfp4(const void* x_bf16, int64_t ld_x, const void* y_bf16, int64_t ld_y, int64_t rows,
+                                 int64_t cols, const void* w_post, const void* gate, int64_t rows_per_gate,
+                                 float alpha, const void* w_norm, float eps, void* r_out, void* h_out,
+                                 const float* g_out, uint8_t* codes, uint8_t* scales, void* stream);
+
 /* Synchronize `stream`, copy the device status word of the current device to
  * *status_host (an nvfp4_status value) and clear it. */
 nvfp4_status nvfp4_get_device_status(int32_t* status_host, void* stream);

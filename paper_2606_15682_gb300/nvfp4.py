@@ -45,6 +45,15 @@ class KVCacheStruct(ctypes.Structure):
                 ("k_gscale", _f32), ("v_gscale", _f32), ("kv_format", _i32)]
 
 
+class KVPagesStruct(ctypes.Structure):
+    _fields_ = [("table", _p), ("seq_lens", _p), ("batch", _i32), ("pages_per_seq", _i32)]
+
+
+class AttentionOptionsStruct(ctypes.Structure):
+    _fields_ = [("softmax_scale", _f32), ("logit_cap", _f32), ("slopes", _p), ("window", _i32),
+                ("prefix_lens", _p), ("doc_start", _p)]
+
+
 def _sig(name, args, res=ctypes.c_int):
     f = getattr(_lib, name)
     f.argtypes = args
@@ -72,6 +81,16 @@ _attn_static = _sig("decode_attention_nvfp4_static_scratch", [ctypes.POINTER(KVC
 _qfit_ws = _sig("nvfp4_qfit_workspace_size", [_i32, _i32, _i32, _i32, _i32, _i32], _sz)
 _qfit = _sig("nvfp4_qfit_calibrate", [_p, _p, _p, _i32, _i32, _i32, _i32, _i32, _p, _i64, _i32, _i32,
                                       ctypes.c_double, _i32, _p, _p, _p, _p, _p, _sz, _p])
+_append_axes = _sig("kv_append_rope_axes_nvfp4",
+                    [ctypes.POINTER(KVCacheStruct), _p, _p, _i64, _i32, _p, _i64, _p, _i64, _p, _p, _p, _i32,
+                     ctypes.c_char_p, _i64, _p, _i64, _p, _p, _p])
+_kv_read = _sig("kv_read_nvfp4", [ctypes.POINTER(KVCacheStruct), _p, _p, _p, _i64, _p, _p, _p])
+_extend_ws = _sig("extend_attention_nvfp4_workspace_size", [_i32, _i64, _i32, _i32, _i64], _sz)
+_extend = _sig("extend_attention_nvfp4",
+               [ctypes.POINTER(KVCacheStruct), _p, _p, _i64, _i64, _i32, _p, ctypes.POINTER(AttentionOptionsStruct), _p,
+                _p, _sz, _p])
+_residual_norm = _sig("residual_norm_nvfp4", [_p, _i64, _p, _i64, _i64, _i64, _p, _p, _i64, _f32, _p, _f32, _p, _p, _p,
+                                              _p, _p, _p])
 _get_status = _sig("nvfp4_get_device_status", [ctypes.POINTER(_i32), _p])
 _status_string = _sig("nvfp4_status_string", [ctypes.c_int], ctypes.c_char_p)
 _launch_count = _sig("nvfp4_launch_count", [], ctypes.c_uint64)
@@ -258,6 +277,111 @@ def decode_attention_nvfp4_static_scratch(cache, q, softmax_scale, out, stream=N
                                                                  _ptr(out), _stream(stream)))
 
 
+def _rows3(x, heads=None):
+    """(pointer, tokens, heads, elements between tokens) of a [tokens, heads, 128] tensor that may be a slice of a
+    wider projection output."""
+    if x.dim() != 3 or x.shape[2] != 128 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != 128):
+        raise ValueError("expected a [tokens, heads, 128] tensor with dense heads")
+    n, h = x.shape[0], x.shape[1]
+    return ctypes.c_void_p(x.data_ptr()), n, h, x.stride(0) if n > 1 else h * 128
+
+
+def _pages(pages):
+    return None if pages is None else ctypes.byref(pages.struct())
+
+
+def _typed(t, dtype, what, numel=None):
+    """Device pointer of an optional argument whose element type the call fixes."""
+    if t is None:
+        return None
+    if t.dtype != dtype or (numel is not None and t.numel() != numel):
+        raise ValueError(f"{what} must be {dtype}" + ("" if numel is None else f" with {numel} elements"))
+    return _ptr(t)
+
+
+def kv_append_rope_axes_nvfp4(cache, q, k, v, seq_idx, pos, rope_pos, axis_of_pair, rope_table, q_out, k_shift=None,
+                              pages=None, stream=None):
+    """Rotate q (-> q_out) and k by rotary positions rope_pos [n, axes] and append k and v to the (paged) cache.
+
+    q, k, v: [n, heads, 128] bf16, may be slices of one projection output; q and q_out may be None.
+    axis_of_pair: 64 integers, the axis that rotates each channel pair (c, c + 64).
+    """
+    kp, n, hk, ld_k = _rows3(k)
+    vp, nv, hv, ld_v = _rows3(v)
+    qp, nq, hq, ld_q = _rows3(q) if q is not None else (None, n, 0, 0)
+    if not (n == nv == nq == rope_pos.shape[0]) or hk != cache.num_kv_heads or hv != hk:
+        raise ValueError("q, k, v and rope_pos must have the same tokens, k and v the cache's heads")
+    if q is not None and (q_out is None or q_out.numel() != n * hq * 128):
+        raise ValueError("q_out must hold the rotated queries")
+    axes = bytes(axis_of_pair)
+    if len(axes) != 64:
+        raise ValueError("axis_of_pair must have 64 entries")
+    bf = torch.bfloat16
+    if k.dtype != bf or v.dtype != bf or (q is not None and (q.dtype != bf or q_out.dtype != bf)):
+        raise ValueError("q, k, v and q_out must be bfloat16")
+    s = cache.struct()
+    _check("kv_append_rope_axes_nvfp4",
+           _append_axes(ctypes.byref(s), _pages(pages), qp, ld_q, hq, kp, ld_k, vp, ld_v,
+                        _typed(seq_idx, torch.int32, "seq_idx", n), _typed(pos, torch.int32, "pos", n),
+                        _typed(rope_pos, torch.int32, "rope_pos"), rope_pos.shape[1], axes, n,
+                        _typed(rope_table, torch.float32, "rope_table"), rope_table.shape[0],
+                        _typed(k_shift, torch.float32, "k_shift", hk * 128),
+                        _ptr(q_out) if q is not None else None, _stream(stream)))
+
+
+def kv_read_nvfp4(cache, seq_idx, pos, k_out, v_out, pages=None, stream=None):
+    """Cached rows (seq_idx[i], pos[i]) as bf16 [n, kv heads, 128]; k_out or v_out may be None."""
+    n = seq_idx.numel()
+    size = n * cache.num_kv_heads * 128
+    s = cache.struct()
+    _check("kv_read_nvfp4",
+           _kv_read(ctypes.byref(s), _pages(pages), _typed(seq_idx, torch.int32, "seq_idx"),
+                    _typed(pos, torch.int32, "pos", n), n, _typed(k_out, torch.bfloat16, "k_out", size),
+                    _typed(v_out, torch.bfloat16, "v_out", size), _stream(stream)))
+
+
+def extend_attention_nvfp4_workspace_size(batch, n_tokens, num_q_heads, num_kv_heads, context):
+    """context: the cache's capacity, or pages_per_seq * page tokens."""
+    return int(_extend_ws(batch, n_tokens, num_q_heads, num_kv_heads, context))
+
+
+def extend_attention_nvfp4(cache, q, softmax_scale, out, workspace, q_start=None, pages=None, logit_cap=0.0, window=0,
+                           slopes=None, prefix_lens=None, doc_start=None, stream=None):
+    """Attention of the new tokens q [n_tokens, heads, 128] over the cache that holds them (see include/nvfp4.h)."""
+    qp, n, hq, ld_q = _rows3(q)
+    batch = cache.batch if pages is None else pages.batch
+    if q.dtype != torch.bfloat16:
+        raise ValueError("q must be bfloat16")
+    i32 = torch.int32
+    o = AttentionOptionsStruct(softmax_scale, logit_cap, _typed(slopes, torch.float32, "slopes", hq), window,
+                               _typed(prefix_lens, i32, "prefix_lens", batch), _typed(doc_start, i32, "doc_start", n))
+    s = cache.struct()
+    _check("extend_attention_nvfp4",
+           _extend(ctypes.byref(s), _pages(pages), qp, ld_q, n, hq, _typed(q_start, i32, "q_start", batch + 1),
+                   ctypes.byref(o), _typed(out, torch.bfloat16, "out", n * hq * 128), _ptr(workspace),
+                   0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def residual_norm_nvfp4(x, y, r_out, h_out, w_norm, eps=1e-6, w_post=None, gate=None, rows_per_gate=1, alpha=1.0,
+                        g_out=None, codes=None, scales=None, stream=None):
+    """r = x + alpha * (y, normed by w_post, gated); h = norm of r: bf16 (h_out) and / or NVFP4 (codes, scales, g_out).
+    y, r_out, h_out, w_norm may be None."""
+    xp, rows, cols, ld_x = _mat(x)
+    yp, yr, yc, ld_y = _mat(y) if y is not None else (None, rows, cols, 0)
+    bf = torch.bfloat16
+    if (yr, yc) != (rows, cols) or x.dtype != bf or (y is not None and y.dtype != bf):
+        raise ValueError("x and y must be bfloat16 of the same shape")
+    if gate is None:
+        rows_per_gate = 1
+    elif gate.shape[-1] != cols or rows_per_gate < 1 or gate.numel() != -(-rows // rows_per_gate) * cols:
+        raise ValueError("gate must be [ceil(rows / rows_per_gate), cols]")
+    n = rows * cols
+    _check("residual_norm_nvfp4",
+           _residual_norm(xp, ld_x, yp, ld_y, rows, cols, _typed(w_post, bf, "w_post", cols), _typed(gate, bf, "gate"),
+                          rows_per_gate, alpha, _typed(w_norm, bf, "w_norm", cols), eps, _typed(r_out, bf, "r_out", n),
+                          _typed(h_out, bf, "h_out", n), _ptr(g_out), _ptr(codes), _ptr(scales), _stream(stream)))
+
+
 def nvfp4_qfit_workspace_size(batch, tokens, num_q_heads, num_kv_heads, grid_s, grid_m):
     return int(_qfit_ws(batch, tokens, num_q_heads, num_kv_heads, grid_s, grid_m))
 
@@ -314,6 +438,21 @@ class KVCache:
                              self.head_dim, self.capacity, self.k_gscale, self.v_gscale, self.kv_format)
 
 
+class KVPages:
+    """Sequences over a paged cache: `table` int32 [batch, pages_per_seq] of page indexes, `seq_lens` int32 [batch].
+    The pool itself is a KVCache whose batch is the number of pages and whose capacity is the page's tokens."""
+
+    def __init__(self, table, seq_lens):
+        if table.dtype != torch.int32 or table.dim() != 2 or seq_lens.dtype != torch.int32 or \
+                seq_lens.numel() != table.shape[0]:
+            raise ValueError("table must be int32 [batch, pages_per_seq], seq_lens int32 [batch]")
+        self.table, self.seq_lens = table, seq_lens
+        self.batch, self.pages_per_seq = table.shape
+
+    def struct(self):
+        return KVPagesStruct(_ptr(self.table), _ptr(self.seq_lens), self.batch, self.pages_per_seq)
+
+
 EXPORTED = ["nvfp4_scales_bytes", "nvfp4_tensor_scale", "nvfp4_quantize", "nvfp4_quantize_dynamic", "nvfp4_scales_relayout", "nvfp4_linear",
             "nvfp4_linear_dynamic",
             "nvfp4_linear_swiglu_quantize", "nvfp4_interleave_gate_up",
@@ -321,4 +460,6 @@ EXPORTED = ["nvfp4_scales_bytes", "nvfp4_tensor_scale", "nvfp4_quantize", "nvfp4
             "kv_append_nvfp4", "kv_append_rope_nvfp4", "nvfp4_rope_table", "decode_attention_nvfp4_workspace_size", "decode_attention_nvfp4",
             "decode_attention_nvfp4_quantize",
             "decode_attention_nvfp4_static_scratch", "nvfp4_qfit_workspace_size", "nvfp4_qfit_calibrate",
+            "kv_append_rope_axes_nvfp4", "kv_read_nvfp4", "extend_attention_nvfp4_workspace_size",
+            "extend_attention_nvfp4", "residual_norm_nvfp4",
             "nvfp4_get_device_status", "nvfp4_status_string", "nvfp4_launch_count", "nvfp4_debug_inject_fault"]
