@@ -1,6 +1,8 @@
 // Attention of new tokens (one, a few, a chunk, a whole prompt) over the 4-bit
 // cache that already holds them, contiguous or paged: scores optionally capped
 // and biased by distance, keys limited by causality, window, prefix, document.
+#include <type_traits>
+
 #include "kv_pages.cuh"
 
 namespace nvfp4 {
@@ -8,6 +10,9 @@ namespace {
 
 constexpr int kD = 128;
 constexpr float kLog2e = 1.4426950408889634f;
+
+constexpr float kRescaleLog2 = 8.0f;  // the running maximum moves only when a score exceeds it by 2^8
+constexpr float kWeightLog2 = 7.0f;   // weights are kept as 2^7 w: at most 2^15 in f16, and fine steps below 1
 
 struct ExtendArgs {
   KVMap map;
@@ -25,6 +30,10 @@ struct ExtendArgs {
   float cap;
   float gv;
   int* status;
+  uint32_t tiles, tiles_per_seq;  // row tiles; of each sequence where q_start is null
+  uint32_t splits;                // parts of a tile's keys
+  float* o_ws;                    // [tile][kv head][split][row][128] and, behind them,
+  float2* ml_ws;                  // (max, sum) of each such row; unused with one split
 };
 
 // Tokens of sequence b: its first query, how many, and its cached length.
@@ -58,70 +67,697 @@ __device__ __forceinline__ int2 visible(const ExtendArgs& a, int p, int len, int
   return make_int2(lo, min(len, max(p + 1, prefix)));
 }
 
-// One CTA per (token, query head): scores of 128 keys, a thread each, then the
-// weighted sum of V, a channel per thread.
-template <bool kE1M2>
-__global__ void __launch_bounds__(kD) extend_simple_kernel(const ExtendArgs a) {
-  __shared__ float q_sh[kD], p_sh[kD], red[4];
-  __shared__ int64_t row_sh[kD];
-  griddep_wait_and_release();
-  const uint32_t tok = blockIdx.x, h = blockIdx.y, kvh = a.group.div(h);
-  uint32_t b = 0;
-  Seq s = sequence(a, 0);
-  while (tok >= s.first + s.n && b + 1 < a.map.batch) s = sequence(a, ++b);
-  const bool mine = tok >= s.first && tok < s.first + s.n;
-  const int p = s.len - static_cast<int>(s.n) + static_cast<int>(tok - s.first);
-  const int2 v = visible(a, p, s.len, a.prefix_lens ? __ldg(a.prefix_lens + b) : 0, a.doc_start ? __ldg(a.doc_start + tok) : 0);
-  const int c = threadIdx.x, lane = c & 31, warp = c >> 5;
-  q_sh[c] = __uint_as_float(static_cast<uint32_t>(a.q[tok * a.ld_q + h * kD + c]) << 16);
-  const float slope = a.slopes ? __ldg(a.slopes + h) : 0.0f;
-  float m = -INFINITY, l = 0.0f, o = 0.0f;
-  const int end = mine && p >= 0 ? v.y : 0;
-  for (int t0 = v.x; t0 < end; t0 += kD) {
-    __syncthreads();
-    const int t = t0 + c;
-    float x = -INFINITY;
-    int64_t row = -1;
-    if (t < end) row = a.map.row(b, t);
-    if (row >= 0) {
-      row += static_cast<int64_t>(kvh) * a.map.size.d;
-      x = 0.0f;
-      for (int i = 0; i < 16; ++i) {
-        uint32_t e[4];
-        elements8<kE1M2>(__ldg(reinterpret_cast<const uint32_t*>(a.map.k_codes + row * 64) + i), e);
-        const float sc = e4m3_value(__ldg(a.map.k_scales + row * 8 + (i >> 1))) * (kE1M2 ? 0.5f : 1.0f);
-        float part = 0.0f;
-        for (int k = 0; k < 4; ++k) part += f16_lo(e[k]) * q_sh[8 * i + 2 * k] + f16_hi(e[k]) * q_sh[8 * i + 2 * k + 1];
-        x += part * sc;
-      }
-      x *= a.scale;
-      if (a.cap > 0.0f) x = a.cap * tanhf(x / a.cap);
-      x -= slope * static_cast<float>(abs(p - t));
+
+// ---- row tiles -----------------------------------------------------------
+// The rows of a (sequence, KV head) are its (token, head of the group) pairs,
+// token-major: row r is token r / group, head r % group.  A tile is kRows of them.
+
+struct Tile {
+  uint32_t b, row0;  // sequence, first row
+};
+// Tile number `tile` of all sequences' tiles, the last tile of a sequence first
+// (causal: it has the most keys).  By a converged warp; b = batch: none.
+template <int kRows>
+__device__ __forceinline__ Tile find_tile(const ExtendArgs& a, uint32_t tile) {
+  const uint32_t lane = threadIdx.x & 31;
+  if (!a.q_start) {
+    const uint32_t b = tile / a.tiles_per_seq;
+    return {b, (a.tiles_per_seq - 1 - (tile - b * a.tiles_per_seq)) * kRows};
+  }
+  uint32_t before = 0;
+  for (uint32_t base = 0; base < a.map.batch; base += 32) {
+    const uint32_t b = base + lane;
+    const uint32_t mine = b < a.map.batch ? (sequence(a, b).n * a.group.d + kRows - 1) / kRows : 0;
+    uint32_t incl = mine;
+#pragma unroll
+    for (int sh = 1; sh < 32; sh <<= 1) {
+      const uint32_t v = __shfl_up_sync(0xffffffffu, incl, sh);
+      if (lane >= static_cast<uint32_t>(sh)) incl += v;
     }
-    float mx = x;
-    for (int sh = 16; sh; sh >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, sh));
-    if (lane == 0) red[warp] = mx;
-    row_sh[c] = row;
-    __syncthreads();
-    const float m_new = fmaxf(m, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-    p_sh[c] = row >= 0 ? exp2f((x - m_new) * kLog2e) : 0.0f;
-    __syncthreads();
-    const float shrink = m_new == -INFINITY ? 1.0f : exp2f((m - m_new) * kLog2e);
-    m = m_new;
-    o *= shrink;
-    l *= shrink;
-    for (int k = 0; k < min(kD, end - t0); ++k) {
-      const int64_t r = row_sh[k];
-      if (r < 0) continue;
-      uint32_t e[4];
-      elements8<kE1M2>(__ldg(a.map.v_codes + r * 64 + (c >> 1)), e);
-      const float sc = e4m3_value(__ldg(a.map.v_scales + r * 8 + (c >> 4))) * (kE1M2 ? 0.5f : 1.0f);
-      o += p_sh[k] * ((c & 1) ? f16_hi(e[0]) : f16_lo(e[0])) * sc;
-      l += p_sh[k];
+    const uint32_t hit = __ballot_sync(0xffffffffu, tile < before + incl);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      const uint32_t end = before + __shfl_sync(0xffffffffu, incl, l);
+      return {base + l, (end - 1 - tile) * kRows};
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return {a.map.batch, 0};
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t f16x2_rn(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
+// What a row's scores are made of: x = s * mult in the log2 domain; capped,
+// x = c log2(e) tanh(s * in), tanh(y) = 1 - 2 / (1 + 2^(2 log2(e) y)) (absolute
+// error some 2^-22, which `cap` scales; the hardware tanh's 2^-11 would show).
+struct RowScore {
+  float mult;   // softmax_scale * g_K * log2(e) / the query's scale
+  float slope;  // slopes[h] * log2(e)
+};
+
+// ---- many rows: tensor cores of the fifth generation ----------------------
+// A CTA holds 256 rows as two 128-row tiles (thread = row), streams blocks of
+// 128 keys, and computes S = Q K^T and O += P V with tcgen05.mma kind::f16.
+//   warps 0-3, 4-7  softmax of tile 0 and 1: read S from TMEM, write P (f16)
+//                   over it, rescale O where a maximum moved by more than 2^8
+//   warps 8-11      dequantize the block's K and V into shared memory (f16,
+//                   exact: an E2M1 x E4M3 product has at most 6 significant bits)
+//   warp 12         issues the MMAs: PV of tile t, then its next QK^T, so that
+//                   one tile's softmax runs beside the other's MMAs
+// With at most 128 rows the second tile takes the same rows with every second
+// block, and the two are joined at the end.
+constexpr int kTileRows = 256;
+constexpr int kBlock = 128;  // keys per block
+constexpr int kTileThreads = 13 * 32;
+constexpr uint32_t kOperand = 32768;  // bytes of a 128 x 128 f16 operand
+constexpr uint32_t kOffK = 2 * kOperand, kOffV = 4 * kOperand;
+constexpr uint32_t kTileSmem = 6 * kOperand + 1024;  // and alignment
+
+// f16 operands, fp32 accumulator, 128 x 128; bit 16: B is stored with N contiguous.
+constexpr uint32_t kIdescQK = (1u << 4) | (16u << 17) | (8u << 24);
+constexpr uint32_t kIdescPV = kIdescQK | (1u << 16);
+constexpr uint32_t kIdescPVFull = kIdescPV | (1u << 7) | (1u << 10);  // bf16 operands
+// 128-byte-swizzled operand: rows of 128 bytes, 8-row groups 1024 bytes apart
+// (sbo), the second 64 columns kOperand / 2 further (lbo, used with N contiguous).
+__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(kOperand / 2 >> 4) << 16) |
+         (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// Byte of 16-byte chunk c (of 16) of row r in such an operand.
+__device__ __forceinline__ uint32_t operand_chunk(uint32_t r, uint32_t c) {
+  return (c >> 3) * (kOperand / 2) + r * 128 + (((c ^ r) & 7) << 4);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+               " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
+               : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+               " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* r) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+      "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
+        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]),
+        "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]),
+        "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* u) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+      "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
+      "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]),
+      "r"(u[19]), "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]),
+      "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+struct TileShared {
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_done[2], drain;
+  uint32_t tmem;
+  Tile tile;
+  Seq seq;
+  int lo, hi;       // keys that some row of the tile sees
+  float mult[kTileRows];
+  float2 ml[kBlock];             // tile 1's (max, sum), for the join
+  alignas(16) uint32_t present[4][4];  // bit per key of a block: loaded, in the last four blocks' slots
+  volatile int abort;
+};
+
+// 32 scores of a row in place -> log2 domain, keys outside `mask` hidden.
+template <bool kMods>
+__device__ __forceinline__ void score32(float* s, const RowScore& rs, const ExtendArgs& a, int p_minus_t0, uint32_t mask) {
+  if (kMods) {
+    const float in = rs.mult * (a.cap > 0.0f ? 2.0f / a.cap : 1.0f);  // cap: 2 log2(e) s / c
+    const float out = a.cap * kLog2e;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      float x = s[i] * in;
+      if (a.cap > 0.0f) x = out - 2.0f * out * rcp(1.0f + ex2(x));
+      s[i] = fmaf(-rs.slope, fabsf(static_cast<float>(p_minus_t0 - i)), x);
     }
   }
-  const uint32_t bits = bf16x2_rn(l > 0.0f ? o / l * a.gv : 0.0f, 0.0f);
-  a.out[(static_cast<uint64_t>(tok) * a.hq + h) * kD + c] = static_cast<uint16_t>(bits);
+  if (mask != 0xffffffffu) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (!((mask >> i) & 1u)) s[i] = -INFINITY;
+  }
+}
+
+// Two f16 values of at most 7 significant bits, at least 2^-14 or zero -> bf16,
+// exact: the 5-bit exponent moves into the 8-bit field, 2^112 makes up for the bias.
+__device__ __forceinline__ uint32_t bf16x2_of_f16x2(uint32_t h) {
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(((h >> 3) & 0x0FFF0FFFu) | (h & 0x80008000u)), "r"(0x77807780u));
+  return d;
+}
+
+// kFull: weights as two bf16 terms (16 significant bits at fp32's range) and V in
+// bf16, a second PV product per block.  In f16 a weight below 2^-31 of the row's
+// largest is lost, which shows only where all heavier keys hold a zero in a
+// channel: among few keys.
+template <bool kE1M2, bool kMods, bool kFull>
+__global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const ExtendArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ TileShared sh;
+  const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.k_full[i], 4);
+      mbar_init(&sh.k_empty[i], 1);
+      mbar_init(&sh.v_full[i], 4);
+      mbar_init(&sh.v_empty[i], 1);
+      mbar_init(&sh.s_full[i], 1);
+      mbar_init(&sh.p_full[i], 4);
+      mbar_init(&sh.o_done[i], 1);
+    }
+    mbar_init(&sh.drain, 1);
+    sh.abort = 0;
+    sh.lo = 0x7fffffff;
+    sh.hi = 0;
+    fence_mbar_init();
+  }
+  if (warp == 12) tmem_alloc(&sh.tmem, 512);
+  griddep_wait_and_release();
+  // Item: split fastest, then KV head, then tile.
+  const uint32_t split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
+  const uint32_t tile_id = rest / a.map.hkv, kvh = rest - tile_id * a.map.hkv;
+  if (warp == 0) {
+    const Tile t = find_tile<kTileRows>(a, tile_id);
+    if (lane == 0) {
+      sh.tile = t;
+      if (t.b < a.map.batch) sh.seq = sequence(a, t.b);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem;
+  const bool none = sh.tile.b >= a.map.batch;  // more CTAs than tiles
+  const Seq seq = sh.seq;
+  const uint32_t group = a.group.d;
+  const uint32_t rows = none ? 0 : min(seq.n * group - sh.tile.row0, static_cast<uint32_t>(kTileRows));
+  const bool two = rows > 128;
+
+  // Row of a softmax thread: tile 1 has rows 128.. of a large tile, or rows 0.. again.
+  const uint32_t local = threadIdx.x < 256 ? (two ? threadIdx.x : threadIdx.x & 127) : 0;
+  const bool live = threadIdx.x < 256 && local < rows;
+  const uint32_t r = sh.tile.row0 + (live ? local : 0), tok = a.group.div(r), head = kvh * group + (r - tok * group);
+  int2 vis = make_int2(0, 0);
+  const int p = seq.len - static_cast<int>(seq.n) + static_cast<int>(tok);
+  RowScore rs = {0.0f, 0.0f};
+  if (live && !none && p >= 0)
+    vis = visible(a, p, seq.len, a.prefix_lens ? __ldg(a.prefix_lens + sh.tile.b) : 0,
+                  a.doc_start ? __ldg(a.doc_start + seq.first + tok) : 0);
+  if (vis.x >= vis.y) vis = make_int2(0x7fffffff, 0);
+  if (warp < 8) {
+    const int lo = __reduce_min_sync(0xffffffffu, vis.x), hi = __reduce_max_sync(0xffffffffu, vis.y);
+    if (lane == 0) {
+      atomicMin(&sh.lo, lo);
+      atomicMax(&sh.hi, hi);
+    }
+    // Q rows as f16: 16 lanes a row, two rows a turn, 32 rows a warp.  Each row is
+    // scaled by a power of two (exact) to below 1; `mult` undoes it.
+    const int c = lane & 15;
+    if (two || warp < 4) {
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t lr = warp * 32 + 2 * i + (lane >> 4);
+        const bool here = lr < rows;
+        const uint32_t rr = sh.tile.row0 + (here ? lr : 0), t = a.group.div(rr);
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (here)
+          w = __ldg(reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(seq.first + t) * a.ld_q +
+                                                   (kvh * group + rr - t * group) * kD) + c);
+        float amax = __uint_as_float(amax_bits_bf16x8(w) << 16);
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, s));
+        // 2^-e with 2^e > amax, both within the normal fp32 range.
+        const int e = max(-125, min(static_cast<int>(__float_as_uint(amax) >> 23) - 126, 126));
+        const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+        if (c == 0) sh.mult[lr] = a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+        float x[8];
+        unpack_bf16x8(w, x);
+        sts128(smem + (lr >> 7) * kOperand + operand_chunk(lr & 127, c), f16x2_rn(x[0] * down, x[1] * down),
+               f16x2_rn(x[2] * down, x[3] * down), f16x2_rn(x[4] * down, x[5] * down), f16x2_rn(x[6] * down, x[7] * down));
+      }
+    }
+    fence_proxy_async_smem();
+  }
+  __syncthreads();
+  // The tile's blocks of keys, and this CTA's part of them.
+  const int lo = sh.lo, total = sh.hi > lo ? (sh.hi - lo + kBlock - 1) / kBlock : 0;
+  const int per = (total + static_cast<int>(a.splits) - 1) / static_cast<int>(a.splits);
+  const int j0 = min(static_cast<int>(split) * per, total), nblk = min(per, total - j0);
+  const int t_base = lo + j0 * kBlock;
+  const int n_of[2] = {two ? nblk : (nblk + 1) / 2, two ? nblk : nblk / 2};  // blocks of each softmax tile
+
+  if (warp < 8) {
+    // ------------------------------------------------------------- softmax ---
+    const int t = warp >> 2, n = n_of[t];
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_col = tmem + lanes + t * 128, o_col = tmem + lanes + 256 + t * 128;
+    rs.mult = sh.mult[live ? local : 0];
+    rs.slope = kMods && a.slopes && live ? __ldg(a.slopes + head) * kLog2e : 0.0f;
+    // Keys that every row of the warp sees need no mask.
+    const int all_lo = __reduce_max_sync(0xffffffffu, live ? vis.x : 0);
+    const int all_hi = __reduce_min_sync(0xffffffffu, live ? vis.y : 0x7fffffff);
+    const float to_log2 = kMods ? 1.0f : rs.mult;
+    float m = -INFINITY, l = 0.0f;
+    bool ok = true;
+    for (int i = 0; i < n; ++i) {
+      const int j = two ? i : 2 * i + t, t0 = t_base + j * kBlock;
+      ok = mbar_wait_bounded(&sh.s_full[t], i & 1, &sh.abort);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      tc_fence_after();
+      const uint4 pres = *reinterpret_cast<const uint4*>(sh.present[j & 3]);
+      const uint32_t pw[4] = {pres.x, pres.y, pres.z, pres.w};
+      const bool open = t0 >= all_lo && t0 + kBlock <= all_hi && (pres.x & pres.y & pres.z & pres.w) == 0xffffffffu;
+      uint32_t mask[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int a0 = max(vis.x - (t0 + 32 * c), 0), a1 = min(vis.y - (t0 + 32 * c), 32);
+        mask[c] = open ? 0xffffffffu : a1 > a0 ? pw[c] & (0xffffffffu << a0) & (0xffffffffu >> (32 - a1)) : 0u;
+      }
+      // Pass 1: the row's maximum.
+      float top = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float s[32];
+        tmem_ld32(s_col + 32 * c, s);
+        tmem_wait_ld();
+        score32<kMods>(s, rs, a, p - t0 - 32 * c, mask[c]);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) top = fmaxf(top, s[k]);
+      }
+      top *= to_log2;
+      const bool up = top > m + kRescaleLog2 || (m == -INFINITY && top > -INFINITY);
+      if (__any_sync(0xffffffffu, up)) {
+        const float shrink = up ? ex2(m - top) : 1.0f;  // 0 where there was none
+        if (up) m = top;
+        l *= shrink;
+        if (i > 0) {
+          ok = mbar_wait_bounded(&sh.o_done[t], (i - 1) & 1, &sh.abort);
+          if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            float o[32];
+            tmem_ld32(o_col + 32 * c, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] *= shrink;
+            tmem_st32(o_col + 32 * c, reinterpret_cast<uint32_t*>(o));
+          }
+        }
+      }
+      const float minus = (m == -INFINITY ? 0.0f : -m) + kWeightLog2;
+      // Pass 2: the weights, over the scores they came from.
+      uint32_t w[64], rest[kFull ? 64 : 1];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float s[32];
+        tmem_ld32(s_col + 32 * c, s);
+        tmem_wait_ld();
+        score32<kMods>(s, rs, a, p - t0 - 32 * c, mask[c]);
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) {
+          const float x = ex2(fmaf(s[k], to_log2, minus)), y = ex2(fmaf(s[k + 1], to_log2, minus));
+          l += x + y;
+          if (kFull) {
+            const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
+            w[16 * c + k / 2] = __byte_perm(xb, yb, 0x7632);
+            rest[16 * c + k / 2] = bf16x2_rn(x - __uint_as_float(xb & 0xFFFF0000u), y - __uint_as_float(yb & 0xFFFF0000u));
+          } else {
+            w[16 * c + k / 2] = f16x2_rn(x, y);
+          }
+        }
+      }
+      tmem_st32(s_col, w);
+      tmem_st32(s_col + 32, w + 32);
+      if (kFull) {
+        tmem_st32(s_col + 64, rest);
+        tmem_st32(s_col + 96, rest + 32);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.p_full[t]);
+    }
+    if (ok && n > 0) {
+      ok = mbar_wait_bounded(&sh.o_done[t], (n - 1) & 1, &sh.abort);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+    }
+    if (!ok && lane == 0 && !sh.abort) {
+      set_status(a.status, NVFP4_ERR_TIMEOUT);
+      sh.abort = 1;
+    }
+    // A tile that took the other blocks of the same rows hands over its part.
+    float m1 = -INFINITY, l1 = 0.0f;
+    float* hand = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + kOffK);  // [channel][row]
+    if (!two && t == 1) {
+      sh.ml[local] = make_float2(m, l);
+      if (ok && n > 0) {
+        for (int c = 0; c < 4; ++c) {
+          float o[32];
+          tmem_ld32(o_col + 32 * c, o);
+          tmem_wait_ld();
+#pragma unroll
+          for (int k = 0; k < 32; ++k) hand[(32 * c + k) * 128 + local] = o[k];
+        }
+      }
+    }
+    if (!two) {
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      const float2 other = sh.ml[local];
+      if (t == 0 && n_of[1] > 0) {
+        m1 = other.x;
+        l1 = other.y;
+      }
+    }
+    if (ok && !none && (two || t == 0)) {
+      const float big = fmaxf(m, m1);
+      const float w0 = m == -INFINITY ? 0.0f : ex2(m - big), w1 = m1 == -INFINITY ? 0.0f : ex2(m1 - big);
+      const float sum = w0 * l + w1 * l1;
+      const float f = a.splits > 1 ? 1.0f : sum > 0.0f ? a.gv / sum : 0.0f;
+      const uint64_t rec = ((static_cast<uint64_t>(tile_id) * a.map.hkv + kvh) * a.splits + split) * kTileRows + local;
+      if (a.splits > 1 && live) a.ml_ws[rec] = make_float2(big, sum);
+      uint4* out = reinterpret_cast<uint4*>(a.out + (static_cast<uint64_t>(seq.first + tok) * a.hq + head) * kD);
+      float4* part = reinterpret_cast<float4*>(a.o_ws + rec * kD);
+      for (int c = 0; c < 4; ++c) {
+        float o[32];
+        if (n > 0) {
+          tmem_ld32(o_col + 32 * c, o);
+          tmem_wait_ld();
+        }
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          o[k] = n > 0 && w0 != 0.0f ? o[k] * w0 : 0.0f;
+          if (w1 != 0.0f) o[k] = fmaf(hand[(32 * c + k) * 128 + local], w1, o[k]);
+          o[k] *= f;
+        }
+        if (!live) continue;
+        if (a.splits > 1) {
+          if (big == -INFINITY) continue;  // the combine does not read it
+#pragma unroll
+          for (int k = 0; k < 8; ++k) part[8 * c + k] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            out[4 * c + k] = make_uint4(bf16x2_rn(o[8 * k], o[8 * k + 1]), bf16x2_rn(o[8 * k + 2], o[8 * k + 3]),
+                                        bf16x2_rn(o[8 * k + 4], o[8 * k + 5]), bf16x2_rn(o[8 * k + 6], o[8 * k + 7]));
+        }
+      }
+    }
+    tc_fence_before();
+  } else if (warp < 12) {
+    // ---------------------------------------------------------- dequantize ---
+    // Four lanes a key: 16 bytes (32 channels) of its codes and two scale bytes
+    // each, so a warp's load covers 8 keys' rows; four turns a block.
+    const int w = warp - 8, sub = lane >> 2, qd = lane & 3;
+    const int64_t head_rows = static_cast<int64_t>(kvh) * a.map.size.d;
+    const int end = sh.hi;
+    int64_t row[4];
+    uint4 kc[4], vc[4];
+    uint32_t ks[4], vs[4];
+    uint32_t here = 0;
+    auto find = [&](int j) {
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int t = t_base + j * kBlock + it * 32 + w * 8 + sub;
+        row[it] = j < nblk && t < end ? a.map.row(sh.tile.b, t) : -1;
+      }
+    };
+    auto load = [&](const uint8_t* codes, const uint8_t* scales, uint4* c, uint32_t* s) {
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int64_t at = row[it] + head_rows;
+        c[it] = row[it] >= 0 ? __ldg(reinterpret_cast<const uint4*>(codes + at * 64) + qd) : make_uint4(0, 0, 0, 0);
+        s[it] = row[it] >= 0 ? __ldg(reinterpret_cast<const uint16_t*>(scales + at * 8) + qd) : 0u;
+      }
+    };
+    auto store = [&](uint32_t base, const uint4* c, const uint32_t* s, bool bf16) {
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const uint32_t rr = it * 32 + w * 8 + sub;
+        const uint32_t f = kv_scales16<kE1M2>(s[it]);
+        const uint32_t f0 = __byte_perm(f, f, 0x1010), f1 = __byte_perm(f, f, 0x3232);
+        // Lanes of the second 64 channels start with their other pair of words, so
+        // that eight lanes' chunks meet eight different bank groups.
+        const bool sw = qd & 2;
+        const uint32_t words[4] = {sw ? c[it].z : c[it].x, sw ? c[it].w : c[it].y, sw ? c[it].x : c[it].z,
+                                   sw ? c[it].y : c[it].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t e[4];
+          elements8<kE1M2>(words[k], e);
+          const uint32_t g = (k < 2) != sw ? f0 : f1;
+          const uint32_t chunk = 4 * qd + (sw ? k ^ 2 : k);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) e[x] = bf16 ? bf16x2_of_f16x2(mul_f16x2(e[x], g)) : mul_f16x2(e[x], g);
+          sts128(base + operand_chunk(rr, chunk), e[0], e[1], e[2], e[3]);
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+    };
+    auto bits = [&] {
+      here = 0;
+#pragma unroll
+      for (int it = 0; it < 4; ++it) here |= row[it] >= 0 ? 1u << it : 0u;
+    };
+    find(0);
+    bits();
+    load(a.map.k_codes, a.map.k_scales, kc, ks);
+    load(a.map.v_codes, a.map.v_scales, vc, vs);
+    find(1);
+    for (int j = 0; j < nblk; ++j) {
+      const int st = j & 1;
+      const uint32_t ph = ((j >> 1) & 1) ^ 1;
+      bool ok = mbar_wait_bounded(&sh.k_empty[st], ph, &sh.abort);
+      if (!__all_sync(0xffffffffu, ok)) {
+        if (lane == 0 && !sh.abort) {
+          set_status(a.status, NVFP4_ERR_TIMEOUT);
+          sh.abort = 1;
+        }
+        break;
+      }
+      // Which keys are there: byte it * 4 + w has this warp's 8 keys of turn it.
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        uint32_t v = __ballot_sync(0xffffffffu, qd == 0 && ((here >> it) & 1u));  // bits 0, 4, 8, ...
+        v = (v | v >> 3) & 0x03030303u;
+        v = (v | v >> 6) & 0x000F000Fu;
+        v = (v | v >> 12) & 0xFFu;
+        if (lane == 0) reinterpret_cast<uint8_t*>(sh.present[j & 3])[it * 4 + w] = static_cast<uint8_t>(v);
+      }
+      store(smem + kOffK + st * kOperand, kc, ks, false);
+      if (lane == 0) mbar_arrive(&sh.k_full[st]);
+      bits();
+      load(a.map.k_codes, a.map.k_scales, kc, ks);
+      ok = mbar_wait_bounded(&sh.v_empty[st], ph, &sh.abort);
+      if (!__all_sync(0xffffffffu, ok)) {
+        if (lane == 0 && !sh.abort) {
+          set_status(a.status, NVFP4_ERR_TIMEOUT);
+          sh.abort = 1;
+        }
+        break;
+      }
+      store(smem + kOffV + st * kOperand, vc, vs, kFull);
+      if (lane == 0) mbar_arrive(&sh.v_full[st]);
+      load(a.map.v_codes, a.map.v_scales, vc, vs);
+      find(j + 2);
+    }
+  } else if (lane == 0) {
+    // ----------------------------------------------------------------- MMA ---
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, int phase) {
+      ok = ok && mbar_wait_bounded(bar, phase & 1, &sh.abort);
+      tc_fence_after();
+      return ok;
+    };
+    auto qk = [&](int t, int st) {
+      const uint64_t q = operand_desc(smem + (two ? t : 0) * kOperand), k = operand_desc(smem + kOffK + st * kOperand);
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const uint64_t at = ((s >> 2) * (kOperand / 2) + (s & 3) * 32) >> 4;
+        mma_ss(tmem + t * 128, q + at, k + at, kIdescQK, s != 0);
+      }
+      tc_commit(&sh.s_full[t]);
+    };
+    auto pv = [&](int t, int st, bool first) {
+      const uint64_t v = operand_desc(smem + kOffV + st * kOperand);
+#pragma unroll
+      for (int s = 0; s < (kFull ? 16 : 8); ++s)
+        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + s * 8, v + (((s & 7) * 2048) >> 4), kFull ? kIdescPVFull : kIdescPV,
+               !(first && s == 0));
+      tc_commit(&sh.o_done[t]);
+    };
+    if (two) {
+      if (nblk > 0 && wait(&sh.k_full[0], 0)) {
+        qk(0, 0);
+        qk(1, 0);
+        tc_commit(&sh.k_empty[0]);
+      }
+      for (int i = 0; i < nblk && ok; ++i) {
+        const int st = i & 1, nx = st ^ 1;
+        const bool more = i + 1 < nblk;
+        if (!wait(&sh.p_full[0], i) || !wait(&sh.v_full[st], i >> 1)) break;
+        pv(0, st, i == 0);
+        if (more) {
+          if (!wait(&sh.k_full[nx], (i + 1) >> 1)) break;
+          qk(0, nx);
+        }
+        if (!wait(&sh.p_full[1], i)) break;
+        pv(1, st, i == 0);
+        tc_commit(&sh.v_empty[st]);
+        if (more) {
+          qk(1, nx);
+          tc_commit(&sh.k_empty[nx]);
+        }
+      }
+    } else {
+      for (int t = 0; t < 2; ++t)
+        if (n_of[t] > 0 && wait(&sh.k_full[t], 0)) {
+          qk(t, t);
+          tc_commit(&sh.k_empty[t]);
+        }
+      for (int i = 0; i < n_of[0] && ok; ++i)
+        for (int t = 0; t < 2 && ok; ++t) {
+          if (i >= n_of[t]) continue;
+          if (!wait(&sh.p_full[t], i) || !wait(&sh.v_full[t], i)) break;
+          pv(t, t, i == 0);
+          tc_commit(&sh.v_empty[t]);
+          if (i + 1 < n_of[t] && wait(&sh.k_full[t], i + 1)) {
+            qk(t, t);
+            tc_commit(&sh.k_empty[t]);
+          }
+        }
+    }
+    if (!ok) {
+      if (!sh.abort) {
+        set_status(a.status, NVFP4_ERR_TIMEOUT);
+        sh.abort = 1;
+      }
+      tc_commit(&sh.drain);  // the MMAs issued so far end before TMEM is freed
+      mbar_wait_bounded(&sh.drain, 0, nullptr, kDrainLimitNs);
+    }
+  }
+  __syncwarp();
+  __syncthreads();
+  if (warp == 12) {
+    tc_fence_after();
+    tmem_relinquish();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// Joins the parts of a tile's rows in split order: one warp a row, four channels
+// a lane.  Rows of a tile are shared out over gridDim.z CTAs.
+template <int kRows>
+__global__ void __launch_bounds__(256) extend_combine_kernel(const ExtendArgs a) {
+  griddep_wait_and_release();
+  const int lane = threadIdx.x & 31;
+  const Tile t = find_tile<kRows>(a, blockIdx.x);
+  if (t.b >= a.map.batch) return;
+  const Seq seq = sequence(a, t.b);
+  const uint32_t rows = min(seq.n * a.group.d - t.row0, static_cast<uint32_t>(kRows)), kvh = blockIdx.y;
+  for (uint32_t local = blockIdx.z * 8 + (threadIdx.x >> 5); local < rows; local += gridDim.z * 8) {
+    const uint64_t rec = (static_cast<uint64_t>(blockIdx.x) * a.map.hkv + kvh) * a.splits * kRows + local;
+    float big = -INFINITY;
+    for (uint32_t s = lane; s < a.splits; s += 32) big = fmaxf(big, a.ml_ws[rec + static_cast<uint64_t>(s) * kRows].x);
+#pragma unroll
+    for (int sh = 16; sh; sh >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, sh));
+    float sum = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (uint32_t s = 0; s < a.splits; ++s) {
+      const uint64_t at = rec + static_cast<uint64_t>(s) * kRows;
+      const float2 ml = a.ml_ws[at];
+      if (ml.x == -INFINITY) continue;
+      const float w = ex2(ml.x - big);
+      const float4 v = reinterpret_cast<const float4*>(a.o_ws + at * kD)[lane];
+      sum = fmaf(w, ml.y, sum);
+      o.x = fmaf(w, v.x, o.x);
+      o.y = fmaf(w, v.y, o.y);
+      o.z = fmaf(w, v.z, o.z);
+      o.w = fmaf(w, v.w, o.w);
+    }
+    const float f = sum > 0.0f ? a.gv / sum : 0.0f;
+    const uint32_t r = t.row0 + local, tok = a.group.div(r), head = kvh * a.group.d + (r - tok * a.group.d);
+    reinterpret_cast<uint2*>(a.out + (static_cast<uint64_t>(seq.first + tok) * a.hq + head) * kD)[lane] =
+        make_uint2(bf16x2_rn(o.x * f, o.y * f), bf16x2_rn(o.z * f, o.w * f));
+  }
+}
+
+// ---- host ----------------------------------------------------------------
+
+struct Plan {
+  int64_t tiles, tiles_per_seq, splits;
+};
+
+// The tiles (at most) and the parts that each tile's keys are cut into: as many
+// as make the last wave of CTAs full, against what a part costs by itself (its
+// prologue; with several, its record written and read).  Costs in blocks of
+// 128 keys.
+Plan plan_for(int64_t batch, int64_t n_tokens, int64_t group, int64_t hkv, int64_t context, bool uniform) {
+  Plan p;
+  p.tiles_per_seq = (n_tokens / batch * group + kTileRows - 1) / kTileRows;
+  const int64_t ragged = n_tokens * group / kTileRows + (batch < n_tokens ? batch : n_tokens);
+  p.tiles = uniform ? batch * p.tiles_per_seq : ragged;
+  const int64_t items = p.tiles * hkv, sms = sm_count(), blocks = (context + kBlock - 1) / kBlock;
+  p.splits = 1;
+  double best = 0.0;
+  for (int64_t s = 1; s == 1 || (s <= blocks && s <= 64 && items * s <= 4 * sms); ++s) {
+    const double cost = static_cast<double>((items * s + sms - 1) / sms) * (static_cast<double>((blocks + s - 1) / s) + (s > 1 ? 6.0 : 2.0));
+    if (s == 1 || cost < best) {
+      best = cost;
+      p.splits = s;
+    }
+  }
+  return p;
+}
+
+size_t workspace_for(const Plan& p, int64_t hkv) {
+  return p.splits > 1 ? static_cast<size_t>(p.tiles) * hkv * p.splits * kTileRows * (kD + 2) * sizeof(float) : 0;
+}
+
+// Contexts of up to this many keys take kFull.
+constexpr uint32_t kFullContext = 512;
+
+using TileKernel = void (*)(const ExtendArgs);
+template <bool kE1M2, bool kMods, bool kFull>
+TileKernel tile_kernel() {
+  // Idempotent and cheap; a failure shows at the launch.
+  cudaFuncSetAttribute(extend_tile_kernel<kE1M2, kMods, kFull>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                       static_cast<int>(kTileSmem));
+  return extend_tile_kernel<kE1M2, kMods, kFull>;
 }
 
 }  // namespace
@@ -131,8 +767,14 @@ using namespace nvfp4;
 
 NVFP4_API size_t extend_attention_nvfp4_workspace_size(int32_t batch, int64_t n_tokens, int32_t num_q_heads,
                                                        int32_t num_kv_heads, int64_t context) {
-  (void)batch, (void)n_tokens, (void)num_q_heads, (void)num_kv_heads, (void)context;
-  return 0;
+  if (batch <= 0 || n_tokens <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads ||
+      context <= 0 || n_tokens >= (1ll << 31) || context >= (1ll << 31))
+    return 0;
+  // Both forms of q_start, so that one buffer serves either.
+  const int64_t group = num_q_heads / num_kv_heads;
+  const size_t ragged = workspace_for(plan_for(batch, n_tokens, group, num_kv_heads, context, false), num_kv_heads);
+  const size_t uniform = workspace_for(plan_for(batch, n_tokens, group, num_kv_heads, context, true), num_kv_heads);
+  return ragged > uniform ? ragged : uniform;
 }
 
 NVFP4_API nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const nvfp4_kv_pages* pages,
@@ -147,7 +789,7 @@ NVFP4_API nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const
   if (!(options->softmax_scale > 0.0f && options->softmax_scale <= FLT_MAX) ||
       !(options->logit_cap >= 0.0f && options->logit_cap <= FLT_MAX) || options->window < 0)
     return NVFP4_ERR_INVALID_ARG;
-  if (n_tokens < 0 || n_tokens >= (1ll << 31) || num_q_heads <= 0 || num_q_heads > 65535 ||
+  if (n_tokens < 0 || num_q_heads <= 0 || num_q_heads > 65535 || n_tokens >= (1ll << 31) / num_q_heads ||
       num_q_heads % cache->num_kv_heads || (!q_start && n_tokens % a.map.batch))
     return NVFP4_ERR_SHAPE;
   if (n_tokens == 0) return NVFP4_OK;
@@ -177,9 +819,30 @@ NVFP4_API nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const
   a.cap = options->logit_cap;
   a.gv = cache->v_gscale;
   a.status = status_word_dev();
-  const auto kernel = cache->kv_format == NVFP4_KV_E1M2 ? extend_simple_kernel<true> : extend_simple_kernel<false>;
-  if (launch_pdl(kernel, dim3(a.n_tokens, a.hq), dim3(kD), 0, static_cast<cudaStream_t>(stream), a) != cudaSuccess)
+  const Plan p = plan_for(a.map.batch, n_tokens, a.group.d, a.map.hkv, a.map.context, !q_start);
+  const int64_t grid = p.tiles * a.map.hkv * p.splits;
+  if (grid >= (1ll << 31)) return NVFP4_ERR_SHAPE;
+  a.tiles = static_cast<uint32_t>(p.tiles);
+  a.tiles_per_seq = static_cast<uint32_t>(p.tiles_per_seq);
+  a.splits = static_cast<uint32_t>(p.splits);
+  a.o_ws = static_cast<float*>(workspace);
+  a.ml_ws = reinterpret_cast<float2*>(a.o_ws + static_cast<size_t>(grid) * kTileRows * kD);
+  const bool mods = options->logit_cap > 0.0f || options->slopes, e1m2 = cache->kv_format == NVFP4_KV_E1M2;
+  const bool full = a.map.context <= kFullContext;
+  const auto of = [&](auto e, auto m) {
+    return full ? tile_kernel<decltype(e)::value, decltype(m)::value, true>()
+                : tile_kernel<decltype(e)::value, decltype(m)::value, false>();
+  };
+  const TileKernel kernel = e1m2 ? (mods ? of(std::true_type(), std::true_type()) : of(std::true_type(), std::false_type()))
+                                 : (mods ? of(std::false_type(), std::true_type()) : of(std::false_type(), std::false_type()));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (launch_pdl(kernel, dim3(static_cast<uint32_t>(grid)), dim3(kTileThreads), kTileSmem, s, a) != cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
+  if (p.splits > 1) {
+    if (launch_pdl(extend_combine_kernel<kTileRows>, dim3(a.tiles, a.map.hkv, 4), dim3(256), 0, s, a) != cudaSuccess)
+      return NVFP4_ERR_CUDA;
+    count_launches(1);
+  }
   return launch_status();
 }

@@ -46,7 +46,7 @@ inline nvfp4_status kv_map(const nvfp4_kv_cache* cache, const nvfp4_kv_pages* pa
       (pages && (pages->batch <= 0 || pages->pages_per_seq <= 0)))
     return NVFP4_ERR_SHAPE;
   const int64_t context = static_cast<int64_t>(cache->capacity) * (pages ? pages->pages_per_seq : 1);
-  if (context >= (1ll << 31)) return NVFP4_ERR_SHAPE;
+  if (context >= (1ll << 31) - 512) return NVFP4_ERR_SHAPE;  // block ends stay within 32 bits
   if (!aligned(cache->k_codes, 16) || !aligned(cache->v_codes, 16) || !aligned(cache->k_scales, 8) ||
       !aligned(cache->v_scales, 8) || (pages && !aligned(pages->table, 4)))
     return NVFP4_ERR_ALIGN;
