@@ -137,12 +137,15 @@ struct RowScore {
 //   warps 8-11      dequantize the block's K and V into shared memory (f16,
 //                   exact: an E2M1 x E4M3 product has at most 6 significant bits)
 //   warp 12         issues the MMAs: PV of tile t, then its next QK^T, so that
-//                   one tile's softmax runs beside the other's MMAs
+//                   one tile's softmax runs beside the other's MMAs; warps 13-15
+//                   complete its warpgroup and idle
+// A row's 128 scores stay in registers, so the softmax warps take 184 registers a
+// thread, dequantizers 104, the rest 40: the 512 x 128 that the CTA starts with.
 // With at most 128 rows the second tile takes the same rows with every second
 // block, and the two are joined at the end.
 constexpr int kTileRows = 256;
 constexpr int kBlock = 128;  // keys per block
-constexpr int kTileThreads = 13 * 32;
+constexpr int kTileThreads = 16 * 32;
 constexpr uint32_t kOperand = 32768;  // bytes of a 128 x 128 f16 operand
 constexpr uint32_t kOffK = 2 * kOperand, kOffV = 4 * kOperand;
 constexpr uint32_t kTileSmem = 6 * kOperand + 1024;  // and alignment
@@ -153,22 +156,25 @@ constexpr uint32_t kIdescPV = kIdescQK | (1u << 16);
 constexpr uint32_t kIdescPVFull = kIdescPV | (1u << 7) | (1u << 10);  // bf16 operands
 // 128-byte-swizzled operand: rows of 128 bytes, 8-row groups 1024 bytes apart
 // (sbo), the second 64 columns kOperand / 2 further (lbo, used with N contiguous).
-__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr) {
-  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(kOperand / 2 >> 4) << 16) |
-         (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+// The low word; the high word is the same for all of them.
+__device__ __forceinline__ uint32_t operand_desc(uint32_t saddr) {
+  return ((saddr & 0x3FFFFu) >> 4) | ((kOperand / 2 >> 4) << 16);
 }
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
 // Byte of 16-byte chunk c (of 16) of row r in such an operand.
 __device__ __forceinline__ uint32_t operand_chunk(uint32_t r, uint32_t c) {
   return (c >> 3) * (kOperand / 2) + r * 128 + (((c ^ r) & 7) << 4);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-               " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n .reg .b64 da, db;\n setp.ne.b32 p, %4, 0;\n mov.b64 da, {%1, %5};\n"
+               " mov.b64 db, {%2, %5};\n tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n}" ::"r"(d),
+               "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"(kDescHigh)
                : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-               " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n .reg .b64 db;\n setp.ne.b32 p, %4, 0;\n mov.b64 db, {%2, %5};\n"
+               " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n}" ::"r"(d),
+               "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"(kDescHigh)
                : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* r) {
@@ -191,6 +197,25 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* u) {
       "r"(u[19]), "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]),
       "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31])
       : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* u) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
+      "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15])
+      : "memory");
+}
+// Two fp32 lanes at once: (x, y) = (x, y) * m + b, and (x, y) += (u, v).
+__device__ __forceinline__ void fma2(float& x, float& y, float m, float b) {
+  asm("{\n .reg .b64 v, w, z;\n mov.b64 v, {%0, %1};\n mov.b64 w, {%2, %2};\n mov.b64 z, {%3, %3};\n"
+      " fma.rn.f32x2 v, v, w, z;\n mov.b64 {%0, %1}, v;\n}"
+      : "+f"(x), "+f"(y)
+      : "f"(m), "f"(b));
+}
+__device__ __forceinline__ void add2(float& x, float& y, float u, float v) {
+  asm("{\n .reg .b64 a, b;\n mov.b64 a, {%0, %1};\n mov.b64 b, {%2, %3};\n add.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}"
+      : "+f"(x), "+f"(y)
+      : "f"(u), "f"(v));
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -340,6 +365,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
 
   if (warp < 8) {
     // ------------------------------------------------------------- softmax ---
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     const int t = warp >> 2, n = n_of[t];
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_col = tmem + lanes + t * 128, o_col = tmem + lanes + 256 + t * 128;
@@ -349,7 +375,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     const int all_lo = __reduce_max_sync(0xffffffffu, live ? vis.x : 0);
     const int all_hi = __reduce_min_sync(0xffffffffu, live ? vis.y : 0x7fffffff);
     const float to_log2 = kMods ? 1.0f : rs.mult;
-    float m = -INFINITY, l = 0.0f;
+    float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
     bool ok = true;
     for (int i = 0; i < n; ++i) {
       const int j = two ? i : 2 * i + t, t0 = t_base + j * kBlock;
@@ -365,28 +391,32 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
         const int a0 = max(vis.x - (t0 + 32 * c), 0), a1 = min(vis.y - (t0 + 32 * c), 32);
         mask[c] = open ? 0xffffffffu : a1 > a0 ? pw[c] & (0xffffffffu << a0) & (0xffffffffu >> (32 - a1)) : 0u;
       }
-      // Pass 1: the row's maximum.
-      float top = -INFINITY;
+      // The row's scores, all in registers, and their maximum.
+      float s[128];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(s_col + 32 * c, s + 32 * c);
+      tmem_wait_ld();
+#pragma unroll
+      for (int c = 0; c < 4; ++c) score32<kMods>(s + 32 * c, rs, a, p - t0 - 32 * c, mask[c]);
+      float tops[4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        float s[32];
-        tmem_ld32(s_col + 32 * c, s);
-        tmem_wait_ld();
-        score32<kMods>(s, rs, a, p - t0 - 32 * c, mask[c]);
+        tops[c] = fmaxf(s[c], s[c + 4]);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) top = fmaxf(top, s[k]);
+        for (int k = 8; k < 128; k += 8) tops[c] = fmaxf(fmaxf(s[k + c], s[k + c + 4]), tops[c]);
       }
-      top *= to_log2;
+      const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * to_log2;
       const bool up = top > m + kRescaleLog2 || (m == -INFINITY && top > -INFINITY);
       if (__any_sync(0xffffffffu, up)) {
         const float shrink = up ? ex2(m - top) : 1.0f;  // 0 where there was none
         if (up) m = top;
-        l *= shrink;
+        l0 *= shrink;
+        l1 *= shrink;
         if (i > 0) {
           ok = mbar_wait_bounded(&sh.o_done[t], (i - 1) & 1, &sh.abort);
           if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
           tc_fence_after();
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < 4; ++c) {
             float o[32];
             tmem_ld32(o_col + 32 * c, o);
@@ -398,32 +428,27 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
         }
       }
       const float minus = (m == -INFINITY ? 0.0f : -m) + kWeightLog2;
-      // Pass 2: the weights, over the scores they came from.
-      uint32_t w[64], rest[kFull ? 64 : 1];
+      // The weights, over the scores they came from.
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        float s[32];
-        tmem_ld32(s_col + 32 * c, s);
-        tmem_wait_ld();
-        score32<kMods>(s, rs, a, p - t0 - 32 * c, mask[c]);
+        uint32_t w[16], rest[kFull ? 16 : 1];
 #pragma unroll
-        for (int k = 0; k < 32; k += 2) {
-          const float x = ex2(fmaf(s[k], to_log2, minus)), y = ex2(fmaf(s[k + 1], to_log2, minus));
-          l += x + y;
+        for (int k = 0; k < 16; ++k) {
+          float x = s[32 * c + 2 * k], y = s[32 * c + 2 * k + 1];
+          fma2(x, y, to_log2, minus);
+          x = ex2(x);
+          y = ex2(y);
+          add2(l0, l1, x, y);
           if (kFull) {
             const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
-            w[16 * c + k / 2] = __byte_perm(xb, yb, 0x7632);
-            rest[16 * c + k / 2] = bf16x2_rn(x - __uint_as_float(xb & 0xFFFF0000u), y - __uint_as_float(yb & 0xFFFF0000u));
+            w[k] = __byte_perm(xb, yb, 0x7632);
+            rest[k] = bf16x2_rn(x - __uint_as_float(xb & 0xFFFF0000u), y - __uint_as_float(yb & 0xFFFF0000u));
           } else {
-            w[16 * c + k / 2] = f16x2_rn(x, y);
+            w[k] = f16x2_rn(x, y);
           }
         }
-      }
-      tmem_st32(s_col, w);
-      tmem_st32(s_col + 32, w + 32);
-      if (kFull) {
-        tmem_st32(s_col + 64, rest);
-        tmem_st32(s_col + 96, rest + 32);
+        tmem_st16(s_col + 16 * c, w);
+        if (kFull) tmem_st16(s_col + 64 + 16 * c, rest);
       }
       tmem_wait_st();
       tc_fence_before();
@@ -439,8 +464,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       set_status(a.status, NVFP4_ERR_TIMEOUT);
       sh.abort = 1;
     }
+    const float l = l0 + l1;
     // A tile that took the other blocks of the same rows hands over its part.
-    float m1 = -INFINITY, l1 = 0.0f;
+    float other_m = -INFINITY, other_l = 0.0f;
     float* hand = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + kOffK);  // [channel][row]
     if (!two && t == 1) {
       sh.ml[local] = make_float2(m, l);
@@ -458,14 +484,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       asm volatile("bar.sync 1, 256;" ::: "memory");
       const float2 other = sh.ml[local];
       if (t == 0 && n_of[1] > 0) {
-        m1 = other.x;
-        l1 = other.y;
+        other_m = other.x;
+        other_l = other.y;
       }
     }
     if (ok && !none && (two || t == 0)) {
-      const float big = fmaxf(m, m1);
-      const float w0 = m == -INFINITY ? 0.0f : ex2(m - big), w1 = m1 == -INFINITY ? 0.0f : ex2(m1 - big);
-      const float sum = w0 * l + w1 * l1;
+      const float big = fmaxf(m, other_m);
+      const float w0 = m == -INFINITY ? 0.0f : ex2(m - big), w1 = other_m == -INFINITY ? 0.0f : ex2(other_m - big);
+      const float sum = w0 * l + w1 * other_l;
       const float f = a.splits > 1 ? 1.0f : sum > 0.0f ? a.gv / sum : 0.0f;
       const uint64_t rec = ((static_cast<uint64_t>(tile_id) * a.map.hkv + kvh) * a.splits + split) * kTileRows + local;
       if (a.splits > 1 && live) a.ml_ws[rec] = make_float2(big, sum);
@@ -499,6 +525,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     tc_fence_before();
   } else if (warp < 12) {
     // ---------------------------------------------------------- dequantize ---
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     // Four lanes a key: 16 bytes (32 channels) of its codes and two scale bytes
     // each, so a warp's load covers 8 keys' rows; four turns a block.
     const int w = warp - 8, sub = lane >> 2, qd = lane & 3;
@@ -595,7 +622,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       load(a.map.v_codes, a.map.v_scales, vc, vs);
       find(j + 2);
     }
-  } else if (lane == 0) {
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == 12 && lane == 0) {
     // ----------------------------------------------------------------- MMA ---
     bool ok = true;
     auto wait = [&](uint64_t* bar, int phase) {
@@ -604,19 +633,21 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       return ok;
     };
     auto qk = [&](int t, int st) {
-      const uint64_t q = operand_desc(smem + (two ? t : 0) * kOperand), k = operand_desc(smem + kOffK + st * kOperand);
+      uint32_t q = operand_desc(smem + (two ? t : 0) * kOperand), k = operand_desc(smem + kOffK + st * kOperand);
+      asm volatile("" : "+r"(q), "+r"(k));  // the steps' descriptors are not kept in registers over the loop
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        const uint64_t at = ((s >> 2) * (kOperand / 2) + (s & 3) * 32) >> 4;
+        const uint32_t at = ((s >> 2) * (kOperand / 2) + (s & 3) * 32) >> 4;
         mma_ss(tmem + t * 128, q + at, k + at, kIdescQK, s != 0);
       }
       tc_commit(&sh.s_full[t]);
     };
     auto pv = [&](int t, int st, bool first) {
-      const uint64_t v = operand_desc(smem + kOffV + st * kOperand);
+      uint32_t v = operand_desc(smem + kOffV + st * kOperand), tm = tmem + t * 128;
+      asm volatile("" : "+r"(v), "+r"(tm));
 #pragma unroll
       for (int s = 0; s < (kFull ? 16 : 8); ++s)
-        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + s * 8, v + (((s & 7) * 2048) >> 4), kFull ? kIdescPVFull : kIdescPV,
+        mma_ts(tm + 256, tm + s * 8, v + (((s & 7) * 2048) >> 4), kFull ? kIdescPVFull : kIdescPV,
                !(first && s == 0));
       tc_commit(&sh.o_done[t]);
     };
@@ -668,6 +699,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       }
       tc_commit(&sh.drain);  // the MMAs issued so far end before TMEM is freed
       mbar_wait_bounded(&sh.drain, 0, nullptr, kDrainLimitNs);
+    }
     }
   }
   __syncwarp();
