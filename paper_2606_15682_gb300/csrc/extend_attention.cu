@@ -130,22 +130,22 @@ struct RowScore {
 };
 
 // ---- many rows: tensor cores of the fifth generation ----------------------
-// A CTA holds 256 rows as two 128-row tiles (thread = row), streams blocks of
-// 128 keys, and computes S = Q K^T and O += P V with tcgen05.mma kind::f16.
-//   warps 0-3, 4-7  softmax of tile 0 and 1: read S from TMEM, write P (f16)
-//                   over it, rescale O where a maximum moved by more than 2^8
-//   warps 8-11      dequantize the block's K and V into shared memory (f16,
-//                   exact: an E2M1 x E4M3 product has at most 6 significant bits)
-//   warp 12         issues the MMAs: PV of tile t, then its next QK^T, so that
-//                   one tile's softmax runs beside the other's MMAs; warps 13-15
-//                   complete its warpgroup and idle
-// A row's 128 scores stay in registers, so the softmax warps take 184 registers a
-// thread, dequantizers 104, the rest 40: the 512 x 128 that the CTA starts with.
+// A CTA holds 256 rows as two 128-row tiles, streams blocks of 128 keys, and
+// computes S = Q K^T and O += P V with tcgen05.mma kind::f16.
+//   warps 0-7, 8-15  softmax of tile 0 and 1, two threads a row with 64 keys (and
+//                    channels of O) each: read S from TMEM, write P over it,
+//                    rescale O where a maximum moved by more than 2^8
+//   warps 16-19      dequantize the block's K and V into shared memory (f16,
+//                    exact: an E2M1 x E4M3 product has at most 6 significant bits)
+//   warp 20          issues the MMAs: PV of tile t, then its next QK^T, so that
+//                    one tile's softmax runs beside the other's MMAs; warps 21-23
+//                    complete its warpgroup and idle
 // With at most 128 rows the second tile takes the same rows with every second
 // block, and the two are joined at the end.
 constexpr int kTileRows = 256;
 constexpr int kBlock = 128;  // keys per block
-constexpr int kTileThreads = 16 * 32;
+constexpr int kTileThreads = 24 * 32;
+constexpr int kDequantWarp = 16, kMmaWarp = 20;
 constexpr uint32_t kOperand = 32768;  // bytes of a 128 x 128 f16 operand
 constexpr uint32_t kOffK = 2 * kOperand, kOffV = 4 * kOperand;
 constexpr uint32_t kTileSmem = 6 * kOperand + 1024;  // and alignment
@@ -188,16 +188,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* r) {
         "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
       : "r"(taddr));
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* u) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
-      "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
-      "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
-      "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]),
-      "r"(u[19]), "r"(u[20]), "r"(u[21]), "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]),
-      "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31])
-      : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* u) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
@@ -217,6 +207,30 @@ __device__ __forceinline__ void add2(float& x, float& y, float u, float v) {
       : "+f"(x), "+f"(y)
       : "f"(u), "f"(v));
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* r) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
+        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// Whether any of a tile's 256 softmax threads says so; also their barrier.
+__device__ __forceinline__ bool tile_any(int barrier, bool mine) {
+  uint32_t any;
+  tc_fence_before();  // what the threads have read from TMEM is read
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, %2, 256, p;\n selp.u32 %0, 1, 0, q;\n}"
+               : "=r"(any)
+               : "r"(static_cast<uint32_t>(mine)), "r"(barrier)
+               : "memory");
+  tc_fence_after();
+  return any != 0;
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
@@ -231,6 +245,7 @@ struct TileShared {
   int lo, hi;       // keys that some row of the tile sees
   float mult[kTileRows];
   float2 ml[kBlock];             // tile 1's (max, sum), for the join
+  float half[2][2][128];         // a value of each row's two threads, by tile and half
   alignas(16) uint32_t present[4][4];  // bit per key of a block: loaded, in the last four blocks' slots
   volatile int abort;
 };
@@ -280,7 +295,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       mbar_init(&sh.v_full[i], 4);
       mbar_init(&sh.v_empty[i], 1);
       mbar_init(&sh.s_full[i], 1);
-      mbar_init(&sh.p_full[i], 4);
+      mbar_init(&sh.p_full[i], 8);
       mbar_init(&sh.o_done[i], 1);
     }
     mbar_init(&sh.drain, 1);
@@ -289,7 +304,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     sh.hi = 0;
     fence_mbar_init();
   }
-  if (warp == 12) tmem_alloc(&sh.tmem, 512);
+  if (warp == kMmaWarp) tmem_alloc(&sh.tmem, 512);
   griddep_wait_and_release();
   // Item: split fastest, then KV head, then tile.
   const uint32_t split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
@@ -312,43 +327,47 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
   const bool two = rows > 128;
 
   // Row of a softmax thread: tile 1 has rows 128.. of a large tile, or rows 0.. again.
-  const uint32_t local = threadIdx.x < 256 ? (two ? threadIdx.x : threadIdx.x & 127) : 0;
-  const bool live = threadIdx.x < 256 && local < rows;
+  const int t = warp >> 3, hf = (warp >> 2) & 1;
+  const uint32_t in_tile = threadIdx.x & 127, local = (two ? t * 128u : 0u) + in_tile;
+  const bool live = warp < kDequantWarp && local < rows;
   const uint32_t r = sh.tile.row0 + (live ? local : 0), tok = a.group.div(r), head = kvh * group + (r - tok * group);
   int2 vis = make_int2(0, 0);
   const int p = seq.len - static_cast<int>(seq.n) + static_cast<int>(tok);
-  RowScore rs = {0.0f, 0.0f};
   if (live && !none && p >= 0)
     vis = visible(a, p, seq.len, a.prefix_lens ? __ldg(a.prefix_lens + sh.tile.b) : 0,
                   a.doc_start ? __ldg(a.doc_start + seq.first + tok) : 0);
   if (vis.x >= vis.y) vis = make_int2(0x7fffffff, 0);
-  if (warp < 8) {
+  if (warp < kDequantWarp) {
     const int lo = __reduce_min_sync(0xffffffffu, vis.x), hi = __reduce_max_sync(0xffffffffu, vis.y);
     if (lane == 0) {
       atomicMin(&sh.lo, lo);
       atomicMax(&sh.hi, hi);
     }
-    // Q rows as f16: 16 lanes a row, two rows a turn, 32 rows a warp.  Each row is
+    // Q rows as f16: 16 lanes a row, two rows a turn, 16 rows a warp.  Each row is
     // scaled by a power of two (exact) to below 1; `mult` undoes it.
     const int c = lane & 15;
-    if (two || warp < 4) {
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t lr = warp * 32 + 2 * i + (lane >> 4);
-        const bool here = lr < rows;
-        const uint32_t rr = sh.tile.row0 + (here ? lr : 0), t = a.group.div(rr);
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (here)
-          w = __ldg(reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(seq.first + t) * a.ld_q +
-                                                   (kvh * group + rr - t * group) * kD) + c);
-        float amax = __uint_as_float(amax_bits_bf16x8(w) << 16);
+    if (two || warp < 8) {
+      uint4 w[8];
 #pragma unroll
-        for (int s = 1; s < 16; s <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, s));
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t lr = warp * 16 + 2 * i + (lane >> 4);
+        const uint32_t rr = sh.tile.row0 + (lr < rows ? lr : 0), tk = a.group.div(rr);
+        w[i] = lr < rows ? __ldg(reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(seq.first + tk) * a.ld_q +
+                                                                (kvh * group + rr - tk * group) * kD) + c)
+                         : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t lr = warp * 16 + 2 * i + (lane >> 4);
+        uint32_t top = amax_bits_bf16x8(w[i]);
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
         // 2^-e with 2^e > amax, both within the normal fp32 range.
-        const int e = max(-125, min(static_cast<int>(__float_as_uint(amax) >> 23) - 126, 126));
+        const int e = max(-125, min(static_cast<int>(top >> 7) - 126, 126));
         const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
         if (c == 0) sh.mult[lr] = a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
         float x[8];
-        unpack_bf16x8(w, x);
+        unpack_bf16x8(w[i], x);
         sts128(smem + (lr >> 7) * kOperand + operand_chunk(lr & 127, c), f16x2_rn(x[0] * down, x[1] * down),
                f16x2_rn(x[2] * down, x[3] * down), f16x2_rn(x[4] * down, x[5] * down), f16x2_rn(x[6] * down, x[7] * down));
       }
@@ -363,12 +382,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
   const int t_base = lo + j0 * kBlock;
   const int n_of[2] = {two ? nblk : (nblk + 1) / 2, two ? nblk : nblk / 2};  // blocks of each softmax tile
 
-  if (warp < 8) {
+  if (warp < kDequantWarp) {
     // ------------------------------------------------------------- softmax ---
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-    const int t = warp >> 2, n = n_of[t];
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+    const int n = n_of[t];
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_col = tmem + lanes + t * 128, o_col = tmem + lanes + 256 + t * 128;
+    const uint32_t s_tile = tmem + lanes + t * 128, s_col = s_tile + 64 * hf, o_col = tmem + lanes + 256 + t * 128 + 64 * hf;
+    RowScore rs;
     rs.mult = sh.mult[live ? local : 0];
     rs.slope = kMods && a.slopes && live ? __ldg(a.slopes + head) * kLog2e : 0.0f;
     // Keys that every row of the warp sees need no mask.
@@ -378,59 +398,61 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
     bool ok = true;
     for (int i = 0; i < n; ++i) {
-      const int j = two ? i : 2 * i + t, t0 = t_base + j * kBlock;
-      ok = mbar_wait_bounded(&sh.s_full[t], i & 1, &sh.abort);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      const int j = two ? i : 2 * i + t, t0 = t_base + j * kBlock + 64 * hf;
+      // A warp whose wait ran out leaves with the others of its tile, below.
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&sh.s_full[t], i & 1, &sh.abort));
       tc_fence_after();
-      const uint4 pres = *reinterpret_cast<const uint4*>(sh.present[j & 3]);
-      const uint32_t pw[4] = {pres.x, pres.y, pres.z, pres.w};
-      const bool open = t0 >= all_lo && t0 + kBlock <= all_hi && (pres.x & pres.y & pres.z & pres.w) == 0xffffffffu;
-      uint32_t mask[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int a0 = max(vis.x - (t0 + 32 * c), 0), a1 = min(vis.y - (t0 + 32 * c), 32);
-        mask[c] = open ? 0xffffffffu : a1 > a0 ? pw[c] & (0xffffffffu << a0) & (0xffffffffu >> (32 - a1)) : 0u;
-      }
-      // The row's scores, all in registers, and their maximum.
-      float s[128];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(s_col + 32 * c, s + 32 * c);
+      const uint2 pres = *reinterpret_cast<const uint2*>(&sh.present[j & 3][2 * hf]);
+      const bool open = t0 >= all_lo && t0 + 64 <= all_hi && (pres.x & pres.y) == 0xffffffffu;
+      // The thread's scores, all in registers, and their maximum.
+      float s[64];
+      tmem_ld32(s_col, s);
+      tmem_ld32(s_col + 32, s + 32);
       tmem_wait_ld();
 #pragma unroll
-      for (int c = 0; c < 4; ++c) score32<kMods>(s + 32 * c, rs, a, p - t0 - 32 * c, mask[c]);
+      for (int c = 0; c < 2; ++c) {
+        const int a0 = max(vis.x - (t0 + 32 * c), 0), a1 = min(vis.y - (t0 + 32 * c), 32);
+        const uint32_t mask = open ? 0xffffffffu
+                                   : a1 > a0 ? (c ? pres.y : pres.x) & (0xffffffffu << a0) & (0xffffffffu >> (32 - a1)) : 0u;
+        score32<kMods>(s + 32 * c, rs, a, p - t0 - 32 * c, mask);
+      }
       float tops[4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         tops[c] = fmaxf(s[c], s[c + 4]);
 #pragma unroll
-        for (int k = 8; k < 128; k += 8) tops[c] = fmaxf(fmaxf(s[k + c], s[k + c + 4]), tops[c]);
+        for (int k = 8; k < 64; k += 8) tops[c] = max3(s[k + c], s[k + c + 4], tops[c]);
       }
-      const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * to_log2;
-      const bool up = top > m + kRescaleLog2 || (m == -INFINITY && top > -INFINITY);
-      if (__any_sync(0xffffffffu, up)) {
+      float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * to_log2;
+      const auto above = [&](float x) { return x > m + kRescaleLog2 || (m == -INFINITY && x > -INFINITY); };
+      if (tile_any(1 + t, above(top) || !ok)) {
+        // Some row's maximum moves: its two threads exchange theirs.
+        sh.half[t][hf][in_tile] = top;
+        if (tile_any(1 + t, !ok)) { ok = false; break; }
+        top = fmaxf(top, sh.half[t][hf ^ 1][in_tile]);
+        const bool up = above(top);
         const float shrink = up ? ex2(m - top) : 1.0f;  // 0 where there was none
         if (up) m = top;
         l0 *= shrink;
         l1 *= shrink;
-        if (i > 0) {
-          ok = mbar_wait_bounded(&sh.o_done[t], (i - 1) & 1, &sh.abort);
-          if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        if (i > 0 && __any_sync(0xffffffffu, up)) {
+          ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.o_done[t], (i - 1) & 1, &sh.abort));
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < 4; ++c) {
-            float o[32];
-            tmem_ld32(o_col + 32 * c, o);
+            float o[16];
+            tmem_ld16(o_col + 16 * c, o);
             tmem_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] *= shrink;
-            tmem_st32(o_col + 32 * c, reinterpret_cast<uint32_t*>(o));
+            for (int k = 0; k < 16; ++k) o[k] *= shrink;
+            tmem_st16(o_col + 16 * c, reinterpret_cast<uint32_t*>(o));
           }
         }
       }
       const float minus = (m == -INFINITY ? 0.0f : -m) + kWeightLog2;
-      // The weights, over the scores they came from.
+      // The weights, over scores that both of the row's threads have read (tile_any).
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < 2; ++c) {
         uint32_t w[16], rest[kFull ? 16 : 1];
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
@@ -447,8 +469,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
             w[k] = f16x2_rn(x, y);
           }
         }
-        tmem_st16(s_col + 16 * c, w);
-        if (kFull) tmem_st16(s_col + 64 + 16 * c, rest);
+        tmem_st16(s_tile + 32 * hf + 16 * c, w);
+        if (kFull) tmem_st16(s_tile + 64 + 32 * hf + 16 * c, rest);
       }
       tmem_wait_st();
       tc_fence_before();
@@ -456,33 +478,34 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       if (lane == 0) mbar_arrive(&sh.p_full[t]);
     }
     if (ok && n > 0) {
-      ok = mbar_wait_bounded(&sh.o_done[t], (n - 1) & 1, &sh.abort);
-      ok = __all_sync(0xffffffffu, ok);
+      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.o_done[t], (n - 1) & 1, &sh.abort));
       tc_fence_after();
     }
     if (!ok && lane == 0 && !sh.abort) {
       set_status(a.status, NVFP4_ERR_TIMEOUT);
       sh.abort = 1;
     }
-    const float l = l0 + l1;
+    sh.half[t][hf][in_tile] = l0 + l1;
+    asm volatile("bar.sync 3, 512;" ::: "memory");
+    const float l = l0 + l1 + sh.half[t][hf ^ 1][in_tile];
     // A tile that took the other blocks of the same rows hands over its part.
-    float other_m = -INFINITY, other_l = 0.0f;
     float* hand = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + kOffK);  // [channel][row]
-    if (!two && t == 1) {
-      sh.ml[local] = make_float2(m, l);
-      if (ok && n > 0) {
-        for (int c = 0; c < 4; ++c) {
-          float o[32];
-          tmem_ld32(o_col + 32 * c, o);
-          tmem_wait_ld();
+    float other_m = -INFINITY, other_l = 0.0f;
+    if (!two) {
+      if (t == 1) {
+        if (hf == 0) sh.ml[in_tile] = make_float2(m, l);
+        if (ok && n > 0) {
+          for (int c = 0; c < 2; ++c) {
+            float o[32];
+            tmem_ld32(o_col + 32 * c, o);
+            tmem_wait_ld();
 #pragma unroll
-          for (int k = 0; k < 32; ++k) hand[(32 * c + k) * 128 + local] = o[k];
+            for (int k = 0; k < 32; ++k) hand[(64 * hf + 32 * c + k) * 128 + in_tile] = o[k];
+          }
         }
       }
-    }
-    if (!two) {
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      const float2 other = sh.ml[local];
+      asm volatile("bar.sync 3, 512;" ::: "memory");
+      const float2 other = sh.ml[in_tile];
       if (t == 0 && n_of[1] > 0) {
         other_m = other.x;
         other_l = other.y;
@@ -494,10 +517,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       const float sum = w0 * l + w1 * other_l;
       const float f = a.splits > 1 ? 1.0f : sum > 0.0f ? a.gv / sum : 0.0f;
       const uint64_t rec = ((static_cast<uint64_t>(tile_id) * a.map.hkv + kvh) * a.splits + split) * kTileRows + local;
-      if (a.splits > 1 && live) a.ml_ws[rec] = make_float2(big, sum);
-      uint4* out = reinterpret_cast<uint4*>(a.out + (static_cast<uint64_t>(seq.first + tok) * a.hq + head) * kD);
-      float4* part = reinterpret_cast<float4*>(a.o_ws + rec * kD);
-      for (int c = 0; c < 4; ++c) {
+      if (a.splits > 1 && live && hf == 0) a.ml_ws[rec] = make_float2(big, sum);
+      uint4* out = reinterpret_cast<uint4*>(a.out + (static_cast<uint64_t>(seq.first + tok) * a.hq + head) * kD) + 8 * hf;
+      float4* part = reinterpret_cast<float4*>(a.o_ws + rec * kD) + 16 * hf;
+      for (int c = 0; c < 2; ++c) {
         float o[32];
         if (n > 0) {
           tmem_ld32(o_col + 32 * c, o);
@@ -506,7 +529,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
           o[k] = n > 0 && w0 != 0.0f ? o[k] * w0 : 0.0f;
-          if (w1 != 0.0f) o[k] = fmaf(hand[(32 * c + k) * 128 + local], w1, o[k]);
+          if (w1 != 0.0f) o[k] = fmaf(hand[(64 * hf + 32 * c + k) * 128 + in_tile], w1, o[k]);
           o[k] *= f;
         }
         if (!live) continue;
@@ -523,12 +546,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       }
     }
     tc_fence_before();
-  } else if (warp < 12) {
+  } else if (warp < kMmaWarp) {
     // ---------------------------------------------------------- dequantize ---
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     // Four lanes a key: 16 bytes (32 channels) of its codes and two scale bytes
     // each, so a warp's load covers 8 keys' rows; four turns a block.
-    const int w = warp - 8, sub = lane >> 2, qd = lane & 3;
+    const int w = warp - kDequantWarp, sub = lane >> 2, qd = lane & 3;
     const int64_t head_rows = static_cast<int64_t>(kvh) * a.map.size.d;
     const int end = sh.hi;
     int64_t row[4];
@@ -623,88 +646,99 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       find(j + 2);
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-    if (warp == 12 && lane == 0) {
-    // ----------------------------------------------------------------- MMA ---
-    bool ok = true;
-    auto wait = [&](uint64_t* bar, int phase) {
-      ok = ok && mbar_wait_bounded(bar, phase & 1, &sh.abort);
-      tc_fence_after();
-      return ok;
-    };
-    auto qk = [&](int t, int st) {
-      uint32_t q = operand_desc(smem + (two ? t : 0) * kOperand), k = operand_desc(smem + kOffK + st * kOperand);
-      asm volatile("" : "+r"(q), "+r"(k));  // the steps' descriptors are not kept in registers over the loop
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 24;");
+    if (warp == kMmaWarp) {
+      // --------------------------------------------------------------- MMA ---
+      // The warp stays converged, so that descriptors live in uniform registers;
+      // one lane issues.
+      const bool leader = elect_one();
+      bool ok = true;
+      auto wait = [&](uint64_t* bar, int phase) {
+        ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1, &sh.abort));
+        tc_fence_after();
+        return ok;
+      };
+      auto commit = [&](uint64_t* bar) {
+        if (leader) tc_commit(bar);
+      };
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      auto qk = [&](int t, int st) {
+        const uint32_t q = operand_desc(smem + (two ? t : 0) * kOperand), k = operand_desc(smem + kOffK + st * kOperand);
+        if (leader) {
 #pragma unroll
-      for (int s = 0; s < 8; ++s) {
-        const uint32_t at = ((s >> 2) * (kOperand / 2) + (s & 3) * 32) >> 4;
-        mma_ss(tmem + t * 128, q + at, k + at, kIdescQK, s != 0);
-      }
-      tc_commit(&sh.s_full[t]);
-    };
-    auto pv = [&](int t, int st, bool first) {
-      uint32_t v = operand_desc(smem + kOffV + st * kOperand), tm = tmem + t * 128;
-      asm volatile("" : "+r"(v), "+r"(tm));
+          for (int s = 0; s < 8; ++s) {
+            const uint32_t at = ((s >> 2) * (kOperand / 2) + (s & 3) * 32) >> 4;
+            mma_ss(tm + t * 128, q + at, k + at, kIdescQK, s != 0);
+          }
+          tc_commit(&sh.s_full[t]);
+        }
+      };
+      auto pv = [&](int t, int st, bool first) {
+        const uint32_t v = operand_desc(smem + kOffV + st * kOperand);
+        if (leader) {
 #pragma unroll
-      for (int s = 0; s < (kFull ? 16 : 8); ++s)
-        mma_ts(tm + 256, tm + s * 8, v + (((s & 7) * 2048) >> 4), kFull ? kIdescPVFull : kIdescPV,
-               !(first && s == 0));
-      tc_commit(&sh.o_done[t]);
-    };
-    if (two) {
-      if (nblk > 0 && wait(&sh.k_full[0], 0)) {
-        qk(0, 0);
-        qk(1, 0);
-        tc_commit(&sh.k_empty[0]);
-      }
-      for (int i = 0; i < nblk && ok; ++i) {
-        const int st = i & 1, nx = st ^ 1;
-        const bool more = i + 1 < nblk;
-        if (!wait(&sh.p_full[0], i) || !wait(&sh.v_full[st], i >> 1)) break;
-        pv(0, st, i == 0);
-        if (more) {
-          if (!wait(&sh.k_full[nx], (i + 1) >> 1)) break;
-          qk(0, nx);
+          for (int s = 0; s < (kFull ? 16 : 8); ++s)
+            mma_ts(tm + 256 + t * 128, tm + t * 128 + s * 8, v + (((s & 7) * 2048) >> 4), kFull ? kIdescPVFull : kIdescPV,
+                   !(first && s == 0));
+          tc_commit(&sh.o_done[t]);
         }
-        if (!wait(&sh.p_full[1], i)) break;
-        pv(1, st, i == 0);
-        tc_commit(&sh.v_empty[st]);
-        if (more) {
-          qk(1, nx);
-          tc_commit(&sh.k_empty[nx]);
+      };
+      if (two) {
+        if (nblk > 0 && wait(&sh.k_full[0], 0)) {
+          qk(0, 0);
+          qk(1, 0);
+          commit(&sh.k_empty[0]);
         }
-      }
-    } else {
-      for (int t = 0; t < 2; ++t)
-        if (n_of[t] > 0 && wait(&sh.k_full[t], 0)) {
-          qk(t, t);
-          tc_commit(&sh.k_empty[t]);
-        }
-      for (int i = 0; i < n_of[0] && ok; ++i)
-        for (int t = 0; t < 2 && ok; ++t) {
-          if (i >= n_of[t]) continue;
-          if (!wait(&sh.p_full[t], i) || !wait(&sh.v_full[t], i)) break;
-          pv(t, t, i == 0);
-          tc_commit(&sh.v_empty[t]);
-          if (i + 1 < n_of[t] && wait(&sh.k_full[t], i + 1)) {
-            qk(t, t);
-            tc_commit(&sh.k_empty[t]);
+        for (int i = 0; i < nblk && ok; ++i) {
+          const int st = i & 1, nx = st ^ 1;
+          const bool more = i + 1 < nblk;
+          if (!wait(&sh.v_full[st], i >> 1) || !wait(&sh.p_full[0], i)) break;
+          pv(0, st, i == 0);
+          if (more) {
+            if (!wait(&sh.k_full[nx], (i + 1) >> 1)) break;
+            qk(0, nx);
+          }
+          if (!wait(&sh.p_full[1], i)) break;
+          pv(1, st, i == 0);
+          commit(&sh.v_empty[st]);
+          if (more) {
+            qk(1, nx);
+            commit(&sh.k_empty[nx]);
           }
         }
-    }
-    if (!ok) {
-      if (!sh.abort) {
-        set_status(a.status, NVFP4_ERR_TIMEOUT);
-        sh.abort = 1;
+      } else {
+        for (int t = 0; t < 2; ++t)
+          if (n_of[t] > 0 && wait(&sh.k_full[t], 0)) {
+            qk(t, t);
+            commit(&sh.k_empty[t]);
+          }
+        for (int i = 0; i < n_of[0] && ok; ++i)
+          for (int t = 0; t < 2 && ok; ++t) {
+            if (i >= n_of[t]) continue;
+            if (!wait(&sh.v_full[t], i) || !wait(&sh.p_full[t], i)) break;
+            pv(t, t, i == 0);
+            commit(&sh.v_empty[t]);
+            if (i + 1 < n_of[t] && wait(&sh.k_full[t], i + 1)) {
+              qk(t, t);
+              commit(&sh.k_empty[t]);
+            }
+          }
       }
-      tc_commit(&sh.drain);  // the MMAs issued so far end before TMEM is freed
-      mbar_wait_bounded(&sh.drain, 0, nullptr, kDrainLimitNs);
-    }
+      if (!ok) {
+        if (leader) {
+          if (!sh.abort) {
+            set_status(a.status, NVFP4_ERR_TIMEOUT);
+            sh.abort = 1;
+          }
+          tc_commit(&sh.drain);  // the MMAs issued so far end before TMEM is freed
+          mbar_wait_bounded(&sh.drain, 0, nullptr, kDrainLimitNs);
+        }
+        __syncwarp();
+      }
     }
   }
-  __syncwarp();
   __syncthreads();
-  if (warp == 12) {
+  if (warp == kMmaWarp) {
     tc_fence_after();
     tmem_relinquish();
     tmem_dealloc(tmem, 512);
