@@ -131,28 +131,31 @@ struct RowScore {
 
 // ---- many rows: tensor cores of the fifth generation ----------------------
 // A CTA holds 256 rows as two 128-row tiles, streams blocks of 128 keys, and
-// computes S = Q K^T and O += P V with tcgen05.mma kind::f16.
-//   warps 0-7, 8-15  softmax of tile 0 and 1, two threads a row with 64 keys (and
-//                    channels of O) each: read S from TMEM, write P over it,
-//                    rescale O where a maximum moved by more than 2^8
-//   warps 16-19      dequantize the block's K and V into shared memory (f16,
-//                    exact: an E2M1 x E4M3 product has at most 6 significant bits)
-//   warp 20          issues the MMAs: PV of tile t, then its next QK^T, so that
-//                    one tile's softmax runs beside the other's MMAs; warps 21-23
-//                    complete its warpgroup and idle
+// computes S = Q K^T and O += P V with tcgen05.mma kind::f16, 64 keys at a time.
+//   warps 0-3, 4-7  softmax of tile 0 and 1 (thread = row): read S from TMEM,
+//                   write P over it, rescale O where a maximum moved by over 2^8
+//   warps 8-11      dequantize the block's K and V into shared memory (f16,
+//                   exact: an E2M1 x E4M3 product has at most 6 significant bits)
+//   warp 12         issues the MMAs; warps 13-15 complete its warpgroup and idle
+// TMEM holds O of both tiles (256 columns) and two 64-column S of each tile: while
+// a softmax works on one, the other is already multiplied, so that neither the
+// softmax nor the tensor core waits for the other's latency.  (One 128-column S
+// a tile, whose QK^T has to wait for PV: 4230 cycles per block and two tiles;
+// N = 64 costs the QK^T a half more shared-memory reads of Q.)
 // With at most 128 rows the second tile takes the same rows with every second
 // block, and the two are joined at the end.
 constexpr int kTileRows = 256;
 constexpr int kBlock = 128;  // keys per block
-constexpr int kTileThreads = 24 * 32;
-constexpr int kDequantWarp = 16, kMmaWarp = 20;
+constexpr int kTileThreads = 16 * 32;
+constexpr int kDequantWarp = 8, kMmaWarp = 12;
 constexpr uint32_t kOperand = 32768;  // bytes of a 128 x 128 f16 operand
 constexpr uint32_t kOffK = 2 * kOperand, kOffV = 4 * kOperand;
 constexpr uint32_t kTileSmem = 6 * kOperand + 1024;  // and alignment
 
-// f16 operands, fp32 accumulator, 128 x 128; bit 16: B is stored with N contiguous.
-constexpr uint32_t kIdescQK = (1u << 4) | (16u << 17) | (8u << 24);
-constexpr uint32_t kIdescPV = kIdescQK | (1u << 16);
+// f16 operands, fp32 accumulator, 128 x 64 (QK^T) and 128 x 128; bit 16: B is
+// stored with N contiguous.
+constexpr uint32_t kIdescQK = (1u << 4) | (8u << 17) | (8u << 24);
+constexpr uint32_t kIdescPV = (1u << 4) | (1u << 16) | (16u << 17) | (8u << 24);
 constexpr uint32_t kIdescPVFull = kIdescPV | (1u << 7) | (1u << 10);  // bf16 operands
 // 128-byte-swizzled operand: rows of 128 bytes, 8-row groups 1024 bytes apart
 // (sbo), the second 64 columns kOperand / 2 further (lbo, used with N contiguous).
@@ -207,29 +210,10 @@ __device__ __forceinline__ void add2(float& x, float& y, float u, float v) {
       : "+f"(x), "+f"(y)
       : "f"(u), "f"(v));
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* r) {
-  uint32_t* u = reinterpret_cast<uint32_t*>(r);
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
-        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
-      : "r"(taddr));
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
-}
-// Whether any of a tile's 256 softmax threads says so; also their barrier.
-__device__ __forceinline__ bool tile_any(int barrier, bool mine) {
-  uint32_t any;
-  tc_fence_before();  // what the threads have read from TMEM is read
-  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, %2, 256, p;\n selp.u32 %0, 1, 0, q;\n}"
-               : "=r"(any)
-               : "r"(static_cast<uint32_t>(mine)), "r"(barrier)
-               : "memory");
-  tc_fence_after();
-  return any != 0;
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -237,15 +221,20 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, ui
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
 struct TileShared {
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_done[2], drain;
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2][2], p_full[2][2], o_done[2], q_full, drain;
   uint32_t tmem;
   Tile tile;
   Seq seq;
   int lo, hi;       // keys that some row of the tile sees
   float mult[kTileRows];
   float2 ml[kBlock];             // tile 1's (max, sum), for the join
-  float half[2][2][128];         // a value of each row's two threads, by tile and half
   alignas(16) uint32_t present[4][4];  // bit per key of a block: loaded, in the last four blocks' slots
   volatile int abort;
 };
@@ -294,10 +283,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       mbar_init(&sh.k_empty[i], 1);
       mbar_init(&sh.v_full[i], 4);
       mbar_init(&sh.v_empty[i], 1);
-      mbar_init(&sh.s_full[i], 1);
-      mbar_init(&sh.p_full[i], 8);
+      for (int v = 0; v < 2; ++v) {
+        mbar_init(&sh.s_full[i][v], 1);
+        mbar_init(&sh.p_full[i][v], 4);
+      }
       mbar_init(&sh.o_done[i], 1);
     }
+    mbar_init(&sh.q_full, 8);
     mbar_init(&sh.drain, 1);
     sh.abort = 0;
     sh.lo = 0x7fffffff;
@@ -327,7 +319,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
   const bool two = rows > 128;
 
   // Row of a softmax thread: tile 1 has rows 128.. of a large tile, or rows 0.. again.
-  const int t = warp >> 3, hf = (warp >> 2) & 1;
+  const int t = warp >> 2;
   const uint32_t in_tile = threadIdx.x & 127, local = (two ? t * 128u : 0u) + in_tile;
   const bool live = warp < kDequantWarp && local < rows;
   const uint32_t r = sh.tile.row0 + (live ? local : 0), tok = a.group.div(r), head = kvh * group + (r - tok * group);
@@ -343,22 +335,34 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       atomicMin(&sh.lo, lo);
       atomicMax(&sh.hi, hi);
     }
-    // Q rows as f16: 16 lanes a row, two rows a turn, 16 rows a warp.  Each row is
+  }
+  __syncthreads();
+  // The tile's blocks of keys, and this CTA's part of them.
+  const int lo = sh.lo, total = sh.hi > lo ? (sh.hi - lo + kBlock - 1) / kBlock : 0;
+  const int per = (total + static_cast<int>(a.splits) - 1) / static_cast<int>(a.splits);
+  const int j0 = min(static_cast<int>(split) * per, total), nblk = min(per, total - j0);
+  const int t_base = lo + j0 * kBlock;
+  const int subs_of[2] = {two ? 2 * nblk : (nblk + 1) / 2 * 2, two ? 2 * nblk : nblk / 2 * 2};  // 64-key steps of a tile
+
+  if (warp < kDequantWarp) {
+    // ------------------------------------------------------------- softmax ---
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    // Q rows as f16: 16 lanes a row, two rows a turn, 32 rows a warp.  Each row is
     // scaled by a power of two (exact) to below 1; `mult` undoes it.
-    const int c = lane & 15;
-    if (two || warp < 8) {
-      uint4 w[8];
+    if (two || warp < 4) {
+      const int c = lane & 15;
+      uint4 w[16];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t lr = warp * 16 + 2 * i + (lane >> 4);
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t lr = warp * 32 + 2 * i + (lane >> 4);
         const uint32_t rr = sh.tile.row0 + (lr < rows ? lr : 0), tk = a.group.div(rr);
         w[i] = lr < rows ? __ldg(reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(seq.first + tk) * a.ld_q +
                                                                 (kvh * group + rr - tk * group) * kD) + c)
                          : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t lr = warp * 16 + 2 * i + (lane >> 4);
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t lr = warp * 32 + 2 * i + (lane >> 4);
         uint32_t top = amax_bits_bf16x8(w[i]);
 #pragma unroll
         for (int s = 1; s < 16; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
@@ -371,23 +375,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
         sts128(smem + (lr >> 7) * kOperand + operand_chunk(lr & 127, c), f16x2_rn(x[0] * down, x[1] * down),
                f16x2_rn(x[2] * down, x[3] * down), f16x2_rn(x[4] * down, x[5] * down), f16x2_rn(x[6] * down, x[7] * down));
       }
+      fence_proxy_async_smem();
     }
-    fence_proxy_async_smem();
-  }
-  __syncthreads();
-  // The tile's blocks of keys, and this CTA's part of them.
-  const int lo = sh.lo, total = sh.hi > lo ? (sh.hi - lo + kBlock - 1) / kBlock : 0;
-  const int per = (total + static_cast<int>(a.splits) - 1) / static_cast<int>(a.splits);
-  const int j0 = min(static_cast<int>(split) * per, total), nblk = min(per, total - j0);
-  const int t_base = lo + j0 * kBlock;
-  const int n_of[2] = {two ? nblk : (nblk + 1) / 2, two ? nblk : nblk / 2};  // blocks of each softmax tile
-
-  if (warp < kDequantWarp) {
-    // ------------------------------------------------------------- softmax ---
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
-    const int n = n_of[t];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.q_full);
+    if (!two) asm volatile("bar.sync 1, 256;" ::: "memory");  // tile 1 reads the multipliers of tile 0's rows
+    const int subs = subs_of[t];
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_tile = tmem + lanes + t * 128, s_col = s_tile + 64 * hf, o_col = tmem + lanes + 256 + t * 128 + 64 * hf;
+    const uint32_t s_tile = tmem + lanes + t * 128, o_col = tmem + lanes + 256 + t * 128;
     RowScore rs;
     rs.mult = sh.mult[live ? local : 0];
     rs.slope = kMods && a.slopes && live ? __ldg(a.slopes + head) * kLog2e : 0.0f;
@@ -397,14 +392,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     const float to_log2 = kMods ? 1.0f : rs.mult;
     float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
     bool ok = true;
-    for (int i = 0; i < n; ++i) {
-      const int j = two ? i : 2 * i + t, t0 = t_base + j * kBlock + 64 * hf;
-      // A warp whose wait ran out leaves with the others of its tile, below.
-      ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&sh.s_full[t], i & 1, &sh.abort));
+    for (int v = 0; v < subs; ++v) {
+      const int j = two ? v >> 1 : (v & ~1) + t, hf = v & 1, t0 = t_base + j * kBlock + 64 * hf;
+      const uint32_t s_col = s_tile + 64 * hf;
+      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.s_full[t][hf], (v >> 1) & 1, &sh.abort));
+      if (!ok) break;
       tc_fence_after();
       const uint2 pres = *reinterpret_cast<const uint2*>(&sh.present[j & 3][2 * hf]);
       const bool open = t0 >= all_lo && t0 + 64 <= all_hi && (pres.x & pres.y) == 0xffffffffu;
-      // The thread's scores, all in registers, and their maximum.
+      // The row's scores, all in registers, and their maximum.
       float s[64];
       tmem_ld32(s_col, s);
       tmem_ld32(s_col + 32, s + 32);
@@ -423,34 +419,31 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
 #pragma unroll
         for (int k = 8; k < 64; k += 8) tops[c] = max3(s[k + c], s[k + c + 4], tops[c]);
       }
-      float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * to_log2;
-      const auto above = [&](float x) { return x > m + kRescaleLog2 || (m == -INFINITY && x > -INFINITY); };
-      if (tile_any(1 + t, above(top) || !ok)) {
-        // Some row's maximum moves: its two threads exchange theirs.
-        sh.half[t][hf][in_tile] = top;
-        if (tile_any(1 + t, !ok)) { ok = false; break; }
-        top = fmaxf(top, sh.half[t][hf ^ 1][in_tile]);
-        const bool up = above(top);
+      const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * to_log2;
+      const bool up = top > m + kRescaleLog2 || (m == -INFINITY && top > -INFINITY);
+      if (__any_sync(0xffffffffu, up)) {
         const float shrink = up ? ex2(m - top) : 1.0f;  // 0 where there was none
         if (up) m = top;
         l0 *= shrink;
         l1 *= shrink;
-        if (i > 0 && __any_sync(0xffffffffu, up)) {
-          ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.o_done[t], (i - 1) & 1, &sh.abort));
+        if (v > 0) {
+          ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.o_done[t], (v - 1) & 1, &sh.abort));
+          if (!ok) break;
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < 4; ++c) {
-            float o[16];
-            tmem_ld16(o_col + 16 * c, o);
+            float o[32];
+            tmem_ld32(o_col + 32 * c, o);
             tmem_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 16; ++k) o[k] *= shrink;
-            tmem_st16(o_col + 16 * c, reinterpret_cast<uint32_t*>(o));
+            for (int k = 0; k < 32; ++k) o[k] *= shrink;
+            tmem_st16(o_col + 32 * c, reinterpret_cast<uint32_t*>(o));
+            tmem_st16(o_col + 32 * c + 16, reinterpret_cast<uint32_t*>(o) + 16);
           }
         }
       }
       const float minus = (m == -INFINITY ? 0.0f : -m) + kWeightLog2;
-      // The weights, over scores that both of the row's threads have read (tile_any).
+      // The weights, over the scores they came from.
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         uint32_t w[16], rest[kFull ? 16 : 1];
@@ -469,184 +462,210 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
             w[k] = f16x2_rn(x, y);
           }
         }
-        tmem_st16(s_tile + 32 * hf + 16 * c, w);
-        if (kFull) tmem_st16(s_tile + 64 + 32 * hf + 16 * c, rest);
+        tmem_st16(s_col + 16 * c, w);
+        if (kFull) tmem_st16(s_col + 32 + 16 * c, rest);
       }
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.p_full[t]);
+      if (lane == 0) mbar_arrive(&sh.p_full[t][hf]);
     }
-    if (ok && n > 0) {
-      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.o_done[t], (n - 1) & 1, &sh.abort));
+    // S of the last step says that PV of the step three back is done; the last
+    // two phases of o_done are waited for in turn.
+    for (int v = max(subs - 2, 0); v < subs && ok; ++v) {
+      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.o_done[t], v & 1, &sh.abort));
       tc_fence_after();
     }
     if (!ok && lane == 0 && !sh.abort) {
       set_status(a.status, NVFP4_ERR_TIMEOUT);
       sh.abort = 1;
     }
-    sh.half[t][hf][in_tile] = l0 + l1;
-    asm volatile("bar.sync 3, 512;" ::: "memory");
-    const float l = l0 + l1 + sh.half[t][hf ^ 1][in_tile];
+    const float l = l0 + l1;
     // A tile that took the other blocks of the same rows hands over its part.
     float* hand = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + kOffK);  // [channel][row]
     float other_m = -INFINITY, other_l = 0.0f;
     if (!two) {
       if (t == 1) {
-        if (hf == 0) sh.ml[in_tile] = make_float2(m, l);
-        if (ok && n > 0) {
-          for (int c = 0; c < 2; ++c) {
+        sh.ml[in_tile] = make_float2(m, l);
+        if (ok && subs > 0) {
+          for (int c = 0; c < 4; ++c) {
             float o[32];
             tmem_ld32(o_col + 32 * c, o);
             tmem_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 32; ++k) hand[(64 * hf + 32 * c + k) * 128 + in_tile] = o[k];
+            for (int k = 0; k < 32; ++k) hand[(32 * c + k) * 128 + in_tile] = o[k];
           }
         }
       }
-      asm volatile("bar.sync 3, 512;" ::: "memory");
+      asm volatile("bar.sync 1, 256;" ::: "memory");
       const float2 other = sh.ml[in_tile];
-      if (t == 0 && n_of[1] > 0) {
+      if (t == 0 && subs_of[1] > 0) {
         other_m = other.x;
         other_l = other.y;
       }
     }
     if (ok && !none && (two || t == 0)) {
+      // Every QK^T is done: the warp's 32 rows of Q hold its output until the
+      // stores, which take whole rows.
       const float big = fmaxf(m, other_m);
       const float w0 = m == -INFINITY ? 0.0f : ex2(m - big), w1 = other_m == -INFINITY ? 0.0f : ex2(other_m - big);
       const float sum = w0 * l + w1 * other_l;
       const float f = a.splits > 1 ? 1.0f : sum > 0.0f ? a.gv / sum : 0.0f;
-      const uint64_t rec = ((static_cast<uint64_t>(tile_id) * a.map.hkv + kvh) * a.splits + split) * kTileRows + local;
-      if (a.splits > 1 && live && hf == 0) a.ml_ws[rec] = make_float2(big, sum);
-      uint4* out = reinterpret_cast<uint4*>(a.out + (static_cast<uint64_t>(seq.first + tok) * a.hq + head) * kD) + 8 * hf;
-      float4* part = reinterpret_cast<float4*>(a.o_ws + rec * kD) + 16 * hf;
-      for (int c = 0; c < 2; ++c) {
+      const uint64_t rec0 = ((static_cast<uint64_t>(tile_id) * a.map.hkv + kvh) * a.splits + split) * kTileRows;
+      if (a.splits > 1 && live) a.ml_ws[rec0 + local] = make_float2(big, sum);
+      const uint32_t stage = smem + warp * 8192, row0 = local - lane;
+      const auto at = [&](uint32_t row, uint32_t c) { return stage + row * 256 + ((c ^ (row & 7)) << 4); };
+#pragma unroll 1
+      for (int c = 0; c < 4; ++c) {
         float o[32];
-        if (n > 0) {
+        if (subs > 0) {
           tmem_ld32(o_col + 32 * c, o);
           tmem_wait_ld();
         }
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
-          o[k] = n > 0 && w0 != 0.0f ? o[k] * w0 : 0.0f;
-          if (w1 != 0.0f) o[k] = fmaf(hand[(64 * hf + 32 * c + k) * 128 + in_tile], w1, o[k]);
+          o[k] = subs > 0 && w0 != 0.0f ? o[k] * w0 : 0.0f;
+          if (w1 != 0.0f) o[k] = fmaf(hand[(32 * c + k) * 128 + in_tile], w1, o[k]);
           o[k] *= f;
         }
-        if (!live) continue;
-        if (a.splits > 1) {
-          if (big == -INFINITY) continue;  // the combine does not read it
-#pragma unroll
-          for (int k = 0; k < 8; ++k) part[8 * c + k] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
-        } else {
+        if (a.splits == 1) {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            out[4 * c + k] = make_uint4(bf16x2_rn(o[8 * k], o[8 * k + 1]), bf16x2_rn(o[8 * k + 2], o[8 * k + 3]),
-                                        bf16x2_rn(o[8 * k + 4], o[8 * k + 5]), bf16x2_rn(o[8 * k + 6], o[8 * k + 7]));
+            sts128(at(lane, 4 * c + k), bf16x2_rn(o[8 * k], o[8 * k + 1]), bf16x2_rn(o[8 * k + 2], o[8 * k + 3]),
+                   bf16x2_rn(o[8 * k + 4], o[8 * k + 5]), bf16x2_rn(o[8 * k + 6], o[8 * k + 7]));
+          continue;
+        }
+        // A record in fp32: 128 bytes of each row at a time.
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          sts128(at(lane, k), __float_as_uint(o[4 * k]), __float_as_uint(o[4 * k + 1]), __float_as_uint(o[4 * k + 2]),
+                 __float_as_uint(o[4 * k + 3]));
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t row = 4 * i + (lane >> 3);
+          if (row0 + row < rows)
+            reinterpret_cast<uint4*>(a.o_ws + (rec0 + row0 + row) * kD)[8 * c + (lane & 7)] = lds128(at(row, lane & 7));
+        }
+        __syncwarp();
+      }
+      if (a.splits == 1) {
+        __syncwarp();
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t row = 2 * i + (lane >> 4);
+          if (row0 + row >= rows) continue;
+          const uint32_t rr = sh.tile.row0 + row0 + row, tk = a.group.div(rr);
+          reinterpret_cast<uint4*>(a.out + (static_cast<uint64_t>(seq.first + tk) * a.hq + kvh * group + rr - tk * group) * kD)
+              [lane & 15] = lds128(at(row, lane & 15));
         }
       }
     }
     tc_fence_before();
   } else if (warp < kMmaWarp) {
     // ---------------------------------------------------------- dequantize ---
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     // Four lanes a key: 16 bytes (32 channels) of its codes and two scale bytes
-    // each, so a warp's load covers 8 keys' rows; four turns a block.
+    // each, so a warp's load covers 8 keys' rows; four turns an operand.  Operands
+    // in the order in which their buffers come free: K0 V0 K1 V1 ..., or, where
+    // the tiles take a block each, K0 K1 V0 V1 K2 ....  Two are in flight.
     const int w = warp - kDequantWarp, sub = lane >> 2, qd = lane & 3;
     const int64_t head_rows = static_cast<int64_t>(kvh) * a.map.size.d;
-    const int end = sh.hi;
-    int64_t row[4];
-    uint4 kc[4], vc[4];
-    uint32_t ks[4], vs[4];
-    uint32_t here = 0;
-    auto find = [&](int j) {
+    const int end = sh.hi, operands = two ? 2 * nblk : (nblk + 1) / 2 * 4;
+    struct Buffer {
+      int64_t row[4];  // of the operand that is loaded next
+      uint4 c[4];
+      uint32_t s[4], here;
+    };
+    const auto is_v = [&](int q) { return (two ? q : q >> 1) & 1; };
+    const auto block = [&](int q) { return two ? q >> 1 : (q >> 2) * 2 + (q & 1); };
+    const auto find = [&](Buffer& f, int q) {
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
-        const int t = t_base + j * kBlock + it * 32 + w * 8 + sub;
-        row[it] = j < nblk && t < end ? a.map.row(sh.tile.b, t) : -1;
+        const int t = t_base + block(q) * kBlock + it * 32 + w * 8 + sub;
+        f.row[it] = q < operands && block(q) < nblk && t < end ? a.map.row(sh.tile.b, t) : -1;
       }
     };
-    auto load = [&](const uint8_t* codes, const uint8_t* scales, uint4* c, uint32_t* s) {
+    const auto load = [&](Buffer& f, int q) {
+      const uint8_t* codes = is_v(q) ? a.map.v_codes : a.map.k_codes;
+      const uint8_t* scales = is_v(q) ? a.map.v_scales : a.map.k_scales;
+      f.here = 0;
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
-        const int64_t at = row[it] + head_rows;
-        c[it] = row[it] >= 0 ? __ldg(reinterpret_cast<const uint4*>(codes + at * 64) + qd) : make_uint4(0, 0, 0, 0);
-        s[it] = row[it] >= 0 ? __ldg(reinterpret_cast<const uint16_t*>(scales + at * 8) + qd) : 0u;
+        const int64_t at = f.row[it] + head_rows;
+        const bool ok = f.row[it] >= 0;
+        f.c[it] = ok ? __ldg(reinterpret_cast<const uint4*>(codes + at * 64) + qd) : make_uint4(0, 0, 0, 0);
+        f.s[it] = ok ? __ldg(reinterpret_cast<const uint16_t*>(scales + at * 8) + qd) : 0u;
+        f.here |= ok ? 1u << it : 0u;
       }
     };
-    auto store = [&](uint32_t base, const uint4* c, const uint32_t* s, bool bf16) {
+    const auto store = [&](const Buffer& f, uint32_t base, bool bf16) {
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
         const uint32_t rr = it * 32 + w * 8 + sub;
-        const uint32_t f = kv_scales16<kE1M2>(s[it]);
-        const uint32_t f0 = __byte_perm(f, f, 0x1010), f1 = __byte_perm(f, f, 0x3232);
+        const uint32_t g = kv_scales16<kE1M2>(f.s[it]);
+        const uint32_t g0 = __byte_perm(g, g, 0x1010), g1 = __byte_perm(g, g, 0x3232);
         // Lanes of the second 64 channels start with their other pair of words, so
         // that eight lanes' chunks meet eight different bank groups.
         const bool sw = qd & 2;
-        const uint32_t words[4] = {sw ? c[it].z : c[it].x, sw ? c[it].w : c[it].y, sw ? c[it].x : c[it].z,
-                                   sw ? c[it].y : c[it].w};
+        const uint32_t words[4] = {sw ? f.c[it].z : f.c[it].x, sw ? f.c[it].w : f.c[it].y, sw ? f.c[it].x : f.c[it].z,
+                                   sw ? f.c[it].y : f.c[it].w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           uint32_t e[4];
           elements8<kE1M2>(words[k], e);
-          const uint32_t g = (k < 2) != sw ? f0 : f1;
+          const uint32_t gk = (k < 2) != sw ? g0 : g1;
           const uint32_t chunk = 4 * qd + (sw ? k ^ 2 : k);
 #pragma unroll
-          for (int x = 0; x < 4; ++x) e[x] = bf16 ? bf16x2_of_f16x2(mul_f16x2(e[x], g)) : mul_f16x2(e[x], g);
+          for (int x = 0; x < 4; ++x) e[x] = bf16 ? bf16x2_of_f16x2(mul_f16x2(e[x], gk)) : mul_f16x2(e[x], gk);
           sts128(base + operand_chunk(rr, chunk), e[0], e[1], e[2], e[3]);
         }
       }
+    };
+    // False: a wait ran out.
+    const auto operand = [&](Buffer& f, int q) {
+      const int j = block(q), st = j & 1;
+      if (j >= nblk) return true;
+      if (!__all_sync(0xffffffffu, mbar_wait_bounded(is_v(q) ? &sh.v_empty[st] : &sh.k_empty[st], ((j >> 1) & 1) ^ 1, &sh.abort)))
+        return false;
+      if (is_v(q)) {
+        store(f, smem + kOffV + st * kOperand, kFull);
+      } else {
+        // Which keys are there: byte it * 4 + w has this warp's 8 keys of turn it.
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          uint32_t v = __ballot_sync(0xffffffffu, qd == 0 && ((f.here >> it) & 1u));  // bits 0, 4, 8, ...
+          v = (v | v >> 3) & 0x03030303u;
+          v = (v | v >> 6) & 0x000F000Fu;
+          v = (v | v >> 12) & 0xFFu;
+          if (lane == 0) reinterpret_cast<uint8_t*>(sh.present[j & 3])[it * 4 + w] = static_cast<uint8_t>(v);
+        }
+        store(f, smem + kOffK + st * kOperand, false);
+      }
       fence_proxy_async_smem();
       __syncwarp();
+      if (lane == 0) mbar_arrive(is_v(q) ? &sh.v_full[st] : &sh.k_full[st]);
+      load(f, q + 2);
+      find(f, q + 4);
+      return true;
     };
-    auto bits = [&] {
-      here = 0;
-#pragma unroll
-      for (int it = 0; it < 4; ++it) here |= row[it] >= 0 ? 1u << it : 0u;
-    };
-    find(0);
-    bits();
-    load(a.map.k_codes, a.map.k_scales, kc, ks);
-    load(a.map.v_codes, a.map.v_scales, vc, vs);
-    find(1);
-    for (int j = 0; j < nblk; ++j) {
-      const int st = j & 1;
-      const uint32_t ph = ((j >> 1) & 1) ^ 1;
-      bool ok = mbar_wait_bounded(&sh.k_empty[st], ph, &sh.abort);
-      if (!__all_sync(0xffffffffu, ok)) {
+    Buffer f0, f1;
+    find(f0, 0);
+    find(f1, 1);
+    load(f0, 0);
+    load(f1, 1);
+    find(f0, 2);
+    find(f1, 3);
+    for (int q = 0; q < operands; q += 2)
+      if (!operand(f0, q) || !operand(f1, q + 1)) {
         if (lane == 0 && !sh.abort) {
           set_status(a.status, NVFP4_ERR_TIMEOUT);
           sh.abort = 1;
         }
         break;
       }
-      // Which keys are there: byte it * 4 + w has this warp's 8 keys of turn it.
-#pragma unroll
-      for (int it = 0; it < 4; ++it) {
-        uint32_t v = __ballot_sync(0xffffffffu, qd == 0 && ((here >> it) & 1u));  // bits 0, 4, 8, ...
-        v = (v | v >> 3) & 0x03030303u;
-        v = (v | v >> 6) & 0x000F000Fu;
-        v = (v | v >> 12) & 0xFFu;
-        if (lane == 0) reinterpret_cast<uint8_t*>(sh.present[j & 3])[it * 4 + w] = static_cast<uint8_t>(v);
-      }
-      store(smem + kOffK + st * kOperand, kc, ks, false);
-      if (lane == 0) mbar_arrive(&sh.k_full[st]);
-      bits();
-      load(a.map.k_codes, a.map.k_scales, kc, ks);
-      ok = mbar_wait_bounded(&sh.v_empty[st], ph, &sh.abort);
-      if (!__all_sync(0xffffffffu, ok)) {
-        if (lane == 0 && !sh.abort) {
-          set_status(a.status, NVFP4_ERR_TIMEOUT);
-          sh.abort = 1;
-        }
-        break;
-      }
-      store(smem + kOffV + st * kOperand, vc, vs, kFull);
-      if (lane == 0) mbar_arrive(&sh.v_full[st]);
-      load(a.map.v_codes, a.map.v_scales, vc, vs);
-      find(j + 2);
-    }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 24;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == kMmaWarp) {
       // --------------------------------------------------------------- MMA ---
       // The warp stays converged, so that descriptors live in uniform registers;
@@ -662,79 +681,53 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
         if (leader) tc_commit(bar);
       };
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-      auto qk = [&](int t, int st) {
-        const uint32_t q = operand_desc(smem + (two ? t : 0) * kOperand), k = operand_desc(smem + kOffK + st * kOperand);
+      // Step v of tile t: half v & 1 of its block v >> 1.
+      const auto block_of = [&](int t, int v) { return two ? v >> 1 : (v & ~1) + t; };
+      auto qk = [&](int t, int v) {
+        const int j = block_of(t, v), st = j & 1, hf = v & 1;
+        if (!wait(&sh.k_full[st], j >> 1)) return;
+        const uint32_t q = operand_desc(smem + (two ? t : 0) * kOperand), k = operand_desc(smem + kOffK + st * kOperand + hf * 8192);
         if (leader) {
 #pragma unroll
           for (int s = 0; s < 8; ++s) {
             const uint32_t at = ((s >> 2) * (kOperand / 2) + (s & 3) * 32) >> 4;
-            mma_ss(tm + t * 128, q + at, k + at, kIdescQK, s != 0);
+            mma_ss(tm + t * 128 + hf * 64, q + at, k + at, kIdescQK, s != 0);
           }
-          tc_commit(&sh.s_full[t]);
+          tc_commit(&sh.s_full[t][hf]);
         }
+        if (hf && (!two || t == 1)) commit(&sh.k_empty[st]);
       };
-      auto pv = [&](int t, int st, bool first) {
-        const uint32_t v = operand_desc(smem + kOffV + st * kOperand);
+      auto pv = [&](int t, int v) {
+        const int j = block_of(t, v), st = j & 1, hf = v & 1;
+        if (!wait(&sh.v_full[st], j >> 1) || !wait(&sh.p_full[t][hf], v >> 1)) return;
+        const uint32_t vd = operand_desc(smem + kOffV + st * kOperand + hf * 8192), p = tm + t * 128 + hf * 64;
         if (leader) {
 #pragma unroll
-          for (int s = 0; s < (kFull ? 16 : 8); ++s)
-            mma_ts(tm + 256 + t * 128, tm + t * 128 + s * 8, v + (((s & 7) * 2048) >> 4), kFull ? kIdescPVFull : kIdescPV,
-                   !(first && s == 0));
+          for (int s = 0; s < (kFull ? 8 : 4); ++s)
+            mma_ts(tm + 256 + t * 128, p + s * 8, vd + (((s & 3) * 2048) >> 4), kFull ? kIdescPVFull : kIdescPV,
+                   v != 0 || s != 0);
           tc_commit(&sh.o_done[t]);
         }
+        if (hf && (!two || t == 1)) commit(&sh.v_empty[st]);
       };
-      if (two) {
-        if (nblk > 0 && wait(&sh.k_full[0], 0)) {
-          qk(0, 0);
-          qk(1, 0);
-          commit(&sh.k_empty[0]);
-        }
-        for (int i = 0; i < nblk && ok; ++i) {
-          const int st = i & 1, nx = st ^ 1;
-          const bool more = i + 1 < nblk;
-          if (!wait(&sh.v_full[st], i >> 1) || !wait(&sh.p_full[0], i)) break;
-          pv(0, st, i == 0);
-          if (more) {
-            if (!wait(&sh.k_full[nx], (i + 1) >> 1)) break;
-            qk(0, nx);
+      wait(&sh.q_full, 0);
+      for (int v = 0; v < 2 && ok; ++v)
+        for (int t = 0; t < 2 && ok; ++t)
+          if (v < subs_of[t]) qk(t, v);
+      for (int v = 0; v < subs_of[0] && ok; ++v)
+        for (int t = 0; t < 2 && ok; ++t)
+          if (v < subs_of[t]) {
+            pv(t, v);
+            if (ok && v + 2 < subs_of[t]) qk(t, v + 2);
           }
-          if (!wait(&sh.p_full[1], i)) break;
-          pv(1, st, i == 0);
-          commit(&sh.v_empty[st]);
-          if (more) {
-            qk(1, nx);
-            commit(&sh.k_empty[nx]);
-          }
-        }
-      } else {
-        for (int t = 0; t < 2; ++t)
-          if (n_of[t] > 0 && wait(&sh.k_full[t], 0)) {
-            qk(t, t);
-            commit(&sh.k_empty[t]);
-          }
-        for (int i = 0; i < n_of[0] && ok; ++i)
-          for (int t = 0; t < 2 && ok; ++t) {
-            if (i >= n_of[t]) continue;
-            if (!wait(&sh.v_full[t], i) || !wait(&sh.p_full[t], i)) break;
-            pv(t, t, i == 0);
-            commit(&sh.v_empty[t]);
-            if (i + 1 < n_of[t] && wait(&sh.k_full[t], i + 1)) {
-              qk(t, t);
-              commit(&sh.k_empty[t]);
-            }
-          }
+      if (!ok && leader && !sh.abort) {
+        set_status(a.status, NVFP4_ERR_TIMEOUT);
+        sh.abort = 1;
       }
-      if (!ok) {
-        if (leader) {
-          if (!sh.abort) {
-            set_status(a.status, NVFP4_ERR_TIMEOUT);
-            sh.abort = 1;
-          }
-          tc_commit(&sh.drain);  // the MMAs issued so far end before TMEM is freed
-          mbar_wait_bounded(&sh.drain, 0, nullptr, kDrainLimitNs);
-        }
-        __syncwarp();
-      }
+      // Nothing that was issued, MMA or arrival, outlives the CTA.
+      commit(&sh.drain);
+      mbar_wait_bounded(&sh.drain, 0, nullptr, kDrainLimitNs);
+      __syncwarp();
     }
   }
   __syncthreads();
