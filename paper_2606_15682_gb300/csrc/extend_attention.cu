@@ -134,9 +134,12 @@ struct RowScore {
 // computes S = Q K^T and O += P V with tcgen05.mma kind::f16, 64 keys at a time.
 //   warps 0-3, 4-7  softmax of tile 0 and 1 (thread = row): read S from TMEM,
 //                   write P over it, rescale O where a maximum moved by over 2^8
-//   warps 8-11      dequantize the block's K and V into shared memory (f16,
-//                   exact: an E2M1 x E4M3 product has at most 6 significant bits)
-//   warp 12         issues the MMAs; warps 13-15 complete its warpgroup and idle
+//   warps 8-15      dequantize the blocks' K and V into shared memory (f16,
+//                   exact: an E2M1 x E4M3 product has at most 6 significant
+//                   bits), one warpgroup each
+//   warps 16, 17    issue the MMAs of tile 0 and 1 (by one warp, the waits before
+//                   one tile's MMAs left the tensor core idle: 4300 cycles a
+//                   block); warps 18, 19 complete their warpgroup and idle
 // TMEM holds O of both tiles (256 columns) and two 64-column S of each tile: while
 // a softmax works on one, the other is already multiplied, so that neither the
 // softmax nor the tensor core waits for the other's latency.  (One 128-column S
@@ -146,8 +149,8 @@ struct RowScore {
 // block, and the two are joined at the end.
 constexpr int kTileRows = 256;
 constexpr int kBlock = 128;  // keys per block
-constexpr int kTileThreads = 16 * 32;
-constexpr int kDequantWarp = 8, kMmaWarp = 12;
+constexpr int kTileThreads = 20 * 32;
+constexpr int kDequantWarp = 8, kMmaWarp = 16;
 constexpr uint32_t kOperand = 32768;  // bytes of a 128 x 128 f16 operand
 constexpr uint32_t kOffK = 2 * kOperand, kOffV = 4 * kOperand;
 constexpr uint32_t kTileSmem = 6 * kOperand + 1024;  // and alignment
@@ -228,7 +231,7 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 }
 
 struct TileShared {
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2][2], p_full[2][2], o_done[2], q_full, drain;
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2][2], p_full[2][2], o_done[2], q_full, drain[2];
   uint32_t tmem;
   Tile tile;
   Seq seq;
@@ -280,17 +283,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.k_full[i], 4);
-      mbar_init(&sh.k_empty[i], 1);
+      mbar_init(&sh.k_empty[i], 2);
       mbar_init(&sh.v_full[i], 4);
-      mbar_init(&sh.v_empty[i], 1);
+      mbar_init(&sh.v_empty[i], 2);
       for (int v = 0; v < 2; ++v) {
         mbar_init(&sh.s_full[i][v], 1);
         mbar_init(&sh.p_full[i][v], 4);
       }
       mbar_init(&sh.o_done[i], 1);
+      mbar_init(&sh.drain[i], 1);
     }
     mbar_init(&sh.q_full, 8);
-    mbar_init(&sh.drain, 1);
     sh.abort = 0;
     sh.lo = 0x7fffffff;
     sh.hi = 0;
@@ -338,7 +341,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
   }
   __syncthreads();
   // The tile's blocks of keys, and this CTA's part of them.
-  const int lo = sh.lo, total = sh.hi > lo ? (sh.hi - lo + kBlock - 1) / kBlock : 0;
+  const int lo = sh.hi > sh.lo ? sh.lo : 0, total = sh.hi > sh.lo ? (sh.hi - lo + kBlock - 1) / kBlock : 0;
   const int per = (total + static_cast<int>(a.splits) - 1) / static_cast<int>(a.splits);
   const int j0 = min(static_cast<int>(split) * per, total), nblk = min(per, total - j0);
   const int t_base = lo + j0 * kBlock;
@@ -346,7 +349,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
 
   if (warp < kDequantWarp) {
     // ------------------------------------------------------------- softmax ---
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
     // Q rows as f16: 16 lanes a row, two rows a turn, 32 rows a warp.  Each row is
     // scaled by a power of two (exact) to below 1; `mult` undoes it.
     if (two || warp < 4) {
@@ -485,6 +488,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     float* hand = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + kOffK);  // [channel][row]
     float other_m = -INFINITY, other_l = 0.0f;
     if (!two) {
+      asm volatile("bar.sync 1, 256;" ::: "memory");  // neither tile's MMAs read K any more
       if (t == 1) {
         sh.ml[in_tile] = make_float2(m, l);
         if (ok && subs > 0) {
@@ -564,52 +568,67 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     tc_fence_before();
   } else if (warp < kMmaWarp) {
     // ---------------------------------------------------------- dequantize ---
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     // Four lanes a key: 16 bytes (32 channels) of its codes and two scale bytes
-    // each, so a warp's load covers 8 keys' rows; four turns an operand.  Operands
-    // in the order in which their buffers come free: K0 V0 K1 V1 ..., or, where
-    // the tiles take a block each, K0 K1 V0 V1 K2 ....  Two are in flight.
-    const int w = warp - kDequantWarp, sub = lane >> 2, qd = lane & 3;
-    const int64_t head_rows = static_cast<int64_t>(kvh) * a.map.size.d;
-    const int end = sh.hi, operands = two ? 2 * nblk : (nblk + 1) / 2 * 4;
-    struct Buffer {
-      int64_t row[4];  // of the operand that is loaded next
-      uint4 c[4];
-      uint32_t s[4], here;
-    };
-    const auto is_v = [&](int q) { return (two ? q : q >> 1) & 1; };
-    const auto block = [&](int q) { return two ? q >> 1 : (q >> 2) * 2 + (q & 1); };
-    const auto find = [&](Buffer& f, int q) {
+    // each, so a warp's load covers 8 keys' rows; four turns an operand.  One
+    // warpgroup takes all K, the other all V; where the tiles take a block each,
+    // the even and the odd blocks.  The next operand is in flight, the rows of the
+    // one after it are known.
+    const int wg = (warp >> 2) & 1, w = warp & 3, sub = lane >> 2, qd = lane & 3;
+    const int end = sh.hi, operands = two ? nblk : (nblk + 1 - wg) / 2 * 2;
+    const auto is_v = [&](int q) { return two ? wg : q & 1; };
+    const auto block = [&](int q) { return two ? q : (q & ~1) + wg; };
+    const int64_t base_row =
+        (static_cast<int64_t>(a.map.table ? 0 : sh.tile.b) * a.map.hkv + kvh) * a.map.size.d;  // contiguous: of token 0
+    const int64_t page_rows = static_cast<int64_t>(a.map.hkv) * a.map.size.d;
+    int64_t row[4];  // of the operand that is loaded next; -1: none
+    uint4 codes[4];
+    uint32_t scales[4], here = 0;
+    const auto find = [&](int q) {
+      const int t0 = t_base + block(q) * kBlock + w * 8 + sub;  // >= 0
+      const int stop = q < operands && block(q) < nblk ? end : 0;
+      if (!a.map.table) {
 #pragma unroll
-      for (int it = 0; it < 4; ++it) {
-        const int t = t_base + block(q) * kBlock + it * 32 + w * 8 + sub;
-        f.row[it] = q < operands && block(q) < nblk && t < end ? a.map.row(sh.tile.b, t) : -1;
+        for (int it = 0; it < 4; ++it) row[it] = t0 + it * 32 < stop ? base_row + t0 + it * 32 : -1;
+      } else {
+        const int32_t* table = a.map.table + static_cast<uint64_t>(sh.tile.b) * a.map.per_seq;
+        uint32_t off[4];
+        int32_t page[4];
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          const uint32_t t = t0 + it * 32, i = a.map.size.div(t);
+          off[it] = t - i * a.map.size.d;
+          page[it] = t0 + it * 32 < stop ? __ldg(table + i) : -1;
+        }
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+          row[it] = static_cast<uint32_t>(page[it]) < a.map.pages
+                        ? page[it] * page_rows + base_row + off[it] : -1;
       }
     };
-    const auto load = [&](Buffer& f, int q) {
-      const uint8_t* codes = is_v(q) ? a.map.v_codes : a.map.k_codes;
-      const uint8_t* scales = is_v(q) ? a.map.v_scales : a.map.k_scales;
-      f.here = 0;
+    const auto load = [&](int q) {
+      const uint8_t* c = is_v(q) ? a.map.v_codes : a.map.k_codes;
+      const uint8_t* s = is_v(q) ? a.map.v_scales : a.map.k_scales;
+      here = 0;
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
-        const int64_t at = f.row[it] + head_rows;
-        const bool ok = f.row[it] >= 0;
-        f.c[it] = ok ? __ldg(reinterpret_cast<const uint4*>(codes + at * 64) + qd) : make_uint4(0, 0, 0, 0);
-        f.s[it] = ok ? __ldg(reinterpret_cast<const uint16_t*>(scales + at * 8) + qd) : 0u;
-        f.here |= ok ? 1u << it : 0u;
+        const bool ok = row[it] >= 0;
+        codes[it] = ok ? __ldg(reinterpret_cast<const uint4*>(c + row[it] * 64) + qd) : make_uint4(0, 0, 0, 0);
+        scales[it] = ok ? __ldg(reinterpret_cast<const uint16_t*>(s + row[it] * 8) + qd) : 0u;
+        here |= ok ? 1u << it : 0u;
       }
     };
-    const auto store = [&](const Buffer& f, uint32_t base, bool bf16) {
+    const auto store = [&](uint32_t base, bool bf16) {
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
         const uint32_t rr = it * 32 + w * 8 + sub;
-        const uint32_t g = kv_scales16<kE1M2>(f.s[it]);
+        const uint32_t g = kv_scales16<kE1M2>(scales[it]);
         const uint32_t g0 = __byte_perm(g, g, 0x1010), g1 = __byte_perm(g, g, 0x3232);
         // Lanes of the second 64 channels start with their other pair of words, so
         // that eight lanes' chunks meet eight different bank groups.
         const bool sw = qd & 2;
-        const uint32_t words[4] = {sw ? f.c[it].z : f.c[it].x, sw ? f.c[it].w : f.c[it].y, sw ? f.c[it].x : f.c[it].z,
-                                   sw ? f.c[it].y : f.c[it].w};
+        const uint32_t words[4] = {sw ? codes[it].z : codes[it].x, sw ? codes[it].w : codes[it].y,
+                                   sw ? codes[it].x : codes[it].z, sw ? codes[it].y : codes[it].w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           uint32_t e[4];
@@ -623,41 +642,36 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       }
     };
     // False: a wait ran out.
-    const auto operand = [&](Buffer& f, int q) {
+    const auto operand = [&](int q) {
       const int j = block(q), st = j & 1;
-      if (j >= nblk) return true;
       if (!__all_sync(0xffffffffu, mbar_wait_bounded(is_v(q) ? &sh.v_empty[st] : &sh.k_empty[st], ((j >> 1) & 1) ^ 1, &sh.abort)))
         return false;
       if (is_v(q)) {
-        store(f, smem + kOffV + st * kOperand, kFull);
+        store(smem + kOffV + st * kOperand, kFull);
       } else {
         // Which keys are there: byte it * 4 + w has this warp's 8 keys of turn it.
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
-          uint32_t v = __ballot_sync(0xffffffffu, qd == 0 && ((f.here >> it) & 1u));  // bits 0, 4, 8, ...
+          uint32_t v = __ballot_sync(0xffffffffu, qd == 0 && ((here >> it) & 1u));  // bits 0, 4, 8, ...
           v = (v | v >> 3) & 0x03030303u;
           v = (v | v >> 6) & 0x000F000Fu;
           v = (v | v >> 12) & 0xFFu;
           if (lane == 0) reinterpret_cast<uint8_t*>(sh.present[j & 3])[it * 4 + w] = static_cast<uint8_t>(v);
         }
-        store(f, smem + kOffK + st * kOperand, false);
+        store(smem + kOffK + st * kOperand, false);
       }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(is_v(q) ? &sh.v_full[st] : &sh.k_full[st]);
-      load(f, q + 2);
-      find(f, q + 4);
+      load(q + 1);
+      find(q + 2);
       return true;
     };
-    Buffer f0, f1;
-    find(f0, 0);
-    find(f1, 1);
-    load(f0, 0);
-    load(f1, 1);
-    find(f0, 2);
-    find(f1, 3);
-    for (int q = 0; q < operands; q += 2)
-      if (!operand(f0, q) || !operand(f1, q + 1)) {
+    find(0);
+    load(0);
+    find(1);
+    for (int q = 0; q < operands; ++q)
+      if (!operand(q)) {
         if (lane == 0 && !sh.abort) {
           set_status(a.status, NVFP4_ERR_TIMEOUT);
           sh.abort = 1;
@@ -665,8 +679,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
         break;
       }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+    if (warp < kMmaWarp + 2) {
       // --------------------------------------------------------------- MMA ---
       // The warp stays converged, so that descriptors live in uniform registers;
       // one lane issues.
@@ -682,51 +696,54 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       };
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
       // Step v of tile t: half v & 1 of its block v >> 1.
-      const auto block_of = [&](int t, int v) { return two ? v >> 1 : (v & ~1) + t; };
-      auto qk = [&](int t, int v) {
-        const int j = block_of(t, v), st = j & 1, hf = v & 1;
-        if (!wait(&sh.k_full[st], j >> 1)) return;
+      const int t = warp - kMmaWarp, subs = subs_of[t];
+      const uint32_t s_tile = tm + t * 128, o_tile = tm + 256 + t * 128;
+      const auto block_of = [&](int v) { return two ? v >> 1 : (v & ~1) + t; };
+      // A buffer is free when both tiles are done with it, or the one that has it.
+      const auto release = [&](uint64_t* bar) {
+        commit(bar);
+        if (!two) commit(bar);
+      };
+      const auto qk = [&](int v) {
+        const int j = block_of(v), st = j & 1, hf = v & 1;
+        if (!hf && !wait(&sh.k_full[st], j >> 1)) return;
         const uint32_t q = operand_desc(smem + (two ? t : 0) * kOperand), k = operand_desc(smem + kOffK + st * kOperand + hf * 8192);
         if (leader) {
 #pragma unroll
           for (int s = 0; s < 8; ++s) {
             const uint32_t at = ((s >> 2) * (kOperand / 2) + (s & 3) * 32) >> 4;
-            mma_ss(tm + t * 128 + hf * 64, q + at, k + at, kIdescQK, s != 0);
+            mma_ss(s_tile + hf * 64, q + at, k + at, kIdescQK, s != 0);
           }
           tc_commit(&sh.s_full[t][hf]);
         }
-        if (hf && (!two || t == 1)) commit(&sh.k_empty[st]);
+        if (hf) release(&sh.k_empty[st]);
       };
-      auto pv = [&](int t, int v) {
-        const int j = block_of(t, v), st = j & 1, hf = v & 1;
-        if (!wait(&sh.v_full[st], j >> 1) || !wait(&sh.p_full[t][hf], v >> 1)) return;
-        const uint32_t vd = operand_desc(smem + kOffV + st * kOperand + hf * 8192), p = tm + t * 128 + hf * 64;
+      const auto pv = [&](int v) {
+        const int j = block_of(v), st = j & 1, hf = v & 1;
+        if (!hf && !wait(&sh.v_full[st], j >> 1)) return;
+        if (!wait(&sh.p_full[t][hf], v >> 1)) return;
+        const uint32_t vd = operand_desc(smem + kOffV + st * kOperand + hf * 8192), p = s_tile + hf * 64;
         if (leader) {
 #pragma unroll
           for (int s = 0; s < (kFull ? 8 : 4); ++s)
-            mma_ts(tm + 256 + t * 128, p + s * 8, vd + (((s & 3) * 2048) >> 4), kFull ? kIdescPVFull : kIdescPV,
-                   v != 0 || s != 0);
+            mma_ts(o_tile, p + s * 8, vd + (((s & 3) * 2048) >> 4), kFull ? kIdescPVFull : kIdescPV, v != 0 || s != 0);
           tc_commit(&sh.o_done[t]);
         }
-        if (hf && (!two || t == 1)) commit(&sh.v_empty[st]);
+        if (hf) release(&sh.v_empty[st]);
       };
       wait(&sh.q_full, 0);
-      for (int v = 0; v < 2 && ok; ++v)
-        for (int t = 0; t < 2 && ok; ++t)
-          if (v < subs_of[t]) qk(t, v);
-      for (int v = 0; v < subs_of[0] && ok; ++v)
-        for (int t = 0; t < 2 && ok; ++t)
-          if (v < subs_of[t]) {
-            pv(t, v);
-            if (ok && v + 2 < subs_of[t]) qk(t, v + 2);
-          }
+      for (int v = 0; v < 2 && v < subs && ok; ++v) qk(v);
+      for (int v = 0; v < subs && ok; ++v) {
+        pv(v);
+        if (ok && v + 2 < subs) qk(v + 2);
+      }
       if (!ok && leader && !sh.abort) {
         set_status(a.status, NVFP4_ERR_TIMEOUT);
         sh.abort = 1;
       }
       // Nothing that was issued, MMA or arrival, outlives the CTA.
-      commit(&sh.drain);
-      mbar_wait_bounded(&sh.drain, 0, nullptr, kDrainLimitNs);
+      commit(&sh.drain[t]);
+      mbar_wait_bounded(&sh.drain[t], 0, nullptr, kDrainLimitNs);
       __syncwarp();
     }
   }
