@@ -202,11 +202,15 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* u) {
       : "memory");
 }
 // Two fp32 lanes at once: (x, y) = (x, y) * m + b, and (x, y) += (u, v).
-__device__ __forceinline__ void fma2(float& x, float& y, float m, float b) {
-  asm("{\n .reg .b64 v, w, z;\n mov.b64 v, {%0, %1};\n mov.b64 w, {%2, %2};\n mov.b64 z, {%3, %3};\n"
-      " fma.rn.f32x2 v, v, w, z;\n mov.b64 {%0, %1}, v;\n}"
+__device__ __forceinline__ uint64_t both(float v) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(d) : "f"(v));
+  return d;
+}
+__device__ __forceinline__ void fma2(float& x, float& y, uint64_t m, uint64_t b) {
+  asm("{\n .reg .b64 v;\n mov.b64 v, {%0, %1};\n fma.rn.f32x2 v, v, %2, %3;\n mov.b64 {%0, %1}, v;\n}"
       : "+f"(x), "+f"(y)
-      : "f"(m), "f"(b));
+      : "l"(m), "l"(b));
 }
 __device__ __forceinline__ void add2(float& x, float& y, float u, float v) {
   asm("{\n .reg .b64 a, b;\n mov.b64 a, {%0, %1};\n mov.b64 b, {%2, %3};\n add.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}"
@@ -230,6 +234,29 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
   return v;
 }
 
+// mbar_wait_bounded with a hint of how long the hardware may suspend the thread,
+// so that waiting warps leave the issue slots to the others.
+__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  const uint32_t addr = smem_u32(bar);
+  const auto once = [&] {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n"
+        " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+        " selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(addr), "r"(parity), "r"(100000u)
+        : "memory");
+    return ok != 0;
+  };
+  if (once()) return true;
+  const uint64_t t0 = globaltimer_ns();
+  while (!once()) {
+    if (*abort || globaltimer_ns() - t0 > kWaitLimitNs) return false;
+  }
+  return true;
+}
+
 struct TileShared {
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2][2], p_full[2][2], o_done[2], q_full, drain[2];
   uint32_t tmem;
@@ -242,23 +269,19 @@ struct TileShared {
   volatile int abort;
 };
 
-// 32 scores of a row in place -> log2 domain, keys outside `mask` hidden.
-template <bool kMods>
-__device__ __forceinline__ void score32(float* s, const RowScore& rs, const ExtendArgs& a, int p_minus_t0, uint32_t mask) {
-  if (kMods) {
-    const float in = rs.mult * (a.cap > 0.0f ? 2.0f / a.cap : 1.0f);  // cap: 2 log2(e) s / c
-    const float out = a.cap * kLog2e;
+// 32 scores of a row, capped and biased, in the log2 domain.
+__device__ __forceinline__ void score32(float* s, const RowScore& rs, const ExtendArgs& a, int p_minus_t0) {
+  if (a.cap > 0.0f) {
+    const float in = rs.mult * (2.0f / a.cap), out = a.cap * kLog2e;  // 2 log2(e) s / c
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      float x = s[i] * in;
-      if (a.cap > 0.0f) x = out - 2.0f * out * rcp(1.0f + ex2(x));
-      s[i] = fmaf(-rs.slope, fabsf(static_cast<float>(p_minus_t0 - i)), x);
-    }
+    for (int i = 0; i < 32; ++i) s[i] = fmaf(-2.0f * out, rcp(1.0f + ex2(s[i] * in)), out);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s[i] *= rs.mult;
   }
-  if (mask != 0xffffffffu) {
+  if (a.slopes) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (!((mask >> i) & 1u)) s[i] = -INFINITY;
+    for (int i = 0; i < 32; ++i) s[i] = fmaf(-rs.slope, fabsf(static_cast<float>(p_minus_t0 - i)), s[i]);
   }
 }
 
@@ -393,27 +416,34 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     const int all_lo = __reduce_max_sync(0xffffffffu, live ? vis.x : 0);
     const int all_hi = __reduce_min_sync(0xffffffffu, live ? vis.y : 0x7fffffff);
     const float to_log2 = kMods ? 1.0f : rs.mult;
+    const uint64_t to_log2x2 = both(to_log2);
     float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
     bool ok = true;
     for (int v = 0; v < subs; ++v) {
       const int j = two ? v >> 1 : (v & ~1) + t, hf = v & 1, t0 = t_base + j * kBlock + 64 * hf;
       const uint32_t s_col = s_tile + 64 * hf;
-      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.s_full[t][hf], (v >> 1) & 1, &sh.abort));
+      ok = __all_sync(0xffffffffu, wait_bar(&sh.s_full[t][hf], (v >> 1) & 1, &sh.abort));
       if (!ok) break;
       tc_fence_after();
       const uint2 pres = *reinterpret_cast<const uint2*>(&sh.present[j & 3][2 * hf]);
-      const bool open = t0 >= all_lo && t0 + 64 <= all_hi && (pres.x & pres.y) == 0xffffffffu;
       // The row's scores, all in registers, and their maximum.
       float s[64];
       tmem_ld32(s_col, s);
       tmem_ld32(s_col + 32, s + 32);
       tmem_wait_ld();
+      if (kMods) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int a0 = max(vis.x - (t0 + 32 * c), 0), a1 = min(vis.y - (t0 + 32 * c), 32);
-        const uint32_t mask = open ? 0xffffffffu
-                                   : a1 > a0 ? (c ? pres.y : pres.x) & (0xffffffffu << a0) & (0xffffffffu >> (32 - a1)) : 0u;
-        score32<kMods>(s + 32 * c, rs, a, p - t0 - 32 * c, mask);
+        for (int k = 0; k < 64; k += 32) score32(s + k, rs, a, p - t0 - k);
+      }
+      if (t0 < all_lo || t0 + 64 > all_hi || (pres.x & pres.y) != 0xffffffffu) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int a0 = max(vis.x - (t0 + 32 * c), 0), a1 = min(vis.y - (t0 + 32 * c), 32);
+          const uint32_t mask = a1 > a0 ? (c ? pres.y : pres.x) & (0xffffffffu << a0) & (0xffffffffu >> (32 - a1)) : 0u;
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (!((mask >> k) & 1u)) s[32 * c + k] = -INFINITY;
+        }
       }
       float tops[4];
 #pragma unroll
@@ -430,7 +460,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
         l0 *= shrink;
         l1 *= shrink;
         if (v > 0) {
-          ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.o_done[t], (v - 1) & 1, &sh.abort));
+          ok = __all_sync(0xffffffffu, wait_bar(&sh.o_done[t], (v - 1) & 1, &sh.abort));
           if (!ok) break;
           tc_fence_after();
 #pragma unroll 1
@@ -445,7 +475,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
           }
         }
       }
-      const float minus = (m == -INFINITY ? 0.0f : -m) + kWeightLog2;
+      const uint64_t minus = both((m == -INFINITY ? 0.0f : -m) + kWeightLog2);
       // The weights, over the scores they came from.
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -453,7 +483,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           float x = s[32 * c + 2 * k], y = s[32 * c + 2 * k + 1];
-          fma2(x, y, to_log2, minus);
+          fma2(x, y, to_log2x2, minus);
           x = ex2(x);
           y = ex2(y);
           add2(l0, l1, x, y);
@@ -473,10 +503,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.p_full[t][hf]);
     }
-    // S of the last step says that PV of the step three back is done; the last
-    // two phases of o_done are waited for in turn.
-    for (int v = max(subs - 2, 0); v < subs && ok; ++v) {
-      ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.o_done[t], v & 1, &sh.abort));
+    // The tile's last MMA.  (Not by o_done, whose last two phases may both have
+    // passed by now, which a parity does not tell from none.)
+    if (ok && subs > 0) {
+      ok = __all_sync(0xffffffffu, wait_bar(&sh.drain[t], 0, &sh.abort));
       tc_fence_after();
     }
     if (!ok && lane == 0 && !sh.abort) {
@@ -581,73 +611,73 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     const int64_t base_row =
         (static_cast<int64_t>(a.map.table ? 0 : sh.tile.b) * a.map.hkv + kvh) * a.map.size.d;  // contiguous: of token 0
     const int64_t page_rows = static_cast<int64_t>(a.map.hkv) * a.map.size.d;
-    int64_t row[4];  // of the operand that is loaded next; -1: none
+    // Of the operand that is loaded next: the page (contiguous: 0) and the row in it.
+    uint32_t page[4], off[4];
     uint4 codes[4];
     uint32_t scales[4], here = 0;
+    constexpr uint32_t kNone = 0xffffffffu;
+    const uint32_t pages = a.map.table ? a.map.pages : 1u;
     const auto find = [&](int q) {
       const int t0 = t_base + block(q) * kBlock + w * 8 + sub;  // >= 0
       const int stop = q < operands && block(q) < nblk ? end : 0;
-      if (!a.map.table) {
+      const int32_t* table = a.map.table + static_cast<uint64_t>(sh.tile.b) * a.map.per_seq;
 #pragma unroll
-        for (int it = 0; it < 4; ++it) row[it] = t0 + it * 32 < stop ? base_row + t0 + it * 32 : -1;
-      } else {
-        const int32_t* table = a.map.table + static_cast<uint64_t>(sh.tile.b) * a.map.per_seq;
-        uint32_t off[4];
-        int32_t page[4];
-#pragma unroll
-        for (int it = 0; it < 4; ++it) {
-          const uint32_t t = t0 + it * 32, i = a.map.size.div(t);
-          off[it] = t - i * a.map.size.d;
-          page[it] = t0 + it * 32 < stop ? __ldg(table + i) : -1;
+      for (int it = 0; it < 4; ++it) {
+        off[it] = t0 + it * 32;
+        page[it] = t0 + it * 32 < stop ? 0u : kNone;
+        if (a.map.table && page[it] == 0u) {
+          const uint32_t i = a.map.size.div(off[it]);
+          off[it] -= i * a.map.size.d;
+          page[it] = static_cast<uint32_t>(__ldg(table + i));
         }
-#pragma unroll
-        for (int it = 0; it < 4; ++it)
-          row[it] = static_cast<uint32_t>(page[it]) < a.map.pages
-                        ? page[it] * page_rows + base_row + off[it] : -1;
       }
     };
     const auto load = [&](int q) {
-      const uint8_t* c = is_v(q) ? a.map.v_codes : a.map.k_codes;
-      const uint8_t* s = is_v(q) ? a.map.v_scales : a.map.k_scales;
+      const uint8_t* c = (is_v(q) ? a.map.v_codes : a.map.k_codes) + base_row * 64 + 16 * qd;
+      const uint8_t* s = (is_v(q) ? a.map.v_scales : a.map.k_scales) + base_row * 8 + 2 * qd;
       here = 0;
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
-        const bool ok = row[it] >= 0;
-        codes[it] = ok ? __ldg(reinterpret_cast<const uint4*>(c + row[it] * 64) + qd) : make_uint4(0, 0, 0, 0);
-        scales[it] = ok ? __ldg(reinterpret_cast<const uint16_t*>(s + row[it] * 8) + qd) : 0u;
+        const bool ok = page[it] < pages;
+        const int64_t row = page[it] * page_rows + off[it];
+        codes[it] = ok ? __ldg(reinterpret_cast<const uint4*>(c + row * 64)) : make_uint4(0, 0, 0, 0);
+        scales[it] = ok ? __ldg(reinterpret_cast<const uint16_t*>(s + row * 8)) : 0u;
         here |= ok ? 1u << it : 0u;
       }
     };
-    const auto store = [&](uint32_t base, bool bf16) {
+    // Lanes of the second 64 channels start with their other pair of words, so that
+    // eight lanes' chunks meet eight different bank groups.
+    const bool sw = qd & 2;
+    uint32_t at[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) at[k] = smem + operand_chunk(w * 8 + sub, 4 * qd + (sw ? k ^ 2 : k));
+    const auto store = [&](uint32_t offset, bool bf16) {
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
-        const uint32_t rr = it * 32 + w * 8 + sub;
         const uint32_t g = kv_scales16<kE1M2>(scales[it]);
-        const uint32_t g0 = __byte_perm(g, g, 0x1010), g1 = __byte_perm(g, g, 0x3232);
-        // Lanes of the second 64 channels start with their other pair of words, so
-        // that eight lanes' chunks meet eight different bank groups.
-        const bool sw = qd & 2;
-        const uint32_t words[4] = {sw ? codes[it].z : codes[it].x, sw ? codes[it].w : codes[it].y,
-                                   sw ? codes[it].x : codes[it].z, sw ? codes[it].y : codes[it].w};
+        const uint32_t g0 = __byte_perm(g, g, sw ? 0x3232 : 0x1010), g1 = __byte_perm(g, g, sw ? 0x1010 : 0x3232);
+        const uint4 v = codes[it];
+        const uint32_t words[4] = {sw ? v.z : v.x, sw ? v.w : v.y, sw ? v.x : v.z, sw ? v.y : v.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           uint32_t e[4];
           elements8<kE1M2>(words[k], e);
-          const uint32_t gk = (k < 2) != sw ? g0 : g1;
-          const uint32_t chunk = 4 * qd + (sw ? k ^ 2 : k);
 #pragma unroll
-          for (int x = 0; x < 4; ++x) e[x] = bf16 ? bf16x2_of_f16x2(mul_f16x2(e[x], gk)) : mul_f16x2(e[x], gk);
-          sts128(base + operand_chunk(rr, chunk), e[0], e[1], e[2], e[3]);
+          for (int x = 0; x < 4; ++x) {
+            e[x] = mul_f16x2(e[x], k < 2 ? g0 : g1);
+            if (bf16) e[x] = bf16x2_of_f16x2(e[x]);
+          }
+          sts128(at[k] + offset + it * 4096, e[0], e[1], e[2], e[3]);  // 32 rows of 128 bytes further
         }
       }
     };
     // False: a wait ran out.
     const auto operand = [&](int q) {
       const int j = block(q), st = j & 1;
-      if (!__all_sync(0xffffffffu, mbar_wait_bounded(is_v(q) ? &sh.v_empty[st] : &sh.k_empty[st], ((j >> 1) & 1) ^ 1, &sh.abort)))
+      if (!__all_sync(0xffffffffu, wait_bar(is_v(q) ? &sh.v_empty[st] : &sh.k_empty[st], ((j >> 1) & 1) ^ 1, &sh.abort)))
         return false;
       if (is_v(q)) {
-        store(smem + kOffV + st * kOperand, kFull);
+        store(kOffV + st * kOperand, kFull);
       } else {
         // Which keys are there: byte it * 4 + w has this warp's 8 keys of turn it.
 #pragma unroll
@@ -658,7 +688,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
           v = (v | v >> 12) & 0xFFu;
           if (lane == 0) reinterpret_cast<uint8_t*>(sh.present[j & 3])[it * 4 + w] = static_cast<uint8_t>(v);
         }
-        store(smem + kOffK + st * kOperand, false);
+        store(kOffK + st * kOperand, false);
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -687,7 +717,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       const bool leader = elect_one();
       bool ok = true;
       auto wait = [&](uint64_t* bar, int phase) {
-        ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1, &sh.abort));
+        ok = ok && __all_sync(0xffffffffu, wait_bar(bar, phase & 1, &sh.abort));
         tc_fence_after();
         return ok;
       };
