@@ -1,8 +1,6 @@
 // Attention of new tokens (one, a few, a chunk, a whole prompt) over the 4-bit
 // cache that already holds them, contiguous or paged: scores optionally capped
 // and biased by distance, keys limited by causality, window, prefix, document.
-#include <type_traits>
-
 #include "kv_pages.cuh"
 
 namespace nvfp4 {
@@ -785,35 +783,499 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
   }
 }
 
+// ---- few rows: registers --------------------------------------------------
+// HBM-bound work: every byte of K and V is needed once for a handful of rows.  A
+// CTA takes 8 kN rows and a range of keys.  Warp 0 streams the keys' codes and
+// scales into a two-stage ring of 128 keys; four warps take two 16-key tiles of a
+// stage each, dequantize in registers (exact in f16) and multiply with mma.sync
+// m16n8k16: S^T[16 keys, 8 rows] = K Q^T, O^T[128, 8 rows] += V^T P^T, for each of
+// the kN groups of rows.  (tcgen05 would take a 128-row operand for these few, and
+// K and V through shared memory: 64 x 16384 ragged tokens 381 us by the tiles.)
+//
+// Lane roles (g = lane / 4, t = lane % 4), as the fragments have them:
+//   K rows g and g + 8 of the tile, channels 32t..32t+31; V rows 2t, 2t+1, 2t+8,
+//   2t+9, channels 16g..16g+15; Q row g of a group, channels 32t..32t+31.
+// Row m of a 16-key tile is key (m & 1) * 4 + (m >> 1 & 3) + (m & 8), so that a V
+// load covers four consecutive keys.
+constexpr int kRowsWarps = 4;
+constexpr int kRowsThreads = 32 * (1 + kRowsWarps);
+constexpr int kRing = 2;
+constexpr uint32_t kStageCodes = kBlock * 64, kStageBytes = 2 * kBlock * (64 + 8);  // K, V codes, K, V scales
+constexpr int kMergeRow = 148;  // floats of a row's 128 channels in the merge buffer: 2 of padding per 16
+
+__device__ __forceinline__ int tile_key(int m) { return (m & 1) * 4 + ((m >> 1) & 3) + (m & 8); }
+__device__ __forceinline__ void mma16816(float c[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+// The eight elements of a code word as pairs.  E2M1: (0,1) (2,3) (4,5) (6,7).
+// E1M2: (0,4) (1,5) (2,6) (3,7), the second and fourth pair times 16 (a nibble in
+// bits 4-7 is decoded where it stands); their scales carry the 1/16.
+template <bool kE1M2>
+__device__ __forceinline__ void pairs8(uint32_t w, uint32_t e[4]) {
+  if (kE1M2) {
+    const uint32_t t = w >> 8;
+    e[0] = sub_f16x2((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
+    e[1] = sub_f16x2((w & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
+    e[2] = sub_f16x2((t & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
+    e[3] = sub_f16x2((t & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
+  } else {
+    elements8<false>(w, e);
+  }
+}
+
+template <int kN>
+struct RowsShared {
+  uint64_t full[kRing], empty[kRing];
+  uint32_t present[kRing][4];
+  Tile tile;
+  Seq seq;
+  int lo, hi;
+  float m[kRowsWarps][8 * kN], l[kRowsWarps][8 * kN];
+  uint2 q[kN > 1 ? kN : 1][8][32];  // Q fragments by group, k-step, lane (one group: in registers)
+  volatile int abort;
+};
+constexpr uint32_t kRowsSmem = kRing * kStageBytes + kRowsWarps * 8 * kMergeRow * 4;
+
+template <int kN, bool kE1M2, bool kMods>
+__global__ void __launch_bounds__(kRowsThreads, kN == 1 ? 4 : kN == 2 ? 3 : 2) extend_rows_kernel(const ExtendArgs a) {
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  __shared__ RowsShared<kN> sh;
+  constexpr uint32_t kRows = 8 * kN;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(&sh.full[i], 1 + 32);  // the armed bytes, and each lane's own copies
+      mbar_init(&sh.empty[i], kRowsWarps);
+    }
+    sh.abort = 0;
+    fence_mbar_init();
+  }
+  griddep_wait_and_release();
+  const uint32_t split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
+  const uint32_t tile_id = rest / a.map.hkv, kvh = rest - tile_id * a.map.hkv, group = a.group.d;
+  if (warp == 0) {
+    const Tile tl = find_tile<kRows>(a, tile_id);
+    Seq sq = {0, 0, 0};
+    if (tl.b < a.map.batch) sq = sequence(a, tl.b);
+    // The keys that the tile's rows see.
+    int lo = 0x7fffffff, hi = 0;
+    const uint32_t rows = tl.b < a.map.batch ? min(sq.n * group - tl.row0, kRows) : 0;
+    if (lane < static_cast<int>(rows)) {
+      const uint32_t tok = a.group.div(tl.row0 + lane);
+      const int p = sq.len - static_cast<int>(sq.n) + static_cast<int>(tok);
+      const int2 vis = visible(a, p, sq.len, a.prefix_lens ? __ldg(a.prefix_lens + tl.b) : 0,
+                               a.doc_start ? __ldg(a.doc_start + sq.first + tok) : 0);
+      if (p >= 0 && vis.x < vis.y) {
+        lo = vis.x;
+        hi = vis.y;
+      }
+    }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (lane == 0) {
+      sh.tile = tl;
+      sh.seq = sq;
+      sh.lo = hi > lo ? lo : 0;
+      sh.hi = hi > lo ? hi : 0;
+    }
+  }
+  __syncthreads();
+  const Tile tile = sh.tile;
+  if (tile.b >= a.map.batch) return;  // more CTAs than tiles
+  const Seq seq = sh.seq;
+  const uint32_t rows = min(seq.n * group - tile.row0, kRows);
+  // This CTA's keys, in whole stages from the tile's first.
+  const int stages = (sh.hi - sh.lo + kBlock - 1) / kBlock;
+  const int per = (stages + static_cast<int>(a.splits) - 1) / static_cast<int>(a.splits);
+  const int s0 = min(static_cast<int>(split) * per, stages), n = min(per, stages - s0);
+  const int t_base = sh.lo + s0 * kBlock, t_end = min(sh.hi, t_base + n * kBlock);
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ producer ---
+    // Lane i has keys i, i + 32, i + 64, i + 96 of a stage.  Codes come by bulk
+    // copies, one for each run of keys within a page; scales, 8 bytes a key, by
+    // the lane's own copies.  A key that is not there (past the end, or its page
+    // absent) gets scales of zero, whatever its codes' bytes.
+    const int64_t head = static_cast<int64_t>(kvh) * a.map.size.d;
+    for (int i = 0; i < n; ++i) {
+      const int st = i & 1, t0 = t_base + i * kBlock;
+      int64_t row[4];
+      uint32_t here[4], total = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int t = t0 + 32 * k + lane;
+        row[k] = t < t_end ? a.map.row(tile.b, t) : -1;
+        here[k] = __ballot_sync(0xffffffffu, row[k] >= 0);
+        total += __popc(here[k]);
+      }
+      if (!__all_sync(0xffffffffu, wait_bar(&sh.empty[st], ((i >> 1) & 1) ^ 1, &sh.abort))) {
+        if (lane == 0 && !sh.abort) {
+          set_status(a.status, NVFP4_ERR_TIMEOUT);
+          sh.abort = 1;
+        }
+        break;
+      }
+      uint8_t* stage = smem_raw + st * kStageBytes;
+      uint8_t* scales = stage + 2 * kStageCodes;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (row[k] < 0) {
+          reinterpret_cast<uint2*>(scales)[32 * k + lane] = make_uint2(0, 0);
+          reinterpret_cast<uint2*>(scales + kBlock * 8)[32 * k + lane] = make_uint2(0, 0);
+        }
+      if (lane < 4) sh.present[st][lane] = lane == 0 ? here[0] : lane == 1 ? here[1] : lane == 2 ? here[2] : here[3];
+      __syncwarp();
+      if (lane == 0) mbar_arrive_expect_tx(&sh.full[st], total * 128);
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = 32 * k + lane;
+        if (row[k] < 0) continue;
+        const int64_t at = row[k] + head;
+        const uint32_t off = static_cast<uint32_t>(a.map.table ? (t0 + c) - static_cast<int>(a.map.size.div(t0 + c)) * static_cast<int>(a.map.size.d) : t0 + c);
+        if (c == 0 || off == 0) {  // a run of keys begins
+          const int len = min(min(static_cast<int>(a.map.size.d - off), kBlock - c), t_end - (t0 + c));
+          bulk_load(stage + c * 64, a.map.k_codes + at * 64, len * 64, &sh.full[st]);
+          bulk_load(stage + kStageCodes + c * 64, a.map.v_codes + at * 64, len * 64, &sh.full[st]);
+        }
+        const uint32_t to = smem_u32(scales + c * 8);
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(a.map.k_scales + at * 8) : "memory");
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to + kBlock * 8), "l"(a.map.v_scales + at * 8) : "memory");
+      }
+      asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.full[st])) : "memory");
+    }
+    // Copies in flight land before the CTA's memory goes to another (its
+    // consumers have waited for them unless a wait ran out).
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (sh.abort)
+      for (int i = max(n - 2, 0); i < n; ++i) mbar_wait_bounded(&sh.full[i & 1], (i >> 1) & 1, nullptr, kDrainLimitNs);
+    return;
+  }
+
+  // ------------------------------------------------------------- consumers ---
+  const int cw = warp - 1, g = lane >> 2, t = lane & 3;
+  // Rows of the lane's columns in a group's tile of scores: 2t and 2t + 1.
+  int2 vis[kN][2];
+  float mult[kN][2], slope[kN][2];
+  int pos[kN][2];
+  int all_lo = 0, all_hi = 0x7fffffff;  // keys that every row sees
+#pragma unroll
+  for (int x = 0; x < kN; ++x)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const uint32_t lr = 8 * x + 2 * t + c;
+      const bool live = lr < rows;
+      const uint32_t r = tile.row0 + (live ? lr : 0), tok = a.group.div(r), h = kvh * group + (r - tok * group);
+      const int p = seq.len - static_cast<int>(seq.n) + static_cast<int>(tok);
+      vis[x][c] = visible(a, p, seq.len, a.prefix_lens ? __ldg(a.prefix_lens + tile.b) : 0,
+                          a.doc_start ? __ldg(a.doc_start + seq.first + tok) : 0);
+      if (!live || p < 0) vis[x][c] = make_int2(0x7fffffff, 0);
+      if (live) {
+        all_lo = max(all_lo, vis[x][c].x);
+        all_hi = min(all_hi, vis[x][c].y);
+      }
+      pos[x][c] = p;
+      slope[x][c] = kMods && a.slopes && live ? __ldg(a.slopes + h) * kLog2e : 0.0f;
+    }
+  all_lo = __reduce_max_sync(0xffffffffu, all_lo);
+  all_hi = __reduce_min_sync(0xffffffffu, all_hi);
+  // Queries: f16 after an exact scaling by a power of two to below 1.
+  uint32_t qf[16];
+#pragma unroll
+  for (int x = 0; x < kN; ++x) {
+    const uint32_t lr = 8 * x + g;
+    const bool live = lr < rows;
+    const uint32_t r = tile.row0 + (live ? lr : 0), tok = a.group.div(r);
+    const uint4* src = reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(seq.first + tok) * a.ld_q +
+                                                      (kvh * group + (r - tok * group)) * kD + 32 * t);
+    uint4 w[4];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = live ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+      top = max(top, amax_bits_bf16x8(w[i]));
+    }
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int e = max(-125, min(static_cast<int>(top >> 7) - 126, 126));
+    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+    const float up = a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+    mult[x][0] = __shfl_sync(0xffffffffu, up, (2 * t) * 4);
+    mult[x][1] = __shfl_sync(0xffffffffu, up, (2 * t + 1) * 4);
+    float v[32];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack_bf16x8(w[i], v + 8 * i);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      // Channels of k-step j, in the order of pairs8.
+      const int c0 = kE1M2 ? 8 * (j >> 1) + 2 * (j & 1) : 4 * j;
+      const int c1 = kE1M2 ? c0 + 4 : c0 + 1, c2 = kE1M2 ? c0 + 1 : c0 + 2, c3 = kE1M2 ? c0 + 5 : c0 + 3;
+      const uint2 f = make_uint2(f16x2_rn(v[c0] * down, v[c1] * down), f16x2_rn(v[c2] * down, v[c3] * down));
+      if (kN == 1) {
+        qf[2 * j] = f.x;
+        qf[2 * j + 1] = f.y;
+      } else if (cw == 0) {
+        sh.q[x][j][lane] = f;
+      }
+    }
+  }
+  if (kN > 1) asm volatile("bar.sync 1, %0;" ::"n"(32 * kRowsWarps) : "memory");
+
+  float o[kN][8][4], m_run[kN][2], l_run[kN][2];
+#pragma unroll
+  for (int x = 0; x < kN; ++x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[x][i][0] = o[x][i][1] = o[x][i][2] = o[x][i][3] = 0.0f;
+    m_run[x][0] = m_run[x][1] = -INFINITY;
+    l_run[x][0] = l_run[x][1] = 0.0f;
+  }
+  const int rk0 = tile_key(g), rk1 = tile_key(g + 8);
+  const int rv[4] = {tile_key(2 * t), tile_key(2 * t + 1), tile_key(2 * t + 8), tile_key(2 * t + 9)};
+  bool ok = true;
+  for (int i = 0; i < n; ++i) {
+    const int st = i & 1;
+    ok = __all_sync(0xffffffffu, wait_bar(&sh.full[st], (i >> 1) & 1, &sh.abort));
+    if (!ok) {
+      if (lane == 0 && !sh.abort) {
+        set_status(a.status, NVFP4_ERR_TIMEOUT);
+        sh.abort = 1;
+      }
+      break;
+    }
+    const uint8_t* stage = smem_raw + st * kStageBytes;
+    const uint8_t* k_scales = stage + 2 * kStageCodes;
+    const uint8_t* v_scales = k_scales + kBlock * 8;
+#pragma unroll(kN == 1 ? 2 : 1)
+    for (int sub = 0; sub < kBlock / (16 * kRowsWarps); ++sub) {
+      const int r0 = 16 * (cw + kRowsWarps * sub), t0 = t_base + i * kBlock + r0;
+      const uint32_t there = (sh.present[st][r0 >> 5] >> (r0 & 31)) & 0xFFFFu;
+      if (!there) continue;
+      // ---- S^T = K Q^T: 8 k-steps of 16 channels --------------------------
+      const uint4 ka = *reinterpret_cast<const uint4*>(stage + (r0 + rk0) * 64 + 16 * t);
+      const uint4 kb = *reinterpret_cast<const uint4*>(stage + (r0 + rk1) * 64 + 16 * t);
+      const uint32_t ksa = kv_scales16<kE1M2>(*reinterpret_cast<const uint16_t*>(k_scales + (r0 + rk0) * 8 + 2 * t));
+      const uint32_t ksb = kv_scales16<kE1M2>(*reinterpret_cast<const uint16_t*>(k_scales + (r0 + rk1) * 8 + 2 * t));
+      const uint32_t sa_lo = __byte_perm(ksa, ksa, 0x1010), sa_hi = __byte_perm(ksa, ksa, 0x3232);
+      const uint32_t sb_lo = __byte_perm(ksb, ksb, 0x1010), sb_hi = __byte_perm(ksb, ksb, 0x3232);
+      float s[kN][4];
+#pragma unroll
+      for (int x = 0; x < kN; ++x) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.0f;
+      const uint32_t kaw[4] = {ka.x, ka.y, ka.z, ka.w}, kbw[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t ha[4], hb[4];
+        pairs8<kE1M2>(kaw[w], ha);
+        pairs8<kE1M2>(kbw[w], hb);
+        const uint32_t sa = w < 2 ? sa_lo : sa_hi, sb = w < 2 ? sb_lo : sb_hi;
+        const uint32_t sa1 = kE1M2 ? mul_f16x2(sa, 0x2C002C00u) : sa, sb1 = kE1M2 ? mul_f16x2(sb, 0x2C002C00u) : sb;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t f[4] = {mul_f16x2(ha[2 * h], sa), mul_f16x2(hb[2 * h], sb), mul_f16x2(ha[2 * h + 1], sa1),
+                                 mul_f16x2(hb[2 * h + 1], sb1)};
+          const int j = 2 * w + h;
+#pragma unroll
+          for (int x = 0; x < kN; ++x) {
+            const uint2 b = kN == 1 ? make_uint2(qf[2 * j], qf[2 * j + 1]) : sh.q[x][j][lane];
+            mma16816(s[x], f, b.x, b.y);
+          }
+        }
+      }
+      // ---- scores, masks, the running maximum ------------------------------
+      const bool open = t0 >= all_lo && t0 + 16 <= all_hi && there == 0xFFFFu;
+      bool up = false;
+#pragma unroll
+      for (int x = 0; x < kN; ++x) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int key = t0 + (c < 2 ? rk0 : rk1), col = c & 1;
+          float v = s[x][c] * mult[x][col];
+          if (kMods) {
+            if (a.cap > 0.0f) {
+              const float out = a.cap * kLog2e;
+              v = fmaf(-2.0f * out, rcp(1.0f + ex2(v * (2.0f / a.cap))), out);
+            }
+            v = fmaf(-slope[x][col], fabsf(static_cast<float>(pos[x][col] - key)), v);
+          }
+          if (!open && (key < vis[x][col].x || key >= vis[x][col].y || !((there >> (key - t0)) & 1u))) v = -INFINITY;
+          s[x][c] = v;
+          up = up || v > m_run[x][col] + kRescaleLog2;
+        }
+      }
+      if (__any_sync(0xffffffffu, up)) {
+#pragma unroll
+        for (int x = 0; x < kN; ++x)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float top = fmaxf(s[x][c], s[x][c + 2]);
+#pragma unroll
+            for (int sh_ = 4; sh_ < 32; sh_ <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, sh_));
+            if (top > m_run[x][c] + kRescaleLog2) {
+              const float shrink = ex2(m_run[x][c] - top);
+              m_run[x][c] = top;
+              l_run[x][c] *= shrink;
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                o[x][k][c] *= shrink;
+                o[x][k][c + 2] *= shrink;
+              }
+            }
+          }
+      }
+      uint32_t pb[kN][2];
+#pragma unroll
+      for (int x = 0; x < kN; ++x) {
+        const float b0 = (m_run[x][0] == -INFINITY ? 0.0f : -m_run[x][0]) + kWeightLog2;
+        const float b1 = (m_run[x][1] == -INFINITY ? 0.0f : -m_run[x][1]) + kWeightLog2;
+        const float p0 = ex2(s[x][0] + b0), p1 = ex2(s[x][1] + b1), p2 = ex2(s[x][2] + b0), p3 = ex2(s[x][3] + b1);
+        l_run[x][0] += p0 + p2;
+        l_run[x][1] += p1 + p3;
+        pb[x][0] = transposed(f16x2_rn(p0, p1));
+        pb[x][1] = transposed(f16x2_rn(p2, p3));
+      }
+      // ---- O^T += V^T P^T: 8 m-tiles, m-tile k = channels 16g+2k, 16g+2k+1 --
+      const uint32_t vs01 = kv_scales16<kE1M2>(v_scales[(r0 + rv[0]) * 8 + g] | v_scales[(r0 + rv[1]) * 8 + g] << 8);
+      const uint32_t vs89 = kv_scales16<kE1M2>(v_scales[(r0 + rv[2]) * 8 + g] | v_scales[(r0 + rv[3]) * 8 + g] << 8);
+      const uint32_t vs01_hi = kE1M2 ? mul_f16x2(vs01, 0x2C002C00u) : vs01;
+      const uint32_t vs89_hi = kE1M2 ? mul_f16x2(vs89, 0x2C002C00u) : vs89;
+      uint2 vw[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) vw[k] = *reinterpret_cast<const uint2*>(stage + kStageCodes + (r0 + rv[k]) * 64 + 8 * g);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {  // channels 16g..16g+7, then the other eight
+        const uint32_t wa = half ? vw[0].y : vw[0].x, wb = half ? vw[1].y : vw[1].x;
+        const uint32_t wc = half ? vw[2].y : vw[2].x, wd = half ? vw[3].y : vw[3].x;
+        uint32_t lo_ab[4], hi_ab[4], lo_cd[4], hi_cd[4];
+        if (kE1M2) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {  // byte k of two keys: its low-nibble channel, and 16 times its high one
+            const uint32_t ab = __byte_perm(wa, wb, 0x4400u + 0x1111u * k), cd = __byte_perm(wc, wd, 0x4400u + 0x1111u * k);
+            lo_ab[k] = sub_f16x2((ab & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
+            hi_ab[k] = sub_f16x2((ab & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
+            lo_cd[k] = sub_f16x2((cd & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
+            hi_cd[k] = sub_f16x2((cd & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
+          }
+        } else {  // the same channel of two keys in one byte, the first key in its low nibble
+          elements8<false>((wa & 0x0F0F0F0Fu) | ((wb << 4) & 0xF0F0F0F0u), lo_ab);
+          elements8<false>(((wa >> 4) & 0x0F0F0F0Fu) | (wb & 0xF0F0F0F0u), hi_ab);
+          elements8<false>((wc & 0x0F0F0F0Fu) | ((wd << 4) & 0xF0F0F0F0u), lo_cd);
+          elements8<false>(((wc >> 4) & 0x0F0F0F0Fu) | (wd & 0xF0F0F0F0u), hi_cd);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t f[4] = {mul_f16x2(lo_ab[k], vs01), mul_f16x2(hi_ab[k], vs01_hi), mul_f16x2(lo_cd[k], vs89),
+                                 mul_f16x2(hi_cd[k], vs89_hi)};
+#pragma unroll
+          for (int x = 0; x < kN; ++x) mma16816(o[x][4 * half + k], f, pb[x][0], pb[x][1]);
+        }
+      }
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.empty[st]);
+  }
+
+  // ---- join the warps, one group of rows at a time -------------------------
+  float* merge = reinterpret_cast<float*>(smem_raw + kRing * kStageBytes);
+#pragma unroll
+  for (int x = 0; x < kN; ++x) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int s = 4; s < 32; s <<= 1) l_run[x][c] += __shfl_xor_sync(0xffffffffu, l_run[x][c], s);
+      if (g == 0) {
+        sh.m[cw][8 * x + 2 * t + c] = m_run[x][c];
+        sh.l[cw][8 * x + 2 * t + c] = l_run[x][c];
+      }
+    }
+    float* mine = merge + cw * 8 * kMergeRow;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int c = 18 * g + 2 * k;  // channels 16g + 2k and the next, 2 floats of padding per 16
+      *reinterpret_cast<float2*>(mine + (2 * t) * kMergeRow + c) = make_float2(o[x][k][0], o[x][k][2]);
+      *reinterpret_cast<float2*>(mine + (2 * t + 1) * kMergeRow + c) = make_float2(o[x][k][1], o[x][k][3]);
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kRowsWarps) : "memory");
+    const int left = min(8, static_cast<int>(rows) - 8 * x);
+    for (int idx = threadIdx.x - 32; idx < left * (kD / 4); idx += 32 * kRowsWarps) {
+      const int lr = idx / (kD / 4), c = idx % (kD / 4) * 4;
+      float big = -INFINITY, sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < kRowsWarps; ++w) big = fmaxf(big, sh.m[w][8 * x + lr]);
+#pragma unroll
+      for (int w = 0; w < kRowsWarps; ++w) {
+        const float mw = sh.m[w][8 * x + lr], f = mw == -INFINITY ? 0.0f : ex2(mw - big);
+        const float2* from = reinterpret_cast<const float2*>(merge + (w * 8 + lr) * kMergeRow + c + 2 * (c >> 4));
+        const float2 u = from[0], v = from[1];
+        sum = fmaf(f, sh.l[w][8 * x + lr], sum);
+        acc[0] = fmaf(f, u.x, acc[0]);
+        acc[1] = fmaf(f, u.y, acc[1]);
+        acc[2] = fmaf(f, v.x, acc[2]);
+        acc[3] = fmaf(f, v.y, acc[3]);
+      }
+      if (a.splits > 1) {
+        const uint64_t rec = ((static_cast<uint64_t>(tile_id) * a.map.hkv + kvh) * a.splits + split) * kRows + 8 * x + lr;
+        if (c == 0) a.ml_ws[rec] = make_float2(big, sum);
+        if (big != -INFINITY) *reinterpret_cast<float4*>(a.o_ws + rec * kD + c) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      } else {
+        const float f = sum > 0.0f ? a.gv / sum : 0.0f;
+        const uint32_t r = tile.row0 + 8 * x + lr, tok = a.group.div(r);
+        *reinterpret_cast<uint2*>(a.out + (static_cast<uint64_t>(seq.first + tok) * a.hq + kvh * group + r - tok * group) * kD + c) =
+            make_uint2(bf16x2_rn(acc[0] * f, acc[1] * f), bf16x2_rn(acc[2] * f, acc[3] * f));
+      }
+    }
+    if (x + 1 < kN) asm volatile("bar.sync 1, %0;" ::"n"(32 * kRowsWarps) : "memory");
+  }
+}
+
 // Joins the parts of a tile's rows in split order: one warp a row, four channels
-// a lane.  Rows of a tile are shared out over gridDim.z CTAs.
+// a lane, eight parts in flight.  Rows of a tile are shared out over gridDim.z
+// CTAs.
 template <int kRows>
 __global__ void __launch_bounds__(256) extend_combine_kernel(const ExtendArgs a) {
   griddep_wait_and_release();
-  const int lane = threadIdx.x & 31;
+  const uint32_t lane = threadIdx.x & 31;
   const Tile t = find_tile<kRows>(a, blockIdx.x);
   if (t.b >= a.map.batch) return;
   const Seq seq = sequence(a, t.b);
   const uint32_t rows = min(seq.n * a.group.d - t.row0, static_cast<uint32_t>(kRows)), kvh = blockIdx.y;
   for (uint32_t local = blockIdx.z * 8 + (threadIdx.x >> 5); local < rows; local += gridDim.z * 8) {
     const uint64_t rec = (static_cast<uint64_t>(blockIdx.x) * a.map.hkv + kvh) * a.splits * kRows + local;
-    float big = -INFINITY;
-    for (uint32_t s = lane; s < a.splits; s += 32) big = fmaxf(big, a.ml_ws[rec + static_cast<uint64_t>(s) * kRows].x);
+    const float2* ml = a.ml_ws + rec;
+    const float4* part = reinterpret_cast<const float4*>(a.o_ws + rec * kD) + lane;
+    float2 mine = lane < a.splits ? ml[static_cast<uint64_t>(lane) * kRows] : make_float2(-INFINITY, 0.0f);
+    float big = mine.x;
+    for (uint32_t s = lane + 32; s < a.splits; s += 32) big = fmaxf(big, ml[static_cast<uint64_t>(s) * kRows].x);
 #pragma unroll
     for (int sh = 16; sh; sh >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, sh));
     float sum = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (uint32_t s = 0; s < a.splits; ++s) {
-      const uint64_t at = rec + static_cast<uint64_t>(s) * kRows;
-      const float2 ml = a.ml_ws[at];
-      if (ml.x == -INFINITY) continue;
-      const float w = ex2(ml.x - big);
-      const float4 v = reinterpret_cast<const float4*>(a.o_ws + at * kD)[lane];
-      sum = fmaf(w, ml.y, sum);
-      o.x = fmaf(w, v.x, o.x);
-      o.y = fmaf(w, v.y, o.y);
-      o.z = fmaf(w, v.z, o.z);
-      o.w = fmaf(w, v.w, o.w);
+    for (uint32_t s0 = 0; s0 < a.splits; s0 += 32) {
+      if (s0) mine = s0 + lane < a.splits ? ml[static_cast<uint64_t>(s0 + lane) * kRows] : make_float2(-INFINITY, 0.0f);
+      const float w = mine.x == -INFINITY ? 0.0f : ex2(mine.x - big);  // an empty part has no O
+      for (uint32_t s = s0; s < min(s0 + 32, a.splits); s += 8) {
+        float4 v[8];
+        float f[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          f[k] = __shfl_sync(0xffffffffu, w, (s + k) & 31);
+          if (s + k >= a.splits) f[k] = 0.0f;
+          v[k] = f[k] != 0.0f ? part[static_cast<uint64_t>(s + k) * kRows * (kD / 4)] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          sum = fmaf(f[k], __shfl_sync(0xffffffffu, mine.y, (s + k) & 31), sum);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          o.x = fmaf(f[k], v[k].x, o.x);
+          o.y = fmaf(f[k], v[k].y, o.y);
+          o.z = fmaf(f[k], v[k].z, o.z);
+          o.w = fmaf(f[k], v[k].w, o.w);
+        }
+      }
     }
     const float f = sum > 0.0f ? a.gv / sum : 0.0f;
     const uint32_t r = t.row0 + local, tok = a.group.div(r), head = kvh * a.group.d + (r - tok * a.group.d);
@@ -825,20 +1287,41 @@ __global__ void __launch_bounds__(256) extend_combine_kernel(const ExtendArgs a)
 // ---- host ----------------------------------------------------------------
 
 struct Plan {
+  int rows;  // of a tile: kTileRows, or 8, 16, 24 by the rows kernel
   int64_t tiles, tiles_per_seq, splits;
+  bool full;  // the tile kernel's exact weights
 };
 
-// The tiles (at most) and the parts that each tile's keys are cut into: as many
-// as make the last wave of CTAs full, against what a part costs by itself (its
-// prologue; with several, its record written and read).  Costs in blocks of
-// 128 keys.
+// Contexts of up to this many keys take the tile kernel's kFull.
+constexpr int64_t kFullContext = 512;
+
+// Which kernel, the tiles (at most), and the parts that each tile's keys are cut into.
 Plan plan_for(int64_t batch, int64_t n_tokens, int64_t group, int64_t hkv, int64_t context, bool uniform) {
   Plan p;
-  p.tiles_per_seq = (n_tokens / batch * group + kTileRows - 1) / kTileRows;
-  const int64_t ragged = n_tokens * group / kTileRows + (batch < n_tokens ? batch : n_tokens);
+  const int64_t sms = sm_count(), blocks = (context + kBlock - 1) / kBlock;
+  const int64_t rows = (n_tokens * group + batch - 1) / batch;  // of a sequence and KV head, on average
+  p.full = context <= kFullContext;
+  p.rows = p.full || rows > 24 ? kTileRows : static_cast<int>((rows + 7) / 8 * 8);
+  p.tiles_per_seq = (n_tokens / batch * group + p.rows - 1) / p.rows;
+  const int64_t ragged = n_tokens * group / p.rows + (batch < n_tokens ? batch : n_tokens);
   p.tiles = uniform ? batch * p.tiles_per_seq : ragged;
-  const int64_t items = p.tiles * hkv, sms = sm_count(), blocks = (context + kBlock - 1) / kBlock;
+  const int64_t items = p.tiles * hkv;
   p.splits = 1;
+  if (p.rows != kTileRows) {
+    // Enough CTAs for six rounds on what is resident, so that sequences of
+    // different lengths even out, in parts of 512 keys or more; failing that,
+    // one round in parts of a stage or more.
+    const int64_t resident = sms * (p.rows == 8 ? 4 : p.rows == 16 ? 3 : 2);
+    const int64_t even = (6 * resident + items - 1) / items, long_parts = (blocks + 3) / 4;
+    const int64_t fill = (resident + items - 1) / items;
+    p.splits = even < long_parts ? even : long_parts;
+    if (fill > p.splits) p.splits = fill;
+    if (p.splits > blocks) p.splits = blocks;
+    return p;
+  }
+  // As many as make the last wave of CTAs full, against what a part costs by
+  // itself (its prologue; with several, its record written and read), in blocks
+  // of 128 keys.
   double best = 0.0;
   for (int64_t s = 1; s == 1 || (s <= blocks && s <= 64 && items * s <= 4 * sms); ++s) {
     const double cost = static_cast<double>((items * s + sms - 1) / sms) * (static_cast<double>((blocks + s - 1) / s) + (s > 1 ? 6.0 : 2.0));
@@ -851,19 +1334,28 @@ Plan plan_for(int64_t batch, int64_t n_tokens, int64_t group, int64_t hkv, int64
 }
 
 size_t workspace_for(const Plan& p, int64_t hkv) {
-  return p.splits > 1 ? static_cast<size_t>(p.tiles) * hkv * p.splits * kTileRows * (kD + 2) * sizeof(float) : 0;
+  return p.splits > 1 ? static_cast<size_t>(p.tiles) * hkv * p.splits * p.rows * (kD + 2) * sizeof(float) : 0;
 }
 
-// Contexts of up to this many keys take kFull.
-constexpr uint32_t kFullContext = 512;
-
-using TileKernel = void (*)(const ExtendArgs);
-template <bool kE1M2, bool kMods, bool kFull>
-TileKernel tile_kernel() {
-  // Idempotent and cheap; a failure shows at the launch.
-  cudaFuncSetAttribute(extend_tile_kernel<kE1M2, kMods, kFull>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                       static_cast<int>(kTileSmem));
-  return extend_tile_kernel<kE1M2, kMods, kFull>;
+using Kernel = void (*)(const ExtendArgs);
+// Raising the limit is idempotent and cheap; a failure shows at the launch.
+Kernel with_smem(Kernel k, uint32_t bytes) {
+  cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  return k;
+}
+template <bool kE1M2, bool kMods>
+Kernel kernel_for(const Plan& p) {
+  switch (p.rows) {
+    case 8: return with_smem(extend_rows_kernel<1, kE1M2, kMods>, kRowsSmem);
+    case 16: return with_smem(extend_rows_kernel<2, kE1M2, kMods>, kRowsSmem);
+    case 24: return with_smem(extend_rows_kernel<3, kE1M2, kMods>, kRowsSmem);
+  }
+  return p.full ? with_smem(extend_tile_kernel<kE1M2, kMods, true>, kTileSmem)
+                : with_smem(extend_tile_kernel<kE1M2, kMods, false>, kTileSmem);
+}
+Kernel combine_for(const Plan& p) {
+  return p.rows == 8 ? extend_combine_kernel<8> : p.rows == 16 ? extend_combine_kernel<16>
+         : p.rows == 24 ? extend_combine_kernel<24> : extend_combine_kernel<kTileRows>;
 }
 
 }  // namespace
@@ -879,7 +1371,8 @@ NVFP4_API size_t extend_attention_nvfp4_workspace_size(int32_t batch, int64_t n_
   // Both forms of q_start, so that one buffer serves either.
   const int64_t group = num_q_heads / num_kv_heads;
   const size_t ragged = workspace_for(plan_for(batch, n_tokens, group, num_kv_heads, context, false), num_kv_heads);
-  const size_t uniform = workspace_for(plan_for(batch, n_tokens, group, num_kv_heads, context, true), num_kv_heads);
+  const size_t uniform =
+      n_tokens % batch ? 0 : workspace_for(plan_for(batch, n_tokens, group, num_kv_heads, context, true), num_kv_heads);
   return ragged > uniform ? ragged : uniform;
 }
 
@@ -932,21 +1425,18 @@ NVFP4_API nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const
   a.tiles_per_seq = static_cast<uint32_t>(p.tiles_per_seq);
   a.splits = static_cast<uint32_t>(p.splits);
   a.o_ws = static_cast<float*>(workspace);
-  a.ml_ws = reinterpret_cast<float2*>(a.o_ws + static_cast<size_t>(grid) * kTileRows * kD);
+  a.ml_ws = reinterpret_cast<float2*>(a.o_ws + static_cast<size_t>(grid) * p.rows * kD);
   const bool mods = options->logit_cap > 0.0f || options->slopes, e1m2 = cache->kv_format == NVFP4_KV_E1M2;
-  const bool full = a.map.context <= kFullContext;
-  const auto of = [&](auto e, auto m) {
-    return full ? tile_kernel<decltype(e)::value, decltype(m)::value, true>()
-                : tile_kernel<decltype(e)::value, decltype(m)::value, false>();
-  };
-  const TileKernel kernel = e1m2 ? (mods ? of(std::true_type(), std::true_type()) : of(std::true_type(), std::false_type()))
-                                 : (mods ? of(std::false_type(), std::true_type()) : of(std::false_type(), std::false_type()));
+  const Kernel kernel = e1m2 ? (mods ? kernel_for<true, true>(p) : kernel_for<true, false>(p))
+                             : (mods ? kernel_for<false, true>(p) : kernel_for<false, false>(p));
+  const bool by_tiles = p.rows == kTileRows;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (launch_pdl(kernel, dim3(static_cast<uint32_t>(grid)), dim3(kTileThreads), kTileSmem, s, a) != cudaSuccess)
+  if (launch_pdl(kernel, dim3(static_cast<uint32_t>(grid)), dim3(by_tiles ? kTileThreads : kRowsThreads),
+                 by_tiles ? kTileSmem : kRowsSmem, s, a) != cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
   if (p.splits > 1) {
-    if (launch_pdl(extend_combine_kernel<kTileRows>, dim3(a.tiles, a.map.hkv, 4), dim3(256), 0, s, a) != cudaSuccess)
+    if (launch_pdl(combine_for(p), dim3(a.tiles, a.map.hkv, by_tiles ? 8 : (p.rows + 7) / 8), dim3(256), 0, s, a) != cudaSuccess)
       return NVFP4_ERR_CUDA;
     count_launches(1);
   }
