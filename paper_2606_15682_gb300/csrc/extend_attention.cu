@@ -232,26 +232,30 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
   return v;
 }
 
-// mbar_wait_bounded with a hint of how long the hardware may suspend the thread,
-// so that waiting warps leave the issue slots to the others.
+__device__ __forceinline__ float warp_max(float v) {
+  float d;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(d) : "f"(v));
+  return d;
+}
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+// Whether any of the barrier's 128 threads says so; also their barrier.
+__device__ __forceinline__ bool any_of_128(bool mine) {
+  uint32_t any;
+  tc_fence_before();
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, %2, 128, p;\n selp.u32 %0, 1, 0, q;\n}"
+               : "=r"(any)
+               : "r"(static_cast<uint32_t>(mine)), "n"(1)
+               : "memory");
+  tc_fence_after();
+  return any != 0;
+}
+
+// mbar_wait_bounded, the flag that another role gave up looked at in every turn.
 __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatile int* abort) {
-  const uint32_t addr = smem_u32(bar);
-  const auto once = [&] {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n"
-        " mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
-        " selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(addr), "r"(parity), "r"(100000u)
-        : "memory");
-    return ok != 0;
-  };
-  if (once()) return true;
+  if (mbar_try_wait(bar, parity)) return true;
   const uint64_t t0 = globaltimer_ns();
-  while (!once()) {
+  while (!mbar_try_wait(bar, parity))
     if (*abort || globaltimer_ns() - t0 > kWaitLimitNs) return false;
-  }
   return true;
 }
 
@@ -281,6 +285,39 @@ __device__ __forceinline__ void score32(float* s, const RowScore& rs, const Exte
 #pragma unroll
     for (int i = 0; i < 32; ++i) s[i] = fmaf(-rs.slope, fabsf(static_cast<float>(p_minus_t0 - i)), s[i]);
   }
+}
+
+// The eight elements of a code word times their block scale (kv_scales16) as four
+// f16x2.  E2M1: channels (0,1) (2,3) (4,5) (6,7).  E1M2: (0,4) (1,5) (2,6) (3,7): a
+// nibble is decoded where it stands, those in bits 4-7 as 16 times their value,
+// for which the scale is divided (exact).  Q is laid out in the same order, and
+// O comes in V's.
+template <bool kE1M2>
+__device__ __forceinline__ void scaled8(uint32_t w, uint32_t scale, uint32_t e[4]) {
+  if (kE1M2) {
+    const uint32_t t = w >> 8, scale16 = mul_f16x2(scale, 0x2C002C00u);
+    e[0] = mul_f16x2(sub_f16x2((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u), scale);
+    e[1] = mul_f16x2(sub_f16x2((w & 0x00F000F0u) ^ 0x64806480u, 0x64806480u), scale16);
+    e[2] = mul_f16x2(sub_f16x2((t & 0x000F000Fu) ^ 0x64086408u, 0x64086408u), scale);
+    e[3] = mul_f16x2(sub_f16x2((t & 0x00F000F0u) ^ 0x64806480u, 0x64806480u), scale16);
+  } else {
+    elements8<false>(w, e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = mul_f16x2(e[i], scale);
+  }
+}
+// Place of channel c, and channel at place c, in that order.
+template <bool kE1M2>
+__device__ __forceinline__ constexpr int place_of(int c) { return kE1M2 ? (c & ~7) | (c & 3) << 1 | (c >> 2 & 1) : c; }
+template <bool kE1M2>
+__device__ __forceinline__ constexpr int channel_of(int c) { return kE1M2 ? (c & ~7) | (c & 1) << 2 | (c >> 1 & 3) : c; }
+// Eight channels of Q, scaled, as f16 in that order.
+template <bool kE1M2>
+__device__ __forceinline__ uint4 q_chunk(const float x[8], float down) {
+  uint32_t f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = f16x2_rn(x[channel_of<kE1M2>(2 * i)] * down, x[channel_of<kE1M2>(2 * i + 1)] * down);
+  return make_uint4(f[0], f[1], f[2], f[3]);
 }
 
 // Two f16 values of at most 7 significant bits, at least 2^-14 or zero -> bf16,
@@ -396,8 +433,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
         if (c == 0) sh.mult[lr] = a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
         float x[8];
         unpack_bf16x8(w[i], x);
-        sts128(smem + (lr >> 7) * kOperand + operand_chunk(lr & 127, c), f16x2_rn(x[0] * down, x[1] * down),
-               f16x2_rn(x[2] * down, x[3] * down), f16x2_rn(x[4] * down, x[5] * down), f16x2_rn(x[6] * down, x[7] * down));
+        const uint4 f = q_chunk<kE1M2>(x, down);
+        sts128(smem + (lr >> 7) * kOperand + operand_chunk(lr & 127, c), f.x, f.y, f.z, f.w);
       }
       fence_proxy_async_smem();
     }
@@ -418,7 +455,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
     bool ok = true;
     for (int v = 0; v < subs; ++v) {
-      const int j = two ? v >> 1 : (v & ~1) + t, hf = v & 1, t0 = t_base + j * kBlock + 64 * hf;
+      const int j = two ? v >> 1 : (v & ~1) + t, hf = v & 1, t0 = t_base + (nblk - 1 - j) * kBlock + 64 * hf;
       const uint32_t s_col = s_tile + 64 * hf;
       ok = __all_sync(0xffffffffu, wait_bar(&sh.s_full[t][hf], (v >> 1) & 1, &sh.abort));
       if (!ok) break;
@@ -562,16 +599,19 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
         }
         if (a.splits == 1) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            sts128(at(lane, 4 * c + k), bf16x2_rn(o[8 * k], o[8 * k + 1]), bf16x2_rn(o[8 * k + 2], o[8 * k + 3]),
-                   bf16x2_rn(o[8 * k + 4], o[8 * k + 5]), bf16x2_rn(o[8 * k + 6], o[8 * k + 7]));
+          for (int k = 0; k < 4; ++k) {
+            uint32_t w[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) w[x] = bf16x2_rn(o[place_of<kE1M2>(8 * k + 2 * x)], o[place_of<kE1M2>(8 * k + 2 * x + 1)]);
+            sts128(at(lane, 4 * c + k), w[0], w[1], w[2], w[3]);
+          }
           continue;
         }
         // A record in fp32: 128 bytes of each row at a time.
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          sts128(at(lane, k), __float_as_uint(o[4 * k]), __float_as_uint(o[4 * k + 1]), __float_as_uint(o[4 * k + 2]),
-                 __float_as_uint(o[4 * k + 3]));
+          sts128(at(lane, k), __float_as_uint(o[place_of<kE1M2>(4 * k)]), __float_as_uint(o[place_of<kE1M2>(4 * k + 1)]),
+                 __float_as_uint(o[place_of<kE1M2>(4 * k + 2)]), __float_as_uint(o[place_of<kE1M2>(4 * k + 3)]));
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -616,7 +656,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     constexpr uint32_t kNone = 0xffffffffu;
     const uint32_t pages = a.map.table ? a.map.pages : 1u;
     const auto find = [&](int q) {
-      const int t0 = t_base + block(q) * kBlock + w * 8 + sub;  // >= 0
+      // The blocks from the last to the first: the newest keys tend to have the
+      // largest scores (with a distance bias, all of them), so maxima settle early.
+      const int t0 = t_base + max(nblk - 1 - block(q), 0) * kBlock + w * 8 + sub;
       const int stop = q < operands && block(q) < nblk ? end : 0;
       const int32_t* table = a.map.table + static_cast<uint64_t>(sh.tile.b) * a.map.per_seq;
 #pragma unroll
@@ -659,12 +701,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           uint32_t e[4];
-          elements8<kE1M2>(words[k], e);
+          scaled8<kE1M2>(words[k], k < 2 ? g0 : g1, e);
+          if (bf16)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            e[x] = mul_f16x2(e[x], k < 2 ? g0 : g1);
-            if (bf16) e[x] = bf16x2_of_f16x2(e[x]);
-          }
+            for (int x = 0; x < 4; ++x) e[x] = bf16x2_of_f16x2(e[x]);
           sts128(at[k] + offset + it * 4096, e[0], e[1], e[2], e[3]);  // 32 rows of 128 bytes further
         }
       }
@@ -783,453 +823,546 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
   }
 }
 
-// ---- few rows: registers --------------------------------------------------
-// HBM-bound work: every byte of K and V is needed once for a handful of rows.  A
-// CTA takes 8 kN rows and a range of keys.  Warp 0 streams the keys' codes and
-// scales into a two-stage ring of 128 keys; four warps take two 16-key tiles of a
-// stage each, dequantize in registers (exact in f16) and multiply with mma.sync
-// m16n8k16: S^T[16 keys, 8 rows] = K Q^T, O^T[128, 8 rows] += V^T P^T, for each of
-// the kN groups of rows.  (tcgen05 would take a 128-row operand for these few, and
-// K and V through shared memory: 64 x 16384 ragged tokens 381 us by the tiles.)
-//
-// Lane roles (g = lane / 4, t = lane % 4), as the fragments have them:
-//   K rows g and g + 8 of the tile, channels 32t..32t+31; V rows 2t, 2t+1, 2t+8,
-//   2t+9, channels 16g..16g+15; Q row g of a group, channels 32t..32t+31.
-// Row m of a 16-key tile is key (m & 1) * 4 + (m >> 1 & 3) + (m & 8), so that a V
-// load covers four consecutive keys.
-constexpr int kRowsWarps = 4;
-constexpr int kRowsThreads = 32 * (1 + kRowsWarps);
-constexpr int kRing = 2;
-constexpr uint32_t kStageCodes = kBlock * 64, kStageBytes = 2 * kBlock * (64 + 8);  // K, V codes, K, V scales
-constexpr int kMergeRow = 148;  // floats of a row's 128 channels in the merge buffer: 2 of padding per 16
+// ---- few rows: keys on the M side -----------------------------------------
+// HBM-bound work: every byte of K and V is needed once for up to 32 rows.  A CTA
+// takes kC rows and a range of keys, and multiplies the other way round, so that
+// the rows are the short side of every product (kN = 16 or 32 of the tensor core):
+//   S^T[128 keys, kN] = K Q^T: K dequantized into TMEM (lane = key), Q in shared memory
+//   O^T[128 channels, kN] += V^T P^T: V dequantized into shared memory, P too
+//   warps 0-3   softmax (thread = key; in the end, channel of O^T)
+//   warps 4-7   K (thread = key)
+//   warps 8-11  V
+//   warp 12, 13 issue the PV and the QK^T; 14, 15 complete the warpgroup
+// Two CTAs share an SM.  What a softmax thread does per block is kept short: the
+// four roles' code does not fit the instruction caches that are near the
+// schedulers, and a role's turn goes by its instructions more than by its work.
+// (By mma.sync in registers the tensor pipe's rate for that form is the bound: 64
+// ragged sequences of up to 16384 tokens 174 us, 32 x 4 new tokens on 4001 148.)
+constexpr int kRowsThreads = 16 * 32;
+constexpr uint32_t kRowsTmem = 256;  // columns: K 2 x 64, S^T 2 x 32, O^T 32
+constexpr uint32_t kColS = 128, kColO = 192;
+constexpr int kAhead = 3;  // blocks whose K and V are on their way to L2, past the one in registers
 
-__device__ __forceinline__ int tile_key(int m) { return (m & 1) * 4 + ((m >> 1) & 3) + (m & 8); }
-__device__ __forceinline__ void mma16816(float c[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t transposed(uint32_t a) {
-  uint32_t d;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
-  return d;
-}
-// The eight elements of a code word as pairs.  E2M1: (0,1) (2,3) (4,5) (6,7).
-// E1M2: (0,4) (1,5) (2,6) (3,7), the second and fourth pair times 16 (a nibble in
-// bits 4-7 is decoded where it stands); their scales carry the 1/16.
-template <bool kE1M2>
-__device__ __forceinline__ void pairs8(uint32_t w, uint32_t e[4]) {
-  if (kE1M2) {
-    const uint32_t t = w >> 8;
-    e[0] = sub_f16x2((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
-    e[1] = sub_f16x2((w & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
-    e[2] = sub_f16x2((t & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
-    e[3] = sub_f16x2((t & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
-  } else {
-    elements8<false>(w, e);
-  }
-}
+template <int kC>
+struct RowsConfig {
+  static constexpr int kN = kC <= 16 ? 16 : 32;
+  // Shared memory: V, two blocks; Q; P, two blocks of one term (two with kFull).
+  static constexpr uint32_t kB = kN * 256;  // bytes of a kN x 128 f16 operand
+  static constexpr uint32_t kOffQ = 2 * kOperand, kOffP = kOffQ + kB;
+  static constexpr uint32_t kBytes = kOffP + 4 * kB + 1024;
+};
 
-template <int kN>
+struct RowInfo {
+  float slope;
+  int pos, lo, hi;
+  uint32_t out;  // (token, head) row of the output; rows past the tile's: none
+};
+template <int kC>
 struct RowsShared {
-  uint64_t full[kRing], empty[kRing];
-  uint32_t present[kRing][4];
+  uint64_t s_full[2], s_free[2], k_full[2], k_free[2], v_full[2], v_free[2], p_full[2], drain, drain_qk;
+  uint32_t tmem;
   Tile tile;
   Seq seq;
-  int lo, hi;
-  float m[kRowsWarps][8 * kN], l[kRowsWarps][8 * kN];
-  uint2 q[kN > 1 ? kN : 1][8][32];  // Q fragments by group, k-step, lane (one group: in registers)
+  int lo, hi, all_lo, all_hi, rows;
+  alignas(16) float mult[kC];   // score -> log2 domain
+  alignas(16) float minus[kC];  // 7 - the row's maximum: x = score + minus is a weight's exponent
+  RowInfo row[kC];
+  float top[4][kC], sum[4][kC];
+  uint32_t present[4][4];
   volatile int abort;
 };
-constexpr uint32_t kRowsSmem = kRing * kStageBytes + kRowsWarps * 8 * kMergeRow * 4;
 
-template <int kN, bool kE1M2, bool kMods>
-__global__ void __launch_bounds__(kRowsThreads, kN == 1 ? 4 : kN == 2 ? 3 : 2) extend_rows_kernel(const ExtendArgs a) {
-  extern __shared__ __align__(128) uint8_t smem_raw[];
-  __shared__ RowsShared<kN> sh;
-  constexpr uint32_t kRows = 8 * kN;
+// kC consecutive columns of the warp's lanes.
+template <int kC>
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, float* r) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  if (kC == 32) {
+    tmem_ld32(taddr, r);
+    return;
+  }
+  if (kC >= 16)
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]),
+                   "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+                 : "r"(taddr));
+  if (kC == 8 || kC == 24) {
+    constexpr int o = kC - 8;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(u[o]), "=r"(u[o + 1]), "=r"(u[o + 2]), "=r"(u[o + 3]), "=r"(u[o + 4]), "=r"(u[o + 5]),
+                   "=r"(u[o + 6]), "=r"(u[o + 7])
+                 : "r"(taddr + o));
+  }
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float* r) {
+  const uint32_t* u = reinterpret_cast<const uint32_t*>(r);
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(u[0]), "r"(u[1]),
+               "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
+               : "memory");
+}
+// P as the operand B: key k's rows 8g..8g+7 are the 16 bytes at 2048 g + 16 k (no
+// swizzle, N contiguous: 8 x 8 core matrices of 128 bytes, 128 bytes from eight
+// keys to the next, 2048 from eight rows to the next).
+constexpr uint32_t kDescPlainHigh = (2048u >> 4) | (1u << 14);
+__device__ __forceinline__ uint32_t plain_desc(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | ((128u >> 4) << 16); }
+__device__ __forceinline__ void mma_v_p(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n .reg .b64 da, db;\n setp.ne.b32 p, %4, 0;\n mov.b64 da, {%1, %5};\n"
+               " mov.b64 db, {%2, %6};\n tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n}" ::"r"(d),
+               "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"(kDescHigh), "n"(kDescPlainHigh)
+               : "memory");
+}
+
+template <int kC, bool kE1M2, bool kFull>
+__global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const ExtendArgs a) {
+  using C = RowsConfig<kC>;
+  constexpr int kN = C::kN;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ RowsShared<kC> sh;
+  const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kRing; ++i) {
-      mbar_init(&sh.full[i], 1 + 32);  // the armed bytes, and each lane's own copies
-      mbar_init(&sh.empty[i], kRowsWarps);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.s_full[i], 1);
+      mbar_init(&sh.s_free[i], 4);
+      mbar_init(&sh.k_full[i], 4);
+      mbar_init(&sh.k_free[i], 1);
+      mbar_init(&sh.v_full[i], 4);
+      mbar_init(&sh.v_free[i], 1);
+      mbar_init(&sh.p_full[i], 4);
     }
+    mbar_init(&sh.drain, 1);
+    mbar_init(&sh.drain_qk, 1);
     sh.abort = 0;
     fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&sh.tmem, kRowsTmem);
+    tmem_relinquish();  // the SM's other CTA allocates too
   }
   griddep_wait_and_release();
   const uint32_t split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
   const uint32_t tile_id = rest / a.map.hkv, kvh = rest - tile_id * a.map.hkv, group = a.group.d;
   if (warp == 0) {
-    const Tile tl = find_tile<kRows>(a, tile_id);
+    const Tile tl = find_tile<kC>(a, tile_id);
+    const bool any = tl.b < a.map.batch;  // else more CTAs than tiles
     Seq sq = {0, 0, 0};
-    if (tl.b < a.map.batch) sq = sequence(a, tl.b);
-    // The keys that the tile's rows see.
-    int lo = 0x7fffffff, hi = 0;
-    const uint32_t rows = tl.b < a.map.batch ? min(sq.n * group - tl.row0, kRows) : 0;
-    if (lane < static_cast<int>(rows)) {
-      const uint32_t tok = a.group.div(tl.row0 + lane);
-      const int p = sq.len - static_cast<int>(sq.n) + static_cast<int>(tok);
-      const int2 vis = visible(a, p, sq.len, a.prefix_lens ? __ldg(a.prefix_lens + tl.b) : 0,
-                               a.doc_start ? __ldg(a.doc_start + sq.first + tok) : 0);
-      if (p >= 0 && vis.x < vis.y) {
-        lo = vis.x;
-        hi = vis.y;
-      }
-    }
-    lo = __reduce_min_sync(0xffffffffu, lo);
-    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (any) sq = sequence(a, tl.b);
+    // A row a lane: what it sees, and where its output goes.
+    const uint32_t rows = any ? min(sq.n * group - tl.row0, static_cast<uint32_t>(kC)) : 0;
+    const bool live = lane < static_cast<int>(rows);
+    const uint32_t r = tl.row0 + (live ? lane : 0), tok = a.group.div(r), h = kvh * group + (r - tok * group);
+    RowInfo row;
+    row.pos = sq.len - static_cast<int>(sq.n) + static_cast<int>(tok);
+    int2 vis = make_int2(0, 0);
+    if (live && row.pos >= 0)
+      vis = visible(a, row.pos, sq.len, a.prefix_lens ? __ldg(a.prefix_lens + tl.b) : 0,
+                    a.doc_start ? __ldg(a.doc_start + sq.first + tok) : 0);
+    if (vis.x >= vis.y) vis = make_int2(0x7fffffff, 0);
+    row.lo = vis.x;
+    row.hi = vis.y;
+    row.slope = a.slopes && live ? __ldg(a.slopes + h) * kLog2e : 0.0f;
+    row.out = live ? (sq.first + tok) * a.hq + h : 0xffffffffu;
+    if (lane < kC) sh.row[lane] = row;
+    const int lo = __reduce_min_sync(0xffffffffu, vis.x), hi = __reduce_max_sync(0xffffffffu, vis.y);
+    const int all_lo = __reduce_max_sync(0xffffffffu, live ? vis.x : 0);
+    const int all_hi = __reduce_min_sync(0xffffffffu, live ? vis.y : 0x7fffffff);
     if (lane == 0) {
       sh.tile = tl;
       sh.seq = sq;
       sh.lo = hi > lo ? lo : 0;
       sh.hi = hi > lo ? hi : 0;
+      sh.rows = static_cast<int>(rows);
+      sh.all_lo = all_lo;
+      sh.all_hi = all_hi;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem;
+  const Tile tile = sh.tile;
+  const bool none = tile.b >= a.map.batch;
+  // This CTA's blocks of keys, counted from the tile's first key.
+  const int end = sh.hi, total = (end - sh.lo + kBlock - 1) / kBlock;
+  const int per = (total + static_cast<int>(a.splits) - 1) / static_cast<int>(a.splits);
+  const int j0 = min(static_cast<int>(split) * per, total), nblk = min(per, total - j0);
+  const int t_base = sh.lo + j0 * kBlock;
+
+  // A key's page and row in it, from the page table or, contiguous, at once.
+  const int64_t base_row = (static_cast<int64_t>(a.map.table ? 0 : tile.b) * a.map.hkv + kvh) * a.map.size.d;
+  const int64_t page_rows = static_cast<int64_t>(a.map.hkv) * a.map.size.d;
+  const int32_t* table = a.map.table + (none ? 0 : static_cast<uint64_t>(tile.b) * a.map.per_seq);
+  const auto find = [&](int j, int key, uint32_t* page, uint32_t* off) {
+    const int t = t_base + max(nblk - 1 - j, 0) * kBlock + key;  // the newest keys first, as in the tile kernel
+    *off = t;
+    *page = j < nblk && t < end ? 0u : 0xffffffffu;
+    if (a.map.table && *page == 0u) {
+      const uint32_t i = a.map.size.div(t);
+      *off -= i * a.map.size.d;
+      *page = static_cast<uint32_t>(__ldg(table + i));
+    }
+  };
+  const uint32_t pages = a.map.table ? a.map.pages : 1u;
+  const auto wait = [&](uint64_t* bar, int phase) {
+    const bool ok = __all_sync(0xffffffffu, wait_bar(bar, phase & 1, &sh.abort));
+    if (!ok && lane == 0 && !sh.abort) {
+      set_status(a.status, NVFP4_ERR_TIMEOUT);
+      sh.abort = 1;
+    }
+    tc_fence_after();
+    return ok;
+  };
+
+  if (warp < 4) {
+    // ------------------------------------------------------------- softmax ---
+    // Q rows as f16, scaled by a power of two (exact) to below 1: 16 lanes a row.
+    uint4 w[kN / 8];
+#pragma unroll
+    for (int i = 0; i < kN / 8; ++i) {
+      const uint32_t lr = i * 8 + warp * 2 + (lane >> 4), out = lr < kC ? sh.row[lr].out : 0xffffffffu;
+      w[i] = make_uint4(0, 0, 0, 0);
+      if (out != 0xffffffffu) {
+        const uint32_t tk = out / a.hq;
+        w[i] = __ldg(reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(tk) * a.ld_q + (out - tk * a.hq) * kD) + (lane & 15));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kN / 8; ++i) {
+      const uint32_t lr = i * 8 + warp * 2 + (lane >> 4), c = lane & 15;
+      uint32_t top = amax_bits_bf16x8(w[i]);
+#pragma unroll
+      for (int s = 1; s < 16; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+      const int e = max(-125, min(static_cast<int>(top >> 7) - 126, 126));
+      const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+      if (c == 0 && lr < kC) {
+        // No maximum yet: any score exceeds it.  (A row past the tile's has scores of 0.)
+        const bool live = sh.row[lr].out != 0xffffffffu;
+        sh.mult[lr] = live ? a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23) : 0.0f;
+        sh.minus[lr] = live ? 1e30f : 0.0f;
+      }
+      float x[8];
+      unpack_bf16x8(w[i], x);
+      const uint4 f = q_chunk<kE1M2>(x, down);
+      sts128(smem + C::kOffQ + (c >> 3) * (kN * 128) + lr * 128 + (((c ^ lr) & 7) << 4), f.x, f.y, f.z, f.w);
+    }
+    fence_proxy_async_smem();
+  }
+  __syncthreads();
+
+  // 104, 64, 64 and 24 registers a thread: the 512 x 64 that the CTA starts with.
+  if (warp < 4) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
+    const int key = warp * 32 + lane;
+    const bool mods = a.cap > 0.0f || a.slopes;
+    float l[kC];
+#pragma unroll
+    for (int n = 0; n < kC; ++n) l[n] = 0.0f;
+    bool ok = true;
+    for (int j = 0; j < nblk; ++j) {
+      const int b = j & 1, t0 = t_base + (nblk - 1 - j) * kBlock, tk = t0 + key;
+      const uint32_t p_at = smem + C::kOffP + b * 2 * C::kB + key * 16;
+      ok = wait(&sh.s_full[b], j >> 1);
+      ok = wait(&sh.v_full[b], j >> 1) && ok;  // and so P of block j - 2 is used up
+      const bool there = (sh.present[j & 3][warp] >> lane) & 1u;
+      const bool open = t0 >= sh.all_lo && t0 + kBlock <= sh.all_hi && __all_sync(0xffffffffu, there);
+      float s[kC];
+      tmem_ld_cols<kC>(tmem + lanes + kColS + b * 32, s);
+      tmem_wait_ld();
+#pragma unroll
+      for (int n = 0; n < kC; n += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(&sh.mult[n]);
+        s[n] *= f.x;
+        s[n + 1] *= f.y;
+        s[n + 2] *= f.z;
+        s[n + 3] *= f.w;
+      }
+      if (mods) {
+        const float cap = a.cap * kLog2e, in = 2.0f / a.cap;  // 2 log2(e) s / c
+#pragma unroll
+        for (int n = 0; n < kC; ++n) {
+          if (a.cap > 0.0f) s[n] = fmaf(-2.0f * cap, rcp(1.0f + ex2(s[n] * in)), cap);
+          s[n] = fmaf(-sh.row[n].slope, fabsf(static_cast<float>(sh.row[n].pos - tk)), s[n]);
+        }
+      }
+      if (!open) {
+#pragma unroll
+        for (int n = 0; n < kC; ++n)
+          if (!there || tk < sh.row[n].lo || tk >= sh.row[n].hi) s[n] = -INFINITY;
+      }
+      // Maxima move only where a weight would exceed 2^8 of its row's maximum.
+      for (;;) {
+        float most = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < kC; n += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(&sh.minus[n]);
+          most = max3(max3(s[n] + f.x, s[n + 1] + f.y, most), s[n + 2] + f.z, s[n + 3] + f.w);
+        }
+        if (!any_of_128(most > kWeightLog2 + kRescaleLog2 || !ok)) break;
+        // Each row's largest score in the block, by warp, then of all four.
+#pragma unroll
+        for (int n = 0; n < kC; ++n) {
+          const float v = warp_max(s[n]);
+          if (lane == 0) sh.top[warp][n] = v;
+        }
+        if (any_of_128(!ok)) {
+          ok = false;
+          break;  // a wait ran out: the four warps leave together
+        }
+        const auto top_of = [&](int n) { return max3(max3(sh.top[0][n], sh.top[1][n], sh.top[2][n]), sh.top[3][n], -INFINITY); };
+        const auto shrink = [&](int n) {
+          const float x = top_of(n) + sh.minus[n];
+          return x > kWeightLog2 + kRescaleLog2 ? ex2(kWeightLog2 - x) : 1.0f;
+        };
+#pragma unroll
+        for (int n = 0; n < kC; ++n) l[n] *= shrink(n);
+        if (j > 0) {
+          ok = wait(&sh.v_free[(j - 1) & 1], (j - 1) >> 1);
+#pragma unroll 1
+          for (int n0 = 0; n0 < kC; n0 += 8) {
+            float o[8];
+            tmem_ld_cols<8>(tmem + lanes + kColO + n0, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int n = 0; n < 8; ++n) o[n] *= shrink(n0 + n);
+            tmem_st8(tmem + lanes + kColO + n0, o);
+          }
+          tmem_wait_st();
+        }
+        any_of_128(false);  // every warp has read the old maxima
+        if (warp == 0 && lane < kC && shrink(lane) != 1.0f) sh.minus[lane] = kWeightLog2 - top_of(lane);
+        any_of_128(false);
+      }
+      if (!ok) break;
+#pragma unroll
+      for (int n = 0; n < kC; n += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(&sh.minus[n]);
+        s[n] = ex2(s[n] + f.x);
+        s[n + 1] = ex2(s[n + 1] + f.y);
+        s[n + 2] = ex2(s[n + 2] + f.z);
+        s[n + 3] = ex2(s[n + 3] + f.w);
+      }
+#pragma unroll
+      for (int n = 0; n < kC; n += 8) {
+        if (kFull) {
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t xb = __float_as_uint(s[n + 2 * k]), yb = __float_as_uint(s[n + 2 * k + 1]);
+            hi[k] = __byte_perm(xb, yb, 0x7632);
+            lo[k] = bf16x2_rn(s[n + 2 * k] - __uint_as_float(xb & 0xFFFF0000u), s[n + 2 * k + 1] - __uint_as_float(yb & 0xFFFF0000u));
+          }
+          sts128(p_at + n * 256, hi[0], hi[1], hi[2], hi[3]);
+          sts128(p_at + n * 256 + C::kB, lo[0], lo[1], lo[2], lo[3]);
+        } else {
+          sts128(p_at + n * 256, f16x2_rn(s[n], s[n + 1]), f16x2_rn(s[n + 2], s[n + 3]), f16x2_rn(s[n + 4], s[n + 5]),
+                 f16x2_rn(s[n + 6], s[n + 7]));
+        }
+      }
+      fence_proxy_async_smem();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&sh.p_full[b]);
+        mbar_arrive(&sh.s_free[b]);
+      }
+#pragma unroll
+      for (int n = 0; n < kC; ++n) l[n] += s[n];
+    }
+    const bool done = wait(&sh.drain, 0);
+    // ---- epilogue: thread = channel -----------------------------------------
+#pragma unroll
+    for (int n = 0; n < kC; ++n) {
+#pragma unroll
+      for (int x = 16; x; x >>= 1) l[n] += __shfl_xor_sync(0xffffffffu, l[n], x);
+      if (lane == 0) sh.sum[warp][n] = l[n];
+    }
+    any_of_128(false);
+    float o[kC];
+    if (nblk > 0) {
+      tmem_ld_cols<kC>(tmem + lanes + kColO, o);
+      tmem_wait_ld();
+    }
+    const uint64_t rec0 = ((static_cast<uint64_t>(tile_id) * a.map.hkv + kvh) * a.splits + split) * kC;
+    const int channel = channel_of<kE1M2>(key);
+    if (done && !none)
+#pragma unroll
+      for (int n = 0; n < kC; ++n) {
+        if (n >= sh.rows) break;
+        const float sum = nblk > 0 ? (sh.sum[0][n] + sh.sum[1][n]) + (sh.sum[2][n] + sh.sum[3][n]) : 0.0f;
+        const float v = sum > 0.0f ? o[n] : 0.0f;
+        if (a.splits > 1) {
+          if (key == 0) a.ml_ws[rec0 + n] = make_float2(sum > 0.0f ? kWeightLog2 - sh.minus[n] : -INFINITY, sum);
+          a.o_ws[(rec0 + n) * kD + channel] = v;
+        } else {
+          const uint32_t bits = bf16x2_rn(sum > 0.0f ? v * (a.gv / sum) : 0.0f, 0.0f);
+          a.out[static_cast<uint64_t>(sh.row[n].out) * kD + channel] = static_cast<uint16_t>(bits);
+        }
+      }
+    tc_fence_before();
+  } else if (warp < 8) {
+    // ------------------------------------------------------------------- K ---
+    const int w = warp - 4, key = w * 32 + lane;
+    const uint32_t k_col = tmem + (static_cast<uint32_t>(w * 32) << 16);
+    const uint8_t* codes = a.map.k_codes + base_row * 64;
+    const uint8_t* scales = a.map.k_scales + base_row * 8;
+    // The next block's row is in flight in registers, and those of the kAhead after
+    // it on their way to L2, with V's; their pages are known.
+    uint32_t page[kAhead + 1], off[kAhead + 1];
+    uint4 c[4];
+    uint2 sc;
+    bool there;
+    const auto load = [&] {
+      there = page[0] < pages;
+      const int64_t row = page[0] * page_rows + off[0];
+      sc = there ? __ldg(reinterpret_cast<const uint2*>(scales + row * 8)) : make_uint2(0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = there ? __ldg(reinterpret_cast<const uint4*>(codes + row * 64) + i) : make_uint4(0, 0, 0, 0);
+    };
+    const auto prefetch = [&](int i) {
+      if (page[i] >= pages) return;
+      const int64_t at = base_row + page[i] * page_rows + off[i];
+      if (!(at & 1) || off[i] == 0) {  // a line has two keys' codes
+        prefetch_l2(a.map.k_codes + at * 64);
+        prefetch_l2(a.map.v_codes + at * 64);
+      }
+      if (!(at & 15) || off[i] == 0) {  // and 16 keys' scales
+        prefetch_l2(a.map.k_scales + at * 8);
+        prefetch_l2(a.map.v_scales + at * 8);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i <= kAhead; ++i) find(i, key, &page[i], &off[i]);
+    load();
+#pragma unroll
+    for (int i = 1; i <= kAhead; ++i) prefetch(i);
+    for (int j = 0; j < nblk; ++j) {
+      const int b = j & 1;
+      const uint32_t here = __ballot_sync(0xffffffffu, there);
+      if (!wait(&sh.k_free[b], (j >> 1) ^ 1)) break;
+      if (lane == 0) sh.present[j & 3][w] = here;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // 32 channels
+        const uint32_t word[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+        const uint32_t f = kv_scales16<kE1M2>(__byte_perm(sc.x, sc.y, 0x10 + 0x22 * i));
+        const uint32_t f0 = __byte_perm(f, f, 0x1010), f1 = __byte_perm(f, f, 0x3232);
+        uint32_t e[16];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) scaled8<kE1M2>(word[k], k < 2 ? f0 : f1, e + 4 * k);
+        tmem_st16(k_col + b * 64 + 16 * i, e);
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        page[i] = page[i + 1];
+        off[i] = off[i + 1];
+      }
+      load();
+      find(j + 1 + kAhead, key, &page[kAhead], &off[kAhead]);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.k_full[b]);
+      prefetch(kAhead);
+    }
+  } else if (warp < 12) {
+    // ------------------------------------------------------------------- V ---
+    // Four lanes a key, 32 channels each; eight keys a warp and turn, four turns.
+    const int w = warp - 8, sub = lane >> 2, qd = lane & 3;
+    const uint8_t* codes = a.map.v_codes + base_row * 64 + 16 * qd;
+    const uint8_t* scales = a.map.v_scales + base_row * 8 + 2 * qd;
+    const bool sw = qd & 2;  // as in the tile kernel: eight lanes, eight bank groups
+    uint32_t at[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) at[k] = smem + operand_chunk(w * 8 + sub, 4 * qd + (sw ? k ^ 2 : k));
+    uint32_t page[4], off[4], sc[4];
+    uint4 c[4];
+    const auto rows_of = [&](int j) {
+#pragma unroll
+      for (int it = 0; it < 4; ++it) find(j, it * 32 + w * 8 + sub, &page[it], &off[it]);
+    };
+    const auto load = [&] {
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const bool there = page[it] < pages;
+        const int64_t row = page[it] * page_rows + off[it];
+        c[it] = there ? __ldg(reinterpret_cast<const uint4*>(codes + row * 64)) : make_uint4(0, 0, 0, 0);
+        sc[it] = there ? __ldg(reinterpret_cast<const uint16_t*>(scales + row * 8)) : 0u;
+      }
+    };
+    rows_of(0);
+    load();
+    rows_of(1);
+    for (int j = 0; j < nblk; ++j) {
+      const int b = j & 1;
+      if (!wait(&sh.v_free[b], (j >> 1) ^ 1)) break;
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const uint32_t g = kv_scales16<kE1M2>(sc[it]);
+        const uint32_t g0 = __byte_perm(g, g, sw ? 0x3232 : 0x1010), g1 = __byte_perm(g, g, sw ? 0x1010 : 0x3232);
+        const uint4 v = c[it];
+        const uint32_t words[4] = {sw ? v.z : v.x, sw ? v.w : v.y, sw ? v.x : v.z, sw ? v.y : v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t e[4];
+          scaled8<kE1M2>(words[k], k < 2 ? g0 : g1, e);
+          if (kFull)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) e[x] = bf16x2_of_f16x2(e[x]);
+          sts128(at[k] + b * kOperand + it * 4096, e[0], e[1], e[2], e[3]);
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.v_full[b]);
+      load();
+      rows_of(j + 2);
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 24;");
+    // ----------------------------------------------------------------- MMA ---
+    if (warp < 14) {
+      const bool leader = elect_one();
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      for (int j = 0; j < nblk; ++j) {
+        const int b = j & 1;
+        if (warp == 12) {
+          if (!wait(&sh.p_full[b], j >> 1)) break;  // V is there too: the softmax has waited for it
+          if (leader) {
+            // A = V^T (bit 15: stored with M contiguous), B = P (bit 16: N), 16 keys a step.
+            constexpr uint32_t kIdesc = (1u << 4) | (3u << 15) | (static_cast<uint32_t>(kN / 8) << 17) | (8u << 24) |
+                                        (kFull ? (1u << 7) | (1u << 10) : 0u);
+            const uint32_t v = operand_desc(smem + b * kOperand), p = plain_desc(smem + C::kOffP + b * 2 * C::kB);
+#pragma unroll
+            for (int s = 0; s < (kFull ? 16 : 8); ++s)
+              mma_v_p(tm + kColO, v + (((s & 7) * 2048) >> 4), p + (((s >> 3) * C::kB + (s & 7) * 256) >> 4), kIdesc,
+                      j != 0 || s != 0);
+            tc_commit(&sh.v_free[b]);
+          }
+        } else {
+          if (!wait(&sh.k_full[b], j >> 1) || (j >= 2 && !wait(&sh.s_free[b], (j >> 1) ^ 1))) break;
+          if (leader) {
+            constexpr uint32_t kIdesc = (1u << 4) | (static_cast<uint32_t>(kN / 8) << 17) | (8u << 24);
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+              const uint32_t at = C::kOffQ + (s >> 2) * (kN * 128) + (s & 3) * 32;
+              mma_ts(tm + kColS + b * 32, tm + b * 64 + s * 8, ((smem + at) & 0x3FFFFu) >> 4, kIdesc, s != 0);
+            }
+            tc_commit(&sh.s_full[b]);
+            tc_commit(&sh.k_free[b]);
+          }
+        }
+        __syncwarp();
+      }
+      // Nothing that was issued, MMA or arrival, outlives the CTA.
+      uint64_t* drain = warp == 12 ? &sh.drain : &sh.drain_qk;
+      if (leader) tc_commit(drain);
+      mbar_wait_bounded(drain, 0, nullptr, kDrainLimitNs);
+      __syncwarp();
     }
   }
   __syncthreads();
-  const Tile tile = sh.tile;
-  if (tile.b >= a.map.batch) return;  // more CTAs than tiles
-  const Seq seq = sh.seq;
-  const uint32_t rows = min(seq.n * group - tile.row0, kRows);
-  // This CTA's keys, in whole stages from the tile's first.
-  const int stages = (sh.hi - sh.lo + kBlock - 1) / kBlock;
-  const int per = (stages + static_cast<int>(a.splits) - 1) / static_cast<int>(a.splits);
-  const int s0 = min(static_cast<int>(split) * per, stages), n = min(per, stages - s0);
-  const int t_base = sh.lo + s0 * kBlock, t_end = min(sh.hi, t_base + n * kBlock);
-
-  if (warp == 0) {
-    // ------------------------------------------------------------ producer ---
-    // Lane i has keys i, i + 32, i + 64, i + 96 of a stage.  Codes come by bulk
-    // copies, one for each run of keys within a page; scales, 8 bytes a key, by
-    // the lane's own copies.  A key that is not there (past the end, or its page
-    // absent) gets scales of zero, whatever its codes' bytes.
-    const int64_t head = static_cast<int64_t>(kvh) * a.map.size.d;
-    for (int i = 0; i < n; ++i) {
-      const int st = i & 1, t0 = t_base + i * kBlock;
-      int64_t row[4];
-      uint32_t here[4], total = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int t = t0 + 32 * k + lane;
-        row[k] = t < t_end ? a.map.row(tile.b, t) : -1;
-        here[k] = __ballot_sync(0xffffffffu, row[k] >= 0);
-        total += __popc(here[k]);
-      }
-      if (!__all_sync(0xffffffffu, wait_bar(&sh.empty[st], ((i >> 1) & 1) ^ 1, &sh.abort))) {
-        if (lane == 0 && !sh.abort) {
-          set_status(a.status, NVFP4_ERR_TIMEOUT);
-          sh.abort = 1;
-        }
-        break;
-      }
-      uint8_t* stage = smem_raw + st * kStageBytes;
-      uint8_t* scales = stage + 2 * kStageCodes;
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (row[k] < 0) {
-          reinterpret_cast<uint2*>(scales)[32 * k + lane] = make_uint2(0, 0);
-          reinterpret_cast<uint2*>(scales + kBlock * 8)[32 * k + lane] = make_uint2(0, 0);
-        }
-      if (lane < 4) sh.present[st][lane] = lane == 0 ? here[0] : lane == 1 ? here[1] : lane == 2 ? here[2] : here[3];
-      __syncwarp();
-      if (lane == 0) mbar_arrive_expect_tx(&sh.full[st], total * 128);
-      __syncwarp();
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int c = 32 * k + lane;
-        if (row[k] < 0) continue;
-        const int64_t at = row[k] + head;
-        const uint32_t off = static_cast<uint32_t>(a.map.table ? (t0 + c) - static_cast<int>(a.map.size.div(t0 + c)) * static_cast<int>(a.map.size.d) : t0 + c);
-        if (c == 0 || off == 0) {  // a run of keys begins
-          const int len = min(min(static_cast<int>(a.map.size.d - off), kBlock - c), t_end - (t0 + c));
-          bulk_load(stage + c * 64, a.map.k_codes + at * 64, len * 64, &sh.full[st]);
-          bulk_load(stage + kStageCodes + c * 64, a.map.v_codes + at * 64, len * 64, &sh.full[st]);
-        }
-        const uint32_t to = smem_u32(scales + c * 8);
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(a.map.k_scales + at * 8) : "memory");
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to + kBlock * 8), "l"(a.map.v_scales + at * 8) : "memory");
-      }
-      asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.full[st])) : "memory");
-    }
-    // Copies in flight land before the CTA's memory goes to another (its
-    // consumers have waited for them unless a wait ran out).
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    if (sh.abort)
-      for (int i = max(n - 2, 0); i < n; ++i) mbar_wait_bounded(&sh.full[i & 1], (i >> 1) & 1, nullptr, kDrainLimitNs);
-    return;
-  }
-
-  // ------------------------------------------------------------- consumers ---
-  const int cw = warp - 1, g = lane >> 2, t = lane & 3;
-  // Rows of the lane's columns in a group's tile of scores: 2t and 2t + 1.
-  int2 vis[kN][2];
-  float mult[kN][2], slope[kN][2];
-  int pos[kN][2];
-  int all_lo = 0, all_hi = 0x7fffffff;  // keys that every row sees
-#pragma unroll
-  for (int x = 0; x < kN; ++x)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const uint32_t lr = 8 * x + 2 * t + c;
-      const bool live = lr < rows;
-      const uint32_t r = tile.row0 + (live ? lr : 0), tok = a.group.div(r), h = kvh * group + (r - tok * group);
-      const int p = seq.len - static_cast<int>(seq.n) + static_cast<int>(tok);
-      vis[x][c] = visible(a, p, seq.len, a.prefix_lens ? __ldg(a.prefix_lens + tile.b) : 0,
-                          a.doc_start ? __ldg(a.doc_start + seq.first + tok) : 0);
-      if (!live || p < 0) vis[x][c] = make_int2(0x7fffffff, 0);
-      if (live) {
-        all_lo = max(all_lo, vis[x][c].x);
-        all_hi = min(all_hi, vis[x][c].y);
-      }
-      pos[x][c] = p;
-      slope[x][c] = kMods && a.slopes && live ? __ldg(a.slopes + h) * kLog2e : 0.0f;
-    }
-  all_lo = __reduce_max_sync(0xffffffffu, all_lo);
-  all_hi = __reduce_min_sync(0xffffffffu, all_hi);
-  // Queries: f16 after an exact scaling by a power of two to below 1.
-  uint32_t qf[16];
-#pragma unroll
-  for (int x = 0; x < kN; ++x) {
-    const uint32_t lr = 8 * x + g;
-    const bool live = lr < rows;
-    const uint32_t r = tile.row0 + (live ? lr : 0), tok = a.group.div(r);
-    const uint4* src = reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(seq.first + tok) * a.ld_q +
-                                                      (kvh * group + (r - tok * group)) * kD + 32 * t);
-    uint4 w[4];
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[i] = live ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
-      top = max(top, amax_bits_bf16x8(w[i]));
-    }
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int e = max(-125, min(static_cast<int>(top >> 7) - 126, 126));
-    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-    const float up = a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
-    mult[x][0] = __shfl_sync(0xffffffffu, up, (2 * t) * 4);
-    mult[x][1] = __shfl_sync(0xffffffffu, up, (2 * t + 1) * 4);
-    float v[32];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) unpack_bf16x8(w[i], v + 8 * i);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      // Channels of k-step j, in the order of pairs8.
-      const int c0 = kE1M2 ? 8 * (j >> 1) + 2 * (j & 1) : 4 * j;
-      const int c1 = kE1M2 ? c0 + 4 : c0 + 1, c2 = kE1M2 ? c0 + 1 : c0 + 2, c3 = kE1M2 ? c0 + 5 : c0 + 3;
-      const uint2 f = make_uint2(f16x2_rn(v[c0] * down, v[c1] * down), f16x2_rn(v[c2] * down, v[c3] * down));
-      if (kN == 1) {
-        qf[2 * j] = f.x;
-        qf[2 * j + 1] = f.y;
-      } else if (cw == 0) {
-        sh.q[x][j][lane] = f;
-      }
-    }
-  }
-  if (kN > 1) asm volatile("bar.sync 1, %0;" ::"n"(32 * kRowsWarps) : "memory");
-
-  float o[kN][8][4], m_run[kN][2], l_run[kN][2];
-#pragma unroll
-  for (int x = 0; x < kN; ++x) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[x][i][0] = o[x][i][1] = o[x][i][2] = o[x][i][3] = 0.0f;
-    m_run[x][0] = m_run[x][1] = -INFINITY;
-    l_run[x][0] = l_run[x][1] = 0.0f;
-  }
-  const int rk0 = tile_key(g), rk1 = tile_key(g + 8);
-  const int rv[4] = {tile_key(2 * t), tile_key(2 * t + 1), tile_key(2 * t + 8), tile_key(2 * t + 9)};
-  bool ok = true;
-  for (int i = 0; i < n; ++i) {
-    const int st = i & 1;
-    ok = __all_sync(0xffffffffu, wait_bar(&sh.full[st], (i >> 1) & 1, &sh.abort));
-    if (!ok) {
-      if (lane == 0 && !sh.abort) {
-        set_status(a.status, NVFP4_ERR_TIMEOUT);
-        sh.abort = 1;
-      }
-      break;
-    }
-    const uint8_t* stage = smem_raw + st * kStageBytes;
-    const uint8_t* k_scales = stage + 2 * kStageCodes;
-    const uint8_t* v_scales = k_scales + kBlock * 8;
-#pragma unroll(kN == 1 ? 2 : 1)
-    for (int sub = 0; sub < kBlock / (16 * kRowsWarps); ++sub) {
-      const int r0 = 16 * (cw + kRowsWarps * sub), t0 = t_base + i * kBlock + r0;
-      const uint32_t there = (sh.present[st][r0 >> 5] >> (r0 & 31)) & 0xFFFFu;
-      if (!there) continue;
-      // ---- S^T = K Q^T: 8 k-steps of 16 channels --------------------------
-      const uint4 ka = *reinterpret_cast<const uint4*>(stage + (r0 + rk0) * 64 + 16 * t);
-      const uint4 kb = *reinterpret_cast<const uint4*>(stage + (r0 + rk1) * 64 + 16 * t);
-      const uint32_t ksa = kv_scales16<kE1M2>(*reinterpret_cast<const uint16_t*>(k_scales + (r0 + rk0) * 8 + 2 * t));
-      const uint32_t ksb = kv_scales16<kE1M2>(*reinterpret_cast<const uint16_t*>(k_scales + (r0 + rk1) * 8 + 2 * t));
-      const uint32_t sa_lo = __byte_perm(ksa, ksa, 0x1010), sa_hi = __byte_perm(ksa, ksa, 0x3232);
-      const uint32_t sb_lo = __byte_perm(ksb, ksb, 0x1010), sb_hi = __byte_perm(ksb, ksb, 0x3232);
-      float s[kN][4];
-#pragma unroll
-      for (int x = 0; x < kN; ++x) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.0f;
-      const uint32_t kaw[4] = {ka.x, ka.y, ka.z, ka.w}, kbw[4] = {kb.x, kb.y, kb.z, kb.w};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint32_t ha[4], hb[4];
-        pairs8<kE1M2>(kaw[w], ha);
-        pairs8<kE1M2>(kbw[w], hb);
-        const uint32_t sa = w < 2 ? sa_lo : sa_hi, sb = w < 2 ? sb_lo : sb_hi;
-        const uint32_t sa1 = kE1M2 ? mul_f16x2(sa, 0x2C002C00u) : sa, sb1 = kE1M2 ? mul_f16x2(sb, 0x2C002C00u) : sb;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t f[4] = {mul_f16x2(ha[2 * h], sa), mul_f16x2(hb[2 * h], sb), mul_f16x2(ha[2 * h + 1], sa1),
-                                 mul_f16x2(hb[2 * h + 1], sb1)};
-          const int j = 2 * w + h;
-#pragma unroll
-          for (int x = 0; x < kN; ++x) {
-            const uint2 b = kN == 1 ? make_uint2(qf[2 * j], qf[2 * j + 1]) : sh.q[x][j][lane];
-            mma16816(s[x], f, b.x, b.y);
-          }
-        }
-      }
-      // ---- scores, masks, the running maximum ------------------------------
-      const bool open = t0 >= all_lo && t0 + 16 <= all_hi && there == 0xFFFFu;
-      bool up = false;
-#pragma unroll
-      for (int x = 0; x < kN; ++x) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int key = t0 + (c < 2 ? rk0 : rk1), col = c & 1;
-          float v = s[x][c] * mult[x][col];
-          if (kMods) {
-            if (a.cap > 0.0f) {
-              const float out = a.cap * kLog2e;
-              v = fmaf(-2.0f * out, rcp(1.0f + ex2(v * (2.0f / a.cap))), out);
-            }
-            v = fmaf(-slope[x][col], fabsf(static_cast<float>(pos[x][col] - key)), v);
-          }
-          if (!open && (key < vis[x][col].x || key >= vis[x][col].y || !((there >> (key - t0)) & 1u))) v = -INFINITY;
-          s[x][c] = v;
-          up = up || v > m_run[x][col] + kRescaleLog2;
-        }
-      }
-      if (__any_sync(0xffffffffu, up)) {
-#pragma unroll
-        for (int x = 0; x < kN; ++x)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            float top = fmaxf(s[x][c], s[x][c + 2]);
-#pragma unroll
-            for (int sh_ = 4; sh_ < 32; sh_ <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, sh_));
-            if (top > m_run[x][c] + kRescaleLog2) {
-              const float shrink = ex2(m_run[x][c] - top);
-              m_run[x][c] = top;
-              l_run[x][c] *= shrink;
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                o[x][k][c] *= shrink;
-                o[x][k][c + 2] *= shrink;
-              }
-            }
-          }
-      }
-      uint32_t pb[kN][2];
-#pragma unroll
-      for (int x = 0; x < kN; ++x) {
-        const float b0 = (m_run[x][0] == -INFINITY ? 0.0f : -m_run[x][0]) + kWeightLog2;
-        const float b1 = (m_run[x][1] == -INFINITY ? 0.0f : -m_run[x][1]) + kWeightLog2;
-        const float p0 = ex2(s[x][0] + b0), p1 = ex2(s[x][1] + b1), p2 = ex2(s[x][2] + b0), p3 = ex2(s[x][3] + b1);
-        l_run[x][0] += p0 + p2;
-        l_run[x][1] += p1 + p3;
-        pb[x][0] = transposed(f16x2_rn(p0, p1));
-        pb[x][1] = transposed(f16x2_rn(p2, p3));
-      }
-      // ---- O^T += V^T P^T: 8 m-tiles, m-tile k = channels 16g+2k, 16g+2k+1 --
-      const uint32_t vs01 = kv_scales16<kE1M2>(v_scales[(r0 + rv[0]) * 8 + g] | v_scales[(r0 + rv[1]) * 8 + g] << 8);
-      const uint32_t vs89 = kv_scales16<kE1M2>(v_scales[(r0 + rv[2]) * 8 + g] | v_scales[(r0 + rv[3]) * 8 + g] << 8);
-      const uint32_t vs01_hi = kE1M2 ? mul_f16x2(vs01, 0x2C002C00u) : vs01;
-      const uint32_t vs89_hi = kE1M2 ? mul_f16x2(vs89, 0x2C002C00u) : vs89;
-      uint2 vw[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) vw[k] = *reinterpret_cast<const uint2*>(stage + kStageCodes + (r0 + rv[k]) * 64 + 8 * g);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {  // channels 16g..16g+7, then the other eight
-        const uint32_t wa = half ? vw[0].y : vw[0].x, wb = half ? vw[1].y : vw[1].x;
-        const uint32_t wc = half ? vw[2].y : vw[2].x, wd = half ? vw[3].y : vw[3].x;
-        uint32_t lo_ab[4], hi_ab[4], lo_cd[4], hi_cd[4];
-        if (kE1M2) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {  // byte k of two keys: its low-nibble channel, and 16 times its high one
-            const uint32_t ab = __byte_perm(wa, wb, 0x4400u + 0x1111u * k), cd = __byte_perm(wc, wd, 0x4400u + 0x1111u * k);
-            lo_ab[k] = sub_f16x2((ab & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
-            hi_ab[k] = sub_f16x2((ab & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
-            lo_cd[k] = sub_f16x2((cd & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
-            hi_cd[k] = sub_f16x2((cd & 0x00F000F0u) ^ 0x64806480u, 0x64806480u);
-          }
-        } else {  // the same channel of two keys in one byte, the first key in its low nibble
-          elements8<false>((wa & 0x0F0F0F0Fu) | ((wb << 4) & 0xF0F0F0F0u), lo_ab);
-          elements8<false>(((wa >> 4) & 0x0F0F0F0Fu) | (wb & 0xF0F0F0F0u), hi_ab);
-          elements8<false>((wc & 0x0F0F0F0Fu) | ((wd << 4) & 0xF0F0F0F0u), lo_cd);
-          elements8<false>(((wc >> 4) & 0x0F0F0F0Fu) | (wd & 0xF0F0F0F0u), hi_cd);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t f[4] = {mul_f16x2(lo_ab[k], vs01), mul_f16x2(hi_ab[k], vs01_hi), mul_f16x2(lo_cd[k], vs89),
-                                 mul_f16x2(hi_cd[k], vs89_hi)};
-#pragma unroll
-          for (int x = 0; x < kN; ++x) mma16816(o[x][4 * half + k], f, pb[x][0], pb[x][1]);
-        }
-      }
-    }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sh.empty[st]);
-  }
-
-  // ---- join the warps, one group of rows at a time -------------------------
-  float* merge = reinterpret_cast<float*>(smem_raw + kRing * kStageBytes);
-#pragma unroll
-  for (int x = 0; x < kN; ++x) {
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-#pragma unroll
-      for (int s = 4; s < 32; s <<= 1) l_run[x][c] += __shfl_xor_sync(0xffffffffu, l_run[x][c], s);
-      if (g == 0) {
-        sh.m[cw][8 * x + 2 * t + c] = m_run[x][c];
-        sh.l[cw][8 * x + 2 * t + c] = l_run[x][c];
-      }
-    }
-    float* mine = merge + cw * 8 * kMergeRow;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int c = 18 * g + 2 * k;  // channels 16g + 2k and the next, 2 floats of padding per 16
-      *reinterpret_cast<float2*>(mine + (2 * t) * kMergeRow + c) = make_float2(o[x][k][0], o[x][k][2]);
-      *reinterpret_cast<float2*>(mine + (2 * t + 1) * kMergeRow + c) = make_float2(o[x][k][1], o[x][k][3]);
-    }
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * kRowsWarps) : "memory");
-    const int left = min(8, static_cast<int>(rows) - 8 * x);
-    for (int idx = threadIdx.x - 32; idx < left * (kD / 4); idx += 32 * kRowsWarps) {
-      const int lr = idx / (kD / 4), c = idx % (kD / 4) * 4;
-      float big = -INFINITY, sum = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int w = 0; w < kRowsWarps; ++w) big = fmaxf(big, sh.m[w][8 * x + lr]);
-#pragma unroll
-      for (int w = 0; w < kRowsWarps; ++w) {
-        const float mw = sh.m[w][8 * x + lr], f = mw == -INFINITY ? 0.0f : ex2(mw - big);
-        const float2* from = reinterpret_cast<const float2*>(merge + (w * 8 + lr) * kMergeRow + c + 2 * (c >> 4));
-        const float2 u = from[0], v = from[1];
-        sum = fmaf(f, sh.l[w][8 * x + lr], sum);
-        acc[0] = fmaf(f, u.x, acc[0]);
-        acc[1] = fmaf(f, u.y, acc[1]);
-        acc[2] = fmaf(f, v.x, acc[2]);
-        acc[3] = fmaf(f, v.y, acc[3]);
-      }
-      if (a.splits > 1) {
-        const uint64_t rec = ((static_cast<uint64_t>(tile_id) * a.map.hkv + kvh) * a.splits + split) * kRows + 8 * x + lr;
-        if (c == 0) a.ml_ws[rec] = make_float2(big, sum);
-        if (big != -INFINITY) *reinterpret_cast<float4*>(a.o_ws + rec * kD + c) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-      } else {
-        const float f = sum > 0.0f ? a.gv / sum : 0.0f;
-        const uint32_t r = tile.row0 + 8 * x + lr, tok = a.group.div(r);
-        *reinterpret_cast<uint2*>(a.out + (static_cast<uint64_t>(seq.first + tok) * a.hq + kvh * group + r - tok * group) * kD + c) =
-            make_uint2(bf16x2_rn(acc[0] * f, acc[1] * f), bf16x2_rn(acc[2] * f, acc[3] * f));
-      }
-    }
-    if (x + 1 < kN) asm volatile("bar.sync 1, %0;" ::"n"(32 * kRowsWarps) : "memory");
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kRowsTmem);
   }
 }
 
@@ -1287,12 +1420,12 @@ __global__ void __launch_bounds__(256) extend_combine_kernel(const ExtendArgs a)
 // ---- host ----------------------------------------------------------------
 
 struct Plan {
-  int rows;  // of a tile: kTileRows, or 8, 16, 24 by the rows kernel
+  int rows;  // of a tile: kTileRows, or 8, 16, 24, 32 by the rows kernel
   int64_t tiles, tiles_per_seq, splits;
-  bool full;  // the tile kernel's exact weights
+  bool full;  // weights in two terms (kFull)
 };
 
-// Contexts of up to this many keys take the tile kernel's kFull.
+// Contexts of up to this many keys take kFull.
 constexpr int64_t kFullContext = 512;
 
 // Which kernel, the tiles (at most), and the parts that each tile's keys are cut into.
@@ -1301,7 +1434,7 @@ Plan plan_for(int64_t batch, int64_t n_tokens, int64_t group, int64_t hkv, int64
   const int64_t sms = sm_count(), blocks = (context + kBlock - 1) / kBlock;
   const int64_t rows = (n_tokens * group + batch - 1) / batch;  // of a sequence and KV head, on average
   p.full = context <= kFullContext;
-  p.rows = p.full || rows > 24 ? kTileRows : static_cast<int>((rows + 7) / 8 * 8);
+  p.rows = rows <= 32 ? static_cast<int>((rows + 7) / 8 * 8) : kTileRows;
   p.tiles_per_seq = (n_tokens / batch * group + p.rows - 1) / p.rows;
   const int64_t ragged = n_tokens * group / p.rows + (batch < n_tokens ? batch : n_tokens);
   p.tiles = uniform ? batch * p.tiles_per_seq : ragged;
@@ -1311,7 +1444,7 @@ Plan plan_for(int64_t batch, int64_t n_tokens, int64_t group, int64_t hkv, int64
     // Enough CTAs for six rounds on what is resident, so that sequences of
     // different lengths even out, in parts of 512 keys or more; failing that,
     // one round in parts of a stage or more.
-    const int64_t resident = sms * (p.rows == 8 ? 4 : p.rows == 16 ? 3 : 2);
+    const int64_t resident = sms * 2;
     const int64_t even = (6 * resident + items - 1) / items, long_parts = (blocks + 3) / 4;
     const int64_t fill = (resident + items - 1) / items;
     p.splits = even < long_parts ? even : long_parts;
@@ -1338,24 +1471,27 @@ size_t workspace_for(const Plan& p, int64_t hkv) {
 }
 
 using Kernel = void (*)(const ExtendArgs);
-// Raising the limit is idempotent and cheap; a failure shows at the launch.
-Kernel with_smem(Kernel k, uint32_t bytes) {
-  cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
-  return k;
+uint32_t smem_for(const Plan& p) {
+  return p.rows == kTileRows ? kTileSmem : p.rows <= 16 ? RowsConfig<16>::kBytes : RowsConfig<32>::kBytes;
 }
-template <bool kE1M2, bool kMods>
-Kernel kernel_for(const Plan& p) {
+template <bool kE1M2, bool kFull>
+Kernel kernel_for(const Plan& p, bool mods) {
   switch (p.rows) {
-    case 8: return with_smem(extend_rows_kernel<1, kE1M2, kMods>, kRowsSmem);
-    case 16: return with_smem(extend_rows_kernel<2, kE1M2, kMods>, kRowsSmem);
-    case 24: return with_smem(extend_rows_kernel<3, kE1M2, kMods>, kRowsSmem);
+    case 8: return extend_rows_kernel<8, kE1M2, kFull>;
+    case 16: return extend_rows_kernel<16, kE1M2, kFull>;
+    case 24: return extend_rows_kernel<24, kE1M2, kFull>;
+    case 32: return extend_rows_kernel<32, kE1M2, kFull>;
   }
-  return p.full ? with_smem(extend_tile_kernel<kE1M2, kMods, true>, kTileSmem)
-                : with_smem(extend_tile_kernel<kE1M2, kMods, false>, kTileSmem);
+  return mods ? extend_tile_kernel<kE1M2, true, kFull> : extend_tile_kernel<kE1M2, false, kFull>;
 }
 Kernel combine_for(const Plan& p) {
-  return p.rows == 8 ? extend_combine_kernel<8> : p.rows == 16 ? extend_combine_kernel<16>
-         : p.rows == 24 ? extend_combine_kernel<24> : extend_combine_kernel<kTileRows>;
+  switch (p.rows) {
+    case 8: return extend_combine_kernel<8>;
+    case 16: return extend_combine_kernel<16>;
+    case 24: return extend_combine_kernel<24>;
+    case 32: return extend_combine_kernel<32>;
+  }
+  return extend_combine_kernel<kTileRows>;
 }
 
 }  // namespace
@@ -1427,12 +1563,14 @@ NVFP4_API nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const
   a.o_ws = static_cast<float*>(workspace);
   a.ml_ws = reinterpret_cast<float2*>(a.o_ws + static_cast<size_t>(grid) * p.rows * kD);
   const bool mods = options->logit_cap > 0.0f || options->slopes, e1m2 = cache->kv_format == NVFP4_KV_E1M2;
-  const Kernel kernel = e1m2 ? (mods ? kernel_for<true, true>(p) : kernel_for<true, false>(p))
-                             : (mods ? kernel_for<false, true>(p) : kernel_for<false, false>(p));
+  const Kernel kernel = e1m2 ? (p.full ? kernel_for<true, true>(p, mods) : kernel_for<true, false>(p, mods))
+                             : (p.full ? kernel_for<false, true>(p, mods) : kernel_for<false, false>(p, mods));
   const bool by_tiles = p.rows == kTileRows;
+  const uint32_t smem = smem_for(p);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (launch_pdl(kernel, dim3(static_cast<uint32_t>(grid)), dim3(by_tiles ? kTileThreads : kRowsThreads),
-                 by_tiles ? kTileSmem : kRowsSmem, s, a) != cudaSuccess)
+  // Raising the limit is idempotent.
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess ||
+      launch_pdl(kernel, dim3(static_cast<uint32_t>(grid)), dim3(by_tiles ? kTileThreads : kRowsThreads), smem, s, a) != cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
   if (p.splits > 1) {
