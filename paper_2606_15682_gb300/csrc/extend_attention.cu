@@ -9,8 +9,10 @@ namespace {
 constexpr int kD = 128;
 constexpr float kLog2e = 1.4426950408889634f;
 
-constexpr float kRescaleLog2 = 8.0f;  // the running maximum moves only when a score exceeds it by 2^8
-constexpr float kWeightLog2 = 7.0f;   // weights are kept as 2^7 w: at most 2^15 in f16, and fine steps below 1
+// The running maximum moves only when a score exceeds it by 2^11: weights are kept
+// as 2^4 w, at most 2^15 in f16, whose steps end at 2^-28 of the maximum.
+constexpr float kRescaleLog2 = 11.0f;
+constexpr float kWeightLog2 = 4.0f;
 
 struct ExtendArgs {
   KVMap map;
@@ -131,7 +133,7 @@ struct RowScore {
 // A CTA holds 256 rows as two 128-row tiles, streams blocks of 128 keys, and
 // computes S = Q K^T and O += P V with tcgen05.mma kind::f16, 64 keys at a time.
 //   warps 0-3, 4-7  softmax of tile 0 and 1 (thread = row): read S from TMEM,
-//                   write P over it, rescale O where a maximum moved by over 2^8
+//                   write P over it, rescale O where a maximum moved
 //   warps 8-15      dequantize the blocks' K and V into shared memory (f16,
 //                   exact: an E2M1 x E4M3 product has at most 6 significant
 //                   bits), one warpgroup each
@@ -329,7 +331,7 @@ __device__ __forceinline__ uint32_t bf16x2_of_f16x2(uint32_t h) {
 }
 
 // kFull: weights as two bf16 terms (16 significant bits at fp32's range) and V in
-// bf16, a second PV product per block.  In f16 a weight below 2^-31 of the row's
+// bf16, a second PV product per block.  In f16 a weight below 2^-28 of the row's
 // largest is lost, which shows only where all heavier keys hold a zero in a
 // channel: among few keys.
 template <bool kE1M2, bool kMods, bool kFull>
@@ -859,13 +861,13 @@ struct RowInfo {
 };
 template <int kC>
 struct RowsShared {
-  uint64_t s_full[2], s_free[2], k_full[2], k_free[2], v_full[2], v_free[2], p_full[2], drain, drain_qk;
+  uint64_t s_full[2], s_free[2], k_full[2], k_free[2], v_full[2], v_free[2], p_full[2], q_full, drain, drain_qk;
   uint32_t tmem;
   Tile tile;
   Seq seq;
   int lo, hi, all_lo, all_hi, rows;
   alignas(16) float mult[kC];   // score -> log2 domain
-  alignas(16) float minus[kC];  // 7 - the row's maximum: x = score + minus is a weight's exponent
+  alignas(16) float minus[kC];  // 4 - the row's maximum: x = score + minus is a weight's exponent
   RowInfo row[kC];
   float top[4][kC], sum[4][kC];
   uint32_t present[4][4];
@@ -931,6 +933,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
     }
     mbar_init(&sh.drain, 1);
     mbar_init(&sh.drain_qk, 1);
+    mbar_init(&sh.q_full, 4);
     sh.abort = 0;
     fence_mbar_init();
   }
@@ -1012,8 +1015,10 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
     return ok;
   };
 
+  // 104, 64, 64 and 24 registers a thread: the 512 x 64 that the CTA starts with.
   if (warp < 4) {
     // ------------------------------------------------------------- softmax ---
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
     // Q rows as f16, scaled by a power of two (exact) to below 1: 16 lanes a row.
     uint4 w[kN / 8];
 #pragma unroll
@@ -1045,12 +1050,9 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       sts128(smem + C::kOffQ + (c >> 3) * (kN * 128) + lr * 128 + (((c ^ lr) & 7) << 4), f.x, f.y, f.z, f.w);
     }
     fence_proxy_async_smem();
-  }
-  __syncthreads();
-
-  // 104, 64, 64 and 24 registers a thread: the 512 x 64 that the CTA starts with.
-  if (warp < 4) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.q_full);
+    any_of_128(false);  // the multipliers of all rows
     const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
     const int key = warp * 32 + lane;
     const bool mods = a.cap > 0.0f || a.slopes;
@@ -1089,7 +1091,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         for (int n = 0; n < kC; ++n)
           if (!there || tk < sh.row[n].lo || tk >= sh.row[n].hi) s[n] = -INFINITY;
       }
-      // Maxima move only where a weight would exceed 2^8 of its row's maximum.
+      // Maxima move only where a weight would be 2^11 times its row's maximum.
       for (;;) {
         float most = -INFINITY;
 #pragma unroll
@@ -1338,7 +1340,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
             tc_commit(&sh.v_free[b]);
           }
         } else {
-          if (!wait(&sh.k_full[b], j >> 1) || (j >= 2 && !wait(&sh.s_free[b], (j >> 1) ^ 1))) break;
+          if ((j == 0 && !wait(&sh.q_full, 0)) || !wait(&sh.k_full[b], j >> 1) || (j >= 2 && !wait(&sh.s_free[b], (j >> 1) ^ 1))) break;
           if (leader) {
             constexpr uint32_t kIdesc = (1u << 4) | (static_cast<uint32_t>(kN / 8) << 17) | (8u << 24);
 #pragma unroll
