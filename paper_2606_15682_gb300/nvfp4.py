@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -54,6 +55,12 @@ class AttentionOptionsStruct(ctypes.Structure):
                 ("prefix_lens", _p), ("doc_start", _p)]
 
 
+# The same structs as bytes: one call makes them.
+_CACHE, _PAGES, _OPTIONS = struct.Struct("PPPPPiiiiffi4x"), struct.Struct("PPii"), struct.Struct("ffPi4xPP")
+assert (_CACHE.size, _PAGES.size, _OPTIONS.size) == tuple(
+    ctypes.sizeof(t) for t in (KVCacheStruct, KVPagesStruct, AttentionOptionsStruct))
+
+
 def _sig(name, args, res=ctypes.c_int):
     f = getattr(_lib, name)
     f.argtypes = args
@@ -82,13 +89,11 @@ _qfit_ws = _sig("nvfp4_qfit_workspace_size", [_i32, _i32, _i32, _i32, _i32, _i32
 _qfit = _sig("nvfp4_qfit_calibrate", [_p, _p, _p, _i32, _i32, _i32, _i32, _i32, _p, _i64, _i32, _i32,
                                       ctypes.c_double, _i32, _p, _p, _p, _p, _p, _sz, _p])
 _append_axes = _sig("kv_append_rope_axes_nvfp4",
-                    [ctypes.POINTER(KVCacheStruct), _p, _p, _i64, _i32, _p, _i64, _p, _i64, _p, _p, _p, _i32,
-                     ctypes.c_char_p, _i64, _p, _i64, _p, _p, _p])
-_kv_read = _sig("kv_read_nvfp4", [ctypes.POINTER(KVCacheStruct), _p, _p, _p, _i64, _p, _p, _p])
+                    [_p, _p, _p, _i64, _i32, _p, _i64, _p, _i64, _p, _p, _p, _i32, _p, _i64, _p, _i64, _p, _p, _p])
+_kv_read = _sig("kv_read_nvfp4", [_p, _p, _p, _p, _i64, _p, _p, _p])
 _extend_ws = _sig("extend_attention_nvfp4_workspace_size", [_i32, _i64, _i32, _i32, _i64], _sz)
 _extend = _sig("extend_attention_nvfp4",
-               [ctypes.POINTER(KVCacheStruct), _p, _p, _i64, _i64, _i32, _p, ctypes.POINTER(AttentionOptionsStruct), _p,
-                _p, _sz, _p])
+               [_p, _p, _p, _i64, _i64, _i32, _p, _p, _p, _p, _sz, _p])
 _residual_norm = _sig("residual_norm_nvfp4", [_p, _i64, _p, _i64, _i64, _i64, _p, _p, _i64, _f32, _p, _f32, _p, _p, _p,
                                               _p, _p, _p])
 _get_status = _sig("nvfp4_get_device_status", [ctypes.POINTER(_i32), _p])
@@ -277,26 +282,28 @@ def decode_attention_nvfp4_static_scratch(cache, q, softmax_scale, out, stream=N
                                                                  _ptr(out), _stream(stream)))
 
 
-def _rows3(x, heads=None):
-    """(pointer, tokens, heads, elements between tokens) of a [tokens, heads, 128] tensor that may be a slice of a
-    wider projection output."""
-    if x.dim() != 3 or x.shape[2] != 128 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != 128):
-        raise ValueError("expected a [tokens, heads, 128] tensor with dense heads")
-    n, h = x.shape[0], x.shape[1]
-    return ctypes.c_void_p(x.data_ptr()), n, h, x.stride(0) if n > 1 else h * 128
+# The calls of a decode step are short, and so is their marshalling: plain integers for
+# pointers, each tensor looked at once, the structs packed (include/nvfp4.h's layout).
+_bf16, _int32, _float32 = torch.bfloat16, torch.int32, torch.float32
 
 
-def _pages(pages):
-    return None if pages is None else ctypes.byref(pages.struct())
+def _rows3(x, what):
+    """(pointer, tokens, heads, elements between tokens) of a bf16 [tokens, heads, 128] tensor that may be a slice of
+    a wider projection output."""
+    n, h, d = x.shape
+    between, head, last = x.stride()
+    if d != 128 or last != 1 or (h > 1 and head != 128) or x.dtype is not _bf16:
+        raise ValueError(f"{what} must be a bfloat16 [tokens, heads, 128] tensor with dense heads")
+    return x.data_ptr(), n, h, between if n > 1 else h * 128
 
 
 def _typed(t, dtype, what, numel=None):
-    """Device pointer of an optional argument whose element type the call fixes."""
+    """Device pointer of a dense argument whose element type the call fixes; None -> NULL."""
     if t is None:
         return None
-    if t.dtype != dtype or (numel is not None and t.numel() != numel):
-        raise ValueError(f"{what} must be {dtype}" + ("" if numel is None else f" with {numel} elements"))
-    return _ptr(t)
+    if t.dtype is not dtype or not t.is_contiguous() or (numel is not None and t.numel() != numel):
+        raise ValueError(f"{what} must be contiguous {dtype}" + ("" if numel is None else f" with {numel} elements"))
+    return t.data_ptr()
 
 
 def kv_append_rope_axes_nvfp4(cache, q, k, v, seq_idx, pos, rope_pos, axis_of_pair, rope_table, q_out, k_shift=None,
@@ -304,40 +311,37 @@ def kv_append_rope_axes_nvfp4(cache, q, k, v, seq_idx, pos, rope_pos, axis_of_pa
     """Rotate q (-> q_out) and k by rotary positions rope_pos [n, axes] and append k and v to the (paged) cache.
 
     q, k, v: [n, heads, 128] bf16, may be slices of one projection output; q and q_out may be None.
-    axis_of_pair: 64 integers, the axis that rotates each channel pair (c, c + 64).
+    axis_of_pair: 64 integers (a bytes object is taken as it is), the axis that rotates each channel pair (c, c + 64).
     """
-    kp, n, hk, ld_k = _rows3(k)
-    vp, nv, hv, ld_v = _rows3(v)
-    qp, nq, hq, ld_q = _rows3(q) if q is not None else (None, n, 0, 0)
-    if not (n == nv == nq == rope_pos.shape[0]) or hk != cache.num_kv_heads or hv != hk:
+    kp, n, hk, ld_k = _rows3(k, "k")
+    vp, nv, hv, ld_v = _rows3(v, "v")
+    qp, nq, hq, ld_q = _rows3(q, "q") if q is not None else (None, n, 0, 0)
+    n_rope, axes = rope_pos.shape
+    if not (n == nv == nq == n_rope) or hk != cache.num_kv_heads or hv != hk:
         raise ValueError("q, k, v and rope_pos must have the same tokens, k and v the cache's heads")
-    if q is not None and (q_out is None or q_out.numel() != n * hq * 128):
+    if q is not None and q_out is None:
         raise ValueError("q_out must hold the rotated queries")
-    axes = bytes(axis_of_pair)
-    if len(axes) != 64:
+    if type(axis_of_pair) is not bytes:
+        axis_of_pair = bytes(axis_of_pair)
+    if len(axis_of_pair) != 64:
         raise ValueError("axis_of_pair must have 64 entries")
-    bf = torch.bfloat16
-    if k.dtype != bf or v.dtype != bf or (q is not None and (q.dtype != bf or q_out.dtype != bf)):
-        raise ValueError("q, k, v and q_out must be bfloat16")
-    s = cache.struct()
     _check("kv_append_rope_axes_nvfp4",
-           _append_axes(ctypes.byref(s), _pages(pages), qp, ld_q, hq, kp, ld_k, vp, ld_v,
-                        _typed(seq_idx, torch.int32, "seq_idx", n), _typed(pos, torch.int32, "pos", n),
-                        _typed(rope_pos, torch.int32, "rope_pos"), rope_pos.shape[1], axes, n,
-                        _typed(rope_table, torch.float32, "rope_table"), rope_table.shape[0],
-                        _typed(k_shift, torch.float32, "k_shift", hk * 128),
-                        _ptr(q_out) if q is not None else None, _stream(stream)))
+           _append_axes(cache.packed(), None if pages is None else pages.packed(), qp, ld_q, hq, kp, ld_k, vp, ld_v,
+                        _typed(seq_idx, _int32, "seq_idx", n), _typed(pos, _int32, "pos", n),
+                        _typed(rope_pos, _int32, "rope_pos"), axes, axis_of_pair, n,
+                        _typed(rope_table, _float32, "rope_table"), len(rope_table),
+                        None if k_shift is None else _typed(k_shift, _float32, "k_shift", hk * 128),
+                        None if q is None else _typed(q_out, _bf16, "q_out", n * hq * 128), _stream(stream)))
 
 
 def kv_read_nvfp4(cache, seq_idx, pos, k_out, v_out, pages=None, stream=None):
     """Cached rows (seq_idx[i], pos[i]) as bf16 [n, kv heads, 128]; k_out or v_out may be None."""
     n = seq_idx.numel()
     size = n * cache.num_kv_heads * 128
-    s = cache.struct()
     _check("kv_read_nvfp4",
-           _kv_read(ctypes.byref(s), _pages(pages), _typed(seq_idx, torch.int32, "seq_idx"),
-                    _typed(pos, torch.int32, "pos", n), n, _typed(k_out, torch.bfloat16, "k_out", size),
-                    _typed(v_out, torch.bfloat16, "v_out", size), _stream(stream)))
+           _kv_read(cache.packed(), None if pages is None else pages.packed(), _typed(seq_idx, _int32, "seq_idx"),
+                    _typed(pos, _int32, "pos", n), n, _typed(k_out, _bf16, "k_out", size),
+                    _typed(v_out, _bf16, "v_out", size), _stream(stream)))
 
 
 def extend_attention_nvfp4_workspace_size(batch, n_tokens, num_q_heads, num_kv_heads, context):
@@ -348,38 +352,47 @@ def extend_attention_nvfp4_workspace_size(batch, n_tokens, num_q_heads, num_kv_h
 def extend_attention_nvfp4(cache, q, softmax_scale, out, workspace, q_start=None, pages=None, logit_cap=0.0, window=0,
                            slopes=None, prefix_lens=None, doc_start=None, stream=None):
     """Attention of the new tokens q [n_tokens, heads, 128] over the cache that holds them (see include/nvfp4.h)."""
-    qp, n, hq, ld_q = _rows3(q)
+    qp, n, hq, ld_q = _rows3(q, "q")
     batch = cache.batch if pages is None else pages.batch
-    if q.dtype != torch.bfloat16:
-        raise ValueError("q must be bfloat16")
-    i32 = torch.int32
-    o = AttentionOptionsStruct(softmax_scale, logit_cap, _typed(slopes, torch.float32, "slopes", hq), window,
-                               _typed(prefix_lens, i32, "prefix_lens", batch), _typed(doc_start, i32, "doc_start", n))
-    s = cache.struct()
+    options = _OPTIONS.pack(softmax_scale, logit_cap, _typed(slopes, _float32, "slopes", hq) or 0, window,
+                            _typed(prefix_lens, _int32, "prefix_lens", batch) or 0,
+                            _typed(doc_start, _int32, "doc_start", n) or 0)
     _check("extend_attention_nvfp4",
-           _extend(ctypes.byref(s), _pages(pages), qp, ld_q, n, hq, _typed(q_start, i32, "q_start", batch + 1),
-                   ctypes.byref(o), _typed(out, torch.bfloat16, "out", n * hq * 128), _ptr(workspace),
-                   0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+           _extend(cache.packed(), None if pages is None else pages.packed(), qp, ld_q, n, hq,
+                   _typed(q_start, _int32, "q_start", batch + 1), options, _typed(out, _bf16, "out", n * hq * 128),
+                   *((None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)), _stream(stream)))
 
 
 def residual_norm_nvfp4(x, y, r_out, h_out, w_norm, eps=1e-6, w_post=None, gate=None, rows_per_gate=1, alpha=1.0,
                         g_out=None, codes=None, scales=None, stream=None):
     """r = x + alpha * (y, normed by w_post, gated); h = norm of r: bf16 (h_out) and / or NVFP4 (codes, scales, g_out).
     y, r_out, h_out, w_norm may be None."""
-    xp, rows, cols, ld_x = _mat(x)
-    yp, yr, yc, ld_y = _mat(y) if y is not None else (None, rows, cols, 0)
-    bf = torch.bfloat16
-    if (yr, yc) != (rows, cols) or x.dtype != bf or (y is not None and y.dtype != bf):
-        raise ValueError("x and y must be bfloat16 of the same shape")
+    rows, cols = x.shape
+    ld_x, step = x.stride()
+    ld_y, yp = 0, None
+    if x.dtype is not _bf16 or (cols > 1 and step != 1):
+        raise ValueError("x must be row-major bfloat16")
+    if y is not None:
+        ld_y, step = y.stride()
+        yp = y.data_ptr()
+        if y.dtype is not _bf16 or y.shape != x.shape or (cols > 1 and step != 1):
+            raise ValueError("y must be row-major bfloat16 of x's shape")
+    if rows == 1:
+        ld_x, ld_y = cols, cols
     if gate is None:
         rows_per_gate = 1
-    elif gate.shape[-1] != cols or rows_per_gate < 1 or gate.numel() != -(-rows // rows_per_gate) * cols:
+    elif rows_per_gate < 1 or gate.shape[-1] != cols or gate.numel() != -(-rows // rows_per_gate) * cols:
         raise ValueError("gate must be [ceil(rows / rows_per_gate), cols]")
     n = rows * cols
+    if codes is not None and (codes.numel() != n // 2 or scales is None or g_out is None or
+                              scales.numel() != _scales_bytes(rows, cols, SCALES_MMA)):
+        raise ValueError("codes [rows, cols/2] come with g_out and MMA-layout scales")
     _check("residual_norm_nvfp4",
-           _residual_norm(xp, ld_x, yp, ld_y, rows, cols, _typed(w_post, bf, "w_post", cols), _typed(gate, bf, "gate"),
-                          rows_per_gate, alpha, _typed(w_norm, bf, "w_norm", cols), eps, _typed(r_out, bf, "r_out", n),
-                          _typed(h_out, bf, "h_out", n), _ptr(g_out), _ptr(codes), _ptr(scales), _stream(stream)))
+           _residual_norm(x.data_ptr(), ld_x, yp, ld_y, rows, cols, _typed(w_post, _bf16, "w_post", cols),
+                          _typed(gate, _bf16, "gate"), rows_per_gate, alpha, _typed(w_norm, _bf16, "w_norm", cols), eps,
+                          _typed(r_out, _bf16, "r_out", n), _typed(h_out, _bf16, "h_out", n),
+                          _typed(g_out, _float32, "g_out"), _typed(codes, torch.uint8, "codes"),
+                          _typed(scales, torch.uint8, "scales"), _stream(stream)))
 
 
 def nvfp4_qfit_workspace_size(batch, tokens, num_q_heads, num_kv_heads, grid_s, grid_m):
@@ -432,6 +445,12 @@ class KVCache:
         self.v_scales = torch.zeros_like(self.k_scales)
         self.seq_lens = torch.zeros(batch, dtype=torch.int32, device=device)
 
+    def packed(self):
+        """The nvfp4_kv_cache's bytes, for the calls that take it packed."""
+        return _CACHE.pack(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
+                           self.v_scales.data_ptr(), self.seq_lens.data_ptr(), self.batch, self.num_kv_heads,
+                           self.head_dim, self.capacity, self.k_gscale, self.v_gscale, self.kv_format)
+
     def struct(self):
         return KVCacheStruct(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
                              self.v_scales.data_ptr(), self.seq_lens.data_ptr(), self.batch, self.num_kv_heads,
@@ -444,13 +463,13 @@ class KVPages:
 
     def __init__(self, table, seq_lens):
         if table.dtype != torch.int32 or table.dim() != 2 or seq_lens.dtype != torch.int32 or \
-                seq_lens.numel() != table.shape[0]:
-            raise ValueError("table must be int32 [batch, pages_per_seq], seq_lens int32 [batch]")
+                seq_lens.numel() != table.shape[0] or not table.is_contiguous() or not seq_lens.is_contiguous():
+            raise ValueError("table must be int32 [batch, pages_per_seq], seq_lens int32 [batch], both contiguous")
         self.table, self.seq_lens = table, seq_lens
         self.batch, self.pages_per_seq = table.shape
 
-    def struct(self):
-        return KVPagesStruct(_ptr(self.table), _ptr(self.seq_lens), self.batch, self.pages_per_seq)
+    def packed(self):
+        return _PAGES.pack(self.table.data_ptr(), self.seq_lens.data_ptr(), self.batch, self.pages_per_seq)
 
 
 EXPORTED = ["nvfp4_scales_bytes", "nvfp4_tensor_scale", "nvfp4_quantize", "nvfp4_quantize_dynamic", "nvfp4_scales_relayout", "nvfp4_linear",
