@@ -41,9 +41,10 @@ struct AppendArgs {
 // HBM-bound at prompt sizes: a token reads 256 bytes for each of its heads and writes
 // 256 (Q) or 72 (K, V), and its table rows come from L2.  The next head's loads are
 // issued before a head is rotated (8192 tokens of 64 + 2 x 8 heads 61 -> 55 us, 84 % of the
-// measured copy rate).
+// measured copy rate; 64 us with the 70 registers that the compiler would take, three CTAs
+// an SM instead of four).
 template <bool kE1M2>
-__global__ void __launch_bounds__(kThreads) append_axes_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) append_axes_kernel(const AppendArgs a) {
   griddep_wait_and_release();
   const uint32_t group = (blockIdx.x * kThreads + threadIdx.x) >> 3, c = threadIdx.x & 7;
   const uint32_t tok_raw = a.split.div(group);
