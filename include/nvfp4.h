@@ -603,18 +603,20 @@ typedef struct {
  * len_b, a document that starts after it, absent pages) gets zeros.  Cached
  * rows past len_b are never used, whatever their bytes.
  * Softmax, sums and products are accumulated in fp32; Q enters the tensor core
- * as f16 after an exact power-of-two scaling of each row, K and V as exact f16,
- * softmax weights rounded to f16.
+ * as f16 after an exact power-of-two scaling of each row, and K as exact f16.
+ * Contexts of at most 512 keys take the softmax weights in two bf16 terms (some
+ * 16 bits) and V as exact bf16; longer ones the weights rounded to f16 (11 bits;
+ * 2^-29 of the largest weight below f16's normal range) and V as exact f16.
  * Where the queries are too few to occupy the GPU, the keys of a group of rows
  * are split and the parts are joined in a fixed order: the result is the same
  * bits in every run for the same arguments, lengths and buffer sizes.
  *   workspace : extend_attention_nvfp4_workspace_size(...) bytes, 16-B aligned
  *              (NULL if that is 0); `context` is the cache's capacity, or
  *              pages_per_seq * page tokens.  Contents on entry are ignored.
- * num_q_heads % num_kv_heads == 0, a group of at most 16, n_tokens % batch == 0
- * where q_start is NULL (SHAPE); softmax_scale > 0, cap and window >= 0, all
- * finite (INVALID_ARG); q, out and cache arrays 16-B aligned, ld_q % 8 == 0
- * (ALIGN).  A length above the capacity is clamped to it, and a length or a
+ * num_q_heads % num_kv_heads == 0, at most 65535 query heads, n_tokens *
+ * num_q_heads < 2^31, n_tokens % batch == 0 where q_start is NULL (SHAPE);
+ * softmax_scale > 0, cap and window >= 0, all finite (INVALID_ARG); q, out and
+ * cache arrays 16-B aligned, ld_q % 8 == 0 (ALIGN).  A length above the capacity is clamped to it, and a length or a
  * q_start out of range is taken as the nearest valid one; both set CAPACITY on
  * the device.  n_tokens == 0 is a no-op.
  */
