@@ -195,7 +195,8 @@ NVFP4_API nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const
   a.group = FastDiv(static_cast<uint32_t>(num_q_heads / cache->num_kv_heads));
   a.window = options->window;
   a.scale = options->softmax_scale * cache->k_gscale;
-  a.cap = options->logit_cap;
+  // The kernels' factors of it and of its inverse stay finite; no score shows the difference.
+  a.cap = options->logit_cap > 0.0f ? fminf(fmaxf(options->logit_cap, 1e-30f), 1e37f) : 0.0f;
   a.gv = cache->v_gscale;
   a.status = status_word_dev();
   const Plan p = plan_for(a.map.batch, n_tokens, a.group.d, a.map.hkv, a.map.context, !q_start);
