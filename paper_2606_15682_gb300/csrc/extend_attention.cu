@@ -208,9 +208,9 @@ NVFP4_API nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const
   a.part_blocks = static_cast<uint32_t>(p.part_blocks);
   a.o_ws = static_cast<float*>(workspace);
   a.ml_ws = reinterpret_cast<float2*>(a.o_ws + static_cast<size_t>(grid) * p.rows * kD);
-  const bool mods = options->logit_cap > 0.0f || options->slopes, e1m2 = cache->kv_format == NVFP4_KV_E1M2;
+  const bool e1m2 = cache->kv_format == NVFP4_KV_E1M2;
   const bool by_tiles = p.rows == kTileRows;
-  const ExtendLaunch l = by_tiles                     ? extend_tiles(e1m2, mods, p.full)
+  const ExtendLaunch l = by_tiles                     ? extend_tiles(e1m2, a.cap > 0.0f, a.slopes != nullptr, p.full)
                          : p.rows == 8 && !p.full ? extend_decode(e1m2)
                                                   : extend_rows(p.rows, e1m2, p.full);
   cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -263,6 +263,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
   return d;
 }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -354,7 +359,7 @@ struct ExtendLaunch {
   ExtendKernel kernel;
   uint32_t threads, smem;
 };
-ExtendLaunch extend_tiles(bool e1m2, bool mods, bool full);  // kTileRows a tile
+ExtendLaunch extend_tiles(bool e1m2, bool cap, bool bias, bool full);  // kTileRows a tile
 ExtendLaunch extend_rows(int rows, bool e1m2, bool full);    // 16, 24, 32; 8 with `full`
 ExtendLaunch extend_decode(bool e1m2);                       // 8
 
