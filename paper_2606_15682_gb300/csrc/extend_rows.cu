@@ -8,7 +8,7 @@
 //   warps 0-3   softmax (thread = key; in the end, channel of O^T)
 //   warps 4-7   K (thread = key)
 //   warps 8-11  V
-//   warp 12, 13 issue the PV and the QK^T; 14, 15 complete the warpgroup
+//   warp 12     issues the MMAs; 13-15 complete its warpgroup
 // Two CTAs share an SM.  What a softmax thread does per block is kept short: the
 // four roles' code does not fit the instruction caches that are near the
 // schedulers, and a role's turn goes by its instructions more than by its work.
@@ -35,12 +35,13 @@ struct RowsConfig {
 
 template <int kC>
 struct RowsShared {
-  uint64_t s_full[2], s_free[2], k_full[2], k_free[2], v_full[2], v_free[2], p_full[2], q_full, drain, drain_qk;
+  uint64_t s_full[2], k_full[2], k_free[2], v_full[2], v_free[2], p_full[2], q_full, drain;
   uint32_t tmem;
   Item item;
   int lo, hi, all_lo, all_hi, rows;
-  alignas(16) float mult[kC];   // score -> log2 domain
-  alignas(16) float minus[kC];  // 4 - the row's maximum: x = score + minus is a weight's exponent
+  alignas(16) float mult[kC];    // score -> log2 domain
+  alignas(16) float factor[kC];  // the same, 1 where a cap has that done
+  alignas(16) float minus[kC], none[kC];  // 4 - the row's maximum: x = score + minus is a weight's exponent
   alignas(16) float slope[kC], pos[kC];  // slopes[h] log2(e); the query's position
   alignas(16) int first[kC], last[kC];  // keys that it sees: first <= t < last
   uint32_t out[kC];                     // its row of the output; past the tile's rows: none
@@ -99,7 +100,6 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.s_full[i], 1);
-      mbar_init(&sh.s_free[i], 4);
       mbar_init(&sh.k_full[i], 4);
       mbar_init(&sh.k_free[i], 1);
       mbar_init(&sh.v_full[i], 4);
@@ -107,7 +107,6 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       mbar_init(&sh.p_full[i], 4);
     }
     mbar_init(&sh.drain, 1);
-    mbar_init(&sh.drain_qk, 1);
     mbar_init(&sh.q_full, 4);
     sh.abort = 0;
     fence_mbar_init();
@@ -218,7 +217,9 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         // No maximum yet: any score exceeds it.  (A row past the tile's has scores of 0.)
         const bool live = sh.out[lr] != 0xffffffffu;
         sh.mult[lr] = live ? a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23) : 0.0f;
+        sh.factor[lr] = a.cap > 0.0f ? 1.0f : sh.mult[lr];
         sh.minus[lr] = live ? 1e30f : 0.0f;
+        sh.none[lr] = 0.0f;
       }
       float x[8];
       unpack_bf16x8(w[i], x);
@@ -238,61 +239,60 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
     for (int j = 0; j < nblk; ++j) {
       const int b = j & 1, t0 = t_base + (nblk - 1 - j) * kBlock, tk = t0 + key;
       const uint32_t p_at = smem + C::kOffP + b * 2 * C::kB + key * 16;
-      ok = wait(&sh.s_full[b], j >> 1);
-      ok = wait(&sh.v_full[b], j >> 1) && ok;  // and so P of block j - 2 is used up
+      ok = wait(&sh.s_full[b], j >> 1);  // and so P of block j - 2 is used up
       const bool there = (sh.present[j & 3][warp] >> lane) & 1u;
       const bool open = t0 >= sh.all_lo && t0 + kBlock <= sh.all_hi && __all_sync(0xffffffffu, there);
-      float s[kC];
-      tmem_ld_cols<kC>(tmem + lanes + kColS + b * 32, s);
-      tmem_wait_ld();
+      // The weights' exponents, score + minus.  Maxima move only where a weight would be
+      // 2^11 times its row's maximum: then the scores alone, once more the exponents.
+      float x[kC];
+      for (const float* minus = sh.minus;;) {
+        tmem_ld_cols<kC>(tmem + lanes + kColS + b * 32, x);
+        tmem_wait_ld();
+        if (a.cap > 0.0f) {
+          const float cap = a.cap * kLog2e, in = 2.0f / a.cap;  // 2 log2(e) s / c
 #pragma unroll
-      for (int n = 0; n < kC; n += 4) {
-        const float4 f = *reinterpret_cast<const float4*>(&sh.mult[n]);
-        s[n] *= f.x;
-        s[n + 1] *= f.y;
-        s[n + 2] *= f.z;
-        s[n + 3] *= f.w;
-      }
-      if (a.cap > 0.0f) {
-        const float cap = a.cap * kLog2e, in = 2.0f / a.cap;  // 2 log2(e) s / c
-#pragma unroll
-        for (int n = 0; n < kC; ++n) s[n] = fmaf(-2.0f * cap, rcp(1.0f + ex2(s[n] * in)), cap);
-      }
-      if (a.slopes) {
-        const float tf = static_cast<float>(tk);
+          for (int n = 0; n < kC; ++n) x[n] = fmaf(-2.0f * cap, rcp(1.0f + ex2(x[n] * sh.mult[n] * in)), cap);
+        }
 #pragma unroll
         for (int n = 0; n < kC; n += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(&sh.slope[n]), at = *reinterpret_cast<const float4*>(&sh.pos[n]);
-          s[n] = fmaf(-f.x, fabsf(at.x - tf), s[n]);
-          s[n + 1] = fmaf(-f.y, fabsf(at.y - tf), s[n + 1]);
-          s[n + 2] = fmaf(-f.z, fabsf(at.z - tf), s[n + 2]);
-          s[n + 3] = fmaf(-f.w, fabsf(at.w - tf), s[n + 3]);
+          const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(&sh.factor[n]), c = *reinterpret_cast<const ulonglong2*>(&minus[n]);
+          unpair(fma2(pair(x[n], x[n + 1]), m.x, c.x), x[n], x[n + 1]);
+          unpair(fma2(pair(x[n + 2], x[n + 3]), m.y, c.y), x[n + 2], x[n + 3]);
         }
-      }
-      if (!open) {
-        const int t = there ? tk : -1;  // below every first key
+        if (a.slopes) {
+          const float tf = static_cast<float>(tk);
 #pragma unroll
-        for (int n = 0; n < kC; n += 4) {
-          const int4 lo = *reinterpret_cast<const int4*>(&sh.first[n]), hi = *reinterpret_cast<const int4*>(&sh.last[n]);
-          if (t < lo.x || t >= hi.x) s[n] = -INFINITY;
-          if (t < lo.y || t >= hi.y) s[n + 1] = -INFINITY;
-          if (t < lo.z || t >= hi.z) s[n + 2] = -INFINITY;
-          if (t < lo.w || t >= hi.w) s[n + 3] = -INFINITY;
+          for (int n = 0; n < kC; n += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(&sh.slope[n]), at = *reinterpret_cast<const float4*>(&sh.pos[n]);
+            x[n] = fmaf(-f.x, fabsf(at.x - tf), x[n]);
+            x[n + 1] = fmaf(-f.y, fabsf(at.y - tf), x[n + 1]);
+            x[n + 2] = fmaf(-f.z, fabsf(at.z - tf), x[n + 2]);
+            x[n + 3] = fmaf(-f.w, fabsf(at.w - tf), x[n + 3]);
+          }
         }
-      }
-      // Maxima move only where a weight would be 2^11 times its row's maximum.
-      for (;;) {
-        float most = -INFINITY;
+        if (!open) {
+          const int t = there ? tk : -1;  // below every first key
 #pragma unroll
-        for (int n = 0; n < kC; n += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(&sh.minus[n]);
-          most = max3(max3(s[n] + f.x, s[n + 1] + f.y, most), s[n + 2] + f.z, s[n + 3] + f.w);
+          for (int n = 0; n < kC; n += 4) {
+            const int4 lo = *reinterpret_cast<const int4*>(&sh.first[n]), hi = *reinterpret_cast<const int4*>(&sh.last[n]);
+            if (t < lo.x || t >= hi.x) x[n] = -INFINITY;
+            if (t < lo.y || t >= hi.y) x[n + 1] = -INFINITY;
+            if (t < lo.z || t >= hi.z) x[n + 2] = -INFINITY;
+            if (t < lo.w || t >= hi.w) x[n + 3] = -INFINITY;
+          }
         }
-        if (!any_of_128(most > kWeightLog2 + kRescaleLog2 || !ok)) break;
+        if (minus == sh.minus) {
+          float most = -INFINITY;
+#pragma unroll
+          for (int n = 0; n < kC; n += 2) most = max3(x[n], x[n + 1], most);
+          if (!any_of_128(most > kWeightLog2 + kRescaleLog2 || !ok)) break;
+          minus = sh.none;
+          continue;
+        }
         // Each row's largest score in the block, by warp, then of all four.
 #pragma unroll
         for (int n = 0; n < kC; ++n) {
-          const float v = warp_max(s[n]);
+          const float v = warp_max(x[n]);
           if (lane == 0) sh.top[warp][n] = v;
         }
         if (any_of_128(!ok)) {
@@ -301,8 +301,8 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         }
         const auto top_of = [&](int n) { return max3(max3(sh.top[0][n], sh.top[1][n], sh.top[2][n]), sh.top[3][n], -INFINITY); };
         const auto shrink = [&](int n) {
-          const float x = top_of(n) + sh.minus[n];
-          return x > kWeightLog2 + kRescaleLog2 ? ex2(kWeightLog2 - x) : 1.0f;
+          const float up = top_of(n) + sh.minus[n];
+          return up > kWeightLog2 + kRescaleLog2 ? ex2(kWeightLog2 - up) : 1.0f;
         };
 #pragma unroll
         for (int n = 0; n < kC; ++n) l[n] *= shrink(n);
@@ -322,42 +322,34 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         any_of_128(false);  // every warp has read the old maxima
         if (warp == 0 && lane < kC && shrink(lane) != 1.0f) sh.minus[lane] = kWeightLog2 - top_of(lane);
         any_of_128(false);
+        minus = sh.minus;
       }
       if (!ok) break;
 #pragma unroll
-      for (int n = 0; n < kC; n += 4) {
-        const float4 f = *reinterpret_cast<const float4*>(&sh.minus[n]);
-        s[n] = ex2(s[n] + f.x);
-        s[n + 1] = ex2(s[n + 1] + f.y);
-        s[n + 2] = ex2(s[n + 2] + f.z);
-        s[n + 3] = ex2(s[n + 3] + f.w);
-      }
+      for (int n = 0; n < kC; ++n) x[n] = ex2(x[n]);
 #pragma unroll
       for (int n = 0; n < kC; n += 8) {
         if (kFull) {
           uint32_t hi[4], lo[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint32_t xb = __float_as_uint(s[n + 2 * k]), yb = __float_as_uint(s[n + 2 * k + 1]);
+            const uint32_t xb = __float_as_uint(x[n + 2 * k]), yb = __float_as_uint(x[n + 2 * k + 1]);
             hi[k] = __byte_perm(xb, yb, 0x7632);
-            lo[k] = bf16x2_rn(s[n + 2 * k] - __uint_as_float(xb & 0xFFFF0000u), s[n + 2 * k + 1] - __uint_as_float(yb & 0xFFFF0000u));
+            lo[k] = bf16x2_rn(x[n + 2 * k] - __uint_as_float(xb & 0xFFFF0000u), x[n + 2 * k + 1] - __uint_as_float(yb & 0xFFFF0000u));
           }
           sts128(p_at + n * 256, hi[0], hi[1], hi[2], hi[3]);
           sts128(p_at + n * 256 + C::kB, lo[0], lo[1], lo[2], lo[3]);
         } else {
-          sts128(p_at + n * 256, f16x2_rn(s[n], s[n + 1]), f16x2_rn(s[n + 2], s[n + 3]), f16x2_rn(s[n + 4], s[n + 5]),
-                 f16x2_rn(s[n + 6], s[n + 7]));
+          sts128(p_at + n * 256, f16x2_rn(x[n], x[n + 1]), f16x2_rn(x[n + 2], x[n + 3]), f16x2_rn(x[n + 4], x[n + 5]),
+                 f16x2_rn(x[n + 6], x[n + 7]));
         }
       }
       fence_proxy_async_smem();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&sh.p_full[b]);
-        mbar_arrive(&sh.s_free[b]);
-      }
+      if (lane == 0) mbar_arrive(&sh.p_full[b]);
 #pragma unroll
-      for (int n = 0; n < kC; ++n) l[n] += s[n];
+      for (int n = 0; n < kC; n += 2) add2(l[n], l[n + 1], x[n], x[n + 1]);
     }
     const bool done = wait(&sh.drain, 0);
     // ---- epilogue: thread = channel -----------------------------------------
@@ -511,43 +503,50 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 24;");
     // ----------------------------------------------------------------- MMA ---
-    if (warp < 14) {
+    if (warp == 12) {
       const bool leader = elect_one();
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-      for (int j = 0; j < nblk; ++j) {
+      const auto qk = [&](int j) {
         const int b = j & 1;
-        if (warp == 12) {
-          if (!wait(&sh.p_full[b], j >> 1)) break;  // V is there too: the softmax has waited for it
-          if (leader) {
-            // A = V^T (bit 15: stored with M contiguous), B = P (bit 16: N), 16 keys a step.
-            constexpr uint32_t kIdesc = (1u << 4) | (3u << 15) | (static_cast<uint32_t>(kN / 8) << 17) | (8u << 24) |
-                                        (kFull ? (1u << 7) | (1u << 10) : 0u);
-            const uint32_t v = operand_desc(smem + b * kOperand), p = plain_desc(smem + C::kOffP + b * 2 * C::kB);
+        if (leader) {
+          constexpr uint32_t kIdesc = (1u << 4) | (static_cast<uint32_t>(kN / 8) << 17) | (8u << 24);
 #pragma unroll
-            for (int s = 0; s < (kFull ? 16 : 8); ++s)
-              mma_v_p(tm + kColO, v + (((s & 7) * 2048) >> 4), p + (((s >> 3) * C::kB + (s & 7) * 256) >> 4), kIdesc,
-                      j != 0 || s != 0);
-            tc_commit(&sh.v_free[b]);
+          for (int s = 0; s < 8; ++s) {
+            const uint32_t at = C::kOffQ + (s >> 2) * (kN * 128) + (s & 3) * 32;
+            mma_ts(tm + kColS + b * 32, tm + b * 64 + s * 8, ((smem + at) & 0x3FFFFu) >> 4, kIdesc, s != 0);
           }
-        } else {
-          if ((j == 0 && !wait(&sh.q_full, 0)) || !wait(&sh.k_full[b], j >> 1) || (j >= 2 && !wait(&sh.s_free[b], (j >> 1) ^ 1))) break;
-          if (leader) {
-            constexpr uint32_t kIdesc = (1u << 4) | (static_cast<uint32_t>(kN / 8) << 17) | (8u << 24);
-#pragma unroll
-            for (int s = 0; s < 8; ++s) {
-              const uint32_t at = C::kOffQ + (s >> 2) * (kN * 128) + (s & 3) * 32;
-              mma_ts(tm + kColS + b * 32, tm + b * 64 + s * 8, ((smem + at) & 0x3FFFFu) >> 4, kIdesc, s != 0);
-            }
-            tc_commit(&sh.s_full[b]);
-            tc_commit(&sh.k_free[b]);
-          }
+          tc_commit(&sh.s_full[b]);
+          tc_commit(&sh.k_free[b]);
         }
         __syncwarp();
+      };
+      bool ok = nblk > 0 && wait(&sh.q_full, 0);
+      for (int j = 0; j < 2 && j < nblk && ok; ++j)
+        if ((ok = wait(&sh.k_full[j], 0))) qk(j);
+      for (int j = 0; j < nblk && ok; ++j) {
+        const int b = j & 1;
+        if (!wait(&sh.v_full[b], j >> 1) || !wait(&sh.p_full[b], j >> 1)) break;
+        if (leader) {
+          // A = V^T (bit 15: stored with M contiguous), B = P (bit 16: N), 16 keys a step.
+          constexpr uint32_t kIdesc = (1u << 4) | (3u << 15) | (static_cast<uint32_t>(kN / 8) << 17) | (8u << 24) |
+                                      (kFull ? (1u << 7) | (1u << 10) : 0u);
+          const uint32_t v = operand_desc(smem + b * kOperand), p = plain_desc(smem + C::kOffP + b * 2 * C::kB);
+#pragma unroll
+          for (int s = 0; s < (kFull ? 16 : 8); ++s)
+            mma_v_p(tm + kColO, v + (((s & 7) * 2048) >> 4), p + (((s >> 3) * C::kB + (s & 7) * 256) >> 4), kIdesc,
+                    j != 0 || s != 0);
+          tc_commit(&sh.v_free[b]);
+        }
+        __syncwarp();
+        // P is there, and so the scores that it came from are read.
+        if (j + 2 < nblk) {
+          if (!wait(&sh.k_full[b], (j + 2) >> 1)) break;
+          qk(j + 2);
+        }
       }
       // Nothing that was issued, MMA or arrival, outlives the CTA.
-      uint64_t* drain = warp == 12 ? &sh.drain : &sh.drain_qk;
-      if (leader) tc_commit(drain);
-      mbar_wait_bounded(drain, 0, nullptr, kDrainLimitNs);
+      if (leader) tc_commit(&sh.drain);
+      mbar_wait_bounded(&sh.drain, 0, nullptr, kDrainLimitNs);
       __syncwarp();
     }
   }
