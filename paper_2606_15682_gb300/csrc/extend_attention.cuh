@@ -314,17 +314,18 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, volatil
 
 // The eight elements of a code word times their block scale (kv_scales16) as four
 // f16x2.  E2M1: channels (0,1) (2,3) (4,5) (6,7).  E1M2: (0,4) (1,5) (2,6) (3,7): a
-// nibble is decoded where it stands, those in bits 4-7 as 16 times their value,
-// for which the scale is divided (exact).  Q is laid out in the same order, and
-// O comes in V's.
+// nibble is decoded where it stands, its sign bit turned over, in the low bits of
+// 1024: 1032 + n, or in bits 4-7 1152 + 16 n, where 1152 scale / 16 has no more than 8
+// significant bits and one FMA gives n scale exactly.  Q is laid out in the same
+// order, and O comes in V's.
 template <bool kE1M2>
 __device__ __forceinline__ void scaled8(uint32_t w, uint32_t scale, uint32_t e[4]) {
   if (kE1M2) {
-    const uint32_t t = w >> 8, scale16 = mul_f16x2(scale, 0x2C002C00u);
+    const uint32_t t = w >> 8, scale16 = mul_f16x2(scale, 0x2C002C00u), less = mul_f16x2(scale, 0xD480D480u);
     e[0] = mul_f16x2(sub_f16x2((w & 0x000F000Fu) ^ 0x64086408u, 0x64086408u), scale);
-    e[1] = mul_f16x2(sub_f16x2((w & 0x00F000F0u) ^ 0x64806480u, 0x64806480u), scale16);
+    e[1] = fma_f16x2((w & 0x00F000F0u) ^ 0x64806480u, scale16, less);
     e[2] = mul_f16x2(sub_f16x2((t & 0x000F000Fu) ^ 0x64086408u, 0x64086408u), scale);
-    e[3] = mul_f16x2(sub_f16x2((t & 0x00F000F0u) ^ 0x64806480u, 0x64806480u), scale16);
+    e[3] = fma_f16x2((t & 0x00F000F0u) ^ 0x64806480u, scale16, less);
   } else {
     elements8<false>(w, e);
 #pragma unroll

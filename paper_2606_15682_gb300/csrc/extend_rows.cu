@@ -39,8 +39,7 @@ struct RowsShared {
   uint32_t tmem;
   Item item;
   int lo, hi, all_lo, all_hi, rows;
-  alignas(16) float mult[kC];    // score -> log2 domain
-  alignas(16) float factor[kC];  // the same, 1 where a cap has that done
+  alignas(16) float mult[kC];  // score -> log2 domain
   alignas(16) float minus[kC], none[kC];  // 4 - the row's maximum: x = score + minus is a weight's exponent
   alignas(16) float slope[kC], pos[kC];  // slopes[h] log2(e); the query's position
   alignas(16) int first[kC], last[kC];  // keys that it sees: first <= t < last
@@ -217,7 +216,6 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         // No maximum yet: any score exceeds it.  (A row past the tile's has scores of 0.)
         const bool live = sh.out[lr] != 0xffffffffu;
         sh.mult[lr] = live ? a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23) : 0.0f;
-        sh.factor[lr] = a.cap > 0.0f ? 1.0f : sh.mult[lr];
         sh.minus[lr] = live ? 1e30f : 0.0f;
         sh.none[lr] = 0.0f;
       }
@@ -243,21 +241,24 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       const bool there = (sh.present[j & 3][warp] >> lane) & 1u;
       const bool open = t0 >= sh.all_lo && t0 + kBlock <= sh.all_hi && __all_sync(0xffffffffu, there);
       // The weights' exponents, score + minus.  Maxima move only where a weight would be
-      // 2^11 times its row's maximum: then the scores alone, once more the exponents.
+      // 2^11 times its row's maximum: then the scores alone (pass 1), and the exponents
+      // once more.  `minus` is added last, so that both see the same rounded scores.
       float x[kC];
-      for (const float* minus = sh.minus;;) {
+#pragma unroll 1
+      for (int pass = 0; pass < 3; ++pass) {
+        const float* minus = pass == 1 ? sh.none : sh.minus;
         tmem_ld_cols<kC>(tmem + lanes + kColS + b * 32, x);
         tmem_wait_ld();
+#pragma unroll
+        for (int n = 0; n < kC; n += 4) {
+          const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(&sh.mult[n]);
+          unpair(mul2(pair(x[n], x[n + 1]), m.x), x[n], x[n + 1]);
+          unpair(mul2(pair(x[n + 2], x[n + 3]), m.y), x[n + 2], x[n + 3]);
+        }
         if (a.cap > 0.0f) {
           const float cap = a.cap * kLog2e, in = 2.0f / a.cap;  // 2 log2(e) s / c
 #pragma unroll
-          for (int n = 0; n < kC; ++n) x[n] = fmaf(-2.0f * cap, rcp(1.0f + ex2(x[n] * sh.mult[n] * in)), cap);
-        }
-#pragma unroll
-        for (int n = 0; n < kC; n += 4) {
-          const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(&sh.factor[n]), c = *reinterpret_cast<const ulonglong2*>(&minus[n]);
-          unpair(fma2(pair(x[n], x[n + 1]), m.x, c.x), x[n], x[n + 1]);
-          unpair(fma2(pair(x[n + 2], x[n + 3]), m.y, c.y), x[n + 2], x[n + 3]);
+          for (int n = 0; n < kC; ++n) x[n] = fmaf(-2.0f * cap, rcp(1.0f + ex2(x[n] * in)), cap);
         }
         if (a.slopes) {
           const float tf = static_cast<float>(tk);
@@ -270,6 +271,12 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
             x[n + 3] = fmaf(-f.w, fabsf(at.w - tf), x[n + 3]);
           }
         }
+#pragma unroll
+        for (int n = 0; n < kC; n += 4) {
+          const ulonglong2 c = *reinterpret_cast<const ulonglong2*>(&minus[n]);
+          unpair(add2(pair(x[n], x[n + 1]), c.x), x[n], x[n + 1]);
+          unpair(add2(pair(x[n + 2], x[n + 3]), c.y), x[n + 2], x[n + 3]);
+        }
         if (!open) {
           const int t = there ? tk : -1;  // below every first key
 #pragma unroll
@@ -281,14 +288,13 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
             if (t < lo.w || t >= hi.w) x[n + 3] = -INFINITY;
           }
         }
-        if (minus == sh.minus) {
+        if (pass == 0) {
           float most = -INFINITY;
 #pragma unroll
           for (int n = 0; n < kC; n += 2) most = max3(x[n], x[n + 1], most);
           if (!any_of_128(most > kWeightLog2 + kRescaleLog2 || !ok)) break;
-          minus = sh.none;
-          continue;
         }
+        if (pass != 1) continue;
         // Each row's largest score in the block, by warp, then of all four.
 #pragma unroll
         for (int n = 0; n < kC; ++n) {
@@ -319,10 +325,13 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
           }
           tmem_wait_st();
         }
-        any_of_128(false);  // every warp has read the old maxima
+        const bool bad = any_of_128(!ok);  // also: every warp has read the old maxima
         if (warp == 0 && lane < kC && shrink(lane) != 1.0f) sh.minus[lane] = kWeightLog2 - top_of(lane);
         any_of_128(false);
-        minus = sh.minus;
+        if (bad) {
+          ok = false;
+          break;
+        }
       }
       if (!ok) break;
 #pragma unroll

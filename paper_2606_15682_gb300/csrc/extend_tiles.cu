@@ -298,6 +298,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
           }
         }
       }
+      // The product and the sum round once, but the maximum was rounded by itself: an
+      // exponent may be above 4 by half a unit in the maximum's last place.  Where that
+      // is more than a little the product is rounded first too.
+      uint64_t factor = to_log2x2;
+      if (kMods == 0 && __any_sync(0xffffffffu, fabsf(m) > 0x1p22f && m != -INFINITY)) {
+        factor = both(1.0f);
+#pragma unroll
+        for (int k = 0; k < 64; ++k) s[k] *= to_log2;
+      }
       const uint64_t minus = both((m == -INFINITY ? 0.0f : -m) + kWeightLog2);
       // The weights, over the scores they came from.
 #pragma unroll
@@ -306,7 +315,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           float x = s[32 * c + 2 * k], y = s[32 * c + 2 * k + 1];
-          fma2(x, y, to_log2x2, minus);
+          fma2(x, y, factor, minus);
           x = ex2(x);
           y = ex2(y);
           add2(l0, l1, x, y);

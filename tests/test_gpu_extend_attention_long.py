@@ -209,3 +209,44 @@ def test_length_above_the_capacity_is_clamped_and_reported(N, news):
     assert N.nvfp4_get_device_status() == 7
     ref, bound, _ = reference(case, q, news)
     assert (np.abs(out.double().cpu().numpy() - ref) <= P.half_ulp(ref) * (1 + 2.0 ** -6) + bound).all()
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_maxima_that_move_by_little(N, seed):
+    """Scores whose running maxima pass the threshold for a new one by roundings: a biased draft over many keys."""
+    news, lens = [4] * 12, [4001 - 97 * i for i in range(12)]
+    case = P.Case(N, lens, 2, 128, 1, seed=350 + seed)
+    slopes = np.concatenate([2.0 ** (-8 * np.arange(1, 6) / 5), -(2.0 ** (-8 * np.arange(1, 6) / 5))]).astype(np.float32)
+    check(N, case, queries(48, 10, seed), news, uniform=True, slopes=slopes)
+    assert N.nvfp4_get_device_status() == 0
+
+
+@pytest.mark.parametrize("news", [[1, 1], [4, 4], [150, 20]])
+@pytest.mark.parametrize("log_spread", [16, 24, 30, 40])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_scores_past_fp32s_integers(N, news, log_spread, cap):
+    """Queries so large that scores are far apart; finite everywhere, and the file's tolerance where the largest key is
+    clear of the others by 40 and by the scores' error (2^-18 of the sum of their terms, more than fp32 sums of 128
+    exact products can lose)."""
+    case = P.Case(N, [1500, 800], 2, 0, 0, seed=360)
+    q = queries(sum(news), 10, 9, spread=2.0 ** log_spread)
+    out = run(N, case, q, news, logit_cap=cap)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out).all()
+    if cap:
+        return
+    clear, first = np.zeros((len(q), 10), bool), 0
+    for b, n in enumerate(news):
+        k = torch.from_numpy(case.rows_of("k", b)[0]).cuda() * float(np.float32(P.GK)) * SCALE
+        t = torch.arange(case.lens[b], device="cuda")
+        hidden = t > (case.lens[b] - n + torch.arange(n, device="cuda"))[:, None]
+        for h in range(10):
+            qq, kk = q[first:first + n, h].double(), k[h // 5]
+            top = (qq @ kk.T).masked_fill(hidden, -math.inf).topk(2, dim=1).values
+            error = 2.0 ** -18 * (qq.abs() @ kk.abs().T).amax(1)
+            clear[first:first + n, h] = (top[:, 0] - top[:, 1] > 2 * error + 40).cpu().numpy()
+        first += n
+    assert clear.any()
+    ref, bound, _ = reference(case, q, news)
+    over = np.abs(out.double().cpu().numpy() - ref) - (P.half_ulp(ref) * (1 + 2.0 ** -6) + bound)
+    assert over[clear].max() <= 0
