@@ -204,6 +204,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         w[i] = __ldg(reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(tk) * a.ld_q + (out - tk * a.hq) * kD) + (lane & 15));
       }
     }
+    bool coarse = false;  // a product of Q and K is below 2^19
 #pragma unroll
     for (int i = 0; i < kN / 8; ++i) {
       const uint32_t lr = i * 8 + warp * 2 + (lane >> 4), c = lane & 15;
@@ -216,6 +217,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         // No maximum yet: any score exceeds it.  (A row past the tile's has scores of 0.)
         const bool live = sh.out[lr] != 0xffffffffu;
         sh.mult[lr] = live ? a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23) : 0.0f;
+        coarse = coarse || !(sh.mult[lr] <= 8.0f) || !(fabsf(sh.slope[lr]) * static_cast<float>(a.map.context) <= 0x1p21f);
         sh.minus[lr] = live ? 1e30f : 0.0f;
         sh.none[lr] = 0.0f;
       }
@@ -227,7 +229,22 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) mbar_arrive(&sh.q_full);
-    any_of_128(false);  // the multipliers of all rows
+    // (Also the barrier after which all rows' multipliers are there.)  Scores that may
+    // pass 2^22 are rounded before `minus` is added, as the maxima are: else an exponent
+    // could be above the largest by the rounding of one product.
+    const bool exact = any_of_128(coarse) || a.cap > 0.0f;
+    const auto bias = [&](float* x, int tk) {
+      if (!a.slopes) return;
+      const float tf = static_cast<float>(tk);
+#pragma unroll
+      for (int n = 0; n < kC; n += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(&sh.slope[n]), at = *reinterpret_cast<const float4*>(&sh.pos[n]);
+        x[n] = fmaf(-f.x, fabsf(at.x - tf), x[n]);
+        x[n + 1] = fmaf(-f.y, fabsf(at.y - tf), x[n + 1]);
+        x[n + 2] = fmaf(-f.z, fabsf(at.z - tf), x[n + 2]);
+        x[n + 3] = fmaf(-f.w, fabsf(at.w - tf), x[n + 3]);
+      }
+    };
     const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
     const int key = warp * 32 + lane;
     float l[kC];
@@ -241,41 +258,31 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       const bool there = (sh.present[j & 3][warp] >> lane) & 1u;
       const bool open = t0 >= sh.all_lo && t0 + kBlock <= sh.all_hi && __all_sync(0xffffffffu, there);
       // The weights' exponents, score + minus.  Maxima move only where a weight would be
-      // 2^11 times its row's maximum: then the scores alone (pass 1), and the exponents
-      // once more.  `minus` is added last, so that both see the same rounded scores.
+      // 2^11 times its row's maximum: then the scores alone, and the exponents once more.
       float x[kC];
-#pragma unroll 1
-      for (int pass = 0; pass < 3; ++pass) {
-        const float* minus = pass == 1 ? sh.none : sh.minus;
+      bool moved = false;
+      for (const float* minus = sh.minus;;) {
         tmem_ld_cols<kC>(tmem + lanes + kColS + b * 32, x);
         tmem_wait_ld();
+        if (exact) {
 #pragma unroll
-        for (int n = 0; n < kC; n += 4) {
-          const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(&sh.mult[n]);
-          unpair(mul2(pair(x[n], x[n + 1]), m.x), x[n], x[n + 1]);
-          unpair(mul2(pair(x[n + 2], x[n + 3]), m.y), x[n + 2], x[n + 3]);
-        }
-        if (a.cap > 0.0f) {
-          const float cap = a.cap * kLog2e, in = 2.0f / a.cap;  // 2 log2(e) s / c
+          for (int n = 0; n < kC; ++n) x[n] *= sh.mult[n];
+          if (a.cap > 0.0f) {
+            const float cap = a.cap * kLog2e, in = 2.0f / a.cap;  // 2 log2(e) s / c
 #pragma unroll
-          for (int n = 0; n < kC; ++n) x[n] = fmaf(-2.0f * cap, rcp(1.0f + ex2(x[n] * in)), cap);
-        }
-        if (a.slopes) {
-          const float tf = static_cast<float>(tk);
+            for (int n = 0; n < kC; ++n) x[n] = fmaf(-2.0f * cap, rcp(1.0f + ex2(x[n] * in)), cap);
+          }
+          bias(x, tk);
+#pragma unroll
+          for (int n = 0; n < kC; ++n) x[n] += minus[n];
+        } else {
 #pragma unroll
           for (int n = 0; n < kC; n += 4) {
-            const float4 f = *reinterpret_cast<const float4*>(&sh.slope[n]), at = *reinterpret_cast<const float4*>(&sh.pos[n]);
-            x[n] = fmaf(-f.x, fabsf(at.x - tf), x[n]);
-            x[n + 1] = fmaf(-f.y, fabsf(at.y - tf), x[n + 1]);
-            x[n + 2] = fmaf(-f.z, fabsf(at.z - tf), x[n + 2]);
-            x[n + 3] = fmaf(-f.w, fabsf(at.w - tf), x[n + 3]);
+            const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(&sh.mult[n]), c = *reinterpret_cast<const ulonglong2*>(&minus[n]);
+            unpair(fma2(pair(x[n], x[n + 1]), m.x, c.x), x[n], x[n + 1]);
+            unpair(fma2(pair(x[n + 2], x[n + 3]), m.y, c.y), x[n + 2], x[n + 3]);
           }
-        }
-#pragma unroll
-        for (int n = 0; n < kC; n += 4) {
-          const ulonglong2 c = *reinterpret_cast<const ulonglong2*>(&minus[n]);
-          unpair(add2(pair(x[n], x[n + 1]), c.x), x[n], x[n + 1]);
-          unpair(add2(pair(x[n + 2], x[n + 3]), c.y), x[n + 2], x[n + 3]);
+          bias(x, tk);
         }
         if (!open) {
           const int t = there ? tk : -1;  // below every first key
@@ -288,13 +295,15 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
             if (t < lo.w || t >= hi.w) x[n + 3] = -INFINITY;
           }
         }
-        if (pass == 0) {
+        if (minus == sh.minus) {
+          if (moved) break;
           float most = -INFINITY;
 #pragma unroll
           for (int n = 0; n < kC; n += 2) most = max3(x[n], x[n + 1], most);
           if (!any_of_128(most > kWeightLog2 + kRescaleLog2 || !ok)) break;
+          minus = sh.none;
+          continue;
         }
-        if (pass != 1) continue;
         // Each row's largest score in the block, by warp, then of all four.
 #pragma unroll
         for (int n = 0; n < kC; ++n) {
@@ -332,6 +341,8 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
           ok = false;
           break;
         }
+        minus = sh.minus;
+        moved = true;
       }
       if (!ok) break;
 #pragma unroll

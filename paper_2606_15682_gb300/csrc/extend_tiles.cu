@@ -238,7 +238,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     const int all_lo = __reduce_max_sync(0xffffffffu, live ? vis.x : 0);
     const int all_hi = __reduce_min_sync(0xffffffffu, live ? vis.y : 0x7fffffff);
     const int p_min = __reduce_min_sync(0xffffffffu, live ? p : 0x7fffffff - 64);
-    const float to_log2 = kMods ? 1.0f : rs.mult;
+    // The product and the sum round once, the maximum was rounded by itself: an exponent
+    // may exceed the largest by half a unit of the maximum's last place.  A product of Q
+    // and K is below 2^19; where scores may pass 2^22 they are rounded first too.
+    const bool coarse = kMods == 0 && __any_sync(0xffffffffu, !(rs.mult <= 8.0f));
+    const float to_log2 = kMods || coarse ? 1.0f : rs.mult;
     const uint64_t to_log2x2 = both(to_log2);
     float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
     bool ok = true;
@@ -254,6 +258,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       tmem_ld32(s_col, s);
       tmem_ld32(s_col + 32, s + 32);
       tmem_wait_ld();
+      if (__builtin_expect(coarse, false)) {
+#pragma unroll
+        for (int k = 0; k < 64; ++k) s[k] *= rs.mult;
+      }
       if (kMods) {
 #pragma unroll
         for (int k = 0; k < 64; k += 32) score32<kMods>(s + k, rs, a, p - t0 - k, t0 + 64 <= p_min + 1);
@@ -298,15 +306,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
           }
         }
       }
-      // The product and the sum round once, but the maximum was rounded by itself: an
-      // exponent may be above 4 by half a unit in the maximum's last place.  Where that
-      // is more than a little the product is rounded first too.
-      uint64_t factor = to_log2x2;
-      if (kMods == 0 && __any_sync(0xffffffffu, fabsf(m) > 0x1p22f && m != -INFINITY)) {
-        factor = both(1.0f);
-#pragma unroll
-        for (int k = 0; k < 64; ++k) s[k] *= to_log2;
-      }
       const uint64_t minus = both((m == -INFINITY ? 0.0f : -m) + kWeightLog2);
       // The weights, over the scores they came from.
 #pragma unroll
@@ -315,7 +314,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           float x = s[32 * c + 2 * k], y = s[32 * c + 2 * k + 1];
-          fma2(x, y, factor, minus);
+          fma2(x, y, to_log2x2, minus);
           x = ex2(x);
           y = ex2(y);
           add2(l0, l1, x, y);
