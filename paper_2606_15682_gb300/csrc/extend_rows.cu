@@ -189,10 +189,16 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
     return ok;
   };
 
-  // 104, 64, 64 and 24 registers a thread: the 512 x 64 that the CTA starts with.
+  // 104, 64, 64 and 24 registers a thread, or 96, 64, 64 and 32: the 512 x 64 that the CTA
+  // starts with.  Which is better is the spills' doing (32 x 4001 keys, the first against
+  // the second: 24 rows 64 and 73 us, 32 rows 79 and 73).
+  constexpr bool kMore = kC < 32;
   if (warp < 4) {
     // ------------------------------------------------------------- softmax ---
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    if (kMore)
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    else
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
     // Q rows as f16, scaled by a power of two (exact) to below 1: 16 lanes a row.
     uint4 w[kN / 8];
 #pragma unroll
@@ -521,7 +527,10 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       rows_of(j + 2);
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 24;");
+    if (kMore)
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 24;");
+    else
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
     // ----------------------------------------------------------------- MMA ---
     if (warp == 12) {
       const bool leader = elect_one();
