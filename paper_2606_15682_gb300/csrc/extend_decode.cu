@@ -5,9 +5,11 @@
 // each, dequantize in registers (exact in f16) and multiply with mma.sync m16n8k16:
 // S^T[16 keys, 8 rows] = K Q^T, O^T[128, 8 rows] += V^T P^T.  Four CTAs an SM.  The
 // tensor pipe gives this form some 32 cycles an MMA: 16 of them per 16 keys are
-// 1024 cycles per 128 keys and SM where HBM takes 790.  (extend_rows_kernel, whose
-// shared-memory traffic does not shrink with the rows, is slower at 8 rows, and this
-// one at 16: it has twice the MMAs then.)
+// 1024 cycles per 128 keys and SM where HBM takes 790.  64 ragged sequences of up to
+// 16384 keys, 40 on 8 heads: 147 us, 3.4 TB/s, 0.50 of the measured copy rate; 38 x 8192
+// keys, parts that fill the GPU once, 99 us, 0.53.  (extend_rows_kernel, whose
+// shared-memory traffic does not shrink with the rows, takes 187 us there, and this
+// one loses at 16 rows: it has twice the MMAs then.)
 //
 // Lane roles (g = lane / 4, t = lane % 4), as the fragments have them:
 //   K rows g and g + 8 of the tile, channels 32t..32t+31; V rows 2t, 2t+1, 2t+8,

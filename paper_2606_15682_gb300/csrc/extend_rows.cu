@@ -9,11 +9,13 @@
 //   warps 4-7   K (thread = key)
 //   warps 8-11  V
 //   warp 12     issues the MMAs; 13-15 complete its warpgroup
-// Two CTAs share an SM.  What a softmax thread does per block is kept short: the
-// four roles' code does not fit the instruction caches that are near the
-// schedulers, and a role's turn goes by its instructions more than by its work.
-// (By mma.sync in registers the tensor pipe's rate for that form is the bound: 64
-// ragged sequences of up to 16384 tokens 174 us, 32 x 4 new tokens on 4001 148.)
+// Two CTAs share an SM.  32 x 4 drafted tokens on 4001 keys, 40 on 8 heads (24 rows),
+// take 64 us in E2M1 and 74 in E1M2, 0.34 and 0.30 of the measured copy rate; HBM alone
+// would take 22.  What bounds it is the softmax warps' turn per block, at one key a
+// thread: it goes by its instructions, which the four roles' code, too long for the
+// instruction caches near the schedulers, makes expensive; 8 rows more cost 5 us, no
+// row at all 50.  (By mma.sync in registers the tensor pipe's rate for that form is the
+// bound: 148 us.)
 #include "extend_attention.cuh"
 
 namespace nvfp4 {
