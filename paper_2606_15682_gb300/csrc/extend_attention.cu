@@ -79,7 +79,7 @@ constexpr int64_t kFullContext = 512;
 
 // Which kernel, the tiles (at most), and the parts that each tile's keys are cut into.
 // By a sequence's rows per KV head: up to 8 the decode kernel (64 ragged sequences of up
-// to 16384 keys 147 us; by 8-row tensor-core tiles 187), up to 32 the rows kernel (32 x 4
+// to 16384 keys 144 us; by 8-row tensor-core tiles 187), up to 32 the rows kernel (32 x 4
 // drafted tokens on 4001 keys 77 us; by mma.sync 148, by 256-row tiles 159), else tiles.
 Plan plan_for(int64_t batch, int64_t n_tokens, int64_t group, int64_t hkv, int64_t context, bool uniform) {
   Plan p;
@@ -214,7 +214,7 @@ NVFP4_API nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const
   const bool e1m2 = cache->kv_format == NVFP4_KV_E1M2;
   const bool by_tiles = p.rows == kTileRows;
   const ExtendLaunch l = by_tiles                     ? extend_tiles(e1m2, a.cap > 0.0f, a.slopes != nullptr, p.full)
-                         : p.rows == 8 && !p.full ? extend_decode(e1m2)
+                         : p.rows == 8 && !p.full ? extend_decode(e1m2, a.cap > 0.0f || a.slopes)
                                                   : extend_rows(p.rows, e1m2, p.full);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // Raising the limit is idempotent.

@@ -362,6 +362,6 @@ struct ExtendLaunch {
 };
 ExtendLaunch extend_tiles(bool e1m2, bool cap, bool bias, bool full);  // kTileRows a tile
 ExtendLaunch extend_rows(int rows, bool e1m2, bool full);    // 16, 24, 32; 8 with `full`
-ExtendLaunch extend_decode(bool e1m2);                       // 8
+ExtendLaunch extend_decode(bool e1m2, bool mods);            // 8
 
 }  // namespace nvfp4

@@ -6,8 +6,8 @@
 // S^T[16 keys, 8 rows] = K Q^T, O^T[128, 8 rows] += V^T P^T.  Four CTAs an SM.  The
 // tensor pipe gives this form some 32 cycles an MMA: 16 of them per 16 keys are
 // 1024 cycles per 128 keys and SM where HBM takes 790.  64 ragged sequences of up to
-// 16384 keys, 40 on 8 heads: 147 us, 3.4 TB/s, 0.50 of the measured copy rate; 38 x 8192
-// keys, parts that fill the GPU once, 99 us, 0.53.  (extend_rows_kernel, whose
+// 16384 keys, 40 on 8 heads: 144 us, 3.5 TB/s, 0.52 of the measured copy rate; 38 x 8192
+// keys, parts that fill the GPU once, 96 us, 0.55 (99 with cap and bias in one kernel).  (extend_rows_kernel, whose
 // shared-memory traffic does not shrink with the rows, takes 187 us there, and this
 // one loses at 16 rows: it has twice the MMAs then.)
 //
@@ -40,7 +40,7 @@ __device__ __forceinline__ uint32_t transposed(uint32_t a) {
 }
 struct DecodeShared {
   uint64_t full[kRing], empty[kRing];
-  uint32_t present[kRing][4];
+  alignas(16) uint32_t present[kRing][4];
   Item item;
   int lo, hi;  // of this part
   float m[kWarps][kRows], l[kWarps][kRows];
@@ -48,7 +48,8 @@ struct DecodeShared {
 };
 constexpr uint32_t kSmem = kRing * kStageBytes + kWarps * kRows * kMergeRow * 4;
 
-template <bool kE1M2>
+// kMods: a cap or a bias.
+template <bool kE1M2, bool kMods>
 __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const ExtendArgs a) {
   extern __shared__ __align__(128) uint8_t smem_raw[];
   __shared__ DecodeShared sh;
@@ -159,7 +160,6 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
 
   // ------------------------------------------------------------- consumers ---
   const int cw = warp - 1, g = lane >> 2, t = lane & 3;
-  const bool mods = a.cap > 0.0f || a.slopes;
   // Rows of the lane's columns in a tile of scores: 2t and 2t + 1.
   int2 vis[2];
   float mult[2], slope[2];
@@ -235,10 +235,14 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
     const uint8_t* stage = smem_raw + st * kStageBytes;
     const uint8_t* k_scales = stage + 2 * kStageCodes;
     const uint8_t* v_scales = k_scales + kBlock * 8;
+    // Every row sees every key of the stage.
+    const uint4 present = *reinterpret_cast<const uint4*>(sh.present[st]);
+    const int t_stage = t_base + (n - 1 - i) * kBlock;
+    const bool open = t_stage >= all_lo && t_stage + kBlock <= all_hi && (present.x & present.y & present.z & present.w) == 0xffffffffu;
 #pragma unroll
     for (int sub = 0; sub < kBlock / (16 * kWarps); ++sub) {
-      const int r0 = 16 * (cw + kWarps * sub), t0 = t_base + (n - 1 - i) * kBlock + r0;
-      const uint32_t there = (sh.present[st][r0 >> 5] >> (r0 & 31)) & 0xFFFFu;
+      const int r0 = 16 * (cw + kWarps * sub), t0 = t_stage + r0;
+      const uint32_t there = open ? 0xFFFFu : (sh.present[st][r0 >> 5] >> (r0 & 31)) & 0xFFFFu;
       if (!there) continue;
       // ---- S^T = K Q^T: 8 k-steps of 16 channels --------------------------
       const uint4 ka = *reinterpret_cast<const uint4*>(stage + (r0 + rk0) * 64 + 16 * t);
@@ -261,11 +265,10 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
         }
       }
       // ---- scores, masks, the running maximum ------------------------------
-      const bool open = t0 >= all_lo && t0 + 16 <= all_hi && there == 0xFFFFu;
       bool up = false;
 #pragma unroll
       for (int c = 0; c < 4; ++c) s[c] *= mult[c & 1];
-      if (mods) {
+      if (kMods) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const float out = a.cap * kLog2e;
@@ -396,8 +399,10 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
 
 }  // namespace
 
-ExtendLaunch extend_decode(bool e1m2) {
-  return {e1m2 ? extend_decode_kernel<true> : extend_decode_kernel<false>, kThreads, kSmem};
+ExtendLaunch extend_decode(bool e1m2, bool mods) {
+  const ExtendKernel k = e1m2 ? (mods ? extend_decode_kernel<true, true> : extend_decode_kernel<true, false>)
+                              : (mods ? extend_decode_kernel<false, true> : extend_decode_kernel<false, false>);
+  return {k, kThreads, kSmem};
 }
 
 }  // namespace nvfp4
