@@ -198,7 +198,8 @@ NVFP4_API nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const
   a.group = FastDiv(static_cast<uint32_t>(num_q_heads / cache->num_kv_heads));
   a.window = options->window;
   a.scale = options->softmax_scale * cache->k_gscale;
-  // The kernels' factors of it and of its inverse stay finite; no score shows the difference.
+  // So that the kernels' factors of it and of its inverse are normal numbers.  A cap below 1e-30 makes all weights
+  // equal, one above 1e37 changes no score below 1e33: neither shows the difference.
   a.cap = options->logit_cap > 0.0f ? fminf(fmaxf(options->logit_cap, 1e-30f), 1e37f) : 0.0f;
   a.gv = cache->v_gscale;
   a.status = status_word_dev();
@@ -215,7 +216,7 @@ NVFP4_API nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const
   const bool by_tiles = p.rows == kTileRows;
   const ExtendLaunch l = by_tiles                     ? extend_tiles(e1m2, a.cap > 0.0f, a.slopes != nullptr, p.full)
                          : p.rows == 8 && !p.full ? extend_decode(e1m2, a.cap > 0.0f || a.slopes)
-                                                  : extend_rows(p.rows, e1m2, p.full);
+                                                  : extend_rows(p.rows, e1m2, a.cap > 0.0f, p.full);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // Raising the limit is idempotent.
   if (cudaFuncSetAttribute(l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(l.smem)) != cudaSuccess ||

@@ -273,6 +273,63 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+
+// A cap in the log2 domain: s <- out tanh(s in), out = c log2(e), for kN scores of a
+// lane.  y = s in.  For |y| <= 0.5 tanh(y) / y is a polynomial in y^2 (the three
+// coefficients that make the largest relative error least, 2^-20.6: a weight's is then
+// below 2^-15 for caps up to 50), two scores an FMA; a score far below the cap keeps its
+// own relative precision whatever the cap.  Else tanh(y) = 1 - 2 / (1 + 2^(2 log2(e) y)):
+// the absolute error, some 2^-22, is then relative to more than 0.46 (and the hardware
+// tanh's 2^-11 would show).  Each score takes its own form, so that a row's result does
+// not go by its neighbours'; a warp without a score past 0.5 leaves the second out, since
+// the special-function unit has every weight's exponential to do (a chunk of 2048 on
+// 16384 keys, 64 heads, took 1565 us by the second alone).
+constexpr float kTanh1 = -0.333281606f, kTanh2 = 0.132053599f, kTanh3 = -0.0447506458f;
+constexpr float kTanhRange = 0.5f;
+__device__ __forceinline__ float capped_far(float y, float out) { return fmaf(-2.0f * out, rcp(1.0f + ex2(y * (2.0f * kLog2e))), out); }
+template <int kN>
+__device__ __forceinline__ void cap_scores(float* s, float in, float out) {
+  float far[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < kN; i += 2) far[(i >> 1) & 1] = max3(fabsf(s[i]), fabsf(s[i + 1]), far[(i >> 1) & 1]);
+  const uint64_t in2 = both(in), c0 = both(out), c1 = both(out * kTanh1), c2 = both(out * kTanh2), c3 = both(out * kTanh3);
+  const auto near = [&](float a, float b) {
+    const uint64_t y = mul2(pair(a, b), in2), u = mul2(y, y);
+    return mul2(y, fma2(fma2(fma2(c3, u, c2), u, c1), u, c0));
+  };
+  if (__any_sync(0xffffffffu, fmaxf(far[0], far[1]) * in > kTanhRange)) {
+#pragma unroll
+    for (int i = 0; i < kN; i += 2) {
+      const float a = s[i] * in, b = s[i + 1] * in;
+      unpair(near(s[i], s[i + 1]), s[i], s[i + 1]);
+      if (fabsf(a) > kTanhRange) s[i] = capped_far(a, out);
+      if (fabsf(b) > kTanhRange) s[i + 1] = capped_far(b, out);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kN; i += 2) unpair(near(s[i], s[i + 1]), s[i], s[i + 1]);
+  }
+}
+// The same where in = 1 / out: out y = s, and the constants are immediates, for the
+// kernels that have no registers for them.
+template <int kN>
+__device__ __forceinline__ void cap_scores(float* s, float out) {
+  const float in = 1.0f / out;
+  float far = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kN; i += 2) far = max3(fabsf(s[i]), fabsf(s[i + 1]), far);
+  const auto near = [&](float x) {
+    const float y = x * in, u = y * y;
+    return x * fmaf(fmaf(fmaf(kTanh3, u, kTanh2), u, kTanh1), u, 1.0f);
+  };
+  if (__any_sync(0xffffffffu, far * in > kTanhRange)) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) s[i] = fabsf(s[i]) * in > kTanhRange ? capped_far(s[i] * in, out) : near(s[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) s[i] = near(s[i]);
+  }
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
@@ -361,7 +418,7 @@ struct ExtendLaunch {
   uint32_t threads, smem;
 };
 ExtendLaunch extend_tiles(bool e1m2, bool cap, bool bias, bool full);  // kTileRows a tile
-ExtendLaunch extend_rows(int rows, bool e1m2, bool full);    // 16, 24, 32; 8 with `full`
-ExtendLaunch extend_decode(bool e1m2, bool mods);            // 8
+ExtendLaunch extend_rows(int rows, bool e1m2, bool cap, bool full);  // 16, 24, 32; 8 with `full`
+ExtendLaunch extend_decode(bool e1m2, bool mods);                    // 8
 
 }  // namespace nvfp4

@@ -269,12 +269,10 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
 #pragma unroll
       for (int c = 0; c < 4; ++c) s[c] *= mult[c & 1];
       if (kMods) {
+        if (a.cap > 0.0f) cap_scores<4>(s, a.cap * kLog2e);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const float out = a.cap * kLog2e;
-          if (a.cap > 0.0f) s[c] = fmaf(-2.0f * out, rcp(1.0f + ex2(s[c] * (2.0f / a.cap))), out);
+        for (int c = 0; c < 4; ++c)
           s[c] = fmaf(-slope[c & 1], fabsf(static_cast<float>(pos[c & 1] - (t0 + (c < 2 ? rk0 : rk1)))), s[c]);
-        }
       }
       if (!open) {
 #pragma unroll

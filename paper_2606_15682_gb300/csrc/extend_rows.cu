@@ -90,7 +90,10 @@ __device__ __forceinline__ void mma_v_p(uint32_t d, uint32_t a, uint32_t b, uint
                : "memory");
 }
 
-template <int kC, bool kE1M2, bool kFull>
+// kCap: the scores may be capped.  (A kernel of its own: the cap's code in the kernel of calls
+// without one cost their softmax warps registers and instruction fetches: 32 x 6 drafted tokens
+// on 4001 keys 81.5 instead of 72.5 us.)
+template <int kC, bool kE1M2, bool kCap, bool kFull>
 __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const ExtendArgs a) {
   using C = RowsConfig<kC>;
   constexpr int kN = C::kN;
@@ -240,7 +243,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
     // (Also the barrier after which all rows' multipliers are there.)  Scores that may
     // pass 2^22 are rounded before `minus` is added, as the maxima are: else an exponent
     // could be above the largest by the rounding of one product.
-    const bool exact = any_of_128(coarse) || a.cap > 0.0f;
+    const bool exact = any_of_128(coarse) || (kCap && a.cap > 0.0f);
     const auto bias = [&](float* x, int tk) {
       if (!a.slopes) return;
       const float tf = static_cast<float>(tk);
@@ -275,11 +278,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         if (exact) {
 #pragma unroll
           for (int n = 0; n < kC; ++n) x[n] *= sh.mult[n];
-          if (a.cap > 0.0f) {
-            const float cap = a.cap * kLog2e, in = 2.0f / a.cap;  // 2 log2(e) s / c
-#pragma unroll
-            for (int n = 0; n < kC; ++n) x[n] = fmaf(-2.0f * cap, rcp(1.0f + ex2(x[n] * in)), cap);
-          }
+          if (kCap && a.cap > 0.0f) cap_scores<kC>(x, a.cap * kLog2e);
           bias(x, tk);
 #pragma unroll
           for (int n = 0; n < kC; ++n) x[n] += minus[n];
@@ -588,20 +587,24 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
   }
 }
 
-template <int kC, bool kE1M2, bool kFull>
-ExtendLaunch launch() {
-  return {extend_rows_kernel<kC, kE1M2, kFull>, kRowsThreads, RowsConfig<kC>::kBytes};
+template <int kC, bool kE1M2>
+ExtendLaunch launch(bool cap, bool full) {
+  const ExtendKernel k = full  ? extend_rows_kernel<kC, kE1M2, true, true>
+                         : cap ? extend_rows_kernel<kC, kE1M2, true, false>
+                               : extend_rows_kernel<kC, kE1M2, false, false>;
+  return {k, kRowsThreads, RowsConfig<kC>::kBytes};
 }
 template <bool kE1M2>
-ExtendLaunch pick(int rows, bool full) {
-  if (rows == 8) return launch<8, kE1M2, true>();  // else extend_decode.cu
-  if (rows == 16) return full ? launch<16, kE1M2, true>() : launch<16, kE1M2, false>();
-  if (rows == 24) return full ? launch<24, kE1M2, true>() : launch<24, kE1M2, false>();
-  return full ? launch<32, kE1M2, true>() : launch<32, kE1M2, false>();
+ExtendLaunch pick(int rows, bool cap, bool full) {
+  if (rows == 8) return {extend_rows_kernel<8, kE1M2, true, true>, kRowsThreads, RowsConfig<8>::kBytes};  // else extend_decode.cu
+  if (rows == 16) return launch<16, kE1M2>(cap, full);
+  return rows == 24 ? launch<24, kE1M2>(cap, full) : launch<32, kE1M2>(cap, full);
 }
 
 }  // namespace
 
-ExtendLaunch extend_rows(int rows, bool e1m2, bool full) { return e1m2 ? pick<true>(rows, full) : pick<false>(rows, full); }
+ExtendLaunch extend_rows(int rows, bool e1m2, bool cap, bool full) {
+  return e1m2 ? pick<true>(rows, cap, full) : pick<false>(rows, cap, full);
+}
 
 }  // namespace nvfp4

@@ -41,15 +41,7 @@ constexpr uint32_t kIdescQK = (1u << 4) | (8u << 17) | (8u << 24);
 constexpr uint32_t kIdescPV = (1u << 4) | (1u << 16) | (16u << 17) | (8u << 24);
 constexpr uint32_t kIdescPVFull = kIdescPV | (1u << 7) | (1u << 10);  // bf16 operands
 // What a row's scores are made of: x = s * mult in the log2 domain; capped,
-// x = c log2(e) tanh(y), y = s * mult / (c log2(e)).  Where the warp's scores are far
-// below the cap, |y| <= 0.5, tanh(y) / y is a polynomial in y^2 (the three coefficients
-// that make the largest relative error least, 2^-20.6: a weight's is then below 2^-15
-// for caps up to 50), two scores an FMA; else tanh(y) = 1 - 2 / (1 + 2^(2 log2(e) y)) (absolute error some 2^-22, which
-// `cap` scales; the hardware tanh's 2^-11 would show).  The special-function unit,
-// which has every weight's exponential to do, is the bound of the second: a chunk of
-// 2048 on 16384 keys, 64 heads, takes 1565 us by it.
-constexpr float kTanh[3] = {-0.333281606f, 0.132053599f, -0.0447506458f};
-constexpr float kTanhRange = 0.5f;
+// x = c log2(e) tanh(s * mult / (c log2(e))) (cap_scores).
 struct RowScore {
   float mult;   // softmax_scale * g_K * log2(e) / the query's scale
   float slope;  // slopes[h] * log2(e)
@@ -80,24 +72,7 @@ __device__ __forceinline__ void score32(float* s, const RowScore& rs, const Exte
   if (capped) {
     // (Finite, so that a score of 0 stays 0 whatever the query's scale.)
     const float out = a.cap * kLog2e, in = fminf(rs.mult / out, FLT_MAX);
-    float far[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < 32; i += 4) {
-      far[0] = max3(fabsf(s[i]), fabsf(s[i + 1]), far[0]);
-      far[1] = max3(fabsf(s[i + 2]), fabsf(s[i + 3]), far[1]);
-    }
-    if (__any_sync(0xffffffffu, fmaxf(far[0], far[1]) * in > kTanhRange)) {
-#pragma unroll
-      for (int i = 0; i < 32; ++i) s[i] = fmaf(-2.0f * out, rcp(1.0f + ex2(s[i] * (2.0f * kLog2e * in))), out);
-    } else {
-      const uint64_t in2 = both(in), c0 = both(out), c1 = both(out * kTanh[0]), c2 = both(out * kTanh[1]), c3 = both(out * kTanh[2]);
-#pragma unroll
-      for (int i = 0; i < 32; i += 2) {
-        const uint64_t y = mul2(pair(s[i], s[i + 1]), in2), u = mul2(y, y);
-        const uint64_t x = mul2(y, fma2(fma2(fma2(c3, u, c2), u, c1), u, c0));
-        unpair(x, s[i], s[i + 1]);
-      }
-    }
+    cap_scores<32>(s, in, out);
   } else if (!(biased && behind)) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) s[i] *= rs.mult;
