@@ -10,8 +10,13 @@ constexpr int kBlock = 128;      // keys per block
 constexpr int kTileRows = 256;   // rows of a tile of the many-row kernel
 constexpr float kLog2e = 1.4426950408889634f;
 
-// The running maximum moves only when a score exceeds it by 2^11: weights are kept
-// as 2^4 w, at most 2^15 in f16, whose steps end at 2^-28 of the maximum.
+// A weight is 2^(score + minus), scores in the log2 domain.  `minus` is 4 - the row's
+// running maximum, rounded once, and moves only where an exponent would pass 15: the
+// sum that is compared is the one that becomes the weight, so that no weight passes f16's
+// range whatever the scores' size (a maximum plus 11, rounded by itself past 2^24, let
+// weights of 2^16 through), and old and new weights differ by exactly the two `minus`.
+// The largest weight is 2^4 or more (below scores of 2^26, from which on 4 is lost in
+// them), and f16's steps end at 2^-28 of it.
 constexpr float kRescaleLog2 = 11.0f;
 constexpr float kWeightLog2 = 4.0f;
 

@@ -216,7 +216,8 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
     }
   }
 
-  float o[8][4], m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.0f, 0.0f};
+  // No maximum yet: any score exceeds it.
+  float o[8][4], minus[2] = {FLT_MAX, FLT_MAX}, l_run[2] = {0.0f, 0.0f};
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
   const int rk0 = tile_key(g), rk1 = tile_key(g + 8);
@@ -282,16 +283,16 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
         }
       }
 #pragma unroll
-      for (int c = 0; c < 4; ++c) up = up || s[c] > m_run[c & 1] + kRescaleLog2;
+      for (int c = 0; c < 4; ++c) up = up || s[c] + minus[c & 1] > kWeightLog2 + kRescaleLog2;
       if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           float top = fmaxf(s[c], s[c + 2]);
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-          if (top > m_run[c] + kRescaleLog2) {
-            const float shrink = ex2(m_run[c] - top);
-            m_run[c] = top;
+          if (top + minus[c] > kWeightLog2 + kRescaleLog2) {
+            const float shrink = ex2(kWeightLog2 - top - minus[c]);
+            minus[c] = kWeightLog2 - top;
             l_run[c] *= shrink;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -301,9 +302,7 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
           }
         }
       }
-      const float b0 = (m_run[0] == -INFINITY ? 0.0f : -m_run[0]) + kWeightLog2;
-      const float b1 = (m_run[1] == -INFINITY ? 0.0f : -m_run[1]) + kWeightLog2;
-      const float p0 = ex2(s[0] + b0), p1 = ex2(s[1] + b1), p2 = ex2(s[2] + b0), p3 = ex2(s[3] + b1);
+      const float p0 = ex2(s[0] + minus[0]), p1 = ex2(s[1] + minus[1]), p2 = ex2(s[2] + minus[0]), p3 = ex2(s[3] + minus[1]);
       l_run[0] += p0 + p2;
       l_run[1] += p1 + p3;
       const uint32_t pb0 = transposed(f16x2_rn(p0, p1)), pb1 = transposed(f16x2_rn(p2, p3));
@@ -354,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
 #pragma unroll
     for (int x = 4; x < 32; x <<= 1) l_run[c] += __shfl_xor_sync(0xffffffffu, l_run[c], x);
     if (g == 0) {
-      sh.m[cw][2 * t + c] = m_run[c];
+      sh.m[cw][2 * t + c] = l_run[c] == 0.0f ? -INFINITY : -minus[c];  // weights are 2^(score - m)
       sh.l[cw][2 * t + c] = l_run[c];
     }
   }

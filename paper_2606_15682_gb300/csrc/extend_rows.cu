@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         const bool live = sh.out[lr] != 0xffffffffu;
         sh.mult[lr] = live ? a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23) : 0.0f;
         coarse = coarse || !(sh.mult[lr] <= 8.0f) || !(fabsf(sh.slope[lr]) * static_cast<float>(a.map.context) <= 0x1p21f);
-        sh.minus[lr] = live ? 1e30f : 0.0f;
+        sh.minus[lr] = live ? FLT_MAX : 0.0f;
         sh.none[lr] = 0.0f;
       }
       float x[8];
@@ -323,8 +323,8 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         }
         const auto top_of = [&](int n) { return max3(max3(sh.top[0][n], sh.top[1][n], sh.top[2][n]), sh.top[3][n], -INFINITY); };
         const auto shrink = [&](int n) {
-          const float up = top_of(n) + sh.minus[n];
-          return up > kWeightLog2 + kRescaleLog2 ? ex2(kWeightLog2 - up) : 1.0f;
+          const float top = top_of(n), minus = sh.minus[n];
+          return top + minus > kWeightLog2 + kRescaleLog2 ? ex2(kWeightLog2 - top - minus) : 1.0f;
         };
 #pragma unroll
         for (int n = 0; n < kC; ++n) l[n] *= shrink(n);
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         const float sum = nblk > 0 ? (sh.sum[0][n] + sh.sum[1][n]) + (sh.sum[2][n] + sh.sum[3][n]) : 0.0f;
         const float v = sum > 0.0f ? o[n] : 0.0f;
         if (joined) {
-          if (key == 0) a.ml_ws[rec0 + n] = make_float2(sum > 0.0f ? kWeightLog2 - sh.minus[n] : -INFINITY, sum);
+          if (key == 0) a.ml_ws[rec0 + n] = make_float2(sum > 0.0f ? -sh.minus[n] : -INFINITY, sum);
           a.o_ws[(rec0 + n) * kD + channel] = v;
         } else {
           const uint32_t bits = bf16x2_rn(sum > 0.0f ? v * (a.gv / sum) : 0.0f, 0.0f);

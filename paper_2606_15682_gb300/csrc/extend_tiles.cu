@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     const bool coarse = kMods == 0 && __any_sync(0xffffffffu, !(rs.mult <= 8.0f));
     const float to_log2 = kMods || coarse ? 1.0f : rs.mult;
     const uint64_t to_log2x2 = both(to_log2);
-    float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+    float minus = FLT_MAX, l0 = 0.0f, l1 = 0.0f;  // no maximum yet: any score exceeds it
     bool ok = true;
     for (int v = 0; v < subs; ++v) {
       const int j = two ? v >> 1 : (v & ~1) + t, hf = v & 1, t0 = t_base + (nblk - 1 - j) * kBlock + 64 * hf;
@@ -267,10 +267,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
         for (int k = 8; k < 64; k += 8) tops[c] = max3(s[k + c], s[k + c + 4], tops[c]);
       }
       const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * to_log2;
-      const bool up = top > m + kRescaleLog2 || (m == -INFINITY && top > -INFINITY);
+      const bool up = top + minus > kWeightLog2 + kRescaleLog2;
       if (__any_sync(0xffffffffu, up)) {
-        const float shrink = up ? ex2(m - top) : 1.0f;  // 0 where there was none
-        if (up) m = top;
+        const float shrink = up ? ex2(kWeightLog2 - top - minus) : 1.0f;  // 0 where there was none
+        if (up) minus = kWeightLog2 - top;
         l0 *= shrink;
         l1 *= shrink;
         if (v > 0) {
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
           }
         }
       }
-      const uint64_t minus = both((m == -INFINITY ? 0.0f : -m) + kWeightLog2);
+      const uint64_t minus2 = both(minus);
       // The weights, over the scores they came from.
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           float x = s[32 * c + 2 * k], y = s[32 * c + 2 * k + 1];
-          fma2(x, y, to_log2x2, minus);
+          fma2(x, y, to_log2x2, minus2);
           x = ex2(x);
           y = ex2(y);
           add2(l0, l1, x, y);
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       set_status(a.status, NVFP4_ERR_TIMEOUT);
       sh.abort = 1;
     }
-    const float l = l0 + l1;
+    const float l = l0 + l1, m = l == 0.0f ? -INFINITY : -minus;  // weights are 2^(score - m)
     // A tile that took the other blocks of the same rows hands over its part.
     float* hand = reinterpret_cast<float*>(smem_raw + (smem - smem_u32(smem_raw)) + kOffK);  // [channel][row]
     float other_m = -INFINITY, other_l = 0.0f;
