@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_tile = tmem + lanes + t * 128, o_col = tmem + lanes + 256 + t * 128;
     RowScore rs;
-    rs.mult = sh.mult[live ? local : 0];
+    rs.mult = sh.mult[local];  // rows past the tile's have one too, of their own warp or behind the barrier
     rs.slope = (kMods & kBias) && a.slopes && live ? __ldg(a.slopes + head) * kLog2e : 0.0f;
     // Keys that every row of the warp sees need no mask.
     const int all_lo = __reduce_max_sync(0xffffffffu, live ? vis.x : 0);
