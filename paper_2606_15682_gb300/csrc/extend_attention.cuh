@@ -67,10 +67,11 @@ __device__ __forceinline__ Seq sequence(const ExtendArgs& a, uint32_t b) {
   return s;
 }
 
-// Keys that the query at position p sees: [lo, hi).
+// Keys that the query at position p >= 0 sees: [lo, hi).  (A query before its sequence's first
+// token, p < 0, sees none; p is raised to 0 so that no window reaches past 32 bits.)
 __device__ __forceinline__ int2 visible(const ExtendArgs& a, int p, int len, int prefix, int doc) {
   int lo = max(doc, 0);
-  if (a.window) lo = max(lo, p - a.window + 1);
+  if (a.window) lo = max(lo, max(p, 0) - a.window + 1);
   return make_int2(lo, min(len, max(p + 1, prefix)));
 }
 
@@ -119,7 +120,8 @@ struct Span {
   uint32_t parts;
 };
 __device__ __forceinline__ Span span_of(const ExtendArgs& a, const Seq& s) {
-  const int lo = a.window ? max(0, s.len - static_cast<int>(s.n) + 1 - a.window) : 0;
+  const int first = max(0, s.len - static_cast<int>(s.n));  // position of the first query that sees any
+  const int lo = a.window ? max(0, first + 1 - a.window) : 0;
   const uint32_t keys = static_cast<uint32_t>(max(s.len - lo, 0)), part = a.part_blocks * kBlock;
   return {lo, max(1u, (keys + part - 1) / part)};
 }
