@@ -43,7 +43,8 @@ struct RowsShared {
   int lo, hi, all_lo, all_hi, rows;
   alignas(16) float mult[kC];  // score -> log2 domain
   alignas(16) float minus[kC], none[kC];  // 4 - the row's maximum: x = score + minus is a weight's exponent
-  alignas(16) float slope[kC], pos[kC];  // slopes[h] log2(e); the query's position
+  int pos0;  // the position of the tile's first query, from which the others and the keys are counted
+  alignas(16) float slope[kC], pos[kC];  // slopes[h] log2(e); the query's position from pos0
   alignas(16) int first[kC], last[kC];  // keys that it sees: first <= t < last
   uint32_t out[kC];                     // its row of the output; past the tile's rows: none
   float top[4][kC], sum[4][kC];
@@ -137,10 +138,11 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       vis = visible(a, pos, sq.len, a.prefix_lens ? __ldg(a.prefix_lens + tl.b) : 0,
                     a.doc_start ? __ldg(a.doc_start + sq.first + tok) : 0);
     if (vis.x >= vis.y) vis = make_int2(0x7fffffff, 0);
+    const int pos0 = __shfl_sync(0xffffffffu, pos, 0);
     if (lane < kC) {
       sh.first[lane] = vis.x;
       sh.last[lane] = vis.y;
-      sh.pos[lane] = static_cast<float>(pos);
+      sh.pos[lane] = static_cast<float>(pos - pos0);
       sh.slope[lane] = a.slopes && live ? __ldg(a.slopes + h) * kLog2e : 0.0f;
       sh.out[lane] = live ? (sq.first + tok) * a.hq + h : 0xffffffffu;
     }
@@ -156,6 +158,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       sh.lo = h > l ? l : 0;
       sh.hi = h > l ? h : 0;
       sh.rows = static_cast<int>(rows);
+      sh.pos0 = pos0;
       sh.all_lo = all_lo;
       sh.all_hi = all_hi;
     }
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
     const bool exact = any_of_128(coarse) || (kCap && a.cap > 0.0f);
     const auto bias = [&](float* x, int tk) {
       if (!a.slopes) return;
-      const float tf = static_cast<float>(tk);
+      const float tf = static_cast<float>(tk - sh.pos0);
 #pragma unroll
       for (int n = 0; n < kC; n += 4) {
         const float4 f = *reinterpret_cast<const float4*>(&sh.slope[n]), at = *reinterpret_cast<const float4*>(&sh.pos[n]);

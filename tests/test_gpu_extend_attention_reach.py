@@ -10,6 +10,7 @@ import _paged as P
 from _util import lib
 from test_gpu_extend_attention import queries, run
 from test_gpu_extend_attention_long import check as check_long
+from test_gpu_extend_attention_long import reference
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +32,32 @@ def test_windows_past_every_key(N, news, lens, window, hq, hkv, capacity):
     out = check_long(N, case, q, news, window=window)
     assert torch.equal(out, run(N, case, q, news))
     assert N.nvfp4_get_device_status() == 0
+
+
+@pytest.mark.parametrize("tokens", [1, 3, 5, 6, 60])
+@pytest.mark.parametrize("length", [2 ** 24 + 41, 2 ** 25 + 1])
+def test_distance_bias_at_positions_past_24_bits(N, tokens, length):
+    """Only the last pages are there.  |p - t| is a small number also where p and t themselves need more bits than fp32 has."""
+    page, hq, present = 4096, 5, 2
+    per = -(-length // page)
+    case = P.Case(N, [page * present], 1, page, 0, seed=610)
+    shown = case.table[0].copy()
+    table = np.full((1, per), -1, np.int32)
+    table[0, per - present:] = shown
+    case.lens, case.per = [length], per
+    case.lens_dev.copy_(torch.tensor([length], dtype=torch.int32))
+    case.set_table(table)
+    q = queries(tokens, hq, 41)
+    slopes = np.array([0.5, 0.25, 0.1, 1.0, 2.0], np.float32)
+    got = run(N, case, q, [tokens], slopes=torch.from_numpy(slopes).cuda())
+    torch.cuda.synchronize()
+    assert N.nvfp4_get_device_status() == 0
+    # The same keys and distances in a sequence that starts at the first page that is there.
+    first = (per - present) * page
+    case.lens, case.per = [length - first], present
+    case.lens_dev.copy_(torch.tensor(case.lens, dtype=torch.int32))
+    case.set_table(shown[None, :])
+    check_long(N, case, q, [tokens], slopes=slopes)
+    want, bound, _ = reference(case, q, [tokens], slopes=slopes)
+    over = np.abs(got.double().cpu().numpy() - want) - (P.half_ulp(want) * (1 + 2.0 ** -6) + bound)
+    assert over.max() <= 0, f"worst excess {over.max():.3e}"
