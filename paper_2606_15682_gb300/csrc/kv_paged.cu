@@ -75,10 +75,10 @@ __global__ void __launch_bounds__(kThreads, 4) append_axes_kernel(const AppendAr
   const float qmax = kE1M2 ? 3.5f : 6.0f;
   const float max_k = __fmul_rn(qmax, a.gk), max_v = __fmul_rn(qmax, a.gv);
 
-  // The lane's 2 x 16 bytes of head h.
+  // The lane's 2 x 16 bytes of head h; of a query off the rotary table zeros, whatever it holds.
   const auto load = [&](uint32_t h, uint4* lo, uint4* hi) {
     *lo = *hi = make_uint4(0, 0, 0, 0);
-    if (!live || h >= a.heads) return;
+    if (!live || h >= a.heads || (!rotary_ok && h < a.hq)) return;
     const uint16_t* src = h < a.hq               ? a.q + tok * a.ld_q + h * 128u
                           : h < a.hq + a.map.hkv ? a.k + tok * a.ld_k + (h - a.hq) * 128u
                                                  : a.v + tok * a.ld_v + (h - a.hq - a.map.hkv) * 128u;
