@@ -600,7 +600,8 @@ typedef struct {
  *   t >= doc_start, t > p - window, and t <= p or t < prefix_lens[b];
  *   s_t = softmax_scale q . K_hat[t], capped, then biased; out = softmax(s) V_hat,
  * kv head = h / (num_q_heads / num_kv_heads).  A query that sees nothing (n_b >
- * len_b, a document that starts after it, absent pages) gets zeros.  Cached
+ * len_b, a document that starts after it, absent pages) gets zeros; one with an
+ * infinity or a NaN that sees a key gets NaN, and no other row does.  Cached
  * rows past len_b are never used, whatever their bytes.
  * Softmax, sums and products are accumulated in fp32; Q enters the tensor core
  * as f16 after an exact power-of-two scaling of each row, and K as exact f16.

@@ -410,6 +410,22 @@ __device__ __forceinline__ uint4 q_chunk(const float x[8], float down) {
   return make_uint4(f[0], f[1], f[2], f[3]);
 }
 
+// A query row's scaling by a power of two to below 1, from the bits of its largest |x|
+// (amax_bits_bf16x8): down = 2^-e, up = 2^e, both normal numbers.  A row with an infinity
+// or a NaN becomes NaN in every channel, so that all its scores are NaN, and its result
+// whatever the signs of the keys that it meets.
+struct RowScale {
+  float down, up;
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t top) {
+  const int e = max(-125, min(static_cast<int>(top >> 7) - 126, 126));
+  if (top >= 0x7F80u) return {__uint_as_float(0x7FC00000u), 1.0f};
+  return {__uint_as_float(static_cast<uint32_t>(127 - e) << 23), __uint_as_float(static_cast<uint32_t>(127 + e) << 23)};
+}
+// The factor of a row's output from the sum of its weights: 0 where it sees no key (a sum
+// of 0 exactly), NaN where a weight was.
+__device__ __forceinline__ float per_sum(float sum, float gv) { return sum == 0.0f ? 0.0f : gv / sum; }
+
 // Two f16 values of at most 7 significant bits, at least 2^-14 or zero -> bf16,
 // exact: the 5-bit exponent moves into the 8-bit field, 2^112 makes up for the bias.
 __device__ __forceinline__ uint32_t bf16x2_of_f16x2(uint32_t h) {

@@ -199,16 +199,15 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
     }
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int e = max(-125, min(static_cast<int>(top >> 7) - 126, 126));
-    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-    const float up = a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+    const RowScale by = row_scale(top);
+    const float up = a.scale * kLog2e * by.up;
     mult[0] = __shfl_sync(0xffffffffu, up, (2 * t) * 4);
     mult[1] = __shfl_sync(0xffffffffu, up, (2 * t + 1) * 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float x[8];
       unpack_bf16x8(w[i], x);
-      const uint4 f = q_chunk<kE1M2>(x, down);  // k-steps 2i and 2i + 1
+      const uint4 f = q_chunk<kE1M2>(x, by.down);  // k-steps 2i and 2i + 1
       qf[4 * i] = f.x;
       qf[4 * i + 1] = f.y;
       qf[4 * i + 2] = f.z;
@@ -386,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
       if (c == 0) a.ml_ws[rec] = make_float2(big, sum);
       if (big != -INFINITY) *reinterpret_cast<float4*>(a.o_ws + rec * kD + c) = make_float4(acc[0], acc[1], acc[2], acc[3]);
     } else {
-      const float f = sum > 0.0f ? a.gv / sum : 0.0f;
+      const float f = per_sum(sum, a.gv);
       const uint32_t r = tile.row0 + lr, tok = a.group.div(r);
       *reinterpret_cast<uint2*>(a.out + (static_cast<uint64_t>(seq.first + tok) * a.hq + kvh * group + r - tok * group) * kD + c) =
           make_uint2(bf16x2_rn(acc[0] * f, acc[1] * f), bf16x2_rn(acc[2] * f, acc[3] * f));

@@ -225,19 +225,18 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       uint32_t top = amax_bits_bf16x8(w[i]);
 #pragma unroll
       for (int s = 1; s < 16; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-      const int e = max(-125, min(static_cast<int>(top >> 7) - 126, 126));
-      const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+      const RowScale by = row_scale(top);
       if (c == 0 && lr < kC) {
         // No maximum yet: any score exceeds it.  (A row past the tile's has scores of 0.)
         const bool live = sh.out[lr] != 0xffffffffu;
-        sh.mult[lr] = live ? a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23) : 0.0f;
+        sh.mult[lr] = live ? a.scale * kLog2e * by.up : 0.0f;
         coarse = coarse || !(sh.mult[lr] <= 8.0f) || !(fabsf(sh.slope[lr]) * static_cast<float>(a.map.context) <= 0x1p21f);
         sh.minus[lr] = live ? FLT_MAX : 0.0f;
         sh.none[lr] = 0.0f;
       }
       float x[8];
       unpack_bf16x8(w[i], x);
-      const uint4 f = q_chunk<kE1M2>(x, down);
+      const uint4 f = q_chunk<kE1M2>(x, by.down);
       sts128(smem + C::kOffQ + (c >> 3) * (kN * 128) + lr * 128 + (((c ^ lr) & 7) << 4), f.x, f.y, f.z, f.w);
     }
     fence_proxy_async_smem();
@@ -403,12 +402,12 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       for (int n = 0; n < kC; ++n) {
         if (n >= sh.rows) break;
         const float sum = nblk > 0 ? (sh.sum[0][n] + sh.sum[1][n]) + (sh.sum[2][n] + sh.sum[3][n]) : 0.0f;
-        const float v = sum > 0.0f ? o[n] : 0.0f;
+        const float v = sum == 0.0f ? 0.0f : o[n];
         if (joined) {
-          if (key == 0) a.ml_ws[rec0 + n] = make_float2(sum > 0.0f ? -sh.minus[n] : -INFINITY, sum);
+          if (key == 0) a.ml_ws[rec0 + n] = make_float2(sum == 0.0f ? -INFINITY : -sh.minus[n], sum);
           a.o_ws[(rec0 + n) * kD + channel] = v;
         } else {
-          const uint32_t bits = bf16x2_rn(sum > 0.0f ? v * (a.gv / sum) : 0.0f, 0.0f);
+          const uint32_t bits = bf16x2_rn(v * per_sum(sum, a.gv), 0.0f);
           a.out[static_cast<uint64_t>(sh.out[n]) * kD + channel] = static_cast<uint16_t>(bits);
         }
       }

@@ -197,13 +197,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
         uint32_t top = amax_bits_bf16x8(w[i]);
 #pragma unroll
         for (int s = 1; s < 16; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-        // 2^-e with 2^e > amax, both within the normal fp32 range.
-        const int e = max(-125, min(static_cast<int>(top >> 7) - 126, 126));
-        const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-        if (c == 0) sh.mult[lr] = a.scale * kLog2e * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+        const RowScale by = row_scale(top);
+        if (c == 0) sh.mult[lr] = a.scale * kLog2e * by.up;
         float x[8];
         unpack_bf16x8(w[i], x);
-        const uint4 f = q_chunk<kE1M2>(x, down);
+        const uint4 f = q_chunk<kE1M2>(x, by.down);
         sts128(smem + (lr >> 7) * kOperand + operand_chunk(lr & 127, c), f.x, f.y, f.z, f.w);
       }
       fence_proxy_async_smem();
@@ -358,7 +356,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       const float big = fmaxf(m, other_m);
       const float w0 = m == -INFINITY ? 0.0f : ex2(m - big), w1 = other_m == -INFINITY ? 0.0f : ex2(other_m - big);
       const float sum = w0 * l + w1 * other_l;
-      const float f = a.splits > 1 ? 1.0f : sum > 0.0f ? a.gv / sum : 0.0f;
+      const float f = a.splits > 1 ? 1.0f : per_sum(sum, a.gv);
       const uint64_t rec0 = ((static_cast<uint64_t>(tile_id) * a.map.hkv + kvh) * a.splits + split) * kTileRows;
       if (a.splits > 1 && live) a.ml_ws[rec0 + local] = make_float2(big, sum);
       const uint32_t stage = smem + warp * 8192, row0 = local - lane;
