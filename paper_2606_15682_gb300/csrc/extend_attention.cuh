@@ -422,6 +422,9 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top) {
   if (top >= 0x7F80u) return {__uint_as_float(0x7FC00000u), 1.0f};
   return {__uint_as_float(static_cast<uint32_t>(127 - e) << 23), __uint_as_float(static_cast<uint32_t>(127 + e) << 23)};
 }
+// What a row's products of Q and K are multiplied by.  Kept a normal number: hidden scores, minus
+// infinity, may be multiplied by it, and products of 0.
+__device__ __forceinline__ float score_factor(float scale, float up) { return fminf(fmaxf(scale * kLog2e * up, FLT_MIN), FLT_MAX); }
 // The factor of a row's output from the sum of its weights: 0 where it sees no key (a sum
 // of 0 exactly), NaN where a weight was.
 __device__ __forceinline__ float per_sum(float sum, float gv) { return sum == 0.0f ? 0.0f : gv / sum; }

@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const RowScale by = row_scale(top);
-    const float up = a.scale * kLog2e * by.up;
+    const float up = score_factor(a.scale, by.up);
     mult[0] = __shfl_sync(0xffffffffu, up, (2 * t) * 4);
     mult[1] = __shfl_sync(0xffffffffu, up, (2 * t + 1) * 4);
 #pragma unroll

@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       if (c == 0 && lr < kC) {
         // No maximum yet: any score exceeds it.  (A row past the tile's has scores of 0.)
         const bool live = sh.out[lr] != 0xffffffffu;
-        sh.mult[lr] = live ? a.scale * kLog2e * by.up : 0.0f;
+        sh.mult[lr] = live ? score_factor(a.scale, by.up) : 0.0f;
         coarse = coarse || !(sh.mult[lr] <= 8.0f) || !(fabsf(sh.slope[lr]) * static_cast<float>(a.map.context) <= 0x1p21f);
         sh.minus[lr] = live ? FLT_MAX : 0.0f;
         sh.none[lr] = 0.0f;

@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
 #pragma unroll
         for (int s = 1; s < 16; s <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
         const RowScale by = row_scale(top);
-        if (c == 0) sh.mult[lr] = a.scale * kLog2e * by.up;
+        if (c == 0) sh.mult[lr] = score_factor(a.scale, by.up);
         float x[8];
         unpack_bf16x8(w[i], x);
         const uint4 f = q_chunk<kE1M2>(x, by.down);

@@ -61,3 +61,31 @@ def test_distance_bias_at_positions_past_24_bits(N, tokens, length):
     want, bound, _ = reference(case, q, [tokens], slopes=slopes)
     over = np.abs(got.double().cpu().numpy() - want) - (P.half_ulp(want) * (1 + 2.0 ** -6) + bound)
     assert over.max() <= 0, f"worst excess {over.max():.3e}"
+
+
+@pytest.mark.parametrize("news", [[1, 1], [4, 4], [150, 20], [40, 40]])
+@pytest.mark.parametrize("scale", [1e-9, 1e-30, 1e-38])
+@pytest.mark.parametrize("capacity", [0, 400])
+@pytest.mark.parametrize("opt", [{}, dict(window=70), dict(logit_cap=5.0)])
+def test_scales_and_queries_whose_product_underflows(N, news, scale, capacity, opt):
+    """Scores of zero: a plain mean of the visible V, with keys hidden from some of a tile's rows."""
+    lens = [390, 200] if capacity else [1500, 800]
+    case = P.Case(N, lens, 2, 0, 0, seed=620, capacity=capacity or None)
+    for spread in (0.0, 2.0 ** -100, 1.0):
+        check_long(N, case, queries(sum(news), 10, 42, spread=spread), news, scale=scale, **opt)
+    assert N.nvfp4_get_device_status() == 0
+
+
+@pytest.mark.parametrize("news", [[1, 1], [4, 4], [150, 20]])
+@pytest.mark.parametrize("capacity", [0, 400])
+def test_zero_keys_under_scales_and_queries_whose_product_overflows(N, news, capacity):
+    """Every product of Q and K is 0, and so is every score."""
+    lens = [390, 200] if capacity else [1500, 800]
+    case = P.Case(N, lens, 2, 0, 0, seed=630, capacity=capacity or None)
+    codes, scales = case.data["k"]
+    case.data["k"] = (np.zeros_like(codes), scales)
+    case.cache.k_codes.zero_()
+    q = queries(sum(news), 10, 43, spread=2.0 ** 125)
+    check_long(N, case, q, news, scale=1e4)
+    check_long(N, case, q, news, scale=3e38, window=70)
+    assert N.nvfp4_get_device_status() == 0
