@@ -564,7 +564,8 @@ nvfp4_status kv_append_rope_axes_nvfp4(const nvfp4_kv_cache* cache, const nvfp4_
 /*
  * Cached rows back as bf16: k_out[i, h] = bf16_rne(e2m1 * e4m3 * g_K) (E1M2 by
  * kv_format) of token pos[i] of sequence seq_idx[i], and v_out likewise; the
- * product is formed in fp32, where e2m1 * e4m3 is exact.
+ * product is formed in fp32, where e2m1 * e4m3 is exact.  What comes back is what
+ * the cache holds: of keys appended with a k_shift m, K~ = R(K_pre) - m.
  *   seq_idx, pos : device int32 [n].
  *   k_out, v_out : [n, num_kv_heads, 128] bf16, dense; one of them may be NULL.
  * A row outside the cache or on an absent page reads as zeros and sets CAPACITY
@@ -576,7 +577,11 @@ nvfp4_status kv_read_nvfp4(const nvfp4_kv_cache* cache, const nvfp4_kv_pages* pa
 /* What a score is made of, and which keys a query sees (extend_attention_nvfp4). */
 typedef struct {
   float softmax_scale;        /* > 0                                          */
-  float logit_cap;            /* c > 0: s <- c tanh(s / c); 0: no cap         */
+  float logit_cap;            /* c > 0: s <- c tanh(s / c); 0: no cap.  Over
+                                 a cache that holds shifted keys K - m the
+                                 scores that it sees lack q . m: not the capped
+                                 attention of K.  (Without a cap q . m is the
+                                 same for all keys and falls out.)            */
   const float* slopes;        /* device float [num_q_heads], or NULL: s <- s -
                                  slopes[h] * |p - t|, after the cap           */
   int32_t window;             /* w > 0: keys t > p - w only; 0: no window     */

@@ -99,7 +99,13 @@ class Batch:
         lens += self.n_new
 
     def run(self, layers, x, norm_out, rope_pos=None, logit_cap=0.0, window=0):
-        """x [n, H] bf16 -> the last norm's output [n, H]; rope_pos [n, axes] int32 (None: the place in the sequence)."""
+        """x [n, H] bf16 -> the last norm's output [n, H]; rope_pos [n, axes] int32 (None: the place in the sequence).
+
+        A cap and a key shift exclude each other: the cache holds K - m, whose scores differ from K's by q.m.  A softmax
+        does not see that, a cap does.
+        """
+        if logit_cap and any(w.k_shift is not None for w in layers):
+            raise ValueError("logit_cap needs the keys themselves: a layer with k_shift caches K - m")
         self.begin()
         rope_pos = self.pos[:, None] if rope_pos is None else rope_pos
         r, y = x, None
