@@ -549,7 +549,7 @@ typedef struct {
  * outside the cache (or on an absent page) is not stored; one with a rotary
  * position outside the table is not stored either and its q_out rows are zero;
  * both set CAPACITY on the device.  Two tokens of one call with the same place
- * leave either row there.
+ * leave a row there whose bytes are of either.
  * Pointers and ld in 16-B steps (ALIGN; seq_idx, pos, rope_pos 4 B), ld at
  * least heads * 128 when n_new > 1, num_q_heads >= 1, n_axes and axis_of_pair
  * in range (SHAPE, INVALID_ARG); n_new == 0 is a no-op.
@@ -608,11 +608,16 @@ typedef struct {
  * len_b, a document that starts after it, absent pages) gets zeros; one with an
  * infinity or a NaN that sees a key gets NaN, and no other row does.  Cached
  * rows past len_b are never used, whatever their bytes.
- * Softmax, sums and products are accumulated in fp32; Q enters the tensor core
- * as f16 after an exact power-of-two scaling of each row, and K as exact f16.
- * Contexts of at most 512 keys take the softmax weights in two bf16 terms (some
- * 16 bits) and V as exact bf16; longer ones the weights rounded to f16 (11 bits;
- * 2^-29 of the largest weight below f16's normal range) and V as exact f16.
+ * Softmax, sums and products are accumulated in fp32; K enters the tensor core
+ * as exact f16, Q as f16 after each row is scaled by a power of two to below 1:
+ * its channels within 2^-16 of the row's largest exactly, smaller ones to within
+ * 2^-24 of it.
+ * The buffers' context (below) chooses the weights' precision, for every sequence
+ * of a call: up to 512 tokens two bf16 terms (some 16 bits) and V as exact bf16;
+ * from 513 on weights rounded to f16 (11 bits; 2^-29 of the largest weight below
+ * f16's normal range) and V as exact f16, also for a sequence that is short itself.
+ * The second shows where all of a row's heavy keys hold a zero in a channel, so that
+ * weights near 2^-29 are what is left in it.
  * Where the queries are too few to occupy the GPU, the keys of a group of rows
  * are split and the parts are joined in a fixed order: the result is the same
  * bits in every run for the same arguments, lengths and buffer sizes.

@@ -72,9 +72,10 @@ struct Plan {
   bool full;            // weights in two terms
 };
 
-// Contexts of up to this many keys take weights in two bf16 terms: among few keys
-// the heavy ones may all hold a zero in a channel, and then what f16 loses of the
-// light ones is the result.
+// Buffers of up to this many keys a sequence take weights in two bf16 terms: among few
+// keys the heavy ones may all hold a zero in a channel, and then what f16 loses of the
+// light ones is the result.  (By the buffers, since the lengths are on the device: a
+// short sequence in a wide table has f16's bound, 2^-29 of its largest weight.)
 constexpr int64_t kFullContext = 512;
 
 // Which kernel, the tiles (at most), and the parts that each tile's keys are cut into.

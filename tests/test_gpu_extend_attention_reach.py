@@ -89,3 +89,18 @@ def test_zero_keys_under_scales_and_queries_whose_product_overflows(N, news, cap
     check_long(N, case, q, news, scale=1e4)
     check_long(N, case, q, news, scale=3e38, window=70)
     assert N.nvfp4_get_device_status() == 0
+
+
+@pytest.mark.parametrize("lens", [[1, 2, 3, 5, 9], [20, 40, 16, 17, 64], [129, 300, 512, 90, 250]])
+@pytest.mark.parametrize("new", [1, 2, 4, 6, 60])
+@pytest.mark.parametrize("capacity", [513, 8192])
+def test_short_sequences_in_a_wide_table(N, lens, new, capacity):
+    """The buffers' context chooses the weights' precision: f16's stated bound, 2^-29 of the largest weight, at any length."""
+    hq, hkv = 10, 2
+    news = [min(new, n) for n in lens]
+    case = P.Case(N, lens, hkv, 64, 0, seed=640, capacity=capacity)
+    for spread in (1.0, 60.0):  # weights that fall off slowly and fast
+        q = queries(sum(news), hq, 44, spread=spread)
+        check_long(N, case, q, news)
+        check_long(N, case, q, news, slopes=np.linspace(0.02, 1.0, hq).astype(np.float32))
+    assert N.nvfp4_get_device_status() == 0
