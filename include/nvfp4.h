@@ -677,7 +677,9 @@ nvfp4_status nvfp4_get_device_status(int32_t* status_host, void* stream);
  *     producer leaves its first ring stage neither armed nor loaded, so the
  *     consumers' bounded wait on it runs out after ~2 s: the call reports
  *     NVFP4_ERR_TIMEOUT through nvfp4_get_device_status, its output is
- *     undefined, and the device stays usable.
+ *     undefined, and the device stays usable.  In the next
+ *     extend_attention_nvfp4, if that comes first, CTA 0's first K stage waits
+ *     for an arrival that never comes, with the same end in each of its kernels.
  *   NVFP4_FAULT_GEMM_SKIP_STAGE: in the next GEMM launch (nvfp4_linear,
  *     mxfp4_linear, nvfp4_linear_dynamic and the fused SwiGLU calls, whichever
  *     kernel serves the shape), the first CTA, or both CTAs of the first CTA

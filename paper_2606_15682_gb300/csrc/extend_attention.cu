@@ -204,6 +204,7 @@ NVFP4_API nvfp4_status extend_attention_nvfp4(const nvfp4_kv_cache* cache, const
   a.cap = options->logit_cap > 0.0f ? fminf(fmaxf(options->logit_cap, 1e-30f), 1e37f) : 0.0f;
   a.gv = cache->v_gscale;
   a.status = status_word_dev();
+  a.fault_lose_stage = take_fault(NVFP4_FAULT_ATTN_SKIP_STAGE) ? 1 : 0;
   const Plan p = plan_for(a.map.batch, n_tokens, a.group.d, a.map.hkv, a.map.context, !q_start);
   const int64_t grid = p.tiles * a.map.hkv * p.splits;
   if (grid >= (1ll << 31)) return NVFP4_ERR_SHAPE;

@@ -41,7 +41,13 @@ struct ExtendArgs {
   uint32_t part_blocks;           // blocks of a part; 0: each tile's keys in `splits` equal parts
   float* o_ws;                    // [tile][kv head][split][row][128] and, behind them,
   float2* ml_ws;                  // (max, sum) of each such row; unused with one part
+  // Test-only (nvfp4_debug_inject_fault): CTA 0's first K stage waits for an arrival that
+  // never comes.
+  int fault_lose_stage;
 };
+__device__ __forceinline__ uint32_t lost_arrivals(const ExtendArgs& a, int stage) {
+  return a.fault_lose_stage && blockIdx.x == 0 && stage == 0 ? 1u : 0u;
+}
 
 // Tokens of sequence b: its first query, how many, and its cached length.
 struct Seq {

@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kRing; ++i) {
-      mbar_init(&sh.full[i], 1 + 32);  // the armed bytes, and each lane's own copies
+      mbar_init(&sh.full[i], 1 + 32 + lost_arrivals(a, i));  // the armed bytes, and each lane's own copies
       mbar_init(&sh.empty[i], kWarps);
     }
     sh.abort = 0;
@@ -103,6 +103,7 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
     // the lane's own copies.  A key that is not there (past the end, or its page
     // absent) gets scales of zero, whatever its codes' bytes.
     const int64_t head = static_cast<int64_t>(kvh) * a.map.size.d;
+    int issued = 0;
     for (int i = 0; i < n; ++i) {
       const int st = i & 1, t0 = t_base + (n - 1 - i) * kBlock;  // the newest keys first: maxima settle early
       int64_t row[4];
@@ -149,12 +150,14 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
         asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to + kBlock * 8), "l"(a.map.v_scales + at * 8) : "memory");
       }
       asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.full[st])) : "memory");
+      issued = i + 1;
     }
     // Copies in flight land before the CTA's memory goes to another (its
-    // consumers have waited for them unless a wait ran out).
+    // consumers have waited for them unless a wait ran out): the last two stages issued.
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (sh.abort)
-      for (int i = max(n - 2, 0); i < n; ++i) mbar_wait_bounded(&sh.full[i & 1], (i >> 1) & 1, nullptr, kDrainLimitNs);
+      for (int i = max(issued - 2, 0); i < issued; ++i)
+        mbar_wait_bounded(&sh.full[i & 1], (i >> 1) & 1, nullptr, kDrainLimitNs);
     return;
   }
 

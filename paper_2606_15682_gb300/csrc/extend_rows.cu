@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.s_full[i], 1);
-      mbar_init(&sh.k_full[i], 4);
+      mbar_init(&sh.k_full[i], 4 + lost_arrivals(a, i));
       mbar_init(&sh.k_free[i], 1);
       mbar_init(&sh.v_full[i], 4);
       mbar_init(&sh.v_free[i], 1);

@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.k_full[i], 4);
+      mbar_init(&sh.k_full[i], 4 + lost_arrivals(a, i));
       mbar_init(&sh.k_empty[i], 2);
       mbar_init(&sh.v_full[i], 4);
       mbar_init(&sh.v_empty[i], 2);
