@@ -57,7 +57,9 @@ __global__ void __launch_bounds__(256) extend_combine_kernel(const ExtendArgs a)
     }
     const float f = per_sum(sum, a.gv);
     const uint32_t r = t.row0 + local, tok = a.group.div(r), head = kvh * a.group.d + (r - tok * a.group.d);
-    reinterpret_cast<uint2*>(a.out + (static_cast<uint64_t>(seq.first + tok) * a.hq + head) * kD)[lane] =
+    const uint64_t row = static_cast<uint64_t>(seq.first + tok) * a.hq + head;
+    if (!out_in_bounds(a, row)) continue;
+    reinterpret_cast<uint2*>(a.out + row * kD)[lane] =
         make_uint2(bf16x2_rn(o.x * f, o.y * f), bf16x2_rn(o.z * f, o.w * f));
   }
 }

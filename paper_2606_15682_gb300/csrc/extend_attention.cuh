@@ -49,6 +49,15 @@ __device__ __forceinline__ uint32_t lost_arrivals(const ExtendArgs& a, int stage
   return a.fault_lose_stage && blockIdx.x == 0 && stage == 0 ? 1u : 0u;
 }
 
+// Bounds-checked build: a (token, head) row of the output, a row's record of a part.
+__device__ __forceinline__ bool out_in_bounds(const ExtendArgs& a, uint64_t row) {
+  return in_bounds(a.status, row < static_cast<uint64_t>(a.n_tokens) * a.hq);
+}
+template <int kRows>
+__device__ __forceinline__ bool record_in_bounds(const ExtendArgs& a, uint64_t rec) {
+  return in_bounds(a.status, rec < static_cast<uint64_t>(a.tiles) * a.map.hkv * a.splits * kRows);
+}
+
 // Tokens of sequence b: its first query, how many, and its cached length.
 struct Seq {
   uint32_t first, n;

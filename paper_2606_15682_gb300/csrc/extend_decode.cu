@@ -385,12 +385,15 @@ __global__ void __launch_bounds__(kThreads, 4) extend_decode_kernel(const Extend
     }
     if (parts > 1) {
       const uint64_t rec = ((static_cast<uint64_t>(sh.item.tile_id) * a.map.hkv + kvh) * a.splits + sh.item.part) * kRows + lr;
+      if (!record_in_bounds<kRows>(a, rec)) continue;
       if (c == 0) a.ml_ws[rec] = make_float2(big, sum);
       if (big != -INFINITY) *reinterpret_cast<float4*>(a.o_ws + rec * kD + c) = make_float4(acc[0], acc[1], acc[2], acc[3]);
     } else {
       const float f = per_sum(sum, a.gv);
       const uint32_t r = tile.row0 + lr, tok = a.group.div(r);
-      *reinterpret_cast<uint2*>(a.out + (static_cast<uint64_t>(seq.first + tok) * a.hq + kvh * group + r - tok * group) * kD + c) =
+      const uint64_t row = static_cast<uint64_t>(seq.first + tok) * a.hq + kvh * group + r - tok * group;
+      if (!out_in_bounds(a, row)) continue;
+      *reinterpret_cast<uint2*>(a.out + row * kD + c) =
           make_uint2(bf16x2_rn(acc[0] * f, acc[1] * f), bf16x2_rn(acc[2] * f, acc[3] * f));
     }
   }

@@ -403,6 +403,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
         if (n >= sh.rows) break;
         const float sum = nblk > 0 ? (sh.sum[0][n] + sh.sum[1][n]) + (sh.sum[2][n] + sh.sum[3][n]) : 0.0f;
         const float v = sum == 0.0f ? 0.0f : o[n];
+        if (!(joined ? record_in_bounds<kC>(a, rec0 + n) : out_in_bounds(a, sh.out[n]))) continue;
         if (joined) {
           if (key == 0) a.ml_ws[rec0 + n] = make_float2(sum == 0.0f ? -INFINITY : -sh.minus[n], sum);
           a.o_ws[(rec0 + n) * kD + channel] = v;

@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       const float sum = w0 * l + w1 * other_l;
       const float f = a.splits > 1 ? 1.0f : per_sum(sum, a.gv);
       const uint64_t rec0 = ((static_cast<uint64_t>(tile_id) * a.map.hkv + kvh) * a.splits + split) * kTileRows;
-      if (a.splits > 1 && live) a.ml_ws[rec0 + local] = make_float2(big, sum);
+      if (a.splits > 1 && live && record_in_bounds<kTileRows>(a, rec0 + local)) a.ml_ws[rec0 + local] = make_float2(big, sum);
       const uint32_t stage = smem + warp * 8192, row0 = local - lane;
       const auto at = [&](uint32_t row, uint32_t c) { return stage + row * 256 + ((c ^ (row & 7)) << 4); };
 #pragma unroll 1
@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const uint32_t row = 4 * i + (lane >> 3);
-          if (row0 + row < rows)
+          if (row0 + row < rows && record_in_bounds<kTileRows>(a, rec0 + row0 + row))
             reinterpret_cast<uint4*>(a.o_ws + (rec0 + row0 + row) * kD)[8 * c + (lane & 7)] = lds128(at(row, lane & 7));
         }
         __syncwarp();
@@ -405,8 +405,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
           const uint32_t row = 2 * i + (lane >> 4);
           if (row0 + row >= rows) continue;
           const uint32_t rr = sh.tile.row0 + row0 + row, tk = a.group.div(rr);
-          reinterpret_cast<uint4*>(a.out + (static_cast<uint64_t>(seq.first + tk) * a.hq + kvh * group + rr - tk * group) * kD)
-              [lane & 15] = lds128(at(row, lane & 15));
+          const uint64_t to = static_cast<uint64_t>(seq.first + tk) * a.hq + kvh * group + rr - tk * group;
+          if (out_in_bounds(a, to)) reinterpret_cast<uint4*>(a.out + to * kD)[lane & 15] = lds128(at(row, lane & 15));
         }
       }
     }
