@@ -329,7 +329,7 @@ def kv_append_rope_axes_nvfp4(cache, q, k, v, seq_idx, pos, rope_pos, axis_of_pa
            _append_axes(cache.packed(), None if pages is None else pages.packed(), qp, ld_q, hq, kp, ld_k, vp, ld_v,
                         _typed(seq_idx, _int32, "seq_idx", n), _typed(pos, _int32, "pos", n),
                         _typed(rope_pos, _int32, "rope_pos"), axes, axis_of_pair, n,
-                        _typed(rope_table, _float32, "rope_table"), len(rope_table),
+                        _typed(rope_table, _float32, "rope_table", len(rope_table) * 128), len(rope_table),
                         None if k_shift is None else _typed(k_shift, _float32, "k_shift", hk * 128),
                         None if q is None else _typed(q_out, _bf16, "q_out", n * hq * 128), _stream(stream)))
 
