@@ -93,7 +93,7 @@ __device__ __forceinline__ void mma_v_p(uint32_t d, uint32_t a, uint32_t b, uint
 
 // kCap: the scores may be capped.  (A kernel of its own: the cap's code in the kernel of calls
 // without one cost their softmax warps registers and instruction fetches: 32 x 6 drafted tokens
-// on 4001 keys 81.5 instead of 72.5 us.)
+// on 4001 keys 81.5 instead of 72.5 us when it was measured.)
 template <int kC, bool kE1M2, bool kCap, bool kFull>
 __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const ExtendArgs a) {
   using C = RowsConfig<kC>;
@@ -197,16 +197,12 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
     return ok;
   };
 
-  // 104, 64, 64 and 24 registers a thread, or 96, 64, 64 and 32: the 512 x 64 that the CTA
-  // starts with.  Which is better is the spills' doing (32 x 4001 keys, the first against
-  // the second: 24 rows 64 and 73 us, 32 rows 79 and 73).
-  constexpr bool kMore = kC < 32;
+  // 104, 64, 64 and 24 registers a thread by warpgroup: the 512 x 64 that the CTA starts with.
+  // (96, 64, 64 and 32, on 32 x 4001 keys: 16 rows 54 to 72 us instead of 56 to 72, 24 rows 62 and
+  // with a cap 85 instead of 65 and 73, 32 rows 75 and 102 instead of 68 and 90.)
   if (warp < 4) {
     // ------------------------------------------------------------- softmax ---
-    if (kMore)
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-    else
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
     // Q rows as f16, scaled by a power of two (exact) to below 1: 16 lanes a row.
     uint4 w[kN / 8];
 #pragma unroll
@@ -531,10 +527,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       rows_of(j + 2);
     }
   } else {
-    if (kMore)
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 24;");
-    else
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 24;");
     // ----------------------------------------------------------------- MMA ---
     if (warp == 12) {
       const bool leader = elect_one();
