@@ -120,6 +120,10 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
     tmem_alloc(&sh.tmem, kRowsTmem);
     tmem_relinquish();  // the SM's other CTA allocates too
   }
+  // The next kernel's CTAs, which may allocate as well, start once this one has its columns.
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
   griddep_wait_and_release();
   const uint32_t group = a.group.d;
   if (warp == 0) {
@@ -163,9 +167,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) extend_rows_kernel(const Exte
       sh.all_hi = all_hi;
     }
   }
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
   const uint32_t tmem = sh.tmem;
   const Tile tile = sh.item.tile;
   const uint32_t kvh = sh.item.kvh;

@@ -128,6 +128,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
     fence_mbar_init();
   }
   if (warp == kMmaWarp) tmem_alloc(&sh.tmem, 512);
+  // The next kernel's CTAs, which may allocate as well, start once this one has its columns.
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
   griddep_wait_and_release();
   // Item: split fastest, then KV head, then tile.
   const uint32_t split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
@@ -139,9 +143,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) extend_tile_kernel(const Exte
       if (t.b < a.map.batch) sh.seq = sequence(a, t.b);
     }
   }
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
   const uint32_t tmem = sh.tmem;
   const bool none = sh.tile.b >= a.map.batch;  // more CTAs than tiles
   const Seq seq = sh.seq;
