@@ -82,7 +82,7 @@ constexpr int64_t kFullContext = 512;
 
 // Which kernel, the tiles (at most), and the parts that each tile's keys are cut into.
 // By a sequence's rows per KV head: up to 8 the decode kernel (64 ragged sequences of up
-// to 16384 keys 144 us; by 8-row tensor-core tiles 187), up to 32 the rows kernel (32 x 4
+// to 16384 keys 143 us; by 8-row tensor-core tiles 187), up to 32 the rows kernel (32 x 4
 // drafted tokens on 4001 keys 77 us; by mma.sync 148, by 256-row tiles 159), else tiles.
 Plan plan_for(int64_t batch, int64_t n_tokens, int64_t group, int64_t hkv, int64_t context, bool uniform) {
   Plan p;

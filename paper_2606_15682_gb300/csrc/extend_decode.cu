@@ -3,13 +3,14 @@
 // A CTA takes 8 rows and a range of keys.  Warp 0 streams the keys' codes and scales
 // into a two-stage ring of 128 keys; four warps take two 16-key tiles of a stage
 // each, dequantize in registers (exact in f16) and multiply with mma.sync m16n8k16:
-// S^T[16 keys, 8 rows] = K Q^T, O^T[128, 8 rows] += V^T P^T.  Four CTAs an SM.  The
-// tensor pipe gives this form some 32 cycles an MMA: 16 of them per 16 keys are
-// 1024 cycles per 128 keys and SM where HBM takes 790.  64 ragged sequences of up to
-// 16384 keys, 40 on 8 heads: 144 us, 3.5 TB/s, 0.52 of the measured copy rate; 38 x 8192
-// keys, parts that fill the GPU once, 96 us, 0.55 (99 with cap and bias in one kernel).  (extend_rows_kernel, whose
-// shared-memory traffic does not shrink with the rows, takes 187 us there, and this
-// one loses at 16 rows: it has twice the MMAs then.)
+// S^T[16 keys, 8 rows] = K Q^T, O^T[128, 8 rows] += V^T P^T.  Four CTAs an SM.  What
+// bounds it is latency: DRAM is at 50 %, the issue slots at 56 %, the tensor pipe at 19 %
+// (38 x 8192 keys); warps wait for their stage and for one another's results in
+// dequantization.  64 ragged sequences of up to 16384 keys, 40 on 8 heads: 143 us,
+// 3.5 TB/s, 0.52 of the measured copy rate; 38 x 8192 keys 95 us, 0.56, 100 with a bias, 103
+// with a cap.  (extend_rows_kernel, whose shared-memory traffic does not shrink with the
+// rows, took 187 us where this one took 149, and this one loses at 16 rows: it has twice
+// the MMAs then.)
 //
 // Lane roles (g = lane / 4, t = lane % 4), as the fragments have them:
 //   K rows g and g + 8 of the tile, channels 32t..32t+31; V rows 2t, 2t+1, 2t+8,

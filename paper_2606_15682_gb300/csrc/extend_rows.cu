@@ -10,12 +10,11 @@
 //   warps 8-11  V
 //   warp 12     issues the MMAs; 13-15 complete its warpgroup
 // Two CTAs share an SM.  32 x 4 drafted tokens on 4001 keys, 40 on 8 heads (24 rows),
-// take 64 us in E2M1 and 74 in E1M2, 0.34 and 0.30 of the measured copy rate; HBM alone
-// would take 22.  What bounds it is the softmax warps' turn per block, at one key a
-// thread: it goes by its instructions, which the four roles' code, too long for the
-// instruction caches near the schedulers, makes expensive; 8 rows more cost 5 us, no
-// row at all 50.  (By mma.sync in registers the tensor pipe's rate for that form is the
-// bound: 148 us.)
+// take 65 us in E2M1 and 74 in E1M2, 0.34 and 0.30 of the measured copy rate; HBM alone
+// would take 22.  16 rows take 56, 32 rows 68.  What bounds it is the softmax warps' turn
+// per block, at one key a thread: it goes by its instructions, which the four roles' code,
+// too long for the instruction caches near the schedulers, makes expensive (issue slots 57 %
+// used, "no instruction" 1.1 stalls an issue).  (By mma.sync in registers it took 148 us.)
 #include "extend_attention.cuh"
 
 namespace nvfp4 {

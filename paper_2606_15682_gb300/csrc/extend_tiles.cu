@@ -18,9 +18,9 @@
 // With at most 128 rows the second tile takes the same rows with every second
 // block, and the two are joined at the end.
 //
-// A prompt of 4096 (40 on 8 heads, causal) takes 181 us, 0.49 of the measured bf16
-// rate; a chunk of 2048 on 16384 keys (64 on 8 heads) 921 us, 0.58, 1113 with a bias,
-// 1433 with a cap.  A step of 64 keys and both tiles takes some 1790 cycles where the
+// A prompt of 4096 (40 on 8 heads, causal) takes 182 us, 0.49 of the measured bf16
+// rate; a chunk of 2048 on 16384 keys (64 on 8 heads) 926 us, 0.58, 1103 with a bias,
+// 1422 with a cap, 1722 with both.  A step of 64 keys and both tiles takes some 1790 cycles where the
 // MMAs need 1250 (48 for 128 x 64 x 16 with Q from shared memory, 64 for 128 x 128 x 16):
 // the rest is the ring softmax, PV, QK^T, softmax, each link short of issue slots
 // beside the dequantizing warps.  (Issuers per half, one thread as issuer, or the two
