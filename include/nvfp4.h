@@ -666,6 +666,202 @@ nvfp4_status residual_norm_nvfp4(const void* x_bf16, int64_t ld_x, const void* y
                                  float alpha, const void* w_norm, float eps, void* r_out, void* h_out,
                                  const float* g_out, uint8_t* codes, uint8_t* scales, void* stream);
 
+/*
+ * A mixture-of-experts layer: each token goes through top_k of num_experts
+ * feed-forward networks, whose outputs are weighted and summed.  A layer's step,
+ * every line one call:
+ *   moe_route                             the tokens' experts and weights from the router's logits
+ *   moe_sort                              the plan: the tokens' rows, sorted by expert
+ *   moe_dispatch_nvfp4                    x quantized into its experts' rows
+ *   nvfp4_linear_grouped_swiglu_quantize  gate_up of each expert, SwiGLU, down's NVFP4 input
+ *   nvfp4_linear_grouped                  down of each expert
+ *   moe_combine                           the rows back to their tokens, weighted and summed
+ * (the mxfp4_ forms likewise; moe_dispatch for experts in bf16).  Gradients:
+ * moe_combine_backward; moe_combine without weights (of moe_dispatch);
+ * moe_route_backward.  A gradient through experts in bf16 needs nothing else.
+ *
+ * The plan.  A token's choice j of an expert is a row of buffers of
+ * moe_max_rows(n_tokens, top_k, num_experts) rows.  Expert e has the rows
+ * row_start[e] .. row_start[e] + rows[e] - 1, in the order of its (token, choice)
+ * pairs; row_start[e] is a multiple of 128, the tensor core's scale tile, so that
+ * up to 127 rows lie unused behind an expert's last one: no call writes them, and
+ * whatever they hold enters no result.
+ *   row_start : device int32 [num_experts + 1], the last one the rows in all.
+ *   rows      : device int32 [num_experts].
+ *   row_of    : device int32 [n_tokens, top_k], or -1: a choice without an expert.
+ * Written by moe_sort, read by the other calls; the struct is read before a call
+ * returns.  1 <= num_experts <= 1024, 1 <= top_k <= 32, moe_max_rows < 2^31
+ * (SHAPE); null arrays (row_of may be null with n_tokens == 0) -> INVALID_ARG;
+ * 4-B aligned (ALIGN).  A plan that names rows outside the buffers is cut to them.
+ */
+typedef struct {
+  int32_t* row_start;
+  int32_t* rows;
+  int32_t* row_of;
+  int64_t n_tokens;
+  int32_t top_k;
+  int32_t num_experts;
+} moe_plan;
+
+/* Rows of the sorted buffers: n = n_tokens * top_k choices and 127 for each of
+ * min(num_experts, n) experts, down to a multiple of 128.  0 for invalid sizes. */
+int64_t moe_max_rows(int64_t n_tokens, int32_t top_k, int32_t num_experts);
+
+typedef enum { NVFP4_F32 = 0, NVFP4_BF16 = 1 } nvfp4_float_type;
+typedef enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 } moe_score;
+
+typedef struct {
+  int32_t score;       /* moe_score: p = softmax(l) over the experts, or 1 / (1 + e^-l) */
+  int32_t renormalize; /* 1: weights divided by their sum (0 where that is 0); 0: not   */
+  float scale;         /* factor of the weights, finite                                 */
+  const float* bias;   /* device float [num_experts] or NULL; with MOE_SCORE_SIGMOID
+                          only: the choice is by p + bias, the weights are by p         */
+} moe_route_options;
+
+/*
+ * The router: the top_k experts of each token and their weights.
+ *   logits     : [n_tokens, num_experts] fp32 or bf16 (logits_type), rows ld apart.
+ *   expert_idx : device int32 [n_tokens, top_k], by falling logit (with a bias: by
+ *                falling p + bias), the lowest index among equal ones.
+ *   weights    : device float [n_tokens, top_k]: scale * p, divided by the sum of the
+ *                chosen p with renormalize.
+ * All in fp32.  Under a bias, p = 1 / (1 + e^-l) with CUDA's expf and one rounding
+ * for each operation.  An expert whose logit (or p + bias) is -inf or NaN is not
+ * chosen and has p = 0; a token without top_k others gets -1 and weight 0 in the
+ * places left (a padded batch: rows of -inf).  Logits of +inf share the softmax.
+ * top_k <= num_experts, ld >= num_experts (SHAPE); enums, scale, bias with softmax
+ * (INVALID_ARG); pointers aligned to their type (ALIGN).  n_tokens == 0 is a no-op.
+ */
+nvfp4_status moe_route(const void* logits, int32_t logits_type, int64_t ld, int64_t n_tokens, int32_t num_experts,
+                       int32_t top_k, const moe_route_options* options, int32_t* expert_idx, float* weights,
+                       void* stream);
+
+/*
+ * The gradient of moe_route's weights with respect to the logits, the choice
+ * taken as given: d_logits [n_tokens, num_experts] dense, of the logits' type.
+ *   d_weights  : device float [n_tokens, top_k].
+ *   expert_idx : as moe_route wrote it, or a caller's own: -1 or a number that is no
+ *                expert has no part; an expert that is named twice gets both parts.
+ * Options as in the forward call; the bias is not read (it moves no weight).
+ */
+nvfp4_status moe_route_backward(const void* logits, int32_t logits_type, int64_t ld, int64_t n_tokens,
+                                int32_t num_experts, int32_t top_k, const moe_route_options* options,
+                                const int32_t* expert_idx, const float* d_weights, void* d_logits, void* stream);
+
+/*
+ * Writes the plan of expert_idx (device int32 [n_tokens, top_k]).  A negative
+ * entry is a choice without an expert; one >= num_experts is taken so too and
+ * sets INVALID_ARG on the device.  A token may name an expert twice: two rows.
+ * With n_tokens == 0 all rows and row_start become 0.  The same bits every time.
+ *   workspace : moe_sort_workspace_size(...) bytes, 16-B aligned (NULL if that is
+ *               0, as for few tokens); contents on entry are ignored.
+ */
+size_t moe_sort_workspace_size(int64_t n_tokens, int32_t top_k, int32_t num_experts);
+nvfp4_status moe_sort(const moe_plan* plan, const int32_t* expert_idx, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/*
+ * Tokens to their rows: rows[row_of[t, j]] = x[t], times weights[t, j] in fp32 and
+ * rounded once where weights (device float [n_tokens, top_k]) are given.
+ *   x_bf16    : [n_tokens, cols] bf16, rows ld_x apart.
+ *   rows_bf16 : [moe_max_rows, cols] bf16, dense.
+ * cols % 8 == 0, cols <= 65536, ld_x >= cols (SHAPE), ld_x % 8 == 0, 16-B aligned
+ * (ALIGN).  n_tokens == 0 is a no-op, here and in all calls below.  No output may
+ * overlap an input, here and in all calls below, but where one says so.
+ */
+nvfp4_status moe_dispatch(const moe_plan* plan, const void* x_bf16, int64_t ld_x, int64_t cols, const float* weights,
+                          void* rows_bf16, void* stream);
+
+/*
+ * Tokens to their rows as NVFP4 by the recipe of nvfp4_quantize with the static
+ * scale g_dev (device float): a row's codes and scales are those of its token.
+ *   codes  : [moe_max_rows, cols/2] bytes.
+ *   scales : nvfp4_scales_bytes(moe_max_rows, cols, NVFP4_SCALES_MMA) bytes, 4-B
+ *            aligned.  Unlike nvfp4_quantize's, padding rows are not written.
+ * cols % 64 == 0.  g_dev <= 0 or not finite: zeros, INVALID_ARG on the device.
+ */
+nvfp4_status moe_dispatch_nvfp4(const moe_plan* plan, const void* x_bf16, int64_t ld_x, int64_t cols,
+                                const float* g_dev, uint8_t* codes, uint8_t* scales, void* stream);
+
+/* The same as MXFP4 by the recipe of mxfp4_quantize (rotate as there); scales:
+ * mxfp4_scales_bytes(moe_max_rows, cols, NVFP4_SCALES_MMA) bytes. */
+nvfp4_status moe_dispatch_mxfp4(const moe_plan* plan, const void* x_bf16, int64_t ld_x, int64_t cols, int rotate,
+                                uint8_t* codes, uint8_t* scales, void* stream);
+
+/*
+ * Rows back to their tokens: out[t] = base[t] + sum_j weights[t, j] * y[row_of[t, j]],
+ * in fp32 in the order of j, rounded once; choices without an expert add nothing.
+ * Without weights all are 1: with y the gradient of moe_dispatch's rows, out is the
+ * gradient of its x.
+ *   y_bf16    : [moe_max_rows, cols] bf16, dense.
+ *   base_bf16 : [n_tokens, cols] bf16, rows ld_base apart, or NULL (nothing): the
+ *               residual stream or a shared expert's output; may be out_bf16 where
+ *               ld_base == ld_out.
+ *   out_bf16  : [n_tokens, cols] bf16, rows ld_out apart.
+ * Sizes and alignment as moe_dispatch.
+ */
+nvfp4_status moe_combine(const moe_plan* plan, const void* y_bf16, int64_t cols, const float* weights,
+                         const void* base_bf16, int64_t ld_base, void* out_bf16, int64_t ld_out, void* stream);
+
+/*
+ * moe_combine's gradients, from d_out (bf16 [n_tokens, cols], rows ld_d_out apart):
+ *   d_y_bf16[row_of[t, j]] = bf16(weights[t, j] * d_out[t])   [moe_max_rows, cols], or NULL
+ *   d_weights[t, j] = sum_c d_out[t, c] * y[row_of[t, j], c]  fp32 [n_tokens, top_k], or NULL
+ * (that of base is d_out).  d_weights is 0 for a choice without an expert.  Both in
+ * fp32, the sum in a fixed order.
+ */
+nvfp4_status moe_combine_backward(const moe_plan* plan, const void* d_out_bf16, int64_t ld_d_out, const void* y_bf16,
+                                  int64_t cols, const float* weights, void* d_y_bf16, float* d_weights, void* stream);
+
+/*
+ * The experts' linears: for every row r of expert e
+ *   out[r, n] = bf16_rne( (g_a g_w) * sum_k a[r, k] * w_e[n, k] ),
+ * as nvfp4_linear of each expert's rows with its weight; the sum in fp32.
+ *   a_codes, a_scales : the sorted rows, [moe_max_rows, K] with MMA-layout scales.
+ *   g_a      : device float [1] (g_a_step 0) or [num_experts] (g_a_step 1).
+ *   w_codes  : [num_experts, N, K/2] bytes; w_scales: for each expert the MMA layout
+ *              of [N, K], nvfp4_scales_bytes(N, K, NVFP4_SCALES_MMA) bytes, one after
+ *              the other; g_w: device float [num_experts].
+ *   out_bf16 : [moe_max_rows, N] bf16, rows ldo apart.
+ * Experts without rows cost nothing.  K % 256 == 0, N % 16 == 0, both positive and at
+ * most 2^20, ldo >= N, ldo % 8 == 0, num_experts * ceil(N / 128) * (K / 32) < 2^31 and
+ * num_experts * N < 2^31 (SHAPE); g_a_step 0 or 1 (INVALID_ARG); 16-B aligned, g's 4-B
+ * (ALIGN).  A bounded on-device wait that expires sets TIMEOUT; out is then undefined.
+ */
+nvfp4_status nvfp4_linear_grouped(const moe_plan* plan, const uint8_t* a_codes, const uint8_t* a_scales,
+                                  const float* g_a, int32_t g_a_step, const uint8_t* w_codes, const uint8_t* w_scales,
+                                  const float* g_w, int64_t N, int64_t K, void* out_bf16, int64_t ldo, void* stream);
+
+/* The same with MXFP4 operands: UE8M0 scales, no tensor scales. */
+nvfp4_status mxfp4_linear_grouped(const moe_plan* plan, const uint8_t* a_codes, const uint8_t* a_scales,
+                                  const uint8_t* w_codes, const uint8_t* w_scales, int64_t N, int64_t K,
+                                  void* out_bf16, int64_t ldo, void* stream);
+
+/*
+ * The experts' gate_up with the down projection's input in the epilogue, as
+ * nvfp4_linear_swiglu_quantize: h = SiLU(G) * U of the fp32 products, NVFP4-quantized
+ * with the static scale of the expert.  SiLU(x) = x / (1 + e^-x) with CUDA's fast
+ * exponential and division (some 2^-19 relative).
+ *   w_codes, w_scales : [num_experts, 2I, K], gate and up rows in turn, 16 of each
+ *                (nvfp4_interleave_gate_up of each expert's, then nvfp4_quantize).
+ *   g_out      : device float [1] (g_out_step 0) or [num_experts] (1); <= 0 or not
+ *                finite for an expert with rows: zeros in them, INVALID_ARG on the device.
+ *   out_codes  : [moe_max_rows, I/2] bytes, 16-B aligned; out_scales:
+ *                nvfp4_scales_bytes(moe_max_rows, I, NVFP4_SCALES_MMA) bytes, 4-B aligned.
+ * I % 128 == 0; otherwise as nvfp4_linear_grouped with N = 2I.
+ */
+nvfp4_status nvfp4_linear_grouped_swiglu_quantize(const moe_plan* plan, const uint8_t* a_codes,
+                                                  const uint8_t* a_scales, const float* g_a, int32_t g_a_step,
+                                                  const uint8_t* w_codes, const uint8_t* w_scales, const float* g_w,
+                                                  int64_t I, int64_t K, const float* g_out, int32_t g_out_step,
+                                                  uint8_t* out_codes, uint8_t* out_scales, void* stream);
+
+/* The same with MXFP4 operands and output (rotate as in mxfp4_linear_swiglu_quantize). */
+nvfp4_status mxfp4_linear_grouped_swiglu_quantize(const moe_plan* plan, const uint8_t* a_codes,
+                                                  const uint8_t* a_scales, const uint8_t* w_codes,
+                                                  const uint8_t* w_scales, int64_t I, int64_t K, int rotate,
+                                                  uint8_t* out_codes, uint8_t* out_scales, void* stream);
+
 /* Synchronize `stream`, copy the device status word of the current device to
  * *status_host (an nvfp4_status value) and clear it. */
 nvfp4_status nvfp4_get_device_status(int32_t* status_host, void* stream);

@@ -33,8 +33,10 @@ LIB = os.path.join(BUILD, "libnvfp4.so")
 BUILD_DEBUG = os.path.join(PKG, "_build_debug")
 BUILD_TIMELINE = os.path.join(PKG, "_build_timeline")
 SOURCES = ["api.cu", "quantize.cu", "kv_append.cu", "attention.cu", "gemm.cu", "qfit.cu", "kv_paged.cu",
-           "extend_attention.cu", "extend_tiles.cu", "extend_rows.cu", "extend_decode.cu", "residual_norm.cu"]
-HEADERS = ["common.cuh", "nvfp4_quant.cuh", "kv_pages.cuh", "extend_attention.cuh", os.path.join("..", "..", "include", "nvfp4.h")]
+           "extend_attention.cu", "extend_tiles.cu", "extend_rows.cu", "extend_decode.cu", "residual_norm.cu",
+           "moe_route.cu", "moe_rows.cu", "gemm_grouped.cu"]
+HEADERS = ["common.cuh", "nvfp4_quant.cuh", "kv_pages.cuh", "extend_attention.cuh", "moe_plan.cuh",
+           os.path.join("..", "..", "include", "nvfp4.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-fvisibility=hidden", "-Xptxas", "-v"]
 

@@ -1,0 +1,510 @@
+// Tokens to their experts' rows and back, with the gradients of both.
+//   moe_sort              the rows: pairs (token, choice) counted and placed by expert
+//   moe_dispatch          rows[row_of[t, j]] = [w[t, j]] x[t], bf16; or quantized to NVFP4 / MXFP4
+//   moe_combine           out[t] = [base[t]] + sum_j [w[t, j]] y[row_of[t, j]]
+//   moe_combine_backward  dy[row_of[t, j]] = w[t, j] g[t],  dw[t, j] = <g[t], y[row_of[t, j]]>
+// All walk tokens, not rows: a token is read once however many experts it has,
+// its sums are in the order of its choices, and no row needs an atomic.
+#include <cfloat>
+
+#include "moe_plan.cuh"
+#include "nvfp4_quant.cuh"
+
+namespace nvfp4 {
+namespace {
+
+// ------------------------------------------------------------------ sort ---
+// A CTA of 32 warps places a chunk of pairs: each warp counts its segment's
+// experts in a histogram of its own (lanes with the same expert find each other
+// by match_any), the histograms are summed along the warps, and a second walk
+// gives each pair its rank.  The order is that of the pairs: no atomics.
+// Several chunks: the counts of all of them come from a kernel before it.
+
+constexpr int kSortWarps = 32;
+constexpr int kSortThreads = 32 * kSortWarps;
+constexpr int64_t kSortChunk = 4096;   // pairs of a CTA
+constexpr int64_t kSortMaxChunks = 256;
+
+struct SortShape {
+  int64_t chunk;  // pairs of a CTA, a multiple of kSortThreads
+  int64_t chunks;
+};
+SortShape sort_shape(int64_t pairs) {
+  SortShape s;
+  s.chunk = kSortChunk;
+  if (pairs > s.chunk * kSortMaxChunks)
+    s.chunk = ((pairs + kSortMaxChunks - 1) / kSortMaxChunks + kSortThreads - 1) / kSortThreads * kSortThreads;
+  s.chunks = pairs ? (pairs + s.chunk - 1) / s.chunk : 1;
+  return s;
+}
+
+struct SortArgs {
+  const int32_t* idx;
+  int32_t* row_start;
+  int32_t* rows;
+  int32_t* row_of;
+  uint32_t* counts;  // [chunks, experts], with more than one chunk
+  int64_t pairs, chunk;
+  int experts;
+  int* status;
+};
+
+// The expert of a pair, or -1: none, or not one of the experts (reported).
+__device__ __forceinline__ int expert_of(const SortArgs& a, int64_t i, int64_t end) {
+  int e = i < end ? __ldg(a.idx + i) : -1;
+  if (e >= a.experts) {
+    set_status(a.status, NVFP4_ERR_INVALID_ARG);
+    e = -1;
+  }
+  return max(e, -1);
+}
+
+__global__ void __launch_bounds__(kSortThreads) moe_count_kernel(const SortArgs a) {
+  __shared__ uint32_t hist[kMoeMaxExperts];
+  griddep_wait_and_release();
+  for (int e = threadIdx.x; e < a.experts; e += kSortThreads) hist[e] = 0;
+  __syncthreads();
+  const int64_t begin = blockIdx.x * a.chunk, end = min(begin + a.chunk, a.pairs);
+  for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads) {
+    const int e = expert_of(a, i, end);
+    if (e >= 0) atomicAdd(&hist[e], 1u);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.experts; e += kSortThreads)
+    a.counts[blockIdx.x * static_cast<uint64_t>(a.experts) + e] = hist[e];
+}
+
+__global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortArgs a) {
+  extern __shared__ uint32_t sort_smem[];  // [warps, experts] counts, then places; [experts] first rows
+  __shared__ uint32_t warp_sum[kSortWarps];
+  griddep_wait_and_release();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = a.experts;
+  uint32_t* hist = sort_smem + warp * E;
+  uint32_t* base = sort_smem + kSortWarps * E;
+  for (int i = threadIdx.x; i < kSortWarps * E; i += kSortThreads) sort_smem[i] = 0;
+  __syncthreads();
+  const int64_t chunk_end = min((blockIdx.x + 1) * a.chunk, a.pairs);
+  const int64_t begin = blockIdx.x * a.chunk + warp * (a.chunk / kSortWarps);
+  const int64_t end = min(begin + a.chunk / kSortWarps, chunk_end);
+  for (int64_t i = begin; i < end; i += 32) {
+    const int e = expert_of(a, i + lane, end);
+    const uint32_t peers = __match_any_sync(0xffffffffu, e);
+    if (e >= 0 && (peers & ((1u << lane) - 1)) == 0) hist[e] += __popc(peers);
+    __syncwarp();
+  }
+  __syncthreads();
+  // Thread e: expert e's rows in this chunk before each warp, before the chunk, and in all.
+  const int e = threadIdx.x;
+  uint32_t total = 0, before = 0;
+  if (e < E) {
+    uint32_t run = 0;
+    for (int w = 0; w < kSortWarps; ++w) {
+      const uint32_t n = sort_smem[w * E + e];
+      sort_smem[w * E + e] = run;
+      run += n;
+    }
+    if (gridDim.x == 1) {
+      total = run;
+    } else {
+#pragma unroll 8
+      for (uint32_t c = 0; c < gridDim.x; ++c) {
+        const uint32_t n = __ldcg(a.counts + c * static_cast<uint64_t>(E) + e);
+        total += n;
+        before += c < blockIdx.x ? n : 0u;
+      }
+    }
+  }
+  const uint32_t padded = (total + kMoeRowTile - 1) / kMoeRowTile * kMoeRowTile;
+  uint32_t sum = padded;  // inclusive over the experts
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) {
+    const uint32_t v = __shfl_up_sync(0xffffffffu, sum, s);
+    if (lane >= s) sum += v;
+  }
+  if (lane == 31) warp_sum[warp] = sum;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) sum += warp_sum[w];
+  if (e < E) {
+    base[e] = sum - padded + before;
+    if (blockIdx.x == 0) {
+      a.rows[e] = static_cast<int32_t>(total);
+      a.row_start[e] = static_cast<int32_t>(sum - padded);
+      if (e == E - 1) a.row_start[E] = static_cast<int32_t>(sum);
+    }
+  }
+  __syncthreads();
+  for (int64_t i = begin; i < end; i += 32) {
+    const int x = expert_of(a, i + lane, end);
+    const uint32_t peers = __match_any_sync(0xffffffffu, x), lower = peers & ((1u << lane) - 1);
+    const uint32_t at = x >= 0 ? hist[x] : 0u;
+    __syncwarp();
+    if (x >= 0 && lower == 0) hist[x] = at + __popc(peers);
+    if (i + lane < end) a.row_of[i + lane] = x >= 0 ? static_cast<int32_t>(base[x] + at + __popc(lower)) : -1;
+    __syncwarp();
+  }
+}
+
+// ------------------------------------------------------- walks over tokens ---
+// `vecs` units of a token's channels; a CTA takes several tokens where they are
+// short.  Loops are uniform in a warp.
+
+constexpr int kWalkThreads = 256;
+
+struct Walk {
+  int64_t tokens;
+  uint32_t vecs, per_cta;  // per_cta: tokens of a CTA's step
+};
+Walk make_walk(int64_t tokens, uint32_t vecs) {
+  return {tokens, vecs, vecs < kWalkThreads ? kWalkThreads / vecs : 1u};
+}
+uint32_t walk_grid(const Walk& w) {
+  const int64_t steps = (w.tokens + w.per_cta - 1) / w.per_cta, cap = static_cast<int64_t>(sm_count()) * 8;
+  return static_cast<uint32_t>(steps < cap ? steps : cap);
+}
+// f(token, unit, live) for all of this thread's units.
+template <class F>
+__device__ __forceinline__ void walk(const Walk& w, F&& f) {
+  const uint32_t sub = w.vecs < kWalkThreads ? threadIdx.x / w.vecs : 0u;
+  const uint32_t v0 = threadIdx.x - sub * w.vecs;
+  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * w.per_cta; t0 < w.tokens;
+       t0 += static_cast<int64_t>(gridDim.x) * w.per_cta)
+    for (uint32_t v = 0; v < w.vecs; v += kWalkThreads)
+      f(t0 + sub, v + v0, sub < w.per_cta && t0 + sub < w.tokens && v + v0 < w.vecs);
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ uint4 pack8(const float v[8]) {
+  return make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+}
+
+struct RowArgs {
+  const int32_t* row_of;
+  int top_k;
+  int64_t max_rows;
+  int* status;
+};
+// The row of choice j of token t, or -1.  A plan that names rows outside the buffers has none there.
+__device__ __forceinline__ int64_t row_of(const RowArgs& a, int64_t t, int j) {
+  const int64_t r = __ldg(a.row_of + t * a.top_k + j);
+  return r < a.max_rows ? r : -1;
+}
+
+__global__ void __launch_bounds__(kWalkThreads)
+    moe_dispatch_kernel(const RowArgs a, const Walk w, const uint16_t* __restrict__ x, int64_t ld,
+                        const float* __restrict__ weights, uint16_t* __restrict__ out) {
+  griddep_wait_and_release();
+  walk(w, [&](int64_t t, uint32_t v, bool live) {
+    if (!live) return;
+    const uint4 in = __ldg(reinterpret_cast<const uint4*>(x + t * ld) + v);
+    for (int j = 0; j < a.top_k; ++j) {
+      const int64_t r = row_of(a, t, j);
+      if (r < 0) continue;
+      uint4 d = in;
+      if (weights) {
+        const float c = __ldg(weights + t * a.top_k + j);
+        float f[8];
+        unpack_bf16x8(in, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= c;
+        d = pack8(f);
+      }
+      reinterpret_cast<uint4*>(out)[r * w.vecs + v] = d;
+    }
+  });
+}
+
+// A thread has 16 channels, one NVFP4 block; four lanes have a scale word.
+__global__ void __launch_bounds__(kWalkThreads)
+    moe_dispatch_nvfp4_kernel(const RowArgs a, const Walk w, const uint16_t* __restrict__ x, int64_t ld,
+                              const float* __restrict__ g_dev, uint2* __restrict__ codes, uint8_t* __restrict__ scales) {
+  griddep_wait_and_release();
+  const float g_in = __ldg(g_dev);
+  const bool g_ok = g_in > 0.0f && g_in <= FLT_MAX;
+  if (!g_ok && blockIdx.x == 0 && threadIdx.x == 0) set_status(a.status, NVFP4_ERR_INVALID_ARG);
+  const float g = g_ok ? g_in : 1.0f, six_g = __fmul_rn(6.0f, g);
+  walk(w, [&](int64_t t, uint32_t v, bool live) {
+    const uint4* src = reinterpret_cast<const uint4*>(x + t * ld) + 2 * v;
+    const uint4 lo = live ? __ldg(src) : make_uint4(0, 0, 0, 0), hi = live ? __ldg(src + 1) : make_uint4(0, 0, 0, 0);
+    float f[16];
+    unpack_bf16x8(lo, f);
+    unpack_bf16x8(hi, f + 8);
+    const BlockScale b =
+        block_scale(__uint_as_float(max(amax_bits_bf16x8(lo), amax_bits_bf16x8(hi)) << 16), g, six_g);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f[i] = __fmul_rn(f[i], b.mult);
+    const uint2 c = g_ok ? make_uint2(e2m1x8(f), e2m1x8(f + 8)) : make_uint2(0, 0);
+    uint32_t word = (g_ok ? b.code : 0u) << (8 * (v & 3));
+    word |= __shfl_xor_sync(0xffffffffu, word, 1);
+    word |= __shfl_xor_sync(0xffffffffu, word, 2);
+    if (!live) return;
+    for (int j = 0; j < a.top_k; ++j) {
+      const int64_t r = row_of(a, t, j);
+      if (r < 0) continue;
+      codes[r * w.vecs + v] = c;
+      if ((v & 3) == 0) {
+        const uint64_t off = mma_scale_offset(static_cast<uint64_t>(r), v, w.vecs >> 2);
+        if (in_bounds(a.status, off + 4 <= static_cast<uint64_t>(a.max_rows) * w.vecs))
+          *reinterpret_cast<uint32_t*>(scales + off) = word;
+      }
+    }
+  });
+}
+
+// A thread has 32 channels, one MXFP4 block, whose scale is stored for both of its halves.
+template <bool kRotate>
+__global__ void __launch_bounds__(kWalkThreads)
+    moe_dispatch_mxfp4_kernel(const RowArgs a, const Walk w, const uint16_t* __restrict__ x, int64_t ld,
+                              uint4* __restrict__ codes, uint8_t* __restrict__ scales) {
+  griddep_wait_and_release();
+  walk(w, [&](int64_t t, uint32_t v, bool live) {
+    const uint4* src = reinterpret_cast<const uint4*>(x + t * ld) + 4 * v;
+    float f[32];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) unpack_bf16x8(live ? __ldg(src + q) : make_uint4(0, 0, 0, 0), f + 8 * q);
+    if (kRotate) hadamard32(f);
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(f[i]));
+    const uint32_t code = mx_scale_code(amax);
+    const float inv = mx_inv_scale(code);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) f[i] = __fmul_rn(f[i], inv);
+    const uint4 c = make_uint4(e2m1x8(f), e2m1x8(f + 8), e2m1x8(f + 16), e2m1x8(f + 24));
+    uint32_t word = (code | (code << 8)) << (16 * (v & 1));
+    word |= __shfl_xor_sync(0xffffffffu, word, 1);
+    if (!live) return;
+    for (int j = 0; j < a.top_k; ++j) {
+      const int64_t r = row_of(a, t, j);
+      if (r < 0) continue;
+      codes[r * w.vecs + v] = c;
+      if ((v & 1) == 0) {
+        const uint64_t off = mma_scale_offset(static_cast<uint64_t>(r), 2 * v, w.vecs >> 1);
+        if (in_bounds(a.status, off + 4 <= static_cast<uint64_t>(a.max_rows) * 2 * w.vecs))
+          *reinterpret_cast<uint32_t*>(scales + off) = word;
+      }
+    }
+  });
+}
+
+// The sum is in 32 bits, in the order of the choices, rounded once.
+__global__ void __launch_bounds__(kWalkThreads)
+    moe_combine_kernel(const RowArgs a, const Walk w, const uint16_t* __restrict__ y, const float* __restrict__ weights,
+                       const uint16_t* base, int64_t ld_base, uint16_t* out, int64_t ld_out) {
+  griddep_wait_and_release();
+  walk(w, [&](int64_t t, uint32_t v, bool live) {
+    if (!live) return;
+    float acc[8] = {};
+    if (base) unpack_bf16x8(reinterpret_cast<const uint4*>(base + t * ld_base)[v], acc);  // not __ldg: out may be base
+    for (int j = 0; j < a.top_k; ++j) {
+      const int64_t r = row_of(a, t, j);
+      if (r < 0) continue;
+      const float c = weights ? __ldg(weights + t * a.top_k + j) : 1.0f;
+      float f[8];
+      unpack_bf16x8(__ldg(reinterpret_cast<const uint4*>(y) + r * w.vecs + v), f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] = fmaf(c, f[i], acc[i]);
+    }
+    reinterpret_cast<uint4*>(out + t * ld_out)[v] = pack8(acc);
+  });
+}
+
+// A warp has a token.
+__global__ void __launch_bounds__(kWalkThreads)
+    moe_combine_backward_kernel(const RowArgs a, int64_t tokens, uint32_t vecs, const uint16_t* __restrict__ d_out,
+                                int64_t ld, const uint16_t* __restrict__ y, const float* __restrict__ weights,
+                                uint16_t* __restrict__ d_y, float* __restrict__ d_weights) {
+  griddep_wait_and_release();
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * (kWalkThreads / 32) + (threadIdx.x >> 5);
+  const uint32_t lane = threadIdx.x & 31;
+  if (t >= tokens) return;
+  const uint4* g4 = reinterpret_cast<const uint4*>(d_out + t * ld);
+  for (int j = 0; j < a.top_k; ++j) {
+    const int64_t r = row_of(a, t, j);
+    float dot = 0.0f;
+    if (r >= 0) {
+      const float c = __ldg(weights + t * a.top_k + j);
+      for (uint32_t v = lane; v < vecs; v += 32) {
+        float g[8], f[8];
+        unpack_bf16x8(__ldg(g4 + v), g);
+        unpack_bf16x8(__ldg(reinterpret_cast<const uint4*>(y) + r * vecs + v), f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          dot = fmaf(g[i], f[i], dot);
+          g[i] *= c;
+        }
+        if (d_y) reinterpret_cast<uint4*>(d_y)[r * vecs + v] = pack8(g);
+      }
+    }
+#pragma unroll
+    for (int s = 16; s; s >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, s);
+    if (d_weights && lane == 0) d_weights[t * a.top_k + j] = dot;
+  }
+}
+
+RowArgs row_args(const moe_plan* p) {
+  RowArgs a;
+  a.row_of = p->row_of;
+  a.top_k = p->top_k;
+  a.max_rows = moe_rows_bound(p->n_tokens, p->top_k, p->num_experts);
+  a.status = status_word_dev();
+  return a;
+}
+
+// What every call over tokens checks: the plan, [tokens, cols] with rows ld apart, cols a multiple of `step`.
+nvfp4_status check_tokens(const moe_plan* p, int64_t cols, int64_t step, int64_t ld) {
+  const nvfp4_status st = check_moe_plan(p);
+  if (st != NVFP4_OK) return st;
+  if (cols < step || cols > 65536 || cols % step || ld < cols) return NVFP4_ERR_SHAPE;
+  return ld % 8 ? NVFP4_ERR_ALIGN : NVFP4_OK;
+}
+
+}  // namespace
+}  // namespace nvfp4
+
+using namespace nvfp4;
+
+NVFP4_API int64_t moe_max_rows(int64_t n_tokens, int32_t top_k, int32_t num_experts) {
+  return check_moe_sizes(n_tokens, top_k, num_experts) == NVFP4_OK ? moe_rows_bound(n_tokens, top_k, num_experts) : 0;
+}
+
+NVFP4_API size_t moe_sort_workspace_size(int64_t n_tokens, int32_t top_k, int32_t num_experts) {
+  if (check_moe_sizes(n_tokens, top_k, num_experts) != NVFP4_OK) return 0;
+  const SortShape s = sort_shape(n_tokens * top_k);
+  return s.chunks > 1 ? static_cast<size_t>(s.chunks) * num_experts * sizeof(uint32_t) : 0;
+}
+
+NVFP4_API nvfp4_status moe_sort(const moe_plan* plan, const int32_t* expert_idx, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  NVFP4_TRACE("moe_sort");
+  const nvfp4_status st = check_moe_plan(plan);
+  if (st != NVFP4_OK) return st;
+  const size_t need = moe_sort_workspace_size(plan->n_tokens, plan->top_k, plan->num_experts);
+  if ((!expert_idx && plan->n_tokens) || (need && !workspace)) return NVFP4_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return NVFP4_ERR_SHAPE;
+  if (!aligned(expert_idx, 4) || (need && !aligned(workspace, 16))) return NVFP4_ERR_ALIGN;
+  SortArgs a;
+  a.idx = expert_idx;
+  a.row_start = plan->row_start;
+  a.rows = plan->rows;
+  a.row_of = plan->row_of;
+  a.counts = static_cast<uint32_t*>(workspace);
+  a.pairs = plan->n_tokens * plan->top_k;
+  a.experts = plan->num_experts;
+  a.status = status_word_dev();
+  const SortShape s = sort_shape(a.pairs);
+  a.chunk = s.chunk;
+  const cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  const dim3 grid(static_cast<uint32_t>(s.chunks)), block(kSortThreads);
+  const size_t smem = static_cast<size_t>(kSortWarps + 1) * a.experts * sizeof(uint32_t);
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(moe_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               static_cast<int>(smem)) != cudaSuccess) {
+    cudaGetLastError();
+    return NVFP4_ERR_CUDA;
+  }
+  if (s.chunks > 1) {
+    if (launch_pdl(moe_count_kernel, grid, block, 0, cs, a) != cudaSuccess) return NVFP4_ERR_CUDA;
+    count_launches(1);
+  }
+  if (launch_pdl(moe_place_kernel, grid, block, smem, cs, a) != cudaSuccess) return NVFP4_ERR_CUDA;
+  count_launches(1);
+  return launch_status();
+}
+
+NVFP4_API nvfp4_status moe_dispatch(const moe_plan* plan, const void* x_bf16, int64_t ld_x, int64_t cols,
+                                    const float* weights, void* rows_bf16, void* stream) {
+  NVFP4_TRACE("moe_dispatch");
+  const nvfp4_status st = check_tokens(plan, cols, 8, ld_x);
+  if (st != NVFP4_OK) return st;
+  if (plan->n_tokens == 0) return NVFP4_OK;
+  if (!x_bf16 || !rows_bf16) return NVFP4_ERR_INVALID_ARG;
+  if (!aligned(x_bf16, 16) || !aligned(rows_bf16, 16) || !aligned(weights, 4)) return NVFP4_ERR_ALIGN;
+  const Walk w = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 8));
+  if (launch_pdl(moe_dispatch_kernel, dim3(walk_grid(w)), dim3(kWalkThreads), 0, static_cast<cudaStream_t>(stream),
+                 row_args(plan), w, static_cast<const uint16_t*>(x_bf16), ld_x, weights,
+                 static_cast<uint16_t*>(rows_bf16)) != cudaSuccess)
+    return NVFP4_ERR_CUDA;
+  count_launches(1);
+  return launch_status();
+}
+
+NVFP4_API nvfp4_status moe_dispatch_nvfp4(const moe_plan* plan, const void* x_bf16, int64_t ld_x, int64_t cols,
+                                          const float* g_dev, uint8_t* codes, uint8_t* scales, void* stream) {
+  NVFP4_TRACE("moe_dispatch_nvfp4");
+  const nvfp4_status st = check_tokens(plan, cols, 64, ld_x);
+  if (st != NVFP4_OK) return st;
+  if (plan->n_tokens == 0) return NVFP4_OK;
+  if (!x_bf16 || !g_dev || !codes || !scales) return NVFP4_ERR_INVALID_ARG;
+  if (!aligned(x_bf16, 16) || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(g_dev, 4)) return NVFP4_ERR_ALIGN;
+  const Walk w = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 16));
+  if (launch_pdl(moe_dispatch_nvfp4_kernel, dim3(walk_grid(w)), dim3(kWalkThreads), 0,
+                 static_cast<cudaStream_t>(stream), row_args(plan), w, static_cast<const uint16_t*>(x_bf16), ld_x,
+                 g_dev, reinterpret_cast<uint2*>(codes), scales) != cudaSuccess)
+    return NVFP4_ERR_CUDA;
+  count_launches(1);
+  return launch_status();
+}
+
+NVFP4_API nvfp4_status moe_dispatch_mxfp4(const moe_plan* plan, const void* x_bf16, int64_t ld_x, int64_t cols,
+                                          int rotate, uint8_t* codes, uint8_t* scales, void* stream) {
+  NVFP4_TRACE("moe_dispatch_mxfp4");
+  const nvfp4_status st = check_tokens(plan, cols, 64, ld_x);
+  if (st != NVFP4_OK) return st;
+  if (rotate != 0 && rotate != 1) return NVFP4_ERR_INVALID_ARG;
+  if (plan->n_tokens == 0) return NVFP4_OK;
+  if (!x_bf16 || !codes || !scales) return NVFP4_ERR_INVALID_ARG;
+  if (!aligned(x_bf16, 16) || !aligned(codes, 16) || !aligned(scales, 4)) return NVFP4_ERR_ALIGN;
+  const Walk w = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 32));
+  if (launch_pdl(rotate ? moe_dispatch_mxfp4_kernel<true> : moe_dispatch_mxfp4_kernel<false>, dim3(walk_grid(w)),
+                 dim3(kWalkThreads), 0, static_cast<cudaStream_t>(stream), row_args(plan), w,
+                 static_cast<const uint16_t*>(x_bf16), ld_x, reinterpret_cast<uint4*>(codes), scales) != cudaSuccess)
+    return NVFP4_ERR_CUDA;
+  count_launches(1);
+  return launch_status();
+}
+
+NVFP4_API nvfp4_status moe_combine(const moe_plan* plan, const void* y_bf16, int64_t cols, const float* weights,
+                                   const void* base_bf16, int64_t ld_base, void* out_bf16, int64_t ld_out,
+                                   void* stream) {
+  NVFP4_TRACE("moe_combine");
+  nvfp4_status st = check_tokens(plan, cols, 8, ld_out);
+  if (st != NVFP4_OK) return st;
+  if (base_bf16 && ld_base < cols) return NVFP4_ERR_SHAPE;
+  if (plan->n_tokens == 0) return NVFP4_OK;
+  if (!y_bf16 || !out_bf16) return NVFP4_ERR_INVALID_ARG;
+  if (!aligned(y_bf16, 16) || !aligned(out_bf16, 16) || !aligned(base_bf16, 16) || !aligned(weights, 4) ||
+      (base_bf16 && ld_base % 8))
+    return NVFP4_ERR_ALIGN;
+  const Walk w = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 8));
+  if (launch_pdl(moe_combine_kernel, dim3(walk_grid(w)), dim3(kWalkThreads), 0, static_cast<cudaStream_t>(stream),
+                 row_args(plan), w, static_cast<const uint16_t*>(y_bf16), weights,
+                 static_cast<const uint16_t*>(base_bf16), ld_base, static_cast<uint16_t*>(out_bf16), ld_out) !=
+      cudaSuccess)
+    return NVFP4_ERR_CUDA;
+  count_launches(1);
+  return launch_status();
+}
+
+NVFP4_API nvfp4_status moe_combine_backward(const moe_plan* plan, const void* d_out_bf16, int64_t ld_d_out,
+                                            const void* y_bf16, int64_t cols, const float* weights, void* d_y_bf16,
+                                            float* d_weights, void* stream) {
+  NVFP4_TRACE("moe_combine_backward");
+  const nvfp4_status st = check_tokens(plan, cols, 8, ld_d_out);
+  if (st != NVFP4_OK) return st;
+  if (plan->n_tokens == 0) return NVFP4_OK;
+  if (!d_out_bf16 || !y_bf16 || !weights || (!d_y_bf16 && !d_weights)) return NVFP4_ERR_INVALID_ARG;
+  if (!aligned(d_out_bf16, 16) || !aligned(y_bf16, 16) || !aligned(d_y_bf16, 16) || !aligned(weights, 4) ||
+      !aligned(d_weights, 4))
+    return NVFP4_ERR_ALIGN;
+  const int64_t grid = (plan->n_tokens + kWalkThreads / 32 - 1) / (kWalkThreads / 32);
+  if (launch_pdl(moe_combine_backward_kernel, dim3(static_cast<uint32_t>(grid)), dim3(kWalkThreads), 0,
+                 static_cast<cudaStream_t>(stream), row_args(plan), plan->n_tokens, static_cast<uint32_t>(cols / 8),
+                 static_cast<const uint16_t*>(d_out_bf16), ld_d_out, static_cast<const uint16_t*>(y_bf16), weights,
+                 static_cast<uint16_t*>(d_y_bf16), d_weights) != cudaSuccess)
+    return NVFP4_ERR_CUDA;
+  count_launches(1);
+  return launch_status();
+}

@@ -55,7 +55,18 @@ class AttentionOptionsStruct(ctypes.Structure):
                 ("prefix_lens", _p), ("doc_start", _p)]
 
 
+class MoEPlanStruct(ctypes.Structure):
+    _fields_ = [("row_start", _p), ("rows", _p), ("row_of", _p), ("n_tokens", _i64), ("top_k", _i32),
+                ("num_experts", _i32)]
+
+
+class MoERouteOptionsStruct(ctypes.Structure):
+    _fields_ = [("score", _i32), ("renormalize", _i32), ("scale", _f32), ("bias", _p)]
+
+
 # The same structs as bytes: one call makes them.
+_PLAN, _ROUTE = struct.Struct("PPPqii"), struct.Struct("iif4xP")
+assert (_PLAN.size, _ROUTE.size) == (ctypes.sizeof(MoEPlanStruct), ctypes.sizeof(MoERouteOptionsStruct))
 _CACHE, _PAGES, _OPTIONS = struct.Struct("PPPPPiiiiffi4x"), struct.Struct("PPii"), struct.Struct("ffPi4xPP")
 assert (_CACHE.size, _PAGES.size, _OPTIONS.size) == tuple(
     ctypes.sizeof(t) for t in (KVCacheStruct, KVPagesStruct, AttentionOptionsStruct))
@@ -96,6 +107,22 @@ _extend = _sig("extend_attention_nvfp4",
                [_p, _p, _p, _i64, _i64, _i32, _p, _p, _p, _p, _sz, _p])
 _residual_norm = _sig("residual_norm_nvfp4", [_p, _i64, _p, _i64, _i64, _i64, _p, _p, _i64, _f32, _p, _f32, _p, _p, _p,
                                               _p, _p, _p])
+_moe_max_rows = _sig("moe_max_rows", [_i64, _i32, _i32], _i64)
+_moe_sort_ws = _sig("moe_sort_workspace_size", [_i64, _i32, _i32], _sz)
+_moe_route = _sig("moe_route", [_p, _i32, _i64, _i64, _i32, _i32, _p, _p, _p, _p])
+_moe_route_backward = _sig("moe_route_backward", [_p, _i32, _i64, _i64, _i32, _i32, _p, _p, _p, _p, _p])
+_moe_sort = _sig("moe_sort", [_p, _p, _p, _sz, _p])
+_moe_dispatch = _sig("moe_dispatch", [_p, _p, _i64, _i64, _p, _p, _p])
+_moe_dispatch_nvfp4 = _sig("moe_dispatch_nvfp4", [_p, _p, _i64, _i64, _p, _p, _p, _p])
+_moe_dispatch_mxfp4 = _sig("moe_dispatch_mxfp4", [_p, _p, _i64, _i64, ctypes.c_int, _p, _p, _p])
+_moe_combine = _sig("moe_combine", [_p, _p, _i64, _p, _p, _i64, _p, _i64, _p])
+_moe_combine_backward = _sig("moe_combine_backward", [_p, _p, _i64, _p, _i64, _p, _p, _p, _p])
+_linear_grouped = _sig("nvfp4_linear_grouped", [_p, _p, _p, _p, _i32, _p, _p, _p, _i64, _i64, _p, _i64, _p])
+_mx_linear_grouped = _sig("mxfp4_linear_grouped", [_p, _p, _p, _p, _p, _i64, _i64, _p, _i64, _p])
+_linear_grouped_swiglu = _sig("nvfp4_linear_grouped_swiglu_quantize",
+                              [_p, _p, _p, _p, _i32, _p, _p, _p, _i64, _i64, _p, _i32, _p, _p, _p])
+_mx_linear_grouped_swiglu = _sig("mxfp4_linear_grouped_swiglu_quantize",
+                                 [_p, _p, _p, _p, _p, _i64, _i64, ctypes.c_int, _p, _p, _p])
 _get_status = _sig("nvfp4_get_device_status", [ctypes.POINTER(_i32), _p])
 _status_string = _sig("nvfp4_status_string", [ctypes.c_int], ctypes.c_char_p)
 _launch_count = _sig("nvfp4_launch_count", [], ctypes.c_uint64)
@@ -284,7 +311,7 @@ def decode_attention_nvfp4_static_scratch(cache, q, softmax_scale, out, stream=N
 
 # The calls of a decode step are short, and so is their marshalling: plain integers for
 # pointers, each tensor looked at once, the structs packed (include/nvfp4.h's layout).
-_bf16, _int32, _float32 = torch.bfloat16, torch.int32, torch.float32
+_bf16, _int32, _float32, _uint8 = torch.bfloat16, torch.int32, torch.float32, torch.uint8
 
 
 def _rows3(x, what):
@@ -395,6 +422,170 @@ def residual_norm_nvfp4(x, y, r_out, h_out, w_norm, eps=1e-6, w_post=None, gate=
                           _typed(scales, torch.uint8, "scales"), _stream(stream)))
 
 
+# ------------------------------------------------- mixture of experts ---
+
+MOE_SOFTMAX, MOE_SIGMOID = 0, 1
+
+
+def moe_max_rows(n_tokens, top_k, num_experts):
+    """Rows of a plan's buffers (include/nvfp4.h)."""
+    return int(_moe_max_rows(n_tokens, top_k, num_experts))
+
+
+def moe_sort_workspace_size(n_tokens, top_k, num_experts):
+    return int(_moe_sort_ws(n_tokens, top_k, num_experts))
+
+
+def _matrix(x, rows, cols, what):
+    """(pointer, elements between rows) of a bf16 [rows, cols] argument whose rows may be padded."""
+    if x.dtype is not _bf16 or x.shape != (rows, cols) or (cols > 1 and x.stride(1) != 1):
+        raise ValueError(f"{what} must be row-major bfloat16 [{rows}, {cols}]")
+    return x.data_ptr(), x.stride(0) if rows > 1 else cols
+
+
+def _router(logits, top_k, score, renormalize, scale, bias):
+    n, experts = logits.shape
+    if logits.dtype not in (_float32, _bf16) or (experts > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be row-major float32 or bfloat16 [tokens, experts]")
+    return (logits.data_ptr(), 1 if logits.dtype is _bf16 else 0, logits.stride(0) if n > 1 else experts, n, experts,
+            top_k, _ROUTE.pack(score, renormalize, scale, _typed(bias, _float32, "bias", experts) or 0))
+
+
+def moe_route(logits, expert_idx, weights, score=MOE_SOFTMAX, renormalize=True, scale=1.0, bias=None, stream=None):
+    """The experts expert_idx [tokens, top_k] (int32) of each token and their weights (float32) from logits [tokens,
+    experts]; bias (with MOE_SIGMOID) moves the choice alone."""
+    n, k = expert_idx.shape
+    if n != logits.shape[0]:
+        raise ValueError("expert_idx must be [tokens, top_k] of the logits' tokens")
+    _check("moe_route", _moe_route(*_router(logits, k, score, renormalize, scale, bias),
+                                   _typed(expert_idx, _int32, "expert_idx"),
+                                   _typed(weights, _float32, "weights", n * k), _stream(stream)))
+
+
+def moe_route_backward(logits, expert_idx, d_weights, d_logits, score=MOE_SOFTMAX, renormalize=True, scale=1.0,
+                       stream=None):
+    """The logits' gradient (dense, of their type) from that of moe_route's weights."""
+    n, k = expert_idx.shape
+    if n != logits.shape[0]:
+        raise ValueError("expert_idx must be [tokens, top_k] of the logits' tokens")
+    _check("moe_route_backward",
+           _moe_route_backward(*_router(logits, k, score, renormalize, scale, None),
+                               _typed(expert_idx, _int32, "expert_idx"),
+                               _typed(d_weights, _float32, "d_weights", n * k),
+                               _typed(d_logits, logits.dtype, "d_logits", logits.numel()), _stream(stream)))
+
+
+def moe_sort(plan, expert_idx, stream=None):
+    """The plan's rows for expert_idx int32 [n_tokens, top_k]; a negative entry is a choice without an expert."""
+    ws = plan.workspace
+    _check("moe_sort", _moe_sort(plan.packed(), _typed(expert_idx, _int32, "expert_idx", plan.n_tokens * plan.top_k),
+                                 *((None, 0) if ws is None else (ws.data_ptr(), ws.nbytes)), _stream(stream)))
+
+
+def moe_dispatch(plan, x, rows, weights=None, stream=None):
+    """x [n_tokens, cols] bf16 to its experts' rows [plan.max_rows, cols], times weights [n_tokens, top_k] if given."""
+    cols = x.shape[1]
+    xp, ld = _matrix(x, plan.n_tokens, cols, "x")
+    _check("moe_dispatch",
+           _moe_dispatch(plan.packed(), xp, ld, cols, _typed(weights, _float32, "weights", plan.n_tokens * plan.top_k),
+                         _typed(rows, _bf16, "rows", plan.max_rows * cols), _stream(stream)))
+
+
+def _row_operand(plan, codes, scales, cols, what):
+    """Pointers of a plan's rows as a linear's 4-bit operand: codes [max_rows, cols/2], MMA-layout scales."""
+    return (_typed(codes, _uint8, what + " codes", plan.max_rows * cols // 2),
+            _typed(scales, _uint8, what + " scales", plan.max_rows * cols // 16))
+
+
+def moe_dispatch_nvfp4(plan, x, g, codes, scales, stream=None):
+    """x [n_tokens, cols] bf16, NVFP4-quantized with the scale g, to its experts' rows (MMA-layout scales)."""
+    cols = x.shape[1]
+    xp, ld = _matrix(x, plan.n_tokens, cols, "x")
+    _check("moe_dispatch_nvfp4",
+           _moe_dispatch_nvfp4(plan.packed(), xp, ld, cols, _typed(g, _float32, "g", 1),
+                               *_row_operand(plan, codes, scales, cols, "rows'"), _stream(stream)))
+
+
+def moe_dispatch_mxfp4(plan, x, codes, scales, rotate=False, stream=None):
+    cols = x.shape[1]
+    xp, ld = _matrix(x, plan.n_tokens, cols, "x")
+    _check("moe_dispatch_mxfp4",
+           _moe_dispatch_mxfp4(plan.packed(), xp, ld, cols, int(bool(rotate)),
+                               *_row_operand(plan, codes, scales, cols, "rows'"), _stream(stream)))
+
+
+def moe_combine(plan, y, out, weights=None, base=None, stream=None):
+    """out [n_tokens, cols] = base + the sum of weights * y over each token's rows; without weights, also the gradient
+    of moe_dispatch's x from that of its rows, y."""
+    cols = out.shape[1]
+    op, ld = _matrix(out, plan.n_tokens, cols, "out")
+    _check("moe_combine",
+           _moe_combine(plan.packed(), _typed(y, _bf16, "y", plan.max_rows * cols), cols,
+                        _typed(weights, _float32, "weights", plan.n_tokens * plan.top_k),
+                        *((None, 0) if base is None else _matrix(base, plan.n_tokens, cols, "base")), op, ld,
+                        _stream(stream)))
+
+
+def moe_combine_backward(plan, d_out, y, weights, d_y, d_weights, stream=None):
+    """moe_combine's gradients: d_y [max_rows, cols] and d_weights [n_tokens, top_k]; one of them may be None."""
+    cols, n = d_out.shape[1], plan.n_tokens * plan.top_k
+    gp, ld = _matrix(d_out, plan.n_tokens, cols, "d_out")
+    _check("moe_combine_backward",
+           _moe_combine_backward(plan.packed(), gp, ld, _typed(y, _bf16, "y", plan.max_rows * cols), cols,
+                                 _typed(weights, _float32, "weights", n),
+                                 _typed(d_y, _bf16, "d_y", plan.max_rows * cols),
+                                 _typed(d_weights, _float32, "d_weights", n), _stream(stream)))
+
+
+def _expert_weights(plan, codes, scales, N, K):
+    E = plan.num_experts
+    return (_typed(codes, _uint8, "w_codes", E * N * K // 2),
+            _typed(scales, _uint8, "w_scales", E * ((N + 127) // 128 * 128) * (K // 16)))
+
+
+def _per_expert(g, plan, what):
+    """(pointer, step) of a tensor scale: one for all, or one an expert."""
+    n = g.numel()
+    if n != 1 and n != plan.num_experts:
+        raise ValueError(f"{what} must have one element or one an expert")
+    return _typed(g, _float32, what), 0 if n == 1 else 1
+
+
+def nvfp4_linear_grouped(plan, a_codes, a_scales, g_a, w_codes, w_scales, g_w, out, N, K, stream=None):
+    """out [plan.max_rows, N]: each expert's rows [.., K] times its weight [N, K]; g_a: one or one an expert."""
+    op, ldo = _matrix(out, plan.max_rows, N, "out")
+    _check("nvfp4_linear_grouped",
+           _linear_grouped(plan.packed(), *_row_operand(plan, a_codes, a_scales, K, "a"), *_per_expert(g_a, plan, "g_a"),
+                           *_expert_weights(plan, w_codes, w_scales, N, K),
+                           _typed(g_w, _float32, "g_w", plan.num_experts), N, K, op, ldo, _stream(stream)))
+
+
+def mxfp4_linear_grouped(plan, a_codes, a_scales, w_codes, w_scales, out, N, K, stream=None):
+    op, ldo = _matrix(out, plan.max_rows, N, "out")
+    _check("mxfp4_linear_grouped",
+           _mx_linear_grouped(plan.packed(), *_row_operand(plan, a_codes, a_scales, K, "a"),
+                              *_expert_weights(plan, w_codes, w_scales, N, K), N, K, op, ldo, _stream(stream)))
+
+
+def nvfp4_linear_grouped_swiglu_quantize(plan, a_codes, a_scales, g_a, w_codes, w_scales, g_w, I, K, g_out, out_codes,
+                                         out_scales, stream=None):
+    """h = SiLU(gate) * up of each expert's rows, NVFP4-quantized with g_out (one or one an expert)."""
+    _check("nvfp4_linear_grouped_swiglu_quantize",
+           _linear_grouped_swiglu(plan.packed(), *_row_operand(plan, a_codes, a_scales, K, "a"),
+                                  *_per_expert(g_a, plan, "g_a"), *_expert_weights(plan, w_codes, w_scales, 2 * I, K),
+                                  _typed(g_w, _float32, "g_w", plan.num_experts), I, K,
+                                  *_per_expert(g_out, plan, "g_out"),
+                                  *_row_operand(plan, out_codes, out_scales, I, "out"), _stream(stream)))
+
+
+def mxfp4_linear_grouped_swiglu_quantize(plan, a_codes, a_scales, w_codes, w_scales, I, K, out_codes, out_scales,
+                                         rotate=False, stream=None):
+    _check("mxfp4_linear_grouped_swiglu_quantize",
+           _mx_linear_grouped_swiglu(plan.packed(), *_row_operand(plan, a_codes, a_scales, K, "a"),
+                                     *_expert_weights(plan, w_codes, w_scales, 2 * I, K), I, K, int(bool(rotate)),
+                                     *_row_operand(plan, out_codes, out_scales, I, "out"), _stream(stream)))
+
+
 def nvfp4_qfit_workspace_size(batch, tokens, num_q_heads, num_kv_heads, grid_s, grid_m):
     return int(_qfit_ws(batch, tokens, num_q_heads, num_kv_heads, grid_s, grid_m))
 
@@ -472,6 +663,27 @@ class KVPages:
         return _PAGES.pack(self.table.data_ptr(), self.seq_lens.data_ptr(), self.batch, self.pages_per_seq)
 
 
+class MoEPlan:
+    """Which rows of the sorted buffers n_tokens tokens with top_k choices among num_experts experts have (layout of
+    include/nvfp4.h): written by moe_sort, read by the calls on rows.  Buffers of rows have max_rows of them."""
+
+    def __init__(self, n_tokens, top_k, num_experts, device="cuda"):
+        self.n_tokens, self.top_k, self.num_experts = n_tokens, top_k, num_experts
+        self.max_rows = moe_max_rows(n_tokens, top_k, num_experts)
+        if self.max_rows == 0 and n_tokens != 0:
+            raise ValueError("n_tokens, top_k or num_experts out of range")
+        self.row_start = torch.zeros(num_experts + 1, dtype=torch.int32, device=device)
+        self.rows = torch.zeros(num_experts, dtype=torch.int32, device=device)
+        self.row_of = torch.full((n_tokens, top_k), -1, dtype=torch.int32, device=device)
+        size = moe_sort_workspace_size(n_tokens, top_k, num_experts)
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=device) if size else None
+
+    def packed(self):
+        """The moe_plan's bytes, for the calls that take it packed."""
+        return _PLAN.pack(self.row_start.data_ptr(), self.rows.data_ptr(), self.row_of.data_ptr(), self.n_tokens,
+                          self.top_k, self.num_experts)
+
+
 EXPORTED = ["nvfp4_scales_bytes", "nvfp4_tensor_scale", "nvfp4_quantize", "nvfp4_quantize_dynamic", "nvfp4_scales_relayout", "nvfp4_linear",
             "nvfp4_linear_dynamic",
             "nvfp4_linear_swiglu_quantize", "nvfp4_interleave_gate_up",
@@ -481,4 +693,7 @@ EXPORTED = ["nvfp4_scales_bytes", "nvfp4_tensor_scale", "nvfp4_quantize", "nvfp4
             "decode_attention_nvfp4_static_scratch", "nvfp4_qfit_workspace_size", "nvfp4_qfit_calibrate",
             "kv_append_rope_axes_nvfp4", "kv_read_nvfp4", "extend_attention_nvfp4_workspace_size",
             "extend_attention_nvfp4", "residual_norm_nvfp4",
+            "moe_max_rows", "moe_route", "moe_route_backward", "moe_sort_workspace_size", "moe_sort", "moe_dispatch",
+            "moe_dispatch_nvfp4", "moe_dispatch_mxfp4", "moe_combine", "moe_combine_backward", "nvfp4_linear_grouped",
+            "mxfp4_linear_grouped", "nvfp4_linear_grouped_swiglu_quantize", "mxfp4_linear_grouped_swiglu_quantize",
             "nvfp4_get_device_status", "nvfp4_status_string", "nvfp4_launch_count", "nvfp4_debug_inject_fault"]
