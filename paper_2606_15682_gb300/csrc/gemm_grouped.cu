@@ -3,9 +3,30 @@
 //   out[r, n] = bf16( g_a[e] g_w[e] sum_k a[r, k] w_e[n, k] ),  r among expert e's rows
 // and the same for gate_up with h = SiLU(gate) up quantized in the epilogue.
 //
-// A 64 x 64 tile per CTA: both operands dequantized into shared memory as fp32,
-// a thread has 4 x 4 sums.
+// A pair of CTAs has a tile of 256 weight rows and up to 256 of one expert's rows
+// by tcgen05.mma.cta_group::2 (kind::mxf4nvf4, 16-element block scales).  The weight
+// is the M side: its rows come in 256s whatever the router does, while an expert may
+// have one row or 700, and N takes any multiple of 32.  So a few rows cost the
+// weight's bytes and no more, and many leave at most 31 columns idle.  Each CTA holds
+// its 128 weight rows and half of the tokens' rows; D[weight row, token] is in its
+// own TMEM lanes.  Which tiles there are follows from the plan on the device: every
+// CTA sums the experts' tiles (shared memory) and takes units u, u + pairs, ...; an
+// expert's units are next to each other, those of one weight tile first, so that its
+// bytes come from DRAM once.
+//   warp 0      codes; a CTA's weight rows and its half of the tokens' rows
+//   warp 1      leader: MMAs; peer: block scales
+//   warp 2      leader: block scales into TMEM
+//   warp 3      leader: block scales
+//   warps 4-11  epilogue: 32 weight rows x every other 32 tokens each
+// The epilogue reads 16 x 8 fragments of D (16x256b), in which a thread has two tokens
+// of two weight rows, and of gate and up at once: bf16 rows are turned into token-major
+// ones by a transposing stmatrix, quantized outputs need shuffles only.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
 #include <cfloat>
+#include <map>
+#include <mutex>
 
 #include "moe_plan.cuh"
 #include "nvfp4_quant.cuh"
@@ -13,7 +34,24 @@
 namespace nvfp4 {
 namespace {
 
-constexpr int kTile = 64, kDepth = 32, kPitch = kTile + 4;
+constexpr int kDepth = 256;  // elements of K per stage: 128 bytes of a row
+constexpr int kStages = 5;
+constexpr int kTokens = 256;  // of a tile
+constexpr int kWRows = 256;
+constexpr int kEpi0 = 4, kEpiWarps = 8;
+constexpr int kThreads = 32 * (kEpi0 + kEpiWarps);
+constexpr uint32_t kWBytes = 128 * kDepth / 2, kXBytes = 128 * kDepth / 2;  // a CTA's codes of a stage
+constexpr uint32_t kScaleTile = 128 * kDepth / 16;                         // block scales of 128 rows: four atoms
+constexpr uint32_t kEpiBytes = 2048;                                       // a warp's 32 tokens x 32 bf16
+constexpr uint32_t kTmemCols = 512, kSfCol = kTokens, kSfCols = 16 + 32;
+constexpr size_t kSmem = 1024 + kStages * (kWBytes + kXBytes + 3 * kScaleTile) + kEpiWarps * kEpiBytes +
+                         kMoeMaxExperts * (sizeof(int) + sizeof(int2)) + 512;
+static_assert(kSfCol + kStages * kSfCols <= kTmemCols, "TMEM budget");
+static_assert(kSmem <= 227 * 1024, "shared memory budget");
+static_assert(3 * kThreads >= kMoeMaxExperts, "three experts a thread");
+// kind::mxf4nvf4: A and B packed E2M1, K-major; M = 256.  N >> 3 is added at bit 17, UE8M0 scales set bit 23.
+constexpr uint32_t kIdesc = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kWRows >> 4) << 24);
+constexpr uint32_t kUE8M0 = 1u << 23;
 
 struct GroupedArgs {
   const int32_t* row_start;
@@ -30,138 +68,690 @@ struct GroupedArgs {
   uint8_t* q_scales;
   int64_t ldo;
   int experts, max_rows, N, K, g_a_step, g_out_step;
+  int w_tiles;        // 256-row tiles of an expert's weight
+  int w_scale_tiles;  // 128-row tiles of its scales
+  int max_units;      // what a plan can have: one of any numbers is cut to it
   bool mx;
-  uint32_t q_mode;  // 0 NVFP4, 1 MXFP4, 2 MXFP4 after the block rotation
+  bool rotate;
+  int fault_skip_stage;  // test-only: pair 0 leaves its first stage neither armed nor loaded
   int* status;
 };
+
+// ------------------------------------------------------------- PTX pieces ---
+
+// K-major operand tile, 128-byte swizzle: rows of 128 B, 8-row groups 1024 B apart.
+__device__ __forceinline__ uint64_t tile_desc(uint32_t saddr) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (1ull << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) |
+         (1ull << 46) | (2ull << 61);
+}
+// A 512-byte scale atom: 32 rows of 16 B, no swizzle, 8-row core matrices 128 B apart.
+__device__ __forceinline__ uint64_t atom_desc(uint32_t saddr) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(128 >> 4) << 16) |
+         (static_cast<uint64_t>(128 >> 4) << 32) | (1ull << 46);
+}
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                         uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%5], [%6], p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
+      : "memory");
+}
+__device__ __forceinline__ void pair_copy_scales(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void pair_commit(uint64_t* bar, uint16_t mask) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                   smem_u32(bar)),
+               "h"(mask)
+               : "memory");
+}
+__device__ __forceinline__ void pair_tmem_alloc(uint32_t* slot, uint32_t cols) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(cols)
+               : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void pair_tmem_free(uint32_t taddr, uint32_t cols) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
+}
+__device__ __forceinline__ uint32_t leader_address(const uint64_t* bar) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(bar)));
+  return r;
+}
+// Boxes into this CTA's shared memory, counted on the leader's barrier at `bar`.
+__device__ __forceinline__ void load_box(void* dst, const void* map, uint64_t* bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(leader_address(bar)), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void load_box3(void* dst, const void* map, uint64_t* bar, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(leader_address(bar)), "r"(0), "r"(y), "r"(z)
+      : "memory");
+}
+// Hands the accumulator back: the warp's TMEM loads are complete and fenced, and no memory that it wrote is read.
+__device__ __forceinline__ void arrive_leader_relaxed(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_address(bar)) : "memory");
+}
+// After a pipeline gave up: lets this thread's copies land before its pair exits.
+__device__ __forceinline__ void wait_for_copies() {
+  const uint64_t t0 = globaltimer_ns();
+  while (globaltimer_ns() - t0 < kDrainLimitNs) __nanosleep(100000);
+}
+// 16 lanes x 32 columns: registers 4j .. 4j + 3 are columns 8j + 2 (lane % 4) and the next one, of lane's row
+// lane / 4 and of the row 8 below.
+__device__ __forceinline__ void tmem_ld_fragments(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_done() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
   uint32_t d;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
 }
+__device__ __forceinline__ uint32_t e2m1x2(float lo, float hi) {
+  uint32_t d;
+  asm("{\n .reg .b8 b;\n .reg .b16 h;\n cvt.rn.satfinite.e2m1x2.f32 b, %2, %1;\n mov.b16 h, {b, 0};\n cvt.u32.u16 %0, h;\n}"
+      : "=r"(d)
+      : "f"(lo), "f"(hi));
+  return d;
+}
+// Four transposed 8 x 8 matrices of 16-bit elements; lane l has the address of row l % 8 of matrix l / 8.
+__device__ __forceinline__ void stmatrix_t(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b),
+               "r"(c), "r"(d)
+               : "memory");
+}
+__device__ __forceinline__ float silu_mul(float gate, float up) {
+  return __fdividef(gate, 1.0f + __expf(-gate)) * up;
+}
+// Two warps of the epilogue meet; true where both gave true.
+__device__ __forceinline__ bool both(int id, bool ok) {
+  int r;
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.b32 p, %2, 0;\n barrier.cta.red.and.pred q, %1, 64, p;\n selp.s32 %0, 1, 0, q;\n}"
+      : "=r"(r)
+      : "r"(id), "r"(ok ? 1 : 0)
+      : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void meet(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
 
-__device__ __forceinline__ float e2m1_value(uint32_t c) {
-  const uint32_t m = c & 7;
-  const float v = m < 2 ? 0.5f * m : __uint_as_float((126 + (m >> 1)) << 23 | (m & 1) << 22);
-  return c & 8 ? -v : v;
+// ------------------------------------------------------------------ units ---
+
+struct Unit {
+  int expert, w_tile;
+  int row0, tokens;  // first row, rows of the tile
+  int n;             // the MMA's N: tokens up to a multiple of 32
+};
+// Unit u, by a converged warp.  ends: [1024] units of the experts up to each one, the total behind the last one.
+__device__ __forceinline__ Unit find_unit(int u, const int* ends, const int2* rows, int lane) {
+  const int block = __popc(__ballot_sync(0xffffffffu, ends[32 * lane + 31] <= u));
+  const int e = 32 * block + __popc(__ballot_sync(0xffffffffu, ends[32 * block + lane] <= u));
+  const int2 r = rows[e];  // first row, rows
+  const int local = u - (e ? ends[e - 1] : 0), tiles = (r.y + kTokens - 1) / kTokens;
+  Unit t;
+  t.expert = e;
+  t.w_tile = local / tiles;
+  const int token_tile = local - t.w_tile * tiles;
+  t.row0 = r.x + token_tile * kTokens;
+  t.tokens = min(kTokens, r.y - token_tile * kTokens);
+  t.n = (t.tokens + 31) & ~31;
+  return t;
 }
 
-template <bool kSwiGLU>
-__global__ void __launch_bounds__(256) grouped_simple_kernel(const GroupedArgs a) {
-  __shared__ float sa[kDepth][kPitch], sw[kDepth][kPitch];
-  __shared__ float tile[kTile][kTile + 1];
+// --------------------------------------------------------------- epilogue ---
+// lo, hi: the fragments of a warp's weight rows 0..15 and 16..31, 32 tokens from token0.
+
+__device__ __forceinline__ void store_rows(const GroupedArgs& a, const Unit& t, const uint32_t* lo, const uint32_t* hi,
+                                           int token0, int n0, float scale, uint32_t buf, int lane) {
+  auto f = [&](uint32_t v) { return __uint_as_float(v) * scale; };
+  // Rows of 64 bytes in 16-byte chunks, chunk c of token t at c ^ (t / 2) % 4: no bank twice, written or read.
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int tk = 8 * j + (lane & 7);
+    stmatrix_t(buf + tk * 64 + (((lane >> 3) ^ ((tk >> 1) & 3)) << 4), pack_pair(f(lo[4 * j]), f(lo[4 * j + 1])),
+               pack_pair(f(lo[4 * j + 2]), f(lo[4 * j + 3])), pack_pair(f(hi[4 * j]), f(hi[4 * j + 1])),
+               pack_pair(f(hi[4 * j + 2]), f(hi[4 * j + 3])));
+  }
+  __syncwarp();
+  const int c = lane & 3, n = n0 + 8 * c;
+#pragma unroll
+  for (int it = 0; it < 4; ++it) {
+    const int tk = 8 * it + (lane >> 2);
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "r"(buf + tk * 64 + ((c ^ ((tk >> 1) & 3)) << 4))
+                 : "memory");
+    // N % 16 == 0: a chunk is inside or outside.
+    if (token0 + tk < t.tokens && n < a.N && in_bounds(a.status, t.row0 + token0 + tk < a.max_rows && n + 8 <= a.N))
+      *reinterpret_cast<uint4*>(a.out + static_cast<int64_t>(t.row0 + token0 + tk) * a.ldo + n) = v;
+  }
+  __syncwarp();
+}
+
+// h = SiLU(gate) up over lo; lane has rows lane / 4 and 8 below, tokens 2 (lane % 4) and the next.
+__device__ __forceinline__ void swiglu_fragments(uint32_t* lo, const uint32_t* hi, float scale) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    lo[i] = __float_as_uint(silu_mul(__uint_as_float(lo[i]) * scale, __uint_as_float(hi[i]) * scale));
+}
+
+// The largest magnitude of 16 outputs of a token: of the even token of the fragment where lane / 4 is even, of the odd.
+__device__ __forceinline__ float token_amax(const uint32_t* h, int lane) {
+  auto f = [&](int i) { return fabsf(__uint_as_float(h[i])); };
+  const float even = fmaxf(f(0), f(2)), odd = fmaxf(f(1), f(3));
+  const bool o = lane & 4;
+  float v = fmaxf(o ? odd : even, __shfl_xor_sync(0xffffffffu, o ? even : odd, 4));
+  v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+  return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+}
+
+// The 16 codes of this lane's token (as token_amax has them), element 0 in the lowest nibble; mult: the token's factor.
+__device__ __forceinline__ uint2 token_codes(const uint32_t* h, float mult, int lane) {
+  auto f = [&](int i, float m) { return __fmul_rn(__uint_as_float(h[i]), m); };
+  const bool o = lane & 4;
+  const float other = __shfl_xor_sync(0xffffffffu, mult, 4);
+  const float m_even = o ? other : mult, m_odd = o ? mult : other;
+  // Low nibble: row lane / 4; high: 8 below.
+  const uint32_t even = e2m1x2(f(0, m_even), f(2, m_even)), odd = e2m1x2(f(1, m_odd), f(3, m_odd));
+  const uint32_t mine = o ? odd : even, got = __shfl_xor_sync(0xffffffffu, o ? even : odd, 4);
+  const uint32_t first = o ? got : mine, second = o ? mine : got;  // of rows 2i and 2i + 1, i = lane / 8
+  const uint32_t low = (first & 15) | (second & 15) << 4, high = first >> 4 | (second & 0xF0);
+  const int s = lane & 8;
+  uint32_t w = low << s | high << (16 + s);
+  w |= __shfl_xor_sync(0xffffffffu, w, 8);
+  const uint32_t v = __shfl_xor_sync(0xffffffffu, w, 16);
+  const uint32_t a = lane & 16 ? v : w, b = lane & 16 ? w : v;  // rows 0-3 and 8-11; 4-7 and 12-15
+  return make_uint2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+}
+
+__device__ __forceinline__ void store_codes(const GroupedArgs& a, const Unit& t, uint2 codes, uint32_t code, int token0,
+                                            uint32_t oc, int lane) {
+  // Lane's token: group lane / 8 of 8, 2 (lane % 4) in it and the next where lane / 4 is odd.
+  const int tk = token0 + 8 * (lane >> 3) + 2 * (lane & 3) + ((lane >> 2) & 1);
+  if (tk >= t.tokens) return;
+  const uint64_t row = t.row0 + tk;
+  const uint32_t cols = static_cast<uint32_t>(a.N) >> 1;
+  const uint64_t off = mma_scale_offset(row, oc >> 4, cols >> 6);
+  if (!in_bounds(a.status, row < static_cast<uint64_t>(a.max_rows) && oc + 16 <= cols &&
+                               off < static_cast<uint64_t>(a.max_rows) * (cols >> 4)))
+    return;
+  *reinterpret_cast<uint2*>(a.q_codes + row * (cols >> 1) + (oc >> 1)) = codes;
+  a.q_scales[off] = static_cast<uint8_t>(code);
+}
+
+// kMode: 0 bf16 rows, 1 SwiGLU to NVFP4, 2 SwiGLU to MXFP4.
+template <int kMode>
+__global__ void __launch_bounds__(kThreads, 1)
+    grouped_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_w_scales,
+                   const __grid_constant__ CUtensorMap map_x16, const __grid_constant__ CUtensorMap map_x64,
+                   const __grid_constant__ CUtensorMap map_x128, const __grid_constant__ CUtensorMap map_x_scales,
+                   const __grid_constant__ CUtensorMap map_x_scales2, const GroupedArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sW = smem;
+  uint8_t* sX = sW + kStages * kWBytes;
+  uint8_t* sWS = sX + kStages * kXBytes;
+  uint8_t* sXS = sWS + kStages * kScaleTile;
+  uint8_t* sEpi = sXS + kStages * 2 * kScaleTile;
+  int2* expert_rows_s = reinterpret_cast<int2*>(sEpi + kEpiWarps * kEpiBytes);
+  int* ends = reinterpret_cast<int*>(expert_rows_s + kMoeMaxExperts);
+  uint64_t* full = reinterpret_cast<uint64_t*>(ends + kMoeMaxExperts);  // codes landed, scales in TMEM
+  uint64_t* empty = full + kStages;                                    // the stage's MMAs are done
+  uint64_t* scales_in = empty + kStages;                               // block scales landed
+  uint64_t* acc_full = scales_in + kStages;
+  uint64_t* acc_empty = acc_full + 1;
+  uint64_t* drain = acc_empty + 1;
+  uint64_t* drain_copies = drain + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_copies + 1);
+  __shared__ volatile int abort_flag;
+  __shared__ int64_t warp_sum[kThreads / 32];
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int kblocks = a.K / kDepth;
+  const uint32_t rank = cluster_ctarank();
+  const bool leader = rank == 0;
+  const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      // The commit of the copies of the stage's scales into TMEM, in the leader also an expect_tx of both CTAs' codes.
+      mbar_init(&full[s], leader ? 2 : 1);
+      mbar_init(&empty[s], 1);
+      mbar_init(&scales_in[s], 1);
+    }
+    mbar_init(acc_full, 1);
+    mbar_init(acc_empty, 2 * kEpiWarps);
+    mbar_init(drain, 1);
+    mbar_init(drain_copies, 1);
+    abort_flag = 0;
+    fence_mbar_init();
+    prefetch_tmap(&map_w);
+    prefetch_tmap(&map_w_scales);
+    prefetch_tmap(&map_x16);
+    prefetch_tmap(&map_x_scales);
+  }
+  if (warp == 1) pair_tmem_alloc(tmem_slot, kTmemCols);
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
   griddep_wait_and_release();
-  // The tile's expert: the last one that starts at or before it.
-  const int r0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
-  int lo = 0, hi = a.experts;  // row_start[lo] <= r0 < row_start[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (__ldg(a.row_start + mid) <= r0) lo = mid; else hi = mid;
-  }
-  const ExpertRows er = expert_rows(a.row_start, a.rows, lo, a.max_rows);
-  const int live = min(kTile, er.first + er.n - r0);
-  if (r0 < er.first || live <= 0) return;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const uint32_t kgroups = a.K / 64;
-  const uint64_t w_tile_bytes = static_cast<uint64_t>((a.N + 127) / 128) * 128 * (a.K / 16);
-  const uint8_t* w_codes = a.w_codes + static_cast<uint64_t>(lo) * a.N * (a.K / 2);
-  const uint8_t* w_scales = a.w_scales + lo * w_tile_bytes;
-  auto scale = [&](uint32_t c) { return a.mx ? __uint_as_float(c ? c << 23 : 1u << 22) : e4m3_value(c); };
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < a.K; k0 += kDepth) {
-    // 64 rows x 32 channels: 2 blocks of 16 a row; half of the threads load each operand.
-    const int half = threadIdx.x >> 7, i = threadIdx.x & 127, r = i >> 1, b = i & 1;
-    const int64_t row = half ? n0 + r : r0 + r;
-    const bool ok = half ? row < a.N : r < live;
-    uint2 c = make_uint2(0, 0);
-    float s = 0.0f;
-    if (ok) {
-      c = *reinterpret_cast<const uint2*>((half ? w_codes : a.a_codes) + row * (a.K / 2) + (k0 + 16 * b) / 2);
-      s = scale((half ? w_scales : a.a_scales)[mma_scale_offset(row, k0 / 16 + b, kgroups)]);
-    }
-    __syncthreads();
+
+  // The experts' rows and units: three experts a thread, summed over the CTA.
+  {
+    int64_t n[3], sum = 0;
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-      (half ? sw : sa)[16 * b + e][r] = s * e2m1_value((e < 8 ? c.x >> (4 * e) : c.y >> (4 * (e - 8))) & 15);
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kDepth; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(&sa[k][4 * ty]);
-      const float4 w = *reinterpret_cast<const float4*>(&sw[k][4 * tx]);
-      const float xs[4] = {x.x, x.y, x.z, x.w}, ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (int p = 0; p < 4; ++p)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) acc[p][q] = fmaf(xs[p], ws[q], acc[p][q]);
-    }
-  }
-  const float g = a.g_a ? __fmul_rn(__ldg(a.g_a + lo * a.g_a_step), __ldg(a.g_w + lo)) : 1.0f;
-  if constexpr (!kSwiGLU) {
-#pragma unroll
-    for (int p = 0; p < 4; ++p)
-      if (4 * ty + p < live && n0 + 4 * tx < a.N)
-        *reinterpret_cast<uint2*>(a.out + static_cast<int64_t>(r0 + 4 * ty + p) * a.ldo + n0 + 4 * tx) =
-            make_uint2(pack_pair(acc[p][0] * g, acc[p][1] * g), pack_pair(acc[p][2] * g, acc[p][3] * g));
-  } else {
-#pragma unroll
-    for (int p = 0; p < 4; ++p)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) tile[4 * ty + p][4 * tx + q] = acc[p][q] * g;
-    __syncthreads();
-    if (static_cast<int>(threadIdx.x) >= live) return;
-    // A thread has a row: 32 outputs of the tile's 16 gate, 16 up, 16 gate, 16 up rows.
-    const int r = threadIdx.x;
-    const uint32_t cols = a.N / 2, oc0 = n0 / 2;
-    float h[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float gate = tile[r][32 * (i >> 4) + (i & 15)], up = tile[r][32 * (i >> 4) + 16 + (i & 15)];
-      h[i] = gate / (1.0f + expf(-gate)) * up;
-    }
-    uint32_t code[2];
-    if (a.q_mode == 0) {
-      const float g_in = __ldg(a.g_out + lo * a.g_out_step);
-      const bool g_ok = g_in > 0.0f && g_in <= FLT_MAX;
-      if (!g_ok) set_status(a.status, NVFP4_ERR_INVALID_ARG);
-      const float go = g_ok ? g_in : 1.0f;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        float amax = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) amax = fmaxf(amax, fabsf(h[16 * b + i]));
-        const BlockScale s = block_scale(amax, go, __fmul_rn(6.0f, go));
-        code[b] = g_ok ? s.code : 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) h[16 * b + i] = g_ok ? __fmul_rn(h[16 * b + i], s.mult) : 0.0f;
+    for (int i = 0; i < 3; ++i) {
+      const int e = 3 * threadIdx.x + i;
+      n[i] = 0;
+      if (e < a.experts) {
+        const ExpertRows r = expert_rows(a.row_start, a.rows, e, a.max_rows);
+        expert_rows_s[e] = make_int2(r.first, r.n);
+        n[i] = static_cast<int64_t>((r.n + kTokens - 1) / kTokens) * a.w_tiles;
       }
-    } else {
-      if (a.q_mode == 2) hadamard32(h);
-      float amax = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(h[i]));
-      code[0] = code[1] = mx_scale_code(amax);
-#pragma unroll
-      for (int i = 0; i < 32; ++i) h[i] = __fmul_rn(h[i], mx_inv_scale(code[0]));
+      sum += n[i];
     }
-    const uint64_t row = r0 + r;
-    *reinterpret_cast<uint4*>(a.q_codes + row * (cols / 2) + oc0 / 2) =
-        make_uint4(e2m1x8(h), e2m1x8(h + 8), e2m1x8(h + 16), e2m1x8(h + 24));
-    *reinterpret_cast<uint16_t*>(a.q_scales + mma_scale_offset(row, oc0 / 16, cols / 64)) =
-        static_cast<uint16_t>(code[0] | code[1] << 8);
+    int64_t upto = sum;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, upto, s);
+      if (lane >= s) upto += v;
+    }
+    if (lane == 31) warp_sum[warp] = upto;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) upto += warp_sum[w];
+    upto -= sum;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      upto += n[i];
+      if (3 * threadIdx.x + i < kMoeMaxExperts)
+        ends[3 * threadIdx.x + i] = static_cast<int>(min(upto, static_cast<int64_t>(a.max_units)));
+    }
+    __syncthreads();
   }
+  const int units = ends[kMoeMaxExperts - 1];
+  const uint32_t tmem = *tmem_slot;
+
+  auto fail = [&]() {
+    set_status(a.status, NVFP4_ERR_TIMEOUT);
+    abort_flag = 1;
+  };
+  // A warp's lanes decide together: a wait that runs out in one of them ends all.
+  const auto wait = [&](uint64_t* bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, &abort_flag)) != 0;
+  };
+  // Walks this pair's units and k-blocks; load(stage, kb, unit), in one lane, fills a stage once `free` says so.
+  auto produce = [&](uint64_t* free, auto&& load) {
+    const bool issuer = elect_one();
+    int stage = 0;
+    uint32_t phase = 0;
+    bool skip = a.fault_skip_stage && pair == 0, ok = true;
+    for (int u = pair; u < units && ok; u += pairs) {
+      const Unit t = find_unit(u, ends, expert_rows_s, lane);
+      for (int kb = 0; kb < kblocks; ++kb) {
+        ok = wait(&free[stage], phase ^ 1u);
+        if (!ok) { fail(); break; }
+        if (issuer && !skip) load(stage, kb, t);
+        skip = false;
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    if (!ok) wait_for_copies();
+  };
+
+  if (warp == 0) {
+    // -------------------------------------------------------------- codes ---
+    produce(empty, [&](int stage, int kb, const Unit& t) {
+      const int half = t.n / 2;  // this CTA's tokens: `half` of them from rank * half
+      const int box = half <= 16 ? 16 : half <= 64 ? 64 : 128;
+      const CUtensorMap* map = half <= 16 ? &map_x16 : half <= 64 ? &map_x64 : &map_x128;
+      if (leader) mbar_arrive_expect_tx(&full[stage], 2 * (kWBytes + box * (kDepth / 2)));
+      load_box(sW + stage * kWBytes, &map_w, &full[stage], kb * (kDepth / 2),
+               t.expert * a.N + t.w_tile * kWRows + static_cast<int>(rank) * 128);
+      load_box(sX + stage * kXBytes, map, &full[stage], kb * (kDepth / 2), t.row0 + static_cast<int>(rank) * half);
+    });
+  } else if (leader ? warp == 3 : warp == 1) {
+    // ------------------------------------------------------- block scales ---
+    // A CTA's own weight rows' and all tokens'.  8 rows of 256 bytes are the four atoms of a (row tile, k-block).
+    // A stage's buffers are free once the copies have read them (`full`).
+    const int tile_rows = a.K / 32;
+    produce(full, [&](int stage, int kb, const Unit& t) {
+      const bool two = t.n > 128;
+      if (leader) mbar_arrive_expect_tx(&scales_in[stage], 2 * (two ? 3 : 2) * kScaleTile);
+      load_box(sWS + stage * kScaleTile, &map_w_scales, &scales_in[stage], 0,
+               (t.expert * a.w_scale_tiles + t.w_tile * 2 + static_cast<int>(rank)) * tile_rows + kb * 8);
+      uint8_t* dst = sXS + stage * 2 * kScaleTile;
+      if (two)
+        load_box3(dst, &map_x_scales2, &scales_in[stage], kb * 8, t.row0 / 128);
+      else
+        load_box(dst, &map_x_scales, &scales_in[stage], 0, t.row0 / 128 * tile_rows + kb * 8);
+    });
+  } else if (warp == 1) {
+    // --------------------------------------------------------------- MMAs ---
+    const bool issuer = elect_one();
+    int stage = 0, local = 0;
+    uint32_t phase = 0;
+    const uint32_t utmem = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint64_t w_desc0 = tile_desc(smem_u32(sW)), x_desc0 = tile_desc(smem_u32(sX));
+    bool ready = false;  // the next stage was seen full
+    for (int u = pair; u < units; u += pairs, ++local) {
+      const Unit t = find_unit(u, ends, expert_rows_s, lane);
+      const uint32_t idesc = kIdesc | static_cast<uint32_t>(t.n >> 3) << 17 | (a.mx ? kUE8M0 : 0u);
+      if (!wait(acc_empty, (local & 1) ^ 1u)) { fail(); break; }
+      tc_fence_after();
+      bool ok = true;
+      for (int kb = 0; kb < kblocks; ++kb) {
+        if (!ready && !wait(&full[stage], phase)) { fail(); ok = false; break; }
+        tc_fence_after();
+        const uint32_t ws = utmem + kSfCol + stage * kSfCols, xs = ws + 16;
+        const uint64_t w_desc = w_desc0 + static_cast<uint32_t>(stage) * (kWBytes >> 4);
+        const uint64_t x_desc = x_desc0 + static_cast<uint32_t>(stage) * (kXBytes >> 4);
+        const int next = stage + 1 == kStages ? 0 : stage + 1;
+        const uint32_t next_phase = next ? phase : phase ^ 1u;
+        if (issuer) {
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            pair_mma(utmem, w_desc + 2 * kk, x_desc + 2 * kk, idesc, ws + kk * 4, xs + kk * 8, (kb | kk) != 0);
+          pair_commit(&empty[stage], 0x3);
+        }
+        ready = __all_sync(0xffffffffu, mbar_test_wait(&full[next], next_phase)) != 0;
+        stage = next;
+        phase = next_phase;
+      }
+      if (!ok) break;
+      if (issuer) pair_commit(acc_full, 0x3);
+    }
+    if (issuer) pair_commit(drain, 0x1);
+    mbar_wait_bounded(drain, 0, nullptr);
+  } else if (warp == 2 && leader) {
+    // -------------------------------------------------- scales into TMEM ---
+    const bool issuer = elect_one();
+    int stage = 0;
+    uint32_t phase = 0;
+    const uint32_t utmem = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint64_t ws_desc0 = atom_desc(smem_u32(sWS)), xs_desc0 = atom_desc(smem_u32(sXS));
+    bool ok = true;
+    for (int u = pair; u < units && ok; u += pairs) {
+      const Unit t = find_unit(u, ends, expert_rows_s, lane);
+      for (int kb = 0; kb < kblocks; ++kb) {
+        // The scales have landed, and the MMAs that read this TMEM slot are done.
+        ok = wait(&scales_in[stage], phase) && wait(&empty[stage], phase ^ 1u);
+        if (!ok) { fail(); break; }
+        tc_fence_after();
+        const uint32_t ws = utmem + kSfCol + stage * kSfCols, xs = ws + 16;
+        const uint64_t ws_desc = ws_desc0 + static_cast<uint32_t>(stage) * (kScaleTile >> 4);
+        const uint64_t xs_desc = xs_desc0 + static_cast<uint32_t>(stage) * (2 * kScaleTile >> 4);
+        if (issuer) {
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            pair_copy_scales(ws + kk * 4, ws_desc + kk * (512 >> 4));
+            pair_copy_scales(xs + kk * 8, xs_desc + kk * (512 >> 4));
+            if (t.n > 128) pair_copy_scales(xs + kk * 8 + 4, xs_desc + (kScaleTile + kk * 512) / 16);
+          }
+          pair_commit(&full[stage], 0x3);
+        }
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    if (issuer) pair_commit(drain_copies, 0x1);
+    mbar_wait_bounded(drain_copies, 0, nullptr);
+  } else if (warp >= kEpi0) {
+    // ----------------------------------------------------------- epilogue ---
+    const int quarter = warp & 3, side = (warp - kEpi0) >> 2;
+    const int meeting = 1 + ((warp - kEpi0) >> 1);  // two warps with the 32 outputs of an MXFP4 block
+    uint8_t* buf_ptr = sEpi + (warp - kEpi0) * kEpiBytes;
+    const uint32_t buf = smem_u32(buf_ptr);
+    int local = 0;
+    for (int u = pair; u < units; u += pairs, ++local) {
+      const Unit t = find_unit(u, ends, expert_rows_s, lane);
+      const float scale =
+          a.g_a ? __fmul_rn(__ldg(a.g_a + static_cast<int64_t>(t.expert) * a.g_a_step), __ldg(a.g_w + t.expert)) : 1.0f;
+      // Lane 0 waits and tells, so that the warp stays converged.
+      int ok = 1;
+      if (lane == 0) {
+        ok = !abort_flag && mbar_wait_bounded(acc_full, local & 1, &abort_flag);
+        if (!ok && !abort_flag) fail();
+      }
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      if (kMode == 2) ok = both(meeting, ok != 0);  // the two warps go on or leave together
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t lo[4][16], hi[4][16];
+      const uint32_t taddr = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int token0 = 32 * (2 * i + side);
+        if (token0 < t.tokens) {
+          tmem_ld_fragments(taddr + token0, lo[i]);
+          tmem_ld_fragments(taddr + (16u << 16) + token0, hi[i]);
+        }
+      }
+      tmem_ld_done();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_leader_relaxed(acc_empty);
+      // The next unit's MMAs run while this warp computes and stores.
+      const int n0 = t.w_tile * kWRows + static_cast<int>(rank) * 128 + quarter * 32;
+      if constexpr (kMode == 0) {
+        if (n0 >= a.N) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int token0 = 32 * (2 * i + side);
+          if (token0 < t.tokens) store_rows(a, t, lo[i], hi[i], token0, n0, scale, buf, lane);
+        }
+      } else if constexpr (kMode == 1) {
+        const float g_in = __ldg(a.g_out + static_cast<int64_t>(t.expert) * a.g_out_step);
+        const bool g_ok = g_in > 0.0f && g_in <= FLT_MAX;
+        if (!g_ok && lane == 0) set_status(a.status, NVFP4_ERR_INVALID_ARG);
+        const float g = g_ok ? g_in : 1.0f, six_g = __fmul_rn(6.0f, g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int token0 = 32 * (2 * i + side);
+          if (token0 >= t.tokens) continue;
+          swiglu_fragments(lo[i], hi[i], scale);
+          uint2 codes = make_uint2(0, 0);
+          uint32_t code = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const BlockScale b = block_scale(token_amax(lo[i] + 4 * j, lane), g, six_g);
+            const uint2 c = token_codes(lo[i] + 4 * j, b.mult, lane);
+            if (lane >> 3 == j) {
+              codes = c;
+              code = b.code;
+            }
+          }
+          if (!g_ok) {
+            codes = make_uint2(0, 0);
+            code = 0;
+          }
+          store_codes(a, t, codes, code, token0, n0 >> 1, lane);
+        }
+      } else {
+        float* mine = reinterpret_cast<float*>(buf_ptr);
+        const float* theirs = reinterpret_cast<const float*>(sEpi + ((warp - kEpi0) ^ 1) * kEpiBytes);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int token0 = 32 * (2 * i + side);
+          if (token0 >= t.tokens) continue;
+          swiglu_fragments(lo[i], hi[i], scale);
+          if (a.rotate) {
+            // H_32 / sqrt(32) over the outputs: strides 1, 2, 4 across lanes, 8 in the thread, 16 across the two warps,
+            // in this order, as hadamard32.
+            float h[16];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) h[v] = __uint_as_float(lo[i][v]);
+#pragma unroll
+            for (int s = 4; s < 32; s <<= 1)
+#pragma unroll
+              for (int v = 0; v < 16; ++v) {
+                const float o = __shfl_xor_sync(0xffffffffu, h[v], s);
+                h[v] = lane & s ? __fsub_rn(o, h[v]) : __fadd_rn(h[v], o);
+              }
+#pragma unroll
+            for (int v = 0; v < 16; v += 4)
+#pragma unroll
+              for (int q = 0; q < 2; ++q) {
+                const float x = h[v + q], y = h[v + q + 2];
+                h[v + q] = __fadd_rn(x, y);
+                h[v + q + 2] = __fsub_rn(x, y);
+              }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) mine[32 * v + lane] = h[v];
+            meet(meeting);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+              const float o = theirs[32 * v + lane];
+              h[v] = __fmul_rn(quarter & 1 ? __fsub_rn(o, h[v]) : __fadd_rn(h[v], o), __uint_as_float(kInvSqrt32Bits));
+              lo[i][v] = __float_as_uint(h[v]);
+            }
+            meet(meeting);
+          }
+          float amax[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            amax[j] = token_amax(lo[i] + 4 * j, lane);
+            if (lane < 8) mine[8 * j + lane] = amax[j];
+          }
+          meet(meeting);
+          uint2 codes = make_uint2(0, 0);
+          uint32_t code = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t c = mx_scale_code(fmaxf(amax[j], theirs[8 * j + (lane & 7)]));
+            const uint2 w = token_codes(lo[i] + 4 * j, mx_inv_scale(c), lane);
+            if (lane >> 3 == j) {
+              codes = w;
+              code = c;
+            }
+          }
+          meet(meeting);
+          store_codes(a, t, codes, code, token0, n0 >> 1, lane);
+        }
+      }
+    }
+  }
+
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  if (warp == 1) pair_tmem_free(tmem, kTmemCols);
 }
 
-nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, bool swiglu, cudaStream_t s) {
+// ------------------------------------------------------------------- host ---
+
+PFN_cuTensorMapEncodeTiled_v12000 encoder() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+  });
+  return fn;
+}
+
+bool encode(CUtensorMap* map, const uint8_t* base, uint32_t rank, const cuuint64_t* dims, const cuuint64_t* strides,
+            const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
+  const auto enc = encoder();
+  const cuuint32_t steps[3] = {1, 1, 1};
+  return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, rank, const_cast<uint8_t*>(base), dims, strides, box, steps,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// [rows, K / 2] bytes, boxes of 128 bytes x box_rows.
+bool codes_map(CUtensorMap* map, const uint8_t* base, int64_t rows, int64_t K, uint32_t box_rows) {
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(K / 2), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(K / 2)};
+  const cuuint32_t box[2] = {kDepth / 2, box_rows};
+  return encode(map, base, 2, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// Block scales in the tensor core's order, `tiles` tiles of 128 rows, as rows of 256 bytes, K / 32 of them a tile: boxes of
+// one (tile, k-block), or of two tiles.
+bool scales_map(CUtensorMap* map, const uint8_t* base, int64_t tiles, int64_t K, bool two) {
+  const cuuint64_t tile_rows = static_cast<cuuint64_t>(K / 32), n = static_cast<cuuint64_t>(tiles);
+  const cuuint64_t dims[3] = {256, two ? tile_rows : tile_rows * n, n};
+  const cuuint64_t strides[2] = {256, 256 * tile_rows};
+  const cuuint32_t box[3] = {256, 8, 2};
+  return encode(map, base, two ? 3 : 2, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
+// Pairs of this kernel that are resident at once on the current device, 0 on failure.
+template <int kMode>
+int resident_pairs(cudaLaunchConfig_t cfg) {
+  static std::mutex mu;
+  static std::map<int, int> cache;
+  int d = 0;
+  if (cudaGetDevice(&d) != cudaSuccess) return 0;
+  std::lock_guard<std::mutex> lock(mu);
+  const auto it = cache.find(d);
+  if (it != cache.end()) return it->second;
+  int pairs = 0;
+  cfg.gridDim = dim3(2 * (sm_count() / 2), 1, 1);
+  cfg.numAttrs = 1;  // the cluster's size
+  if (cudaFuncSetAttribute(grouped_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           static_cast<int>(kSmem)) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&pairs, grouped_kernel<kMode>, &cfg) != cudaSuccess || pairs <= 0) {
+    cudaGetLastError();
+    return 0;
+  }
+  cache[d] = pairs;
+  return pairs;
+}
+
+template <int kMode>
+nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s) {
   if (plan->n_tokens == 0) return NVFP4_OK;
   a.row_start = plan->row_start;
   a.rows = plan->rows;
   a.experts = plan->num_experts;
   a.max_rows = static_cast<int>(moe_rows_bound(plan->n_tokens, plan->top_k, plan->num_experts));
+  a.w_tiles = (a.N + kWRows - 1) / kWRows;
+  a.w_scale_tiles = (a.N + 127) / 128;
+  const int64_t choices = plan->n_tokens * plan->top_k, used = choices < a.experts ? choices : a.experts;
+  const int64_t units = (choices + (kTokens - 1) * used) / kTokens * a.w_tiles;  // at most
+  if (units >= (1ll << 31)) return NVFP4_ERR_SHAPE;
+  a.max_units = static_cast<int>(units);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.attrs = attr;
+  const int resident = resident_pairs<kMode>(cfg);
+  if (resident <= 0) return NVFP4_ERR_CUDA;
+  CUtensorMap w, ws, x16, x64, x128, xs, xs2;
+  const int64_t R = a.max_rows, K = a.K;
+  if (!codes_map(&w, a.w_codes, static_cast<int64_t>(a.experts) * a.N, K, 128) ||
+      !scales_map(&ws, a.w_scales, static_cast<int64_t>(a.experts) * a.w_scale_tiles, K, false) ||
+      !codes_map(&x16, a.a_codes, R, K, 16) || !codes_map(&x64, a.a_codes, R, K, 64) ||
+      !codes_map(&x128, a.a_codes, R, K, 128) || !scales_map(&xs, a.a_scales, R / 128, K, false) ||
+      !scales_map(&xs2, a.a_scales, R / 128, K, true))
+    return NVFP4_ERR_CUDA;
   a.status = status_word_dev();
-  const dim3 grid((a.N + kTile - 1) / kTile, a.max_rows / kTile);
-  if (launch_pdl(swiglu ? grouped_simple_kernel<true> : grouped_simple_kernel<false>, grid, dim3(256), 0, s, a) !=
-      cudaSuccess)
+  a.fault_skip_stage = take_fault(NVFP4_FAULT_GEMM_SKIP_STAGE) ? 1 : 0;
+  cfg.gridDim = dim3(static_cast<uint32_t>(2 * (units < resident ? units : resident)), 1, 1);
+  cfg.stream = s;
+  cfg.numAttrs = 2;
+  if (cudaLaunchKernelEx(&cfg, grouped_kernel<kMode>, w, ws, x16, x64, x128, xs, xs2, a) != cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
   return launch_status();
@@ -176,7 +766,8 @@ nvfp4_status check_operands(const moe_plan* plan, const GroupedArgs& a, int64_t 
   if (!a.a_codes || !a.a_scales || !a.w_codes || !a.w_scales || (g && (!a.g_a || !a.g_w))) return NVFP4_ERR_INVALID_ARG;
   if ((a.g_a_step != 0 && a.g_a_step != 1) || (a.g_out_step != 0 && a.g_out_step != 1)) return NVFP4_ERR_INVALID_ARG;
   if (N <= 0 || K <= 0 || N > kMaxSide || K > kMaxSide || K % 256 || N % n_step) return NVFP4_ERR_SHAPE;
-  if (plan->num_experts * ((N + 127) / 128) * (K / 32) >= (1ll << 31) || plan->num_experts * N >= (1ll << 31))
+  if (plan->num_experts * ((N + 127) / 128) * (K / 32) >= (1ll << 31) || plan->num_experts * N >= (1ll << 31) ||
+      moe_rows_bound(plan->n_tokens, plan->top_k, plan->num_experts) / 128 * (K / 32) >= (1ll << 31))
     return NVFP4_ERR_SHAPE;
   if (!aligned(a.a_codes, 16) || !aligned(a.a_scales, 16) || !aligned(a.w_codes, 16) || !aligned(a.w_scales, 16) ||
       !aligned(a.g_a, 4) || !aligned(a.g_w, 4))
@@ -194,7 +785,7 @@ nvfp4_status linear(const moe_plan* plan, GroupedArgs a, int64_t N, int64_t K, v
   a.ldo = ldo;
   a.N = static_cast<int>(N);
   a.K = static_cast<int>(K);
-  return launch_grouped(plan, a, false, static_cast<cudaStream_t>(stream));
+  return launch_grouped<0>(plan, a, static_cast<cudaStream_t>(stream));
 }
 
 nvfp4_status swiglu(const moe_plan* plan, GroupedArgs a, int64_t I, int64_t K, uint8_t* codes, uint8_t* scales,
@@ -207,7 +798,8 @@ nvfp4_status swiglu(const moe_plan* plan, GroupedArgs a, int64_t I, int64_t K, u
   a.q_scales = scales;
   a.N = static_cast<int>(2 * I);
   a.K = static_cast<int>(K);
-  return launch_grouped(plan, a, true, static_cast<cudaStream_t>(stream));
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return a.mx ? launch_grouped<2>(plan, a, s) : launch_grouped<1>(plan, a, s);
 }
 
 GroupedArgs operands(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* w_codes, const uint8_t* w_scales) {
@@ -269,6 +861,6 @@ NVFP4_API nvfp4_status mxfp4_linear_grouped_swiglu_quantize(const moe_plan* plan
   if (rotate != 0 && rotate != 1) return NVFP4_ERR_INVALID_ARG;
   GroupedArgs a = operands(a_codes, a_scales, w_codes, w_scales);
   a.mx = true;
-  a.q_mode = rotate ? 2u : 1u;
+  a.rotate = rotate != 0;
   return swiglu(plan, a, I, K, out_codes, out_scales, stream);
 }

@@ -220,3 +220,32 @@ def test_a_plan_beyond_its_buffers_is_cut_to_them(N):
     linear(N, plan, a, w, guard[:R], 256, 256, False)
     torch.cuda.synchronize()
     assert (guard[R:] == -7).all()
+
+
+@pytest.mark.parametrize("form", ["rows", "nvfp4", "mxfp4", "mxfp4 rotated"])
+def test_a_lost_stage_is_a_timeout_and_the_next_call_is_right(N, form):
+    """The injected fault leaves a stage unloaded: the waits run out (2 s), the status says so, the device stays usable."""
+    plan = M.make_plan(N, M.choices([100, 600], 1, 0), 2)
+    mx = form.startswith("mx")
+    a, w = M.Rows(N, plan, 512, 2, mx), M.Weights(N, 2, 512, 512, 5, mx)
+    out = torch.empty(plan.max_rows, 512, dtype=BF, device="cuda")
+    codes = torch.empty(plan.max_rows, 128, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(plan.max_rows * 16, dtype=torch.uint8, device="cuda")
+
+    def call():
+        if form == "rows":
+            linear(N, plan, a, w, out, 512, 512, False)
+        elif mx:
+            N.mxfp4_linear_grouped_swiglu_quantize(plan, a.codes, a.scales, w.codes, w.scales, 256, 512, codes, scales,
+                                                   rotate=form.endswith("rotated"))
+        else:
+            N.nvfp4_linear_grouped_swiglu_quantize(plan, a.codes, a.scales, a.g, w.codes, w.scales, w.g, 256, 512,
+                                                   torch.tensor([0.02], device="cuda"), codes, scales)
+    N.nvfp4_debug_inject_fault(N.FAULT_GEMM_SKIP_STAGE)
+    call()
+    torch.cuda.synchronize()
+    assert N.nvfp4_get_device_status() == 6
+    if form == "rows":
+        check_linear(N, [100, 600], 512, 512)
+    else:
+        check_swiglu(N, [100, 600], 256, 512, mx, form.endswith("rotated"))
