@@ -80,28 +80,20 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const RouteArg
   int chosen = -1;
   float chosen_l = -kInf;
   for (int j = 0; j < a.top_k; ++j) {
-    uint32_t best = 0;
-    int at = 0;
-    float best_l = -kInf;
+    uint32_t best = key[0];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (key[i] > best) {
-        best = key[i];
-        at = i * 32 + lane;
-        best_l = l[i];
-      }
+    for (int i = 1; i < kPer; ++i) best = max(best, key[i]);
     const uint32_t all = __reduce_max_sync(0xffffffffu, best);
     if (all == 0) break;
-    const uint32_t e = __reduce_min_sync(0xffffffffu, best == all ? static_cast<uint32_t>(at) : 0xffffffffu);
-    const float le = __shfl_sync(0xffffffffu, best_l, e & 31);
+    uint32_t at = 0xffffffffu;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (e == static_cast<uint32_t>(i * 32 + lane)) key[i] = 0;
-    if (lane == j) {
-      chosen = static_cast<int>(e);
-      chosen_l = le;
-    }
+    for (int i = kPer - 1; i >= 0; --i) at = key[i] == all ? i * 32 + lane : at;
+    const uint32_t e = __reduce_min_sync(0xffffffffu, at);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) key[i] = e == static_cast<uint32_t>(i * 32 + lane) ? 0u : key[i];
+    if (lane == j) chosen = static_cast<int>(e);
   }
+  if (chosen >= 0) chosen_l = load_logit(a, t * a.ld + chosen);
   float p;
   if (a.sigmoid) {
     p = chosen >= 0 ? sigmoid_rn(chosen_l) : 0.0f;

@@ -19,11 +19,14 @@ namespace {
 // by match_any), the histograms are summed along the warps, and a second walk
 // gives each pair its rank.  The order is that of the pairs: no atomics.
 // Several chunks: the counts of all of them come from a kernel before it.
+// Latency-bound: up to kSortAlone pairs one CTA walks them in one launch, beyond it
+// chunks are one step of a CTA's warps, which spreads the walk over the SMs until
+// reading all chunks' counts costs more.
 
 constexpr int kSortWarps = 32;
 constexpr int kSortThreads = 32 * kSortWarps;
-constexpr int64_t kSortChunk = 4096;   // pairs of a CTA
-constexpr int64_t kSortMaxChunks = 256;
+constexpr int64_t kSortAlone = 4096;
+constexpr int64_t kSortMaxChunks = 128;
 
 struct SortShape {
   int64_t chunk;  // pairs of a CTA, a multiple of kSortThreads
@@ -31,9 +34,9 @@ struct SortShape {
 };
 SortShape sort_shape(int64_t pairs) {
   SortShape s;
-  s.chunk = kSortChunk;
-  if (pairs > s.chunk * kSortMaxChunks)
-    s.chunk = ((pairs + kSortMaxChunks - 1) / kSortMaxChunks + kSortThreads - 1) / kSortThreads * kSortThreads;
+  const int64_t chunks = pairs <= kSortAlone ? 1 : kSortMaxChunks;
+  s.chunk = ((pairs + chunks - 1) / chunks + kSortThreads - 1) / kSortThreads * kSortThreads;
+  if (s.chunk < kSortThreads) s.chunk = kSortThreads;
   s.chunks = pairs ? (pairs + s.chunk - 1) / s.chunk : 1;
   return s;
 }
@@ -97,20 +100,37 @@ __global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortArgs 
   const int e = threadIdx.x;
   uint32_t total = 0, before = 0;
   if (e < E) {
-    uint32_t run = 0;
+    uint32_t n[kSortWarps], run = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) n[w] = sort_smem[w * E + e];
+#pragma unroll
     for (int w = 0; w < kSortWarps; ++w) {
-      const uint32_t n = sort_smem[w * E + e];
       sort_smem[w * E + e] = run;
-      run += n;
+      run += n[w];
     }
-    if (gridDim.x == 1) {
-      total = run;
-    } else {
+    total = run;
+  }
+  if (gridDim.x > 1) {
+    // The chunks in as many shares as there are threads for.
+    __shared__ uint32_t sums[2][kSortThreads];
+    const uint32_t shares = kSortThreads / E, share = threadIdx.x / E, x = threadIdx.x - share * E;
+    uint32_t all = 0, lower = 0;
+    if (share < shares) {
 #pragma unroll 8
-      for (uint32_t c = 0; c < gridDim.x; ++c) {
-        const uint32_t n = __ldcg(a.counts + c * static_cast<uint64_t>(E) + e);
-        total += n;
-        before += c < blockIdx.x ? n : 0u;
+      for (uint32_t c = share; c < gridDim.x; c += shares) {
+        const uint32_t n = __ldcg(a.counts + c * static_cast<uint64_t>(E) + x);
+        all += n;
+        lower += c < blockIdx.x ? n : 0u;
+      }
+      sums[0][threadIdx.x] = all;
+      sums[1][threadIdx.x] = lower;
+    }
+    __syncthreads();
+    if (e < E) {
+      total = 0;
+      for (uint32_t i = 0; i < shares; ++i) {
+        total += sums[0][i * E + e];
+        before += sums[1][i * E + e];
       }
     }
   }
@@ -123,7 +143,7 @@ __global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortArgs 
   }
   if (lane == 31) warp_sum[warp] = sum;
   __syncthreads();
-  for (int w = 0; w < warp; ++w) sum += warp_sum[w];
+  sum += __reduce_add_sync(0xffffffffu, lane < warp ? warp_sum[lane] : 0u);
   if (e < E) {
     base[e] = sum - padded + before;
     if (blockIdx.x == 0) {
@@ -183,14 +203,17 @@ __device__ __forceinline__ uint4 pack8(const float v[8]) {
 
 struct RowArgs {
   const int32_t* row_of;
-  int top_k;
-  int64_t max_rows;
+  int top_k, max_rows;
   int* status;
 };
-// The row of choice j of token t, or -1.  A plan that names rows outside the buffers has none there.
-__device__ __forceinline__ int64_t row_of(const RowArgs& a, int64_t t, int j) {
-  const int64_t r = __ldg(a.row_of + t * a.top_k + j);
-  return r < a.max_rows ? r : -1;
+constexpr int kBatch = 4;  // choices whose loads are in flight together
+// The rows of choices j0 .. j0 + 3 of token t, or -1.  A plan that names rows outside the buffers has none there.
+__device__ __forceinline__ void rows_of(const RowArgs& a, int64_t t, int j0, int r[kBatch]) {
+#pragma unroll
+  for (int i = 0; i < kBatch; ++i) {
+    r[i] = j0 + i < a.top_k ? __ldg(a.row_of + t * a.top_k + j0 + i) : -1;
+    if (r[i] >= a.max_rows) r[i] = -1;
+  }
 }
 
 __global__ void __launch_bounds__(kWalkThreads)
@@ -200,57 +223,77 @@ __global__ void __launch_bounds__(kWalkThreads)
   walk(w, [&](int64_t t, uint32_t v, bool live) {
     if (!live) return;
     const uint4 in = __ldg(reinterpret_cast<const uint4*>(x + t * ld) + v);
-    for (int j = 0; j < a.top_k; ++j) {
-      const int64_t r = row_of(a, t, j);
-      if (r < 0) continue;
-      uint4 d = in;
-      if (weights) {
-        const float c = __ldg(weights + t * a.top_k + j);
-        float f[8];
-        unpack_bf16x8(in, f);
+    for (int j0 = 0; j0 < a.top_k; j0 += kBatch) {
+      int r[kBatch];
+      rows_of(a, t, j0, r);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] *= c;
-        d = pack8(f);
+      for (int j = 0; j < kBatch; ++j) {
+        if (r[j] < 0) continue;
+        uint4 d = in;
+        if (weights) {
+          const float c = __ldg(weights + t * a.top_k + j0 + j);
+          float f[8];
+          unpack_bf16x8(in, f);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] *= c;
+          d = pack8(f);
+        }
+        reinterpret_cast<uint4*>(out)[static_cast<int64_t>(r[j]) * w.vecs + v] = d;
       }
-      reinterpret_cast<uint4*>(out)[r * w.vecs + v] = d;
     }
   });
 }
 
-// A thread has 16 channels, one NVFP4 block; four lanes have a scale word.
+// Codes and scale word of a thread's 32 channels to the token's rows.
+__device__ __forceinline__ void store_operand(const RowArgs& a, const Walk& w, int64_t t, uint32_t v, uint4 codes,
+                                              uint32_t word, uint4* out_codes, uint8_t* scales) {
+  for (int j0 = 0; j0 < a.top_k; j0 += kBatch) {
+    int r[kBatch];
+    rows_of(a, t, j0, r);
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      if (r[j] < 0) continue;
+      out_codes[static_cast<int64_t>(r[j]) * w.vecs + v] = codes;
+      if ((v & 1) == 0) {
+        const uint64_t off = mma_scale_offset(static_cast<uint64_t>(r[j]), 2 * v, w.vecs >> 1);
+        if (in_bounds(a.status, off + 4 <= static_cast<uint64_t>(a.max_rows) * 2 * w.vecs))
+          *reinterpret_cast<uint32_t*>(scales + off) = word;
+      }
+    }
+  }
+}
+
+// A thread has 32 channels, two NVFP4 blocks; two lanes have a scale word.
 __global__ void __launch_bounds__(kWalkThreads)
     moe_dispatch_nvfp4_kernel(const RowArgs a, const Walk w, const uint16_t* __restrict__ x, int64_t ld,
-                              const float* __restrict__ g_dev, uint2* __restrict__ codes, uint8_t* __restrict__ scales) {
+                              const float* __restrict__ g_dev, uint4* __restrict__ codes, uint8_t* __restrict__ scales) {
   griddep_wait_and_release();
   const float g_in = __ldg(g_dev);
   const bool g_ok = g_in > 0.0f && g_in <= FLT_MAX;
   if (!g_ok && blockIdx.x == 0 && threadIdx.x == 0) set_status(a.status, NVFP4_ERR_INVALID_ARG);
   const float g = g_ok ? g_in : 1.0f, six_g = __fmul_rn(6.0f, g);
   walk(w, [&](int64_t t, uint32_t v, bool live) {
-    const uint4* src = reinterpret_cast<const uint4*>(x + t * ld) + 2 * v;
-    const uint4 lo = live ? __ldg(src) : make_uint4(0, 0, 0, 0), hi = live ? __ldg(src + 1) : make_uint4(0, 0, 0, 0);
-    float f[16];
-    unpack_bf16x8(lo, f);
-    unpack_bf16x8(hi, f + 8);
-    const BlockScale b =
-        block_scale(__uint_as_float(max(amax_bits_bf16x8(lo), amax_bits_bf16x8(hi)) << 16), g, six_g);
+    const uint4* src = reinterpret_cast<const uint4*>(x + t * ld) + 4 * v;
+    uint4 in[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = __fmul_rn(f[i], b.mult);
-    const uint2 c = g_ok ? make_uint2(e2m1x8(f), e2m1x8(f + 8)) : make_uint2(0, 0);
-    uint32_t word = (g_ok ? b.code : 0u) << (8 * (v & 3));
-    word |= __shfl_xor_sync(0xffffffffu, word, 1);
-    word |= __shfl_xor_sync(0xffffffffu, word, 2);
-    if (!live) return;
-    for (int j = 0; j < a.top_k; ++j) {
-      const int64_t r = row_of(a, t, j);
-      if (r < 0) continue;
-      codes[r * w.vecs + v] = c;
-      if ((v & 3) == 0) {
-        const uint64_t off = mma_scale_offset(static_cast<uint64_t>(r), v, w.vecs >> 2);
-        if (in_bounds(a.status, off + 4 <= static_cast<uint64_t>(a.max_rows) * w.vecs))
-          *reinterpret_cast<uint32_t*>(scales + off) = word;
-      }
+    for (int q = 0; q < 4; ++q) in[q] = live ? __ldg(src + q) : make_uint4(0, 0, 0, 0);
+    uint32_t c[4], word = 0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      float f[16];
+      unpack_bf16x8(in[2 * b], f);
+      unpack_bf16x8(in[2 * b + 1], f + 8);
+      const uint32_t top = max(amax_bits_bf16x8(in[2 * b]), amax_bits_bf16x8(in[2 * b + 1]));
+      const BlockScale s = block_scale(__uint_as_float(top << 16), g, six_g);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = __fmul_rn(f[i], s.mult);
+      c[2 * b] = e2m1x8(f);
+      c[2 * b + 1] = e2m1x8(f + 8);
+      word |= s.code << (8 * (2 * (v & 1) + b));
     }
+    word |= __shfl_xor_sync(0xffffffffu, word, 1);
+    if (live) store_operand(a, w, t, v, g_ok ? make_uint4(c[0], c[1], c[2], c[3]) : make_uint4(0, 0, 0, 0),
+                            g_ok ? word : 0u, codes, scales);
   });
 }
 
@@ -276,72 +319,140 @@ __global__ void __launch_bounds__(kWalkThreads)
     const uint4 c = make_uint4(e2m1x8(f), e2m1x8(f + 8), e2m1x8(f + 16), e2m1x8(f + 24));
     uint32_t word = (code | (code << 8)) << (16 * (v & 1));
     word |= __shfl_xor_sync(0xffffffffu, word, 1);
-    if (!live) return;
-    for (int j = 0; j < a.top_k; ++j) {
-      const int64_t r = row_of(a, t, j);
-      if (r < 0) continue;
-      codes[r * w.vecs + v] = c;
-      if ((v & 1) == 0) {
-        const uint64_t off = mma_scale_offset(static_cast<uint64_t>(r), 2 * v, w.vecs >> 1);
-        if (in_bounds(a.status, off + 4 <= static_cast<uint64_t>(a.max_rows) * 2 * w.vecs))
-          *reinterpret_cast<uint32_t*>(scales + off) = word;
+    if (live) store_operand(a, w, t, v, c, word, codes, scales);
+  });
+}
+
+// The sum is in 32 bits, in the order of the choices, rounded once.  A thread has U units of a token, units
+// blockDim.x apart, whose loads of a batch of choices are all in flight.
+template <int U>
+__global__ void __launch_bounds__(512)
+    moe_combine_kernel(const RowArgs a, int64_t tokens, uint32_t vecs, uint32_t per_cta, const uint16_t* __restrict__ y,
+                       const float* __restrict__ weights, const uint16_t* base, int64_t ld_base, uint16_t* out,
+                       int64_t ld_out) {
+  griddep_wait_and_release();
+  const uint32_t sub = per_cta > 1 ? threadIdx.x / vecs : 0u, v0 = threadIdx.x - sub * vecs;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * per_cta + sub;
+  if (sub >= per_cta || t >= tokens) return;
+  float acc[U][8] = {};
+  if (base) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t v = v0 + u * blockDim.x;
+      if (v < vecs) unpack_bf16x8(reinterpret_cast<const uint4*>(base + t * ld_base)[v], acc[u]);  // out may be base
+    }
+  }
+  for (int j0 = 0; j0 < a.top_k; j0 += kBatch) {
+    int r[kBatch];
+    float c[kBatch];
+    uint4 in[kBatch][U];
+    rows_of(a, t, j0, r);
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      c[j] = r[j] < 0 ? 0.0f : weights ? __ldg(weights + t * a.top_k + j0 + j) : 1.0f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t v = v0 + u * blockDim.x;
+        if (r[j] >= 0 && v < vecs)
+          in[j][u] = __ldg(reinterpret_cast<const uint4*>(y) + static_cast<int64_t>(r[j]) * vecs + v);
       }
     }
-  });
-}
-
-// The sum is in 32 bits, in the order of the choices, rounded once.
-__global__ void __launch_bounds__(kWalkThreads)
-    moe_combine_kernel(const RowArgs a, const Walk w, const uint16_t* __restrict__ y, const float* __restrict__ weights,
-                       const uint16_t* base, int64_t ld_base, uint16_t* out, int64_t ld_out) {
-  griddep_wait_and_release();
-  walk(w, [&](int64_t t, uint32_t v, bool live) {
-    if (!live) return;
-    float acc[8] = {};
-    if (base) unpack_bf16x8(reinterpret_cast<const uint4*>(base + t * ld_base)[v], acc);  // not __ldg: out may be base
-    for (int j = 0; j < a.top_k; ++j) {
-      const int64_t r = row_of(a, t, j);
-      if (r < 0) continue;
-      const float c = weights ? __ldg(weights + t * a.top_k + j) : 1.0f;
-      float f[8];
-      unpack_bf16x8(__ldg(reinterpret_cast<const uint4*>(y) + r * w.vecs + v), f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] = fmaf(c, f[i], acc[i]);
+    for (int j = 0; j < kBatch; ++j) {
+      if (r[j] < 0) continue;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float f[8];
+        unpack_bf16x8(in[j][u], f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[u][i] = fmaf(c[j], f[i], acc[u][i]);
+      }
     }
-    reinterpret_cast<uint4*>(out + t * ld_out)[v] = pack8(acc);
-  });
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint32_t v = v0 + u * blockDim.x;
+    if (v < vecs) reinterpret_cast<uint4*>(out + t * ld_out)[v] = pack8(acc[u]);
+  }
 }
 
-// A warp has a token.
+template <int U>
+cudaError_t launch_combine(const RowArgs& a, int64_t tokens, uint32_t vecs, const void* y, const float* weights,
+                           const void* base, int64_t ld_base, void* out, int64_t ld_out, cudaStream_t s) {
+  const uint32_t threads = ((vecs + U - 1) / U + 31) / 32 * 32;
+  uint32_t per_cta = 1, cta = threads;
+  if (U == 1 && vecs < 128) {  // several short tokens
+    per_cta = 256 / vecs;
+    cta = 256;
+  }
+  return launch_pdl(moe_combine_kernel<U>, dim3(static_cast<uint32_t>((tokens + per_cta - 1) / per_cta)), dim3(cta), 0, s,
+                    a, tokens, vecs, per_cta, static_cast<const uint16_t*>(y), weights,
+                    static_cast<const uint16_t*>(base), ld_base, static_cast<uint16_t*>(out), ld_out);
+}
+
+// kWarps warps have a token, a batch of choices at a time: one load of d_out serves the batch.  More warps where the
+// tokens are few; their parts of a sum are added in order.
+template <int kWarps>
 __global__ void __launch_bounds__(kWalkThreads)
     moe_combine_backward_kernel(const RowArgs a, int64_t tokens, uint32_t vecs, const uint16_t* __restrict__ d_out,
                                 int64_t ld, const uint16_t* __restrict__ y, const float* __restrict__ weights,
                                 uint16_t* __restrict__ d_y, float* __restrict__ d_weights) {
+  constexpr int kPer = kWalkThreads / 32 / kWarps;  // tokens of a CTA
+  __shared__ float parts[kWarps > 1 ? kMoeMaxTopK : 1][kPer][kWarps];
   griddep_wait_and_release();
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * (kWalkThreads / 32) + (threadIdx.x >> 5);
+  const int warp = threadIdx.x >> 5, sub = warp / kWarps, part = warp % kWarps;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * kPer + sub;
   const uint32_t lane = threadIdx.x & 31;
-  if (t >= tokens) return;
+  const bool live = t < tokens;
   const uint4* g4 = reinterpret_cast<const uint4*>(d_out + t * ld);
-  for (int j = 0; j < a.top_k; ++j) {
-    const int64_t r = row_of(a, t, j);
-    float dot = 0.0f;
-    if (r >= 0) {
-      const float c = __ldg(weights + t * a.top_k + j);
-      for (uint32_t v = lane; v < vecs; v += 32) {
-        float g[8], f[8];
-        unpack_bf16x8(__ldg(g4 + v), g);
-        unpack_bf16x8(__ldg(reinterpret_cast<const uint4*>(y) + r * vecs + v), f);
+  for (int j0 = 0; live && j0 < a.top_k; j0 += kBatch) {
+    int r[kBatch];
+    float c[kBatch], dot[kBatch] = {};
+    rows_of(a, t, j0, r);
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) c[j] = r[j] >= 0 ? __ldg(weights + t * a.top_k + j0 + j) : 0.0f;
+#pragma unroll 2
+    for (uint32_t v = part * 32 + lane; v < vecs; v += 32 * kWarps) {
+      const uint4 gv = __ldg(g4 + v);
+      uint4 in[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (r[j] >= 0) in[j] = __ldg(reinterpret_cast<const uint4*>(y) + static_cast<int64_t>(r[j]) * vecs + v);
+      float g[8];
+      unpack_bf16x8(gv, g);
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        if (r[j] < 0) continue;
+        float f[8];
+        unpack_bf16x8(in[j], f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          dot = fmaf(g[i], f[i], dot);
-          g[i] *= c;
+          dot[j] = fmaf(g[i], f[i], dot[j]);
+          f[i] = g[i] * c[j];
         }
-        if (d_y) reinterpret_cast<uint4*>(d_y)[r * vecs + v] = pack8(g);
+        if (d_y) reinterpret_cast<uint4*>(d_y)[static_cast<int64_t>(r[j]) * vecs + v] = pack8(f);
       }
     }
 #pragma unroll
-    for (int s = 16; s; s >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, s);
-    if (d_weights && lane == 0) d_weights[t * a.top_k + j] = dot;
+    for (int j = 0; j < kBatch; ++j) {
+#pragma unroll
+      for (int s = 16; s; s >>= 1) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], s);
+      if (lane == 0 && j0 + j < a.top_k) {
+        if constexpr (kWarps > 1)
+          parts[j0 + j][sub][part] = dot[j];
+        else if (d_weights)
+          d_weights[t * a.top_k + j0 + j] = dot[j];
+      }
+    }
+  }
+  if constexpr (kWarps > 1) {
+    __syncthreads();
+    if (d_weights && live && part == 0 && static_cast<int>(lane) < a.top_k) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) sum += parts[lane][sub][w];
+      d_weights[t * a.top_k + lane] = sum;
+    }
   }
 }
 
@@ -349,7 +460,7 @@ RowArgs row_args(const moe_plan* p) {
   RowArgs a;
   a.row_of = p->row_of;
   a.top_k = p->top_k;
-  a.max_rows = moe_rows_bound(p->n_tokens, p->top_k, p->num_experts);
+  a.max_rows = static_cast<int>(moe_rows_bound(p->n_tokens, p->top_k, p->num_experts));
   a.status = status_word_dev();
   return a;
 }
@@ -439,10 +550,10 @@ NVFP4_API nvfp4_status moe_dispatch_nvfp4(const moe_plan* plan, const void* x_bf
   if (plan->n_tokens == 0) return NVFP4_OK;
   if (!x_bf16 || !g_dev || !codes || !scales) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(x_bf16, 16) || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(g_dev, 4)) return NVFP4_ERR_ALIGN;
-  const Walk w = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 16));
+  const Walk w = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 32));
   if (launch_pdl(moe_dispatch_nvfp4_kernel, dim3(walk_grid(w)), dim3(kWalkThreads), 0,
                  static_cast<cudaStream_t>(stream), row_args(plan), w, static_cast<const uint16_t*>(x_bf16), ld_x,
-                 g_dev, reinterpret_cast<uint2*>(codes), scales) != cudaSuccess)
+                 g_dev, reinterpret_cast<uint4*>(codes), scales) != cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
   return launch_status();
@@ -478,11 +589,11 @@ NVFP4_API nvfp4_status moe_combine(const moe_plan* plan, const void* y_bf16, int
   if (!aligned(y_bf16, 16) || !aligned(out_bf16, 16) || !aligned(base_bf16, 16) || !aligned(weights, 4) ||
       (base_bf16 && ld_base % 8))
     return NVFP4_ERR_ALIGN;
-  const Walk w = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 8));
-  if (launch_pdl(moe_combine_kernel, dim3(walk_grid(w)), dim3(kWalkThreads), 0, static_cast<cudaStream_t>(stream),
-                 row_args(plan), w, static_cast<const uint16_t*>(y_bf16), weights,
-                 static_cast<const uint16_t*>(base_bf16), ld_base, static_cast<uint16_t*>(out_bf16), ld_out) !=
-      cudaSuccess)
+  const uint32_t vecs = static_cast<uint32_t>(cols / 8);
+  const auto launch = vecs <= 256 ? launch_combine<1>
+                      : vecs <= 1024 ? launch_combine<2> : vecs <= 2048 ? launch_combine<4> : launch_combine<16>;
+  if (launch(row_args(plan), plan->n_tokens, vecs, y_bf16, weights, base_bf16, ld_base, out_bf16, ld_out,
+             static_cast<cudaStream_t>(stream)) != cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
   return launch_status();
@@ -499,8 +610,13 @@ NVFP4_API nvfp4_status moe_combine_backward(const moe_plan* plan, const void* d_
   if (!aligned(d_out_bf16, 16) || !aligned(y_bf16, 16) || !aligned(d_y_bf16, 16) || !aligned(weights, 4) ||
       !aligned(d_weights, 4))
     return NVFP4_ERR_ALIGN;
-  const int64_t grid = (plan->n_tokens + kWalkThreads / 32 - 1) / (kWalkThreads / 32);
-  if (launch_pdl(moe_combine_backward_kernel, dim3(static_cast<uint32_t>(grid)), dim3(kWalkThreads), 0,
+  // Eight warps a token until one warp each fills the GPU.
+  const int64_t slots = static_cast<int64_t>(sm_count()) * 32;
+  const int warps = plan->n_tokens >= slots ? 1 : 4 * plan->n_tokens >= slots ? 4 : 8;
+  const auto kernel = warps == 1 ? moe_combine_backward_kernel<1>
+                      : warps == 4 ? moe_combine_backward_kernel<4> : moe_combine_backward_kernel<8>;
+  const int64_t per = kWalkThreads / 32 / warps, grid = (plan->n_tokens + per - 1) / per;
+  if (launch_pdl(kernel, dim3(static_cast<uint32_t>(grid)), dim3(kWalkThreads), 0,
                  static_cast<cudaStream_t>(stream), row_args(plan), plan->n_tokens, static_cast<uint32_t>(cols / 8),
                  static_cast<const uint16_t*>(d_out_bf16), ld_d_out, static_cast<const uint16_t*>(y_bf16), weights,
                  static_cast<uint16_t*>(d_y_bf16), d_weights) != cudaSuccess)

@@ -672,16 +672,21 @@ class MoEPlan:
         self.max_rows = moe_max_rows(n_tokens, top_k, num_experts)
         if self.max_rows == 0 and n_tokens != 0:
             raise ValueError("n_tokens, top_k or num_experts out of range")
-        self.row_start = torch.zeros(num_experts + 1, dtype=torch.int32, device=device)
-        self.rows = torch.zeros(num_experts, dtype=torch.int32, device=device)
-        self.row_of = torch.full((n_tokens, top_k), -1, dtype=torch.int32, device=device)
+        self._arrays = (torch.zeros(num_experts + 1, dtype=torch.int32, device=device),
+                        torch.zeros(num_experts, dtype=torch.int32, device=device),
+                        torch.full((n_tokens, top_k), -1, dtype=torch.int32, device=device))
         size = moe_sort_workspace_size(n_tokens, top_k, num_experts)
         self.workspace = torch.empty(size, dtype=torch.uint8, device=device) if size else None
+        self._packed = _PLAN.pack(*(t.data_ptr() for t in self._arrays), n_tokens, top_k, num_experts)
+
+    # The arrays are the plan's own for its life: their addresses are packed once.
+    row_start = property(lambda self: self._arrays[0])
+    rows = property(lambda self: self._arrays[1])
+    row_of = property(lambda self: self._arrays[2])
 
     def packed(self):
         """The moe_plan's bytes, for the calls that take it packed."""
-        return _PLAN.pack(self.row_start.data_ptr(), self.rows.data_ptr(), self.row_of.data_ptr(), self.n_tokens,
-                          self.top_k, self.num_experts)
+        return self._packed
 
 
 EXPORTED = ["nvfp4_scales_bytes", "nvfp4_tensor_scale", "nvfp4_quantize", "nvfp4_quantize_dynamic", "nvfp4_scales_relayout", "nvfp4_linear",
