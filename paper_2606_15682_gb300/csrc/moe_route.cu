@@ -34,11 +34,49 @@ struct RouteArgs {
   bool bf16, sigmoid, renormalize;
 };
 
-// A logit; -inf in place of NaN.
+template <bool kBf16>
 __device__ __forceinline__ float load_logit(const RouteArgs& a, int64_t at) {
-  const float l = a.bf16 ? __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t*>(a.logits) + at)) << 16)
-                         : __ldg(static_cast<const float*>(a.logits) + at);
-  return l == l ? l : -kInf;
+  if (kBf16) return __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t*>(a.logits) + at)) << 16);
+  return __ldg(static_cast<const float*>(a.logits) + at);
+}
+
+// A lane's experts: 4 in a row of every 128, in wide loads, or (kWide false: rows that are not aligned for them) every 32nd.
+template <bool kWide>
+__device__ __forceinline__ int expert_at(int i, int lane) {
+  return kWide ? (i >> 2) * 128 + 4 * lane + (i & 3) : 32 * i + lane;
+}
+// The lane's logits of token t: -inf in place of NaN and behind the last expert.
+template <int kPer, bool kBf16, bool kWide>
+__device__ __forceinline__ void load_logits(const RouteArgs& a, int64_t t, int lane, float l[kPer]) {
+  const int64_t row = t * a.ld;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) l[i] = -kInf;
+  if constexpr (kWide) {
+#pragma unroll
+    for (int i = 0; i < kPer; i += 4) {
+      const int e = 32 * i + 4 * lane;  // the experts are a multiple of 4
+      if (e >= a.experts) continue;
+      if constexpr (kBf16) {
+        const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.logits) + row + e));
+        l[i] = __uint_as_float(v.x << 16);
+        l[i + 1] = __uint_as_float(v.x & 0xFFFF0000u);
+        l[i + 2] = __uint_as_float(v.y << 16);
+        l[i + 3] = __uint_as_float(v.y & 0xFFFF0000u);
+      } else {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(a.logits) + row + e));
+        l[i] = v.x;
+        l[i + 1] = v.y;
+        l[i + 2] = v.z;
+        l[i + 3] = v.w;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (32 * i + lane < a.experts) l[i] = load_logit<kBf16>(a, row + 32 * i + lane);
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) l[i] = fmaxf(l[i], -kInf);  // the number where the other is NaN
 }
 
 // Each operation rounded to nearest: the choice under a bias is by these 32 bits.
@@ -47,53 +85,107 @@ __device__ __forceinline__ float sigmoid_rn(float l) { return __frcp_rn(__fadd_r
 // e^(l - m), also where both are infinite.
 __device__ __forceinline__ float exp_below(float l, float m) { return l == m ? 1.0f : __expf(l - m); }
 
+__device__ __forceinline__ uint32_t pack_rn(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int s = 16; s; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
   return v;
 }
 
-// Unsigned integers in the order of the floats, both zeros alike; 0 for -inf and NaN: no choice.
-__device__ __forceinline__ uint32_t order_key(float f) {
-  if (!(f > -kInf)) return 0;
-  const uint32_t b = __float_as_uint(f + 0.0f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+// The largest of the warp's numbers (no NaN).
+__device__ __forceinline__ float warp_max(float v) {
+  float m;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+  return m;
 }
 
-template <int kPer>
+// Keys are numbers, -inf those of experts that are not to be chosen; equal ones (both zeros are) go to the lowest expert.
+// One choice after another: the largest key of the warp, of the lowest expert that has it.
+template <int kPer, bool kWide>
+__device__ __forceinline__ int choose_in_turn(float key[kPer], int top_k, int lane) {
+  int chosen = -1;
+  for (int j = 0; j < top_k; ++j) {
+    float best = key[0];
+#pragma unroll
+    for (int i = 1; i < kPer; ++i) best = fmaxf(best, key[i]);
+    const float all = warp_max(best);
+    if (!(all > -kInf)) break;
+    uint32_t at = 0xffffffffu;
+#pragma unroll
+    for (int i = kPer - 1; i >= 0; --i) at = key[i] == all ? expert_at<kWide>(i, lane) : at;
+    const uint32_t e = __reduce_min_sync(0xffffffffu, at);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) key[i] = e == static_cast<uint32_t>(expert_at<kWide>(i, lane)) ? -kInf : key[i];
+    if (lane == j) chosen = static_cast<int>(e);
+  }
+  return chosen;
+}
+
+// The same with fewer steps: the top_k-th largest of the lanes' own maxima is at most the top_k-th largest key, so few
+// keys reach it; those are gathered, one a lane, and chosen in turn.  More than 32 (many equal keys), or fewer lanes with
+// a key than top_k: all in turn.  list: [32] of the warp.
+template <int kPer, bool kWide>
+__device__ __forceinline__ int choose(float key[kPer], int top_k, int lane, float2* list) {
+  if constexpr (kPer == 1) return choose_in_turn<kPer, kWide>(key, top_k, lane);
+  float best = key[0];
+#pragma unroll
+  for (int i = 1; i < kPer; ++i) best = fmaxf(best, key[i]);
+  float least = -kInf;
+  for (int j = 0; j < top_k; ++j) {
+    least = warp_max(best);
+    best = best == least ? -kInf : best;
+  }
+  int n = 0;
+  const uint32_t lower = (1u << lane) - 1;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const bool in = key[i] >= least;
+    const uint32_t vote = __ballot_sync(0xffffffffu, in);
+    const int at = n + __popc(vote & lower);
+    if (in && at < 32) list[at] = make_float2(key[i], __int_as_float(expert_at<kWide>(i, lane)));
+    n += __popc(vote);
+  }
+  if (!(least > -kInf) || n > 32) return choose_in_turn<kPer, kWide>(key, top_k, lane);
+  __syncwarp();
+  const float2 mine = list[min(lane, n - 1)];
+  float k = lane < n ? mine.x : -kInf;
+  const uint32_t expert = __float_as_uint(mine.y);
+  int chosen = -1;
+  for (int j = 0; j < top_k; ++j) {
+    const float all = warp_max(k);
+    const uint32_t e = __reduce_min_sync(0xffffffffu, k == all ? expert : 0xffffffffu);
+    k = expert == e ? -kInf : k;
+    if (lane == j) chosen = static_cast<int>(e);
+  }
+  return chosen;
+}
+
+template <int kPer, bool kBf16, bool kWide>
 __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const RouteArgs a) {
+  __shared__ float2 lists[kRouteThreads / 32][32];
   griddep_wait_and_release();
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (kRouteThreads / 32) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (t >= a.tokens) return;
-  float l[kPer];
-  uint32_t key[kPer];
-  float top = -kInf;
+  float l[kPer], key[kPer];
+  load_logits<kPer, kBf16, kWide>(a, t, lane, l);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int e = i * 32 + lane;
-    l[i] = e < a.experts ? load_logit(a, t * a.ld + e) : -kInf;
-    key[i] = order_key(!a.bias || !(l[i] > -kInf) ? l[i] : __fadd_rn(sigmoid_rn(l[i]), __ldg(a.bias + e)));
-    top = fmaxf(top, l[i]);
+  for (int i = 0; i < kPer; ++i) key[i] = l[i];
+  if (a.bias) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = expert_at<kWide>(i, lane);
+      if (l[i] > -kInf) key[i] = fmaxf(__fadd_rn(sigmoid_rn(l[i]), __ldg(a.bias + e)), -kInf);  // not NaN
+    }
   }
   // Lane j: choice j and its logit.
-  int chosen = -1;
-  float chosen_l = -kInf;
-  for (int j = 0; j < a.top_k; ++j) {
-    uint32_t best = key[0];
-#pragma unroll
-    for (int i = 1; i < kPer; ++i) best = max(best, key[i]);
-    const uint32_t all = __reduce_max_sync(0xffffffffu, best);
-    if (all == 0) break;
-    uint32_t at = 0xffffffffu;
-#pragma unroll
-    for (int i = kPer - 1; i >= 0; --i) at = key[i] == all ? i * 32 + lane : at;
-    const uint32_t e = __reduce_min_sync(0xffffffffu, at);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) key[i] = e == static_cast<uint32_t>(i * 32 + lane) ? 0u : key[i];
-    if (lane == j) chosen = static_cast<int>(e);
-  }
-  if (chosen >= 0) chosen_l = load_logit(a, t * a.ld + chosen);
+  const int chosen = choose<kPer, kWide>(key, a.top_k, lane, lists[threadIdx.x >> 5]);
+  const float chosen_l = chosen >= 0 ? load_logit<kBf16>(a, t * a.ld + chosen) : -kInf;
   float p;
   if (a.sigmoid) {
     p = chosen >= 0 ? sigmoid_rn(chosen_l) : 0.0f;
@@ -102,8 +194,7 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const RouteArg
       p = total > 0.0f ? p / total : 0.0f;
     }
   } else {
-#pragma unroll
-    for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+    const float top = __shfl_sync(0xffffffffu, chosen_l, 0);  // the first choice's
     p = chosen >= 0 ? exp_below(chosen_l, top) : 0.0f;
     float total = 0.0f;
     if (a.renormalize) {
@@ -121,7 +212,7 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const RouteArg
   }
 }
 
-template <int kPer>
+template <int kPer, bool kBf16, bool kWide>
 __global__ void __launch_bounds__(kRouteThreads) moe_route_backward_kernel(const RouteArgs a) {
   __shared__ float rows[kRouteThreads / 32][kPer * 32];
   griddep_wait_and_release();
@@ -130,13 +221,12 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_backward_kernel(const
   if (t >= a.tokens) return;
   float* row = rows[threadIdx.x >> 5];
   float l[kPer];
+  load_logits<kPer, kBf16, kWide>(a, t, lane, l);
   float top = -kInf;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int e = i * 32 + lane;
-    l[i] = e < a.experts ? load_logit(a, t * a.ld + e) : -kInf;
     top = fmaxf(top, l[i]);
-    row[e] = l[i];
+    row[expert_at<kWide>(i, lane)] = l[i];
   }
   __syncwarp();
   // Lane j: choice j, its D and its logit.
@@ -150,7 +240,7 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_backward_kernel(const
   }
   __syncwarp();
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) row[i * 32 + lane] = 0.0f;
+  for (int i = 0; i < kPer; ++i) row[expert_at<kWide>(i, lane)] = 0.0f;
   __syncwarp();
   float p, spread = 0.0f;  // spread: what softmax without norming takes off all experts
   float total = 0.0f;
@@ -166,8 +256,7 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_backward_kernel(const
       D = D * p * q;
     }
   } else {
-#pragma unroll
-    for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+    top = warp_max(top);
     p = e >= 0 ? exp_below(le, top) : 0.0f;
     if (a.renormalize) {
       total = warp_sum(p);
@@ -194,28 +283,45 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_backward_kernel(const
     row[e] = D;
   }
   __syncwarp();
+  float d[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int x = i * 32 + lane;
+    d[i] = row[expert_at<kWide>(i, lane)];
+    if (!a.sigmoid && !a.renormalize && l[i] > -kInf) d[i] -= exp_below(l[i], top) * spread;
+  }
+  const int64_t out = t * a.experts;
+#pragma unroll
+  for (int i = 0; i < kPer; i += kWide ? 4 : 1) {
+    const int x = expert_at<kWide>(i, lane);
     if (x >= a.experts) continue;
-    float d = row[x];
-    if (!a.sigmoid && !a.renormalize && l[i] > -kInf) d -= exp_below(l[i], top) * spread;
-    const int64_t at = t * a.experts + x;
-    if (a.bf16) {
-      uint16_t b;
-      asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(b) : "f"(d));
-      static_cast<uint16_t*>(a.d_logits)[at] = b;
+    if constexpr (kWide && kBf16) {
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.d_logits) + out + x) =
+          make_uint2(pack_rn(d[i], d[i + 1]), pack_rn(d[i + 2], d[i + 3]));
+    } else if constexpr (kWide) {
+      *reinterpret_cast<float4*>(static_cast<float*>(a.d_logits) + out + x) =
+          make_float4(d[i], d[i + 1], d[i + 2], d[i + 3]);
+    } else if constexpr (kBf16) {
+      static_cast<uint16_t*>(a.d_logits)[out + x] = static_cast<uint16_t>(pack_rn(d[i], 0.0f));
     } else {
-      static_cast<float*>(a.d_logits)[at] = d;
+      static_cast<float*>(a.d_logits)[out + x] = d[i];
     }
   }
 }
 
-template <int kPer>
+template <int kPer, bool kBf16, bool kWide>
 cudaError_t launch_route(const RouteArgs& a, cudaStream_t s) {
   const dim3 grid(static_cast<uint32_t>((a.tokens + kRouteThreads / 32 - 1) / (kRouteThreads / 32)));
-  return launch_pdl(a.d_logits ? moe_route_backward_kernel<kPer> : moe_route_kernel<kPer>, grid, dim3(kRouteThreads), 0,
-                    s, a);
+  return launch_pdl(a.d_logits ? moe_route_backward_kernel<kPer, kBf16, kWide> : moe_route_kernel<kPer, kBf16, kWide>,
+                    grid, dim3(kRouteThreads), 0, s, a);
+}
+template <int kPer>
+cudaError_t launch_route(const RouteArgs& a, cudaStream_t s) {
+  if constexpr (kPer >= 4) {
+    const uintptr_t wide = a.bf16 ? 8 : 16;
+    if (a.experts % 4 == 0 && a.ld % 4 == 0 && aligned(a.logits, wide) && aligned(a.d_logits, wide))
+      return a.bf16 ? launch_route<kPer, true, true>(a, s) : launch_route<kPer, false, true>(a, s);
+  }
+  return a.bf16 ? launch_route<kPer, true, false>(a, s) : launch_route<kPer, false, false>(a, s);
 }
 
 nvfp4_status route(const moe_route_options* o, const void* logits, int32_t type, int64_t ld, int64_t n_tokens,

@@ -14,30 +14,40 @@ namespace nvfp4 {
 namespace {
 
 // ------------------------------------------------------------------ sort ---
-// A CTA of 32 warps places a chunk of pairs: each warp counts its segment's
-// experts in a histogram of its own (lanes with the same expert find each other
-// by match_any), the histograms are summed along the warps, and a second walk
-// gives each pair its rank.  The order is that of the pairs: no atomics.
-// Several chunks: the counts of all of them come from a kernel before it.
-// Latency-bound: up to kSortAlone pairs one CTA walks them in one launch, beyond it
-// chunks are one step of a CTA's warps, which spreads the walk over the SMs until
-// reading all chunks' counts costs more.
+// A CTA of 32 warps places a chunk of pairs.  Each warp ranks its segment's pairs
+// among those of the same expert (lanes with the same expert find each other by
+// votes; a histogram in shared memory has what came before), the warps' counts
+// are summed, and a pair's row is its expert's first row + the pairs of earlier
+// chunks + of earlier warps + its rank.  The order is that of the pairs: no atomics
+// decide it.  Latency-bound, so the chunks' counts travel the shortest way: none for
+// up to 2048 pairs (one CTA), through the shared memory of a cluster of 8 CTAs for up
+// to 32768, beyond it through global memory from a kernel before (131072 pairs: in the
+// cluster 16 us, a few SMs' issue slots).
 
 constexpr int kSortWarps = 32;
 constexpr int kSortThreads = 32 * kSortWarps;
-constexpr int64_t kSortAlone = 4096;
-constexpr int64_t kSortMaxChunks = 128;
+constexpr int kSortSteps = 16;  // steps of a warp over its segment, at most
+constexpr int64_t kSortAlone = 2048;
+constexpr int kSortCluster = 8;
+constexpr int64_t kSortClustered = 32768;
+constexpr int64_t kSortSpread = 64;  // CTAs of kChunks, until a chunk is kSortChunk
+constexpr int64_t kSortChunk = kSortSteps * kSortThreads;
 
+enum SortForm { kAlone, kCluster, kChunks };
 struct SortShape {
+  SortForm form;
   int64_t chunk;  // pairs of a CTA, a multiple of kSortThreads
   int64_t chunks;
 };
 SortShape sort_shape(int64_t pairs) {
+  auto up = [](int64_t n) { return (n + kSortThreads - 1) / kSortThreads * kSortThreads; };
   SortShape s;
-  const int64_t chunks = pairs <= kSortAlone ? 1 : kSortMaxChunks;
-  s.chunk = ((pairs + chunks - 1) / chunks + kSortThreads - 1) / kSortThreads * kSortThreads;
-  if (s.chunk < kSortThreads) s.chunk = kSortThreads;
-  s.chunks = pairs ? (pairs + s.chunk - 1) / s.chunk : 1;
+  s.form = pairs <= kSortAlone ? kAlone : pairs <= kSortClustered ? kCluster : kChunks;
+  const int64_t ctas = s.form == kAlone ? 1 : s.form == kCluster ? kSortCluster : kSortSpread;
+  s.chunk = up((pairs + ctas - 1) / ctas);
+  if (s.chunk == 0) s.chunk = kSortThreads;
+  if (s.chunk > kSortChunk) s.chunk = kSortChunk;
+  s.chunks = s.form == kChunks ? (pairs + s.chunk - 1) / s.chunk : ctas;
   return s;
 }
 
@@ -46,7 +56,7 @@ struct SortArgs {
   int32_t* row_start;
   int32_t* rows;
   int32_t* row_of;
-  uint32_t* counts;  // [chunks, experts], with more than one chunk
+  uint32_t* counts;  // [chunks, experts] of kChunks
   int64_t pairs, chunk;
   int experts;
   int* status;
@@ -77,45 +87,97 @@ __global__ void __launch_bounds__(kSortThreads) moe_count_kernel(const SortArgs 
     a.counts[blockIdx.x * static_cast<uint64_t>(a.experts) + e] = hist[e];
 }
 
+__device__ __forceinline__ uint32_t ld_cluster_u32(const uint32_t* p, uint32_t rank) {
+  uint32_t at, v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+
+// The lanes with this lane's expert, -1 counting as one: a vote for each of its bits and the sign.  (match_any takes some
+// 60 cycles of a unit that all warps of an SM share: 131072 pairs on 8 SMs 19.5 us.)
+__device__ __forceinline__ uint32_t same_expert(int e, int bits) {
+  const uint32_t some = __ballot_sync(0xffffffffu, e >= 0);
+  uint32_t peers = e >= 0 ? some : ~some;
+  for (int b = 0; b < bits; ++b) {
+    const bool on = e >> b & 1;
+    const uint32_t vote = __ballot_sync(0xffffffffu, on);
+    peers &= on ? vote : ~vote;
+  }
+  return peers;
+}
+
+template <SortForm kForm>
 __global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortArgs a) {
-  extern __shared__ uint32_t sort_smem[];  // [warps, experts] counts, then places; [experts] first rows
+  constexpr int kSteps = kForm == kAlone ? static_cast<int>(kSortAlone / kSortThreads) : kSortSteps;
+  extern __shared__ uint32_t sort_smem[];  // [warps, experts] counts, then places; [experts] first rows; [experts] counts
   __shared__ uint32_t warp_sum[kSortWarps];
-  griddep_wait_and_release();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = a.experts;
   uint32_t* hist = sort_smem + warp * E;
   uint32_t* base = sort_smem + kSortWarps * E;
+  uint32_t* count = base + E;
   for (int i = threadIdx.x; i < kSortWarps * E; i += kSortThreads) sort_smem[i] = 0;
-  __syncthreads();
+  griddep_wait_and_release();
   const int64_t chunk_end = min((blockIdx.x + 1) * a.chunk, a.pairs);
-  const int64_t begin = blockIdx.x * a.chunk + warp * (a.chunk / kSortWarps);
-  const int64_t end = min(begin + a.chunk / kSortWarps, chunk_end);
-  for (int64_t i = begin; i < end; i += 32) {
-    const int e = expert_of(a, i + lane, end);
-    const uint32_t peers = __match_any_sync(0xffffffffu, e);
-    if (e >= 0 && (peers & ((1u << lane) - 1)) == 0) hist[e] += __popc(peers);
+  const int64_t begin = blockIdx.x * a.chunk + warp * (a.chunk / kSortWarps) + lane;
+  const int steps = static_cast<int>(a.chunk / kSortThreads), bits = 32 - __clz(E - 1);
+  int at[kSteps];  // a pair's expert, and then its rank among the warp's << 10 | expert; -1: none
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) at[i] = i < steps ? expert_of(a, begin + 32 * i, chunk_end) : -1;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    if (i >= steps) break;
+    const int e = at[i];
+    const uint32_t peers = same_expert(e, bits), lower = peers & ((1u << lane) - 1);
+    uint32_t before = 0;
+    if (e >= 0) before = hist[e];
+    __syncwarp();
+    if (e >= 0) {
+      if (lower == 0) hist[e] = before + __popc(peers);
+      at[i] = static_cast<int>((before + __popc(lower)) << 10) | e;
+    }
     __syncwarp();
   }
   __syncthreads();
-  // Thread e: expert e's rows in this chunk before each warp, before the chunk, and in all.
+  // Thread e: expert e's pairs in this chunk before each warp, in earlier chunks, and in all.
   const int e = threadIdx.x;
   uint32_t total = 0, before = 0;
   if (e < E) {
-    uint32_t n[kSortWarps], run = 0;
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) n[w] = sort_smem[w * E + e];
+    for (int half = 0; half < 2; ++half) {
+      uint32_t n[kSortWarps / 2];
+      uint32_t* h = sort_smem + half * (kSortWarps / 2) * E + e;
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) {
-      sort_smem[w * E + e] = run;
-      run += n[w];
+      for (int w = 0; w < kSortWarps / 2; ++w) n[w] = h[w * E];
+#pragma unroll
+      for (int w = 0; w < kSortWarps / 2; ++w) {
+        h[w * E] = total;
+        total += n[w];
+      }
     }
-    total = run;
   }
-  if (gridDim.x > 1) {
+  if constexpr (kForm == kCluster) {
+    if (e < E) count[e] = total;
+    cluster_sync_all();
+    if (e < E) {
+      const uint32_t own = cluster_ctarank();
+      uint32_t n[kSortCluster];
+#pragma unroll
+      for (uint32_t c = 0; c < kSortCluster; ++c) n[c] = ld_cluster_u32(count + e, c);
+      total = 0;
+#pragma unroll
+      for (uint32_t c = 0; c < kSortCluster; ++c) {
+        total += n[c];
+        before += c < own ? n[c] : 0u;
+      }
+    }
+  } else if constexpr (kForm == kChunks) {
     // The chunks in as many shares as there are threads for.
     __shared__ uint32_t sums[2][kSortThreads];
     const uint32_t shares = kSortThreads / E, share = threadIdx.x / E, x = threadIdx.x - share * E;
-    uint32_t all = 0, lower = 0;
     if (share < shares) {
+      uint32_t all = 0, lower = 0;
 #pragma unroll 8
       for (uint32_t c = share; c < gridDim.x; c += shares) {
         const uint32_t n = __ldcg(a.counts + c * static_cast<uint64_t>(E) + x);
@@ -153,43 +215,51 @@ __global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortArgs 
     }
   }
   __syncthreads();
-  for (int64_t i = begin; i < end; i += 32) {
-    const int x = expert_of(a, i + lane, end);
-    const uint32_t peers = __match_any_sync(0xffffffffu, x), lower = peers & ((1u << lane) - 1);
-    const uint32_t at = x >= 0 ? hist[x] : 0u;
-    __syncwarp();
-    if (x >= 0 && lower == 0) hist[x] = at + __popc(peers);
-    if (i + lane < end) a.row_of[i + lane] = x >= 0 ? static_cast<int32_t>(base[x] + at + __popc(lower)) : -1;
-    __syncwarp();
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    if (i >= steps) break;
+    int row = -1;
+    if (at[i] >= 0) {
+      const int x = at[i] & 1023;
+      row = static_cast<int>(base[x] + hist[x]) + (at[i] >> 10);
+    }
+    if (begin + 32 * i < chunk_end) a.row_of[begin + 32 * i] = row;
   }
+  if constexpr (kForm == kCluster) cluster_sync_all();  // no CTA leaves while another may read its counts
 }
 
 // ------------------------------------------------------- walks over tokens ---
-// `vecs` units of a token's channels; a CTA takes several tokens where they are
-// short.  Loops are uniform in a warp.
+// `vecs` units of a token's channels.  A CTA has a token, or several short ones; the
+// GPU's many CTAs cover the latency, without a loop over tokens (one over resident
+// CTAs: 8192 tokens of 5120 to 4 rows each in NVFP4 39 us).  Loops are uniform in a
+// warp.
 
-constexpr int kWalkThreads = 256;
+constexpr uint32_t kWalkThreads = 512;  // at most
 
 struct Walk {
   int64_t tokens;
-  uint32_t vecs, per_cta;  // per_cta: tokens of a CTA's step
+  uint32_t vecs, per_cta;  // per_cta: tokens of a CTA
 };
-Walk make_walk(int64_t tokens, uint32_t vecs) {
-  return {tokens, vecs, vecs < kWalkThreads ? kWalkThreads / vecs : 1u};
-}
-uint32_t walk_grid(const Walk& w) {
-  const int64_t steps = (w.tokens + w.per_cta - 1) / w.per_cta, cap = static_cast<int64_t>(sm_count()) * 8;
-  return static_cast<uint32_t>(steps < cap ? steps : cap);
+struct WalkLaunch {
+  Walk w;
+  dim3 grid, block;
+};
+WalkLaunch make_walk(int64_t tokens, uint32_t vecs) {
+  WalkLaunch l;
+  l.w = {tokens, vecs, vecs < 128 ? 256 / vecs : 1u};
+  const uint32_t passes = (vecs + kWalkThreads - 1) / kWalkThreads;
+  l.block = dim3(l.w.per_cta > 1 ? 256 : ((vecs + passes - 1) / passes + 31) / 32 * 32);
+  l.grid = dim3(static_cast<uint32_t>((tokens + l.w.per_cta - 1) / l.w.per_cta));
+  return l;
 }
 // f(token, unit, live) for all of this thread's units.
 template <class F>
 __device__ __forceinline__ void walk(const Walk& w, F&& f) {
-  const uint32_t sub = w.vecs < kWalkThreads ? threadIdx.x / w.vecs : 0u;
+  const uint32_t sub = w.per_cta > 1 ? threadIdx.x / w.vecs : 0u;
   const uint32_t v0 = threadIdx.x - sub * w.vecs;
-  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * w.per_cta; t0 < w.tokens;
-       t0 += static_cast<int64_t>(gridDim.x) * w.per_cta)
-    for (uint32_t v = 0; v < w.vecs; v += kWalkThreads)
-      f(t0 + sub, v + v0, sub < w.per_cta && t0 + sub < w.tokens && v + v0 < w.vecs);
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * w.per_cta + sub;
+  for (uint32_t v = 0; v < w.vecs; v += blockDim.x)
+    f(t, v + v0, sub < w.per_cta && t < w.tokens && v + v0 < w.vecs);
 }
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -392,12 +462,13 @@ cudaError_t launch_combine(const RowArgs& a, int64_t tokens, uint32_t vecs, cons
 
 // kWarps warps have a token, a batch of choices at a time: one load of d_out serves the batch.  More warps where the
 // tokens are few; their parts of a sum are added in order.
+constexpr int kBackThreads = 256;
 template <int kWarps>
-__global__ void __launch_bounds__(kWalkThreads)
+__global__ void __launch_bounds__(kBackThreads)
     moe_combine_backward_kernel(const RowArgs a, int64_t tokens, uint32_t vecs, const uint16_t* __restrict__ d_out,
                                 int64_t ld, const uint16_t* __restrict__ y, const float* __restrict__ weights,
                                 uint16_t* __restrict__ d_y, float* __restrict__ d_weights) {
-  constexpr int kPer = kWalkThreads / 32 / kWarps;  // tokens of a CTA
+  constexpr int kPer = kBackThreads / 32 / kWarps;  // tokens of a CTA
   __shared__ float parts[kWarps > 1 ? kMoeMaxTopK : 1][kPer][kWarps];
   griddep_wait_and_release();
   const int warp = threadIdx.x >> 5, sub = warp / kWarps, part = warp % kWarps;
@@ -485,7 +556,7 @@ NVFP4_API int64_t moe_max_rows(int64_t n_tokens, int32_t top_k, int32_t num_expe
 NVFP4_API size_t moe_sort_workspace_size(int64_t n_tokens, int32_t top_k, int32_t num_experts) {
   if (check_moe_sizes(n_tokens, top_k, num_experts) != NVFP4_OK) return 0;
   const SortShape s = sort_shape(n_tokens * top_k);
-  return s.chunks > 1 ? static_cast<size_t>(s.chunks) * num_experts * sizeof(uint32_t) : 0;
+  return s.form == kChunks ? static_cast<size_t>(s.chunks) * num_experts * sizeof(uint32_t) : 0;
 }
 
 NVFP4_API nvfp4_status moe_sort(const moe_plan* plan, const int32_t* expert_idx, void* workspace,
@@ -509,18 +580,34 @@ NVFP4_API nvfp4_status moe_sort(const moe_plan* plan, const int32_t* expert_idx,
   const SortShape s = sort_shape(a.pairs);
   a.chunk = s.chunk;
   const cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  const dim3 grid(static_cast<uint32_t>(s.chunks)), block(kSortThreads);
-  const size_t smem = static_cast<size_t>(kSortWarps + 1) * a.experts * sizeof(uint32_t);
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(moe_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  const size_t smem = static_cast<size_t>(kSortWarps + 2) * a.experts * sizeof(uint32_t);
+  const auto kernel = s.form == kAlone ? moe_place_kernel<kAlone>
+                      : s.form == kCluster ? moe_place_kernel<kCluster> : moe_place_kernel<kChunks>;
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                static_cast<int>(smem)) != cudaSuccess) {
     cudaGetLastError();
     return NVFP4_ERR_CUDA;
   }
-  if (s.chunks > 1) {
-    if (launch_pdl(moe_count_kernel, grid, block, 0, cs, a) != cudaSuccess) return NVFP4_ERR_CUDA;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = kSortCluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<uint32_t>(s.chunks));
+  cfg.blockDim = dim3(kSortThreads);
+  cfg.stream = cs;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (s.form == kChunks) {
+    if (cudaLaunchKernelEx(&cfg, moe_count_kernel, a) != cudaSuccess) return NVFP4_ERR_CUDA;
     count_launches(1);
   }
-  if (launch_pdl(moe_place_kernel, grid, block, smem, cs, a) != cudaSuccess) return NVFP4_ERR_CUDA;
+  cfg.dynamicSmemBytes = smem;
+  cfg.numAttrs = s.form == kCluster ? 2 : 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) return NVFP4_ERR_CUDA;
   count_launches(1);
   return launch_status();
 }
@@ -533,9 +620,9 @@ NVFP4_API nvfp4_status moe_dispatch(const moe_plan* plan, const void* x_bf16, in
   if (plan->n_tokens == 0) return NVFP4_OK;
   if (!x_bf16 || !rows_bf16) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(x_bf16, 16) || !aligned(rows_bf16, 16) || !aligned(weights, 4)) return NVFP4_ERR_ALIGN;
-  const Walk w = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 8));
-  if (launch_pdl(moe_dispatch_kernel, dim3(walk_grid(w)), dim3(kWalkThreads), 0, static_cast<cudaStream_t>(stream),
-                 row_args(plan), w, static_cast<const uint16_t*>(x_bf16), ld_x, weights,
+  const WalkLaunch l = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 8));
+  if (launch_pdl(moe_dispatch_kernel, l.grid, l.block, 0, static_cast<cudaStream_t>(stream),
+                 row_args(plan), l.w, static_cast<const uint16_t*>(x_bf16), ld_x, weights,
                  static_cast<uint16_t*>(rows_bf16)) != cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
@@ -550,9 +637,9 @@ NVFP4_API nvfp4_status moe_dispatch_nvfp4(const moe_plan* plan, const void* x_bf
   if (plan->n_tokens == 0) return NVFP4_OK;
   if (!x_bf16 || !g_dev || !codes || !scales) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(x_bf16, 16) || !aligned(codes, 16) || !aligned(scales, 4) || !aligned(g_dev, 4)) return NVFP4_ERR_ALIGN;
-  const Walk w = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 32));
-  if (launch_pdl(moe_dispatch_nvfp4_kernel, dim3(walk_grid(w)), dim3(kWalkThreads), 0,
-                 static_cast<cudaStream_t>(stream), row_args(plan), w, static_cast<const uint16_t*>(x_bf16), ld_x,
+  const WalkLaunch l = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 32));
+  if (launch_pdl(moe_dispatch_nvfp4_kernel, l.grid, l.block, 0,
+                 static_cast<cudaStream_t>(stream), row_args(plan), l.w, static_cast<const uint16_t*>(x_bf16), ld_x,
                  g_dev, reinterpret_cast<uint4*>(codes), scales) != cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
@@ -568,9 +655,8 @@ NVFP4_API nvfp4_status moe_dispatch_mxfp4(const moe_plan* plan, const void* x_bf
   if (plan->n_tokens == 0) return NVFP4_OK;
   if (!x_bf16 || !codes || !scales) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(x_bf16, 16) || !aligned(codes, 16) || !aligned(scales, 4)) return NVFP4_ERR_ALIGN;
-  const Walk w = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 32));
-  if (launch_pdl(rotate ? moe_dispatch_mxfp4_kernel<true> : moe_dispatch_mxfp4_kernel<false>, dim3(walk_grid(w)),
-                 dim3(kWalkThreads), 0, static_cast<cudaStream_t>(stream), row_args(plan), w,
+  const WalkLaunch l = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 32));
+  if (launch_pdl(rotate ? moe_dispatch_mxfp4_kernel<true> : moe_dispatch_mxfp4_kernel<false>, l.grid, l.block, 0, static_cast<cudaStream_t>(stream), row_args(plan), l.w,
                  static_cast<const uint16_t*>(x_bf16), ld_x, reinterpret_cast<uint4*>(codes), scales) != cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
@@ -615,8 +701,8 @@ NVFP4_API nvfp4_status moe_combine_backward(const moe_plan* plan, const void* d_
   const int warps = plan->n_tokens >= slots ? 1 : 4 * plan->n_tokens >= slots ? 4 : 8;
   const auto kernel = warps == 1 ? moe_combine_backward_kernel<1>
                       : warps == 4 ? moe_combine_backward_kernel<4> : moe_combine_backward_kernel<8>;
-  const int64_t per = kWalkThreads / 32 / warps, grid = (plan->n_tokens + per - 1) / per;
-  if (launch_pdl(kernel, dim3(static_cast<uint32_t>(grid)), dim3(kWalkThreads), 0,
+  const int64_t per = kBackThreads / 32 / warps, grid = (plan->n_tokens + per - 1) / per;
+  if (launch_pdl(kernel, dim3(static_cast<uint32_t>(grid)), dim3(kBackThreads), 0,
                  static_cast<cudaStream_t>(stream), row_args(plan), plan->n_tokens, static_cast<uint32_t>(cols / 8),
                  static_cast<const uint16_t*>(d_out_bf16), ld_d_out, static_cast<const uint16_t*>(y_bf16), weights,
                  static_cast<uint16_t*>(d_y_bf16), d_weights) != cudaSuccess)
