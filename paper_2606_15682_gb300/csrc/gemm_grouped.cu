@@ -10,12 +10,14 @@
 // weight's bytes and no more, and many leave at most 31 columns idle.  Each CTA holds
 // its 128 weight rows and half of the tokens' rows; D[weight row, token] is in its
 // own TMEM lanes.  Which tiles there are follows from the plan on the device: every
-// CTA sums the experts' tiles (shared memory) and takes units u, u + pairs, ...; an
-// expert's units are next to each other, those of one weight tile first, so that its
-// bytes come from DRAM once.
+// CTA sums the experts' tiles (shared memory); an expert's units are next to each
+// other, those of one weight tile first, so that its bytes come from DRAM once.  The
+// launch has a cluster for each unit that there may be; those that run take the next
+// ones that have not started (cluster launch control) and stay on their SMs: units of
+// 32 to 256 tokens even out.
 //   warp 0      codes; a CTA's weight rows and its half of the tokens' rows
 //   warp 1      leader: MMAs; peer: block scales
-//   warp 2      leader: block scales into TMEM
+//   warp 2      leader: block scales into TMEM; peer: the queue of units
 //   warp 3      leader: block scales
 //   warps 4-11  epilogue: 32 weight rows x every other 32 tokens each
 // The epilogue reads 16 x 8 fragments of D (16x256b), in which a thread has two tokens
@@ -40,6 +42,7 @@ constexpr int kTokens = 256;  // of a tile
 constexpr int kWRows = 256;
 constexpr int kEpi0 = 4, kEpiWarps = 8;
 constexpr int kThreads = 32 * (kEpi0 + kEpiWarps);
+constexpr int kQueue = 4;  // answers on their way to the warps
 constexpr uint32_t kWBytes = 128 * kDepth / 2, kXBytes = 128 * kDepth / 2;  // a CTA's codes of a stage
 constexpr uint32_t kScaleTile = 128 * kDepth / 16;                         // block scales of 128 rows: four atoms
 constexpr uint32_t kEpiBytes = 2048;                                       // a warp's 32 tokens x 32 bf16
@@ -134,9 +137,10 @@ __device__ __forceinline__ void load_box3(void* dst, const void* map, uint64_t* 
       "l"(reinterpret_cast<uint64_t>(map)), "r"(leader_address(bar)), "r"(0), "r"(y), "r"(z)
       : "memory");
 }
-// Hands the accumulator back: the warp's TMEM loads are complete and fenced, and no memory that it wrote is read.
-__device__ __forceinline__ void arrive_leader_relaxed(uint64_t* bar) {
-  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_address(bar)) : "memory");
+// Arrives without release: hands back an accumulator whose TMEM loads are complete and fenced, or an answer that was
+// read and used; no memory that the warp wrote is read after it.
+__device__ __forceinline__ void arrive_relaxed(uint32_t pair_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(pair_addr) : "memory");
 }
 // After a pipeline gave up: lets this thread's copies land before its pair exits.
 __device__ __forceinline__ void wait_for_copies() {
@@ -184,6 +188,37 @@ __device__ __forceinline__ bool both(int id, bool ok) {
       : "r"(id), "r"(ok ? 1 : 0)
       : "memory");
   return r != 0;
+}
+// The launch's clusters that have not started are its queue: a CTA of a running cluster takes one (its first CTA's index)
+// in place of a start.  The answer, 16 bytes, goes to both CTAs' shared memory and barriers at the same offsets.
+__device__ __forceinline__ void take_cluster(void* answer, uint64_t* bar) {
+  asm volatile(
+      "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.multicast::cluster::all.b128 [%0], [%1];" ::"r"(
+          smem_u32(answer)),
+      "r"(smem_u32(bar))
+      : "memory");
+}
+// The index of the cluster that was taken, -1: none was left.
+__device__ __forceinline__ int taken_cluster(const void* answer) {
+  uint32_t some, x;
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b128 h;\n ld.shared.b128 h, [%2];\n"
+      " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n selp.u32 %0, 1, 0, p;\n mov.u32 %1, 0;\n"
+      " @p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, h;\n}"
+      : "=r"(some), "=r"(x)
+      : "r"(smem_u32(answer))
+      : "memory");
+  return some ? static_cast<int>(x / 2) : -1;
+}
+// Of the barrier at this offset in CTA `rank` of the pair.
+__device__ __forceinline__ uint32_t pair_address(const uint64_t* bar, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(bar)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void expect_in_pair(const uint64_t* bar, uint32_t rank, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(pair_address(bar, rank)), "r"(bytes)
+               : "memory");
 }
 __device__ __forceinline__ void meet(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
 
@@ -315,7 +350,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* acc_empty = acc_full + 1;
   uint64_t* drain = acc_empty + 1;
   uint64_t* drain_copies = drain + 1;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_copies + 1);
+  uint64_t* answer_full = drain_copies + 1;
+  uint64_t* answer_empty = answer_full + kQueue;  // the peer's is used
+  uint8_t* answers = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(answer_empty + kQueue) + 15) & ~uintptr_t(15));
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(answers + 16 * kQueue);
   __shared__ volatile int abort_flag;
   __shared__ int64_t warp_sum[kThreads / 32];
 
@@ -323,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int kblocks = a.K / kDepth;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
-  const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+  const int first_unit = blockIdx.x / 2;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -336,6 +374,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(acc_empty, 2 * kEpiWarps);
     mbar_init(drain, 1);
     mbar_init(drain_copies, 1);
+    for (int i = 0; i < kQueue; ++i) {
+      mbar_init(&answer_full[i], 1);
+      mbar_init(&answer_empty[i], 4 + 2 + 2 * kEpiWarps);  // the leader's four first warps, the peer's two
+    }
     abort_flag = 0;
     fence_mbar_init();
     prefetch_tmap(&map_w);
@@ -392,23 +434,50 @@ __global__ void __launch_bounds__(kThreads, 1)
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
     return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, &abort_flag)) != 0;
   };
-  // Walks this pair's units and k-blocks; load(stage, kb, unit), in one lane, fills a stage once `free` says so.
+  // The next unit of the pair, to each of its warps by itself (n: its count of answers).  False: there is none, or, with
+  // *ok false, the wait ran out.
+  auto next_unit = [&](int* u, int* n, bool* ok) {
+    const int slot = *n % kQueue;
+    *ok = wait(&answer_full[slot], (*n / kQueue) & 1);
+    if (!*ok) {
+      fail();
+      return false;
+    }
+    ++*n;
+    *u = __shfl_sync(0xffffffffu, taken_cluster(answers + 16 * slot), 0);
+    fence_proxy_async_smem();  // read here, then written by the next answer
+    __syncwarp();
+    if (lane == 0) arrive_relaxed(pair_address(&answer_empty[slot], 1));
+    return *u >= 0;
+  };
+  // Walks the pair's units; body(unit) gives false where a wait ran out.
+  auto walk_units = [&](auto&& body) {
+    int u = first_unit, n = 0;
+    bool ok = true;
+    do {
+      if (u < units) ok = body(find_unit(u, ends, expert_rows_s, lane));
+    } while (ok && next_unit(&u, &n, &ok));
+    return ok;
+  };
+  // A producer's walk; load(stage, kb, unit), in one lane, fills a stage once `free` says so.
   auto produce = [&](uint64_t* free, auto&& load) {
     const bool issuer = elect_one();
     int stage = 0;
     uint32_t phase = 0;
-    bool skip = a.fault_skip_stage && pair == 0, ok = true;
-    for (int u = pair; u < units && ok; u += pairs) {
-      const Unit t = find_unit(u, ends, expert_rows_s, lane);
+    bool skip = a.fault_skip_stage && first_unit == 0;
+    const bool done = walk_units([&](const Unit& t) {
       for (int kb = 0; kb < kblocks; ++kb) {
-        ok = wait(&free[stage], phase ^ 1u);
-        if (!ok) { fail(); break; }
+        if (!wait(&free[stage], phase ^ 1u)) {
+          fail();
+          return false;
+        }
         if (issuer && !skip) load(stage, kb, t);
         skip = false;
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
-    }
-    if (!ok) wait_for_copies();
+      return true;
+    });
+    if (!done) wait_for_copies();
   };
 
   if (warp == 0) {
@@ -446,14 +515,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t utmem = __shfl_sync(0xffffffffu, tmem, 0);
     const uint64_t w_desc0 = tile_desc(smem_u32(sW)), x_desc0 = tile_desc(smem_u32(sX));
     bool ready = false;  // the next stage was seen full
-    for (int u = pair; u < units; u += pairs, ++local) {
-      const Unit t = find_unit(u, ends, expert_rows_s, lane);
+    walk_units([&](const Unit& t) {
       const uint32_t idesc = kIdesc | static_cast<uint32_t>(t.n >> 3) << 17 | (a.mx ? kUE8M0 : 0u);
-      if (!wait(acc_empty, (local & 1) ^ 1u)) { fail(); break; }
+      if (!wait(acc_empty, (local & 1) ^ 1u)) {
+        fail();
+        return false;
+      }
+      ++local;
       tc_fence_after();
-      bool ok = true;
       for (int kb = 0; kb < kblocks; ++kb) {
-        if (!ready && !wait(&full[stage], phase)) { fail(); ok = false; break; }
+        if (!ready && !wait(&full[stage], phase)) {
+          fail();
+          return false;
+        }
         tc_fence_after();
         const uint32_t ws = utmem + kSfCol + stage * kSfCols, xs = ws + 16;
         const uint64_t w_desc = w_desc0 + static_cast<uint32_t>(stage) * (kWBytes >> 4);
@@ -470,9 +544,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         stage = next;
         phase = next_phase;
       }
-      if (!ok) break;
       if (issuer) pair_commit(acc_full, 0x3);
-    }
+      return true;
+    });
     if (issuer) pair_commit(drain, 0x1);
     mbar_wait_bounded(drain, 0, nullptr);
   } else if (warp == 2 && leader) {
@@ -482,13 +556,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t phase = 0;
     const uint32_t utmem = __shfl_sync(0xffffffffu, tmem, 0);
     const uint64_t ws_desc0 = atom_desc(smem_u32(sWS)), xs_desc0 = atom_desc(smem_u32(sXS));
-    bool ok = true;
-    for (int u = pair; u < units && ok; u += pairs) {
-      const Unit t = find_unit(u, ends, expert_rows_s, lane);
+    walk_units([&](const Unit& t) {
       for (int kb = 0; kb < kblocks; ++kb) {
         // The scales have landed, and the MMAs that read this TMEM slot are done.
-        ok = wait(&scales_in[stage], phase) && wait(&empty[stage], phase ^ 1u);
-        if (!ok) { fail(); break; }
+        if (!wait(&scales_in[stage], phase) || !wait(&empty[stage], phase ^ 1u)) {
+          fail();
+          return false;
+        }
         tc_fence_after();
         const uint32_t ws = utmem + kSfCol + stage * kSfCols, xs = ws + 16;
         const uint64_t ws_desc = ws_desc0 + static_cast<uint32_t>(stage) * (kScaleTile >> 4);
@@ -504,9 +578,33 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
-    }
+      return true;
+    });
     if (issuer) pair_commit(drain_copies, 0x1);
     mbar_wait_bounded(drain_copies, 0, nullptr);
+  } else if (warp == 2) {
+    // ------------------------------------------------------ peer: the queue ---
+    const bool issuer = elect_one();
+    for (int n = 0;; ++n) {
+      const int slot = n % kQueue;
+      const uint32_t phase = (n / kQueue) & 1;
+      if (!wait(&answer_empty[slot], phase ^ 1u)) {
+        fail();
+        break;
+      }
+      if (issuer) {
+        expect_in_pair(&answer_full[slot], 0, 16);
+        expect_in_pair(&answer_full[slot], 1, 16);
+        take_cluster(answers + 16 * slot, &answer_full[slot]);
+      }
+      __syncwarp();
+      if (!wait(&answer_full[slot], phase)) {
+        fail();
+        break;
+      }
+      // Asking again after the queue was found empty is not allowed.
+      if (__shfl_sync(0xffffffffu, taken_cluster(answers + 16 * slot), 0) < 0) break;
+    }
   } else if (warp >= kEpi0) {
     // ----------------------------------------------------------- epilogue ---
     const int quarter = warp & 3, side = (warp - kEpi0) >> 2;
@@ -514,8 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint8_t* buf_ptr = sEpi + (warp - kEpi0) * kEpiBytes;
     const uint32_t buf = smem_u32(buf_ptr);
     int local = 0;
-    for (int u = pair; u < units; u += pairs, ++local) {
-      const Unit t = find_unit(u, ends, expert_rows_s, lane);
+    auto finish = [&](const Unit& t) {
       const float scale =
           a.g_a ? __fmul_rn(__ldg(a.g_a + static_cast<int64_t>(t.expert) * a.g_a_step), __ldg(a.g_w + t.expert)) : 1.0f;
       // Lane 0 waits and tells, so that the warp stays converged.
@@ -526,7 +623,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       ok = __shfl_sync(0xffffffffu, ok, 0);
       if (kMode == 2) ok = both(meeting, ok != 0);  // the two warps go on or leave together
-      if (!ok) break;
+      if (!ok) return false;
+      ++local;
       tc_fence_after();
       uint32_t lo[4][16], hi[4][16];
       const uint32_t taddr = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
@@ -541,15 +639,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       tmem_ld_done();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) arrive_leader_relaxed(acc_empty);
+      if (lane == 0) arrive_relaxed(leader_address(acc_empty));
       // The next unit's MMAs run while this warp computes and stores.
       const int n0 = t.w_tile * kWRows + static_cast<int>(rank) * 128 + quarter * 32;
       if constexpr (kMode == 0) {
-        if (n0 >= a.N) continue;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int token0 = 32 * (2 * i + side);
-          if (token0 < t.tokens) store_rows(a, t, lo[i], hi[i], token0, n0, scale, buf, lane);
+          if (token0 < t.tokens && n0 < a.N) store_rows(a, t, lo[i], hi[i], token0, n0, scale, buf, lane);
         }
       } else if constexpr (kMode == 1) {
         const float g_in = __ldg(a.g_out + static_cast<int64_t>(t.expert) * a.g_out_step);
@@ -640,6 +737,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           store_codes(a, t, codes, code, token0, n0 >> 1, lane);
         }
       }
+      return true;
+    };
+    int u = first_unit, n = 0;
+    bool ok = true, more = true;
+    while (more) {
+      if (u < units && !finish(find_unit(u, ends, expert_rows_s, lane))) break;
+      more = next_unit(&u, &n, &ok);
+      if (kMode == 2 && !both(meeting, ok)) break;
     }
   }
 
@@ -689,27 +794,21 @@ bool scales_map(CUtensorMap* map, const uint8_t* base, int64_t tiles, int64_t K,
   return encode(map, base, two ? 3 : 2, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-// Pairs of this kernel that are resident at once on the current device, 0 on failure.
+// The shared-memory opt-in, once for each device.
 template <int kMode>
-int resident_pairs(cudaLaunchConfig_t cfg) {
+bool opted_in() {
   static std::mutex mu;
-  static std::map<int, int> cache;
+  static std::map<int, bool> done;
   int d = 0;
-  if (cudaGetDevice(&d) != cudaSuccess) return 0;
+  if (cudaGetDevice(&d) != cudaSuccess) return false;
   std::lock_guard<std::mutex> lock(mu);
-  const auto it = cache.find(d);
-  if (it != cache.end()) return it->second;
-  int pairs = 0;
-  cfg.gridDim = dim3(2 * (sm_count() / 2), 1, 1);
-  cfg.numAttrs = 1;  // the cluster's size
+  if (done[d]) return true;
   if (cudaFuncSetAttribute(grouped_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           static_cast<int>(kSmem)) != cudaSuccess ||
-      cudaOccupancyMaxActiveClusters(&pairs, grouped_kernel<kMode>, &cfg) != cudaSuccess || pairs <= 0) {
+                           static_cast<int>(kSmem)) != cudaSuccess) {
     cudaGetLastError();
-    return 0;
+    return false;
   }
-  cache[d] = pairs;
-  return pairs;
+  return done[d] = true;
 }
 
 template <int kMode>
@@ -723,7 +822,7 @@ nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s
   a.w_scale_tiles = (a.N + 127) / 128;
   const int64_t choices = plan->n_tokens * plan->top_k, used = choices < a.experts ? choices : a.experts;
   const int64_t units = (choices + (kTokens - 1) * used) / kTokens * a.w_tiles;  // at most
-  if (units >= (1ll << 31)) return NVFP4_ERR_SHAPE;
+  if (units >= (1ll << 30)) return NVFP4_ERR_SHAPE;
   a.max_units = static_cast<int>(units);
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -736,8 +835,7 @@ nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.dynamicSmemBytes = kSmem;
   cfg.attrs = attr;
-  const int resident = resident_pairs<kMode>(cfg);
-  if (resident <= 0) return NVFP4_ERR_CUDA;
+  if (!opted_in<kMode>()) return NVFP4_ERR_CUDA;
   CUtensorMap w, ws, x16, x64, x128, xs, xs2;
   const int64_t R = a.max_rows, K = a.K;
   if (!codes_map(&w, a.w_codes, static_cast<int64_t>(a.experts) * a.N, K, 128) ||
@@ -748,7 +846,7 @@ nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s
     return NVFP4_ERR_CUDA;
   a.status = status_word_dev();
   a.fault_skip_stage = take_fault(NVFP4_FAULT_GEMM_SKIP_STAGE) ? 1 : 0;
-  cfg.gridDim = dim3(static_cast<uint32_t>(2 * (units < resident ? units : resident)), 1, 1);
+  cfg.gridDim = dim3(static_cast<uint32_t>(2 * units), 1, 1);
   cfg.stream = s;
   cfg.numAttrs = 2;
   if (cudaLaunchKernelEx(&cfg, grouped_kernel<kMode>, w, ws, x16, x64, x128, xs, xs2, a) != cudaSuccess)
