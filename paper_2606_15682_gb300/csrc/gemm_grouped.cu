@@ -42,7 +42,7 @@ constexpr int kTokens = 256;  // of a tile
 constexpr int kWRows = 256;
 constexpr int kEpi0 = 4, kEpiWarps = 8;
 constexpr int kThreads = 32 * (kEpi0 + kEpiWarps);
-constexpr int kQueue = 4;  // answers on their way to the warps
+constexpr int kQueue = 4;  // units on their way to the warps
 constexpr uint32_t kWBytes = 128 * kDepth / 2, kXBytes = 128 * kDepth / 2;  // a CTA's codes of a stage
 constexpr uint32_t kScaleTile = 128 * kDepth / 16;                         // block scales of 128 rows: four atoms
 constexpr uint32_t kEpiBytes = 2048;                                       // a warp's 32 tokens x 32 bf16
@@ -176,8 +176,12 @@ __device__ __forceinline__ void stmatrix_t(uint32_t addr, uint32_t a, uint32_t b
                "r"(c), "r"(d)
                : "memory");
 }
+// SiLU(gate) * up by the hardware's 2^x and 1 / x, within 2^-22 each; 2^x takes an argument rounded to 2^-24 of itself.
 __device__ __forceinline__ float silu_mul(float gate, float up) {
-  return __fdividef(gate, 1.0f + __expf(-gate)) * up;
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(gate * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  return gate * r * up;
 }
 // Two warps of the epilogue meet; true where both gave true.
 __device__ __forceinline__ bool both(int id, bool ok) {
@@ -190,13 +194,12 @@ __device__ __forceinline__ bool both(int id, bool ok) {
   return r != 0;
 }
 // The launch's clusters that have not started are its queue: a CTA of a running cluster takes one (its first CTA's index)
-// in place of a start.  The answer, 16 bytes, goes to both CTAs' shared memory and barriers at the same offsets.
+// in place of a start.  The answer is 16 bytes of this CTA's shared memory.
 __device__ __forceinline__ void take_cluster(void* answer, uint64_t* bar) {
-  asm volatile(
-      "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.multicast::cluster::all.b128 [%0], [%1];" ::"r"(
-          smem_u32(answer)),
-      "r"(smem_u32(bar))
-      : "memory");
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                   smem_u32(answer)),
+               "r"(smem_u32(bar))
+               : "memory");
 }
 // The index of the cluster that was taken, -1: none was left.
 __device__ __forceinline__ int taken_cluster(const void* answer) {
@@ -210,11 +213,18 @@ __device__ __forceinline__ int taken_cluster(const void* answer) {
       : "memory");
   return some ? static_cast<int>(x / 2) : -1;
 }
-// Of the barrier at this offset in CTA `rank` of the pair.
-__device__ __forceinline__ uint32_t pair_address(const uint64_t* bar, uint32_t rank) {
+// Of what is at this offset in CTA `rank` of the pair.
+__device__ __forceinline__ uint32_t pair_address(const void* p, uint32_t rank) {
   uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(bar)), "r"(rank));
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
   return r;
+}
+// 16 bytes to CTA `rank` of the pair, counted on its barrier.
+__device__ __forceinline__ void send_16(const void* dst, const uint64_t* bar, uint32_t rank, int4 v) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
+                   pair_address(dst, rank)),
+               "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "r"(pair_address(bar, rank))
+               : "memory");
 }
 __device__ __forceinline__ void expect_in_pair(const uint64_t* bar, uint32_t rank, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(pair_address(bar, rank)), "r"(bytes)
@@ -226,22 +236,28 @@ __device__ __forceinline__ void meet(int id) { asm volatile("barrier.cta.sync %0
 
 struct Unit {
   int expert, w_tile;
-  int row0, tokens;  // first row, rows of the tile
-  int n;             // the MMA's N: tokens up to a multiple of 32
+  int row0, tokens;  // first row, rows of the tile; tokens 0: there is no unit
+  float scale, g_out;
+  int n;  // the MMA's N: tokens up to a multiple of 32
+  int unused;
 };
+static_assert(sizeof(Unit) == 32, "two 16-byte words");
 // Unit u, by a converged warp.  ends: [1024] units of the experts up to each one, the total behind the last one.
-__device__ __forceinline__ Unit find_unit(int u, const int* ends, const int2* rows, int lane) {
+__device__ __forceinline__ Unit find_unit(const GroupedArgs& a, int u, const int* ends, const int2* rows, int lane) {
   const int block = __popc(__ballot_sync(0xffffffffu, ends[32 * lane + 31] <= u));
   const int e = 32 * block + __popc(__ballot_sync(0xffffffffu, ends[32 * block + lane] <= u));
   const int2 r = rows[e];  // first row, rows
-  const int local = u - (e ? ends[e - 1] : 0), tiles = (r.y + kTokens - 1) / kTokens;
   Unit t;
+  t.scale = a.g_a ? __fmul_rn(__ldg(a.g_a + static_cast<int64_t>(e) * a.g_a_step), __ldg(a.g_w + e)) : 1.0f;
+  t.g_out = a.g_out ? __ldg(a.g_out + static_cast<int64_t>(e) * a.g_out_step) : 0.0f;
+  const int local = u - (e ? ends[e - 1] : 0), tiles = (r.y + kTokens - 1) / kTokens;
   t.expert = e;
   t.w_tile = local / tiles;
   const int token_tile = local - t.w_tile * tiles;
   t.row0 = r.x + token_tile * kTokens;
   t.tokens = min(kTokens, r.y - token_tile * kTokens);
   t.n = (t.tokens + 31) & ~31;
+  t.unused = 0;
   return t;
 }
 
@@ -249,31 +265,33 @@ __device__ __forceinline__ Unit find_unit(int u, const int* ends, const int2* ro
 // lo, hi: the fragments of a warp's weight rows 0..15 and 16..31, 32 tokens from token0.
 
 __device__ __forceinline__ void store_rows(const GroupedArgs& a, const Unit& t, const uint32_t* lo, const uint32_t* hi,
-                                           int token0, int n0, float scale, uint32_t buf, int lane) {
-  auto f = [&](uint32_t v) { return __uint_as_float(v) * scale; };
+                                           int token0, int n0, uint32_t buf, int lane) {
+  auto f = [&](uint32_t v) { return __uint_as_float(v) * t.scale; };
   // Rows of 64 bytes in 16-byte chunks, chunk c of token t at c ^ (t / 2) % 4: no bank twice, written or read.
+  const uint32_t put = buf + (lane & 7) * 64 + (((lane >> 3) ^ ((lane >> 1) & 3)) << 4);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int tk = 8 * j + (lane & 7);
-    stmatrix_t(buf + tk * 64 + (((lane >> 3) ^ ((tk >> 1) & 3)) << 4), pack_pair(f(lo[4 * j]), f(lo[4 * j + 1])),
-               pack_pair(f(lo[4 * j + 2]), f(lo[4 * j + 3])), pack_pair(f(hi[4 * j]), f(hi[4 * j + 1])),
-               pack_pair(f(hi[4 * j + 2]), f(hi[4 * j + 3])));
-  }
+  for (int j = 0; j < 4; ++j)
+    stmatrix_t(put + j * 512, pack_pair(f(lo[4 * j]), f(lo[4 * j + 1])), pack_pair(f(lo[4 * j + 2]), f(lo[4 * j + 3])),
+               pack_pair(f(hi[4 * j]), f(hi[4 * j + 1])), pack_pair(f(hi[4 * j + 2]), f(hi[4 * j + 3])));
   __syncwarp();
-  const int c = lane & 3, n = n0 + 8 * c;
+  const int c = lane & 3, n = n0 + 8 * c, tk0 = lane >> 2;
+  const uint32_t get = buf + tk0 * 64 + ((c ^ ((tk0 >> 1) & 3)) << 4);
+  uint4 v[4];
+#pragma unroll
+  for (int it = 0; it < 4; ++it)
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v[it].x), "=r"(v[it].y), "=r"(v[it].z), "=r"(v[it].w)
+                 : "r"(get + it * 512)
+                 : "memory");
+  __syncwarp();
+  if (n >= a.N || !in_bounds(a.status, t.row0 + min(token0 + 32, t.tokens) <= a.max_rows && n + 8 <= a.N))
+    return;  // N % 16 == 0: a chunk is inside or outside
+  uint16_t* dst = a.out + static_cast<int64_t>(t.row0 + token0 + tk0) * a.ldo + n;
 #pragma unroll
   for (int it = 0; it < 4; ++it) {
-    const int tk = 8 * it + (lane >> 2);
-    uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                 : "r"(buf + tk * 64 + ((c ^ ((tk >> 1) & 3)) << 4))
-                 : "memory");
-    // N % 16 == 0: a chunk is inside or outside.
-    if (token0 + tk < t.tokens && n < a.N && in_bounds(a.status, t.row0 + token0 + tk < a.max_rows && n + 8 <= a.N))
-      *reinterpret_cast<uint4*>(a.out + static_cast<int64_t>(t.row0 + token0 + tk) * a.ldo + n) = v;
+    if (token0 + tk0 + 8 * it < t.tokens) *reinterpret_cast<uint4*>(dst) = v[it];
+    dst += 8 * a.ldo;
   }
-  __syncwarp();
 }
 
 // h = SiLU(gate) up over lo; lane has rows lane / 4 and 8 below, tokens 2 (lane % 4) and the next.
@@ -283,38 +301,58 @@ __device__ __forceinline__ void swiglu_fragments(uint32_t* lo, const uint32_t* h
     lo[i] = __float_as_uint(silu_mul(__uint_as_float(lo[i]) * scale, __uint_as_float(hi[i]) * scale));
 }
 
-// The largest magnitude of 16 outputs of a token: of the even token of the fragment where lane / 4 is even, of the odd.
+// Quantization of 32 tokens of 16 outputs.  A lane's own token is 8 (lane / 8) + 2 (lane % 4) + (lane / 4) % 2: what a
+// token needs once (its largest magnitude, its scale, its codes' word) is with its lane.  The eight lanes with the
+// same lane % 4 hold all of eight tokens' outputs: fragment 4j + p of token 8j + 2 (lane % 4) + p.
+
+// The largest magnitude of the lane's token: each step halves the tokens that a lane keeps.
 __device__ __forceinline__ float token_amax(const uint32_t* h, int lane) {
-  auto f = [&](int i) { return fabsf(__uint_as_float(h[i])); };
-  const float even = fmaxf(f(0), f(2)), odd = fmaxf(f(1), f(3));
-  const bool o = lane & 4;
-  float v = fmaxf(o ? odd : even, __shfl_xor_sync(0xffffffffu, o ? even : odd, 4));
-  v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
-  return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+  float m[8];  // tokens 2j + p of the eight
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    const int i = 4 * (s >> 1) + (s & 1);
+    m[s] = fmaxf(fabsf(__uint_as_float(h[i])), fabsf(__uint_as_float(h[i + 2])));
+  }
+#pragma unroll
+  for (int half = 4; half; half >>= 1) {
+    const bool upper = lane & (4 * half);
+#pragma unroll
+    for (int s = 0; s < half; ++s)
+      m[s] = fmaxf(upper ? m[s + half] : m[s], __shfl_xor_sync(0xffffffffu, upper ? m[s] : m[s + half], 4 * half));
+  }
+  return m[0];
 }
 
-// The 16 codes of this lane's token (as token_amax has them), element 0 in the lowest nibble; mult: the token's factor.
+// The 16 codes of the lane's token, output 0 in the lowest nibble; mult: the token's factor.
 __device__ __forceinline__ uint2 token_codes(const uint32_t* h, float mult, int lane) {
-  auto f = [&](int i, float m) { return __fmul_rn(__uint_as_float(h[i]), m); };
-  const bool o = lane & 4;
-  const float other = __shfl_xor_sync(0xffffffffu, mult, 4);
-  const float m_even = o ? other : mult, m_odd = o ? mult : other;
-  // Low nibble: row lane / 4; high: 8 below.
-  const uint32_t even = e2m1x2(f(0, m_even), f(2, m_even)), odd = e2m1x2(f(1, m_odd), f(3, m_odd));
-  const uint32_t mine = o ? odd : even, got = __shfl_xor_sync(0xffffffffu, o ? even : odd, 4);
-  const uint32_t first = o ? got : mine, second = o ? mine : got;  // of rows 2i and 2i + 1, i = lane / 8
-  const uint32_t low = (first & 15) | (second & 15) << 4, high = first >> 4 | (second & 0xF0);
-  const int s = lane & 8;
-  uint32_t w = low << s | high << (16 + s);
-  w |= __shfl_xor_sync(0xffffffffu, w, 8);
-  const uint32_t v = __shfl_xor_sync(0xffffffffu, w, 16);
-  const uint32_t a = lane & 16 ? v : w, b = lane & 16 ? w : v;  // rows 0-3 and 8-11; 4-7 and 12-15
-  return make_uint2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+  // Bytes of the eight tokens: the code of row lane / 4 in the low nibble, of 8 below in the high one.
+  uint32_t byte[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    const float m = __shfl_sync(0xffffffffu, mult, (lane & 3) | s << 2);
+    const int i = 4 * (s >> 1) + (s & 1);
+    byte[s] = e2m1x2(__fmul_rn(__uint_as_float(h[i]), m), __fmul_rn(__uint_as_float(h[i + 2]), m));
+  }
+  const uint32_t w0 = byte[0] | byte[1] << 8 | byte[2] << 16 | byte[3] << 24;
+  const uint32_t w1 = byte[4] | byte[5] << 8 | byte[6] << 16 | byte[7] << 24;
+  // Transposed over the eight lanes, a bit of lane / 4 a step: x0, y0, z0 come from the lane where it is 0.
+  const bool b4 = lane & 16, b3 = lane & 8, b2 = lane & 4;
+  uint32_t keep = b4 ? w1 : w0, got = __shfl_xor_sync(0xffffffffu, b4 ? w0 : w1, 16);
+  const uint32_t x0 = b4 ? got : keep, x1 = b4 ? keep : got;
+  keep = __byte_perm(x0, x1, b3 ? 0x7632 : 0x5410);
+  got = __shfl_xor_sync(0xffffffffu, __byte_perm(x0, x1, b3 ? 0x5410 : 0x7632), 8);
+  const uint32_t y0 = b3 ? got : keep, y1 = b3 ? keep : got;
+  keep = __byte_perm(y0, y1, b2 ? 0x7531 : 0x6420);
+  got = __shfl_xor_sync(0xffffffffu, __byte_perm(y0, y1, b2 ? 0x6420 : 0x7531), 4);
+  const uint32_t z0 = b2 ? got : keep, z1 = b2 ? keep : got;
+  const uint32_t a = __byte_perm(z0, z1, 0x6240), b = __byte_perm(z0, z1, 0x7351);  // rows 0-3 and 4-7
+  // Nibbles of a row's byte into the words of rows 0-7 and 8-15.
+  auto join = [](uint32_t x, uint32_t y) { return __byte_perm(x | x >> 4, y | y >> 4, 0x6420); };
+  return make_uint2(join(a & 0x0F0F0F0Fu, b & 0x0F0F0F0Fu), join(a >> 4 & 0x0F0F0F0Fu, b >> 4 & 0x0F0F0F0Fu));
 }
 
 __device__ __forceinline__ void store_codes(const GroupedArgs& a, const Unit& t, uint2 codes, uint32_t code, int token0,
                                             uint32_t oc, int lane) {
-  // Lane's token: group lane / 8 of 8, 2 (lane % 4) in it and the next where lane / 4 is odd.
   const int tk = token0 + 8 * (lane >> 3) + 2 * (lane & 3) + ((lane >> 2) & 1);
   if (tk >= t.tokens) return;
   const uint64_t row = t.row0 + tk;
@@ -350,10 +388,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* acc_empty = acc_full + 1;
   uint64_t* drain = acc_empty + 1;
   uint64_t* drain_copies = drain + 1;
-  uint64_t* answer_full = drain_copies + 1;
-  uint64_t* answer_empty = answer_full + kQueue;  // the peer's is used
-  uint8_t* answers = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(answer_empty + kQueue) + 15) & ~uintptr_t(15));
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(answers + 16 * kQueue);
+  uint64_t* unit_full = drain_copies + 1;
+  uint64_t* unit_empty = unit_full + kQueue;  // the peer's is used
+  uint64_t* answer_in = unit_empty + kQueue;  // the peer's
+  Unit* queue = reinterpret_cast<Unit*>((reinterpret_cast<uintptr_t>(answer_in + 1) + 15) & ~uintptr_t(15));
+  uint8_t* answer = reinterpret_cast<uint8_t*>(queue + kQueue);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(answer + 16);
   __shared__ volatile int abort_flag;
   __shared__ int64_t warp_sum[kThreads / 32];
 
@@ -374,9 +414,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(acc_empty, 2 * kEpiWarps);
     mbar_init(drain, 1);
     mbar_init(drain_copies, 1);
+    mbar_init(answer_in, 1);
     for (int i = 0; i < kQueue; ++i) {
-      mbar_init(&answer_full[i], 1);
-      mbar_init(&answer_empty[i], 4 + 2 + 2 * kEpiWarps);  // the leader's four first warps, the peer's two
+      mbar_init(&unit_full[i], 1);
+      mbar_init(&unit_empty[i], 4 + 2 + 2 * kEpiWarps);  // the leader's four first warps, the peer's two
     }
     abort_flag = 0;
     fence_mbar_init();
@@ -391,8 +432,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   griddep_wait_and_release();
 
-  // The experts' rows and units: three experts a thread, summed over the CTA.
-  {
+  // The experts' rows and units, in the peer, which hands them out: three experts a thread, summed over the CTA.
+  if (!leader) {
     int64_t n[3], sum = 0;
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
@@ -423,7 +464,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncthreads();
   }
-  const int units = ends[kMoeMaxExperts - 1];
   const uint32_t tmem = *tmem_slot;
 
   auto fail = [&]() {
@@ -434,29 +474,27 @@ __global__ void __launch_bounds__(kThreads, 1)
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
     return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, &abort_flag)) != 0;
   };
-  // The next unit of the pair, to each of its warps by itself (n: its count of answers).  False: there is none, or, with
+  // The next unit of the pair, to each of its warps by itself (n: its count of them).  False: there is none, or, with
   // *ok false, the wait ran out.
-  auto next_unit = [&](int* u, int* n, bool* ok) {
+  auto next_unit = [&](Unit* t, int* n, bool* ok) {
     const int slot = *n % kQueue;
-    *ok = wait(&answer_full[slot], (*n / kQueue) & 1);
+    *ok = wait(&unit_full[slot], (*n / kQueue) & 1);
     if (!*ok) {
       fail();
       return false;
     }
     ++*n;
-    *u = __shfl_sync(0xffffffffu, taken_cluster(answers + 16 * slot), 0);
-    fence_proxy_async_smem();  // read here, then written by the next answer
-    __syncwarp();
-    if (lane == 0) arrive_relaxed(pair_address(&answer_empty[slot], 1));
-    return *u >= 0;
+    *t = queue[slot];
+    const bool some = __shfl_sync(0xffffffffu, t->tokens, 0) != 0;  // all lanes have read
+    if (lane == 0) arrive_relaxed(pair_address(&unit_empty[slot], 1));
+    return some;
   };
   // Walks the pair's units; body(unit) gives false where a wait ran out.
   auto walk_units = [&](auto&& body) {
-    int u = first_unit, n = 0;
+    Unit t;
+    int n = 0;
     bool ok = true;
-    do {
-      if (u < units) ok = body(find_unit(u, ends, expert_rows_s, lane));
-    } while (ok && next_unit(&u, &n, &ok));
+    while (ok && next_unit(&t, &n, &ok)) ok = body(t);
     return ok;
   };
   // A producer's walk; load(stage, kb, unit), in one lane, fills a stage once `free` says so.
@@ -585,25 +623,48 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == 2) {
     // ------------------------------------------------------ peer: the queue ---
     const bool issuer = elect_one();
-    for (int n = 0;; ++n) {
+    const int units = ends[kMoeMaxExperts - 1];
+    int n = 0;
+    // A unit to the pair's warps; false where the wait ran out.
+    auto hand_out = [&](const Unit& t) {
       const int slot = n % kQueue;
-      const uint32_t phase = (n / kQueue) & 1;
-      if (!wait(&answer_empty[slot], phase ^ 1u)) {
+      if (!wait(&unit_empty[slot], ((n / kQueue) & 1) ^ 1u)) {
         fail();
-        break;
+        return false;
       }
+      ++n;
+      if (issuer)
+#pragma unroll
+        for (uint32_t r = 0; r < 2; ++r) {
+          expect_in_pair(&unit_full[slot], r, sizeof(Unit));
+          send_16(&queue[slot].expert, &unit_full[slot], r, make_int4(t.expert, t.w_tile, t.row0, t.tokens));
+          send_16(&queue[slot].scale, &unit_full[slot], r,
+                  make_int4(__float_as_int(t.scale), __float_as_int(t.g_out), t.n, 0));
+        }
+      __syncwarp();
+      return true;
+    };
+    uint32_t phase = 0;
+    for (int u = first_unit;;) {
+      // The next unit is asked for while this one is handed out.
       if (issuer) {
-        expect_in_pair(&answer_full[slot], 0, 16);
-        expect_in_pair(&answer_full[slot], 1, 16);
-        take_cluster(answers + 16 * slot, &answer_full[slot]);
+        mbar_arrive_expect_tx(answer_in, 16);
+        take_cluster(answer, answer_in);
       }
       __syncwarp();
-      if (!wait(&answer_full[slot], phase)) {
+      const bool out = u >= units || hand_out(find_unit(a, u, ends, expert_rows_s, lane));
+      if (!wait(answer_in, phase)) {
         fail();
         break;
       }
-      // Asking again after the queue was found empty is not allowed.
-      if (__shfl_sync(0xffffffffu, taken_cluster(answers + 16 * slot), 0) < 0) break;
+      phase ^= 1u;
+      u = __shfl_sync(0xffffffffu, taken_cluster(answer), 0);
+      fence_proxy_async_smem();  // read here, then written by the next answer
+      if (!out) break;
+      if (u < 0) {  // asking again is not allowed
+        hand_out(Unit{});
+        break;
+      }
     }
   } else if (warp >= kEpi0) {
     // ----------------------------------------------------------- epilogue ---
@@ -613,8 +674,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t buf = smem_u32(buf_ptr);
     int local = 0;
     auto finish = [&](const Unit& t) {
-      const float scale =
-          a.g_a ? __fmul_rn(__ldg(a.g_a + static_cast<int64_t>(t.expert) * a.g_a_step), __ldg(a.g_w + t.expert)) : 1.0f;
       // Lane 0 waits and tells, so that the warp stays converged.
       int ok = 1;
       if (lane == 0) {
@@ -646,34 +705,20 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int token0 = 32 * (2 * i + side);
-          if (token0 < t.tokens && n0 < a.N) store_rows(a, t, lo[i], hi[i], token0, n0, scale, buf, lane);
+          if (token0 < t.tokens && n0 < a.N) store_rows(a, t, lo[i], hi[i], token0, n0, buf, lane);
         }
       } else if constexpr (kMode == 1) {
-        const float g_in = __ldg(a.g_out + static_cast<int64_t>(t.expert) * a.g_out_step);
-        const bool g_ok = g_in > 0.0f && g_in <= FLT_MAX;
+        const bool g_ok = t.g_out > 0.0f && t.g_out <= FLT_MAX;
         if (!g_ok && lane == 0) set_status(a.status, NVFP4_ERR_INVALID_ARG);
-        const float g = g_ok ? g_in : 1.0f, six_g = __fmul_rn(6.0f, g);
+        const float g = g_ok ? t.g_out : 1.0f, six_g = __fmul_rn(6.0f, g);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int token0 = 32 * (2 * i + side);
           if (token0 >= t.tokens) continue;
-          swiglu_fragments(lo[i], hi[i], scale);
-          uint2 codes = make_uint2(0, 0);
-          uint32_t code = 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const BlockScale b = block_scale(token_amax(lo[i] + 4 * j, lane), g, six_g);
-            const uint2 c = token_codes(lo[i] + 4 * j, b.mult, lane);
-            if (lane >> 3 == j) {
-              codes = c;
-              code = b.code;
-            }
-          }
-          if (!g_ok) {
-            codes = make_uint2(0, 0);
-            code = 0;
-          }
-          store_codes(a, t, codes, code, token0, n0 >> 1, lane);
+          swiglu_fragments(lo[i], hi[i], t.scale);
+          const BlockScale b = block_scale(token_amax(lo[i], lane), g, six_g);
+          const uint2 codes = token_codes(lo[i], b.mult, lane);
+          store_codes(a, t, g_ok ? codes : make_uint2(0, 0), g_ok ? b.code : 0u, token0, n0 >> 1, lane);
         }
       } else {
         float* mine = reinterpret_cast<float*>(buf_ptr);
@@ -682,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < 4; ++i) {
           const int token0 = 32 * (2 * i + side);
           if (token0 >= t.tokens) continue;
-          swiglu_fragments(lo[i], hi[i], scale);
+          swiglu_fragments(lo[i], hi[i], t.scale);
           if (a.rotate) {
             // H_32 / sqrt(32) over the outputs: strides 1, 2, 4 across lanes, 8 in the thread, 16 across the two warps,
             // in this order, as hadamard32.
@@ -715,36 +760,23 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             meet(meeting);
           }
-          float amax[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            amax[j] = token_amax(lo[i] + 4 * j, lane);
-            if (lane < 8) mine[8 * j + lane] = amax[j];
-          }
+          const float amax = token_amax(lo[i], lane);
+          mine[lane] = amax;
           meet(meeting);
-          uint2 codes = make_uint2(0, 0);
-          uint32_t code = 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t c = mx_scale_code(fmaxf(amax[j], theirs[8 * j + (lane & 7)]));
-            const uint2 w = token_codes(lo[i] + 4 * j, mx_inv_scale(c), lane);
-            if (lane >> 3 == j) {
-              codes = w;
-              code = c;
-            }
-          }
+          const uint32_t code = mx_scale_code(fmaxf(amax, theirs[lane]));
           meet(meeting);
-          store_codes(a, t, codes, code, token0, n0 >> 1, lane);
+          store_codes(a, t, token_codes(lo[i], mx_inv_scale(code), lane), code, token0, n0 >> 1, lane);
         }
       }
       return true;
     };
-    int u = first_unit, n = 0;
+    Unit t;
+    int n = 0;
     bool ok = true, more = true;
     while (more) {
-      if (u < units && !finish(find_unit(u, ends, expert_rows_s, lane))) break;
-      more = next_unit(&u, &n, &ok);
+      more = next_unit(&t, &n, &ok);
       if (kMode == 2 && !both(meeting, ok)) break;
+      if (more && !finish(t)) break;
     }
   }
 
