@@ -237,27 +237,21 @@ __device__ __forceinline__ void meet(int id) { asm volatile("barrier.cta.sync %0
 struct Unit {
   int expert, w_tile;
   int row0, tokens;  // first row, rows of the tile; tokens 0: there is no unit
-  float scale, g_out;
-  int n;  // the MMA's N: tokens up to a multiple of 32
-  int unused;
+  __device__ __forceinline__ int n() const { return (tokens + 31) & ~31; }  // the MMA's N
 };
-static_assert(sizeof(Unit) == 32, "two 16-byte words");
+static_assert(sizeof(Unit) == 16, "one store of the queue");
 // Unit u, by a converged warp.  ends: [1024] units of the experts up to each one, the total behind the last one.
-__device__ __forceinline__ Unit find_unit(const GroupedArgs& a, int u, const int* ends, const int2* rows, int lane) {
+__device__ __forceinline__ Unit find_unit(int u, const int* ends, const int2* rows, int lane) {
   const int block = __popc(__ballot_sync(0xffffffffu, ends[32 * lane + 31] <= u));
   const int e = 32 * block + __popc(__ballot_sync(0xffffffffu, ends[32 * block + lane] <= u));
   const int2 r = rows[e];  // first row, rows
-  Unit t;
-  t.scale = a.g_a ? __fmul_rn(__ldg(a.g_a + static_cast<int64_t>(e) * a.g_a_step), __ldg(a.g_w + e)) : 1.0f;
-  t.g_out = a.g_out ? __ldg(a.g_out + static_cast<int64_t>(e) * a.g_out_step) : 0.0f;
   const int local = u - (e ? ends[e - 1] : 0), tiles = (r.y + kTokens - 1) / kTokens;
+  Unit t;
   t.expert = e;
   t.w_tile = local / tiles;
   const int token_tile = local - t.w_tile * tiles;
   t.row0 = r.x + token_tile * kTokens;
   t.tokens = min(kTokens, r.y - token_tile * kTokens);
-  t.n = (t.tokens + 31) & ~31;
-  t.unused = 0;
   return t;
 }
 
@@ -265,8 +259,8 @@ __device__ __forceinline__ Unit find_unit(const GroupedArgs& a, int u, const int
 // lo, hi: the fragments of a warp's weight rows 0..15 and 16..31, 32 tokens from token0.
 
 __device__ __forceinline__ void store_rows(const GroupedArgs& a, const Unit& t, const uint32_t* lo, const uint32_t* hi,
-                                           int token0, int n0, uint32_t buf, int lane) {
-  auto f = [&](uint32_t v) { return __uint_as_float(v) * t.scale; };
+                                           int token0, int n0, float scale, uint32_t buf, int lane) {
+  auto f = [&](uint32_t v) { return __uint_as_float(v) * scale; };
   // Rows of 64 bytes in 16-byte chunks, chunk c of token t at c ^ (t / 2) % 4: no bank twice, written or read.
   const uint32_t put = buf + (lane & 7) * 64 + (((lane >> 3) ^ ((lane >> 1) & 3)) << 4);
 #pragma unroll
@@ -432,8 +426,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   griddep_wait_and_release();
 
-  // The experts' rows and units, in the peer, which hands them out: three experts a thread, summed over the CTA.
-  if (!leader) {
+  // The experts' rows and units: three experts a thread, summed over the CTA.
+  {
     int64_t n[3], sum = 0;
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
@@ -464,6 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncthreads();
   }
+  const int units = ends[kMoeMaxExperts - 1];
   const uint32_t tmem = *tmem_slot;
 
   auto fail = [&]() {
@@ -489,12 +484,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) arrive_relaxed(pair_address(&unit_empty[slot], 1));
     return some;
   };
-  // Walks the pair's units; body(unit) gives false where a wait ran out.
+  // Walks the pair's units, the first one found without the queue; body(unit) gives false where a wait ran out.
   auto walk_units = [&](auto&& body) {
-    Unit t;
+    if (first_unit >= units) return true;
+    Unit t = find_unit(first_unit, ends, expert_rows_s, lane);
     int n = 0;
     bool ok = true;
-    while (ok && next_unit(&t, &n, &ok)) ok = body(t);
+    do ok = body(t);
+    while (ok && next_unit(&t, &n, &ok));
     return ok;
   };
   // A producer's walk; load(stage, kb, unit), in one lane, fills a stage once `free` says so.
@@ -521,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 0) {
     // -------------------------------------------------------------- codes ---
     produce(empty, [&](int stage, int kb, const Unit& t) {
-      const int half = t.n / 2;  // this CTA's tokens: `half` of them from rank * half
+      const int half = t.n() / 2;  // this CTA's tokens: `half` of them from rank * half
       const int box = half <= 16 ? 16 : half <= 64 ? 64 : 128;
       const CUtensorMap* map = half <= 16 ? &map_x16 : half <= 64 ? &map_x64 : &map_x128;
       if (leader) mbar_arrive_expect_tx(&full[stage], 2 * (kWBytes + box * (kDepth / 2)));
@@ -535,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // A stage's buffers are free once the copies have read them (`full`).
     const int tile_rows = a.K / 32;
     produce(full, [&](int stage, int kb, const Unit& t) {
-      const bool two = t.n > 128;
+      const bool two = t.n() > 128;
       if (leader) mbar_arrive_expect_tx(&scales_in[stage], 2 * (two ? 3 : 2) * kScaleTile);
       load_box(sWS + stage * kScaleTile, &map_w_scales, &scales_in[stage], 0,
                (t.expert * a.w_scale_tiles + t.w_tile * 2 + static_cast<int>(rank)) * tile_rows + kb * 8);
@@ -554,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t w_desc0 = tile_desc(smem_u32(sW)), x_desc0 = tile_desc(smem_u32(sX));
     bool ready = false;  // the next stage was seen full
     walk_units([&](const Unit& t) {
-      const uint32_t idesc = kIdesc | static_cast<uint32_t>(t.n >> 3) << 17 | (a.mx ? kUE8M0 : 0u);
+      const uint32_t idesc = kIdesc | static_cast<uint32_t>(t.n() >> 3) << 17 | (a.mx ? kUE8M0 : 0u);
       if (!wait(acc_empty, (local & 1) ^ 1u)) {
         fail();
         return false;
@@ -610,7 +607,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int kk = 0; kk < 4; ++kk) {
             pair_copy_scales(ws + kk * 4, ws_desc + kk * (512 >> 4));
             pair_copy_scales(xs + kk * 8, xs_desc + kk * (512 >> 4));
-            if (t.n > 128) pair_copy_scales(xs + kk * 8 + 4, xs_desc + (kScaleTile + kk * 512) / 16);
+            if (t.n() > 128) pair_copy_scales(xs + kk * 8 + 4, xs_desc + (kScaleTile + kk * 512) / 16);
           }
           pair_commit(&full[stage], 0x3);
         }
@@ -622,49 +619,49 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_wait_bounded(drain_copies, 0, nullptr);
   } else if (warp == 2) {
     // ------------------------------------------------------ peer: the queue ---
+    // Cluster c of `clusters` has the units c, c + clusters, ...  The next cluster is asked for while one's units are
+    // handed out to the pair's warps.
     const bool issuer = elect_one();
-    const int units = ends[kMoeMaxExperts - 1];
+    const int clusters = gridDim.x / 2;
     int n = 0;
-    // A unit to the pair's warps; false where the wait ran out.
-    auto hand_out = [&](const Unit& t) {
-      const int slot = n % kQueue;
-      if (!wait(&unit_empty[slot], ((n / kQueue) & 1) ^ 1u)) {
-        fail();
-        return false;
-      }
-      ++n;
-      if (issuer)
-#pragma unroll
-        for (uint32_t r = 0; r < 2; ++r) {
-          expect_in_pair(&unit_full[slot], r, sizeof(Unit));
-          send_16(&queue[slot].expert, &unit_full[slot], r, make_int4(t.expert, t.w_tile, t.row0, t.tokens));
-          send_16(&queue[slot].scale, &unit_full[slot], r,
-                  make_int4(__float_as_int(t.scale), __float_as_int(t.g_out), t.n, 0));
-        }
-      __syncwarp();
-      return true;
-    };
-    uint32_t phase = 0;
-    for (int u = first_unit;;) {
-      // The next unit is asked for while this one is handed out.
+    bool ok = true;
+    auto ask = [&]() {
       if (issuer) {
         mbar_arrive_expect_tx(answer_in, 16);
         take_cluster(answer, answer_in);
       }
       __syncwarp();
-      const bool out = u >= units || hand_out(find_unit(a, u, ends, expert_rows_s, lane));
-      if (!wait(answer_in, phase)) {
+    };
+    auto hand_out = [&](const Unit& t) {
+      const int slot = n % kQueue;
+      ok = ok && wait(&unit_empty[slot], ((n / kQueue) & 1) ^ 1u);
+      if (ok && issuer)
+#pragma unroll
+        for (uint32_t r = 0; r < 2; ++r) {
+          expect_in_pair(&unit_full[slot], r, sizeof(Unit));
+          send_16(&queue[slot], &unit_full[slot], r, make_int4(t.expert, t.w_tile, t.row0, t.tokens));
+        }
+      __syncwarp();
+      ++n;
+    };
+    uint32_t phase = 0;
+    ask();
+    for (int64_t u = static_cast<int64_t>(first_unit) + clusters;;) {
+      for (; ok && u < units; u += clusters) hand_out(find_unit(static_cast<int>(u), ends, expert_rows_s, lane));
+      ok = wait(answer_in, phase) && ok;  // after a failure too: the answer is on its way
+      phase ^= 1u;
+      if (!ok) {
         fail();
         break;
       }
-      phase ^= 1u;
       u = __shfl_sync(0xffffffffu, taken_cluster(answer), 0);
       fence_proxy_async_smem();  // read here, then written by the next answer
-      if (!out) break;
-      if (u < 0) {  // asking again is not allowed
-        hand_out(Unit{});
+      if (u < 0) {  // none is left; asking again is not allowed
+        if (first_unit < units) hand_out(Unit{});
+        if (!ok) fail();
         break;
       }
+      ask();
     }
   } else if (warp >= kEpi0) {
     // ----------------------------------------------------------- epilogue ---
@@ -674,6 +671,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t buf = smem_u32(buf_ptr);
     int local = 0;
     auto finish = [&](const Unit& t) {
+      const float scale =
+          a.g_a ? __fmul_rn(__ldg(a.g_a + static_cast<int64_t>(t.expert) * a.g_a_step), __ldg(a.g_w + t.expert)) : 1.0f;
+      const float g_in = kMode == 1 ? __ldg(a.g_out + static_cast<int64_t>(t.expert) * a.g_out_step) : 1.0f;
       // Lane 0 waits and tells, so that the warp stays converged.
       int ok = 1;
       if (lane == 0) {
@@ -705,17 +705,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int token0 = 32 * (2 * i + side);
-          if (token0 < t.tokens && n0 < a.N) store_rows(a, t, lo[i], hi[i], token0, n0, buf, lane);
+          if (token0 < t.tokens && n0 < a.N) store_rows(a, t, lo[i], hi[i], token0, n0, scale, buf, lane);
         }
       } else if constexpr (kMode == 1) {
-        const bool g_ok = t.g_out > 0.0f && t.g_out <= FLT_MAX;
+        const bool g_ok = g_in > 0.0f && g_in <= FLT_MAX;
         if (!g_ok && lane == 0) set_status(a.status, NVFP4_ERR_INVALID_ARG);
-        const float g = g_ok ? t.g_out : 1.0f, six_g = __fmul_rn(6.0f, g);
+        const float g = g_ok ? g_in : 1.0f, six_g = __fmul_rn(6.0f, g);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int token0 = 32 * (2 * i + side);
           if (token0 >= t.tokens) continue;
-          swiglu_fragments(lo[i], hi[i], t.scale);
+          swiglu_fragments(lo[i], hi[i], scale);
           const BlockScale b = block_scale(token_amax(lo[i], lane), g, six_g);
           const uint2 codes = token_codes(lo[i], b.mult, lane);
           store_codes(a, t, g_ok ? codes : make_uint2(0, 0), g_ok ? b.code : 0u, token0, n0 >> 1, lane);
@@ -727,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < 4; ++i) {
           const int token0 = 32 * (2 * i + side);
           if (token0 >= t.tokens) continue;
-          swiglu_fragments(lo[i], hi[i], t.scale);
+          swiglu_fragments(lo[i], hi[i], scale);
           if (a.rotate) {
             // H_32 / sqrt(32) over the outputs: strides 1, 2, 4 across lanes, 8 in the thread, 16 across the two warps,
             // in this order, as hadamard32.
@@ -770,13 +770,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       return true;
     };
-    Unit t;
+    Unit t = {};
     int n = 0;
-    bool ok = true, more = true;
-    while (more) {
+    bool ok = true, more = first_unit < units;
+    if (more) t = find_unit(first_unit, ends, expert_rows_s, lane);
+    while (more && finish(t)) {
       more = next_unit(&t, &n, &ok);
       if (kMode == 2 && !both(meeting, ok)) break;
-      if (more && !finish(t)) break;
     }
   }
 
@@ -856,6 +856,10 @@ nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s
   const int64_t units = (choices + (kTokens - 1) * used) / kTokens * a.w_tiles;  // at most
   if (units >= (1ll << 30)) return NVFP4_ERR_SHAPE;
   a.max_units = static_cast<int>(units);
+  // Clusters for about as many as there are, were half of the experts' last tiles none: one too many is asked for in
+  // vain, one too few gives the first clusters two units.
+  const int64_t about = (choices / kTokens + used / 2) * a.w_tiles, least = 2ll * sm_count();
+  const int64_t clusters = units < least ? units : about < least ? least : about < units ? about : units;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2;
@@ -878,7 +882,7 @@ nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s
     return NVFP4_ERR_CUDA;
   a.status = status_word_dev();
   a.fault_skip_stage = take_fault(NVFP4_FAULT_GEMM_SKIP_STAGE) ? 1 : 0;
-  cfg.gridDim = dim3(static_cast<uint32_t>(2 * units), 1, 1);
+  cfg.gridDim = dim3(static_cast<uint32_t>(2 * clusters), 1, 1);
   cfg.stream = s;
   cfg.numAttrs = 2;
   if (cudaLaunchKernelEx(&cfg, grouped_kernel<kMode>, w, ws, x16, x64, x128, xs, xs2, a) != cudaSuccess)
