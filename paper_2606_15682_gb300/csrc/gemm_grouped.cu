@@ -384,7 +384,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* drain_copies = drain + 1;
   uint64_t* unit_full = drain_copies + 1;
   uint64_t* unit_empty = unit_full + kQueue;  // the peer's is used
-  uint64_t* answer_in = unit_empty + kQueue;  // the peer's
+  uint64_t* unit_begun = unit_empty + kQueue;  // the peer's: its first load is about to be issued
+  uint64_t* answer_in = unit_begun + kQueue;   // the peer's
   Unit* queue = reinterpret_cast<Unit*>((reinterpret_cast<uintptr_t>(answer_in + 1) + 15) & ~uintptr_t(15));
   uint8_t* answer = reinterpret_cast<uint8_t*>(queue + kQueue);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(answer + 16);
@@ -412,6 +413,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < kQueue; ++i) {
       mbar_init(&unit_full[i], 1);
       mbar_init(&unit_empty[i], 4 + 2 + 2 * kEpiWarps);  // the leader's four first warps, the peer's two
+      mbar_init(&unit_begun[i], 1);
     }
     abort_flag = 0;
     fence_mbar_init();
@@ -481,7 +483,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     ++*n;
     *t = queue[slot];
     const bool some = __shfl_sync(0xffffffffu, t->tokens, 0) != 0;  // all lanes have read
-    if (lane == 0) arrive_relaxed(pair_address(&unit_empty[slot], 1));
+    if (lane == 0) {
+      arrive_relaxed(pair_address(&unit_empty[slot], 1));
+      if (leader && warp == 0) arrive_relaxed(pair_address(&unit_begun[slot], 1));
+    }
     return some;
   };
   // Walks the pair's units, the first one found without the queue; body(unit) gives false where a wait ran out.
@@ -619,8 +624,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_wait_bounded(drain_copies, 0, nullptr);
   } else if (warp == 2) {
     // ------------------------------------------------------ peer: the queue ---
-    // Cluster c of `clusters` has the units c, c + clusters, ...  The next cluster is asked for while one's units are
-    // handed out to the pair's warps.
+    // Cluster c of `clusters` has the units c, c + clusters, ...  A pair asks for units only so far ahead that its loads
+    // never wait for one, some 8 k-blocks: with more, the first pairs take them all (224 units on 76 pairs: 2 to 4 each).
+    const int ahead = max(1, min(kQueue - 1, 8 / kblocks));
     const bool issuer = elect_one();
     const int clusters = gridDim.x / 2;
     int n = 0;
@@ -642,13 +648,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           send_16(&queue[slot], &unit_full[slot], r, make_int4(t.expert, t.w_tile, t.row0, t.tokens));
         }
       __syncwarp();
-      ++n;
+      const int old = ++n - ahead;
+      if (old >= 0) ok = ok && wait(&unit_begun[old % kQueue], (old / kQueue) & 1);
     };
     uint32_t phase = 0;
-    ask();
     for (int64_t u = static_cast<int64_t>(first_unit) + clusters;;) {
       for (; ok && u < units; u += clusters) hand_out(find_unit(static_cast<int>(u), ends, expert_rows_s, lane));
-      ok = wait(answer_in, phase) && ok;  // after a failure too: the answer is on its way
+      if (!ok) {
+        fail();
+        break;
+      }
+      ask();
+      ok = wait(answer_in, phase);
       phase ^= 1u;
       if (!ok) {
         fail();
@@ -661,7 +672,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) fail();
         break;
       }
-      ask();
     }
   } else if (warp >= kEpi0) {
     // ----------------------------------------------------------- epilogue ---
