@@ -882,13 +882,15 @@ nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s
   cfg.dynamicSmemBytes = kSmem;
   cfg.attrs = attr;
   if (!opted_in<kMode>()) return NVFP4_ERR_CUDA;
-  CUtensorMap w, ws, x16, x64, x128, xs, xs2;
+  CUtensorMap w, ws, x16, x64 = {}, x128 = {}, xs, xs2 = {};
   const int64_t R = a.max_rows, K = a.K;
+  // No tile has more tokens than there are choices: few need no map of the larger boxes.
+  const bool mid = choices > 32, wide = choices > 128;
   if (!codes_map(&w, a.w_codes, static_cast<int64_t>(a.experts) * a.N, K, 128) ||
       !scales_map(&ws, a.w_scales, static_cast<int64_t>(a.experts) * a.w_scale_tiles, K, false) ||
-      !codes_map(&x16, a.a_codes, R, K, 16) || !codes_map(&x64, a.a_codes, R, K, 64) ||
-      !codes_map(&x128, a.a_codes, R, K, 128) || !scales_map(&xs, a.a_scales, R / 128, K, false) ||
-      !scales_map(&xs2, a.a_scales, R / 128, K, true))
+      !codes_map(&x16, a.a_codes, R, K, 16) || (mid && !codes_map(&x64, a.a_codes, R, K, 64)) ||
+      (wide && !codes_map(&x128, a.a_codes, R, K, 128)) || !scales_map(&xs, a.a_scales, R / 128, K, false) ||
+      (wide && !scales_map(&xs2, a.a_scales, R / 128, K, true)))
     return NVFP4_ERR_CUDA;
   a.status = status_word_dev();
   a.fault_skip_stage = take_fault(NVFP4_FAULT_GEMM_SKIP_STAGE) ? 1 : 0;

@@ -141,16 +141,17 @@ _mx_linear_swiglu = _sig("mxfp4_linear_swiglu_quantize", [_p, _p, _p, _p, _i64, 
 
 
 # The current stream's raw handle without building a torch.cuda.Stream object
-# (0.1 us instead of ~3 us per call); the public call where it is absent.
+# (0.1 us instead of ~3 us per call); the public calls where these are absent.
 _raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream):
     if stream is None:
-        if _raw_current_stream is not None:
-            return ctypes.c_void_p(_raw_current_stream(torch.cuda.current_device()))
+        if _raw_current_stream is not None and torch.cuda.is_initialized():
+            return _raw_current_stream(_raw_current_device())
         stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _ptr(t):
@@ -328,7 +329,7 @@ def _typed(t, dtype, what, numel=None):
     """Device pointer of a dense argument whose element type the call fixes; None -> NULL."""
     if t is None:
         return None
-    if t.dtype is not dtype or not t.is_contiguous() or (numel is not None and t.numel() != numel):
+    if t.dtype is not dtype or (numel is not None and t.numel() != numel) or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous {dtype}" + ("" if numel is None else f" with {numel} elements"))
     return t.data_ptr()
 
