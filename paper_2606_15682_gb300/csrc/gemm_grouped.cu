@@ -258,15 +258,31 @@ __device__ __forceinline__ Unit find_unit(int u, const int* ends, const int2* ro
 // --------------------------------------------------------------- epilogue ---
 // lo, hi: the fragments of a warp's weight rows 0..15 and 16..31, 32 tokens from token0.
 
-__device__ __forceinline__ void store_rows(const GroupedArgs& a, const Unit& t, const uint32_t* lo, const uint32_t* hi,
+__device__ __forceinline__ void store_rows(const GroupedArgs& a, const void* map_out, const Unit& t, const uint32_t* lo, const uint32_t* hi,
                                            int token0, int n0, float scale, uint32_t buf, int lane) {
   auto f = [&](uint32_t v) { return __uint_as_float(v) * scale; };
   // Rows of 64 bytes in 16-byte chunks, chunk c of token t at c ^ (t / 2) % 4: no bank twice, written or read.
+  // That is also the 64-byte swizzle of a box of 32 x 32, which goes out by itself while the warp turns to the next; rows
+  // that are fewer go out by the lanes.
+  if (lane == 0) bulk_wait_read_all();  // the last box has left the buffer
+  __syncwarp();
   const uint32_t put = buf + (lane & 7) * 64 + (((lane >> 3) ^ ((lane >> 1) & 3)) << 4);
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     stmatrix_t(put + j * 512, pack_pair(f(lo[4 * j]), f(lo[4 * j + 1])), pack_pair(f(lo[4 * j + 2]), f(lo[4 * j + 3])),
                pack_pair(f(hi[4 * j]), f(hi[4 * j + 1])), pack_pair(f(hi[4 * j + 2]), f(hi[4 * j + 3])));
+  if (token0 + 32 <= t.tokens) {
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0 && in_bounds(a.status, t.row0 + token0 + 32 <= a.max_rows)) {
+      asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                       reinterpret_cast<uint64_t>(map_out)),
+                   "r"(buf), "r"(n0), "r"(t.row0 + token0)
+                   : "memory");
+      bulk_commit_group();
+    }
+    return;
+  }
   __syncwarp();
   const int c = lane & 3, n = n0 + 8 * c, tk0 = lane >> 2;
   const uint32_t get = buf + tk0 * 64 + ((c ^ ((tk0 >> 1) & 3)) << 4);
@@ -365,7 +381,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     grouped_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_w_scales,
                    const __grid_constant__ CUtensorMap map_x16, const __grid_constant__ CUtensorMap map_x64,
                    const __grid_constant__ CUtensorMap map_x128, const __grid_constant__ CUtensorMap map_x_scales,
-                   const __grid_constant__ CUtensorMap map_x_scales2, const GroupedArgs a) {
+                   const __grid_constant__ CUtensorMap map_x_scales2, const __grid_constant__ CUtensorMap map_out,
+                   const GroupedArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sW = smem;
@@ -715,7 +732,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int token0 = 32 * (2 * i + side);
-          if (token0 < t.tokens && n0 < a.N) store_rows(a, t, lo[i], hi[i], token0, n0, scale, buf, lane);
+          if (token0 < t.tokens && n0 < a.N) store_rows(a, &map_out, t, lo[i], hi[i], token0, n0, scale, buf, lane);
         }
       } else if constexpr (kMode == 1) {
         const bool g_ok = g_in > 0.0f && g_in <= FLT_MAX;
@@ -788,6 +805,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       more = next_unit(&t, &n, &ok);
       if (kMode == 2 && !both(meeting, ok)) break;
     }
+    if (kMode == 0 && lane == 0) bulk_wait_all();
   }
 
   tc_fence_before();
@@ -825,6 +843,16 @@ bool codes_map(CUtensorMap* map, const uint8_t* base, int64_t rows, int64_t K, u
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(K / 2)};
   const cuuint32_t box[2] = {kDepth / 2, box_rows};
   return encode(map, base, 2, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// bf16 [rows, N], rows ldo apart, boxes of 32 x 32.
+bool out_map(CUtensorMap* map, void* base, int64_t rows, int64_t N, int64_t ldo) {
+  const auto enc = encoder();
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ldo * 2)};
+  const cuuint32_t box[2] = {32, 32}, steps[2] = {1, 1};
+  return enc && enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, steps,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // Block scales in the tensor core's order, `tiles` tiles of 128 rows, as rows of 256 bytes, K / 32 of them a tile: boxes of
 // one (tile, k-block), or of two tiles.
@@ -882,7 +910,7 @@ nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s
   cfg.dynamicSmemBytes = kSmem;
   cfg.attrs = attr;
   if (!opted_in<kMode>()) return NVFP4_ERR_CUDA;
-  CUtensorMap w, ws, x16, x64 = {}, x128 = {}, xs, xs2 = {};
+  CUtensorMap w, ws, x16, x64 = {}, x128 = {}, xs, xs2 = {}, out = {};
   const int64_t R = a.max_rows, K = a.K;
   // No tile has more tokens than there are choices: few need no map of the larger boxes.
   const bool mid = choices > 32, wide = choices > 128;
@@ -890,14 +918,16 @@ nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s
       !scales_map(&ws, a.w_scales, static_cast<int64_t>(a.experts) * a.w_scale_tiles, K, false) ||
       !codes_map(&x16, a.a_codes, R, K, 16) || (mid && !codes_map(&x64, a.a_codes, R, K, 64)) ||
       (wide && !codes_map(&x128, a.a_codes, R, K, 128)) || !scales_map(&xs, a.a_scales, R / 128, K, false) ||
-      (wide && !scales_map(&xs2, a.a_scales, R / 128, K, true)))
+      (wide && !scales_map(&xs2, a.a_scales, R / 128, K, true)) ||
+      (kMode == 0 && !out_map(&out, a.out, R, a.N, a.ldo)))
     return NVFP4_ERR_CUDA;
   a.status = status_word_dev();
   a.fault_skip_stage = take_fault(NVFP4_FAULT_GEMM_SKIP_STAGE) ? 1 : 0;
   cfg.gridDim = dim3(static_cast<uint32_t>(2 * clusters), 1, 1);
   cfg.stream = s;
   cfg.numAttrs = 2;
-  if (cudaLaunchKernelEx(&cfg, grouped_kernel<kMode>, w, ws, x16, x64, x128, xs, xs2, a) != cudaSuccess)
+  if (cudaLaunchKernelEx(&cfg, grouped_kernel<kMode>, w, ws, x16, x64, x128, xs, xs2, out, a) !=
+      cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
   return launch_status();
