@@ -19,7 +19,7 @@
 //   warp 1      leader: MMAs; peer: block scales
 //   warp 2      leader: block scales into TMEM; peer: the queue of units
 //   warp 3      leader: block scales
-//   warps 4-11  epilogue: 32 weight rows x every other 32 tokens each
+//   warps 4-    epilogue: 32 weight rows x every second (of 8 warps) or fourth (of 16) 32 tokens each
 // The epilogue reads 16 x 8 fragments of D (16x256b), in which a thread has two tokens
 // of two weight rows, and of gate and up at once: bf16 rows are turned into token-major
 // ones by a transposing stmatrix, quantized outputs need shuffles only.
@@ -40,18 +40,28 @@ constexpr int kDepth = 256;  // elements of K per stage: 128 bytes of a row
 constexpr int kStages = 5;
 constexpr int kTokens = 256;  // of a tile
 constexpr int kWRows = 256;
-constexpr int kEpi0 = 4, kEpiWarps = 8;
-constexpr int kThreads = 32 * (kEpi0 + kEpiWarps);
+constexpr int kEpi0 = 4;
 constexpr int kQueue = 4;  // units on their way to the warps
 constexpr uint32_t kWBytes = 128 * kDepth / 2, kXBytes = 128 * kDepth / 2;  // a CTA's codes of a stage
 constexpr uint32_t kScaleTile = 128 * kDepth / 16;                         // block scales of 128 rows: four atoms
 constexpr uint32_t kEpiBytes = 2048;                                       // a warp's 32 tokens x 32 bf16
 constexpr uint32_t kTmemCols = 512, kSfCol = kTokens, kSfCols = 16 + 32;
-constexpr size_t kSmem = 1024 + kStages * (kWBytes + kXBytes + 3 * kScaleTile) + kEpiWarps * kEpiBytes +
-                         kMoeMaxExperts * (sizeof(int) + sizeof(int2)) + 512;
 static_assert(kSfCol + kStages * kSfCols <= kTmemCols, "TMEM budget");
-static_assert(kSmem <= 227 * 1024, "shared memory budget");
-static_assert(3 * kThreads >= kMoeMaxExperts, "three experts a thread");
+
+// 0 bf16 rows, 1 SwiGLU to NVFP4, 2 SwiGLU to MXFP4.  The first and the last have 8 epilogue warps with 128 accumulator
+// registers a thread.  The second needs no shared memory and is bound by its own latency where K is short: 16 warps with 64.
+template <int kMode>
+struct Form {
+  static constexpr int kEpiWarps = kMode == 1 ? 16 : 8;
+  static constexpr int kThreads = 32 * (kEpi0 + kEpiWarps);
+  static constexpr int kSides = kEpiWarps / 4;      // warps with the same weight rows
+  static constexpr int kChunks = 8 / kSides;        // of 32 tokens, a warp's
+  static constexpr int kEpiSmem = kMode == 1 ? 0 : kEpiWarps * static_cast<int>(kEpiBytes);
+  static constexpr int kPer = (kMoeMaxExperts + kThreads - 1) / kThreads;  // experts of a thread
+  static constexpr size_t kSmem = 1024 + kStages * (kWBytes + kXBytes + 3 * kScaleTile) + kEpiSmem +
+                                  kMoeMaxExperts * (sizeof(int) + sizeof(int2)) + 512;
+  static_assert(kSmem <= 227 * 1024, "shared memory budget");
+};
 // kind::mxf4nvf4: A and B packed E2M1, K-major; M = 256.  N >> 3 is added at bit 17, UE8M0 scales set bit 23.
 constexpr uint32_t kIdesc = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kWRows >> 4) << 24);
 constexpr uint32_t kUE8M0 = 1u << 23;
@@ -375,14 +385,14 @@ __device__ __forceinline__ void store_codes(const GroupedArgs& a, const Unit& t,
   a.q_scales[off] = static_cast<uint8_t>(code);
 }
 
-// kMode: 0 bf16 rows, 1 SwiGLU to NVFP4, 2 SwiGLU to MXFP4.
 template <int kMode>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
     grouped_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_w_scales,
                    const __grid_constant__ CUtensorMap map_x16, const __grid_constant__ CUtensorMap map_x64,
                    const __grid_constant__ CUtensorMap map_x128, const __grid_constant__ CUtensorMap map_x_scales,
                    const __grid_constant__ CUtensorMap map_x_scales2, const __grid_constant__ CUtensorMap map_out,
                    const GroupedArgs a) {
+  using F = Form<kMode>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sW = smem;
@@ -390,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* sWS = sX + kStages * kXBytes;
   uint8_t* sXS = sWS + kStages * kScaleTile;
   uint8_t* sEpi = sXS + kStages * 2 * kScaleTile;
-  int2* expert_rows_s = reinterpret_cast<int2*>(sEpi + kEpiWarps * kEpiBytes);
+  int2* expert_rows_s = reinterpret_cast<int2*>(sEpi + F::kEpiSmem);
   int* ends = reinterpret_cast<int*>(expert_rows_s + kMoeMaxExperts);
   uint64_t* full = reinterpret_cast<uint64_t*>(ends + kMoeMaxExperts);  // codes landed, scales in TMEM
   uint64_t* empty = full + kStages;                                    // the stage's MMAs are done
@@ -407,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* answer = reinterpret_cast<uint8_t*>(queue + kQueue);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(answer + 16);
   __shared__ volatile int abort_flag;
-  __shared__ int64_t warp_sum[kThreads / 32];
+  __shared__ int64_t warp_sum[F::kThreads / 32];
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int kblocks = a.K / kDepth;
@@ -423,13 +433,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&scales_in[s], 1);
     }
     mbar_init(acc_full, 1);
-    mbar_init(acc_empty, 2 * kEpiWarps);
+    mbar_init(acc_empty, 2 * F::kEpiWarps);
     mbar_init(drain, 1);
     mbar_init(drain_copies, 1);
     mbar_init(answer_in, 1);
     for (int i = 0; i < kQueue; ++i) {
       mbar_init(&unit_full[i], 1);
-      mbar_init(&unit_empty[i], 4 + 2 + 2 * kEpiWarps);  // the leader's four first warps, the peer's two
+      mbar_init(&unit_empty[i], 4 + 2 + 2 * F::kEpiWarps);  // the leader's four first warps, the peer's two
       mbar_init(&unit_begun[i], 1);
     }
     abort_flag = 0;
@@ -445,12 +455,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   griddep_wait_and_release();
 
-  // The experts' rows and units: three experts a thread, summed over the CTA.
+  // The experts' rows and units: a few experts a thread, summed over the CTA.
   {
-    int64_t n[3], sum = 0;
+    int64_t n[F::kPer], sum = 0;
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      const int e = 3 * threadIdx.x + i;
+    for (int i = 0; i < F::kPer; ++i) {
+      const int e = F::kPer * threadIdx.x + i;
       n[i] = 0;
       if (e < a.experts) {
         const ExpertRows r = expert_rows(a.row_start, a.rows, e, a.max_rows);
@@ -470,10 +480,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int w = 0; w < warp; ++w) upto += warp_sum[w];
     upto -= sum;
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < F::kPer; ++i) {
       upto += n[i];
-      if (3 * threadIdx.x + i < kMoeMaxExperts)
-        ends[3 * threadIdx.x + i] = static_cast<int>(min(upto, static_cast<int64_t>(a.max_units)));
+      if (F::kPer * threadIdx.x + i < kMoeMaxExperts)
+        ends[F::kPer * threadIdx.x + i] = static_cast<int>(min(upto, static_cast<int64_t>(a.max_units)));
     }
     __syncthreads();
   }
@@ -712,11 +722,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) return false;
       ++local;
       tc_fence_after();
-      uint32_t lo[4][16], hi[4][16];
+      uint32_t lo[F::kChunks][16], hi[F::kChunks][16];
       const uint32_t taddr = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int token0 = 32 * (2 * i + side);
+      for (int i = 0; i < F::kChunks; ++i) {
+        const int token0 = 32 * (F::kSides * i + side);
         if (token0 < t.tokens) {
           tmem_ld_fragments(taddr + token0, lo[i]);
           tmem_ld_fragments(taddr + (16u << 16) + token0, hi[i]);
@@ -730,8 +740,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int n0 = t.w_tile * kWRows + static_cast<int>(rank) * 128 + quarter * 32;
       if constexpr (kMode == 0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int token0 = 32 * (2 * i + side);
+        for (int i = 0; i < F::kChunks; ++i) {
+          const int token0 = 32 * (F::kSides * i + side);
           if (token0 < t.tokens && n0 < a.N) store_rows(a, &map_out, t, lo[i], hi[i], token0, n0, scale, buf, lane);
         }
       } else if constexpr (kMode == 1) {
@@ -739,8 +749,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!g_ok && lane == 0) set_status(a.status, NVFP4_ERR_INVALID_ARG);
         const float g = g_ok ? g_in : 1.0f, six_g = __fmul_rn(6.0f, g);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int token0 = 32 * (2 * i + side);
+        for (int i = 0; i < F::kChunks; ++i) {
+          const int token0 = 32 * (F::kSides * i + side);
           if (token0 >= t.tokens) continue;
           swiglu_fragments(lo[i], hi[i], scale);
           const BlockScale b = block_scale(token_amax(lo[i], lane), g, six_g);
@@ -751,8 +761,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         float* mine = reinterpret_cast<float*>(buf_ptr);
         const float* theirs = reinterpret_cast<const float*>(sEpi + ((warp - kEpi0) ^ 1) * kEpiBytes);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int token0 = 32 * (2 * i + side);
+        for (int i = 0; i < F::kChunks; ++i) {
+          const int token0 = 32 * (F::kSides * i + side);
           if (token0 >= t.tokens) continue;
           swiglu_fragments(lo[i], hi[i], scale);
           if (a.rotate) {
@@ -874,7 +884,7 @@ bool opted_in() {
   std::lock_guard<std::mutex> lock(mu);
   if (done[d]) return true;
   if (cudaFuncSetAttribute(grouped_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           static_cast<int>(kSmem)) != cudaSuccess) {
+                           static_cast<int>(Form<kMode>::kSmem)) != cudaSuccess) {
     cudaGetLastError();
     return false;
   }
@@ -906,8 +916,8 @@ nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.blockDim = dim3(kThreads, 1, 1);
-  cfg.dynamicSmemBytes = kSmem;
+  cfg.blockDim = dim3(Form<kMode>::kThreads, 1, 1);
+  cfg.dynamicSmemBytes = Form<kMode>::kSmem;
   cfg.attrs = attr;
   if (!opted_in<kMode>()) return NVFP4_ERR_CUDA;
   CUtensorMap w, ws, x16, x64 = {}, x128 = {}, xs, xs2 = {}, out = {};
