@@ -148,7 +148,7 @@ _raw_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_de
 
 def _stream(stream):
     if stream is None:
-        if _raw_current_stream is not None and torch.cuda.is_initialized():
+        if _raw_current_stream is not None:
             return _raw_current_stream(_raw_current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
@@ -437,11 +437,36 @@ def moe_sort_workspace_size(n_tokens, top_k, num_experts):
     return int(_moe_sort_ws(n_tokens, top_k, num_experts))
 
 
-def _matrix(x, rows, cols, what):
-    """(pointer, elements between rows) of a bf16 [rows, cols] argument whose rows may be padded."""
-    if x.dtype is not _bf16 or x.shape != (rows, cols) or (cols > 1 and x.stride(1) != 1):
-        raise ValueError(f"{what} must be row-major bfloat16 [{rows}, {cols}]")
-    return x.data_ptr(), x.stride(0) if rows > 1 else cols
+# Each tensor is looked at once: these calls are a few microseconds of a decode step whose kernels are no longer.
+
+def _matrix(x, rows, what):
+    """(pointer, elements between rows, cols) of a bf16 [rows, cols] argument whose rows may be padded."""
+    n, cols = x.shape
+    between, step = x.stride()
+    if x.dtype is not _bf16 or n != rows or (step != 1 and cols > 1):
+        raise ValueError(f"{what} must be row-major bfloat16 [{rows}, cols]")
+    return x.data_ptr(), between if rows > 1 else cols, cols
+
+
+def _bytes(t, numel, what):
+    """Device pointer of a dense uint8 argument of `numel` bytes."""
+    if t.dtype is not _uint8 or t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous uint8 with {numel} elements")
+    return t.data_ptr()
+
+
+def _floats(t, numel, what):
+    """Device pointer of a dense float32 argument of `numel` numbers."""
+    if t.dtype is not _float32 or t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous float32 with {numel} elements")
+    return t.data_ptr()
+
+
+def _rows(t, numel, what):
+    """Device pointer of a plan's dense bf16 rows."""
+    if t.dtype is not _bf16 or t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous bfloat16 with {numel} elements")
+    return t.data_ptr()
 
 
 def _router(logits, top_k, score, renormalize, scale, bias):
@@ -479,69 +504,59 @@ def moe_route_backward(logits, expert_idx, d_weights, d_logits, score=MOE_SOFTMA
 def moe_sort(plan, expert_idx, stream=None):
     """The plan's rows for expert_idx int32 [n_tokens, top_k]; a negative entry is a choice without an expert."""
     ws = plan.workspace
-    _check("moe_sort", _moe_sort(plan.packed(), _typed(expert_idx, _int32, "expert_idx", plan.n_tokens * plan.top_k),
+    _check("moe_sort", _moe_sort(plan.packed(), _typed(expert_idx, _int32, "expert_idx", plan.choices),
                                  *((None, 0) if ws is None else (ws.data_ptr(), ws.nbytes)), _stream(stream)))
 
 
 def moe_dispatch(plan, x, rows, weights=None, stream=None):
     """x [n_tokens, cols] bf16 to its experts' rows [plan.max_rows, cols], times weights [n_tokens, top_k] if given."""
-    cols = x.shape[1]
-    xp, ld = _matrix(x, plan.n_tokens, cols, "x")
+    xp, ld, cols = _matrix(x, plan.n_tokens, "x")
     _check("moe_dispatch",
-           _moe_dispatch(plan.packed(), xp, ld, cols, _typed(weights, _float32, "weights", plan.n_tokens * plan.top_k),
-                         _typed(rows, _bf16, "rows", plan.max_rows * cols), _stream(stream)))
-
-
-def _row_operand(plan, codes, scales, cols, what):
-    """Pointers of a plan's rows as a linear's 4-bit operand: codes [max_rows, cols/2], MMA-layout scales."""
-    return (_typed(codes, _uint8, what + " codes", plan.max_rows * cols // 2),
-            _typed(scales, _uint8, what + " scales", plan.max_rows * cols // 16))
+           _moe_dispatch(plan.packed(), xp, ld, cols, None if weights is None else _floats(weights, plan.choices, "weights"),
+                         _rows(rows, plan.max_rows * cols, "rows"), _stream(stream)))
 
 
 def moe_dispatch_nvfp4(plan, x, g, codes, scales, stream=None):
-    """x [n_tokens, cols] bf16, NVFP4-quantized with the scale g, to its experts' rows (MMA-layout scales)."""
-    cols = x.shape[1]
-    xp, ld = _matrix(x, plan.n_tokens, cols, "x")
+    """x [n_tokens, cols] bf16, NVFP4-quantized with the scale g, to its experts' rows: codes [plan.max_rows, cols/2] and
+    MMA-layout scales."""
+    xp, ld, cols = _matrix(x, plan.n_tokens, "x")
+    n = plan.max_rows * cols
     _check("moe_dispatch_nvfp4",
-           _moe_dispatch_nvfp4(plan.packed(), xp, ld, cols, _typed(g, _float32, "g", 1),
-                               *_row_operand(plan, codes, scales, cols, "rows'"), _stream(stream)))
+           _moe_dispatch_nvfp4(plan.packed(), xp, ld, cols, _floats(g, 1, "g"), _bytes(codes, n // 2, "codes"),
+                               _bytes(scales, n // 16, "scales"), _stream(stream)))
 
 
 def moe_dispatch_mxfp4(plan, x, codes, scales, rotate=False, stream=None):
-    cols = x.shape[1]
-    xp, ld = _matrix(x, plan.n_tokens, cols, "x")
+    """The same as MXFP4, optionally after the 32-element block rotation."""
+    xp, ld, cols = _matrix(x, plan.n_tokens, "x")
+    n = plan.max_rows * cols
     _check("moe_dispatch_mxfp4",
-           _moe_dispatch_mxfp4(plan.packed(), xp, ld, cols, int(bool(rotate)),
-                               *_row_operand(plan, codes, scales, cols, "rows'"), _stream(stream)))
+           _moe_dispatch_mxfp4(plan.packed(), xp, ld, cols, int(bool(rotate)), _bytes(codes, n // 2, "codes"),
+                               _bytes(scales, n // 16, "scales"), _stream(stream)))
 
 
 def moe_combine(plan, y, out, weights=None, base=None, stream=None):
     """out [n_tokens, cols] = base + the sum of weights * y over each token's rows; without weights, also the gradient
     of moe_dispatch's x from that of its rows, y."""
-    cols = out.shape[1]
-    op, ld = _matrix(out, plan.n_tokens, cols, "out")
+    op, ld, cols = _matrix(out, plan.n_tokens, "out")
+    bp, ld_base, base_cols = (None, 0, cols) if base is None else _matrix(base, plan.n_tokens, "base")
+    if base_cols != cols:
+        raise ValueError("base must have out's shape")
     _check("moe_combine",
-           _moe_combine(plan.packed(), _typed(y, _bf16, "y", plan.max_rows * cols), cols,
-                        _typed(weights, _float32, "weights", plan.n_tokens * plan.top_k),
-                        *((None, 0) if base is None else _matrix(base, plan.n_tokens, cols, "base")), op, ld,
+           _moe_combine(plan.packed(), _rows(y, plan.max_rows * cols, "y"), cols,
+                        None if weights is None else _floats(weights, plan.choices, "weights"), bp, ld_base, op, ld,
                         _stream(stream)))
 
 
 def moe_combine_backward(plan, d_out, y, weights, d_y, d_weights, stream=None):
     """moe_combine's gradients: d_y [max_rows, cols] and d_weights [n_tokens, top_k]; one of them may be None."""
-    cols, n = d_out.shape[1], plan.n_tokens * plan.top_k
-    gp, ld = _matrix(d_out, plan.n_tokens, cols, "d_out")
+    gp, ld, cols = _matrix(d_out, plan.n_tokens, "d_out")
+    n = plan.max_rows * cols
     _check("moe_combine_backward",
-           _moe_combine_backward(plan.packed(), gp, ld, _typed(y, _bf16, "y", plan.max_rows * cols), cols,
-                                 _typed(weights, _float32, "weights", n),
-                                 _typed(d_y, _bf16, "d_y", plan.max_rows * cols),
-                                 _typed(d_weights, _float32, "d_weights", n), _stream(stream)))
-
-
-def _expert_weights(plan, codes, scales, N, K):
-    E = plan.num_experts
-    return (_typed(codes, _uint8, "w_codes", E * N * K // 2),
-            _typed(scales, _uint8, "w_scales", E * ((N + 127) // 128 * 128) * (K // 16)))
+           _moe_combine_backward(plan.packed(), gp, ld, _rows(y, n, "y"), cols, _floats(weights, plan.choices, "weights"),
+                                 None if d_y is None else _rows(d_y, n, "d_y"),
+                                 None if d_weights is None else _floats(d_weights, plan.choices, "d_weights"),
+                                 _stream(stream)))
 
 
 def _per_expert(g, plan, what):
@@ -549,42 +564,59 @@ def _per_expert(g, plan, what):
     n = g.numel()
     if n != 1 and n != plan.num_experts:
         raise ValueError(f"{what} must have one element or one an expert")
-    return _typed(g, _float32, what), 0 if n == 1 else 1
+    return _floats(g, n, what), 0 if n == 1 else 1
 
 
 def nvfp4_linear_grouped(plan, a_codes, a_scales, g_a, w_codes, w_scales, g_w, out, N, K, stream=None):
     """out [plan.max_rows, N]: each expert's rows [.., K] times its weight [N, K]; g_a: one or one an expert."""
-    op, ldo = _matrix(out, plan.max_rows, N, "out")
+    E, R = plan.num_experts, plan.max_rows
+    op, ldo, cols = _matrix(out, R, "out")
+    if cols != N:
+        raise ValueError("out must be [plan.max_rows, N]")
+    ga, ga_step = _per_expert(g_a, plan, "g_a")
     _check("nvfp4_linear_grouped",
-           _linear_grouped(plan.packed(), *_row_operand(plan, a_codes, a_scales, K, "a"), *_per_expert(g_a, plan, "g_a"),
-                           *_expert_weights(plan, w_codes, w_scales, N, K),
-                           _typed(g_w, _float32, "g_w", plan.num_experts), N, K, op, ldo, _stream(stream)))
+           _linear_grouped(plan.packed(), _bytes(a_codes, R * K // 2, "a_codes"), _bytes(a_scales, R * K // 16, "a_scales"),
+                           ga, ga_step, _bytes(w_codes, E * N * K // 2, "w_codes"),
+                           _bytes(w_scales, E * ((N + 127) // 128 * 128) * (K // 16), "w_scales"), _floats(g_w, E, "g_w"),
+                           N, K, op, ldo, _stream(stream)))
 
 
 def mxfp4_linear_grouped(plan, a_codes, a_scales, w_codes, w_scales, out, N, K, stream=None):
-    op, ldo = _matrix(out, plan.max_rows, N, "out")
+    E, R = plan.num_experts, plan.max_rows
+    op, ldo, cols = _matrix(out, R, "out")
+    if cols != N:
+        raise ValueError("out must be [plan.max_rows, N]")
     _check("mxfp4_linear_grouped",
-           _mx_linear_grouped(plan.packed(), *_row_operand(plan, a_codes, a_scales, K, "a"),
-                              *_expert_weights(plan, w_codes, w_scales, N, K), N, K, op, ldo, _stream(stream)))
+           _mx_linear_grouped(plan.packed(), _bytes(a_codes, R * K // 2, "a_codes"),
+                              _bytes(a_scales, R * K // 16, "a_scales"), _bytes(w_codes, E * N * K // 2, "w_codes"),
+                              _bytes(w_scales, E * ((N + 127) // 128 * 128) * (K // 16), "w_scales"), N, K, op, ldo,
+                              _stream(stream)))
 
 
 def nvfp4_linear_grouped_swiglu_quantize(plan, a_codes, a_scales, g_a, w_codes, w_scales, g_w, I, K, g_out, out_codes,
                                          out_scales, stream=None):
     """h = SiLU(gate) * up of each expert's rows, NVFP4-quantized with g_out (one or one an expert)."""
+    E, R, N = plan.num_experts, plan.max_rows, 2 * I
+    ga, ga_step = _per_expert(g_a, plan, "g_a")
+    go, go_step = _per_expert(g_out, plan, "g_out")
     _check("nvfp4_linear_grouped_swiglu_quantize",
-           _linear_grouped_swiglu(plan.packed(), *_row_operand(plan, a_codes, a_scales, K, "a"),
-                                  *_per_expert(g_a, plan, "g_a"), *_expert_weights(plan, w_codes, w_scales, 2 * I, K),
-                                  _typed(g_w, _float32, "g_w", plan.num_experts), I, K,
-                                  *_per_expert(g_out, plan, "g_out"),
-                                  *_row_operand(plan, out_codes, out_scales, I, "out"), _stream(stream)))
+           _linear_grouped_swiglu(plan.packed(), _bytes(a_codes, R * K // 2, "a_codes"),
+                                  _bytes(a_scales, R * K // 16, "a_scales"), ga, ga_step,
+                                  _bytes(w_codes, E * N * K // 2, "w_codes"),
+                                  _bytes(w_scales, E * ((N + 127) // 128 * 128) * (K // 16), "w_scales"),
+                                  _floats(g_w, E, "g_w"), I, K, go, go_step, _bytes(out_codes, R * I // 2, "out_codes"),
+                                  _bytes(out_scales, R * I // 16, "out_scales"), _stream(stream)))
 
 
 def mxfp4_linear_grouped_swiglu_quantize(plan, a_codes, a_scales, w_codes, w_scales, I, K, out_codes, out_scales,
                                          rotate=False, stream=None):
+    E, R, N = plan.num_experts, plan.max_rows, 2 * I
     _check("mxfp4_linear_grouped_swiglu_quantize",
-           _mx_linear_grouped_swiglu(plan.packed(), *_row_operand(plan, a_codes, a_scales, K, "a"),
-                                     *_expert_weights(plan, w_codes, w_scales, 2 * I, K), I, K, int(bool(rotate)),
-                                     *_row_operand(plan, out_codes, out_scales, I, "out"), _stream(stream)))
+           _mx_linear_grouped_swiglu(plan.packed(), _bytes(a_codes, R * K // 2, "a_codes"),
+                                     _bytes(a_scales, R * K // 16, "a_scales"), _bytes(w_codes, E * N * K // 2, "w_codes"),
+                                     _bytes(w_scales, E * ((N + 127) // 128 * 128) * (K // 16), "w_scales"), I, K,
+                                     int(bool(rotate)), _bytes(out_codes, R * I // 2, "out_codes"),
+                                     _bytes(out_scales, R * I // 16, "out_scales"), _stream(stream)))
 
 
 def nvfp4_qfit_workspace_size(batch, tokens, num_q_heads, num_kv_heads, grid_s, grid_m):
@@ -670,7 +702,7 @@ class MoEPlan:
 
     def __init__(self, n_tokens, top_k, num_experts, device="cuda"):
         self.n_tokens, self.top_k, self.num_experts = n_tokens, top_k, num_experts
-        self.max_rows = moe_max_rows(n_tokens, top_k, num_experts)
+        self.max_rows, self.choices = moe_max_rows(n_tokens, top_k, num_experts), n_tokens * top_k
         if self.max_rows == 0 and n_tokens != 0:
             raise ValueError("n_tokens, top_k or num_experts out of range")
         self._arrays = (torch.zeros(num_experts + 1, dtype=torch.int32, device=device),
