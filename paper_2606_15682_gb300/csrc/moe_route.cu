@@ -45,36 +45,50 @@ template <bool kWide>
 __device__ __forceinline__ int expert_at(int i, int lane) {
   return kWide ? (i >> 2) * 128 + 4 * lane + (i & 3) : 32 * i + lane;
 }
-// The lane's logits of token t: -inf in place of NaN and behind the last expert.
-template <int kPer, bool kBf16, bool kWide>
-__device__ __forceinline__ void load_logits(const RouteArgs& a, int64_t t, int lane, float l[kPer]) {
-  const int64_t row = t * a.ld;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) l[i] = -kInf;
+// The lane's numbers of a row of `experts`; those behind the last one stay as they are.
+template <int kPer, class T, bool kWide>
+__device__ __forceinline__ void load_row(const T* row, int experts, int lane, float v[kPer]) {
+  constexpr bool kBf16 = sizeof(T) == 2;
   if constexpr (kWide) {
 #pragma unroll
     for (int i = 0; i < kPer; i += 4) {
       const int e = 32 * i + 4 * lane;  // the experts are a multiple of 4
-      if (e >= a.experts) continue;
+      if (e >= experts) continue;
       if constexpr (kBf16) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.logits) + row + e));
-        l[i] = __uint_as_float(v.x << 16);
-        l[i + 1] = __uint_as_float(v.x & 0xFFFF0000u);
-        l[i + 2] = __uint_as_float(v.y << 16);
-        l[i + 3] = __uint_as_float(v.y & 0xFFFF0000u);
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(row + e));
+        v[i] = __uint_as_float(w.x << 16);
+        v[i + 1] = __uint_as_float(w.x & 0xFFFF0000u);
+        v[i + 2] = __uint_as_float(w.y << 16);
+        v[i + 3] = __uint_as_float(w.y & 0xFFFF0000u);
       } else {
-        const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(a.logits) + row + e));
-        l[i] = v.x;
-        l[i + 1] = v.y;
-        l[i + 2] = v.z;
-        l[i + 3] = v.w;
+        const float4 w = __ldg(reinterpret_cast<const float4*>(row + e));
+        v[i] = w.x;
+        v[i + 1] = w.y;
+        v[i + 2] = w.z;
+        v[i + 3] = w.w;
       }
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (32 * i + lane < a.experts) l[i] = load_logit<kBf16>(a, row + 32 * i + lane);
+    for (int i = 0; i < kPer; ++i) {
+      const int e = 32 * i + lane;
+      if (e >= experts) continue;
+      if constexpr (kBf16)
+        v[i] = __uint_as_float(static_cast<uint32_t>(__ldg(row + e)) << 16);
+      else
+        v[i] = __ldg(row + e);
+    }
   }
+}
+// The lane's logits of token t: -inf in place of NaN and behind the last expert.
+template <int kPer, bool kBf16, bool kWide>
+__device__ __forceinline__ void load_logits(const RouteArgs& a, int64_t t, int lane, float l[kPer]) {
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) l[i] = -kInf;
+  if constexpr (kBf16)
+    load_row<kPer, uint16_t, kWide>(static_cast<const uint16_t*>(a.logits) + t * a.ld, a.experts, lane, l);
+  else
+    load_row<kPer, float, kWide>(static_cast<const float*>(a.logits) + t * a.ld, a.experts, lane, l);
 #pragma unroll
   for (int i = 0; i < kPer; ++i) l[i] = fmaxf(l[i], -kInf);  // the number where the other is NaN
 }
@@ -126,37 +140,68 @@ __device__ __forceinline__ int choose_in_turn(float key[kPer], int top_k, int la
   return chosen;
 }
 
+// The key under a bias, as it is defined, and within 2^-20 of it (and the sum's rounding) by the hardware's 2^x and 1 / x.
+__device__ __forceinline__ float biased_key(float l, float bias) {
+  return l > -kInf ? fmaxf(__fadd_rn(sigmoid_rn(l), bias), -kInf) : -kInf;  // not NaN
+}
+__device__ __forceinline__ float about_biased_key(float l, float bias) {
+  float e, s;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(l * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.0f + e));
+  return l > -kInf ? fmaxf(s + bias, -kInf) : -kInf;
+}
+
 // The same with fewer steps: the top_k-th largest of the lanes' own maxima is at most the top_k-th largest key, so few
-// keys reach it; those are gathered, one a lane, and chosen in turn.  More than 32 (many equal keys), or fewer lanes with
-// a key than top_k: all in turn.  list: [32] of the warp.
-template <int kPer, bool kWide>
-__device__ __forceinline__ int choose(float key[kPer], int top_k, int lane, float2* list) {
-  if constexpr (kPer == 1) return choose_in_turn<kPer, kWide>(key, top_k, lane);
+// keys reach it; those are gathered, one a lane, and chosen in turn.  Under a bias the first part goes by approximate keys
+// and a margin of more than twice their error, and a lane forms the key of its own candidate alone.  More than 32
+// candidates (many equal keys), or fewer lanes with a key than top_k: all in turn.  list: [32] of the warp.
+template <int kPer, bool kBf16, bool kWide>
+__device__ __forceinline__ int choose(const RouteArgs& a, int64_t t, const float l[kPer], int lane, float2* list) {
+  float key[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) key[i] = l[i];
+  if (a.bias) {
+    float b[kPer] = {};
+    load_row<kPer, float, kWide>(a.bias, a.experts, lane, b);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) key[i] = kPer == 1 ? biased_key(l[i], b[i]) : about_biased_key(l[i], b[i]);
+  }
+  if constexpr (kPer == 1) return choose_in_turn<kPer, kWide>(key, a.top_k, lane);
   float best = key[0];
 #pragma unroll
   for (int i = 1; i < kPer; ++i) best = fmaxf(best, key[i]);
   float least = -kInf;
-  for (int j = 0; j < top_k; ++j) {
+  for (int j = 0; j < a.top_k; ++j) {
     least = warp_max(best);
     best = best == least ? -kInf : best;
   }
+  const float from = a.bias ? least - 0x1p-18f * (1.0f + fabsf(least)) : least;
   int n = 0;
   const uint32_t lower = (1u << lane) - 1;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const bool in = key[i] >= least;
+    const bool in = key[i] >= from;
     const uint32_t vote = __ballot_sync(0xffffffffu, in);
     const int at = n + __popc(vote & lower);
     if (in && at < 32) list[at] = make_float2(key[i], __int_as_float(expert_at<kWide>(i, lane)));
     n += __popc(vote);
   }
-  if (!(least > -kInf) || n > 32) return choose_in_turn<kPer, kWide>(key, top_k, lane);
+  if (!(least > -kInf) || n > 32 || n < a.top_k) {
+    if (a.bias) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (l[i] > -kInf) key[i] = biased_key(l[i], __ldg(a.bias + expert_at<kWide>(i, lane)));
+    }
+    return choose_in_turn<kPer, kWide>(key, a.top_k, lane);
+  }
   __syncwarp();
   const float2 mine = list[min(lane, n - 1)];
-  float k = lane < n ? mine.x : -kInf;
   const uint32_t expert = __float_as_uint(mine.y);
+  float k = mine.x;
+  if (a.bias) k = biased_key(fmaxf(load_logit<kBf16>(a, t * a.ld + expert), -kInf), __ldg(a.bias + expert));
+  if (lane >= n) k = -kInf;
   int chosen = -1;
-  for (int j = 0; j < top_k; ++j) {
+  for (int j = 0; j < a.top_k; ++j) {
     const float all = warp_max(k);
     const uint32_t e = __reduce_min_sync(0xffffffffu, k == all ? expert : 0xffffffffu);
     k = expert == e ? -kInf : k;
@@ -172,19 +217,10 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const RouteArg
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (kRouteThreads / 32) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (t >= a.tokens) return;
-  float l[kPer], key[kPer];
+  float l[kPer];
   load_logits<kPer, kBf16, kWide>(a, t, lane, l);
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) key[i] = l[i];
-  if (a.bias) {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = expert_at<kWide>(i, lane);
-      if (l[i] > -kInf) key[i] = fmaxf(__fadd_rn(sigmoid_rn(l[i]), __ldg(a.bias + e)), -kInf);  // not NaN
-    }
-  }
   // Lane j: choice j and its logit.
-  const int chosen = choose<kPer, kWide>(key, a.top_k, lane, lists[threadIdx.x >> 5]);
+  const int chosen = choose<kPer, kBf16, kWide>(a, t, l, lane, lists[threadIdx.x >> 5]);
   const float chosen_l = chosen >= 0 ? load_logit<kBf16>(a, t * a.ld + chosen) : -kInf;
   float p;
   if (a.sigmoid) {
@@ -318,7 +354,8 @@ template <int kPer>
 cudaError_t launch_route(const RouteArgs& a, cudaStream_t s) {
   if constexpr (kPer >= 4) {
     const uintptr_t wide = a.bf16 ? 8 : 16;
-    if (a.experts % 4 == 0 && a.ld % 4 == 0 && aligned(a.logits, wide) && aligned(a.d_logits, wide))
+    if (a.experts % 4 == 0 && a.ld % 4 == 0 && aligned(a.logits, wide) && aligned(a.d_logits, wide) &&
+        aligned(a.bias, 16))
       return a.bf16 ? launch_route<kPer, true, true>(a, s) : launch_route<kPer, false, true>(a, s);
   }
   return a.bf16 ? launch_route<kPer, true, false>(a, s) : launch_route<kPer, false, false>(a, s);

@@ -244,9 +244,14 @@ struct WalkLaunch {
   Walk w;
   dim3 grid, block;
 };
+// Tokens of a CTA of 256 threads where a token has few units: not more than leave a CTA to each SM.
+uint32_t short_tokens(int64_t tokens, uint32_t vecs) {
+  const int64_t spread = tokens / sm_count();
+  return vecs >= 128 || spread <= 1 ? 1u : static_cast<uint32_t>(spread < 256 / vecs ? spread : 256 / vecs);
+}
 WalkLaunch make_walk(int64_t tokens, uint32_t vecs) {
   WalkLaunch l;
-  l.w = {tokens, vecs, vecs < 128 ? 256 / vecs : 1u};
+  l.w = {tokens, vecs, short_tokens(tokens, vecs)};
   const uint32_t passes = (vecs + kWalkThreads - 1) / kWalkThreads;
   l.block = dim3(l.w.per_cta > 1 ? 256 : ((vecs + passes - 1) / passes + 31) / 32 * 32);
   l.grid = dim3(static_cast<uint32_t>((tokens + l.w.per_cta - 1) / l.w.per_cta));
@@ -450,11 +455,7 @@ template <int U>
 cudaError_t launch_combine(const RowArgs& a, int64_t tokens, uint32_t vecs, const void* y, const float* weights,
                            const void* base, int64_t ld_base, void* out, int64_t ld_out, cudaStream_t s) {
   const uint32_t threads = ((vecs + U - 1) / U + 31) / 32 * 32;
-  uint32_t per_cta = 1, cta = threads;
-  if (U == 1 && vecs < 128) {  // several short tokens
-    per_cta = 256 / vecs;
-    cta = 256;
-  }
+  const uint32_t per_cta = U == 1 ? short_tokens(tokens, vecs) : 1u, cta = per_cta > 1 ? 256 : threads;
   return launch_pdl(moe_combine_kernel<U>, dim3(static_cast<uint32_t>((tokens + per_cta - 1) / per_cta)), dim3(cta), 0, s,
                     a, tokens, vecs, per_cta, static_cast<const uint16_t*>(y), weights,
                     static_cast<const uint16_t*>(base), ld_base, static_cast<uint16_t*>(out), ld_out);

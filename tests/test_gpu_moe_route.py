@@ -220,3 +220,16 @@ def test_gradient_is_that_of_differences(N, score, renormalize):
             side.append((weights_of(moved, ii, sig, renormalize, 1.25) * d64).sum(1))
         want = (side[0] - side[1]) / (2 * h)
         assert np.abs(out[:, e].double().cpu().numpy() - want).max() < 1e-6 * np.abs(d64).sum(1).max()
+
+
+@pytest.mark.parametrize("experts", [40, 256, 1000])
+@pytest.mark.parametrize("scale", [1e-7, 1.0, 1e6])
+def test_a_choice_between_close_biased_scores_is_by_their_32_bits(N, experts, scale):
+    """Scores that differ by a few units, and biases that hide them or drown in them: the choice is the one by 1 / (1 + e^-l)
+    + bias with one rounding for each operation, which torch's elementwise operations on the GPU have too."""
+    g = torch.Generator(device="cuda").manual_seed(experts)
+    l = 0.3 + 1e-6 * torch.randn(500, experts, generator=g, device="cuda")
+    bias = scale * torch.randint(-2, 3, (experts,), generator=g, device="cuda").float()
+    idx, _ = run(N, l, 8, score=N.MOE_SIGMOID, bias=bias)
+    key = torch.reciprocal(1 + torch.exp(-l)) + bias
+    assert np.array_equal(idx, choice(key.double().cpu().numpy(), 8))
