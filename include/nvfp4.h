@@ -824,8 +824,8 @@ nvfp4_status moe_combine_backward(const moe_plan* plan, const void* d_out_bf16, 
  *              the other; g_w: device float [num_experts].
  *   out_bf16 : [moe_max_rows, N] bf16, rows ldo apart.
  * Experts without rows cost nothing.  K % 256 == 0, N % 16 == 0, both positive and at
- * most 2^20, ldo >= N, ldo % 8 == 0, num_experts * ceil(N / 128) * (K / 32) < 2^31 and
- * num_experts * N < 2^31 (SHAPE); g_a_step 0 or 1 (INVALID_ARG); 16-B aligned, g's 4-B
+ * most 2^20, ldo >= N, ldo % 8 == 0, (num_experts * ceil(N / 128) + 2) * (K / 32) and
+ * num_experts * N + 256 and moe_max_rows / 128 * (K / 32) below 2^31 (SHAPE); g_a_step 0 or 1 (INVALID_ARG); 16-B aligned, g's 4-B
  * (ALIGN).  A bounded on-device wait that expires sets TIMEOUT; out is then undefined.
  */
 nvfp4_status nvfp4_linear_grouped(const moe_plan* plan, const uint8_t* a_codes, const uint8_t* a_scales,
@@ -840,8 +840,8 @@ nvfp4_status mxfp4_linear_grouped(const moe_plan* plan, const uint8_t* a_codes, 
 /*
  * The experts' gate_up with the down projection's input in the epilogue, as
  * nvfp4_linear_swiglu_quantize: h = SiLU(G) * U of the fp32 products, NVFP4-quantized
- * with the static scale of the expert.  SiLU(x) = x / (1 + e^-x) with CUDA's fast
- * exponential and division (some 2^-19 relative).
+ * with the static scale of the expert.  SiLU(x) = x / (1 + e^-x) by the hardware's 2^x
+ * and 1 / x: within (2 + |x| / 4) * 2^-21 of its size.
  *   w_codes, w_scales : [num_experts, 2I, K], gate and up rows in turn, 16 of each
  *                (nvfp4_interleave_gate_up of each expert's, then nvfp4_quantize).
  *   g_out      : device float [1] (g_out_step 0) or [num_experts] (1); <= 0 or not

@@ -952,7 +952,8 @@ nvfp4_status check_operands(const moe_plan* plan, const GroupedArgs& a, int64_t 
   if (!a.a_codes || !a.a_scales || !a.w_codes || !a.w_scales || (g && (!a.g_a || !a.g_w))) return NVFP4_ERR_INVALID_ARG;
   if ((a.g_a_step != 0 && a.g_a_step != 1) || (a.g_out_step != 0 && a.g_out_step != 1)) return NVFP4_ERR_INVALID_ARG;
   if (N <= 0 || K <= 0 || N > kMaxSide || K > kMaxSide || K % 256 || N % n_step) return NVFP4_ERR_SHAPE;
-  if (plan->num_experts * ((N + 127) / 128) * (K / 32) >= (1ll << 31) || plan->num_experts * N >= (1ll << 31) ||
+  // Box coordinates, those of a last tile that reaches past the last expert too.
+  if ((plan->num_experts * ((N + 127) / 128) + 2) * (K / 32) >= (1ll << 31) || plan->num_experts * N + 256 >= (1ll << 31) ||
       moe_rows_bound(plan->n_tokens, plan->top_k, plan->num_experts) / 128 * (K / 32) >= (1ll << 31))
     return NVFP4_ERR_SHAPE;
   if (!aligned(a.a_codes, 16) || !aligned(a.a_scales, 16) || !aligned(a.w_codes, 16) || !aligned(a.w_scales, 16) ||

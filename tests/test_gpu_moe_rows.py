@@ -36,7 +36,8 @@ def near(got, want, slack):
 @pytest.mark.parametrize("tokens,top_k,experts,idle", [
     (1, 1, 1, 0.0), (1, 8, 64, 0.0), (1, 32, 1024, 0.0), (3, 2, 2, 0.5), (32, 8, 64, 0.0), (127, 3, 5, 0.1),
     (1024, 4, 1024, 0.0), (1365, 3, 37, 0.2), (512, 8, 256, 0.0), (4099, 8, 64, 0.125), (4097, 1, 1, 0.0),
-    (16384, 8, 256, 0.0), (20001, 7, 1000, 0.3), (300000, 4, 64, 0.0)])
+    (16384, 8, 256, 0.0), (20001, 7, 1000, 0.3), (300000, 4, 64, 0.0), (32769, 1, 340, 0.0), (9000, 1, 365, 0.1),
+    (4096, 8, 8, 0.0), (2049, 1, 300, 0.0)])
 def test_sort(N, tokens, top_k, experts, idle):
     rng = np.random.default_rng(tokens + top_k)
     p = rng.dirichlet(np.full(experts, 0.3))
@@ -81,7 +82,7 @@ def some_plan(N, tokens, top_k=3, experts=7, seed=5):
     return M.make_plan(N, idx, experts), idx
 
 
-COLS = [8, 72, 1000, 2048, 2056, 5120, 65536]
+COLS = [8, 72, 1000, 2048, 2056, 5120, 16392, 65536]
 
 
 @pytest.mark.parametrize("cols", COLS)
