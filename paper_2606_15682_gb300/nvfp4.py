@@ -146,12 +146,17 @@ _raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _raw_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _stream(stream):
+def _handle(stream):
+    """A stream's handle as an integer; None: the current one's."""
     if stream is None:
         if _raw_current_stream is not None:
             return _raw_current_stream(_raw_current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _stream(stream):
+    return ctypes.c_void_p(_handle(stream))
 
 
 def _ptr(t):
@@ -485,7 +490,7 @@ def moe_route(logits, expert_idx, weights, score=MOE_SOFTMAX, renormalize=True, 
         raise ValueError("expert_idx must be [tokens, top_k] of the logits' tokens")
     _check("moe_route", _moe_route(*_router(logits, k, score, renormalize, scale, bias),
                                    _typed(expert_idx, _int32, "expert_idx"),
-                                   _typed(weights, _float32, "weights", n * k), _stream(stream)))
+                                   _typed(weights, _float32, "weights", n * k), _handle(stream)))
 
 
 def moe_route_backward(logits, expert_idx, d_weights, d_logits, score=MOE_SOFTMAX, renormalize=True, scale=1.0,
@@ -498,14 +503,14 @@ def moe_route_backward(logits, expert_idx, d_weights, d_logits, score=MOE_SOFTMA
            _moe_route_backward(*_router(logits, k, score, renormalize, scale, None),
                                _typed(expert_idx, _int32, "expert_idx"),
                                _typed(d_weights, _float32, "d_weights", n * k),
-                               _typed(d_logits, logits.dtype, "d_logits", logits.numel()), _stream(stream)))
+                               _typed(d_logits, logits.dtype, "d_logits", logits.numel()), _handle(stream)))
 
 
 def moe_sort(plan, expert_idx, stream=None):
     """The plan's rows for expert_idx int32 [n_tokens, top_k]; a negative entry is a choice without an expert."""
     ws = plan.workspace
     _check("moe_sort", _moe_sort(plan.packed(), _typed(expert_idx, _int32, "expert_idx", plan.choices),
-                                 *((None, 0) if ws is None else (ws.data_ptr(), ws.nbytes)), _stream(stream)))
+                                 *((None, 0) if ws is None else (ws.data_ptr(), ws.nbytes)), _handle(stream)))
 
 
 def moe_dispatch(plan, x, rows, weights=None, stream=None):
@@ -513,7 +518,7 @@ def moe_dispatch(plan, x, rows, weights=None, stream=None):
     xp, ld, cols = _matrix(x, plan.n_tokens, "x")
     _check("moe_dispatch",
            _moe_dispatch(plan.packed(), xp, ld, cols, None if weights is None else _floats(weights, plan.choices, "weights"),
-                         _rows(rows, plan.max_rows * cols, "rows"), _stream(stream)))
+                         _rows(rows, plan.max_rows * cols, "rows"), _handle(stream)))
 
 
 def moe_dispatch_nvfp4(plan, x, g, codes, scales, stream=None):
@@ -523,7 +528,7 @@ def moe_dispatch_nvfp4(plan, x, g, codes, scales, stream=None):
     n = plan.max_rows * cols
     _check("moe_dispatch_nvfp4",
            _moe_dispatch_nvfp4(plan.packed(), xp, ld, cols, _floats(g, 1, "g"), _bytes(codes, n // 2, "codes"),
-                               _bytes(scales, n // 16, "scales"), _stream(stream)))
+                               _bytes(scales, n // 16, "scales"), _handle(stream)))
 
 
 def moe_dispatch_mxfp4(plan, x, codes, scales, rotate=False, stream=None):
@@ -532,7 +537,7 @@ def moe_dispatch_mxfp4(plan, x, codes, scales, rotate=False, stream=None):
     n = plan.max_rows * cols
     _check("moe_dispatch_mxfp4",
            _moe_dispatch_mxfp4(plan.packed(), xp, ld, cols, int(bool(rotate)), _bytes(codes, n // 2, "codes"),
-                               _bytes(scales, n // 16, "scales"), _stream(stream)))
+                               _bytes(scales, n // 16, "scales"), _handle(stream)))
 
 
 def moe_combine(plan, y, out, weights=None, base=None, stream=None):
@@ -545,7 +550,7 @@ def moe_combine(plan, y, out, weights=None, base=None, stream=None):
     _check("moe_combine",
            _moe_combine(plan.packed(), _rows(y, plan.max_rows * cols, "y"), cols,
                         None if weights is None else _floats(weights, plan.choices, "weights"), bp, ld_base, op, ld,
-                        _stream(stream)))
+                        _handle(stream)))
 
 
 def moe_combine_backward(plan, d_out, y, weights, d_y, d_weights, stream=None):
@@ -556,7 +561,7 @@ def moe_combine_backward(plan, d_out, y, weights, d_y, d_weights, stream=None):
            _moe_combine_backward(plan.packed(), gp, ld, _rows(y, n, "y"), cols, _floats(weights, plan.choices, "weights"),
                                  None if d_y is None else _rows(d_y, n, "d_y"),
                                  None if d_weights is None else _floats(d_weights, plan.choices, "d_weights"),
-                                 _stream(stream)))
+                                 _handle(stream)))
 
 
 def _per_expert(g, plan, what):
@@ -578,7 +583,7 @@ def nvfp4_linear_grouped(plan, a_codes, a_scales, g_a, w_codes, w_scales, g_w, o
            _linear_grouped(plan.packed(), _bytes(a_codes, R * K // 2, "a_codes"), _bytes(a_scales, R * K // 16, "a_scales"),
                            ga, ga_step, _bytes(w_codes, E * N * K // 2, "w_codes"),
                            _bytes(w_scales, E * ((N + 127) // 128 * 128) * (K // 16), "w_scales"), _floats(g_w, E, "g_w"),
-                           N, K, op, ldo, _stream(stream)))
+                           N, K, op, ldo, _handle(stream)))
 
 
 def mxfp4_linear_grouped(plan, a_codes, a_scales, w_codes, w_scales, out, N, K, stream=None):
@@ -590,7 +595,7 @@ def mxfp4_linear_grouped(plan, a_codes, a_scales, w_codes, w_scales, out, N, K, 
            _mx_linear_grouped(plan.packed(), _bytes(a_codes, R * K // 2, "a_codes"),
                               _bytes(a_scales, R * K // 16, "a_scales"), _bytes(w_codes, E * N * K // 2, "w_codes"),
                               _bytes(w_scales, E * ((N + 127) // 128 * 128) * (K // 16), "w_scales"), N, K, op, ldo,
-                              _stream(stream)))
+                              _handle(stream)))
 
 
 def nvfp4_linear_grouped_swiglu_quantize(plan, a_codes, a_scales, g_a, w_codes, w_scales, g_w, I, K, g_out, out_codes,
@@ -605,7 +610,7 @@ def nvfp4_linear_grouped_swiglu_quantize(plan, a_codes, a_scales, g_a, w_codes, 
                                   _bytes(w_codes, E * N * K // 2, "w_codes"),
                                   _bytes(w_scales, E * ((N + 127) // 128 * 128) * (K // 16), "w_scales"),
                                   _floats(g_w, E, "g_w"), I, K, go, go_step, _bytes(out_codes, R * I // 2, "out_codes"),
-                                  _bytes(out_scales, R * I // 16, "out_scales"), _stream(stream)))
+                                  _bytes(out_scales, R * I // 16, "out_scales"), _handle(stream)))
 
 
 def mxfp4_linear_grouped_swiglu_quantize(plan, a_codes, a_scales, w_codes, w_scales, I, K, out_codes, out_scales,
@@ -616,7 +621,7 @@ def mxfp4_linear_grouped_swiglu_quantize(plan, a_codes, a_scales, w_codes, w_sca
                                      _bytes(a_scales, R * K // 16, "a_scales"), _bytes(w_codes, E * N * K // 2, "w_codes"),
                                      _bytes(w_scales, E * ((N + 127) // 128 * 128) * (K // 16), "w_scales"), I, K,
                                      int(bool(rotate)), _bytes(out_codes, R * I // 2, "out_codes"),
-                                     _bytes(out_scales, R * I // 16, "out_scales"), _stream(stream)))
+                                     _bytes(out_scales, R * I // 16, "out_scales"), _handle(stream)))
 
 
 def nvfp4_qfit_workspace_size(batch, tokens, num_q_heads, num_kv_heads, grid_s, grid_m):
