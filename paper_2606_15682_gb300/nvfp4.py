@@ -474,36 +474,36 @@ def _rows(t, numel, what):
     return t.data_ptr()
 
 
-def _router(logits, top_k, score, renormalize, scale, bias):
+def _logits(logits, tokens):
+    """(pointer, nvfp4_float_type, elements between rows, experts) of a router's [tokens, experts]."""
     n, experts = logits.shape
-    if logits.dtype not in (_float32, _bf16) or (experts > 1 and logits.stride(1) != 1):
-        raise ValueError("logits must be row-major float32 or bfloat16 [tokens, experts]")
-    return (logits.data_ptr(), 1 if logits.dtype is _bf16 else 0, logits.stride(0) if n > 1 else experts, n, experts,
-            top_k, _ROUTE.pack(score, renormalize, scale, _typed(bias, _float32, "bias", experts) or 0))
+    between, step = logits.stride()
+    dtype = logits.dtype
+    if (dtype is not _float32 and dtype is not _bf16) or (step != 1 and experts > 1) or n != tokens:
+        raise ValueError("logits must be row-major float32 or bfloat16 [tokens, experts] of expert_idx's tokens")
+    return logits.data_ptr(), 1 if dtype is _bf16 else 0, between if n > 1 else experts, experts
 
 
 def moe_route(logits, expert_idx, weights, score=MOE_SOFTMAX, renormalize=True, scale=1.0, bias=None, stream=None):
     """The experts expert_idx [tokens, top_k] (int32) of each token and their weights (float32) from logits [tokens,
     experts]; bias (with MOE_SIGMOID) moves the choice alone."""
     n, k = expert_idx.shape
-    if n != logits.shape[0]:
-        raise ValueError("expert_idx must be [tokens, top_k] of the logits' tokens")
-    _check("moe_route", _moe_route(*_router(logits, k, score, renormalize, scale, bias),
-                                   _typed(expert_idx, _int32, "expert_idx"),
-                                   _typed(weights, _float32, "weights", n * k), _handle(stream)))
+    lp, kind, ld, experts = _logits(logits, n)
+    _check("moe_route",
+           _moe_route(lp, kind, ld, n, experts, k,
+                      _ROUTE.pack(score, renormalize, scale, 0 if bias is None else _floats(bias, experts, "bias")),
+                      _typed(expert_idx, _int32, "expert_idx"), _floats(weights, n * k, "weights"), _handle(stream)))
 
 
 def moe_route_backward(logits, expert_idx, d_weights, d_logits, score=MOE_SOFTMAX, renormalize=True, scale=1.0,
                        stream=None):
     """The logits' gradient (dense, of their type) from that of moe_route's weights."""
     n, k = expert_idx.shape
-    if n != logits.shape[0]:
-        raise ValueError("expert_idx must be [tokens, top_k] of the logits' tokens")
+    lp, kind, ld, experts = _logits(logits, n)
     _check("moe_route_backward",
-           _moe_route_backward(*_router(logits, k, score, renormalize, scale, None),
-                               _typed(expert_idx, _int32, "expert_idx"),
-                               _typed(d_weights, _float32, "d_weights", n * k),
-                               _typed(d_logits, logits.dtype, "d_logits", logits.numel()), _handle(stream)))
+           _moe_route_backward(lp, kind, ld, n, experts, k, _ROUTE.pack(score, renormalize, scale, 0),
+                               _typed(expert_idx, _int32, "expert_idx"), _floats(d_weights, n * k, "d_weights"),
+                               _typed(d_logits, logits.dtype, "d_logits", n * experts), _handle(stream)))
 
 
 def moe_sort(plan, expert_idx, stream=None):
