@@ -250,34 +250,24 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const RouteArg
 
 template <int kPer, bool kBf16, bool kWide>
 __global__ void __launch_bounds__(kRouteThreads) moe_route_backward_kernel(const RouteArgs a) {
-  __shared__ float rows[kRouteThreads / 32][kPer * 32];
   griddep_wait_and_release();
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (kRouteThreads / 32) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (t >= a.tokens) return;
-  float* row = rows[threadIdx.x >> 5];
-  float l[kPer];
-  load_logits<kPer, kBf16, kWide>(a, t, lane, l);
-  float top = -kInf;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    top = fmaxf(top, l[i]);
-    row[expert_at<kWide>(i, lane)] = l[i];
-  }
-  __syncwarp();
   // Lane j: choice j, its D and its logit.
   int e = lane < a.top_k ? __ldg(a.idx + t * a.top_k + lane) : -1;
   if (e >= a.experts) e = -1;
-  const float le = e >= 0 ? row[e] : -kInf;
   float D = e >= 0 ? a.scale * __ldg(a.d_weights + t * a.top_k + lane) : 0.0f;
+  float l[kPer];
+  load_logits<kPer, kBf16, kWide>(a, t, lane, l);
+  const float le = e >= 0 ? fmaxf(load_logit<kBf16>(a, t * a.ld + e), -kInf) : -kInf;
   if (!(le > -kInf)) {  // never chosen by the forward pass
     e = -1;
     D = 0.0f;
   }
-  __syncwarp();
+  float top = -kInf;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) row[expert_at<kWide>(i, lane)] = 0.0f;
-  __syncwarp();
+  for (int i = 0; i < kPer; ++i) top = fmaxf(top, l[i]);
   float p, spread = 0.0f;  // spread: what softmax without norming takes off all experts
   float total = 0.0f;
   if (a.sigmoid) {
@@ -308,22 +298,17 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_backward_kernel(const
       spread = warp_sum(D) * inv;
     }
   }
-  // An expert that a caller's choices name twice gets both.
-  const uint32_t peers = __match_any_sync(0xffffffffu, e >= 0 ? e : -1 - lane);
-  if (__any_sync(0xffffffffu, __popc(peers) > 1)) {
-    for (int j = 0; j < a.top_k; ++j) {
-      if (lane == j && e >= 0) row[e] += D;
-      __syncwarp();
-    }
-  } else if (e >= 0) {
-    row[e] = D;
-  }
-  __syncwarp();
+  // To the lanes that hold the chosen experts; one that a caller's choices name twice gets both, in order.
   float d[kPer];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    d[i] = row[expert_at<kWide>(i, lane)];
-    if (!a.sigmoid && !a.renormalize && l[i] > -kInf) d[i] -= exp_below(l[i], top) * spread;
+  for (int i = 0; i < kPer; ++i)
+    d[i] = !a.sigmoid && !a.renormalize && l[i] > -kInf ? -exp_below(l[i], top) * spread : 0.0f;
+  for (int j = 0; j < a.top_k; ++j) {
+    const int x = __shfl_sync(0xffffffffu, e, j);
+    const float v = __shfl_sync(0xffffffffu, D, j);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (x == expert_at<kWide>(i, lane)) d[i] += v;
   }
   const int64_t out = t * a.experts;
 #pragma unroll
