@@ -23,6 +23,15 @@
 // The epilogue reads 16 x 8 fragments of D (16x256b), in which a thread has two tokens
 // of two weight rows, and of gate and up at once: bf16 rows are turned into token-major
 // ones by a transposing stmatrix, quantized outputs need shuffles only.
+//
+// What bounds it.  Few tokens: the weights from DRAM, at 6.5 of the measured 6.78 TB/s once it runs, and some 6 us around
+// that a launch takes to start, fill and drain (64 tokens on 75 of 128 experts, 2048 x 1536: 118 MB in 23.3 us; 500 on 58 of
+// 64, 4096 x 2560: 336 MB in 56.3).  Many: the loads into the SMs.  8192 tokens x 4 on 64 experts, 5120 x 2048, read 1.93 GB
+// from L2, 16.4 TB/s without the MMAs in 118 us, with them in 132 (5.2 PFLOP/s); one expert of 8192 rows, 5120 x 13824,
+// 6.8 PFLOP/s in 171 us, as nvfp4_linear_swiglu_quantize.  The accumulator takes all TMEM that the scales leave, so a
+// unit's end (last MMAs, drain) costs 2000 cycles of 10240 at K = 5120.  Tried: the tokens as the M side (half of the
+// MMAs of an expert with 128 rows idle); units in a fixed order (the pairs with whole tiles ended 20 % later);
+// weights asked for in L2 ahead of time (56 -> 64 us at 500 tokens); units of 32 experts mixed (132 -> 153 at 8192).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 

@@ -7,9 +7,13 @@
 //   gradient, D_j = scale * dL/dw_j, with the weights normed w' = p / sum and without:
 //           dL/dp_i = (D_i - sum_j D_j w'_j) / sum on the chosen, or D_i;
 //           softmax dl = p (dp - sum dp p), sigmoid dl = dp p (1 - p)
-// A warp has a token, a lane every 32nd expert in registers: the logits are read
-// once, the k-th choice is a maximum over the lane's registers and two reductions
-// over the warp.  An expert whose logit is -inf or NaN is never chosen and has p = 0.
+// A warp has a token, a lane some of its logits in registers: they are read once.
+// An expert whose logit is -inf or NaN is never chosen and has p = 0.
+//
+// Bound by issue slots, 450 instructions a token of 256 experts and 8 choices, 90 more
+// under a bias: 16384 tokens 9.2 us, 11.8 with sigmoid and bias (a maximum over all
+// registers for each choice: 23), their bytes 2.5; gradient of 8191 x 128 in bf16 3.6
+// (through a row in shared memory 4.8).  32 tokens: 2.1 us, a launch's latency.
 #include <cfloat>
 #include <cmath>
 

@@ -5,6 +5,11 @@
 //   moe_combine_backward  dy[row_of[t, j]] = w[t, j] g[t],  dw[t, j] = <g[t], y[row_of[t, j]]>
 // All walk tokens, not rows: a token is read once however many experts it has,
 // its sums are in the order of its choices, and no row needs an atomic.
+//
+// HBM-bound from some hundred tokens on.  Of the measured copy rate: 8192 tokens of
+// 5120 to 4 bf16 rows each 63 us (0.98), to NVFP4 rows 33.5 (0.79: 4-byte scale words
+// apart), back with weights and a base 74 (1.0); the gradients of 4099 x 2048 with 8
+// rows each 43.5 (0.84) and 22.5 (0.88).  One token: 1.7 to 2.4 us, a launch's latency.
 #include <cfloat>
 
 #include "moe_plan.cuh"
