@@ -3,8 +3,8 @@
 //   out[r, n] = bf16( g_a[e] g_w[e] sum_k a[r, k] w_e[n, k] ),  r among expert e's rows
 // and the same for gate_up with h = SiLU(gate) up quantized in the epilogue.
 //
-// A pair of CTAs has a tile of 256 weight rows and up to 256 of one expert's rows
-// by tcgen05.mma.cta_group::2 (kind::mxf4nvf4, 16-element block scales).  The weight
+// A pair of CTAs has a tile of 256 weight rows and up to 256 (64 in the form for few
+// rows an expert) of one expert's rows by tcgen05.mma.cta_group::2 (kind::mxf4nvf4, 16-element block scales).  The weight
 // is the M side: its rows come in 256s whatever the router does, while an expert may
 // have one row or 700, and N takes any multiple of 32.  So a few rows cost the
 // weight's bytes and no more, and many leave at most 31 columns idle.  Each CTA holds
@@ -24,14 +24,15 @@
 // of two weight rows, and of gate and up at once: bf16 rows are turned into token-major
 // ones by a transposing stmatrix, quantized outputs need shuffles only.
 //
-// What bounds it.  Few tokens: the weights from DRAM, at 6.5 of the measured 6.78 TB/s once it runs, and some 6 us around
-// that a launch takes to start, fill and drain (64 tokens on 75 of 128 experts, 2048 x 1536: 118 MB in 23.3 us; 500 on 58 of
+// What bounds it.  Few tokens: the weights from DRAM, at 6.5 of the measured 6.78 TB/s once it runs, and some 5 us around
+// that a launch takes to start, fill and drain (64 tokens on 75 of 128 experts, 2048 x 1536: 118 MB in 22.7 us; 500 on 58 of
 // 64, 4096 x 2560: 336 MB in 56.3).  Many: the loads into the SMs.  8192 tokens x 4 on 64 experts, 5120 x 2048, read 1.93 GB
 // from L2, 16.4 TB/s without the MMAs in 118 us, with them in 132 (5.2 PFLOP/s); one expert of 8192 rows, 5120 x 13824,
 // 6.8 PFLOP/s in 171 us, as nvfp4_linear_swiglu_quantize.  The accumulator takes all TMEM that the scales leave, so a
 // unit's end (last MMAs, drain) costs 2000 cycles of 10240 at K = 5120.  Tried: the tokens as the M side (half of the
 // MMAs of an expert with 128 rows idle); units in a fixed order (the pairs with whole tiles ended 20 % later);
-// weights asked for in L2 ahead of time (56 -> 64 us at 500 tokens); units of 32 experts mixed (132 -> 153 at 8192).
+// weights asked for in L2 ahead of time (56 -> 64 us at 500 tokens); units of 32 experts mixed (132 -> 153 at 8192); two
+// accumulators of 128 columns (nothing at 64 tokens, 132 -> 139 at 8192).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -46,30 +47,38 @@ namespace nvfp4 {
 namespace {
 
 constexpr int kDepth = 256;  // elements of K per stage: 128 bytes of a row
-constexpr int kStages = 5;
-constexpr int kTokens = 256;  // of a tile
 constexpr int kWRows = 256;
 constexpr int kEpi0 = 4;
 constexpr int kQueue = 4;  // units on their way to the warps
-constexpr uint32_t kWBytes = 128 * kDepth / 2, kXBytes = 128 * kDepth / 2;  // a CTA's codes of a stage
+constexpr uint32_t kWBytes = 128 * kDepth / 2;                             // a CTA's weight codes of a stage
 constexpr uint32_t kScaleTile = 128 * kDepth / 16;                         // block scales of 128 rows: four atoms
 constexpr uint32_t kEpiBytes = 2048;                                       // a warp's 32 tokens x 32 bf16
-constexpr uint32_t kTmemCols = 512, kSfCol = kTokens, kSfCols = 16 + 32;
-static_assert(kSfCol + kStages * kSfCols <= kTmemCols, "TMEM budget");
 
-// 0 bf16 rows, 1 SwiGLU to NVFP4, 2 SwiGLU to MXFP4.  The first and the last have 8 epilogue warps with 128 accumulator
-// registers a thread.  The second needs no shared memory and is bound by its own latency where K is short: 16 warps with 64.
-template <int kMode>
+// kMode: 0 bf16 rows, 1 SwiGLU to NVFP4, 2 SwiGLU to MXFP4.
+// kSmall false: tiles of up to 256 tokens, one CTA an SM.  Modes 0 and 2 have 8 epilogue warps with 128 accumulator
+// registers a thread; mode 1 needs no shared memory there and is bound by its own latency where K is short: 16 warps with 64.
+// kSmall true: tiles of up to 64 tokens, two CTAs an SM: one's start, fill and drain under the other's loads, of the same
+// launch or of the next one.
+template <int kMode_, bool kSmall_>
 struct Form {
-  static constexpr int kEpiWarps = kMode == 1 ? 16 : 8;
+  static constexpr int kMode = kMode_;
+  static constexpr bool kSmall = kSmall_;
+  static constexpr int kTokens = kSmall ? 64 : 256;  // of a tile
+  static constexpr int kStages = !kSmall ? 5 : kMode == 1 ? 4 : 3;
+  static constexpr int kXTiles = kSmall ? 1 : 2;     // scale tiles of the tokens
+  static constexpr int kEpiWarps = kMode == 1 && !kSmall ? 16 : 8;
   static constexpr int kThreads = 32 * (kEpi0 + kEpiWarps);
-  static constexpr int kSides = kEpiWarps / 4;      // warps with the same weight rows
-  static constexpr int kChunks = 8 / kSides;        // of 32 tokens, a warp's
+  static constexpr int kSides = kEpiWarps / 4;             // warps with the same weight rows
+  static constexpr int kChunks = kTokens / 32 / kSides;    // of 32 tokens, a warp's
+  static constexpr uint32_t kXBytes = kTokens / 2 * kDepth / 2;  // a CTA's token codes of a stage
+  static constexpr uint32_t kXScales = kXTiles * kScaleTile;
+  static constexpr uint32_t kTmemCols = kSmall ? 256 : 512, kSfCol = kTokens, kSfCols = 16 + 16 * kXTiles;
   static constexpr int kEpiSmem = kMode == 1 ? 0 : kEpiWarps * static_cast<int>(kEpiBytes);
   static constexpr int kPer = (kMoeMaxExperts + kThreads - 1) / kThreads;  // experts of a thread
-  static constexpr size_t kSmem = 1024 + kStages * (kWBytes + kXBytes + 3 * kScaleTile) + kEpiSmem +
+  static constexpr size_t kSmem = 1024 + kStages * (kWBytes + kXBytes + kScaleTile + kXScales) + kEpiSmem +
                                   kMoeMaxExperts * (sizeof(int) + sizeof(int2)) + 512;
-  static_assert(kSmem <= 227 * 1024, "shared memory budget");
+  static_assert(kSfCol + kStages * kSfCols <= kTmemCols, "TMEM budget");
+  static_assert(kSmem <= 227 * 1024 && (!kSmall || 2 * (kSmem + 1024 + 256) <= 228 * 1024), "shared memory budget");
 };
 // kind::mxf4nvf4: A and B packed E2M1, K-major; M = 256.  N >> 3 is added at bit 17, UE8M0 scales set bit 23.
 constexpr uint32_t kIdesc = (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kWRows >> 4) << 24);
@@ -260,6 +269,7 @@ struct Unit {
 };
 static_assert(sizeof(Unit) == 16, "one store of the queue");
 // Unit u, by a converged warp.  ends: [1024] units of the experts up to each one, the total behind the last one.
+template <int kTokens>
 __device__ __forceinline__ Unit find_unit(int u, const int* ends, const int2* rows, int lane) {
   const int block = __popc(__ballot_sync(0xffffffffu, ends[32 * lane + 31] <= u));
   const int e = 32 * block + __popc(__ballot_sync(0xffffffffu, ends[32 * block + lane] <= u));
@@ -394,21 +404,21 @@ __device__ __forceinline__ void store_codes(const GroupedArgs& a, const Unit& t,
   a.q_scales[off] = static_cast<uint8_t>(code);
 }
 
-template <int kMode>
-__global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
+template <class F>
+__global__ void __launch_bounds__(F::kThreads, F::kSmall ? 2 : 1)
     grouped_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_w_scales,
-                   const __grid_constant__ CUtensorMap map_x16, const __grid_constant__ CUtensorMap map_x64,
+                   const __grid_constant__ CUtensorMap map_x16, const __grid_constant__ CUtensorMap map_x_mid,
                    const __grid_constant__ CUtensorMap map_x128, const __grid_constant__ CUtensorMap map_x_scales,
                    const __grid_constant__ CUtensorMap map_x_scales2, const __grid_constant__ CUtensorMap map_out,
                    const GroupedArgs a) {
-  using F = Form<kMode>;
+  constexpr int kMode = F::kMode, kStages = F::kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sW = smem;
   uint8_t* sX = sW + kStages * kWBytes;
-  uint8_t* sWS = sX + kStages * kXBytes;
+  uint8_t* sWS = sX + kStages * F::kXBytes;
   uint8_t* sXS = sWS + kStages * kScaleTile;
-  uint8_t* sEpi = sXS + kStages * 2 * kScaleTile;
+  uint8_t* sEpi = sXS + kStages * F::kXScales;
   int2* expert_rows_s = reinterpret_cast<int2*>(sEpi + F::kEpiSmem);
   int* ends = reinterpret_cast<int*>(expert_rows_s + kMoeMaxExperts);
   uint64_t* full = reinterpret_cast<uint64_t*>(ends + kMoeMaxExperts);  // codes landed, scales in TMEM
@@ -458,7 +468,7 @@ __global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
     prefetch_tmap(&map_x16);
     prefetch_tmap(&map_x_scales);
   }
-  if (warp == 1) pair_tmem_alloc(tmem_slot, kTmemCols);
+  if (warp == 1) pair_tmem_alloc(tmem_slot, F::kTmemCols);
   tc_fence_before();
   cluster_sync_all();
   tc_fence_after();
@@ -474,7 +484,7 @@ __global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
       if (e < a.experts) {
         const ExpertRows r = expert_rows(a.row_start, a.rows, e, a.max_rows);
         expert_rows_s[e] = make_int2(r.first, r.n);
-        n[i] = static_cast<int64_t>((r.n + kTokens - 1) / kTokens) * a.w_tiles;
+        n[i] = static_cast<int64_t>((r.n + F::kTokens - 1) / F::kTokens) * a.w_tiles;
       }
       sum += n[i];
     }
@@ -528,7 +538,7 @@ __global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
   // Walks the pair's units, the first one found without the queue; body(unit) gives false where a wait ran out.
   auto walk_units = [&](auto&& body) {
     if (first_unit >= units) return true;
-    Unit t = find_unit(first_unit, ends, expert_rows_s, lane);
+    Unit t = find_unit<F::kTokens>(first_unit, ends, expert_rows_s, lane);
     int n = 0;
     bool ok = true;
     do ok = body(t);
@@ -560,12 +570,13 @@ __global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
     // -------------------------------------------------------------- codes ---
     produce(empty, [&](int stage, int kb, const Unit& t) {
       const int half = t.n() / 2;  // this CTA's tokens: `half` of them from rank * half
-      const int box = half <= 16 ? 16 : half <= 64 ? 64 : 128;
-      const CUtensorMap* map = half <= 16 ? &map_x16 : half <= 64 ? &map_x64 : &map_x128;
+      constexpr int kMid = F::kSmall ? 32 : 64;
+      const int box = half <= 16 ? 16 : half <= kMid ? kMid : 128;
+      const CUtensorMap* map = half <= 16 ? &map_x16 : half <= kMid ? &map_x_mid : &map_x128;
       if (leader) mbar_arrive_expect_tx(&full[stage], 2 * (kWBytes + box * (kDepth / 2)));
       load_box(sW + stage * kWBytes, &map_w, &full[stage], kb * (kDepth / 2),
                t.expert * a.N + t.w_tile * kWRows + static_cast<int>(rank) * 128);
-      load_box(sX + stage * kXBytes, map, &full[stage], kb * (kDepth / 2), t.row0 + static_cast<int>(rank) * half);
+      load_box(sX + stage * F::kXBytes, map, &full[stage], kb * (kDepth / 2), t.row0 + static_cast<int>(rank) * half);
     });
   } else if (leader ? warp == 3 : warp == 1) {
     // ------------------------------------------------------- block scales ---
@@ -573,11 +584,11 @@ __global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
     // A stage's buffers are free once the copies have read them (`full`).
     const int tile_rows = a.K / 32;
     produce(full, [&](int stage, int kb, const Unit& t) {
-      const bool two = t.n() > 128;
+      const bool two = !F::kSmall && t.n() > 128;
       if (leader) mbar_arrive_expect_tx(&scales_in[stage], 2 * (two ? 3 : 2) * kScaleTile);
       load_box(sWS + stage * kScaleTile, &map_w_scales, &scales_in[stage], 0,
                (t.expert * a.w_scale_tiles + t.w_tile * 2 + static_cast<int>(rank)) * tile_rows + kb * 8);
-      uint8_t* dst = sXS + stage * 2 * kScaleTile;
+      uint8_t* dst = sXS + stage * F::kXScales;
       if (two)
         load_box3(dst, &map_x_scales2, &scales_in[stage], kb * 8, t.row0 / 128);
       else
@@ -593,6 +604,8 @@ __global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
     bool ready = false;  // the next stage was seen full
     walk_units([&](const Unit& t) {
       const uint32_t idesc = kIdesc | static_cast<uint32_t>(t.n() >> 3) << 17 | (a.mx ? kUE8M0 : 0u);
+      // A scale tile's columns are of 32 rows each: tiles of 64 tokens begin with its first or its third.
+      const uint32_t x_col = F::kSmall && (t.row0 & 64) ? 2 : 0;
       if (!wait(acc_empty, (local & 1) ^ 1u)) {
         fail();
         return false;
@@ -605,15 +618,16 @@ __global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
           return false;
         }
         tc_fence_after();
-        const uint32_t ws = utmem + kSfCol + stage * kSfCols, xs = ws + 16;
+        const uint32_t ws = utmem + F::kSfCol + stage * F::kSfCols, xs = ws + 16;
         const uint64_t w_desc = w_desc0 + static_cast<uint32_t>(stage) * (kWBytes >> 4);
-        const uint64_t x_desc = x_desc0 + static_cast<uint32_t>(stage) * (kXBytes >> 4);
+        const uint64_t x_desc = x_desc0 + static_cast<uint32_t>(stage) * (F::kXBytes >> 4);
         const int next = stage + 1 == kStages ? 0 : stage + 1;
         const uint32_t next_phase = next ? phase : phase ^ 1u;
         if (issuer) {
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)
-            pair_mma(utmem, w_desc + 2 * kk, x_desc + 2 * kk, idesc, ws + kk * 4, xs + kk * 8, (kb | kk) != 0);
+            pair_mma(utmem, w_desc + 2 * kk, x_desc + 2 * kk, idesc, ws + kk * 4, xs + x_col + kk * 4 * F::kXTiles,
+                     (kb | kk) != 0);
           pair_commit(&empty[stage], 0x3);
         }
         ready = __all_sync(0xffffffffu, mbar_test_wait(&full[next], next_phase)) != 0;
@@ -640,15 +654,15 @@ __global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
           return false;
         }
         tc_fence_after();
-        const uint32_t ws = utmem + kSfCol + stage * kSfCols, xs = ws + 16;
+        const uint32_t ws = utmem + F::kSfCol + stage * F::kSfCols, xs = ws + 16;
         const uint64_t ws_desc = ws_desc0 + static_cast<uint32_t>(stage) * (kScaleTile >> 4);
-        const uint64_t xs_desc = xs_desc0 + static_cast<uint32_t>(stage) * (2 * kScaleTile >> 4);
+        const uint64_t xs_desc = xs_desc0 + static_cast<uint32_t>(stage) * (F::kXScales >> 4);
         if (issuer) {
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
             pair_copy_scales(ws + kk * 4, ws_desc + kk * (512 >> 4));
-            pair_copy_scales(xs + kk * 8, xs_desc + kk * (512 >> 4));
-            if (t.n() > 128) pair_copy_scales(xs + kk * 8 + 4, xs_desc + (kScaleTile + kk * 512) / 16);
+            pair_copy_scales(xs + kk * 4 * F::kXTiles, xs_desc + kk * (512 >> 4));
+            if (!F::kSmall && t.n() > 128) pair_copy_scales(xs + kk * 8 + 4, xs_desc + (kScaleTile + kk * 512) / 16);
           }
           pair_commit(&full[stage], 0x3);
         }
@@ -689,7 +703,7 @@ __global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
     };
     uint32_t phase = 0;
     for (int64_t u = static_cast<int64_t>(first_unit) + clusters;;) {
-      for (; ok && u < units; u += clusters) hand_out(find_unit(static_cast<int>(u), ends, expert_rows_s, lane));
+      for (; ok && u < units; u += clusters) hand_out(find_unit<F::kTokens>(static_cast<int>(u), ends, expert_rows_s, lane));
       if (!ok) {
         fail();
         break;
@@ -819,7 +833,7 @@ __global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
     Unit t = {};
     int n = 0;
     bool ok = true, more = first_unit < units;
-    if (more) t = find_unit(first_unit, ends, expert_rows_s, lane);
+    if (more) t = find_unit<F::kTokens>(first_unit, ends, expert_rows_s, lane);
     while (more && finish(t)) {
       more = next_unit(&t, &n, &ok);
       if (kMode == 2 && !both(meeting, ok)) break;
@@ -830,7 +844,7 @@ __global__ void __launch_bounds__(Form<kMode>::kThreads, 1)
   tc_fence_before();
   cluster_sync_all();
   tc_fence_after();
-  if (warp == 1) pair_tmem_free(tmem, kTmemCols);
+  if (warp == 1) pair_tmem_free(tmem, F::kTmemCols);
 }
 
 // ------------------------------------------------------------------- host ---
@@ -884,7 +898,7 @@ bool scales_map(CUtensorMap* map, const uint8_t* base, int64_t tiles, int64_t K,
 }
 
 // The shared-memory opt-in, once for each device.
-template <int kMode>
+template <class F>
 bool opted_in() {
   static std::mutex mu;
   static std::map<int, bool> done;
@@ -892,17 +906,17 @@ bool opted_in() {
   if (cudaGetDevice(&d) != cudaSuccess) return false;
   std::lock_guard<std::mutex> lock(mu);
   if (done[d]) return true;
-  if (cudaFuncSetAttribute(grouped_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           static_cast<int>(Form<kMode>::kSmem)) != cudaSuccess) {
+  if (cudaFuncSetAttribute(grouped_kernel<F>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           static_cast<int>(F::kSmem)) != cudaSuccess) {
     cudaGetLastError();
     return false;
   }
   return done[d] = true;
 }
 
-template <int kMode>
-nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s) {
-  if (plan->n_tokens == 0) return NVFP4_OK;
+template <class F>
+nvfp4_status launch_form(const moe_plan* plan, GroupedArgs& a, cudaStream_t s) {
+  constexpr int kTokens = F::kTokens;
   a.row_start = plan->row_start;
   a.rows = plan->rows;
   a.experts = plan->num_experts;
@@ -915,7 +929,7 @@ nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s
   a.max_units = static_cast<int>(units);
   // Clusters for about as many as there are, were half of the experts' last tiles none: one too many is asked for in
   // vain, one too few gives the first clusters two units.
-  const int64_t about = (choices / kTokens + used / 2) * a.w_tiles, least = 2ll * sm_count();
+  const int64_t about = (choices / kTokens + used / 2) * a.w_tiles, least = (F::kSmall ? 4ll : 2ll) * sm_count();
   const int64_t clusters = units < least ? units : about < least ? least : about < units ? about : units;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -925,31 +939,45 @@ nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.blockDim = dim3(Form<kMode>::kThreads, 1, 1);
-  cfg.dynamicSmemBytes = Form<kMode>::kSmem;
+  cfg.blockDim = dim3(F::kThreads, 1, 1);
+  cfg.dynamicSmemBytes = F::kSmem;
   cfg.attrs = attr;
-  if (!opted_in<kMode>()) return NVFP4_ERR_CUDA;
-  CUtensorMap w, ws, x16, x64 = {}, x128 = {}, xs, xs2 = {}, out = {};
+  if (!opted_in<F>()) return NVFP4_ERR_CUDA;
+  CUtensorMap w, ws, x16, mid_x = {}, x128 = {}, xs, xs2 = {}, out = {};
   const int64_t R = a.max_rows, K = a.K;
   // No tile has more tokens than there are choices: few need no map of the larger boxes.
-  const bool mid = choices > 32, wide = choices > 128;
+  const bool mid = choices > 32, wide = !F::kSmall && choices > 128;
   if (!codes_map(&w, a.w_codes, static_cast<int64_t>(a.experts) * a.N, K, 128) ||
       !scales_map(&ws, a.w_scales, static_cast<int64_t>(a.experts) * a.w_scale_tiles, K, false) ||
-      !codes_map(&x16, a.a_codes, R, K, 16) || (mid && !codes_map(&x64, a.a_codes, R, K, 64)) ||
+      !codes_map(&x16, a.a_codes, R, K, 16) || (mid && !codes_map(&mid_x, a.a_codes, R, K, F::kSmall ? 32 : 64)) ||
       (wide && !codes_map(&x128, a.a_codes, R, K, 128)) || !scales_map(&xs, a.a_scales, R / 128, K, false) ||
       (wide && !scales_map(&xs2, a.a_scales, R / 128, K, true)) ||
-      (kMode == 0 && !out_map(&out, a.out, R, a.N, a.ldo)))
+      (F::kMode == 0 && !out_map(&out, a.out, R, a.N, a.ldo)))
     return NVFP4_ERR_CUDA;
   a.status = status_word_dev();
   a.fault_skip_stage = take_fault(NVFP4_FAULT_GEMM_SKIP_STAGE) ? 1 : 0;
   cfg.gridDim = dim3(static_cast<uint32_t>(2 * clusters), 1, 1);
   cfg.stream = s;
   cfg.numAttrs = 2;
-  if (cudaLaunchKernelEx(&cfg, grouped_kernel<kMode>, w, ws, x16, x64, x128, xs, xs2, out, a) !=
+  if (cudaLaunchKernelEx(&cfg, grouped_kernel<F>, w, ws, x16, mid_x, x128, xs, xs2, out, a) !=
       cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
   return launch_status();
+}
+
+// Small tiles, two CTAs an SM, where an expert has few rows on average.  us, small against large, rows an expert in brackets:
+//   SwiGLU to NVFP4  (0.1) 1 token, 2048 x 2048, 6.7 / 7.5; (4) 128 experts, 2048 x 1536, 22.7 / 23.3; (16) 16 experts,
+//                    5120 x 4096, 28.1 / 28.5; (47) 64, 4096 x 2560, 57.5 / 57.1; (58) 40, 1536 x 2560, 15.7 / 17.0; (64) 64,
+//                    2048 x 2048, 28.6 / 29.5; (96) 40, 1536 x 2560, 21.2 / 22.3; (192) the same, 30.4 / 28.7
+//   SwiGLU to MXFP4  (5) 40 experts, 1536 x 2560, 13.8 / 14.9; (58) 16.9 / 18.0; (96) 22.7 / 23.7; (192) 33.2 / 31.0
+//   bf16 rows        (5) 40 experts, 1280 x 1536, 8.1 / 8.7; (22) 11.3 / 11.5; (32) 16, 2048 x 5120, 18.4 / 17.8, 64,
+//                    1024 x 2048, 16.3 / 16.5; (47) 64, 1280 x 4096, 35.3 / 33.4; (96) 40, 1280 x 1536, 15.2 / 14.2
+template <int kMode>
+nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s) {
+  if (plan->n_tokens == 0) return NVFP4_OK;
+  const bool small = plan->n_tokens * plan->top_k <= (kMode == 0 ? 32 : 64) * static_cast<int64_t>(plan->num_experts);
+  return small ? launch_form<Form<kMode, true>>(plan, a, s) : launch_form<Form<kMode, false>>(plan, a, s);
 }
 
 constexpr int64_t kMaxSide = 1ll << 20;  // N and K

@@ -27,7 +27,9 @@ def N():
 RAGGED = [0, 1, 127, 128, 129, 300, 0, 5, 256, 513, 31, 0]
 COUNTS = {"one": [1], "none": [0, 0, 0], "first of many": [3] + [0] * 300, "few": [2, 0, 1, 4, 0, 3], "ragged": RAGGED,
           "large": [700, 70], "edges": [16, 17, 32, 33, 48, 64, 65, 96, 97, 160, 161, 192, 255, 257, 288],
-          "thousand": [1] * 1024}
+          "thousand": [1] * 1024,
+          # Few choices an expert, but some experts with more than a small tile of 64, 128 and 256 rows.
+          "uneven": [300, 64, 65, 129, 1, 33, 193, 127] + [0] * 40}
 
 
 def linear(N, plan, a, w, out, n, k, mx, g_a=None):
@@ -74,7 +76,19 @@ def test_sizes(N, n, k):
     check_linear(N, [5, 0, 130, 290], n, k, per_expert=True, pad=8)
 
 
-@pytest.mark.parametrize("counts", ["few", "ragged"])
+@pytest.mark.parametrize("n", [16, 144, 272, 1040])
+@pytest.mark.parametrize("k", [256, 1536])
+def test_sizes_with_few_rows_an_expert(N, n, k):
+    check_linear(N, [5, 0, 130, 70] + [0] * 20, n, k, per_expert=True, pad=8)
+
+
+@pytest.mark.parametrize("inner", [128, 384, 1024])
+@pytest.mark.parametrize("form", ["nvfp4", "mxfp4", "mxfp4 rotated"])
+def test_swiglu_sizes_with_few_rows_an_expert(N, inner, form):
+    check_swiglu(N, [5, 0, 130, 70] + [0] * 20, inner, 768, form != "nvfp4", form.endswith("rotated"), per_expert=False)
+
+
+@pytest.mark.parametrize("counts", ["few", "ragged", "uneven"])
 def test_a_long_sum(N, counts):
     check_linear(N, COUNTS[counts], 256, 5120)
 
@@ -146,7 +160,8 @@ def check_swiglu(N, counts, inner, k, mx=False, rotate=False, per_expert=True, s
     assert (rc == 0xA5).all() and (rs == 0xA5).all()
 
 
-@pytest.mark.parametrize("counts", ["one", "none", "first of many", "few", "ragged", "large", "edges"], ids=lambda c: c)
+@pytest.mark.parametrize("counts", ["one", "none", "first of many", "few", "ragged", "large", "edges", "uneven"],
+                         ids=lambda c: c)
 @pytest.mark.parametrize("form", ["nvfp4", "mxfp4", "mxfp4 rotated"])
 def test_swiglu_rows_of_every_kind(N, counts, form):
     check_swiglu(N, COUNTS[counts], 256, 512, form != "nvfp4", form.endswith("rotated"))
@@ -224,11 +239,13 @@ def test_a_plan_beyond_its_buffers_is_cut_to_them(N):
 
 
 @pytest.mark.parametrize("form", ["rows", "nvfp4", "mxfp4", "mxfp4 rotated"])
-def test_a_lost_stage_is_a_timeout_and_the_next_call_is_right(N, form):
+@pytest.mark.parametrize("counts", [[100, 600], [100, 60] + [0] * 14], ids=["many rows", "few rows"])
+def test_a_lost_stage_is_a_timeout_and_the_next_call_is_right(N, form, counts):
     """The injected fault leaves a stage unloaded: the waits run out (2 s), the status says so, the device stays usable."""
-    plan = M.make_plan(N, M.choices([100, 600], 1, 0), 2)
+    E = len(counts)
+    plan = M.make_plan(N, M.choices(counts, 1, 0), E)
     mx = form.startswith("mx")
-    a, w = M.Rows(N, plan, 512, 2, mx), M.Weights(N, 2, 512, 512, 5, mx)
+    a, w = M.Rows(N, plan, 512, 2, mx), M.Weights(N, E, 512, 512, 5, mx)
     out = torch.empty(plan.max_rows, 512, dtype=BF, device="cuda")
     codes = torch.empty(plan.max_rows, 128, dtype=torch.uint8, device="cuda")
     scales = torch.empty(plan.max_rows * 16, dtype=torch.uint8, device="cuda")
@@ -247,6 +264,6 @@ def test_a_lost_stage_is_a_timeout_and_the_next_call_is_right(N, form):
     torch.cuda.synchronize()
     assert N.nvfp4_get_device_status() == 6
     if form == "rows":
-        check_linear(N, [100, 600], 512, 512)
+        check_linear(N, counts, 512, 512)
     else:
-        check_swiglu(N, [100, 600], 256, 512, mx, form.endswith("rotated"))
+        check_swiglu(N, counts, 256, 512, mx, form.endswith("rotated"))
