@@ -3,8 +3,9 @@
 //   out[r, n] = bf16( g_a[e] g_w[e] sum_k a[r, k] w_e[n, k] ),  r among expert e's rows
 // and the same for gate_up with h = SiLU(gate) up quantized in the epilogue.
 //
-// A pair of CTAs has a tile of 256 weight rows and up to 256 (64 in the form for few
-// rows an expert) of one expert's rows by tcgen05.mma.cta_group::2 (kind::mxf4nvf4, 16-element block scales).  The weight
+// A pair of CTAs has a tile of 256 weight rows and up to 256 of one expert's rows (64
+// in the form for few rows an expert) by tcgen05.mma.cta_group::2 (kind::mxf4nvf4,
+// 16-element block scales).  The weight
 // is the M side: its rows come in 256s whatever the router does, while an expert may
 // have one row or 700, and N takes any multiple of 32.  So a few rows cost the
 // weight's bytes and no more, and many leave at most 31 columns idle.  Each CTA holds
@@ -27,12 +28,13 @@
 // What bounds it.  Few tokens: the weights from DRAM, at 6.5 of the measured 6.78 TB/s once it runs, and some 5 us around
 // that a launch takes to start, fill and drain (64 tokens on 75 of 128 experts, 2048 x 1536: 118 MB in 22.7 us; 500 on 58 of
 // 64, 4096 x 2560: 336 MB in 56.3).  Many: the loads into the SMs.  8192 tokens x 4 on 64 experts, 5120 x 2048, read 1.93 GB
-// from L2, 16.4 TB/s without the MMAs in 118 us, with them in 132 (5.2 PFLOP/s); one expert of 8192 rows, 5120 x 13824,
+// from L2, 16.4 TB/s without the MMAs in 118 us, with them in 132 to 136 (5.2 PFLOP/s); one expert of 8192 rows, 5120 x 13824,
 // 6.8 PFLOP/s in 171 us, as nvfp4_linear_swiglu_quantize.  The accumulator takes all TMEM that the scales leave, so a
 // unit's end (last MMAs, drain) costs 2000 cycles of 10240 at K = 5120.  Tried: the tokens as the M side (half of the
 // MMAs of an expert with 128 rows idle); units in a fixed order (the pairs with whole tiles ended 20 % later);
 // weights asked for in L2 ahead of time (56 -> 64 us at 500 tokens); units of 32 experts mixed (132 -> 153 at 8192); two
-// accumulators of 128 columns (nothing at 64 tokens, 132 -> 139 at 8192).
+// accumulators of 128 columns (nothing at 64 tokens, 132 -> 139 at 8192); two CTAs an SM with tiles of 128 tokens (between the
+// two forms or behind both: 2048 tokens on 16 experts 28.3 with 64, 24.7 with 128, 22.8 with 256; 8192 tokens 153).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
