@@ -287,12 +287,16 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_backward_kernel(const
     }
   } else {
     top = warp_max(top);
-    p = e >= 0 ? exp_below(le, top) : 0.0f;
     if (a.renormalize) {
+      // Shares among the chosen: against the largest of them, which a caller's own choices may have far below the rest.
+      const bool none = top == kInf && le < kInf;
+      top = warp_max(le);
+      p = e >= 0 && !none ? exp_below(le, top) : 0.0f;
       total = warp_sum(p);
       const float w = total > 0.0f ? p / total : 0.0f;
       D = w * (D - warp_sum(D * w));
     } else {
+      p = e >= 0 ? exp_below(le, top) : 0.0f;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) total += l[i] > -kInf ? exp_below(l[i], top) : 0.0f;
       total = warp_sum(total);

@@ -199,6 +199,31 @@ def test_gradient(N, tokens, experts, k, score, renormalize, dtype):
     assert N.nvfp4_get_device_status() == 0
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("experts", [20, 40, 256])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_gradient_of_choices_far_below_the_largest_logit(N, renormalize, experts, dtype):
+    """A caller's own choices: normed weights are shares among the chosen, however little softmax leaves to all of them;
+    beside a logit of +inf it leaves nothing."""
+    l = logits(6, experts, 3, dtype)
+    l[1, 0], l[2, 0], l[3, 0], l[4, 0] = 60, 150, 3e38, float("inf")
+    idx = torch.arange(1, 6, dtype=torch.int32, device="cuda").repeat(6, 1)
+    d = torch.randn(6, 5, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    out = torch.full((6, experts), float("nan"), dtype=dtype, device="cuda")
+    N.moe_route_backward(l, idx, d, out, renormalize=renormalize, scale=0.8)
+    l64 = l.double().cpu().numpy()
+    got = out.double().cpu().numpy()
+    assert (got[4] == 0).all()
+    if renormalize:
+        l64[3, 0] = 150  # the shares do not depend on it, and 64 bits have e^-150
+    else:
+        assert (got[3] == 0).all()
+    some = [0, 1, 2] + [3] * renormalize + [5]
+    want, mag = gradient(l64[some], idx.cpu().numpy()[some], d.double().cpu().numpy()[some], False, renormalize, 0.8)
+    half = M.half_ulp(want) * (1 + 2.0 ** -6) if dtype == torch.bfloat16 else 0
+    assert (np.abs(got[some] - want) <= half + 200 * UNIT * mag + 1e-37).all()
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("renormalize", [True, False])
 def test_gradient_is_that_of_differences(N, score, renormalize):
