@@ -824,9 +824,11 @@ nvfp4_status moe_combine_backward(const moe_plan* plan, const void* d_out_bf16, 
  *              the other; g_w: device float [num_experts].
  *   out_bf16 : [moe_max_rows, N] bf16, rows ldo apart.
  * Experts without rows cost nothing.  K % 256 == 0, N % 16 == 0, both positive and at
- * most 2^20, ldo >= N, ldo % 8 == 0, (num_experts * ceil(N / 128) + 2) * (K / 32) and
- * num_experts * N + 256 and moe_max_rows / 128 * (K / 32) below 2^31 (SHAPE); g_a_step 0 or 1 (INVALID_ARG); 16-B aligned, g's 4-B
- * (ALIGN).  A bounded on-device wait that expires sets TIMEOUT; out is then undefined.
+ * most 2^20, ldo >= N, ldo % 8 == 0, (num_experts * ceil(N / 128) + 2) * (K / 32),
+ * num_experts * N + 256 and moe_max_rows / 128 * (K / 32) below 2^31, fewer than 2^30
+ * tiles of 256 weight rows and an expert's next 256 rows (SHAPE); g_a_step 0 or 1
+ * (INVALID_ARG); 16-B aligned, g's 4-B (ALIGN).  A bounded on-device wait that expires
+ * sets TIMEOUT; out is then undefined.
  */
 nvfp4_status nvfp4_linear_grouped(const moe_plan* plan, const uint8_t* a_codes, const uint8_t* a_scales,
                                   const float* g_a, int32_t g_a_step, const uint8_t* w_codes, const uint8_t* w_scales,
