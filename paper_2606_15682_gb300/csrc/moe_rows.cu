@@ -9,7 +9,7 @@
 // HBM-bound from some hundred tokens on.  Of the measured copy rate: 8192 tokens of
 // 5120 to 4 bf16 rows each 63 us (0.98), to NVFP4 rows 33.5 (0.79: 4-byte scale words
 // apart), back with weights and a base 74 (1.0); the gradients of 4099 x 2048 with 8
-// rows each 43.5 (0.84) and 22.5 (0.88).  One token: 1.7 to 2.4 us, a launch's latency.
+// rows each 41.4 (0.88) and 22.5 (0.88).  One token: 1.7 to 2.4 us, a launch's latency.
 #include <cfloat>
 
 #include "moe_plan.cuh"
@@ -472,8 +472,8 @@ cudaError_t launch_combine(const RowArgs& a, int64_t tokens, uint32_t vecs, cons
                     static_cast<const uint16_t*>(base), ld_base, static_cast<uint16_t*>(out), ld_out);
 }
 
-// kWarps warps have a token, a batch of choices at a time: one load of d_out serves the batch.  More warps where the
-// tokens are few; their parts of a sum are added in order.
+// kWarps warps have a token, a batch of choices at a time: one load of d_out serves the batch.  Their parts of a sum are
+// added in order.
 constexpr int kBackThreads = 256;
 template <int kWarps>
 __global__ void __launch_bounds__(kBackThreads)
@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(kBackThreads)
                                 int64_t ld, const uint16_t* __restrict__ y, const float* __restrict__ weights,
                                 uint16_t* __restrict__ d_y, float* __restrict__ d_weights) {
   constexpr int kPer = kBackThreads / 32 / kWarps;  // tokens of a CTA
-  __shared__ float parts[kWarps > 1 ? kMoeMaxTopK : 1][kPer][kWarps];
+  __shared__ float parts[kMoeMaxTopK][kPer][kWarps];
   griddep_wait_and_release();
   const int warp = threadIdx.x >> 5, sub = warp / kWarps, part = warp % kWarps;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * kPer + sub;
@@ -520,22 +520,15 @@ __global__ void __launch_bounds__(kBackThreads)
     for (int j = 0; j < kBatch; ++j) {
 #pragma unroll
       for (int s = 16; s; s >>= 1) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], s);
-      if (lane == 0 && j0 + j < a.top_k) {
-        if constexpr (kWarps > 1)
-          parts[j0 + j][sub][part] = dot[j];
-        else if (d_weights)
-          d_weights[t * a.top_k + j0 + j] = dot[j];
-      }
+      if (lane == 0 && j0 + j < a.top_k) parts[j0 + j][sub][part] = dot[j];
     }
   }
-  if constexpr (kWarps > 1) {
-    __syncthreads();
-    if (d_weights && live && part == 0 && static_cast<int>(lane) < a.top_k) {
-      float sum = 0.0f;
+  __syncthreads();
+  if (d_weights && live && part == 0 && static_cast<int>(lane) < a.top_k) {
+    float sum = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) sum += parts[lane][sub][w];
-      d_weights[t * a.top_k + lane] = sum;
-    }
+    for (int w = 0; w < kWarps; ++w) sum += parts[lane][sub][w];
+    d_weights[t * a.top_k + lane] = sum;
   }
 }
 
@@ -709,11 +702,13 @@ NVFP4_API nvfp4_status moe_combine_backward(const moe_plan* plan, const void* d_
   if (!aligned(d_out_bf16, 16) || !aligned(y_bf16, 16) || !aligned(d_y_bf16, 16) || !aligned(weights, 4) ||
       !aligned(d_weights, 4))
     return NVFP4_ERR_ALIGN;
-  // Eight warps a token until one warp each fills the GPU.
-  const int64_t slots = static_cast<int64_t>(sm_count()) * 32;
-  const int warps = plan->n_tokens >= slots ? 1 : 4 * plan->n_tokens >= slots ? 4 : 8;
-  const auto kernel = warps == 1 ? moe_combine_backward_kernel<1>
-                      : warps == 4 ? moe_combine_backward_kernel<4> : moe_combine_backward_kernel<8>;
+  // A token's warps: eight where it has many units, or where the tokens are few; us with eight / two:
+  //   8192 tokens  2048 x 8 rows 87.8 / 90.3, 5120 x 4 112 / 114, 2048 x 2 38.5 / 33.5, 512 x 8 50.8 / 26.1
+  //   600 tokens   2048 x 8 7.9 / 11.8, 2048 x 2 3.6 / 5.5, 512 x 8 4.0 / 3.6;  64 tokens  2048 x 8 2.8 / 5.5, 512 x 8 2.3 / 2.6
+  // (one: 97, 119, 33.5, 26.8 at 8192 tokens; four: 89.8, 113, 36.3, 36.2).
+  const bool eight = cols / 8 * plan->top_k >= 1024 || 8 * plan->n_tokens <= 32 * static_cast<int64_t>(sm_count());
+  const int warps = eight ? 8 : 2;
+  const auto kernel = eight ? moe_combine_backward_kernel<8> : moe_combine_backward_kernel<2>;
   const int64_t per = kBackThreads / 32 / warps, grid = (plan->n_tokens + per - 1) / per;
   if (launch_pdl(kernel, dim3(static_cast<uint32_t>(grid)), dim3(kBackThreads), 0,
                  static_cast<cudaStream_t>(stream), row_args(plan), plan->n_tokens, static_cast<uint32_t>(cols / 8),

@@ -190,7 +190,7 @@ def test_combine(N, tokens, cols, weighted, based):
 
 
 @pytest.mark.parametrize("cols", COLS)
-@pytest.mark.parametrize("tokens,top_k", [(1, 3), (2, 1), (33, 8), (400, 5), (3, 32), (900, 2)])
+@pytest.mark.parametrize("tokens,top_k", [(1, 3), (2, 1), (33, 8), (400, 5), (3, 32), (900, 2), (701, 5)])
 def test_combine_backward(N, tokens, top_k, cols):
     if tokens > 100 and cols == 65536:
         tokens = 40
