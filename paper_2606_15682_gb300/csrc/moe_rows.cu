@@ -296,32 +296,74 @@ __device__ __forceinline__ void rows_of(const RowArgs& a, int64_t t, int j0, int
   }
 }
 
-__global__ void __launch_bounds__(kWalkThreads)
-    moe_dispatch_kernel(const RowArgs a, const Walk w, const uint16_t* __restrict__ x, int64_t ld,
+// A token's units among `threads` threads, U for each (and a pass), `threads` apart.  Bf16 rows with U = 2 / 1, us, there and
+// back: 16384 tokens of 2048, one row each 21.0 / 30.4 and 30.0 / 36.1, two 30.9 / 37.6 and 35.6 / 40.9, eight 92 / 91 and
+// 86 / 88; 600, one each 1.54 / 1.93 and 1.99 / 2.57; one token to and from eight, 2.05 / 1.89 and 2.90 / 2.57: 1 for up to a
+// token an SM.  Four take long tokens in one pass; a loop over passes (5120 channels back 89 for 74) only the longest (2000 x
+// 32768 from four rows in passes of two units 112, of four 99).
+struct Split {
+  int64_t tokens;
+  uint32_t vecs, threads, per_cta;
+  dim3 grid() const { return dim3(static_cast<uint32_t>((tokens + per_cta - 1) / per_cta)); }
+  dim3 block() const { return dim3((per_cta * threads + 31) / 32 * 32); }
+};
+template <int U>
+Split make_split(int64_t tokens, uint32_t vecs) {
+  const uint32_t passes = (vecs + 512 * U - 1) / (512 * U);
+  Split w = {tokens, vecs, (vecs + U * passes - 1) / (U * passes), 1u};
+  w.per_cta = short_tokens(tokens, w.threads);
+  return w;
+}
+
+template <int U, bool kLoop>
+__global__ void __launch_bounds__(512)
+    moe_dispatch_kernel(const RowArgs a, const Split w, const uint16_t* __restrict__ x, int64_t ld,
                         const float* __restrict__ weights, uint16_t* __restrict__ out) {
   griddep_wait_and_release();
-  walk(w, [&](int64_t t, uint32_t v, bool live) {
-    if (!live) return;
-    const uint4 in = __ldg(reinterpret_cast<const uint4*>(x + t * ld) + v);
+  const uint32_t sub = w.per_cta > 1 ? threadIdx.x / w.threads : threadIdx.x >= w.threads, vecs = w.vecs;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * w.per_cta + sub;
+  if (sub >= w.per_cta || t >= w.tokens) return;
+  uint32_t v0 = threadIdx.x - sub * w.threads;
+  do {
+    uint4 in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t v = v0 + u * w.threads;
+      if (v < vecs) in[u] = __ldg(reinterpret_cast<const uint4*>(x + t * ld) + v);
+    }
     for (int j0 = 0; j0 < a.top_k; j0 += kBatch) {
       int r[kBatch];
       rows_of(a, t, j0, r);
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
         if (r[j] < 0) continue;
-        uint4 d = in;
-        if (weights) {
-          const float c = __ldg(weights + t * a.top_k + j0 + j);
-          float f[8];
-          unpack_bf16x8(in, f);
+        const float c = weights ? __ldg(weights + t * a.top_k + j0 + j) : 1.0f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) f[i] *= c;
-          d = pack8(f);
+        for (int u = 0; u < U; ++u) {
+          const uint32_t v = v0 + u * w.threads;
+          if (v >= vecs) continue;
+          uint4 d = in[u];
+          if (weights) {
+            float f[8];
+            unpack_bf16x8(in[u], f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] *= c;
+            d = pack8(f);
+          }
+          reinterpret_cast<uint4*>(out)[static_cast<int64_t>(r[j]) * vecs + v] = d;
         }
-        reinterpret_cast<uint4*>(out)[static_cast<int64_t>(r[j]) * w.vecs + v] = d;
       }
     }
-  });
+    v0 += U * w.threads;
+  } while (kLoop && v0 < vecs);
+}
+
+template <int U, bool kLoop = false>
+cudaError_t launch_dispatch(const RowArgs& a, int64_t tokens, uint32_t vecs, const void* x, int64_t ld,
+                            const float* weights, void* rows, cudaStream_t s) {
+  const Split w = make_split<U>(tokens, vecs);
+  return launch_pdl(moe_dispatch_kernel<U, kLoop>, w.grid(), w.block(), 0, s, a, w, static_cast<const uint16_t*>(x), ld,
+                    weights, static_cast<uint16_t*>(rows));
 }
 
 // Codes and scale word of a thread's 32 channels to the token's rows.
@@ -403,26 +445,24 @@ __global__ void __launch_bounds__(kWalkThreads)
   });
 }
 
-// The sum is in 32 bits, in the order of the choices, rounded once.  A thread has U units of a token, units
-// blockDim.x apart, whose loads of a batch of choices are all in flight (without the batch 89 us for 8192 tokens of 5120
-// from 4 rows each; with it 74, the measured copy rate; in a loop over the units 89 again, so that only the longest
-// tokens, kLoop, have one).
+// The sum is in 32 bits, in the order of the choices, rounded once.  The loads of a batch of choices are all in flight
+// (without the batch 89 us for 8192 tokens of 5120 from 4 rows each; with it 74, the measured copy rate).
 template <int U, bool kLoop>
 __global__ void __launch_bounds__(512)
-    moe_combine_kernel(const RowArgs a, int64_t tokens, uint32_t vecs, uint32_t per_cta, const uint16_t* __restrict__ y,
+    moe_combine_kernel(const RowArgs a, const Split w, const uint16_t* __restrict__ y,
                        const float* __restrict__ weights, const uint16_t* base, int64_t ld_base, uint16_t* out,
                        int64_t ld_out) {
   griddep_wait_and_release();
-  const uint32_t sub = per_cta > 1 ? threadIdx.x / vecs : 0u;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * per_cta + sub;
-  if (sub >= per_cta || t >= tokens) return;
-  uint32_t v0 = threadIdx.x - sub * vecs;
+  const uint32_t sub = w.per_cta > 1 ? threadIdx.x / w.threads : threadIdx.x >= w.threads, vecs = w.vecs;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * w.per_cta + sub;
+  if (sub >= w.per_cta || t >= w.tokens) return;
+  uint32_t v0 = threadIdx.x - sub * w.threads;
   do {
     float acc[U][8] = {};
     if (base) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const uint32_t v = v0 + u * blockDim.x;
+        const uint32_t v = v0 + u * w.threads;
         if (v < vecs) unpack_bf16x8(reinterpret_cast<const uint4*>(base + t * ld_base)[v], acc[u]);  // out may be base
       }
     }
@@ -436,7 +476,7 @@ __global__ void __launch_bounds__(512)
         c[j] = r[j] < 0 ? 0.0f : weights ? __ldg(weights + t * a.top_k + j0 + j) : 1.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const uint32_t v = v0 + u * blockDim.x;
+          const uint32_t v = v0 + u * w.threads;
           if (r[j] >= 0 && v < vecs)
             in[j][u] = __ldg(reinterpret_cast<const uint4*>(y) + static_cast<int64_t>(r[j]) * vecs + v);
         }
@@ -455,21 +495,19 @@ __global__ void __launch_bounds__(512)
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t v = v0 + u * blockDim.x;
+      const uint32_t v = v0 + u * w.threads;
       if (v < vecs) reinterpret_cast<uint4*>(out + t * ld_out)[v] = pack8(acc[u]);
     }
-    v0 += U * blockDim.x;
+    v0 += U * w.threads;
   } while (kLoop && v0 < vecs);
 }
 
 template <int U, bool kLoop = false>
 cudaError_t launch_combine(const RowArgs& a, int64_t tokens, uint32_t vecs, const void* y, const float* weights,
                            const void* base, int64_t ld_base, void* out, int64_t ld_out, cudaStream_t s) {
-  const uint32_t passes = (vecs + 512 * U - 1) / (512 * U), units = (vecs + U * passes - 1) / (U * passes);
-  const uint32_t per_cta = U == 1 ? short_tokens(tokens, vecs) : 1u, cta = per_cta > 1 ? 256 : (units + 31) / 32 * 32;
-  return launch_pdl(moe_combine_kernel<U, kLoop>, dim3(static_cast<uint32_t>((tokens + per_cta - 1) / per_cta)), dim3(cta), 0, s,
-                    a, tokens, vecs, per_cta, static_cast<const uint16_t*>(y), weights,
-                    static_cast<const uint16_t*>(base), ld_base, static_cast<uint16_t*>(out), ld_out);
+  const Split w = make_split<U>(tokens, vecs);
+  return launch_pdl(moe_combine_kernel<U, kLoop>, w.grid(), w.block(), 0, s, a, w, static_cast<const uint16_t*>(y),
+                    weights, static_cast<const uint16_t*>(base), ld_base, static_cast<uint16_t*>(out), ld_out);
 }
 
 // kWarps warps have a token, a batch of choices at a time: one load of d_out serves the batch.  Their parts of a sum are
@@ -626,10 +664,11 @@ NVFP4_API nvfp4_status moe_dispatch(const moe_plan* plan, const void* x_bf16, in
   if (plan->n_tokens == 0) return NVFP4_OK;
   if (!x_bf16 || !rows_bf16) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(x_bf16, 16) || !aligned(rows_bf16, 16) || !aligned(weights, 4)) return NVFP4_ERR_ALIGN;
-  const WalkLaunch l = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 8));
-  if (launch_pdl(moe_dispatch_kernel, l.grid, l.block, 0, static_cast<cudaStream_t>(stream),
-                 row_args(plan), l.w, static_cast<const uint16_t*>(x_bf16), ld_x, weights,
-                 static_cast<uint16_t*>(rows_bf16)) != cudaSuccess)
+  const uint32_t vecs = static_cast<uint32_t>(cols / 8);
+  const auto launch = vecs <= 512 && plan->n_tokens <= sm_count() ? launch_dispatch<1>
+                      : vecs <= 1024 ? launch_dispatch<2> : vecs <= 2048 ? launch_dispatch<4> : launch_dispatch<2, true>;
+  if (launch(row_args(plan), plan->n_tokens, vecs, x_bf16, ld_x, weights, rows_bf16,
+             static_cast<cudaStream_t>(stream)) != cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
   return launch_status();
@@ -682,7 +721,7 @@ NVFP4_API nvfp4_status moe_combine(const moe_plan* plan, const void* y_bf16, int
       (base_bf16 && ld_base % 8))
     return NVFP4_ERR_ALIGN;
   const uint32_t vecs = static_cast<uint32_t>(cols / 8);
-  const auto launch = vecs <= 256 ? launch_combine<1>
+  const auto launch = vecs <= 512 && plan->n_tokens <= sm_count() ? launch_combine<1>
                       : vecs <= 1024 ? launch_combine<2> : vecs <= 2048 ? launch_combine<4> : launch_combine<4, true>;
   if (launch(row_args(plan), plan->n_tokens, vecs, y_bf16, weights, base_bf16, ld_base, out_bf16, ld_out,
              static_cast<cudaStream_t>(stream)) != cudaSuccess)
