@@ -287,10 +287,11 @@ struct RowArgs {
   int* status;
 };
 constexpr int kBatch = 4;  // choices whose loads are in flight together
-// The rows of choices j0 .. j0 + 3 of token t, or -1.  A plan that names rows outside the buffers has none there.
-__device__ __forceinline__ void rows_of(const RowArgs& a, int64_t t, int j0, int r[kBatch]) {
+// The rows of choices j0 .. j0 + B - 1 of token t, or -1.  A plan that names rows outside the buffers has none there.
+template <int B>
+__device__ __forceinline__ void rows_of(const RowArgs& a, int64_t t, int j0, int (&r)[B]) {
 #pragma unroll
-  for (int i = 0; i < kBatch; ++i) {
+  for (int i = 0; i < B; ++i) {
     r[i] = j0 + i < a.top_k ? __ldg(a.row_of + t * a.top_k + j0 + i) : -1;
     if (r[i] >= a.max_rows) r[i] = -1;
   }
@@ -446,8 +447,10 @@ __global__ void __launch_bounds__(kWalkThreads)
 }
 
 // The sum is in 32 bits, in the order of the choices, rounded once.  The loads of a batch of choices are all in flight
-// (without the batch 89 us for 8192 tokens of 5120 from 4 rows each; with it 74, the measured copy rate).
-template <int U, bool kLoop>
+// (without the batch 89 us for 8192 tokens of 5120 from 4 rows each; with it 74, the measured copy rate); a
+// batch of two where there are no more choices, for its fewer registers (16384 tokens of 2048 from one row each 30.0 -> 26.7,
+// from two 35.7 -> 32.9; of 5120 from two 90.9 -> 86.9).
+template <int U, bool kLoop, int B>
 __global__ void __launch_bounds__(512)
     moe_combine_kernel(const RowArgs a, const Split w, const uint16_t* __restrict__ y,
                        const float* __restrict__ weights, const uint16_t* base, int64_t ld_base, uint16_t* out,
@@ -466,13 +469,13 @@ __global__ void __launch_bounds__(512)
         if (v < vecs) unpack_bf16x8(reinterpret_cast<const uint4*>(base + t * ld_base)[v], acc[u]);  // out may be base
       }
     }
-    for (int j0 = 0; j0 < a.top_k; j0 += kBatch) {
-      int r[kBatch];
-      float c[kBatch];
-      uint4 in[kBatch][U];
+    for (int j0 = 0; j0 < a.top_k; j0 += B) {
+      int r[B];
+      float c[B];
+      uint4 in[B][U];
       rows_of(a, t, j0, r);
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
+      for (int j = 0; j < B; ++j) {
         c[j] = r[j] < 0 ? 0.0f : weights ? __ldg(weights + t * a.top_k + j0 + j) : 1.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -482,7 +485,7 @@ __global__ void __launch_bounds__(512)
         }
       }
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
+      for (int j = 0; j < B; ++j) {
         if (r[j] < 0) continue;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -502,11 +505,11 @@ __global__ void __launch_bounds__(512)
   } while (kLoop && v0 < vecs);
 }
 
-template <int U, bool kLoop = false>
+template <int U, bool kLoop = false, int B = kBatch>
 cudaError_t launch_combine(const RowArgs& a, int64_t tokens, uint32_t vecs, const void* y, const float* weights,
                            const void* base, int64_t ld_base, void* out, int64_t ld_out, cudaStream_t s) {
   const Split w = make_split<U>(tokens, vecs);
-  return launch_pdl(moe_combine_kernel<U, kLoop>, w.grid(), w.block(), 0, s, a, w, static_cast<const uint16_t*>(y),
+  return launch_pdl(moe_combine_kernel<U, kLoop, B>, w.grid(), w.block(), 0, s, a, w, static_cast<const uint16_t*>(y),
                     weights, static_cast<const uint16_t*>(base), ld_base, static_cast<uint16_t*>(out), ld_out);
 }
 
@@ -722,7 +725,8 @@ NVFP4_API nvfp4_status moe_combine(const moe_plan* plan, const void* y_bf16, int
     return NVFP4_ERR_ALIGN;
   const uint32_t vecs = static_cast<uint32_t>(cols / 8);
   const auto launch = vecs <= 512 && plan->n_tokens <= sm_count() ? launch_combine<1>
-                      : vecs <= 1024 ? launch_combine<2> : vecs <= 2048 ? launch_combine<4> : launch_combine<4, true>;
+                      : vecs <= 1024 ? (plan->top_k <= 2 ? launch_combine<2, false, 2> : launch_combine<2>)
+                      : vecs <= 2048 ? launch_combine<4> : launch_combine<4, true>;
   if (launch(row_args(plan), plan->n_tokens, vecs, y_bf16, weights, base_bf16, ld_base, out_bf16, ld_out,
              static_cast<cudaStream_t>(stream)) != cudaSuccess)
     return NVFP4_ERR_CUDA;

@@ -189,6 +189,26 @@ def test_combine(N, tokens, cols, weighted, based):
     ok(N)
 
 
+@pytest.mark.parametrize("cols", [64, 2048, 4104, 16384])
+@pytest.mark.parametrize("tokens", [1, 150, 701])
+@pytest.mark.parametrize("top_k", [1, 2, 4, 9, 32])
+def test_combine_of_any_number_of_choices(N, top_k, tokens, cols):
+    """A token's sum has top_k fused steps: at most that many roundings of at most the sum of magnitudes."""
+    plan, _ = some_plan(N, tokens, top_k=top_k, experts=33)
+    y, w = M.rand_bf16((plan.max_rows, cols), 8), torch.randn(tokens, top_k, device="cuda")
+    out = torch.full((tokens, cols), 9.0, dtype=BF, device="cuda")
+    N.moe_combine(plan, y, out, weights=w)
+    want = torch.zeros(tokens, cols, dtype=torch.float64, device="cuda")
+    mag = want.clone()
+    for j in range(top_k):
+        has = (plan.row_of[:, j] >= 0).nonzero()[:, 0]
+        term = y[plan.row_of[has, j].long()].double() * w[has, j, None].double()
+        want[has] += term
+        mag[has] += term.abs()
+    near(out, want.cpu().numpy(), top_k * 2.0 ** -24 * mag.cpu().numpy())
+    ok(N)
+
+
 @pytest.mark.parametrize("cols", COLS)
 @pytest.mark.parametrize("tokens,top_k", [(1, 3), (2, 1), (33, 8), (400, 5), (3, 32), (900, 2), (701, 5)])
 def test_combine_backward(N, tokens, top_k, cols):
