@@ -289,8 +289,8 @@ __device__ __forceinline__ Unit find_unit(int u, const int* ends, const int2* ro
 // --------------------------------------------------------------- epilogue ---
 // lo, hi: the fragments of a warp's weight rows 0..15 and 16..31, 32 tokens from token0.
 
-__device__ __forceinline__ void store_rows(const GroupedArgs& a, const void* map_out, const Unit& t, const uint32_t* lo, const uint32_t* hi,
-                                           int token0, int n0, float scale, uint32_t buf, int lane) {
+__device__ __forceinline__ void store_rows(const GroupedArgs& a, const void* map_out, const Unit& t, const uint32_t* lo,
+                                           const uint32_t* hi, int token0, int n0, float scale, uint32_t buf, int lane) {
   auto f = [&](uint32_t v) { return __uint_as_float(v) * scale; };
   // Rows of 64 bytes in 16-byte chunks, chunk c of token t at c ^ (t / 2) % 4: no bank twice, written or read.
   // That is also the 64-byte swizzle of a box of 32 x 32, which goes out by itself while the warp turns to the next; rows

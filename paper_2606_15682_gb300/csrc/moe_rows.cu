@@ -9,7 +9,7 @@
 // HBM-bound from some hundred tokens on.  Of the measured copy rate: 8192 tokens of
 // 5120 to 4 bf16 rows each 63 us (0.98), to NVFP4 rows 33.5 (0.79: 4-byte scale words
 // apart), back with weights and a base 74 (1.0); the gradients of 4099 x 2048 with 8
-// rows each 41.4 (0.88) and 22.5 (0.88).  One token: 1.7 to 2.4 us, a launch's latency.
+// rows each 41.8 (0.87) and 22.0 (0.90).  One token: 1.7 to 2.4 us, a launch's latency.
 #include <cfloat>
 
 #include "moe_plan.cuh"
@@ -704,8 +704,9 @@ NVFP4_API nvfp4_status moe_dispatch_mxfp4(const moe_plan* plan, const void* x_bf
   if (!x_bf16 || !codes || !scales) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(x_bf16, 16) || !aligned(codes, 16) || !aligned(scales, 4)) return NVFP4_ERR_ALIGN;
   const WalkLaunch l = make_walk(plan->n_tokens, static_cast<uint32_t>(cols / 32));
-  if (launch_pdl(rotate ? moe_dispatch_mxfp4_kernel<true> : moe_dispatch_mxfp4_kernel<false>, l.grid, l.block, 0, static_cast<cudaStream_t>(stream), row_args(plan), l.w,
-                 static_cast<const uint16_t*>(x_bf16), ld_x, reinterpret_cast<uint4*>(codes), scales) != cudaSuccess)
+  if (launch_pdl(rotate ? moe_dispatch_mxfp4_kernel<true> : moe_dispatch_mxfp4_kernel<false>, l.grid, l.block, 0,
+                 static_cast<cudaStream_t>(stream), row_args(plan), l.w, static_cast<const uint16_t*>(x_bf16), ld_x,
+                 reinterpret_cast<uint4*>(codes), scales) != cudaSuccess)
     return NVFP4_ERR_CUDA;
   count_launches(1);
   return launch_status();
