@@ -692,7 +692,9 @@ nvfp4_status residual_norm_nvfp4(const void* x_bf16, int64_t ld_x, const void* y
  * Written by moe_sort, read by the other calls; the struct is read before a call
  * returns.  1 <= num_experts <= 1024, 1 <= top_k <= 32, moe_max_rows < 2^31
  * (SHAPE); null arrays (row_of may be null with n_tokens == 0) -> INVALID_ARG;
- * 4-B aligned (ALIGN).  A plan that names rows outside the buffers is cut to them.
+ * 4-B aligned (ALIGN).  A plan that names rows outside the buffers is cut to them, and
+ * one that names more rows of an expert than there are choices to those (a plan left
+ * from a larger step).
  */
 typedef struct {
   int32_t* row_start;

@@ -100,7 +100,7 @@ struct GroupedArgs {
   uint8_t* q_codes;
   uint8_t* q_scales;
   int64_t ldo;
-  int experts, max_rows, N, K, g_a_step, g_out_step;
+  int experts, max_rows, choices, N, K, g_a_step, g_out_step;
   int w_tiles;        // 256-row tiles of an expert's weight
   int w_scale_tiles;  // 128-row tiles of its scales
   int max_units;      // what a plan can have: one of any numbers is cut to it
@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(F::kThreads, F::kSmall ? 2 : 1)
       const int e = F::kPer * threadIdx.x + i;
       n[i] = 0;
       if (e < a.experts) {
-        const ExpertRows r = expert_rows(a.row_start, a.rows, e, a.max_rows);
+        const ExpertRows r = expert_rows(a.row_start, a.rows, e, a.max_rows, a.choices);
         expert_rows_s[e] = make_int2(r.first, r.n);
         n[i] = static_cast<int64_t>((r.n + F::kTokens - 1) / F::kTokens) * a.w_tiles;
       }
@@ -926,6 +926,7 @@ nvfp4_status launch_form(const moe_plan* plan, GroupedArgs& a, cudaStream_t s) {
   a.w_tiles = (a.N + kWRows - 1) / kWRows;
   a.w_scale_tiles = (a.N + 127) / 128;
   const int64_t choices = plan->n_tokens * plan->top_k, used = choices < a.experts ? choices : a.experts;
+  a.choices = static_cast<int>(choices);  // below moe_rows_bound
   const int64_t units = (choices + (kTokens - 1) * used) / kTokens * a.w_tiles;  // at most
   if (units >= (1ll << 30)) return NVFP4_ERR_SHAPE;
   a.max_units = static_cast<int>(units);
@@ -947,7 +948,7 @@ nvfp4_status launch_form(const moe_plan* plan, GroupedArgs& a, cudaStream_t s) {
   if (!opted_in<F>()) return NVFP4_ERR_CUDA;
   CUtensorMap w, ws, x16, mid_x = {}, x128 = {}, xs, xs2 = {}, out = {};
   const int64_t R = a.max_rows, K = a.K;
-  // No tile has more tokens than there are choices: few need no map of the larger boxes.
+  // No tile has more tokens than there are choices (expert_rows cuts to them): few need no map of the larger boxes.
   const bool mid = choices > 32, wide = !F::kSmall && choices > 128;
   if (!codes_map(&w, a.w_codes, static_cast<int64_t>(a.experts) * a.N, K, 128) ||
       !scales_map(&ws, a.w_scales, static_cast<int64_t>(a.experts) * a.w_scale_tiles, K, false) ||

@@ -33,16 +33,18 @@ inline nvfp4_status check_moe_plan(const moe_plan* p) {
   return NVFP4_OK;
 }
 
-// An expert's rows in the sorted buffers, cut to what the buffers hold whatever the plan says.
+// An expert's rows in the sorted buffers, cut to what the buffers hold and to the tokens' choices whatever the plan says:
+// the host goes by these two alone where it decides what a launch can need.
 struct ExpertRows {
   int first, n;
 };
-__device__ __forceinline__ ExpertRows expert_rows(const int32_t* row_start, const int32_t* rows, int e, int max_rows) {
+__device__ __forceinline__ ExpertRows expert_rows(const int32_t* row_start, const int32_t* rows, int e, int max_rows,
+                                                  int choices) {
   ExpertRows r;
   r.first = __ldg(row_start + e);
   r.n = __ldg(rows + e);
   if (r.first < 0 || r.first > max_rows || (r.first & (kMoeRowTile - 1))) r.first = r.n = 0;
-  r.n = max(0, min(r.n, max_rows - r.first));
+  r.n = max(0, min(min(r.n, choices), max_rows - r.first));
   return r;
 }
 
