@@ -10,6 +10,7 @@
 // 5120 to 4 bf16 rows each 63 us (0.98), to NVFP4 rows 33.5 (0.79: 4-byte scale words
 // apart), back with weights and a base 74 (1.0); the gradients of 4099 x 2048 with 8
 // rows each 41.8 (0.87) and 22.0 (0.90).  One token: 1.7 to 2.4 us, a launch's latency.
+#include <atomic>
 #include <cfloat>
 
 #include "moe_plan.cuh"
@@ -231,6 +232,25 @@ __global__ void __launch_bounds__(kSortThreads) moe_place_kernel(const SortArgs 
     if (begin + 32 * i < chunk_end) a.row_of[begin + 32 * i] = row;
   }
   if constexpr (kForm == kCluster) cluster_sync_all();  // no CTA leaves while another may read its counts
+}
+
+size_t place_smem(int experts) { return static_cast<size_t>(kSortWarps + 2) * experts * sizeof(uint32_t); }
+
+// The shared-memory opt-in of a form's kernel, once for each device and for as many experts as there can be: the limit is
+// the kernel's, whose other callers, in other threads, may need more than this one.
+bool place_opted_in(void (*kernel)(SortArgs), SortForm form) {
+  static std::atomic<uint64_t> done[3];  // a bit a device
+  int d = 0;
+  if (cudaGetDevice(&d) != cudaSuccess) return false;
+  const uint64_t bit = d < 64 ? 1ull << d : 0;
+  if (done[form].load(std::memory_order_acquire) & bit) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           static_cast<int>(place_smem(kMoeMaxExperts))) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  done[form].fetch_or(bit, std::memory_order_release);
+  return true;
 }
 
 // ------------------------------------------------------- walks over tokens ---
@@ -626,15 +646,11 @@ NVFP4_API nvfp4_status moe_sort(const moe_plan* plan, const int32_t* expert_idx,
   const SortShape s = sort_shape(a.pairs);
   a.chunk = s.chunk;
   const cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  const size_t smem = static_cast<size_t>(kSortWarps + 2) * a.experts * sizeof(uint32_t);
+  const size_t smem = place_smem(a.experts);
   const auto kernel = s.form == kAlone ? moe_place_kernel<kAlone>
                       : s.form == kCluster ? moe_place_kernel<kCluster> : moe_place_kernel<kChunks>;
   // With the static part beside it, 48 KB are passed earlier.
-  if (smem > 32 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               static_cast<int>(smem)) != cudaSuccess) {
-    cudaGetLastError();
-    return NVFP4_ERR_CUDA;
-  }
+  if (smem > 32 * 1024 && !place_opted_in(kernel, s.form)) return NVFP4_ERR_CUDA;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
