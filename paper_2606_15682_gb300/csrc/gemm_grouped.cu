@@ -978,24 +978,25 @@ nvfp4_status launch_form(const moe_plan* plan, GroupedArgs& a, cudaStream_t s) {
 //                    1024 x 2048, 16.3 / 16.5; (47) 64, 1280 x 4096, 35.3 / 33.4; (96) 40, 1280 x 1536, 15.2 / 14.2
 template <int kMode>
 nvfp4_status launch_grouped(const moe_plan* plan, GroupedArgs& a, cudaStream_t s) {
-  if (plan->n_tokens == 0) return NVFP4_OK;
   const bool small = plan->n_tokens * plan->top_k <= (kMode == 0 ? 32 : 64) * static_cast<int64_t>(plan->num_experts);
   return small ? launch_form<Form<kMode, true>>(plan, a, s) : launch_form<Form<kMode, false>>(plan, a, s);
 }
 
 constexpr int64_t kMaxSide = 1ll << 20;  // N and K
 
-// The operands' checks that all four calls share; g: whether there are tensor scales.
+// The operands' checks that all four calls share; g: whether there are tensor scales.  Without tokens the sorted rows are
+// empty buffers, whose addresses may be null.
 nvfp4_status check_operands(const moe_plan* plan, const GroupedArgs& a, int64_t N, int64_t K, bool g, int64_t n_step) {
   const nvfp4_status st = check_moe_plan(plan);
   if (st != NVFP4_OK) return st;
-  if (!a.a_codes || !a.a_scales || !a.w_codes || !a.w_scales || (g && (!a.g_a || !a.g_w))) return NVFP4_ERR_INVALID_ARG;
   if ((a.g_a_step != 0 && a.g_a_step != 1) || (a.g_out_step != 0 && a.g_out_step != 1)) return NVFP4_ERR_INVALID_ARG;
   if (N <= 0 || K <= 0 || N > kMaxSide || K > kMaxSide || K % 256 || N % n_step) return NVFP4_ERR_SHAPE;
   // Box coordinates, those of a last tile that reaches past the last expert too.
   if ((plan->num_experts * ((N + 127) / 128) + 2) * (K / 32) >= (1ll << 31) || plan->num_experts * N + 256 >= (1ll << 31) ||
       moe_rows_bound(plan->n_tokens, plan->top_k, plan->num_experts) / 128 * (K / 32) >= (1ll << 31))
     return NVFP4_ERR_SHAPE;
+  if (plan->n_tokens == 0) return NVFP4_OK;
+  if (!a.a_codes || !a.a_scales || !a.w_codes || !a.w_scales || (g && (!a.g_a || !a.g_w))) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(a.a_codes, 16) || !aligned(a.a_scales, 16) || !aligned(a.w_codes, 16) || !aligned(a.w_scales, 16) ||
       !aligned(a.g_a, 4) || !aligned(a.g_w, 4))
     return NVFP4_ERR_ALIGN;
@@ -1005,8 +1006,9 @@ nvfp4_status check_operands(const moe_plan* plan, const GroupedArgs& a, int64_t 
 nvfp4_status linear(const moe_plan* plan, GroupedArgs a, int64_t N, int64_t K, void* out, int64_t ldo, void* stream) {
   const nvfp4_status st = check_operands(plan, a, N, K, !a.mx, 16);
   if (st != NVFP4_OK) return st;
-  if (!out) return NVFP4_ERR_INVALID_ARG;
   if (ldo < N || ldo % 8) return NVFP4_ERR_SHAPE;
+  if (plan->n_tokens == 0) return NVFP4_OK;
+  if (!out) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(out, 16)) return NVFP4_ERR_ALIGN;
   a.out = static_cast<uint16_t*>(out);
   a.ldo = ldo;
@@ -1019,6 +1021,7 @@ nvfp4_status swiglu(const moe_plan* plan, GroupedArgs a, int64_t I, int64_t K, u
                     void* stream) {
   const nvfp4_status st = check_operands(plan, a, 2 * I, K, !a.mx, 256);
   if (st != NVFP4_OK) return st;
+  if (plan->n_tokens == 0) return NVFP4_OK;
   if (!codes || !scales || (!a.mx && !a.g_out)) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(codes, 16) || !aligned(scales, 4) || !aligned(a.g_out, 4)) return NVFP4_ERR_ALIGN;
   a.q_codes = codes;
