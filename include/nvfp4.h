@@ -881,18 +881,23 @@ nvfp4_status nvfp4_get_device_status(int32_t* status_host, void* stream);
  *     extend_attention_nvfp4, if that comes first, CTA 0's first K stage waits
  *     for an arrival that never comes, with the same end in each of its kernels.
  *   NVFP4_FAULT_GEMM_SKIP_STAGE: in the next GEMM launch (nvfp4_linear,
- *     mxfp4_linear, nvfp4_linear_dynamic and the fused SwiGLU calls, whichever
+ *     mxfp4_linear, nvfp4_linear_dynamic, the fused SwiGLU calls and the grouped
+ *     linears, whichever
  *     kernel serves the shape), the first CTA, or both CTAs of the first CTA
  *     pair, leave their first ring stage neither armed nor loaded; the MMA
  *     issuer's and the scale copiers' bounded waits run out after ~2 s, every
  *     role of the CTA or pair stops, the MMAs issued so far drain and TMEM is
  *     freed.  The call reports NVFP4_ERR_TIMEOUT, its output is undefined, and
  *     the device stays usable.
+ *   NVFP4_FAULT_GROUPED_REVERSED: in the next grouped linear launch the thread-block
+ *     clusters have their tiles in reverse, as if the last cluster started first.  No
+ *     error: the output is the same.
  *   NVFP4_FAULT_NONE disarms.  Other values -> INVALID_ARG.
  */
 #define NVFP4_FAULT_NONE 0
 #define NVFP4_FAULT_ATTN_SKIP_STAGE 1
 #define NVFP4_FAULT_GEMM_SKIP_STAGE 2
+#define NVFP4_FAULT_GROUPED_REVERSED 3
 nvfp4_status nvfp4_debug_inject_fault(int what);
 
 /* Static, human-readable name of a status. */

@@ -107,6 +107,7 @@ struct GroupedArgs {
   bool mx;
   bool rotate;
   int fault_skip_stage;  // test-only: pair 0 leaves its first stage neither armed nor loaded
+  int reversed;          // test-only: the clusters' units from the last cluster on, as if the clusters started so
   int* status;
 };
 
@@ -437,14 +438,16 @@ __global__ void __launch_bounds__(F::kThreads, F::kSmall ? 2 : 1)
   Unit* queue = reinterpret_cast<Unit*>((reinterpret_cast<uintptr_t>(answer_in + 1) + 15) & ~uintptr_t(15));
   uint8_t* answer = reinterpret_cast<uint8_t*>(queue + kQueue);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(answer + 16);
-  __shared__ volatile int abort_flag;
+  __shared__ volatile int abort_flag, late_unit;
   __shared__ int64_t warp_sum[F::kThreads / 32];
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int kblocks = a.K / kDepth;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0;
-  const int first_unit = blockIdx.x / 2;
+  const int clusters = gridDim.x / 2;
+  const auto unit_of = [&](int cluster) { return a.reversed ? clusters - 1 - cluster : cluster; };
+  int first_unit = unit_of(blockIdx.x / 2);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -519,6 +522,46 @@ __global__ void __launch_bounds__(F::kThreads, F::kSmall ? 2 : 1)
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
     return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, &abort_flag)) != 0;
   };
+  // The peer's warp 2: takes a cluster; the unit that it begins with, -1 where none is left (asking again is not allowed).
+  // False: the wait ran out.
+  uint32_t answers = 0;  // the phase of answer_in
+  const auto take = [&](int64_t* u) {
+    if (elect_one()) {
+      mbar_arrive_expect_tx(answer_in, 16);
+      take_cluster(answer, answer_in);
+    }
+    __syncwarp();
+    if (!wait(answer_in, answers)) return false;
+    answers ^= 1u;
+    const int taken = __shfl_sync(0xffffffffu, taken_cluster(answer), 0);
+    fence_proxy_async_smem();  // read here, then written by the next answer
+    *u = taken < 0 ? -1 : unit_of(taken);
+    return true;
+  };
+  // Clusters start in any order: a pair whose own unit is not there takes others until one has a unit, and begins with that.
+  // Here, before the roles: one token's gate_up and down 6.84 and 5.27 us, for 7.01 and 5.30 with a look at each unit in the
+  // roles.  Without it, which leaves the others to start and end by themselves, 6.84 and 5.14, but 100 rows of 32768 choices
+  // 27.9 and 38.6 for 10.8 and 16.6.
+  if (first_unit >= units) {
+    if (!leader && warp == 2) {
+      int64_t u;
+      do
+        if (!take(&u)) {
+          fail();
+          u = -1;
+        }
+      while (u >= units);
+      if (lane == 0)
+#pragma unroll
+        for (uint32_t r = 0; r < 2; ++r)
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(pair_address(const_cast<int*>(&late_unit), r)),
+                       "r"(static_cast<int>(u))
+                       : "memory");
+      __syncwarp();
+    }
+    cluster_sync_all();
+    if (late_unit >= 0) first_unit = late_unit;
+  }
   // The next unit of the pair, to each of its warps by itself (n: its count of them).  False: there is none, or, with
   // *ok false, the wait ran out.
   auto next_unit = [&](Unit* t, int* n, bool* ok) {
@@ -680,16 +723,8 @@ __global__ void __launch_bounds__(F::kThreads, F::kSmall ? 2 : 1)
     // never wait for one, some 8 k-blocks: with more, the first pairs take them all (224 units on 76 pairs: 2 to 4 each).
     const int ahead = max(1, min(kQueue - 1, 8 / kblocks));
     const bool issuer = elect_one();
-    const int clusters = gridDim.x / 2;
     int n = 0;
     bool ok = true;
-    auto ask = [&]() {
-      if (issuer) {
-        mbar_arrive_expect_tx(answer_in, 16);
-        take_cluster(answer, answer_in);
-      }
-      __syncwarp();
-    };
     auto hand_out = [&](const Unit& t) {
       const int slot = n % kQueue;
       ok = ok && wait(&unit_empty[slot], ((n / kQueue) & 1) ^ 1u);
@@ -703,27 +738,12 @@ __global__ void __launch_bounds__(F::kThreads, F::kSmall ? 2 : 1)
       const int old = ++n - ahead;
       if (old >= 0) ok = ok && wait(&unit_begun[old % kQueue], (old / kQueue) & 1);
     };
-    uint32_t phase = 0;
-    for (int64_t u = static_cast<int64_t>(first_unit) + clusters;;) {
+    for (int64_t u = static_cast<int64_t>(first_unit) + clusters; first_unit < units;) {
       for (; ok && u < units; u += clusters) hand_out(find_unit<F::kTokens>(static_cast<int>(u), ends, expert_rows_s, lane));
-      if (!ok) {
-        fail();
-        break;
-      }
-      ask();
-      ok = wait(answer_in, phase);
-      phase ^= 1u;
-      if (!ok) {
-        fail();
-        break;
-      }
-      u = __shfl_sync(0xffffffffu, taken_cluster(answer), 0);
-      fence_proxy_async_smem();  // read here, then written by the next answer
-      if (u < 0) {  // none is left; asking again is not allowed
-        if (first_unit < units) hand_out(Unit{});
-        if (!ok) fail();
-        break;
-      }
+      ok = ok && take(&u);
+      if (ok && u < 0) hand_out(Unit{});
+      if (!ok) fail();
+      if (!ok || u < 0) break;
     }
   } else if (warp >= kEpi0) {
     // ----------------------------------------------------------- epilogue ---
@@ -959,6 +979,7 @@ nvfp4_status launch_form(const moe_plan* plan, GroupedArgs& a, cudaStream_t s) {
     return NVFP4_ERR_CUDA;
   a.status = status_word_dev();
   a.fault_skip_stage = take_fault(NVFP4_FAULT_GEMM_SKIP_STAGE) ? 1 : 0;
+  a.reversed = take_fault(NVFP4_FAULT_GROUPED_REVERSED) ? 1 : 0;
   cfg.gridDim = dim3(static_cast<uint32_t>(2 * clusters), 1, 1);
   cfg.stream = s;
   cfg.numAttrs = 2;
