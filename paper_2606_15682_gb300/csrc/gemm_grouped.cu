@@ -168,8 +168,9 @@ __device__ __forceinline__ void load_box3(void* dst, const void* map, uint64_t* 
       "l"(reinterpret_cast<uint64_t>(map)), "r"(leader_address(bar)), "r"(0), "r"(y), "r"(z)
       : "memory");
 }
-// Arrives without release: hands back an accumulator whose TMEM loads are complete and fenced, or an answer that was
-// read and used; no memory that the warp wrote is read after it.
+// Arrives without release: hands back an accumulator whose TMEM loads are complete and fenced, or a place of the queue
+// whose 16 bytes one load has brought into registers that the warp has used; no memory that the warp wrote is read after it.
+// (With release, which waits for the epilogue's stores, down of 8192 tokens takes 143 us for 106.)
 __device__ __forceinline__ void arrive_relaxed(uint32_t pair_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(pair_addr) : "memory");
 }
@@ -270,7 +271,15 @@ struct Unit {
   int row0, tokens;  // first row, rows of the tile; tokens 0: there is no unit
   __device__ __forceinline__ int n() const { return (tokens + 31) & ~31; }  // the MMA's N
 };
-static_assert(sizeof(Unit) == 16, "one store of the queue");
+static_assert(sizeof(Unit) == 16, "one store of the queue, and one load");
+__device__ __forceinline__ Unit load_unit(const Unit* slot) {
+  Unit t;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(t.expert), "=r"(t.w_tile), "=r"(t.row0), "=r"(t.tokens)
+               : "r"(smem_u32(slot))
+               : "memory");
+  return t;
+}
 // Unit u, by a converged warp.  ends: [1024] units of the experts up to each one, the total behind the last one.
 template <int kTokens>
 __device__ __forceinline__ Unit find_unit(int u, const int* ends, const int2* rows, int lane) {
@@ -522,6 +531,10 @@ __global__ void __launch_bounds__(F::kThreads, F::kSmall ? 2 : 1)
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
     return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, &abort_flag)) != 0;
   };
+  // The same for a barrier that the other CTA of the pair arrives on.
+  const auto wait_pair = [&](uint64_t* bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, mbar_wait_bounded_cluster(bar, parity, &abort_flag)) != 0;
+  };
   // The peer's warp 2: takes a cluster; the unit that it begins with, -1 where none is left (asking again is not allowed).
   // False: the wait ran out.
   uint32_t answers = 0;  // the phase of answer_in
@@ -566,14 +579,14 @@ __global__ void __launch_bounds__(F::kThreads, F::kSmall ? 2 : 1)
   // *ok false, the wait ran out.
   auto next_unit = [&](Unit* t, int* n, bool* ok) {
     const int slot = *n % kQueue;
-    *ok = wait(&unit_full[slot], (*n / kQueue) & 1);
+    *ok = wait_pair(&unit_full[slot], (*n / kQueue) & 1);
     if (!*ok) {
       fail();
       return false;
     }
     ++*n;
-    *t = queue[slot];
-    const bool some = __shfl_sync(0xffffffffu, t->tokens, 0) != 0;  // all lanes have read
+    *t = load_unit(&queue[slot]);
+    const bool some = __all_sync(0xffffffffu, t->tokens != 0);  // all lanes have their load's answer
     if (lane == 0) {
       arrive_relaxed(pair_address(&unit_empty[slot], 1));
       if (leader && warp == 0) arrive_relaxed(pair_address(&unit_begun[slot], 1));
@@ -651,7 +664,7 @@ __global__ void __launch_bounds__(F::kThreads, F::kSmall ? 2 : 1)
       const uint32_t idesc = kIdesc | static_cast<uint32_t>(t.n() >> 3) << 17 | (a.mx ? kUE8M0 : 0u);
       // A scale tile's columns are of 32 rows each: tiles of 64 tokens begin with its first or its third.
       const uint32_t x_col = F::kSmall && (t.row0 & 64) ? 2 : 0;
-      if (!wait(acc_empty, (local & 1) ^ 1u)) {
+      if (!wait_pair(acc_empty, (local & 1) ^ 1u)) {
         fail();
         return false;
       }
@@ -727,7 +740,7 @@ __global__ void __launch_bounds__(F::kThreads, F::kSmall ? 2 : 1)
     bool ok = true;
     auto hand_out = [&](const Unit& t) {
       const int slot = n % kQueue;
-      ok = ok && wait(&unit_empty[slot], ((n / kQueue) & 1) ^ 1u);
+      ok = ok && wait_pair(&unit_empty[slot], ((n / kQueue) & 1) ^ 1u);
       if (ok && issuer)
 #pragma unroll
         for (uint32_t r = 0; r < 2; ++r) {
@@ -736,7 +749,7 @@ __global__ void __launch_bounds__(F::kThreads, F::kSmall ? 2 : 1)
         }
       __syncwarp();
       const int old = ++n - ahead;
-      if (old >= 0) ok = ok && wait(&unit_begun[old % kQueue], (old / kQueue) & 1);
+      if (old >= 0) ok = ok && wait_pair(&unit_begun[old % kQueue], (old / kQueue) & 1);
     };
     for (int64_t u = static_cast<int64_t>(first_unit) + clusters; first_unit < units;) {
       for (; ok && u < units; u += clusters) hand_out(find_unit<F::kTokens>(static_cast<int>(u), ends, expert_rows_s, lane));
