@@ -101,6 +101,11 @@ class Layer:
         self.g = [torch.tensor([g], dtype=torch.float32, device=dev) for g in act_scales]
 
 
+def _experts(layer):
+    """(experts, top_k) of a layer; of one with an MLP, which need not know of experts, (0, 0)."""
+    return getattr(layer, "experts", 0), getattr(layer, "top_k", 0)
+
+
 class Batch:
     """n_new tokens of each of `batch` sequences on their way through the layers, and the buffers they need.
 
@@ -128,7 +133,7 @@ class Batch:
         self.qkv, self.q, self.attn = bf16(n, (hq + 2 * hkv) * D), bf16(n, hq, D), bf16(n, hq, D)
         self.r, self.o, self.y, self.h = bf16(n, H), bf16(n, H), bf16(n, H), bf16(n, H)
         self.a_qkv, self.a_o, self.a_gu = fp4(n, H), fp4(n, hq * D), fp4(n, H)
-        self.experts = getattr(layer, "experts", 0), getattr(layer, "top_k", 0)
+        self.experts = _experts(layer)
         if self.experts[0]:
             self.plan = N.MoEPlan(n, layer.top_k, layer.experts, device=dev)
             rows = self.plan.max_rows
@@ -156,7 +161,7 @@ class Batch:
         """
         if logit_cap and any(w.k_shift is not None for w in layers):
             raise ValueError("logit_cap needs the keys themselves: a layer with k_shift caches K - m")
-        if any((w.experts, w.top_k) != self.experts for w in layers):
+        if any(_experts(w) != self.experts for w in layers):
             raise ValueError("a Batch runs layers with the experts and top_k of the one that it was made for")
         self.begin()
         rope_pos = self.pos[:, None] if rope_pos is None else rope_pos
@@ -175,10 +180,10 @@ class Batch:
                                      logit_cap=logit_cap, window=window)
             N.nvfp4_quantize(self.attn.view(n, hq * D), w.g[1], *self.a_o, N.SCALES_MMA)
             N.nvfp4_linear(*self.a_o, w.g[1], *w.o, self.o, n, H, hq * D)
-            N.residual_norm_nvfp4(r, self.o, self.r, self.h2 if w.experts else None, w.norm2, g_out=w.g[2],
+            N.residual_norm_nvfp4(r, self.o, self.r, self.h2 if self.experts[0] else None, w.norm2, g_out=w.g[2],
                                   codes=self.a_gu[0], scales=self.a_gu[1])
             r = self.r
-            if w.experts:
+            if self.experts[0]:
                 self.run_experts(w)
             else:
                 N.nvfp4_linear_swiglu_quantize(*self.a_gu, w.g[2], *w.gate_up, n, I, H, w.g[3], *self.a_down)
