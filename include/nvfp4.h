@@ -677,8 +677,9 @@ nvfp4_status residual_norm_nvfp4(const void* x_bf16, int64_t ld_x, const void* y
  *   nvfp4_linear_grouped                  down of each expert
  *   moe_combine                           the rows back to their tokens, weighted and summed
  * (the mxfp4_ forms likewise; moe_dispatch for experts in bf16).  Gradients:
- * moe_combine_backward; moe_combine without weights (of moe_dispatch);
- * moe_route_backward.  A gradient through experts in bf16 needs nothing else.
+ * moe_combine_backward; moe_combine without weights (of moe_dispatch; of one with
+ * weights as said there); moe_route_backward.  A gradient through experts in bf16
+ * needs nothing else.
  *
  * The plan.  A token's choice j of an expert is a row of buffers of
  * moe_max_rows(n_tokens, top_k, num_experts) rows.  Expert e has the rows
@@ -767,6 +768,9 @@ nvfp4_status moe_sort(const moe_plan* plan, const int32_t* expert_idx, void* wor
  * rounded once where weights (device float [n_tokens, top_k]) are given.
  *   x_bf16    : [n_tokens, cols] bf16, rows ld_x apart.
  *   rows_bf16 : [moe_max_rows, cols] bf16, dense.
+ * Gradients from d_rows [moe_max_rows, cols]: of x, moe_combine of d_rows with the same
+ * weights, or without any; of weights, moe_combine_backward with x as its d_out, d_rows
+ * as its y and d_y NULL.
  * cols % 8 == 0, cols <= 65536, ld_x >= cols (SHAPE), ld_x % 8 == 0, 16-B aligned
  * (ALIGN).  n_tokens == 0 is a no-op, here and in all calls below.  No output may
  * overlap an input, here and in all calls below, but where one says so.
@@ -818,7 +822,9 @@ nvfp4_status moe_combine_backward(const moe_plan* plan, const void* d_out_bf16, 
 /*
  * The experts' linears: for every row r of expert e
  *   out[r, n] = bf16_rne( (g_a g_w) * sum_k a[r, k] * w_e[n, k] ),
- * as nvfp4_linear of each expert's rows with its weight; the sum in fp32.
+ * as nvfp4_linear of each expert's rows with its weight; the sum in fp32.  The rows are
+ * bf16, as all linears' outputs here: what moe_combine makes of them has their rounding
+ * and its own (of rows of equal size, sqrt(2) of the error of one).
  *   a_codes, a_scales : the sorted rows, [moe_max_rows, K] with MMA-layout scales.
  *   g_a      : device float [1] (g_a_step 0) or [num_experts] (g_a_step 1).
  *   w_codes  : [num_experts, N, K/2] bytes; w_scales: for each expert the MMA layout
@@ -845,7 +851,8 @@ nvfp4_status mxfp4_linear_grouped(const moe_plan* plan, const uint8_t* a_codes, 
  * The experts' gate_up with the down projection's input in the epilogue, as
  * nvfp4_linear_swiglu_quantize: h = SiLU(G) * U of the fp32 products, NVFP4-quantized
  * with the static scale of the expert.  SiLU(x) = x / (1 + e^-x) by the hardware's 2^x
- * and 1 / x: within (2 + |x| / 4) * 2^-21 of its size.
+ * and 1 / x: within (2 + |x| / 4) * 2^-21 of its size, and 0 below x = -87.3, where it is
+ * under 2^-119.
  *   w_codes, w_scales : [num_experts, 2I, K], gate and up rows in turn, 16 of each
  *                (nvfp4_interleave_gate_up of each expert's, then nvfp4_quantize).
  *   g_out      : device float [1] (g_out_step 0) or [num_experts] (1); <= 0 or not

@@ -541,8 +541,8 @@ def moe_dispatch_mxfp4(plan, x, codes, scales, rotate=False, stream=None):
 
 
 def moe_combine(plan, y, out, weights=None, base=None, stream=None):
-    """out [n_tokens, cols] = base + the sum of weights * y over each token's rows; without weights, also the gradient
-    of moe_dispatch's x from that of its rows, y."""
+    """out [n_tokens, cols] = base + the sum of weights * y over each token's rows; also the gradient of moe_dispatch's x
+    from that of its rows, y, with the weights that it had or without."""
     op, ld, cols = _matrix(out, plan.n_tokens, "out")
     bp, ld_base, base_cols = (None, 0, cols) if base is None else _matrix(base, plan.n_tokens, "base")
     if base_cols != cols:
@@ -554,7 +554,8 @@ def moe_combine(plan, y, out, weights=None, base=None, stream=None):
 
 
 def moe_combine_backward(plan, d_out, y, weights, d_y, d_weights, stream=None):
-    """moe_combine's gradients: d_y [max_rows, cols] and d_weights [n_tokens, top_k]; one of them may be None."""
+    """moe_combine's gradients: d_y [max_rows, cols] and d_weights [n_tokens, top_k]; one of them may be None.  With x in place
+    of d_out and the rows' gradient in place of y, d_weights is that of a weighted moe_dispatch."""
     gp, ld, cols = _matrix(d_out, plan.n_tokens, "d_out")
     n = plan.max_rows * cols
     _check("moe_combine_backward",
