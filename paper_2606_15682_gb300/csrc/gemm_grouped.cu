@@ -21,23 +21,24 @@
 //   warp 2      leader: block scales into TMEM; peer: the queue of units
 //   warp 3      leader: block scales
 //   warps 4-    epilogue: 32 weight rows x every second (of 8 warps) or fourth (of 16) 32 tokens each
-// Output rows are bf16, the type that the rows' other calls take: the one rounding of the fp32 sum; quantized outputs have the
-// recipe's own alone.  The epilogue reads 16 x 8 fragments of D (16x256b), in which a thread has two tokens
-// of two weight rows, and of gate and up at once: bf16 rows are turned into token-major
-// ones by a transposing stmatrix, quantized outputs need shuffles only.
+// Output rows are bf16, the type that the rows' other calls take: the one rounding of
+// the fp32 sum; quantized outputs have the recipe's own alone.  The epilogue reads 16 x
+// 8 fragments of D (16x256b), in which a thread has two tokens of two weight rows, and
+// of gate and up at once: bf16 rows are turned into token-major ones by a transposing
+// stmatrix, quantized outputs need shuffles only.
 //
-// What bounds it.  Few tokens: the weights from DRAM, at 6.3 of the measured 6.78 TB/s from one size to the other, and some
-// 4 us around that a launch takes to start, fill and drain (means of three batches: 64 tokens on 69 of 128 experts, 2048 x
-// 1536, 123 MB of codes and scales in 23.4 us; 500 on 56 of 64, 4096 x 2560, 330 MB in 56.5).  Many: the loads into the SMs.  8192 tokens x 4 on 64 experts, 5120 x 2048, read 1.93 GB
-// from L2, 16.4 TB/s without the MMAs in 118 us, with them in 132 to 136 (5.2 PFLOP/s); one expert of 8192 rows, 5120 x 13824,
-// 6.8 PFLOP/s in 171 us, as nvfp4_linear_swiglu_quantize.  The accumulator takes all TMEM that the scales leave, so a
-// unit's end (last MMAs, drain) costs 2000 cycles of 10240 at K = 5120, and at K = 1024 a unit's loads, MMAs and stores run
-// almost one after another: some 2000 cycles each of 5000, with L2 at 46 %, DRAM at 56 and the tensor pipe at 34 (8192 x 4,
-// 1024 x 5120: 106 us).  Tried: the tokens as the M side (half of the
-// MMAs of an expert with 128 rows idle); units in a fixed order (the pairs with whole tiles ended 20 % later);
-// weights asked for in L2 ahead of time (56 -> 64 us at 500 tokens); units of 32 experts mixed (132 -> 153 at 8192); two
-// accumulators of 128 columns (nothing at 64 tokens, 132 -> 139 at 8192); two CTAs an SM with tiles of 128 tokens (between the
-// two forms or behind both: 2048 tokens on 16 experts 28.3 with 64, 24.7 with 128, 22.8 with 256; 8192 tokens 153).
+// What bounds it.  Few tokens: the weights from DRAM, at 6.3 of the measured 6.78 TB/s from one size to the other, and some 4
+// us around that a launch takes to start, fill and drain (means of three batches: 64 tokens on 69 of 128 experts, 2048 x
+// 1536, 123 MB of codes and scales in 23.4 us; 500 on 56 of 64, 4096 x 2560, 330 MB in 56.5).  Many: the loads into the SMs.
+// 8192 tokens x 4 on 64 experts, 5120 x 2048, read 1.93 GB from L2, 16.4 TB/s without the MMAs in 118 us, with them in 132 to
+// 136 (5.2 PFLOP/s); one expert of 8192 rows, 5120 x 13824, 6.8 PFLOP/s in 171 us, as nvfp4_linear_swiglu_quantize.  The
+// accumulator takes all TMEM that the scales leave, so a unit's end (last MMAs, drain) costs 2000 cycles of 10240 at K =
+// 5120, and at K = 1024 a unit's loads, MMAs and stores run almost one after another: some 2000 cycles each of 5000, with L2
+// at 46 %, DRAM at 56 and the tensor pipe at 34 (8192 x 4, 1024 x 5120: 106 us).  Tried: the tokens as the M side (half of
+// the MMAs of an expert with 128 rows idle); units in a fixed order (the pairs with whole tiles ended 20 % later); weights
+// asked for in L2 ahead of time (56 -> 64 us at 500 tokens); units of 32 experts mixed (132 -> 153 at 8192); two accumulators
+// of 128 columns (nothing at 64 tokens, 132 -> 139 at 8192); two CTAs an SM with tiles of 128 tokens (between the two forms
+// or behind both: 2048 tokens on 16 experts 28.3 with 64, 24.7 with 128, 22.8 with 256; 8192 tokens 153).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 

@@ -11,8 +11,8 @@
 // An expert whose logit is -inf or NaN is never chosen and has p = 0.
 //
 // Bound by issue slots for most of its time: 459 instructions a token of 256 experts and 8
-// choices, 650 with sigmoid and a bias, of which a scheduler issues one in 0.71 of its cycles;
-// the choices' reductions wait for each other in the rest.  16384 tokens: 9.2 us, 11.8 with
+// choices, 650 with sigmoid and a bias, of which a scheduler issues 0.71 a cycle: the choices'
+// reductions wait for each other.  16384 tokens: 9.2 us, 11.8 with
 // sigmoid and bias (a maximum over all registers for each choice: 23), of which the issue alone
 // is 6.0 and 8.5 at 2.05 GHz and the rest 2.25 waves of CTAs, a start and an end; their bytes
 // 2.5.  Gradient of 8191 x 128 in bf16 3.6 (through a row in shared memory 4.8).  32 tokens:
